@@ -563,6 +563,126 @@ rr_status rr_plan_check(const rr_plan* plan, cudaStream_t stream);
  * usable.  It touches no buffer. */
 rr_status rr_plan_selftest_wait(const rr_plan* plan, cudaStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Products of the rollout's weights.
+ *
+ * What a rollout does with the tensors that rr_unpack has written: a token
+ * step's products with 1 to 16 tokens, whose cost is reading the weights once.
+ * No counterpart in the paper, whose rollouts run an inference engine of their
+ * own (Section 7.1).  rr_quantize follows a sync, so that the step reads a
+ * quarter of the bytes; rr_matvec and rr_moe are the products.
+ *
+ * All of these calls are stream-ordered and asynchronous, allocate nothing, may be
+ * captured into a CUDA graph (rr_moe_check apart, which blocks), and may run from several threads and streams at once
+ * as long as their outputs and workspaces are distinct.  Matrices are in this
+ * GPU's device (or managed) memory, 16-byte aligned; tokens, outputs, ids and weights
+ * have their elements' alignment.  Row strides (ld...) are in elements and at
+ * least the row's length.  Argument errors come back at once (RR_EINVAL; a
+ * shape outside the limits RR_ELAYOUT) and nothing is launched.
+ *
+ * Arithmetic.  Products of 16-bit values are summed in float32; a result is
+ * rounded once to its type.  Infinities and NaN follow the formulas.
+ * ------------------------------------------------------------------------- */
+
+/* A stack of matrices in 4 bits with group scales.  Per row, columns
+ * [i * group, (i + 1) * group) (the last group may be shorter) share a scale:
+ *   a = max |w| over the group;
+ *   s = a / 7 in float32, rounded to the 16-bit type; 0 when s < 2^-126;
+ *       NaN when a is not finite (all products of the row become NaN);
+ *   q = w / s rounded to the nearest integer, ties to even, clamped to -7..7;
+ *       0 when s is 0 or NaN.
+ * An element stands for s * q.
+ *
+ * Storage.  A matrix is cut into strips of 16 rows and blocks of 128 columns,
+ * zero-filled at the edges; a strip's blocks follow one another, then the next
+ * strip's.  Slot r of strip i is row 16 i + r, or with `pair`, where the rows
+ * are [gate; up], slots 0..7 are gate rows 8 i + r and slots 8..15 the up rows of
+ * the same index.  A block is 1024 bytes of codes, then 4096 / group bytes of
+ * scales:
+ *   the 16 bytes at 512 h + 16 (4 g + t), h = 0..1, g = 0..7, t = 0..3, hold
+ *   slot 8 h + g: their 32-bit word j = 0..3 holds columns 32 j + 8 t + 0..7,
+ *   column 32 j + 8 t + i in bits 4 n .. 4 n + 3 with n = i / 2 + 4 (i % 2),
+ *   as q + 8;
+ *   scale i (of 128 / group) of slot 8 h + g is 16-bit word
+ *   2 (g * (128 / group) + i) + h of the scales. */
+typedef struct {
+    int64_t rows, cols;   /* of one matrix; 1 .. 2^31 - 1 rows, 1 .. 2^24 columns        */
+    int32_t count;        /* matrices in the stack (a layer's experts), 1 .. 65535       */
+    int32_t group;        /* columns that share a scale: 32, 64 or 128                   */
+    int32_t dtype;        /* rr_dst_dtype of the elements, scales, tokens and outputs    */
+    int32_t pair;         /* 1: rows are [gate; up] (an even number), as above; else 0   */
+} rr_quant;
+
+/* Bytes of one packed matrix (a multiple of 16; matrix m of the stack starts
+ * at m times that) and of the whole stack.  Either pointer may be NULL. */
+rr_status rr_quant_bytes(const rr_quant* q, int64_t* matrix_bytes, int64_t* total_bytes);
+
+/* 16-bit matrices -> packed.  w: `count` matrices of `rows` rows, ld elements
+ * apart, each matrix rows * ld elements after the one before (2-byte aligned).
+ * packed: rr_quant_bytes' total. */
+rr_status rr_quantize(const rr_quant* q, const void* w, int64_t ld, void* packed,
+                      cudaStream_t stream);
+
+/* packed -> the values it stands for, in the 16-bit type (rounded once) or, with
+ * f32 = 1, in float32 (exact).  w as for rr_quantize, aligned to its elements. */
+rr_status rr_dequantize(const rr_quant* q, const void* packed, void* w, int64_t ld, int32_t f32,
+                        cudaStream_t stream);
+
+/* out[t] = W x[t] for n_tokens (0..16) rows of `cols` 16-bit elements.  q
+ * describes one matrix (count 1).  out: n_tokens rows of `rows` elements, in
+ * the 16-bit type or, with f32 = 1, in float32; with q->pair, rows / 2
+ * elements silu(gate) * up, silu(z) = z / (1 + exp(-z)).  x and out must not
+ * overlap. */
+enum { RR_MATVEC_MAX_TOKENS = 16 };
+rr_status rr_matvec(const rr_quant* q, const void* packed, const void* x, int64_t ldx,
+                    int32_t n_tokens, void* out, int64_t ldo, int32_t f32, cudaStream_t stream);
+
+/* A mixture-of-experts layer.  With l = x R^T over all n_experts (float32) and
+ * p = softmax(l), a token takes the top_k experts of largest l (ties: the
+ * lowest index; NaN counts as the largest), with weights c = p, or, with
+ * norm_topk, p / (sum of the chosen p).  Its output is the sum over the chosen
+ * experts e in first_expert .. first_expert + n_local - 1, in the order of
+ * their rank, of c W2_e (silu(W1_e x) * (W3_e x)); zero if there is none.  A rank of
+ * an expert-parallel or tensor-parallel rollout thus gets its part of the sum.
+ *   router: [n_experts, hidden] 16-bit elements.
+ *   w13, w2: with group 0, 16-bit stacks as rr_unpack writes them:
+ *     w13 [n_local, 2 inter, hidden], each expert [gate; up], and
+ *     w2 [n_local, hidden, inter].  Else packed stacks of n_local matrices with this
+ *     group: w13 of [2 inter, hidden] with pair = 1, w2 of [hidden, inter]. */
+typedef struct {
+    int32_t n_experts;                /* 1 .. 512: rows of the router                    */
+    int32_t first_expert, n_local;    /* the experts held here, within 0 .. n_experts    */
+    int32_t top_k;                    /* 1 .. 16, at most n_experts                      */
+    int64_t hidden, inter;            /* 1 .. 65536 each                                 */
+    int32_t dtype;                    /* rr_dst_dtype                                    */
+    int32_t group;                    /* 0, or 32, 64, 128                               */
+    int32_t norm_topk;                /* 0 or 1                                          */
+    int32_t reserved;                 /* 0                                               */
+} rr_moe_layer;
+
+enum { RR_MOE_MAX_TOKENS = 64 };
+
+/* Bytes of device workspace that a call with up to max_tokens (1..64) tokens
+ * needs.  The caller zero-fills it once; every call leaves it ready for the
+ * next.  Calls that overlap in time need distinct workspaces. */
+rr_status rr_moe_workspace(const rr_moe_layer* layer, int32_t max_tokens, int64_t* bytes);
+
+/* One layer for n_tokens (0..64) rows of `hidden` 16-bit elements.  ids
+ * (n_tokens x top_k int32) and weights (float32, likewise; either may be NULL)
+ * receive the chosen experts, by descending l, and their c: what a trainer
+ * needs to repeat the rollout's routing.  workspace: 16-byte aligned, of
+ * workspace_bytes.  x and out must not overlap. */
+rr_status rr_moe(const rr_moe_layer* layer, const void* router, const void* w13, const void* w2,
+                 const void* x, int64_t ldx, int32_t n_tokens, void* out, int64_t ldo,
+                 int32_t* ids, float* weights, void* workspace, int64_t workspace_bytes,
+                 cudaStream_t stream);
+
+/* Waits for `stream`, then reports (and clears) whether a call on this workspace
+ * gave up a bounded wait: RR_ECUDA if so (that call's outputs are incomplete), else
+ * RR_OK.  No other call on this workspace may be running. */
+rr_status rr_moe_check(const rr_moe_layer* layer, int32_t max_tokens, void* workspace,
+                       cudaStream_t stream);
+
 /* A static description of a status code ("RR_OK", "RR_EINVAL: invalid
  * argument", ...; "unknown rr_status" otherwise), and this thread's
  * description of its most recent failure ("" if none).  The

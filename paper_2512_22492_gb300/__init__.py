@@ -13,6 +13,8 @@ from .rr import (Block, DstLayout, DstTensor, Param, Plan, PlanOptions, Pointers
                  rr_unpack_range, rr_unpack_verify, rr_unpack_verify_async, rr_verify,
                  rr_verify_noalloc,
                  rr_verify_range)
+from .products import (MoeLayer, MoeWorkspace, Quantized, rr_dequantize, rr_matvec, rr_moe,
+                       rr_moe_check, rr_quantize)
 from .layouts import qwen3_layer_units, qwen3_manifest, qwen3_rollout, qwen3_sync
 
 __all__ = ["Block", "DstLayout", "DstTensor", "Param", "Plan", "PlanOptions", "Pointers",
@@ -20,4 +22,6 @@ __all__ = ["Block", "DstLayout", "DstTensor", "Param", "Plan", "PlanOptions", "P
            "SrcLayout", "rr_pack", "rr_plan_create", "rr_status_str", "rr_unpack", "rr_verify",
            "rr_pack_range", "rr_unpack_range", "rr_verify_range", "rr_clear_range",
            "rr_unpack_verify", "rr_unpack_verify_async", "rr_plan_check", "rr_plan_selftest_wait", "rr_verify_noalloc",
+           "Quantized", "MoeLayer", "MoeWorkspace", "rr_quantize", "rr_dequantize", "rr_matvec",
+           "rr_moe", "rr_moe_check",
            "qwen3_layer_units", "qwen3_manifest", "qwen3_rollout", "qwen3_sync"]

@@ -31,7 +31,8 @@ def _cuda_home() -> str:
 
 
 def _sources():
-    return [os.path.join(CSRC, f) for f in ("rr_plan.cpp", "rr_device.cu", "rr_internal.h")] + \
+    return [os.path.join(CSRC, f) for f in ("rr_plan.cpp", "rr_device.cu", "rr_products.cu",
+                                             "rr_internal.h")] + \
         [os.path.join(INCLUDE, "rr.h")]
 
 
@@ -53,13 +54,15 @@ def build(force: bool = False, verbose: bool = False) -> str:
     inc = ["-I", INCLUDE, "-I", CSRC, "-I", os.path.join(cuda, "include")]
     plan_o = os.path.join(BUILD, "rr_plan.o")
     dev_o = os.path.join(BUILD, "rr_device.o")
+    prod_o = os.path.join(BUILD, "rr_products.o")
+    device = [nvcc, "-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xptxas", "-v"] + \
+        ARCH + os.environ.get("RR_EXTRA_NVCC_FLAGS", "").split()
     jobs = [
         ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall"] +
         os.environ.get("RR_EXTRA_CXX_FLAGS", "").split() +
         ["-c", os.path.join(CSRC, "rr_plan.cpp"), "-o", plan_o] + inc,
-        [nvcc, "-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xptxas", "-v"] + ARCH +
-        os.environ.get("RR_EXTRA_NVCC_FLAGS", "").split() +
-        ["-c", os.path.join(CSRC, "rr_device.cu"), "-o", dev_o] + inc,
+        device + ["-c", os.path.join(CSRC, "rr_device.cu"), "-o", dev_o] + inc,
+        device + ["-c", os.path.join(CSRC, "rr_products.cu"), "-o", prod_o] + inc,
     ]
     procs = [subprocess.Popen(j, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
              for j in jobs]
@@ -70,11 +73,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if p.returncode != 0:
             raise RuntimeError(f"build failed: {' '.join(j)}\n{out}")
     with open(os.path.join(BUILD, "ptxas.log"), "w") as f:
-        f.write(logs[1])
+        f.write(logs[1] + logs[2])
     if verbose:
-        print(logs[1])
+        print(logs[1] + logs[2])
     tmp = LIB + ".tmp"
-    subprocess.check_call([nvcc, "-shared"] + ARCH + [plan_o, dev_o, "-o", tmp])
+    subprocess.check_call([nvcc, "-shared"] + ARCH + [plan_o, dev_o, prod_o, "-o", tmp])
     os.replace(tmp, LIB)
     return LIB
 

@@ -1,0 +1,634 @@
+// Products of the rollout's weights for GB300 (sm_103a): quantisation to 4-bit
+// strips with group scales, matrix-vector products with them, and a
+// mixture-of-experts layer for a few tokens (include/rr.h has the definitions).
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <climits>
+
+#include "rr_internal.h"
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// 16-bit element types
+// ---------------------------------------------------------------------------
+
+struct BF16 {
+    static __device__ __forceinline__ float widen(uint16_t b) { return __uint_as_float(uint32_t(b) << 16); }
+    static __device__ __forceinline__ uint16_t round(float f) { return __bfloat16_as_ushort(__float2bfloat16_rn(f)); }
+    static constexpr uint16_t kNaN = 0x7FC0;
+};
+struct F16 {
+    static __device__ __forceinline__ float widen(uint16_t b) { return __half2float(__ushort_as_half(b)); }
+    static __device__ __forceinline__ uint16_t round(float f) { return __half_as_ushort(__float2half_rn(f)); }
+    static constexpr uint16_t kNaN = 0x7E00;
+};
+
+template <class T, bool F32>
+__device__ __forceinline__ void put(void* out, int64_t i, float f) {
+    if (F32) static_cast<float*>(out)[i] = f;
+    else static_cast<uint16_t*>(out)[i] = T::round(f);
+}
+
+// silu(z) = z / (1 + exp(-z)) as the formula reads.
+__device__ __forceinline__ float silu(float z) { return z / (1.0f + expf(-z)); }
+
+// ---------------------------------------------------------------------------
+// Packed matrices
+// ---------------------------------------------------------------------------
+
+constexpr int kStrip = 16;     // rows of a strip
+constexpr int kBlock = 128;    // columns of a block
+constexpr int kCodes = kStrip * kBlock / 2;   // bytes of a block's codes
+constexpr float kLeastScale = 1.17549435e-38f;   // 2^-126
+
+__host__ __device__ constexpr int block_bytes(int group) { return kCodes + 4096 / group; }
+
+// The shape that the kernels take.
+struct Packed {
+    int64_t rows, cols;
+    int64_t strips, blocks;    // of one matrix
+    int64_t matrix_bytes;
+    int32_t pair;
+    // The row in slot r of strip s, or -1 past the edge.
+    __device__ __forceinline__ int64_t row(int64_t s, int r) const {
+        if (!pair) {
+            const int64_t i = s * kStrip + r;
+            return i < rows ? i : -1;
+        }
+        const int64_t i = s * (kStrip / 2) + (r & 7);
+        return i < rows / 2 ? (r < 8 ? i : rows / 2 + i) : -1;
+    }
+};
+
+__device__ __forceinline__ int code(uint32_t word, int i) {
+    return int((word >> (4 * (i / 2 + 4 * (i % 2)))) & 15u) - 8;
+}
+
+// One warp takes one block: lane 4 g + t holds slots g and g + 8, of each the
+// columns 32 j + 8 t + 0..7, so that a lane's 16 bytes of codes and a group's
+// maximum need no memory between lanes.  Bound by HBM: 2 bytes read and about
+// half a byte written per element.
+template <class T, int G>
+__global__ void __launch_bounds__(256) rr_quantize_kernel(Packed m, const uint16_t* w, int64_t ld,
+                                                          char* packed, int64_t total) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int64_t item = int64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    if (item >= total) return;
+    const int64_t b = item % m.blocks, strip = item / m.blocks % m.strips;
+    const int64_t mat = item / m.blocks / m.strips;
+    char* const to = packed + mat * m.matrix_bytes + (strip * m.blocks + b) * block_bytes(G);
+    for (int half = 0; half < 2; ++half) {
+        const int64_t row = m.row(strip, 8 * half + g);
+        float v[4][8];
+        const uint16_t* const src = w + (mat * m.rows + row) * ld;
+        for (int j = 0; j < 4; ++j) {
+            const int64_t c = b * kBlock + 32 * j + 8 * t;
+            for (int i = 0; i < 8; ++i)
+                v[j][i] = row >= 0 && c + i < m.cols ? T::widen(src[c + i]) : 0.0f;
+        }
+        uint32_t words[4];
+        for (int k = 0; k < kBlock / G; ++k) {
+            constexpr int kWords = G / 32;
+            float top = 0.0f;
+            bool fine = true;
+            for (int j = k * kWords; j < (k + 1) * kWords; ++j)
+                for (int i = 0; i < 8; ++i) {
+                    top = fmaxf(top, fabsf(v[j][i]));
+                    fine = fine && isfinite(v[j][i]);
+                }
+            for (int o = 1; o < 4; o *= 2) {
+                top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+                fine = __shfl_xor_sync(~0u, int(fine), o) && fine;
+            }
+            uint16_t s16 = T::round(top / 7.0f);
+            float s = T::widen(s16);
+            if (s < kLeastScale) s16 = 0, s = 0.0f;
+            if (!fine) s16 = T::kNaN, s = 0.0f;
+            if (t == 0)
+                reinterpret_cast<uint16_t*>(to + kCodes)[2 * (g * (kBlock / G) + k) + half] = s16;
+            for (int j = k * kWords; j < (k + 1) * kWords; ++j) {
+                uint32_t word = 0;
+                for (int i = 0; i < 8; ++i) {
+                    const float q = s > 0.0f ? fminf(fmaxf(rintf(v[j][i] / s), -7.0f), 7.0f) : 0.0f;
+                    word |= uint32_t(int(q) + 8) << (4 * (i / 2 + 4 * (i % 2)));
+                }
+                words[j] = word;
+            }
+        }
+        *reinterpret_cast<uint4*>(to + 512 * half + 16 * lane) =
+            make_uint4(words[0], words[1], words[2], words[3]);
+    }
+}
+
+// The inverse, by the same lanes.
+template <class T, int G, bool F32>
+__global__ void __launch_bounds__(256) rr_dequantize_kernel(Packed m, const char* packed, void* w,
+                                                            int64_t ld, int64_t total) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int64_t item = int64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    if (item >= total) return;
+    const int64_t b = item % m.blocks, strip = item / m.blocks % m.strips;
+    const int64_t mat = item / m.blocks / m.strips;
+    const char* const from = packed + mat * m.matrix_bytes + (strip * m.blocks + b) * block_bytes(G);
+    for (int half = 0; half < 2; ++half) {
+        const int64_t row = m.row(strip, 8 * half + g);
+        if (row < 0) continue;
+        const uint4 q = *reinterpret_cast<const uint4*>(from + 512 * half + 16 * lane);
+        const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+        for (int j = 0; j < 4; ++j) {
+            const float s = T::widen(reinterpret_cast<const uint16_t*>(
+                from + kCodes)[2 * (g * (kBlock / G) + 32 * j / G) + half]);
+            const int64_t c = b * kBlock + 32 * j + 8 * t;
+            for (int i = 0; i < 8; ++i)
+                if (c + i < m.cols)
+                    put<T, F32>(w, (mat * m.rows + row) * ld + c + i, s * float(code(words[j], i)));
+        }
+    }
+}
+
+// One warp takes one strip and every token.
+template <class T, int G, bool F32>
+__global__ void __launch_bounds__(128) rr_matvec_kernel(Packed m, const char* packed,
+                                                        const uint16_t* x, int64_t ldx, int tokens,
+                                                        void* out, int64_t ldo) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int64_t strip = int64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    if (strip >= m.strips) return;
+    for (int n = 0; n < tokens; ++n) {
+        float sum[2] = {0.0f, 0.0f};
+        for (int64_t b = 0; b < m.blocks; ++b) {
+            const char* const from = packed + (strip * m.blocks + b) * block_bytes(G);
+            for (int half = 0; half < 2; ++half) {
+                const uint4 q = *reinterpret_cast<const uint4*>(from + 512 * half + 16 * lane);
+                const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+                for (int j = 0; j < 4; ++j) {
+                    const float s = T::widen(reinterpret_cast<const uint16_t*>(
+                        from + kCodes)[2 * (g * (kBlock / G) + 32 * j / G) + half]);
+                    const int64_t c = b * kBlock + 32 * j + 8 * t;
+                    float part = 0.0f;
+                    for (int i = 0; i < 8; ++i)
+                        if (c + i < m.cols)
+                            part += float(code(words[j], i)) * T::widen(x[n * ldx + c + i]);
+                    sum[half] += s * part;
+                }
+            }
+        }
+        for (int h = 0; h < 2; ++h)
+            for (int o = 1; o < 4; o *= 2) sum[h] += __shfl_xor_sync(~0u, sum[h], o);
+        if (t != 0) continue;
+        const int64_t lo = m.row(strip, g), hi = m.row(strip, 8 + g);
+        if (m.pair) {
+            if (lo >= 0) put<T, F32>(out, n * ldo + lo, silu(sum[0]) * sum[1]);
+        } else {
+            if (lo >= 0) put<T, F32>(out, n * ldo + lo, sum[0]);
+            if (hi >= 0) put<T, F32>(out, n * ldo + hi, sum[1]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Mixture of experts
+// ---------------------------------------------------------------------------
+
+constexpr int kMaxExperts = 512, kMaxTopK = 16, kMaxInner = 65536;
+
+struct MoeArgs {
+    const uint16_t* router;
+    const char *w13, *w2;
+    const uint16_t* x;
+    int64_t ldx, ldo;
+    uint16_t* out;
+    int32_t* ids;
+    float* weights;
+    // Workspace.
+    float* logits;     // [tokens, n_experts]
+    int32_t* chosen;   // [tokens, top_k]
+    float* c;          // [tokens, top_k]
+    float* h;          // [tokens * top_k, inter]
+    int32_t tokens, n_experts, first, n_local, top_k, norm, hidden, inter;
+    Packed m13, m2;
+};
+
+// A matrix element, whatever the form it is stored in.
+template <class T, int G>
+__device__ float element(const char* base, const Packed& m, int64_t mat, int64_t row, int64_t col) {
+    if (G == 0)
+        return T::widen(reinterpret_cast<const uint16_t*>(base)[(mat * m.rows + row) * m.cols + col]);
+    const int64_t i = m.pair && row >= m.rows / 2 ? row - m.rows / 2 : row;
+    const int64_t strip = m.pair ? i / 8 : i / 16;
+    const int half = m.pair ? row >= m.rows / 2 : (i / 8) & 1, g = i & 7;
+    const int c = col % kBlock, j = c / 32, t = c % 32 / 8;
+    constexpr int kGroup = G ? G : 128;
+    const char* const from =
+        base + mat * m.matrix_bytes + (strip * m.blocks + col / kBlock) * block_bytes(kGroup);
+    const uint32_t word =
+        reinterpret_cast<const uint32_t*>(from + 512 * half + 16 * (4 * g + t))[j];
+    const uint16_t s =
+        reinterpret_cast<const uint16_t*>(from + kCodes)[2 * (g * (kBlock / kGroup) + c / kGroup) + half];
+    return T::widen(s) * float(code(word, c % 8));
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+    for (int o = 16; o; o /= 2) v += __shfl_xor_sync(~0u, v, o);
+    return v;
+}
+
+template <class T>
+__global__ void __launch_bounds__(128) rr_moe_logits_kernel(const MoeArgs a) {
+    const int lane = threadIdx.x & 31;
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (i >= a.tokens * a.n_experts) return;
+    const int t = i / a.n_experts, e = i % a.n_experts;
+    float sum = 0.0f;
+    for (int k = lane; k < a.hidden; k += 32)
+        sum = fmaf(T::widen(a.x[t * a.ldx + k]), T::widen(a.router[int64_t(e) * a.hidden + k]), sum);
+    sum = warp_sum(sum);
+    if (lane == 0) a.logits[i] = sum;
+}
+
+// Descending order of logits as unsigned integers: NaN first, +0 and -0 alike.
+__device__ __forceinline__ uint32_t rank_key(float l) {
+    if (isnan(l)) return ~0u;
+    const uint32_t b = __float_as_uint(l + 0.0f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+__global__ void __launch_bounds__(32) rr_moe_choose_kernel(const MoeArgs a) {
+    __shared__ uint32_t key[kMaxExperts];
+    const int t = blockIdx.x, lane = threadIdx.x;
+    const float* const l = a.logits + t * a.n_experts;
+    float top = -INFINITY;
+    for (int e = lane; e < a.n_experts; e += 32) {
+        key[e] = rank_key(l[e]);
+        top = fmaxf(top, l[e]);
+    }
+    for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    float sum = 0.0f;
+    for (int e = lane; e < a.n_experts; e += 32) sum += expf(l[e] - top);
+    sum = warp_sum(sum);
+    __syncwarp();
+    float mine = 0.0f, total = 0.0f;
+    int my_id = 0;
+    for (int j = 0; j < a.top_k; ++j) {
+        unsigned long long best = 0;   // (key, lowest index first)
+        for (int e = lane; e < a.n_experts; e += 32)
+            if (key[e])
+                best = max(best, (unsigned long long)key[e] << 32 | uint32_t(~e));
+        for (int o = 16; o; o /= 2) best = max(best, __shfl_xor_sync(~0u, best, o));
+        const int e = int(~uint32_t(best));
+        const float p = expf(l[e] - top) / sum;
+        total += p;
+        if (lane == j) mine = p, my_id = e;
+        __syncwarp();
+        if (lane == e % 32) key[e] = 0;
+        __syncwarp();
+    }
+    if (lane < a.top_k) {
+        if (a.norm) mine /= total;
+        a.chosen[t * a.top_k + lane] = my_id;
+        a.c[t * a.top_k + lane] = mine;
+        if (a.ids) a.ids[t * a.top_k + lane] = my_id;
+        if (a.weights) a.weights[t * a.top_k + lane] = mine;
+    }
+}
+
+template <class T, int G>
+__global__ void __launch_bounds__(128) rr_moe_up_kernel(const MoeArgs a) {
+    const int lane = threadIdx.x & 31;
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 5), p = blockIdx.y;
+    const int e = a.chosen[p] - a.first;
+    if (i >= a.inter || e < 0 || e >= a.n_local) return;
+    const uint16_t* const x = a.x + p / a.top_k * a.ldx;
+    float gate = 0.0f, up = 0.0f;
+    for (int k = lane; k < a.hidden; k += 32) {
+        const float v = T::widen(x[k]);
+        gate = fmaf(v, element<T, G>(a.w13, a.m13, e, i, k), gate);
+        up = fmaf(v, element<T, G>(a.w13, a.m13, e, a.inter + i, k), up);
+    }
+    gate = warp_sum(gate);
+    up = warp_sum(up);
+    if (lane == 0) a.h[int64_t(p) * a.inter + i] = silu(gate) * up;
+}
+
+template <class T, int G>
+__global__ void __launch_bounds__(128) rr_moe_down_kernel(const MoeArgs a) {
+    const int lane = threadIdx.x & 31;
+    const int n = blockIdx.x * 4 + (threadIdx.x >> 5), t = blockIdx.y;
+    if (n >= a.hidden) return;
+    float y = 0.0f;
+    for (int j = 0; j < a.top_k; ++j) {
+        const int p = t * a.top_k + j, e = a.chosen[p] - a.first;
+        if (e < 0 || e >= a.n_local) continue;
+        float sum = 0.0f;
+        for (int k = lane; k < a.inter; k += 32)
+            sum = fmaf(a.h[int64_t(p) * a.inter + k], element<T, G>(a.w2, a.m2, e, n, k), sum);
+        y += a.c[p] * warp_sum(sum);
+    }
+    if (lane == 0) a.out[t * a.ldo + n] = T::round(y);
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+
+rr_status cuda_fail(cudaError_t e, const char* what) {
+    return rr_fail(RR_ECUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+#define RR_CUDA(call)                                   \
+    do {                                                \
+        cudaError_t e_ = (call);                        \
+        if (e_ != cudaSuccess) return cuda_fail(e_, #call); \
+    } while (0)
+
+#define RR_TRY(call)                     \
+    do {                                 \
+        rr_status s_ = (call);           \
+        if (s_ != RR_OK) return s_;      \
+    } while (0)
+
+// Memory of the current device, `align`ed.
+rr_status check_device(const void* p, size_t align, const char* what) {
+    if (!p || (uintptr_t)p % align) return rr_fail(RR_EINVAL, "%s is NULL or not %zu-byte aligned", what, align);
+    cudaPointerAttributes at;
+    int dev = -1;
+    RR_CUDA(cudaGetDevice(&dev));
+    if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
+        cudaGetLastError();
+        return rr_fail(RR_EINVAL, "%s is not memory of this GPU", what);
+    }
+    if (at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeDevice && at.device == dev)) return RR_OK;
+    return rr_fail(RR_EINVAL, "%s is not memory of this GPU", what);
+}
+
+rr_status check_quant(const rr_quant* q) {
+    if (!q) return rr_fail(RR_EINVAL, "matrix description is NULL");
+    if (q->rows < 1 || q->rows > INT32_MAX || q->cols < 1 || q->cols > (1 << 24))
+        return rr_fail(RR_ELAYOUT, "matrix of %lld x %lld: 1..2^31-1 rows and 1..2^24 columns",
+                       (long long)q->rows, (long long)q->cols);
+    if (q->count < 1 || q->count > 65535) return rr_fail(RR_ELAYOUT, "count %d: 1..65535", q->count);
+    if (q->group != 32 && q->group != 64 && q->group != 128)
+        return rr_fail(RR_ELAYOUT, "group %d: 32, 64 or 128", q->group);
+    if (q->dtype != RR_DST_BF16 && q->dtype != RR_DST_F16)
+        return rr_fail(RR_EINVAL, "unknown element type %d", q->dtype);
+    if (q->pair != 0 && q->pair != 1) return rr_fail(RR_EINVAL, "pair is 0 or 1, not %d", q->pair);
+    if (q->pair && q->rows % 2) return rr_fail(RR_ELAYOUT, "paired rows are an even number, not %lld", (long long)q->rows);
+    return RR_OK;
+}
+
+Packed packed_of(int64_t rows, int64_t cols, int group, int pair) {
+    Packed m;
+    m.rows = rows;
+    m.cols = cols;
+    m.strips = pair ? (rows / 2 + 7) / 8 : (rows + 15) / 16;
+    m.blocks = (cols + kBlock - 1) / kBlock;
+    m.matrix_bytes = m.strips * m.blocks * block_bytes(group ? group : 128);
+    m.pair = pair;
+    return m;
+}
+
+// Calls f with the element type and the group as template arguments.
+template <class F>
+rr_status with_group(int dtype, int group, F f) {
+    using std::integral_constant;
+    if (dtype == RR_DST_F16) {
+        if (group == 32) return f(F16{}, integral_constant<int, 32>{});
+        if (group == 64) return f(F16{}, integral_constant<int, 64>{});
+        if (group == 128) return f(F16{}, integral_constant<int, 128>{});
+        return f(F16{}, integral_constant<int, 0>{});
+    }
+    if (group == 32) return f(BF16{}, integral_constant<int, 32>{});
+    if (group == 64) return f(BF16{}, integral_constant<int, 64>{});
+    if (group == 128) return f(BF16{}, integral_constant<int, 128>{});
+    return f(BF16{}, integral_constant<int, 0>{});
+}
+
+rr_status check_moe(const rr_moe_layer* L) {
+    if (!L) return rr_fail(RR_EINVAL, "layer description is NULL");
+    if (L->n_experts < 1 || L->n_experts > kMaxExperts)
+        return rr_fail(RR_ELAYOUT, "%d experts: 1..%d", L->n_experts, kMaxExperts);
+    if (L->first_expert < 0 || L->n_local < 1 || L->n_local > L->n_experts || L->first_expert > L->n_experts - L->n_local)
+        return rr_fail(RR_ELAYOUT, "experts %d + %d are not within 0..%d", L->first_expert, L->n_local, L->n_experts);
+    if (L->top_k < 1 || L->top_k > kMaxTopK || L->top_k > L->n_experts)
+        return rr_fail(RR_ELAYOUT, "top_k %d: 1..%d, at most the experts", L->top_k, kMaxTopK);
+    if (L->hidden < 1 || L->hidden > kMaxInner || L->inter < 1 || L->inter > kMaxInner)
+        return rr_fail(RR_ELAYOUT, "hidden %lld, inter %lld: 1..%d", (long long)L->hidden, (long long)L->inter, kMaxInner);
+    if (L->dtype != RR_DST_BF16 && L->dtype != RR_DST_F16) return rr_fail(RR_EINVAL, "unknown element type %d", L->dtype);
+    if (L->group != 0 && L->group != 32 && L->group != 64 && L->group != 128)
+        return rr_fail(RR_ELAYOUT, "group %d: 0, 32, 64 or 128", L->group);
+    if (L->norm_topk != 0 && L->norm_topk != 1) return rr_fail(RR_EINVAL, "norm_topk is 0 or 1, not %d", L->norm_topk);
+    if (L->reserved != 0) return rr_fail(RR_EINVAL, "reserved is 0, not %d", L->reserved);
+    return RR_OK;
+}
+
+// Workspace: a control block, then the arrays.  Offsets in bytes.
+struct MoeSpace {
+    int64_t logits, chosen, c, h, total;
+};
+constexpr int64_t kControlBytes = 256;   // word 0: the error word
+
+int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
+
+MoeSpace moe_space(const rr_moe_layer* L, int64_t tokens) {
+    MoeSpace s;
+    s.logits = kControlBytes;
+    s.chosen = s.logits + up16(4 * tokens * L->n_experts);
+    s.c = s.chosen + up16(4 * tokens * L->top_k);
+    s.h = s.c + up16(4 * tokens * L->top_k);
+    s.total = s.h + up16(4 * tokens * L->top_k * L->inter);
+    return s;
+}
+
+}  // namespace
+
+extern "C" rr_status rr_quant_bytes(const rr_quant* q, int64_t* matrix_bytes, int64_t* total_bytes) {
+    rr_clear_error();
+    RR_TRY(check_quant(q));
+    const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
+    if (matrix_bytes) *matrix_bytes = m.matrix_bytes;
+    if (total_bytes) *total_bytes = m.matrix_bytes * q->count;
+    return RR_OK;
+}
+
+namespace {
+
+// Blocks of warps for `items`, or an error where the grid cannot hold them.
+rr_status grid_of(int64_t items, int per_block, unsigned* grid) {
+    const int64_t n = (items + per_block - 1) / per_block;
+    if (n > INT32_MAX) return rr_fail(RR_ELAYOUT, "the stack is too large for one call");
+    *grid = unsigned(n);
+    return RR_OK;
+}
+
+}  // namespace
+
+extern "C" rr_status rr_quantize(const rr_quant* q, const void* w, int64_t ld, void* packed,
+                                 cudaStream_t stream) {
+    RR_TRACE("rr_quantize");
+    rr_clear_error();
+    RR_TRY(check_quant(q));
+    if (ld < q->cols) return rr_fail(RR_EINVAL, "row stride %lld of rows of %lld", (long long)ld, (long long)q->cols);
+    RR_TRY(check_device(w, 2, "w"));
+    RR_TRY(check_device(packed, 16, "packed"));
+    const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
+    const int64_t total = m.strips * m.blocks * q->count;
+    unsigned grid;
+    RR_TRY(grid_of(total, 8, &grid));
+    return with_group(q->dtype, q->group, [&](auto t, auto g) -> rr_status {
+        constexpr int G = decltype(g)::value ? decltype(g)::value : 128;
+        rr_quantize_kernel<decltype(t), G><<<grid, 256, 0, stream>>>(
+            m, static_cast<const uint16_t*>(w), ld, static_cast<char*>(packed), total);
+        RR_CUDA(cudaGetLastError());
+        return RR_OK;
+    });
+}
+
+extern "C" rr_status rr_dequantize(const rr_quant* q, const void* packed, void* w, int64_t ld,
+                                   int32_t f32, cudaStream_t stream) {
+    RR_TRACE("rr_dequantize");
+    rr_clear_error();
+    RR_TRY(check_quant(q));
+    if (f32 != 0 && f32 != 1) return rr_fail(RR_EINVAL, "f32 is 0 or 1, not %d", f32);
+    if (ld < q->cols) return rr_fail(RR_EINVAL, "row stride %lld of rows of %lld", (long long)ld, (long long)q->cols);
+    RR_TRY(check_device(packed, 16, "packed"));
+    RR_TRY(check_device(w, f32 ? 4 : 2, "w"));
+    const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
+    const int64_t total = m.strips * m.blocks * q->count;
+    unsigned grid;
+    RR_TRY(grid_of(total, 8, &grid));
+    return with_group(q->dtype, q->group, [&](auto t, auto g) -> rr_status {
+        constexpr int G = decltype(g)::value ? decltype(g)::value : 128;
+        if (f32)
+            rr_dequantize_kernel<decltype(t), G, true><<<grid, 256, 0, stream>>>(
+                m, static_cast<const char*>(packed), w, ld, total);
+        else
+            rr_dequantize_kernel<decltype(t), G, false><<<grid, 256, 0, stream>>>(
+                m, static_cast<const char*>(packed), w, ld, total);
+        RR_CUDA(cudaGetLastError());
+        return RR_OK;
+    });
+}
+
+extern "C" rr_status rr_matvec(const rr_quant* q, const void* packed, const void* x, int64_t ldx,
+                               int32_t n_tokens, void* out, int64_t ldo, int32_t f32,
+                               cudaStream_t stream) {
+    RR_TRACE("rr_matvec");
+    rr_clear_error();
+    RR_TRY(check_quant(q));
+    if (q->count != 1) return rr_fail(RR_EINVAL, "rr_matvec takes one matrix, not a stack of %d", q->count);
+    if (n_tokens < 0 || n_tokens > RR_MATVEC_MAX_TOKENS)
+        return rr_fail(RR_EINVAL, "%d tokens: 0..%d", n_tokens, RR_MATVEC_MAX_TOKENS);
+    if (f32 != 0 && f32 != 1) return rr_fail(RR_EINVAL, "f32 is 0 or 1, not %d", f32);
+    const int64_t n_out = q->pair ? q->rows / 2 : q->rows;
+    if (ldx < q->cols || ldo < n_out)
+        return rr_fail(RR_EINVAL, "row strides %lld and %lld of rows of %lld and %lld", (long long)ldx,
+                       (long long)ldo, (long long)q->cols, (long long)n_out);
+    if (n_tokens == 0) return RR_OK;
+    RR_TRY(check_device(packed, 16, "packed"));
+    RR_TRY(check_device(x, 2, "x"));
+    RR_TRY(check_device(out, f32 ? 4 : 2, "out"));
+    const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
+    unsigned grid;
+    RR_TRY(grid_of(m.strips, 4, &grid));
+    return with_group(q->dtype, q->group, [&](auto t, auto g) -> rr_status {
+        constexpr int G = decltype(g)::value ? decltype(g)::value : 128;
+        const char* const p = static_cast<const char*>(packed);
+        const uint16_t* const v = static_cast<const uint16_t*>(x);
+        if (f32)
+            rr_matvec_kernel<decltype(t), G, true><<<grid, 128, 0, stream>>>(m, p, v, ldx, n_tokens, out, ldo);
+        else
+            rr_matvec_kernel<decltype(t), G, false><<<grid, 128, 0, stream>>>(m, p, v, ldx, n_tokens, out, ldo);
+        RR_CUDA(cudaGetLastError());
+        return RR_OK;
+    });
+}
+
+extern "C" rr_status rr_moe_workspace(const rr_moe_layer* L, int32_t max_tokens, int64_t* bytes) {
+    rr_clear_error();
+    RR_TRY(check_moe(L));
+    if (max_tokens < 1 || max_tokens > RR_MOE_MAX_TOKENS)
+        return rr_fail(RR_EINVAL, "%d tokens: 1..%d", max_tokens, RR_MOE_MAX_TOKENS);
+    if (!bytes) return rr_fail(RR_EINVAL, "bytes is NULL");
+    *bytes = moe_space(L, max_tokens).total;
+    return RR_OK;
+}
+
+extern "C" rr_status rr_moe(const rr_moe_layer* L, const void* router, const void* w13, const void* w2,
+                            const void* x, int64_t ldx, int32_t n_tokens, void* out, int64_t ldo,
+                            int32_t* ids, float* weights, void* workspace, int64_t workspace_bytes,
+                            cudaStream_t stream) {
+    RR_TRACE("rr_moe");
+    rr_clear_error();
+    RR_TRY(check_moe(L));
+    if (n_tokens < 0 || n_tokens > RR_MOE_MAX_TOKENS)
+        return rr_fail(RR_EINVAL, "%d tokens: 0..%d", n_tokens, RR_MOE_MAX_TOKENS);
+    if (ldx < L->hidden || ldo < L->hidden)
+        return rr_fail(RR_EINVAL, "row strides %lld and %lld of rows of %lld", (long long)ldx, (long long)ldo, (long long)L->hidden);
+    if (n_tokens == 0) return RR_OK;
+    const MoeSpace S = moe_space(L, n_tokens);
+    if (workspace_bytes < S.total)
+        return rr_fail(RR_EINVAL, "workspace of %lld bytes, the call needs %lld", (long long)workspace_bytes, (long long)S.total);
+    RR_TRY(check_device(router, 16, "router"));
+    RR_TRY(check_device(w13, 16, "w13"));
+    RR_TRY(check_device(w2, 16, "w2"));
+    RR_TRY(check_device(x, 2, "x"));
+    RR_TRY(check_device(out, 2, "out"));
+    if (ids) RR_TRY(check_device(ids, 4, "ids"));
+    if (weights) RR_TRY(check_device(weights, 4, "weights"));
+    RR_TRY(check_device(workspace, 16, "workspace"));
+    char* const ws = static_cast<char*>(workspace);
+    MoeArgs a;
+    a.router = static_cast<const uint16_t*>(router);
+    a.w13 = static_cast<const char*>(w13);
+    a.w2 = static_cast<const char*>(w2);
+    a.x = static_cast<const uint16_t*>(x);
+    a.ldx = ldx;
+    a.ldo = ldo;
+    a.out = static_cast<uint16_t*>(out);
+    a.ids = ids;
+    a.weights = weights;
+    a.logits = reinterpret_cast<float*>(ws + S.logits);
+    a.chosen = reinterpret_cast<int32_t*>(ws + S.chosen);
+    a.c = reinterpret_cast<float*>(ws + S.c);
+    a.h = reinterpret_cast<float*>(ws + S.h);
+    a.tokens = n_tokens;
+    a.n_experts = L->n_experts;
+    a.first = L->first_expert;
+    a.n_local = L->n_local;
+    a.top_k = L->top_k;
+    a.norm = L->norm_topk;
+    a.hidden = int32_t(L->hidden);
+    a.inter = int32_t(L->inter);
+    a.m13 = packed_of(2 * L->inter, L->hidden, L->group, 1);
+    a.m2 = packed_of(L->hidden, L->inter, L->group, 0);
+    return with_group(L->dtype, L->group, [&](auto t, auto g) -> rr_status {
+        using T = decltype(t);
+        constexpr int G = decltype(g)::value;
+        rr_moe_logits_kernel<T><<<(n_tokens * a.n_experts + 3) / 4, 128, 0, stream>>>(a);
+        rr_moe_choose_kernel<<<n_tokens, 32, 0, stream>>>(a);
+        rr_moe_up_kernel<T, G><<<dim3((a.inter + 3) / 4, n_tokens * a.top_k), 128, 0, stream>>>(a);
+        rr_moe_down_kernel<T, G><<<dim3((a.hidden + 3) / 4, n_tokens), 128, 0, stream>>>(a);
+        RR_CUDA(cudaGetLastError());
+        return RR_OK;
+    });
+}
+
+extern "C" rr_status rr_moe_check(const rr_moe_layer* L, int32_t max_tokens, void* workspace,
+                                  cudaStream_t stream) {
+    rr_clear_error();
+    RR_TRY(check_moe(L));
+    if (max_tokens < 1 || max_tokens > RR_MOE_MAX_TOKENS)
+        return rr_fail(RR_EINVAL, "%d tokens: 1..%d", max_tokens, RR_MOE_MAX_TOKENS);
+    RR_TRY(check_device(workspace, 16, "workspace"));
+    uint32_t err = 0;
+    RR_CUDA(cudaMemcpyAsync(&err, workspace, 4, cudaMemcpyDeviceToHost, stream));
+    RR_CUDA(cudaStreamSynchronize(stream));
+    if (!err) return RR_OK;
+    RR_CUDA(cudaMemsetAsync(workspace, 0, kControlBytes, stream));
+    RR_CUDA(cudaStreamSynchronize(stream));
+    return rr_fail(RR_ECUDA, "a wait between the layer's blocks ran out");
+}
