@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "rr_internal.h"
 
@@ -43,6 +44,7 @@ __device__ __forceinline__ float silu(float z) { return z / (1.0f + expf(-z)); }
 constexpr int kStrip = 16;     // rows of a strip
 constexpr int kBlock = 128;    // columns of a block
 constexpr int kCodes = kStrip * kBlock / 2;   // bytes of a block's codes
+constexpr int kMaxCols = 1 << 18;
 constexpr float kLeastScale = 1.17549435e-38f;   // 2^-126
 
 __host__ __device__ constexpr int block_bytes(int group) { return kCodes + 4096 / group; }
@@ -150,44 +152,276 @@ __global__ void __launch_bounds__(256) rr_dequantize_kernel(Packed m, const char
     }
 }
 
-// One warp takes one strip and every token.
-template <class T, int G, bool F32>
-__global__ void __launch_bounds__(128) rr_matvec_kernel(Packed m, const char* packed,
-                                                        const uint16_t* x, int64_t ldx, int tokens,
-                                                        void* out, int64_t ldo) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int64_t strip = int64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    if (strip >= m.strips) return;
-    for (int n = 0; n < tokens; ++n) {
-        float sum[2] = {0.0f, 0.0f};
-        for (int64_t b = 0; b < m.blocks; ++b) {
-            const char* const from = packed + (strip * m.blocks + b) * block_bytes(G);
-            for (int half = 0; half < 2; ++half) {
-                const uint4 q = *reinterpret_cast<const uint4*>(from + 512 * half + 16 * lane);
-                const uint32_t words[4] = {q.x, q.y, q.z, q.w};
-                for (int j = 0; j < 4; ++j) {
-                    const float s = T::widen(reinterpret_cast<const uint16_t*>(
-                        from + kCodes)[2 * (g * (kBlock / G) + 32 * j / G) + half]);
-                    const int64_t c = b * kBlock + 32 * j + 8 * t;
-                    float part = 0.0f;
-                    for (int i = 0; i < 8; ++i)
-                        if (c + i < m.cols)
-                            part += float(code(words[j], i)) * T::widen(x[n * ldx + c + i]);
-                    sum[half] += s * part;
-                }
+// ---------------------------------------------------------------------------
+// Inner products on matrix instructions
+// ---------------------------------------------------------------------------
+
+// Weights are the 16-row operand A, tokens the 8-column operand B: a warp's lane
+// 4 g + t holds rows g and g + 8 of A, token g of B, and of the sums rows g and
+// g + 8 of tokens 2 t and 2 t + 1.  Which columns of a row form an instruction's
+// 16 is free as long as A and B agree, so a lane's 8 columns of each 32 are
+// adjacent: 16 bytes of tokens, 32 bits of codes, and no exchange between lanes.
+template <class T>
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                    uint32_t b0, uint32_t b1) {
+    if (std::is_same<T, BF16>::value)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Codes n and n + 4 of a word (columns 2 n, 2 n + 1) as a pair of 16-bit numbers:
+// placed in the low mantissa bits of 128 (float16: 1024) they read 128 + q + 8,
+// and the subtraction is exact.
+template <class T>
+__device__ __forceinline__ uint32_t codes(uint32_t word, int n) {
+    constexpr bool kB = std::is_same<T, BF16>::value;
+    constexpr uint32_t kBias = kB ? 0x43004300u : 0x64006400u;
+    const uint32_t v = ((word >> (4 * n)) & 0x000F000Fu) | kBias;
+    if (kB) {
+        const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v),
+                                         __nv_bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308)));
+        return *reinterpret_cast<const uint32_t*>(&d);
+    }
+    const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&v),
+                              __half2(__ushort_as_half(0x6408), __ushort_as_half(0x6408)));
+    return *reinterpret_cast<const uint32_t*>(&d);
+}
+
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
+
+template <int N>
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
+    if (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(N) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+constexpr int kWarps = 16;         // of a block: one block per SM
+constexpr int kProdThreads = 32 * kWarps;
+constexpr int kStages = 5;         // blocks of weights that a warp has in flight
+
+// A lane's part of a block of codes: two runs of 16 bytes and its scales.  A lane
+// copies what it will read itself, so a stage needs no barrier between lanes.
+template <int G>
+struct Stage {
+    static constexpr int kScale = 512 / G;                 // bytes of a slot pair's scales
+    static constexpr int kBytes = kCodes + 8 * kScale;     // = block_bytes(G)
+    static __device__ __forceinline__ void load(uint32_t to, const char* from, int lane) {
+        copy_async<16>(to + 16 * lane, from + 16 * lane);
+        copy_async<16>(to + 512 + 16 * lane, from + 512 + 16 * lane);
+        const int g = lane >> 2;
+        // Four lanes share a slot pair's scales; each copies them for itself to
+        // the same place.
+        copy_async<kScale>(to + kCodes + kScale * g, from + kCodes + kScale * g);
+    }
+};
+
+// sum += W x over one block of 128 columns.  x: shared memory, the tokens' rows
+// `pitch` bytes apart, at the block's first column; lanes of absent tokens hold
+// zeros.  Groups are summed in the matrix unit and scaled in float32.
+template <class T, int G, int NT>
+__device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* stage, const char* x,
+                                              int pitch, int tokens, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+    const uint4 lo = *reinterpret_cast<const uint4*>(stage + 16 * lane);
+    const uint4 hi = *reinterpret_cast<const uint4*>(stage + 512 + 16 * lane);
+    uint32_t s[128 / G];       // {slot g, slot g + 8}
+#pragma unroll
+    for (int k = 0; k < 128 / G; ++k)
+        s[k] = reinterpret_cast<const uint32_t*>(stage + kCodes)[g * (128 / G) + k];
+    const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
+    float part[NT][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (32 * j % G == 0)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) part[n][0] = part[n][1] = part[n][2] = part[n][3] = 0.0f;
+        uint32_t al[4], ah[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) al[i] = codes<T>(wl[j], i), ah[i] = codes<T>(wh[j], i);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (8 * n + g < tokens)
+                v = *reinterpret_cast<const uint4*>(x + (8 * n + g) * pitch + 64 * j + 16 * t);
+            mma<T>(part[n], al[0], ah[0], al[1], ah[1], v.x, v.y);
+            mma<T>(part[n], al[2], ah[2], al[3], ah[3], v.z, v.w);
+        }
+        if (32 * (j + 1) % G == 0) {
+            const float sl = T::widen(uint16_t(s[32 * j / G])), sh = T::widen(uint16_t(s[32 * j / G] >> 16));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                sum[n][0] = fmaf(sl, part[n][0], sum[n][0]);
+                sum[n][1] = fmaf(sl, part[n][1], sum[n][1]);
+                sum[n][2] = fmaf(sh, part[n][2], sum[n][2]);
+                sum[n][3] = fmaf(sh, part[n][3], sum[n][3]);
             }
         }
-        for (int h = 0; h < 2; ++h)
-            for (int o = 1; o < 4; o *= 2) sum[h] += __shfl_xor_sync(~0u, sum[h], o);
-        if (t != 0) continue;
-        const int64_t lo = m.row(strip, g), hi = m.row(strip, 8 + g);
-        if (m.pair) {
-            if (lo >= 0) put<T, F32>(out, n * ldo + lo, silu(sum[0]) * sum[1]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Matrix-vector products
+// ---------------------------------------------------------------------------
+
+struct MatvecArgs {
+    Packed m;
+    const char* packed;
+    const uint16_t* x;
+    void* out;
+    int64_t ldx, ldo;
+    int32_t tokens, f32;
+    int32_t vec;          // x's rows can be read 16 bytes at a time
+    int32_t pitch;        // bytes between tokens in shared memory
+    int32_t team;         // warps that share a strip's columns: 1, 2, 4, 8 or 16
+    int32_t cluster;      // blocks that share the columns
+    int32_t batch;        // strips between two joins of the teams' sums
+};
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive;\nbarrier.cluster.wait;" ::: "memory");
+}
+
+// The epilogue of rows g, g + 8 and tokens 2 t, 2 t + 1 (+ 8 n) of a strip.
+template <class T>
+__device__ __forceinline__ void put_strip(const MatvecArgs& a, int64_t strip, int lane, int n, const float (&v)[4]) {
+    const int g = lane >> 2, t = lane & 3;
+    const int64_t lo = a.m.row(strip, g), hi = a.m.row(strip, 8 + g);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int tok = 8 * n + 2 * t + i;
+        if (tok >= a.tokens || lo < 0) continue;
+        const int64_t at = tok * a.ldo;
+        if (a.m.pair) {
+            const float h = silu(v[i]) * v[2 + i];
+            if (a.f32) put<T, true>(a.out, at + lo, h);
+            else put<T, false>(a.out, at + lo, h);
         } else {
-            if (lo >= 0) put<T, F32>(out, n * ldo + lo, sum[0]);
-            if (hi >= 0) put<T, F32>(out, n * ldo + hi, sum[1]);
+            if (a.f32) put<T, true>(a.out, at + lo, v[i]);
+            else put<T, false>(a.out, at + lo, v[i]);
+            if (hi >= 0) {
+                if (a.f32) put<T, true>(a.out, at + hi, v[2 + i]);
+                else put<T, false>(a.out, at + hi, v[2 + i]);
+            }
         }
     }
+}
+
+// A cluster takes a run of strips; each of its blocks takes a share of the
+// columns, whose tokens it keeps in shared memory, and of these each warp of a
+// team every team-th block of 128.  Warps stream their blocks through stages of
+// their own without meeting; sums of a batch of strips are joined through shared
+// memory in a fixed order.
+template <class T, int G, int NT>
+__global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid_constant__ MatvecArgs a) {
+    extern __shared__ __align__(128) char smem[];
+    using S = Stage<G>;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int rank = blockIdx.x % a.cluster, cl = blockIdx.x / a.cluster, n_cl = gridDim.x / a.cluster;
+    // Programmatic dependent launch: the next kernel may be scheduled, and waits
+    // as this one does for the kernels before it.
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    char* const fifo = smem + warp * (kStages * S::kBytes);
+    char* const xs = smem + kWarps * kStages * S::kBytes;
+    float4* const red = reinterpret_cast<float4*>(xs + a.tokens * a.pitch);
+
+    const int64_t s0 = cl * a.m.strips / n_cl, s1 = (cl + 1) * a.m.strips / n_cl;
+    const int b0 = int(rank * a.m.blocks / a.cluster), b1 = int((rank + 1) * a.m.blocks / a.cluster);
+    const int teams = kWarps / a.team, team = warp / a.team, part = warp % a.team;
+
+    // The load cursor runs kStages blocks ahead of the products.
+    int64_t ls = s0 + team;
+    int lb = b0 + part, slot = 0;
+    if (lb >= b1) ls = s1;
+    const uint32_t fifo_at = smem_at(fifo);
+    auto load = [&](int to) {
+        if (ls < s1) {
+            S::load(fifo_at + to * S::kBytes, a.packed + (ls * a.m.blocks + lb) * S::kBytes, lane);
+            lb += a.team;
+            if (lb >= b1) lb = b0 + part, ls += teams;
+        }
+        copy_commit();
+    };
+    for (int i = 0; i < kStages; ++i) load(i);
+
+    // Tokens: this block's columns, zeros past the matrix's.
+    const int cols = (b1 - b0) * kBlock;
+    const int64_t c0 = int64_t(b0) * kBlock;
+    if (a.vec) {
+        for (int i = threadIdx.x; i < a.tokens * (cols / 8); i += kProdThreads) {
+            const int n = i / (cols / 8), c = 8 * (i % (cols / 8));
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (c0 + c + 8 <= a.m.cols) {
+                v = *reinterpret_cast<const uint4*>(a.x + n * a.ldx + c0 + c);
+            } else {
+                uint32_t w[4] = {0, 0, 0, 0};
+                for (int k = 0; k < 8; ++k)
+                    if (c0 + c + k < a.m.cols) w[k / 2] |= uint32_t(a.x[n * a.ldx + c0 + c + k]) << (16 * (k % 2));
+                v = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            *reinterpret_cast<uint4*>(xs + n * a.pitch + 2 * c) = v;
+        }
+    } else {
+        for (int i = threadIdx.x; i < a.tokens * cols; i += kProdThreads) {
+            const int n = i / cols, c = i % cols;
+            *reinterpret_cast<uint16_t*>(xs + n * a.pitch + 2 * c) =
+                c0 + c < a.m.cols ? a.x[n * a.ldx + c0 + c] : uint16_t(0);
+        }
+    }
+    __syncthreads();
+
+    const bool alone = a.team == 1 && a.cluster == 1;
+    for (int64_t from = s0; from < s1; from += a.batch) {
+        const int64_t to = min(from + a.batch, s1);
+        for (int64_t strip = from + team; strip < to; strip += teams) {
+            float sum[NT][4] = {};
+            for (int b = b0 + part; b < b1; b += a.team) {
+                copy_wait<kStages - 1>();
+                block_product<T, G, NT>(sum, fifo + slot * S::kBytes, xs + (b - b0) * (2 * kBlock), a.pitch,
+                                        a.tokens, lane);
+                __syncwarp();      // the scales that lanes share have been read
+                load(slot);
+                slot = slot + 1 == kStages ? 0 : slot + 1;
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if (alone) put_strip<T>(a, strip, lane, n, sum[n]);
+                else
+                    red[((part * a.batch + int(strip - from)) * NT + n) * 32 + lane] =
+                        make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
+            }
+        }
+        if (alone) continue;
+        if (a.cluster > 1) cluster_sync();
+        else __syncthreads();
+        const int count = int(to - from) * NT * 32;
+        for (int i = rank * kProdThreads + threadIdx.x; i < count; i += a.cluster * kProdThreads) {
+            float v[4] = {};
+            for (int r = 0; r < a.cluster; ++r) {
+                uint32_t at = smem_at(red + i);
+                if (a.cluster > 1) asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(at), "r"(r));
+                for (int p = 0; p < a.team; ++p) {
+                    float4 f;
+                    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+                                 : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
+                                 : "r"(at + uint32_t(p * a.batch * NT * 32 * sizeof(float4))) : "memory");
+                    v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+                }
+            }
+            put_strip<T>(a, from + i / (NT * 32), i & 31, i / 32 % NT, v);
+        }
+        // The sums have been read, here and by the cluster's other blocks, before
+        // they are overwritten or this block ends.
+        if (a.cluster > 1) cluster_sync();
+        else __syncthreads();
+    }
+    copy_wait<0>();
 }
 
 // ---------------------------------------------------------------------------
@@ -367,8 +601,8 @@ rr_status check_device(const void* p, size_t align, const char* what) {
 
 rr_status check_quant(const rr_quant* q) {
     if (!q) return rr_fail(RR_EINVAL, "matrix description is NULL");
-    if (q->rows < 1 || q->rows > INT32_MAX || q->cols < 1 || q->cols > (1 << 24))
-        return rr_fail(RR_ELAYOUT, "matrix of %lld x %lld: 1..2^31-1 rows and 1..2^24 columns",
+    if (q->rows < 1 || q->rows > INT32_MAX || q->cols < 1 || q->cols > kMaxCols)
+        return rr_fail(RR_ELAYOUT, "matrix of %lld x %lld: 1..2^31-1 rows and 1..2^18 columns",
                        (long long)q->rows, (long long)q->cols);
     if (q->count < 1 || q->count > 65535) return rr_fail(RR_ELAYOUT, "count %d: 1..65535", q->count);
     if (q->group != 32 && q->group != 64 && q->group != 128)
@@ -513,6 +747,81 @@ extern "C" rr_status rr_dequantize(const rr_quant* q, const void* packed, void* 
     });
 }
 
+namespace {
+
+struct MatvecShape {
+    unsigned grid;
+    int smem;
+};
+constexpr int kSmem = 227 * 1024;
+constexpr int kJoinBytes = 24 * 1024;   // shared memory of the teams' sums
+constexpr int kSms = 152;
+
+// How a product is shared out, for a.tokens tokens; false if these do not fit.
+// The time of a launch goes by the blocks of 128 columns that the busiest warp
+// takes; joins cost about one of them.  Measured on GB300: see the table of
+// DESIGN.
+bool matvec_shape(MatvecArgs* a, int group, MatvecShape* shape) {
+    const int tiles = a->tokens > 8 ? 2 : 1;
+    const int room = kSmem - kWarps * kStages * block_bytes(group) - kJoinBytes;
+    int64_t best = INT64_MAX;
+    for (int cluster = 1; cluster <= 8; cluster *= 2) {
+        if (cluster > a->m.blocks) break;
+        const int64_t blocks = (a->m.blocks + cluster - 1) / cluster;
+        // Rows 64 bytes past a multiple of 128, so that two tokens' rows are on
+        // different halves of the banks.
+        const int64_t pitch = blocks * 2 * kBlock + 64;
+        if (pitch * a->tokens > room) continue;
+        const int64_t groups = std::min<int64_t>(kSms / cluster, a->m.strips);
+        const int64_t strips = (a->m.strips + groups - 1) / groups;
+        for (int team = 1; team <= kWarps; team *= 2) {
+            const int teams = kWarps / team;
+            // (Warps stream on from batch to batch: whole rounds of the teams.)
+            const bool alone = team == 1 && cluster == 1;
+            const int64_t fit = kJoinBytes / (512 * tiles * team) / teams * teams;
+            const int64_t batch = alone ? strips : std::min(strips, fit);
+            const int64_t joins = alone ? 0 : (strips + batch - 1) / batch;
+            const int64_t steps = (blocks + team - 1) / team;
+            int64_t cost = 0;
+            for (int64_t left = strips; left > 0; left -= batch)
+                cost += (std::min(left, batch) + teams - 1) / teams * steps;
+            cost += joins * (cluster > 1 ? 2 : 1);
+            if (cost >= best) continue;
+            best = cost;
+            a->pitch = int32_t(pitch);
+            a->team = team;
+            a->cluster = cluster;
+            a->batch = int32_t(batch);
+            shape->grid = unsigned(groups * cluster);
+            shape->smem = kWarps * kStages * block_bytes(group) + int(pitch) * a->tokens
+                          + (joins ? int(batch) * 512 * tiles * team : 0);
+        }
+    }
+    return best != INT64_MAX;
+}
+
+cudaError_t launch_matvec(void (*kernel)(MatvecArgs), const MatvecArgs& a, const MatvecShape& shape,
+                          cudaStream_t stream) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = unsigned(a.cluster);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(shape.grid);
+    cfg.blockDim = dim3(kProdThreads);
+    cfg.dynamicSmemBytes = size_t(shape.smem);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+}  // namespace
+
 extern "C" rr_status rr_matvec(const rr_quant* q, const void* packed, const void* x, int64_t ldx,
                                int32_t n_tokens, void* out, int64_t ldo, int32_t f32,
                                cudaStream_t stream) {
@@ -531,18 +840,31 @@ extern "C" rr_status rr_matvec(const rr_quant* q, const void* packed, const void
     RR_TRY(check_device(packed, 16, "packed"));
     RR_TRY(check_device(x, 2, "x"));
     RR_TRY(check_device(out, f32 ? 4 : 2, "out"));
-    const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
-    unsigned grid;
-    RR_TRY(grid_of(m.strips, 4, &grid));
     return with_group(q->dtype, q->group, [&](auto t, auto g) -> rr_status {
+        using T = decltype(t);
         constexpr int G = decltype(g)::value ? decltype(g)::value : 128;
-        const char* const p = static_cast<const char*>(packed);
-        const uint16_t* const v = static_cast<const uint16_t*>(x);
-        if (f32)
-            rr_matvec_kernel<decltype(t), G, true><<<grid, 128, 0, stream>>>(m, p, v, ldx, n_tokens, out, ldo);
-        else
-            rr_matvec_kernel<decltype(t), G, false><<<grid, 128, 0, stream>>>(m, p, v, ldx, n_tokens, out, ldo);
-        RR_CUDA(cudaGetLastError());
+        MatvecArgs a;
+        a.m = packed_of(q->rows, q->cols, q->group, q->pair);
+        a.packed = static_cast<const char*>(packed);
+        a.ldx = ldx;
+        a.ldo = ldo;
+        a.f32 = f32;
+        a.vec = (uintptr_t)x % 16 == 0 && (ldx % 8 == 0 || n_tokens == 1);
+        // Tokens that one launch takes: all of them but for very long rows, whose
+        // tokens would not fit the blocks' shared memory.
+        for (int n0 = 0; n0 < n_tokens; n0 += a.tokens) {
+            a.tokens = n_tokens - n0;
+            a.x = static_cast<const uint16_t*>(x) + n0 * ldx;
+            a.out = static_cast<char*>(out) + n0 * ldo * (f32 ? 4 : 2);
+            MatvecShape shape;
+            while (!matvec_shape(&a, G, &shape)) {
+                if (a.tokens == 1) return rr_fail(RR_ELAYOUT, "rows of %lld columns", (long long)q->cols);
+                a.tokens = (a.tokens + 1) / 2;
+            }
+            const cudaError_t e = a.tokens > 8 ? launch_matvec(rr_matvec_kernel<T, G, 2>, a, shape, stream)
+                                               : launch_matvec(rr_matvec_kernel<T, G, 1>, a, shape, stream);
+            if (e != cudaSuccess) return cuda_fail(e, "rr_matvec");
+        }
         return RR_OK;
     });
 }
