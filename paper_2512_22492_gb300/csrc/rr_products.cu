@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <mutex>
 #include <type_traits>
 
 #include "rr_internal.h"
@@ -178,8 +179,8 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
 template <class T>
 __device__ __forceinline__ uint32_t codes(uint32_t word, int n) {
     constexpr bool kB = std::is_same<T, BF16>::value;
-    constexpr uint32_t kBias = kB ? 0x43004300u : 0x64006400u;
-    const uint32_t v = ((word >> (4 * n)) & 0x000F000Fu) | kBias;
+    uint32_t v;
+    asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(v) : "r"(word >> (4 * n)), "r"(kB ? 0x43004300u : 0x64006400u));
     if (kB) {
         const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v),
                                          __nv_bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308)));
@@ -196,6 +197,10 @@ template <int N>
 __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
     if (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(N) : "memory");
+}
+// 16 bytes of shared memory: `bytes` copied, the rest zero.
+__device__ __forceinline__ void copy_async_cut(uint32_t to, const void* from, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -221,13 +226,13 @@ struct Stage {
     }
 };
 
-// sum += W x over one block of 128 columns.  x: shared memory, the tokens' rows
-// `pitch` bytes apart, at the block's first column; lanes of absent tokens hold
-// zeros.  Groups are summed in the matrix unit and scaled in float32.
+// sum += W x over one block of 128 columns.  x[n]: this lane's 16 bytes of its
+// token's row at the block's first column, in shared memory.  Groups are summed
+// in the matrix unit and scaled in float32.
 template <class T, int G, int NT>
-__device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* stage, const char* x,
-                                              int pitch, int tokens, int lane) {
-    const int g = lane >> 2, t = lane & 3;
+__device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* stage, const char* const (&x)[NT],
+                                              int at, int lane) {
+    const int g = lane >> 2;
     const uint4 lo = *reinterpret_cast<const uint4*>(stage + 16 * lane);
     const uint4 hi = *reinterpret_cast<const uint4*>(stage + 512 + 16 * lane);
     uint32_t s[128 / G];       // {slot g, slot g + 8}
@@ -246,9 +251,7 @@ __device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* s
         for (int i = 0; i < 4; ++i) al[i] = codes<T>(wl[j], i), ah[i] = codes<T>(wh[j], i);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (8 * n + g < tokens)
-                v = *reinterpret_cast<const uint4*>(x + (8 * n + g) * pitch + 64 * j + 16 * t);
+            const uint4 v = *reinterpret_cast<const uint4*>(x[n] + at + 64 * j);
             mma<T>(part[n], al[0], ah[0], al[1], ah[1], v.x, v.y);
             mma<T>(part[n], al[2], ah[2], al[3], ah[3], v.z, v.w);
         }
@@ -336,55 +339,64 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
     const int teams = kWarps / a.team, team = warp / a.team, part = warp % a.team;
 
     // The load cursor runs kStages blocks ahead of the products.
-    int64_t ls = s0 + team;
-    int lb = b0 + part, slot = 0;
-    if (lb >= b1) ls = s1;
+    int left_strips = int((s1 - s0 - team + teams - 1) / teams);
+    const int steps = (b1 - b0 - part + a.team - 1) / a.team;      // blocks of a strip that this warp takes
+    if (steps <= 0) left_strips = 0;
+    int left = steps, slot = 0;
+    const char* from_w = a.packed + ((s0 + team) * a.m.blocks + b0 + part) * S::kBytes;
+    const int64_t next_block = int64_t(a.team) * S::kBytes;
+    const int64_t next_strip = (teams * a.m.blocks - int64_t(steps - 1) * a.team) * S::kBytes;
     const uint32_t fifo_at = smem_at(fifo);
     auto load = [&](int to) {
-        if (ls < s1) {
-            S::load(fifo_at + to * S::kBytes, a.packed + (ls * a.m.blocks + lb) * S::kBytes, lane);
-            lb += a.team;
-            if (lb >= b1) lb = b0 + part, ls += teams;
+        if (left_strips > 0) {
+            S::load(fifo_at + to * S::kBytes, from_w, lane);
+            if (--left == 0) {
+                left = steps;
+                --left_strips;
+                from_w += next_strip;
+            } else {
+                from_w += next_block;
+            }
         }
         copy_commit();
     };
-    for (int i = 0; i < kStages; ++i) load(i);
 
     // Tokens: this block's columns, zeros past the matrix's.
     const int cols = (b1 - b0) * kBlock;
     const int64_t c0 = int64_t(b0) * kBlock;
     if (a.vec) {
-        for (int i = threadIdx.x; i < a.tokens * (cols / 8); i += kProdThreads) {
-            const int n = i / (cols / 8), c = 8 * (i % (cols / 8));
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (c0 + c + 8 <= a.m.cols) {
-                v = *reinterpret_cast<const uint4*>(a.x + n * a.ldx + c0 + c);
-            } else {
-                uint32_t w[4] = {0, 0, 0, 0};
-                for (int k = 0; k < 8; ++k)
-                    if (c0 + c + k < a.m.cols) w[k / 2] |= uint32_t(a.x[n * a.ldx + c0 + c + k]) << (16 * (k % 2));
-                v = make_uint4(w[0], w[1], w[2], w[3]);
+        // 16-byte copies, cut off (and zero-filled) at the row's end.
+        for (int n = 0; n < a.tokens; ++n)
+            for (int c = 8 * threadIdx.x; c < cols; c += 8 * kProdThreads) {
+                const int64_t left = a.m.cols - c0 - c;
+                copy_async_cut(smem_at(xs + n * a.pitch + 2 * c), a.x + n * a.ldx + (left > 0 ? c0 + c : 0),
+                               left >= 8 ? 16 : left > 0 ? 2 * int(left) : 0);
             }
-            *reinterpret_cast<uint4*>(xs + n * a.pitch + 2 * c) = v;
-        }
     } else {
-        for (int i = threadIdx.x; i < a.tokens * cols; i += kProdThreads) {
-            const int n = i / cols, c = i % cols;
-            *reinterpret_cast<uint16_t*>(xs + n * a.pitch + 2 * c) =
-                c0 + c < a.m.cols ? a.x[n * a.ldx + c0 + c] : uint16_t(0);
-        }
+        for (int n = 0; n < a.tokens; ++n)
+#pragma unroll 8
+            for (int c = threadIdx.x; c < cols; c += kProdThreads)
+                *reinterpret_cast<uint16_t*>(xs + n * a.pitch + 2 * c) =
+                    c0 + c < a.m.cols ? a.x[n * a.ldx + c0 + c] : uint16_t(0);
     }
+    copy_commit();
+    for (int i = 0; i < kStages; ++i) load(i);
+    copy_wait<kStages>();
     __syncthreads();
 
+    // A lane of an absent token reads the last one's row; its sums go nowhere.
+    const char* x[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+        x[n] = xs + min(8 * n + (lane >> 2), a.tokens - 1) * a.pitch + 16 * (lane & 3);
     const bool alone = a.team == 1 && a.cluster == 1;
     for (int64_t from = s0; from < s1; from += a.batch) {
         const int64_t to = min(from + a.batch, s1);
         for (int64_t strip = from + team; strip < to; strip += teams) {
             float sum[NT][4] = {};
-            for (int b = b0 + part; b < b1; b += a.team) {
+            for (int i = 0; i < steps; ++i) {
                 copy_wait<kStages - 1>();
-                block_product<T, G, NT>(sum, fifo + slot * S::kBytes, xs + (b - b0) * (2 * kBlock), a.pitch,
-                                        a.tokens, lane);
+                block_product<T, G, NT>(sum, fifo + slot * S::kBytes, x, (part + i * a.team) * (2 * kBlock), lane);
                 __syncwarp();      // the scales that lanes share have been read
                 load(slot);
                 slot = slot + 1 == kStages ? 0 : slot + 1;
@@ -755,7 +767,39 @@ struct MatvecShape {
 };
 constexpr int kSmem = 227 * 1024;
 constexpr int kJoinBytes = 24 * 1024;   // shared memory of the teams' sums
-constexpr int kSms = 152;
+
+// Clusters of a size that this GPU runs at once with one block per SM (GB300: 152,
+// 76, 36 and 15 of 1, 2, 4 and 8 blocks, since a cluster stays within one GPC).
+// Asked once per device.
+template <class K>
+int clusters_at_once(K* kernel, int cluster) {
+    static std::mutex mutex;
+    static int known[16][4] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev > 15) return 1;
+    const int i = cluster == 1 ? 0 : cluster == 2 ? 1 : cluster == 4 ? 2 : 3;
+    const std::lock_guard<std::mutex> lock(mutex);
+    if (!known[dev][i]) {
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = unsigned(cluster);
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(unsigned(cluster));
+        cfg.blockDim = dim3(kProdThreads);
+        cfg.dynamicSmemBytes = kSmem;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+            cudaGetLastError();
+            return 1;
+        }
+        known[dev][i] = n;
+    }
+    return known[dev][i];
+}
 
 // How a product is shared out, for a.tokens tokens; false if these do not fit.
 // The time of a launch goes by the blocks of 128 columns that the busiest warp
@@ -772,7 +816,7 @@ bool matvec_shape(MatvecArgs* a, int group, MatvecShape* shape) {
         // different halves of the banks.
         const int64_t pitch = blocks * 2 * kBlock + 64;
         if (pitch * a->tokens > room) continue;
-        const int64_t groups = std::min<int64_t>(kSms / cluster, a->m.strips);
+        const int64_t groups = std::min<int64_t>(clusters_at_once(rr_matvec_kernel<BF16, 128, 1>, cluster), a->m.strips);
         const int64_t strips = (a->m.strips + groups - 1) / groups;
         for (int team = 1; team <= kWarps; team *= 2) {
             const int teams = kWarps / team;
