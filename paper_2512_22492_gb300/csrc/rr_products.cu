@@ -173,6 +173,20 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// c = A B.
+template <class T>
+__device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                          uint32_t b0, uint32_t b1) {
+    if (std::is_same<T, BF16>::value)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+
 // Codes n and n + 4 of a word (columns 2 n, 2 n + 1) as a pair of 16-bit numbers:
 // placed in the low mantissa bits of 128 (float16: 1024) they read 128 + q + 8,
 // and the subtraction is exact.
@@ -208,21 +222,28 @@ __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group 
 
 constexpr int kWarps = 16;         // of a block: one block per SM
 constexpr int kProdThreads = 32 * kWarps;
-constexpr int kStages = 5;         // blocks of weights that a warp has in flight
 
-// A lane's part of a block of codes: two runs of 16 bytes and its scales.  A lane
-// copies what it will read itself, so a stage needs no barrier between lanes.
-template <int G>
+// A warp's stages of U adjacent blocks of codes each: enough of them that a block
+// has 64 to 100 KB in flight, and a wait, a copy's address and a loop's step for
+// U blocks at a time.  A lane copies the 16-byte runs that it reads itself; of
+// the scales, which four lanes share, lanes 0..7 copy a slot pair's each.
+template <int G, int U>
 struct Stage {
     static constexpr int kScale = 512 / G;                 // bytes of a slot pair's scales
-    static constexpr int kBytes = kCodes + 8 * kScale;     // = block_bytes(G)
-    static __device__ __forceinline__ void load(uint32_t to, const char* from, int lane) {
-        copy_async<16>(to + 16 * lane, from + 16 * lane);
-        copy_async<16>(to + 512 + 16 * lane, from + 512 + 16 * lane);
-        const int g = lane >> 2;
-        // Four lanes share a slot pair's scales; each copies them for itself to
-        // the same place.
-        copy_async<kScale>(to + kCodes + kScale * g, from + kCodes + kScale * g);
+    static constexpr int kBlockBytes = kCodes + 8 * kScale;     // = block_bytes(G)
+    static constexpr int kBytes = U * kBlockBytes;
+    static constexpr int kStages = 6 / U;
+    // from: the block's codes at this lane's run; scales: at this lane's (< 8) scales.
+    static __device__ __forceinline__ void load(uint32_t to, const char* from, const char* scales, int blocks,
+                                                int lane) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u > 0 && blocks <= u) break;
+            copy_async<16>(to + u * kBlockBytes + 16 * lane, from + u * kBlockBytes);
+            copy_async<16>(to + u * kBlockBytes + 512 + 16 * lane, from + u * kBlockBytes + 512);
+            if (lane < 8) copy_async<kScale>(to + u * kBlockBytes + kCodes + kScale * lane, scales + u * kBlockBytes);
+        }
+        copy_commit();
     }
 };
 
@@ -243,16 +264,14 @@ __device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* s
     float part[NT][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        if (32 * j % G == 0)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) part[n][0] = part[n][1] = part[n][2] = part[n][3] = 0.0f;
         uint32_t al[4], ah[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) al[i] = codes<T>(wl[j], i), ah[i] = codes<T>(wh[j], i);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const uint4 v = *reinterpret_cast<const uint4*>(x[n] + at + 64 * j);
-            mma<T>(part[n], al[0], ah[0], al[1], ah[1], v.x, v.y);
+            if (32 * j % G == 0) mma_first<T>(part[n], al[0], ah[0], al[1], ah[1], v.x, v.y);
+            else mma<T>(part[n], al[0], ah[0], al[1], ah[1], v.x, v.y);
             mma<T>(part[n], al[2], ah[2], al[3], ah[3], v.z, v.w);
         }
         if (32 * (j + 1) % G == 0) {
@@ -317,48 +336,52 @@ __device__ __forceinline__ void put_strip(const MatvecArgs& a, int64_t strip, in
 
 // A cluster takes a run of strips; each of its blocks takes a share of the
 // columns, whose tokens it keeps in shared memory, and of these each warp of a
-// team every team-th block of 128.  Warps stream their blocks through stages of
-// their own without meeting; sums of a batch of strips are joined through shared
-// memory in a fixed order.
-template <class T, int G, int NT>
+// team every team-th run of U blocks of 128.  Warps stream their blocks through
+// stages of their own without meeting; sums of a batch of strips are joined
+// through shared memory in a fixed order.
+template <class T, int G, int NT, int U>
 __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid_constant__ MatvecArgs a) {
     extern __shared__ __align__(128) char smem[];
-    using S = Stage<G>;
+    using S = Stage<G, U>;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rank = blockIdx.x % a.cluster, cl = blockIdx.x / a.cluster, n_cl = gridDim.x / a.cluster;
     // Programmatic dependent launch: the next kernel may be scheduled, and waits
     // as this one does for the kernels before it.
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    char* const fifo = smem + warp * (kStages * S::kBytes);
-    char* const xs = smem + kWarps * kStages * S::kBytes;
+    char* const fifo = smem + warp * (S::kStages * S::kBytes);
+    char* const xs = smem + kWarps * S::kStages * S::kBytes;
     float4* const red = reinterpret_cast<float4*>(xs + a.tokens * a.pitch);
 
     const int64_t s0 = cl * a.m.strips / n_cl, s1 = (cl + 1) * a.m.strips / n_cl;
     const int b0 = int(rank * a.m.blocks / a.cluster), b1 = int((rank + 1) * a.m.blocks / a.cluster);
     const int teams = kWarps / a.team, team = warp / a.team, part = warp % a.team;
 
-    // The load cursor runs kStages blocks ahead of the products.
-    int left_strips = int((s1 - s0 - team + teams - 1) / teams);
-    const int steps = (b1 - b0 - part + a.team - 1) / a.team;      // blocks of a strip that this warp takes
-    if (steps <= 0) left_strips = 0;
-    int left = steps, slot = 0;
-    const char* from_w = a.packed + ((s0 + team) * a.m.blocks + b0 + part) * S::kBytes;
-    const int64_t next_block = int64_t(a.team) * S::kBytes;
-    const int64_t next_strip = (teams * a.m.blocks - int64_t(steps - 1) * a.team) * S::kBytes;
+    // This warp takes runs part, part + team, ... of a strip.  The load cursor
+    // goes over them, strip after strip, ahead of the products.
+    const int runs = (b1 - b0 + U - 1) / U;
+    const int steps = (runs - part + a.team - 1) / a.team;
+    int left_strips = steps > 0 ? int((s1 - s0 - team + teams - 1) / teams) : 0;
+    int lb = b0 + U * part, slot = 0;
+    const char* from = a.packed + ((s0 + team) * a.m.blocks + lb) * S::kBlockBytes + 16 * lane;
+    const int64_t scales = kCodes + (S::kScale - 16) * lane;      // from a run's codes to its scales
+    const int64_t next_run = int64_t(a.team) * S::kBytes;
+    const int64_t next_strip = (teams * a.m.blocks - int64_t(steps - 1) * a.team * U) * S::kBlockBytes;
     const uint32_t fifo_at = smem_at(fifo);
     auto load = [&](int to) {
         if (left_strips > 0) {
-            S::load(fifo_at + to * S::kBytes, from_w, lane);
-            if (--left == 0) {
-                left = steps;
+            S::load(fifo_at + to * S::kBytes, from, from + scales, b1 - lb, lane);
+            lb += a.team * U;
+            if (lb >= b1) {
+                lb = b0 + U * part;
                 --left_strips;
-                from_w += next_strip;
+                from += next_strip;
             } else {
-                from_w += next_block;
+                from += next_run;
             }
+        } else {
+            copy_commit();
         }
-        copy_commit();
     };
 
     // Tokens: this block's columns, zeros past the matrix's.
@@ -380,8 +403,8 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
                     c0 + c < a.m.cols ? a.x[n * a.ldx + c0 + c] : uint16_t(0);
     }
     copy_commit();
-    for (int i = 0; i < kStages; ++i) load(i);
-    copy_wait<kStages>();
+    for (int i = 0; i < S::kStages - 1; ++i) load(i);
+    copy_wait<S::kStages - 1>();
     __syncthreads();
 
     // A lane of an absent token reads the last one's row; its sums go nowhere.
@@ -395,11 +418,16 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
         for (int64_t strip = from + team; strip < to; strip += teams) {
             float sum[NT][4] = {};
             for (int i = 0; i < steps; ++i) {
-                copy_wait<kStages - 1>();
-                block_product<T, G, NT>(sum, fifo + slot * S::kBytes, x, (part + i * a.team) * (2 * kBlock), lane);
-                __syncwarp();      // the scales that lanes share have been read
-                load(slot);
-                slot = slot + 1 == kStages ? 0 : slot + 1;
+                copy_wait<S::kStages - 2>();
+                __syncwarp();      // the scales are there for every lane, and the last stage has been read
+                load(slot == 0 ? S::kStages - 1 : slot - 1);
+                const int at = U * (part + i * a.team);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (u == 0 || at + u < b1 - b0)
+                        block_product<T, G, NT>(sum, fifo + slot * S::kBytes + u * S::kBlockBytes, x,
+                                                (at + u) * (2 * kBlock), lane);
+                slot = slot + 1 == S::kStages ? 0 : slot + 1;
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -764,6 +792,7 @@ namespace {
 struct MatvecShape {
     unsigned grid;
     int smem;
+    int run;        // blocks of a stage
 };
 constexpr int kSmem = 227 * 1024;
 constexpr int kJoinBytes = 24 * 1024;   // shared memory of the teams' sums
@@ -807,7 +836,8 @@ int clusters_at_once(K* kernel, int cluster) {
 // DESIGN.
 bool matvec_shape(MatvecArgs* a, int group, MatvecShape* shape) {
     const int tiles = a->tokens > 8 ? 2 : 1;
-    const int room = kSmem - kWarps * kStages * block_bytes(group) - kJoinBytes;
+    const int fifo = kWarps * 6 * block_bytes(group);
+    const int room = kSmem - fifo - kJoinBytes;
     int64_t best = INT64_MAX;
     for (int cluster = 1; cluster <= 8; cluster *= 2) {
         if (cluster > a->m.blocks) break;
@@ -816,7 +846,7 @@ bool matvec_shape(MatvecArgs* a, int group, MatvecShape* shape) {
         // different halves of the banks.
         const int64_t pitch = blocks * 2 * kBlock + 64;
         if (pitch * a->tokens > room) continue;
-        const int64_t groups = std::min<int64_t>(clusters_at_once(rr_matvec_kernel<BF16, 128, 1>, cluster), a->m.strips);
+        const int64_t groups = std::min<int64_t>(clusters_at_once(rr_matvec_kernel<BF16, 128, 1, 1>, cluster), a->m.strips);
         const int64_t strips = (a->m.strips + groups - 1) / groups;
         for (int team = 1; team <= kWarps; team *= 2) {
             const int teams = kWarps / team;
@@ -825,7 +855,9 @@ bool matvec_shape(MatvecArgs* a, int group, MatvecShape* shape) {
             const int64_t fit = kJoinBytes / (512 * tiles * team) / teams * teams;
             const int64_t batch = alone ? strips : std::min(strips, fit);
             const int64_t joins = alone ? 0 : (strips + batch - 1) / batch;
-            const int64_t steps = (blocks + team - 1) / team;
+            // Runs of two blocks where they cost nothing.
+            const int64_t one = (blocks + team - 1) / team, two = 2 * (((blocks + 1) / 2 + team - 1) / team);
+            const int64_t steps = one;
             int64_t cost = 0;
             for (int64_t left = strips; left > 0; left -= batch)
                 cost += (std::min(left, batch) + teams - 1) / teams * steps;
@@ -836,8 +868,9 @@ bool matvec_shape(MatvecArgs* a, int group, MatvecShape* shape) {
             a->team = team;
             a->cluster = cluster;
             a->batch = int32_t(batch);
+            shape->run = two == one ? 2 : 1;
             shape->grid = unsigned(groups * cluster);
-            shape->smem = kWarps * kStages * block_bytes(group) + int(pitch) * a->tokens
+            shape->smem = fifo + int(pitch) * a->tokens
                           + (joins ? int(batch) * 512 * tiles * team : 0);
         }
     }
@@ -905,8 +938,12 @@ extern "C" rr_status rr_matvec(const rr_quant* q, const void* packed, const void
                 if (a.tokens == 1) return rr_fail(RR_ELAYOUT, "rows of %lld columns", (long long)q->cols);
                 a.tokens = (a.tokens + 1) / 2;
             }
-            const cudaError_t e = a.tokens > 8 ? launch_matvec(rr_matvec_kernel<T, G, 2>, a, shape, stream)
-                                               : launch_matvec(rr_matvec_kernel<T, G, 1>, a, shape, stream);
+            const cudaError_t e =
+                a.tokens > 8
+                    ? shape.run == 2 ? launch_matvec(rr_matvec_kernel<T, G, 2, 2>, a, shape, stream)
+                                     : launch_matvec(rr_matvec_kernel<T, G, 2, 1>, a, shape, stream)
+                    : shape.run == 2 ? launch_matvec(rr_matvec_kernel<T, G, 1, 2>, a, shape, stream)
+                                     : launch_matvec(rr_matvec_kernel<T, G, 1, 1>, a, shape, stream);
             if (e != cudaSuccess) return cuda_fail(e, "rr_matvec");
         }
         return RR_OK;
