@@ -653,7 +653,7 @@ typedef struct {
     int32_t n_experts;                /* 1 .. 512: rows of the router                    */
     int32_t first_expert, n_local;    /* the experts held here, within 0 .. n_experts    */
     int32_t top_k;                    /* 1 .. 16, at most n_experts                      */
-    int64_t hidden, inter;            /* 1 .. 65536 each                                 */
+    int64_t hidden, inter;            /* 1 .. 32768 and 1 .. 16384                       */
     int32_t dtype;                    /* rr_dst_dtype                                    */
     int32_t group;                    /* 0, or 32, 64, 128                               */
     int32_t norm_topk;                /* 0 or 1                                          */

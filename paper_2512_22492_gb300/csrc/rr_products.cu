@@ -234,25 +234,29 @@ struct Stage {
     static constexpr int kBytes = U * kBlockBytes;
     static constexpr int kStages = 6 / U;
     // from: the block's codes at this lane's run; scales: at this lane's (< 8) scales.
+    static __device__ __forceinline__ void copy(uint32_t to, const char* from, const char* scales, int lane) {
+        copy_async<16>(to + 16 * lane, from);
+        copy_async<16>(to + 512 + 16 * lane, from + 512);
+        if (lane < 8) copy_async<kScale>(to + kCodes + kScale * lane, scales);
+    }
     static __device__ __forceinline__ void load(uint32_t to, const char* from, const char* scales, int blocks,
                                                 int lane) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (u > 0 && blocks <= u) break;
-            copy_async<16>(to + u * kBlockBytes + 16 * lane, from + u * kBlockBytes);
-            copy_async<16>(to + u * kBlockBytes + 512 + 16 * lane, from + u * kBlockBytes + 512);
-            if (lane < 8) copy_async<kScale>(to + u * kBlockBytes + kCodes + kScale * lane, scales + u * kBlockBytes);
+            copy(to + u * kBlockBytes, from + u * kBlockBytes, scales + u * kBlockBytes, lane);
         }
         copy_commit();
     }
 };
 
 // sum += W x over one block of 128 columns.  x[n]: this lane's 16 bytes of its
-// token's row at the block's first column, in shared memory.  Groups are summed
-// in the matrix unit and scaled in float32.
-template <class T, int G, int NT>
+// token's row at the block's first column, in shared memory (with PARTS 2, the
+// element is the sum of that and one `apart` bytes on).  Groups are summed in the
+// matrix unit and scaled in float32.
+template <class T, int G, int NT, int PARTS = 1>
 __device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* stage, const char* const (&x)[NT],
-                                              int at, int lane) {
+                                              int at, int lane, int apart = 0) {
     const int g = lane >> 2;
     const uint4 lo = *reinterpret_cast<const uint4*>(stage + 16 * lane);
     const uint4 hi = *reinterpret_cast<const uint4*>(stage + 512 + 16 * lane);
@@ -273,6 +277,11 @@ __device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* s
             if (32 * j % G == 0) mma_first<T>(part[n], al[0], ah[0], al[1], ah[1], v.x, v.y);
             else mma<T>(part[n], al[0], ah[0], al[1], ah[1], v.x, v.y);
             mma<T>(part[n], al[2], ah[2], al[3], ah[3], v.z, v.w);
+            if (PARTS == 2) {
+                const uint4 r = *reinterpret_cast<const uint4*>(x[n] + apart + at + 64 * j);
+                mma<T>(part[n], al[0], ah[0], al[1], ah[1], r.x, r.y);
+                mma<T>(part[n], al[2], ah[2], al[3], ah[3], r.z, r.w);
+            }
         }
         if (32 * (j + 1) % G == 0) {
             const float sl = T::widen(uint16_t(s[32 * j / G])), sh = T::widen(uint16_t(s[32 * j / G] >> 16));
@@ -468,7 +477,17 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
 // Mixture of experts
 // ---------------------------------------------------------------------------
 
-constexpr int kMaxExperts = 512, kMaxTopK = 16, kMaxInner = 65536;
+constexpr int kMaxExperts = 512, kMaxTopK = 16, kMaxHidden = 32768, kMaxInter = 16384;
+constexpr int kMaxPairs = RR_MOE_MAX_TOKENS * kMaxTopK;
+constexpr int kJoinBytes = 24 * 1024;   // shared memory of the teams' sums
+constexpr int kSmem = 227 * 1024;
+
+// The workspace's control block.
+struct MoeControl {
+    uint32_t error;        // a wait ran out: calls do nothing until rr_moe_check
+    uint32_t barrier[3];   // blocks that have arrived
+    uint32_t left;         // blocks that have finished
+};
 
 struct MoeArgs {
     const uint16_t* router;
@@ -478,32 +497,116 @@ struct MoeArgs {
     uint16_t* out;
     int32_t* ids;
     float* weights;
-    // Workspace.
+    MoeControl* control;
     float* logits;     // [tokens, n_experts]
-    int32_t* chosen;   // [tokens, top_k]
-    float* c;          // [tokens, top_k]
-    float* h;          // [tokens * top_k, inter]
+    float* h;          // [pairs, inter]: silu(gate) * up, by expert, then token
+    float* y;          // [pairs, hidden]: each pair's product with w2
     int32_t tokens, n_experts, first, n_local, top_k, norm, hidden, inter;
-    Packed m13, m2;
+    int32_t x_vec, r_vec;      // rows of x, of the router can be read 16 bytes at a time
+    int32_t cap;               // tokens of a pass: at most 16
+    int32_t x_pitch, h_pitch;  // bytes between tokens in shared memory
 };
 
-// A matrix element, whatever the form it is stored in.
-template <class T, int G>
-__device__ float element(const char* base, const Packed& m, int64_t mat, int64_t row, int64_t col) {
-    if (G == 0)
-        return T::widen(reinterpret_cast<const uint16_t*>(base)[(mat * m.rows + row) * m.cols + col]);
-    const int64_t i = m.pair && row >= m.rows / 2 ? row - m.rows / 2 : row;
-    const int64_t strip = m.pair ? i / 8 : i / 16;
-    const int half = m.pair ? row >= m.rows / 2 : (i / 8) & 1, g = i & 7;
-    const int c = col % kBlock, j = c / 32, t = c % 32 / 8;
-    constexpr int kGroup = G ? G : 128;
-    const char* const from =
-        base + mat * m.matrix_bytes + (strip * m.blocks + col / kBlock) * block_bytes(kGroup);
-    const uint32_t word =
-        reinterpret_cast<const uint32_t*>(from + 512 * half + 16 * (4 * g + t))[j];
-    const uint16_t s =
-        reinterpret_cast<const uint16_t*>(from + kCodes)[2 * (g * (kBlock / kGroup) + c / kGroup) + half];
-    return T::widen(s) * float(code(word, c % 8));
+// A warp's stages of weights.  W: 0 for 16-bit matrices whose rows start at 16
+// bytes, 1 for others, or the group of packed ones.
+//   0: a block is 64 columns; a lane copies the 16-byte runs that it reads.
+//   1: the 9 runs of 16 bytes that hold a row's 64 columns, wherever they start;
+//      rows 144 bytes apart.  Lanes read the 20 bytes that theirs are in.
+//   Copies end at a row's end, and zeros follow.
+template <int W>
+struct Weights {
+    static constexpr int kCols = 64, kBytes = W ? 16 * 144 : 16 * 128, kStages = 3;
+    const char *lo, *hi;      // the block's first column in rows g, g + 8 (null: no such row)
+    int32_t left;             // bytes from there to the rows' ends
+    __device__ __forceinline__ void seek(const char* base, int64_t mat, const Packed& m, int64_t strip, int b,
+                                         int lane) {
+        const int64_t l = m.row(strip, lane >> 2), h = m.row(strip, 8 + (lane >> 2));
+        const char* const at = base + mat * m.rows * m.cols * 2 + b * (2 * kCols);
+        lo = l < 0 ? nullptr : at + l * m.cols * 2;
+        hi = h < 0 ? nullptr : at + h * m.cols * 2;
+        left = int32_t(2 * (m.cols - int64_t(b) * kCols));
+    }
+    __device__ __forceinline__ void skip(int blocks) {
+        if (lo) lo += blocks * (2 * kCols);
+        if (hi) hi += blocks * (2 * kCols);
+        left -= blocks * (2 * kCols);
+    }
+    __device__ __forceinline__ void load(uint32_t to, const char* base, int lane) const {
+        const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const char* const row = half ? hi : lo;
+            const int bytes = row ? left : 0;
+            if (W == 0) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int at = 64 * j + 16 * t;
+                    copy_async_cut(to + 1024 * half + 512 * j + 16 * lane, at < bytes ? row + at : base,
+                                   max(0, min(16, bytes - at)));
+                }
+            } else {
+                const int shift = int(reinterpret_cast<uintptr_t>(row) & 15);
+#pragma unroll
+                for (int j = 0; j < 3; ++j) {
+                    const int at = 16 * (4 * j + t) - shift;
+                    if (j < 2 || t == 0)
+                        copy_async_cut(to + 144 * (8 * half + g) + 64 * j + 16 * t, at < bytes ? row + at : base,
+                                       max(0, min(16, bytes - at)));
+                }
+            }
+        }
+    }
+    // The 4 words of this lane's columns 32 j + 8 t + 0..7 of row g + 8 half.
+    static __device__ __forceinline__ uint4 read(const char* stage, int half, int j, int shift, int lane) {
+        if (W == 0) return *reinterpret_cast<const uint4*>(stage + 1024 * half + 512 * j + 16 * lane);
+        const uint32_t* const p = reinterpret_cast<const uint32_t*>(
+            stage + 144 * (8 * half + (lane >> 2)) + 64 * j + 16 * (lane & 3) + (shift & 12));
+        const uint32_t w0 = p[0], w1 = p[1], w2 = p[2], w3 = p[3], w4 = shift & 2 ? p[4] : 0;
+        const uint32_t pick = shift & 2 ? 0x5432 : 0x3210;
+        return make_uint4(__byte_perm(w0, w1, pick), __byte_perm(w1, w2, pick), __byte_perm(w2, w3, pick),
+                          __byte_perm(w3, w4, pick));
+    }
+};
+
+template <int G>
+struct PackedWeights {
+    using S = Stage<G, 1>;
+    static constexpr int kCols = kBlock, kBytes = S::kBytes, kStages = S::kStages;
+    const char* from;
+    __device__ __forceinline__ void seek(const char* base, int64_t mat, const Packed& m, int64_t strip, int b,
+                                         int lane) {
+        from = base + mat * m.matrix_bytes + (strip * m.blocks + b) * kBytes + 16 * lane;
+    }
+    __device__ __forceinline__ void skip(int blocks) { from += int64_t(blocks) * kBytes; }
+    __device__ __forceinline__ void load(uint32_t to, const char*, int lane) const {
+        S::copy(to, from, from + (kCodes + (S::kScale - 16) * lane), lane);
+    }
+};
+template <> struct Weights<32> : PackedWeights<32> {};
+template <> struct Weights<64> : PackedWeights<64> {};
+template <> struct Weights<128> : PackedWeights<128> {};
+
+// sum += W x over one block, x in PARTS 16-bit parts `apart` bytes from one another.
+template <class T, int W, int NT, int PARTS>
+__device__ __forceinline__ void moe_block(float (&sum)[NT][4], const char* stage, const char* const (&x)[NT],
+                                          int apart, int at, int shift_lo, int shift_hi, int lane) {
+    if constexpr (W >= 32) {
+        block_product<T, W, NT, PARTS>(sum, stage, x, at, lane, apart);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint4 l = Weights<W>::read(stage, 0, j, shift_lo, lane);
+            const uint4 h = Weights<W>::read(stage, 1, j, shift_hi, lane);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(x[n] + p * apart + at + 64 * j);
+                    mma<T>(sum[n], l.x, h.x, l.y, h.y, v.x, v.y);
+                    mma<T>(sum[n], l.z, h.z, l.w, h.w, v.z, v.w);
+                }
+        }
+    }
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -511,98 +614,509 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-template <class T>
-__global__ void __launch_bounds__(128) rr_moe_logits_kernel(const MoeArgs a) {
-    const int lane = threadIdx.x & 31;
-    const int i = blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (i >= a.tokens * a.n_experts) return;
-    const int t = i / a.n_experts, e = i % a.n_experts;
-    float sum = 0.0f;
-    for (int k = lane; k < a.hidden; k += 32)
-        sum = fmaf(T::widen(a.x[t * a.ldx + k]), T::widen(a.router[int64_t(e) * a.hidden + k]), sum);
-    sum = warp_sum(sum);
-    if (lane == 0) a.logits[i] = sum;
-}
-
-// Descending order of logits as unsigned integers: NaN first, +0 and -0 alike.
+// Descending order of logits as unsigned integers: NaN first, +0 and -0 alike; 0
+// is below all of them.
 __device__ __forceinline__ uint32_t rank_key(float l) {
     if (isnan(l)) return ~0u;
     const uint32_t b = __float_as_uint(l + 0.0f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(32) rr_moe_choose_kernel(const MoeArgs a) {
-    __shared__ uint32_t key[kMaxExperts];
-    const int t = blockIdx.x, lane = threadIdx.x;
-    const float* const l = a.logits + t * a.n_experts;
+// What every block works out for itself from the logits.
+struct MoeTables {
+    uint32_t mask[2][kMaxExperts];     // the tokens of a local expert
+    float c[kMaxPairs];                // by token and rank
+    int16_t chosen[kMaxPairs];
+    uint16_t first[kMaxExperts];       // a local expert's first pair
+    uint16_t pass_expert[kMaxPairs], pass_first[kMaxPairs];
+    uint8_t pass_count[kMaxPairs];
+    uint8_t token[kMaxPairs];          // of a pair
+    float scale[16];                   // of the pass's tokens' h (float16)
+    uint32_t scan[kWarps];
+    uint32_t total;                    // pairs << 16 | passes
+    uint32_t stop;
+};
+
+// The sum of router row e with up to N tokens' rows from t0.
+template <class T, int N>
+__device__ __forceinline__ void logit_item(const MoeArgs& a, int e, int t0, int n, int lane) {
+    const uint16_t* const r = a.router + int64_t(e) * a.hidden;
+    const uint16_t* const x = a.x + t0 * a.ldx;
+    float sum[N] = {};
+    if (a.x_vec && a.r_vec) {
+#pragma unroll 8 / N
+        for (int k = 8 * lane; k < a.hidden; k += 256) {
+            const uint4 w = *reinterpret_cast<const uint4*>(r + k);
+            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (i >= n) break;
+                const uint4 v = *reinterpret_cast<const uint4*>(x + i * a.ldx + k);
+                const uint32_t vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    sum[i] = fmaf(T::widen(uint16_t(vv[q])), T::widen(uint16_t(ww[q])), sum[i]);
+                    sum[i] = fmaf(T::widen(uint16_t(vv[q] >> 16)), T::widen(uint16_t(ww[q] >> 16)), sum[i]);
+                }
+            }
+        }
+    } else {
+#pragma unroll 4
+        for (int k = lane; k < a.hidden; k += 32) {
+            const float w = T::widen(r[k]);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < n) sum[i] = fmaf(T::widen(x[i * a.ldx + k]), w, sum[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float s = warp_sum(sum[i]);
+        if (lane == 0 && i < n) a.logits[(t0 + i) * a.n_experts + e] = s;
+    }
+}
+
+// One warp: token t's softmax and its top_k experts.
+__device__ __forceinline__ void choose(const MoeArgs& a, MoeTables& tab, int t, int lane) {
+    constexpr int kEach = kMaxExperts / 32;
+    float l[kEach];
+    uint32_t key[kEach];
     float top = -INFINITY;
-    for (int e = lane; e < a.n_experts; e += 32) {
-        key[e] = rank_key(l[e]);
-        top = fmaxf(top, l[e]);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int e = 32 * i + lane;
+        l[i] = e < a.n_experts ? __ldcg(a.logits + t * a.n_experts + e) : 0.0f;
+        key[i] = e < a.n_experts ? rank_key(l[i]) : 0;
+        if (e < a.n_experts) top = fmaxf(top, l[i]);
     }
     for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
     float sum = 0.0f;
-    for (int e = lane; e < a.n_experts; e += 32) sum += expf(l[e] - top);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (32 * i + lane < a.n_experts) sum += expf(l[i] - top);
     sum = warp_sum(sum);
-    __syncwarp();
     float mine = 0.0f, total = 0.0f;
     int my_id = 0;
     for (int j = 0; j < a.top_k; ++j) {
-        unsigned long long best = 0;   // (key, lowest index first)
-        for (int e = lane; e < a.n_experts; e += 32)
-            if (key[e])
-                best = max(best, (unsigned long long)key[e] << 32 | uint32_t(~e));
-        for (int o = 16; o; o /= 2) best = max(best, __shfl_xor_sync(~0u, best, o));
-        const int e = int(~uint32_t(best));
-        const float p = expf(l[e] - top) / sum;
+        uint32_t best = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) best = max(best, key[i]);
+        best = __reduce_max_sync(~0u, best);
+        uint32_t at = ~0u;
+        float lv = 0.0f;
+#pragma unroll
+        for (int i = kEach - 1; i >= 0; --i)
+            if (key[i] == best) at = 32 * i + lane, lv = l[i];
+        const uint32_t e = __reduce_min_sync(~0u, at);
+        lv = __shfl_sync(~0u, lv, e & 31);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (32 * i + lane == int(e)) key[i] = 0;
+        const float p = expf(lv - top) / sum;
         total += p;
-        if (lane == j) mine = p, my_id = e;
-        __syncwarp();
-        if (lane == e % 32) key[e] = 0;
-        __syncwarp();
+        if (lane == j) mine = p, my_id = int(e);
     }
     if (lane < a.top_k) {
+        const int i = t * a.top_k + lane;
         if (a.norm) mine /= total;
-        a.chosen[t * a.top_k + lane] = my_id;
-        a.c[t * a.top_k + lane] = mine;
-        if (a.ids) a.ids[t * a.top_k + lane] = my_id;
-        if (a.weights) a.weights[t * a.top_k + lane] = mine;
+        tab.chosen[i] = int16_t(my_id);
+        tab.c[i] = mine;
+        const int local = my_id - a.first;
+        if (local >= 0 && local < a.n_local) atomicOr(&tab.mask[t >> 5][local], 1u << (t & 31));
+        if (blockIdx.x == 0) {
+            if (a.ids) a.ids[i] = my_id;
+            if (a.weights) a.weights[i] = mine;
+        }
     }
 }
 
-template <class T, int G>
-__global__ void __launch_bounds__(128) rr_moe_up_kernel(const MoeArgs a) {
-    const int lane = threadIdx.x & 31;
-    const int i = blockIdx.x * 4 + (threadIdx.x >> 5), p = blockIdx.y;
-    const int e = a.chosen[p] - a.first;
-    if (i >= a.inter || e < 0 || e >= a.n_local) return;
-    const uint16_t* const x = a.x + p / a.top_k * a.ldx;
-    float gate = 0.0f, up = 0.0f;
-    for (int k = lane; k < a.hidden; k += 32) {
-        const float v = T::widen(x[k]);
-        gate = fmaf(v, element<T, G>(a.w13, a.m13, e, i, k), gate);
-        up = fmaf(v, element<T, G>(a.w13, a.m13, e, a.inter + i, k), up);
+// Waits until every block has arrived; false when the wait ran out (about two
+// seconds), which marks the workspace.
+__device__ bool grid_barrier(const MoeArgs& a, MoeTables& tab, int which) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t* const b = &a.control->barrier[which];
+        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(b) : "memory");
+        uint32_t seen = 0;
+        long long since = 0;
+        for (;;) {
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(b) : "memory");
+            if (seen >= gridDim.x) break;
+            long long now;
+            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+            if (since == 0) since = now;
+            if (now - since > 2000000000ll) {
+                atomicExch(&a.control->error, 1u);
+                tab.stop = 1;
+                break;
+            }
+        }
     }
-    gate = warp_sum(gate);
-    up = warp_sum(up);
-    if (lane == 0) a.h[int64_t(p) * a.inter + i] = silu(gate) * up;
+    __syncthreads();
+    return tab.stop == 0;
 }
 
-template <class T, int G>
-__global__ void __launch_bounds__(128) rr_moe_down_kernel(const MoeArgs a) {
-    const int lane = threadIdx.x & 31;
-    const int n = blockIdx.x * 4 + (threadIdx.x >> 5), t = blockIdx.y;
-    if (n >= a.hidden) return;
-    float y = 0.0f;
-    for (int j = 0; j < a.top_k; ++j) {
-        const int p = t * a.top_k + j, e = a.chosen[p] - a.first;
-        if (e < 0 || e >= a.n_local) continue;
+// One of the two products: a run of (pass, strip) items per block.
+struct MoePhase {
+    const char* base;
+    Packed m;
+    int blocks;            // of a strip
+    int f0, n;             // this block's items: pass f / strips, strip f % strips
+    int team, batch;
+    // Items between two joins, all of one pass.
+    __device__ __forceinline__ int batch_end(int i0) const {
+        const int strips = int(m.strips), f = f0 + i0;
+        return min(min(i0 + batch, n), (f / strips + 1) * strips - f0);
+    }
+};
+
+// The order in which a warp takes a phase's blocks of weights.
+template <int W>
+struct Feed {
+    Weights<W> w;
+    int phase, i, i1, b;
+    // The next item of this warp from batch i0 on; moves to the next phase at the end.
+    __device__ __forceinline__ void find(const MoePhase* ph, const MoeTables& tab, int i0, int warp, int lane) {
+        while (phase < 2) {
+            const MoePhase& p = ph[phase];
+            const int part = warp % p.team, team = warp / p.team;
+            if (part < p.blocks) {
+                while (i0 < p.n) {
+                    i1 = p.batch_end(i0);
+                    i = i0 + team;
+                    if (i < i1) {
+                        aim(p, tab, part, lane);
+                        return;
+                    }
+                    i0 = i1;
+                }
+            }
+            ++phase;
+            i0 = 0;
+        }
+    }
+    __device__ __forceinline__ void aim(const MoePhase& p, const MoeTables& tab, int part, int lane) {
+        const int strips = int(p.m.strips), f = p.f0 + i;
+        b = part;
+        w.seek(p.base, tab.pass_expert[f / strips], p.m, f % strips, b, lane);
+    }
+    __device__ __forceinline__ void load(const MoePhase* ph, const MoeTables& tab, uint32_t to, int warp, int lane) {
+        if (phase < 2) {
+            const MoePhase& p = ph[phase];
+            w.load(to, p.base, lane);
+            b += p.team;
+            if (b < p.blocks) {
+                w.skip(p.team);
+            } else {
+                i += kWarps / p.team;
+                if (i < i1) aim(p, tab, warp % p.team, lane);
+                else find(ph, tab, i1, warp, lane);
+            }
+        }
+        copy_commit();
+    }
+};
+
+// Tokens' rows (16-bit) of a pass to shared memory, zero-filled to whole blocks.
+__device__ __forceinline__ void stage_tokens(const MoeArgs& a, const MoeTables& tab, char* to, int first, int count,
+                                             int cols) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i = warp; i < count * 4; i += kWarps) {      // four warps' shares of a row each
+        const uint16_t* const row = a.x + tab.token[first + i / 4] * a.ldx;
+        char* const dst = to + i / 4 * a.x_pitch;
+        if (a.x_vec) {
+#pragma unroll 4
+            for (int c = 8 * (32 * (i % 4) + lane); c < cols; c += 1024) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (c + 8 <= a.hidden) {
+                    v = *reinterpret_cast<const uint4*>(row + c);
+                } else if (c < a.hidden) {
+                    uint32_t p[4] = {0, 0, 0, 0};
+                    for (int k = 0; c + k < a.hidden; ++k) p[k / 2] |= uint32_t(row[c + k]) << (16 * (k % 2));
+                    v = make_uint4(p[0], p[1], p[2], p[3]);
+                }
+                *reinterpret_cast<uint4*>(dst + 2 * c) = v;
+            }
+        } else {
+#pragma unroll 4
+            for (int c = 32 * (i % 4) + lane; c < cols; c += 128)
+                *reinterpret_cast<uint16_t*>(dst + 2 * c) = c < a.hidden ? row[c] : uint16_t(0);
+        }
+    }
+}
+
+// A pass's h as two 16-bit parts, v = hi + lo to 2^-16 of v: the product then
+// keeps what float32 h would give, at twice the matrix instructions, which are
+// not what bounds it.  float16 parts are of v times a power of two that brings the
+// token's largest finite element to 2^14..2^15, so that none overflows and what
+// underflows is below 2^-39 of the largest.
+template <class T>
+__device__ __forceinline__ void stage_h(const MoeArgs& a, MoeTables& tab, char* to, int first, int count, int cols) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i = warp; i < count; i += kWarps) {
+        const float* const row = a.h + int64_t(first + i) * a.inter;
+        float up = 1.0f;
+        if (std::is_same<T, F16>::value) {
+            float top = 0.0f;
+#pragma unroll 8
+            for (int c = lane; c < a.inter; c += 32) {
+                const float v = fabsf(__ldcg(row + c));
+                if (v < INFINITY) top = fmaxf(top, v);
+            }
+            for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+            const int e = top > 0.0f ? max(-100, min(100, 14 - ilogbf(top))) : 0;
+            up = ldexpf(1.0f, e);
+            if (lane == 0) tab.scale[i] = ldexpf(1.0f, -e);
+        }
+        char* const dst = to + i * a.h_pitch;
+        char* const low = dst + a.cap * a.h_pitch;
+#pragma unroll 8
+        for (int c = lane; c < cols; c += 32) {
+            const float v = c < a.inter ? __ldcg(row + c) * up : 0.0f;
+            const uint16_t hi = T::round(v);
+            const float rest = v - T::widen(hi);
+            reinterpret_cast<uint16_t*>(dst)[c] = hi;
+            // (An infinite v has no rest; one just under the largest may round to
+            // infinity in bfloat16, as the result then does.)
+            reinterpret_cast<uint16_t*>(low)[c] = T::round(isfinite(rest) ? rest : 0.0f);
+        }
+    }
+}
+
+// One pass's strips [i0, i1) of a phase.  NT: groups of 8 tokens.  The first phase
+// ends in silu(gate) * up, the second in the pair's part of the output.
+template <class T, int W, int NT, int PHASE>
+__device__ __forceinline__ void moe_batch(const MoeArgs& a, const MoePhase* ph, const MoeTables& tab, Feed<W>& feed,
+                                          char* fifo, int& slot, const char* region, float4* red, int i0, int i1,
+                                          int first, int count) {
+    constexpr int kParts = PHASE == 0 ? 1 : 2, kStages = Weights<W>::kStages, kBytes = Weights<W>::kBytes;
+    const MoePhase& p = ph[PHASE];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int team = warp / p.team, part = warp % p.team, teams = kWarps / p.team;
+    const int pitch = PHASE == 0 ? a.x_pitch : a.h_pitch;
+    const uint32_t fifo_at = smem_at(fifo);
+    const char* x[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) x[n] = region + min(8 * n + g, count - 1) * pitch + 16 * t;
+
+    auto put_item = [&](int i, int ln, int n, const float (&v)[4]) {
+        const int strip = (p.f0 + i) % int(p.m.strips);
+        const int64_t lo = p.m.row(strip, ln >> 2), hi = p.m.row(strip, 8 + (ln >> 2));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int tok = 8 * n + 2 * (ln & 3) + k;
+            if (tok >= count) continue;
+            if (PHASE == 0) {
+                if (lo >= 0) __stcg(a.h + int64_t(first + tok) * a.inter + lo, silu(v[k]) * v[2 + k]);
+            } else {
+                const float s = std::is_same<T, F16>::value ? tab.scale[tok] : 1.0f;
+                float* const y = a.y + int64_t(first + tok) * a.hidden;
+                if (lo >= 0) __stcg(y + lo, v[k] * s);
+                if (hi >= 0) __stcg(y + hi, v[2 + k] * s);
+            }
+        }
+    };
+
+    for (int i = i0 + team; i < i1; i += teams) {
+        float sum[NT][4] = {};
+        int shift_lo = 0, shift_hi = 0;
+        if constexpr (W == 1) {
+            const int f = p.f0 + i, strips = int(p.m.strips);
+            Weights<1> w;
+            w.seek(p.base, tab.pass_expert[f / strips], p.m, f % strips, 0, lane);
+            shift_lo = int(reinterpret_cast<uintptr_t>(w.lo) & 15);
+            shift_hi = int(reinterpret_cast<uintptr_t>(w.hi) & 15);
+        }
+        for (int b = part; b < p.blocks; b += p.team) {
+            copy_wait<kStages - 2>();
+            __syncwarp();      // what lanes share is there, and the last stage has been read
+            feed.load(ph, tab, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
+            moe_block<T, W, NT, kParts>(sum, fifo + slot * kBytes, x, a.cap * a.h_pitch,
+                                        b * (2 * Weights<W>::kCols), shift_lo, shift_hi, lane);
+            slot = slot + 1 == kStages ? 0 : slot + 1;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (p.team == 1) put_item(i, lane, n, sum[n]);
+            else
+                red[((part * p.batch + i - i0) * NT + n) * 32 + lane] =
+                    make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
+        }
+    }
+    if (p.team == 1) return;
+    __syncthreads();
+    for (int k = threadIdx.x; k < (i1 - i0) * NT * 32; k += kProdThreads) {
+        float v[4] = {};
+        for (int q = 0; q < p.team; ++q) {
+            const float4 f = red[q * p.batch * NT * 32 + k];
+            v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+        }
+        put_item(i0 + k / (NT * 32), k & 31, k / 32 % NT, v);
+    }
+    __syncthreads();
+}
+
+template <class T, int W, int PHASE>
+__device__ __forceinline__ void moe_phase(const MoeArgs& a, const MoePhase* ph, MoeTables& tab, Feed<W>& feed,
+                                          char* fifo, int& slot, char* region, float4* red) {
+    const MoePhase& p = ph[PHASE];
+    int staged = -1;
+    for (int i0 = 0; i0 < p.n;) {
+        const int i1 = p.batch_end(i0), pass = (p.f0 + i0) / int(p.m.strips);
+        const int first = tab.pass_first[pass], count = tab.pass_count[pass];
+        if (pass != staged) {
+            __syncthreads();
+            if (PHASE == 0) stage_tokens(a, tab, region, first, count, p.blocks * Weights<W>::kCols);
+            else stage_h<T>(a, tab, region, first, count, p.blocks * Weights<W>::kCols);
+            __syncthreads();
+            staged = pass;
+        }
+        if (count <= 8) moe_batch<T, W, 1, PHASE>(a, ph, tab, feed, fifo, slot, region, red, i0, i1, first, count);
+        else moe_batch<T, W, 2, PHASE>(a, ph, tab, feed, fifo, slot, region, red, i0, i1, first, count);
+        i0 = i1;
+    }
+}
+
+// The whole layer in one cooperative launch, one block per SM:
+//   logits, a warp per expert row and 8 tokens          | barrier
+//   every block: softmax, choice, the experts' tokens
+//   gate and up of every chosen expert, silu             | barrier
+//   down                                                 | barrier
+//   each token's weighted sum
+// Bound by HBM: each chosen expert's weights are read once per 16 tokens.  Blocks
+// take equal runs of (pass, strip of 16 rows) items; warps stream weights through
+// stages that already fill with the next phase's while the blocks wait.
+template <class T, int W>
+__global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_constant__ MoeArgs a) {
+    extern __shared__ __align__(128) char smem[];
+    constexpr int kFifo = kWarps * Weights<W>::kStages * Weights<W>::kBytes;
+    __shared__ MoePhase ph[2];
+    MoeTables& tab = *reinterpret_cast<MoeTables*>(smem + kFifo + kJoinBytes);
+    char* const region = smem + kFifo + kJoinBytes + (sizeof(MoeTables) + 127) / 128 * 128;
+    float4* const red = reinterpret_cast<float4*>(smem + kFifo);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+
+    if (threadIdx.x == 0) {
+        uint32_t e;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(e) : "l"(&a.control->error) : "memory");
+        tab.stop = e;
+    }
+    for (int i = threadIdx.x; i < a.n_local; i += kProdThreads) tab.mask[0][i] = tab.mask[1][i] = 0;
+    __syncthreads();
+    if (tab.stop) return;
+
+    // Logits.
+    {
+        const int each = a.tokens == 1 ? 1 : a.tokens <= 4 ? 4 : 8;
+        const int groups = (a.tokens + each - 1) / each;
+        for (int i = warp * gridDim.x + blockIdx.x; i < a.n_experts * groups; i += kWarps * gridDim.x) {
+            const int e = i % a.n_experts, t0 = i / a.n_experts * each, n = min(each, a.tokens - t0);
+            if (each == 1) logit_item<T, 1>(a, e, t0, n, lane);
+            else if (each == 4) logit_item<T, 4>(a, e, t0, n, lane);
+            else logit_item<T, 8>(a, e, t0, n, lane);
+        }
+    }
+    if (!grid_barrier(a, tab, 0)) return;
+
+    for (int t = warp; t < a.tokens; t += kWarps) choose(a, tab, t, lane);
+    __syncthreads();
+    // Pairs by expert, then token; passes of up to `cap` tokens of one expert.
+    {
+        const int e = threadIdx.x;
+        const uint32_t m0 = e < a.n_local ? tab.mask[0][e] : 0, m1 = e < a.n_local ? tab.mask[1][e] : 0;
+        const int count = __popc(m0) + __popc(m1), passes = (count + a.cap - 1) / a.cap;
+        uint32_t v = uint32_t(count) << 16 | uint32_t(passes);
+        const uint32_t own = v;
+        for (int o = 1; o < 32; o *= 2) {
+            const uint32_t u = __shfl_up_sync(~0u, v, o);
+            if (lane >= o) v += u;
+        }
+        if (lane == 31) tab.scan[warp] = v;
+        __syncthreads();
+        uint32_t before = 0;
+        for (int q = 0; q < warp; ++q) before += tab.scan[q];
+        v += before;
+        if (threadIdx.x == kProdThreads - 1) tab.total = v;
+        v -= own;
+        int pair = int(v >> 16), pass = int(v & 0xFFFF);
+        if (e < a.n_local) tab.first[e] = uint16_t(pair);
+        for (int q = 0; q < passes; ++q, ++pass) {
+            tab.pass_expert[pass] = uint16_t(e);
+            tab.pass_first[pass] = uint16_t(pair + q * a.cap);
+            tab.pass_count[pass] = uint8_t(min(a.cap, count - q * a.cap));
+        }
+        for (uint32_t m = m0; m; m &= m - 1) tab.token[pair++] = uint8_t(__ffs(m) - 1);
+        for (uint32_t m = m1; m; m &= m - 1) tab.token[pair++] = uint8_t(31 + __ffs(m));
+        __syncthreads();
+    }
+    // The phases' items, and the team of the fewest rounds (a join costs one).
+    if (threadIdx.x < 2) {
+        const int k = threadIdx.x, passes = int(tab.total & 0xFFFF);
+        MoePhase p;
+        p.base = k ? a.w2 : a.w13;
+        p.m.rows = k ? a.hidden : 2 * a.inter;
+        p.m.cols = k ? a.inter : a.hidden;
+        p.m.pair = !k;
+        p.m.strips = k ? (a.hidden + 15) / 16 : (a.inter + 7) / 8;
+        p.m.blocks = (p.m.cols + kBlock - 1) / kBlock;
+        p.m.matrix_bytes = p.m.strips * p.m.blocks * block_bytes(W >= 32 ? W : 128);
+        p.blocks = int(p.m.cols + Weights<W>::kCols - 1) / Weights<W>::kCols;
+        const int all = passes * int(p.m.strips), grid = gridDim.x;      // under 2^31: 1024 passes of 2048 strips
+        p.f0 = int(int64_t(blockIdx.x) * all / grid);
+        p.n = int(int64_t(blockIdx.x + 1) * all / grid) - p.f0;
+        const int most = (all + grid - 1) / grid;
+        int best = INT_MAX;
+        for (int team = 1; team <= kWarps; team *= 2) {
+            const int teams = kWarps / team;
+            const int batch = team == 1 ? INT_MAX / 2 : kJoinBytes / (512 * (a.tokens > 8 ? 2 : 1) * team) / teams * teams;
+            const int steps = (p.blocks + team - 1) / team;
+            const int cost = (most + teams - 1) / teams * steps + (team == 1 ? 0 : (most + batch - 1) / batch);
+            if (cost < best) best = cost, p.team = team, p.batch = batch;
+        }
+        ph[k] = p;
+    }
+    __syncthreads();
+
+    char* const fifo = smem + warp * (Weights<W>::kStages * Weights<W>::kBytes);
+    int slot = 0;
+    Feed<W> feed;
+    feed.phase = 0;
+    feed.find(ph, tab, 0, warp, lane);
+    for (int i = 0; i < Weights<W>::kStages - 1; ++i)
+        feed.load(ph, tab, smem_at(fifo) + i * Weights<W>::kBytes, warp, lane);
+
+    moe_phase<T, W, 0>(a, ph, tab, feed, fifo, slot, region, red);
+    if (!grid_barrier(a, tab, 1)) {
+        copy_wait<0>();
+        return;
+    }
+    moe_phase<T, W, 1>(a, ph, tab, feed, fifo, slot, region, red);
+    copy_wait<0>();
+    if (!grid_barrier(a, tab, 2)) return;
+
+    for (int64_t i = int64_t(blockIdx.x) * kProdThreads + threadIdx.x; i < int64_t(a.tokens) * a.hidden;
+         i += int64_t(gridDim.x) * kProdThreads) {
+        const int t = int(i / a.hidden), n = int(i % a.hidden);
         float sum = 0.0f;
-        for (int k = lane; k < a.inter; k += 32)
-            sum = fmaf(a.h[int64_t(p) * a.inter + k], element<T, G>(a.w2, a.m2, e, n, k), sum);
-        y += a.c[p] * warp_sum(sum);
+#pragma unroll 8
+        for (int j = 0; j < a.top_k; ++j) {
+            const int e = tab.chosen[t * a.top_k + j] - a.first;
+            if (e < 0 || e >= a.n_local) continue;
+            const uint32_t m0 = tab.mask[0][e], m1 = tab.mask[1][e];
+            const int before = t < 32 ? __popc(m0 & ((1u << t) - 1)) : __popc(m0) + __popc(m1 & ((1u << (t - 32)) - 1));
+            sum += tab.c[t * a.top_k + j] * __ldcg(a.y + int64_t(tab.first[e] + before) * a.hidden + n);
+        }
+        a.out[t * a.ldo + n] = T::round(sum);
     }
-    if (lane == 0) a.out[t * a.ldo + n] = T::round(y);
+    // The last block to finish leaves the counters at zero for the next call.
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        if (atomicAdd(&a.control->left, 1u) == gridDim.x - 1) {
+            a.control->barrier[0] = a.control->barrier[1] = a.control->barrier[2] = 0;
+            a.control->left = 0;
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -689,8 +1203,9 @@ rr_status check_moe(const rr_moe_layer* L) {
         return rr_fail(RR_ELAYOUT, "experts %d + %d are not within 0..%d", L->first_expert, L->n_local, L->n_experts);
     if (L->top_k < 1 || L->top_k > kMaxTopK || L->top_k > L->n_experts)
         return rr_fail(RR_ELAYOUT, "top_k %d: 1..%d, at most the experts", L->top_k, kMaxTopK);
-    if (L->hidden < 1 || L->hidden > kMaxInner || L->inter < 1 || L->inter > kMaxInner)
-        return rr_fail(RR_ELAYOUT, "hidden %lld, inter %lld: 1..%d", (long long)L->hidden, (long long)L->inter, kMaxInner);
+    if (L->hidden < 1 || L->hidden > kMaxHidden || L->inter < 1 || L->inter > kMaxInter)
+        return rr_fail(RR_ELAYOUT, "hidden %lld, inter %lld: 1..%d and 1..%d", (long long)L->hidden,
+                       (long long)L->inter, kMaxHidden, kMaxInter);
     if (L->dtype != RR_DST_BF16 && L->dtype != RR_DST_F16) return rr_fail(RR_EINVAL, "unknown element type %d", L->dtype);
     if (L->group != 0 && L->group != 32 && L->group != 64 && L->group != 128)
         return rr_fail(RR_ELAYOUT, "group %d: 0, 32, 64 or 128", L->group);
@@ -701,20 +1216,59 @@ rr_status check_moe(const rr_moe_layer* L) {
 
 // Workspace: a control block, then the arrays.  Offsets in bytes.
 struct MoeSpace {
-    int64_t logits, chosen, c, h, total;
+    int64_t logits, h, y, total;
 };
-constexpr int64_t kControlBytes = 256;   // word 0: the error word
+constexpr int64_t kControlBytes = 256;
 
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
 MoeSpace moe_space(const rr_moe_layer* L, int64_t tokens) {
     MoeSpace s;
+    const int64_t pairs = tokens * std::min(L->top_k, L->n_local);
     s.logits = kControlBytes;
-    s.chosen = s.logits + up16(4 * tokens * L->n_experts);
-    s.c = s.chosen + up16(4 * tokens * L->top_k);
-    s.h = s.c + up16(4 * tokens * L->top_k);
-    s.total = s.h + up16(4 * tokens * L->top_k * L->inter);
+    s.h = s.logits + up16(4 * tokens * L->n_experts);
+    s.y = s.h + up16(4 * pairs * L->inter);
+    s.total = s.y + up16(4 * pairs * L->hidden);
     return s;
+}
+
+template <class T, int W>
+rr_status launch_moe(MoeArgs a, cudaStream_t stream) {
+    // Tokens that a pass holds in shared memory, by the longer of the two phases' rows.
+    constexpr int kFixed = kWarps * Weights<W>::kStages * Weights<W>::kBytes + kJoinBytes +
+                           (sizeof(MoeTables) + 127) / 128 * 128 + 1024 /* static */;
+    constexpr int kCols = Weights<W>::kCols;
+    // Rows 64 bytes past a multiple of 128, as for the matrix-vector products.
+    const auto pitch = [](int cols) { return (cols + kCols - 1) / kCols * (2 * kCols) + 64; };
+    a.x_pitch = pitch(a.hidden);
+    a.h_pitch = pitch(a.inter);
+    const int each = std::max(a.x_pitch, 2 * a.h_pitch), room = kSmem - kFixed;
+    a.cap = std::min(16, room / each);
+    if (a.cap > 8 && a.cap < 16) a.cap = 8;
+    a.cap = std::min(a.cap, a.tokens);
+    if (a.cap < 1) return rr_fail(RR_ELAYOUT, "hidden %d, inter %d: rows too long", a.hidden, a.inter);
+    const int smem = kFixed - 1024 + a.cap * each;
+    static std::mutex mutex;
+    static int grids[16] = {};
+    int dev = 0, grid;
+    RR_CUDA(cudaGetDevice(&dev));
+    if (dev < 0 || dev > 15) return rr_fail(RR_EINVAL, "device %d", dev);
+    {
+        const std::lock_guard<std::mutex> lock(mutex);
+        if (!grids[dev]) {
+            int sms = 0, coop = 0;
+            RR_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+            RR_CUDA(cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev));
+            if (!coop) return rr_fail(RR_ECUDA, "the device has no cooperative launches");
+            RR_CUDA(cudaFuncSetAttribute(rr_moe_kernel<T, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem - 1024));
+            grids[dev] = sms;
+        }
+        grid = grids[dev];
+    }
+    void* args[] = {&a};
+    RR_CUDA(cudaLaunchCooperativeKernel((const void*)rr_moe_kernel<T, W>, dim3(unsigned(grid)), dim3(kProdThreads), args,
+                                        size_t(smem), stream));
+    return RR_OK;
 }
 
 }  // namespace
@@ -794,8 +1348,6 @@ struct MatvecShape {
     int smem;
     int run;        // blocks of a stage
 };
-constexpr int kSmem = 227 * 1024;
-constexpr int kJoinBytes = 24 * 1024;   // shared memory of the teams' sums
 
 // Clusters of a size that this GPU runs at once with one block per SM (GB300: 152,
 // 76, 36 and 15 of 1, 2, 4 and 8 blocks, since a cluster stays within one GPC).
@@ -994,10 +1546,10 @@ extern "C" rr_status rr_moe(const rr_moe_layer* L, const void* router, const voi
     a.out = static_cast<uint16_t*>(out);
     a.ids = ids;
     a.weights = weights;
+    a.control = reinterpret_cast<MoeControl*>(ws);
     a.logits = reinterpret_cast<float*>(ws + S.logits);
-    a.chosen = reinterpret_cast<int32_t*>(ws + S.chosen);
-    a.c = reinterpret_cast<float*>(ws + S.c);
     a.h = reinterpret_cast<float*>(ws + S.h);
+    a.y = reinterpret_cast<float*>(ws + S.y);
     a.tokens = n_tokens;
     a.n_experts = L->n_experts;
     a.first = L->first_expert;
@@ -1006,17 +1558,14 @@ extern "C" rr_status rr_moe(const rr_moe_layer* L, const void* router, const voi
     a.norm = L->norm_topk;
     a.hidden = int32_t(L->hidden);
     a.inter = int32_t(L->inter);
-    a.m13 = packed_of(2 * L->inter, L->hidden, L->group, 1);
-    a.m2 = packed_of(L->hidden, L->inter, L->group, 0);
+    a.x_vec = (uintptr_t)x % 16 == 0 && (ldx % 8 == 0 || n_tokens == 1);
+    a.r_vec = L->hidden % 8 == 0;
     return with_group(L->dtype, L->group, [&](auto t, auto g) -> rr_status {
         using T = decltype(t);
         constexpr int G = decltype(g)::value;
-        rr_moe_logits_kernel<T><<<(n_tokens * a.n_experts + 3) / 4, 128, 0, stream>>>(a);
-        rr_moe_choose_kernel<<<n_tokens, 32, 0, stream>>>(a);
-        rr_moe_up_kernel<T, G><<<dim3((a.inter + 3) / 4, n_tokens * a.top_k), 128, 0, stream>>>(a);
-        rr_moe_down_kernel<T, G><<<dim3((a.hidden + 3) / 4, n_tokens), 128, 0, stream>>>(a);
-        RR_CUDA(cudaGetLastError());
-        return RR_OK;
+        if constexpr (G != 0) return launch_moe<T, G>(a, stream);
+        else if (L->hidden % 8 == 0 && L->inter % 8 == 0) return launch_moe<T, 0>(a, stream);
+        else return launch_moe<T, 1>(a, stream);
     });
 }
 
