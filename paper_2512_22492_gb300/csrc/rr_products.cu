@@ -71,84 +71,167 @@ __device__ __forceinline__ int code(uint32_t word, int i) {
     return int((word >> (4 * (i / 2 + 4 * (i % 2)))) & 15u) - 8;
 }
 
+// A block of 128 columns by its number within a stack.
+struct Item {
+    int64_t mat, strip;
+    int b;
+    __device__ __forceinline__ Item(uint32_t i, const Packed& m) {
+        const uint32_t blocks = uint32_t(m.blocks), strips = uint32_t(m.strips);
+        b = int(i % blocks);
+        i /= blocks;
+        strip = i % strips;
+        mat = i / strips;
+    }
+};
+
+// Programmatic dependent launch: the next kernel on the stream may be scheduled
+// while this one runs; each waits for the kernels before it to complete before it
+// touches memory.
+__device__ __forceinline__ void after_previous() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+// The code of v in a group of scale s, as the last bits of a float: q + 8 in the low
+// four of 0x4B400000 + q + 8.  q is v / s rounded to the nearest integer, ties to
+// even, without a division: v (1 / s) is within 2^-21 of the quotient, and a
+// quotient of two numbers of at most 11 significant bits that is not m + 1/2 is at
+// least 2^-12 from it; rounding the product to multiples of 2^-13 (the sum with
+// 1536 does that) thus leaves it on the side where it is, or on m + 1/2 exactly.
+template <class T>
+__device__ __forceinline__ uint32_t code_bits(float v, float inverse) {
+    float q = fmaf(v, inverse, 1536.0f);
+    // A float16 scale under its normal range is too coarse to keep q within 7.
+    if (std::is_same<T, F16>::value) q = fminf(fmaxf(q, 1536.0f - 7.0f), 1536.0f + 7.0f);
+    return __float_as_uint(q + (12582912.0f + 8.0f - 1536.0f));
+}
+
 // One warp takes one block: lane 4 g + t holds slots g and g + 8, of each the
-// columns 32 j + 8 t + 0..7, so that a lane's 16 bytes of codes and a group's
-// maximum need no memory between lanes.  Bound by HBM: 2 bytes read and about
-// half a byte written per element.
-template <class T, int G>
-__global__ void __launch_bounds__(256) rr_quantize_kernel(Packed m, const uint16_t* w, int64_t ld,
-                                                          char* packed, int64_t total) {
+// columns 32 j + 8 t + 0..7, so that codes need no exchange between lanes and a
+// group's maximum at most two.  VEC: rows can be read 16 bytes at a time.  Bound
+// by HBM: 2 bytes read and about half a byte written per element.
+template <class T, int G, bool VEC>
+__global__ void __launch_bounds__(256) rr_quantize_kernel(const __grid_constant__ Packed m, const uint16_t* w,
+                                                          int64_t ld, char* packed, uint32_t total) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int64_t item = int64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    if (item >= total) return;
-    const int64_t b = item % m.blocks, strip = item / m.blocks % m.strips;
-    const int64_t mat = item / m.blocks / m.strips;
-    char* const to = packed + mat * m.matrix_bytes + (strip * m.blocks + b) * block_bytes(G);
+    const uint32_t i = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    after_previous();
+    if (i >= total) return;
+    const Item it(i, m);
+    char* const to = packed + it.mat * m.matrix_bytes + (it.strip * m.blocks + it.b) * block_bytes(G);
+    uint32_t v[2][4][4];       // pairs of elements
+#pragma unroll
     for (int half = 0; half < 2; ++half) {
-        const int64_t row = m.row(strip, 8 * half + g);
-        float v[4][8];
-        const uint16_t* const src = w + (mat * m.rows + row) * ld;
+        const int64_t row = m.row(it.strip, 8 * half + g);
+        const uint16_t* const src = w + (it.mat * m.rows + max(row, int64_t(0))) * ld;
+#pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int64_t c = b * kBlock + 32 * j + 8 * t;
-            for (int i = 0; i < 8; ++i)
-                v[j][i] = row >= 0 && c + i < m.cols ? T::widen(src[c + i]) : 0.0f;
-        }
-        uint32_t words[4];
-        for (int k = 0; k < kBlock / G; ++k) {
-            constexpr int kWords = G / 32;
-            float top = 0.0f;
-            bool fine = true;
-            for (int j = k * kWords; j < (k + 1) * kWords; ++j)
-                for (int i = 0; i < 8; ++i) {
-                    top = fmaxf(top, fabsf(v[j][i]));
-                    fine = fine && isfinite(v[j][i]);
-                }
-            for (int o = 1; o < 4; o *= 2) {
-                top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-                fine = __shfl_xor_sync(~0u, int(fine), o) && fine;
+            const int64_t c = int64_t(it.b) * kBlock + 32 * j + 8 * t;
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (VEC && row >= 0 && c + 8 <= m.cols) {
+                u = __ldcs(reinterpret_cast<const uint4*>(src + c));
+            } else if (row >= 0) {
+                uint32_t p[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) p[k] = c + k < m.cols ? src[c + k] : 0;
+                u = make_uint4(p[0] | p[1] << 16, p[2] | p[3] << 16, p[4] | p[5] << 16, p[6] | p[7] << 16);
             }
-            uint16_t s16 = T::round(top / 7.0f);
+            v[half][j][0] = u.x, v[half][j][1] = u.y, v[half][j][2] = u.z, v[half][j][3] = u.w;
+        }
+    }
+    constexpr int kWords = G / 32, kGroups = kBlock / G;
+    uint16_t scale[kGroups][2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        uint32_t words[4];
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+            uint32_t top = 0;      // magnitudes are ordered as their bits are
+#pragma unroll
+            for (int j = k * kWords; j < (k + 1) * kWords; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) top = __vmaxu2(top, v[half][j][q] & 0x7FFF7FFFu);
+            top = max(top >> 16, top & 0xFFFFu);
+            top = max(top, __shfl_xor_sync(~0u, top, 1));
+            top = max(top, __shfl_xor_sync(~0u, top, 2));
+            const float a = T::widen(uint16_t(top));
+            uint16_t s16 = T::round(a / 7.0f);
             float s = T::widen(s16);
-            if (s < kLeastScale) s16 = 0, s = 0.0f;
-            if (!fine) s16 = T::kNaN, s = 0.0f;
-            if (t == 0)
-                reinterpret_cast<uint16_t*>(to + kCodes)[2 * (g * (kBlock / G) + k) + half] = s16;
+            if (s < kLeastScale) s16 = 0;
+            if (!(a < INFINITY)) s16 = T::kNaN;
+            const bool dead = s < kLeastScale || !(a < INFINITY);
+            const float inverse = 1.0f / s;
+            scale[k][half] = s16;
+#pragma unroll
             for (int j = k * kWords; j < (k + 1) * kWords; ++j) {
-                uint32_t word = 0;
-                for (int i = 0; i < 8; ++i) {
-                    const float q = s > 0.0f ? fminf(fmaxf(rintf(v[j][i] / s), -7.0f), 7.0f) : 0.0f;
-                    word |= uint32_t(int(q) + 8) << (4 * (i / 2 + 4 * (i % 2)));
+                // The floats' other bits, shifted like the codes, add up to a constant.
+                uint32_t word = 0, rest = 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    word += code_bits<T>(T::widen(uint16_t(v[half][j][q])), inverse) << (4 * q);
+                    word += code_bits<T>(T::widen(uint16_t(v[half][j][q] >> 16)), inverse) << (4 * q + 16);
+                    rest += (0x4B400000u << (4 * q)) + (0x4B400000u << (4 * q + 16));
                 }
-                words[j] = word;
+                words[j] = dead ? 0x88888888u : word - rest;
             }
         }
         *reinterpret_cast<uint4*>(to + 512 * half + 16 * lane) =
             make_uint4(words[0], words[1], words[2], words[3]);
     }
+    if (t == 0)
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k)
+            reinterpret_cast<uint32_t*>(to + kCodes)[g * kGroups + k] =
+                uint32_t(scale[k][0]) | uint32_t(scale[k][1]) << 16;
 }
 
 // The inverse, by the same lanes.
-template <class T, int G, bool F32>
-__global__ void __launch_bounds__(256) rr_dequantize_kernel(Packed m, const char* packed, void* w,
-                                                            int64_t ld, int64_t total) {
+template <class T, int G, bool F32, bool VEC>
+__global__ void __launch_bounds__(256) rr_dequantize_kernel(const __grid_constant__ Packed m, const char* packed,
+                                                            void* w, int64_t ld, uint32_t total) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int64_t item = int64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    if (item >= total) return;
-    const int64_t b = item % m.blocks, strip = item / m.blocks % m.strips;
-    const int64_t mat = item / m.blocks / m.strips;
-    const char* const from = packed + mat * m.matrix_bytes + (strip * m.blocks + b) * block_bytes(G);
+    const uint32_t i = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    after_previous();
+    if (i >= total) return;
+    const Item it(i, m);
+    const char* const from = packed + it.mat * m.matrix_bytes + (it.strip * m.blocks + it.b) * block_bytes(G);
+    uint4 codes_of[2];
+    uint32_t scale[kBlock / G];
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+        codes_of[half] = __ldcs(reinterpret_cast<const uint4*>(from + 512 * half + 16 * lane));
+#pragma unroll
+    for (int k = 0; k < kBlock / G; ++k)
+        scale[k] = reinterpret_cast<const uint32_t*>(from + kCodes)[g * (kBlock / G) + k];
+#pragma unroll
     for (int half = 0; half < 2; ++half) {
-        const int64_t row = m.row(strip, 8 * half + g);
+        const int64_t row = m.row(it.strip, 8 * half + g);
         if (row < 0) continue;
-        const uint4 q = *reinterpret_cast<const uint4*>(from + 512 * half + 16 * lane);
-        const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+        const uint32_t words[4] = {codes_of[half].x, codes_of[half].y, codes_of[half].z, codes_of[half].w};
+#pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float s = T::widen(reinterpret_cast<const uint16_t*>(
-                from + kCodes)[2 * (g * (kBlock / G) + 32 * j / G) + half]);
-            const int64_t c = b * kBlock + 32 * j + 8 * t;
-            for (int i = 0; i < 8; ++i)
-                if (c + i < m.cols)
-                    put<T, F32>(w, (mat * m.rows + row) * ld + c + i, s * float(code(words[j], i)));
+            const float s = T::widen(uint16_t(half ? scale[32 * j / G] >> 16 : scale[32 * j / G]));
+            const int64_t c = int64_t(it.b) * kBlock + 32 * j + 8 * t;
+            const int64_t at = (it.mat * m.rows + row) * ld + c;
+            float f[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = s * float(code(words[j], k));
+            if (VEC && c + 8 <= m.cols) {
+                if (F32) {
+                    float4* const p = reinterpret_cast<float4*>(static_cast<float*>(w) + at);
+                    p[0] = make_float4(f[0], f[1], f[2], f[3]);
+                    p[1] = make_float4(f[4], f[5], f[6], f[7]);
+                } else {
+                    uint32_t p[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) p[k] = uint32_t(T::round(f[2 * k])) | uint32_t(T::round(f[2 * k + 1])) << 16;
+                    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(w) + at) = make_uint4(p[0], p[1], p[2], p[3]);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (c + k < m.cols) put<T, F32>(w, at + k, f[k]);
+            }
         }
     }
 }
@@ -354,10 +437,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
     using S = Stage<G, U>;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rank = blockIdx.x % a.cluster, cl = blockIdx.x / a.cluster, n_cl = gridDim.x / a.cluster;
-    // Programmatic dependent launch: the next kernel may be scheduled, and waits
-    // as this one does for the kernels before it.
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    after_previous();
     char* const fifo = smem + warp * (S::kStages * S::kBytes);
     char* const xs = smem + kWarps * S::kStages * S::kBytes;
     float4* const red = reinterpret_cast<float4*>(xs + a.tokens * a.pitch);
@@ -1284,12 +1364,27 @@ extern "C" rr_status rr_quant_bytes(const rr_quant* q, int64_t* matrix_bytes, in
 
 namespace {
 
-// Blocks of warps for `items`, or an error where the grid cannot hold them.
-rr_status grid_of(int64_t items, int per_block, unsigned* grid) {
-    const int64_t n = (items + per_block - 1) / per_block;
+// Eight warps to a block, one item each.
+rr_status grid_of(const Packed& m, int32_t count, uint32_t* total, unsigned* grid) {
+    const int64_t n = m.strips * m.blocks * count;
     if (n > INT32_MAX) return rr_fail(RR_ELAYOUT, "the stack is too large for one call");
-    *grid = unsigned(n);
+    *total = uint32_t(n);
+    *grid = unsigned((n + 7) / 8);
     return RR_OK;
+}
+
+template <class... Params, class... Args>
+cudaError_t launch_after(void (*kernel)(Params...), unsigned grid, int threads, cudaStream_t stream, Args... args) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(unsigned(threads));
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
 }
 
 }  // namespace
@@ -1303,14 +1398,15 @@ extern "C" rr_status rr_quantize(const rr_quant* q, const void* w, int64_t ld, v
     RR_TRY(check_device(w, 2, "w"));
     RR_TRY(check_device(packed, 16, "packed"));
     const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
-    const int64_t total = m.strips * m.blocks * q->count;
+    uint32_t total;
     unsigned grid;
-    RR_TRY(grid_of(total, 8, &grid));
+    RR_TRY(grid_of(m, q->count, &total, &grid));
+    const bool vec = (uintptr_t)w % 16 == 0 && ld % 8 == 0;
     return with_group(q->dtype, q->group, [&](auto t, auto g) -> rr_status {
+        using T = decltype(t);
         constexpr int G = decltype(g)::value ? decltype(g)::value : 128;
-        rr_quantize_kernel<decltype(t), G><<<grid, 256, 0, stream>>>(
-            m, static_cast<const uint16_t*>(w), ld, static_cast<char*>(packed), total);
-        RR_CUDA(cudaGetLastError());
+        RR_CUDA(launch_after(vec ? rr_quantize_kernel<T, G, true> : rr_quantize_kernel<T, G, false>, grid, 256, stream,
+                             m, static_cast<const uint16_t*>(w), ld, static_cast<char*>(packed), total));
         return RR_OK;
     });
 }
@@ -1325,18 +1421,16 @@ extern "C" rr_status rr_dequantize(const rr_quant* q, const void* packed, void* 
     RR_TRY(check_device(packed, 16, "packed"));
     RR_TRY(check_device(w, f32 ? 4 : 2, "w"));
     const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
-    const int64_t total = m.strips * m.blocks * q->count;
+    uint32_t total;
     unsigned grid;
-    RR_TRY(grid_of(total, 8, &grid));
+    RR_TRY(grid_of(m, q->count, &total, &grid));
+    const bool vec = (uintptr_t)w % 16 == 0 && ld % (f32 ? 4 : 8) == 0;
     return with_group(q->dtype, q->group, [&](auto t, auto g) -> rr_status {
+        using T = decltype(t);
         constexpr int G = decltype(g)::value ? decltype(g)::value : 128;
-        if (f32)
-            rr_dequantize_kernel<decltype(t), G, true><<<grid, 256, 0, stream>>>(
-                m, static_cast<const char*>(packed), w, ld, total);
-        else
-            rr_dequantize_kernel<decltype(t), G, false><<<grid, 256, 0, stream>>>(
-                m, static_cast<const char*>(packed), w, ld, total);
-        RR_CUDA(cudaGetLastError());
+        const auto kernel = f32 ? (vec ? rr_dequantize_kernel<T, G, true, true> : rr_dequantize_kernel<T, G, true, false>)
+                                : (vec ? rr_dequantize_kernel<T, G, false, true> : rr_dequantize_kernel<T, G, false, false>);
+        RR_CUDA(launch_after(kernel, grid, 256, stream, m, static_cast<const char*>(packed), w, ld, total));
         return RR_OK;
     });
 }
