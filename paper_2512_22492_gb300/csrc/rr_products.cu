@@ -579,12 +579,15 @@ struct MoeArgs {
     float* weights;
     MoeControl* control;
     float* logits;     // [tokens, n_experts]
-    float* h;          // [pairs, inter]: silu(gate) * up, by expert, then token
-    float* y;          // [pairs, hidden]: each pair's product with w2
+    float* h;          // [pairs, h_ld]: silu(gate) * up, by expert, then token
+    float* y;          // [pairs, y_ld]: each pair's product with w2
+    uint32_t* h_top;   // [pairs]: the largest finite |h|, as bits (float16)
+    int32_t h_ld, y_ld;        // multiples of 4
     int32_t tokens, n_experts, first, n_local, top_k, norm, hidden, inter;
     int32_t x_vec, r_vec;      // rows of x, of the router can be read 16 bytes at a time
     int32_t cap;               // tokens of a pass: at most 16
     int32_t x_pitch, h_pitch;  // bytes between tokens in shared memory
+    int32_t all_x;             // shared memory holds every token's row
 };
 
 // A warp's stages of weights.  W: 0 for 16-bit matrices whose rows start at 16
@@ -717,95 +720,117 @@ struct MoeTables {
     uint32_t stop;
 };
 
-// The sum of router row e with up to N tokens' rows from t0.
-template <class T, int N>
-__device__ __forceinline__ void logit_item(const MoeArgs& a, int e, int t0, int n, int lane) {
-    const uint16_t* const r = a.router + int64_t(e) * a.hidden;
-    const uint16_t* const x = a.x + t0 * a.ldx;
-    float sum[N] = {};
+// Logits of 16 tokens from t0 and 8 experts from e0: a block's warps share the
+// columns, tokens are operand A, router rows operand B.  red: 8 KB.
+template <class T>
+__device__ __forceinline__ void logit_item(const MoeArgs& a, int e0, int t0, float4* red) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const uint16_t* const r = a.router + int64_t(min(e0 + g, a.n_experts - 1)) * a.hidden + 8 * t;
+    const uint16_t* const lo = a.x + min(t0 + g, a.tokens - 1) * a.ldx + 8 * t;
+    const uint16_t* const hi = a.x + min(t0 + 8 + g, a.tokens - 1) * a.ldx + 8 * t;
+    float sum[4] = {};
     if (a.x_vec && a.r_vec) {
-#pragma unroll 8 / N
-        for (int k = 8 * lane; k < a.hidden; k += 256) {
-            const uint4 w = *reinterpret_cast<const uint4*>(r + k);
-            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if (i >= n) break;
-                const uint4 v = *reinterpret_cast<const uint4*>(x + i * a.ldx + k);
-                const uint32_t vv[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    sum[i] = fmaf(T::widen(uint16_t(vv[q])), T::widen(uint16_t(ww[q])), sum[i]);
-                    sum[i] = fmaf(T::widen(uint16_t(vv[q] >> 16)), T::widen(uint16_t(ww[q] >> 16)), sum[i]);
-                }
+#pragma unroll 4
+        for (int k = 32 * warp; k < a.hidden; k += 32 * kWarps) {
+            uint4 w = make_uint4(0, 0, 0, 0), u = w, v = w;
+            if (k + 8 * t < a.hidden) {
+                w = *reinterpret_cast<const uint4*>(r + k);
+                u = *reinterpret_cast<const uint4*>(lo + k);
+                if (t0 + 8 < a.tokens) v = *reinterpret_cast<const uint4*>(hi + k);
             }
+            mma<T>(sum, u.x, v.x, u.y, v.y, w.x, w.y);
+            mma<T>(sum, u.z, v.z, u.w, v.w, w.z, w.w);
         }
     } else {
-#pragma unroll 4
-        for (int k = lane; k < a.hidden; k += 32) {
-            const float w = T::widen(r[k]);
+        for (int k = 32 * warp; k < a.hidden; k += 32 * kWarps) {
+            uint32_t w[4], u[4], v[4];
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (i < n) sum[i] = fmaf(T::widen(x[i * a.ldx + k]), w, sum[i]);
+            for (int q = 0; q < 4; ++q) {
+                const bool in0 = k + 8 * t + 2 * q < a.hidden, in1 = k + 8 * t + 2 * q + 1 < a.hidden;
+                w[q] = (in0 ? r[k + 2 * q] : 0u) | (in1 ? uint32_t(r[k + 2 * q + 1]) << 16 : 0u);
+                u[q] = (in0 ? lo[k + 2 * q] : 0u) | (in1 ? uint32_t(lo[k + 2 * q + 1]) << 16 : 0u);
+                v[q] = (in0 ? hi[k + 2 * q] : 0u) | (in1 ? uint32_t(hi[k + 2 * q + 1]) << 16 : 0u);
+            }
+            mma<T>(sum, u[0], v[0], u[1], v[1], w[0], w[1]);
+            mma<T>(sum, u[2], v[2], u[3], v[3], w[2], w[3]);
         }
     }
+    red[threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    __syncthreads();
+    if (threadIdx.x < 128) {
+        const int i = threadIdx.x;
+        float v = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float s = warp_sum(sum[i]);
-        if (lane == 0 && i < n) a.logits[(t0 + i) * a.n_experts + e] = s;
+        for (int q = 0; q < kWarps; ++q) v += reinterpret_cast<const float*>(red)[128 * q + i];
+        const int tok = t0 + i / 16 + 8 * (i >> 1 & 1), e = e0 + 2 * (i / 4 % 4) + (i & 1);
+        if (tok < a.tokens && e < a.n_experts) __stcg(a.logits + tok * a.n_experts + e, v);
     }
+    __syncthreads();
 }
 
-// One warp: token t's softmax and its top_k experts.
-__device__ __forceinline__ void choose(const MoeArgs& a, MoeTables& tab, int t, int lane) {
-    constexpr int kEach = kMaxExperts / 32;
-    float l[kEach];
-    uint32_t key[kEach];
-    float top = -INFINITY;
+// One warp: the softmax and the top_k experts of tokens warp, warp + kWarps, ...
+// kEach: experts of a lane.
+template <int kEach>
+__device__ __forceinline__ void choose(const MoeArgs& a, MoeTables& tab, int warp, int lane) {
+    constexpr int kTokens = RR_MOE_MAX_TOKENS / kWarps;
+    float l[kTokens][kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int e = 32 * i + lane;
-        l[i] = e < a.n_experts ? __ldcg(a.logits + t * a.n_experts + e) : 0.0f;
-        key[i] = e < a.n_experts ? rank_key(l[i]) : 0;
-        if (e < a.n_experts) top = fmaxf(top, l[i]);
-    }
-    for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-    float sum = 0.0f;
+    for (int q = 0; q < kTokens; ++q)
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
-        if (32 * i + lane < a.n_experts) sum += expf(l[i] - top);
-    sum = warp_sum(sum);
-    float mine = 0.0f, total = 0.0f;
-    int my_id = 0;
-    for (int j = 0; j < a.top_k; ++j) {
-        uint32_t best = 0;
+        for (int i = 0; i < kEach; ++i) {
+            const int t = warp + q * kWarps, e = 32 * i + lane;
+            l[q][i] = t < a.tokens && e < a.n_experts ? __ldcg(a.logits + t * a.n_experts + e) : 0.0f;
+        }
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) best = max(best, key[i]);
-        best = __reduce_max_sync(~0u, best);
-        uint32_t at = ~0u;
-        float lv = 0.0f;
+    for (int q = 0; q < kTokens; ++q) {
+        const int t = warp + q * kWarps;
+        if (t >= a.tokens) break;
+        uint32_t key[kEach];
+        float top = -INFINITY;
 #pragma unroll
-        for (int i = kEach - 1; i >= 0; --i)
-            if (key[i] == best) at = 32 * i + lane, lv = l[i];
-        const uint32_t e = __reduce_min_sync(~0u, at);
-        lv = __shfl_sync(~0u, lv, e & 31);
+        for (int i = 0; i < kEach; ++i) {
+            const bool in = 32 * i + lane < a.n_experts;
+            key[i] = in ? rank_key(l[q][i]) : 0;
+            if (in) top = fmaxf(top, l[q][i]);
+        }
+#pragma unroll
+        for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+        float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
-            if (32 * i + lane == int(e)) key[i] = 0;
-        const float p = expf(lv - top) / sum;
-        total += p;
-        if (lane == j) mine = p, my_id = int(e);
-    }
-    if (lane < a.top_k) {
-        const int i = t * a.top_k + lane;
-        if (a.norm) mine /= total;
-        tab.chosen[i] = int16_t(my_id);
-        tab.c[i] = mine;
-        const int local = my_id - a.first;
-        if (local >= 0 && local < a.n_local) atomicOr(&tab.mask[t >> 5][local], 1u << (t & 31));
-        if (blockIdx.x == 0) {
-            if (a.ids) a.ids[i] = my_id;
-            if (a.weights) a.weights[i] = mine;
+            if (32 * i + lane < a.n_experts) sum += expf(l[q][i] - top);
+        sum = warp_sum(sum);
+        float mine = -INFINITY;
+        int my_id = 0;
+        for (int j = 0; j < a.top_k; ++j) {
+            uint32_t best = 0;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) best = max(best, key[i]);
+            best = __reduce_max_sync(~0u, best);
+            uint32_t at = ~0u;
+            float lv = 0.0f;
+#pragma unroll
+            for (int i = kEach - 1; i >= 0; --i)
+                if (key[i] == best) at = 32 * i + lane, lv = l[q][i];
+            const uint32_t e = __reduce_min_sync(~0u, at);
+            lv = __shfl_sync(~0u, lv, e & 31);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (32 * i + lane == int(e)) key[i] = 0;
+            if (lane == j) mine = lv, my_id = int(e);
+        }
+        float p = lane < a.top_k ? expf(mine - top) / sum : 0.0f;
+        if (a.norm) p /= warp_sum(p);
+        if (lane < a.top_k) {
+            const int i = t * a.top_k + lane;
+            tab.chosen[i] = int16_t(my_id);
+            tab.c[i] = p;
+            const int local = my_id - a.first;
+            if (local >= 0 && local < a.n_local) atomicOr(&tab.mask[t >> 5][local], 1u << (t & 31));
+            if (blockIdx.x == 0) {
+                if (a.ids) a.ids[i] = my_id;
+                if (a.weights) a.weights[i] = p;
+            }
         }
     }
 }
@@ -897,16 +922,16 @@ struct Feed {
     }
 };
 
-// Tokens' rows (16-bit) of a pass to shared memory, zero-filled to whole blocks.
+// Tokens' rows (16-bit) to shared memory, zero-filled to whole blocks: those of
+// pairs first, first + 1, ..., or with all_x simply tokens 0, 1, ...
 __device__ __forceinline__ void stage_tokens(const MoeArgs& a, const MoeTables& tab, char* to, int first, int count,
                                              int cols) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int i = warp; i < count * 4; i += kWarps) {      // four warps' shares of a row each
-        const uint16_t* const row = a.x + tab.token[first + i / 4] * a.ldx;
-        char* const dst = to + i / 4 * a.x_pitch;
-        if (a.x_vec) {
 #pragma unroll 4
-            for (int c = 8 * (32 * (i % 4) + lane); c < cols; c += 1024) {
+    for (int i = 0; i < count; ++i) {
+        const uint16_t* const row = a.x + (a.all_x ? i : tab.token[first + i]) * a.ldx;
+        char* const dst = to + i * a.x_pitch;
+        if (a.x_vec) {
+            for (int c = 8 * threadIdx.x; c < cols; c += 8 * kProdThreads) {
                 uint4 v = make_uint4(0, 0, 0, 0);
                 if (c + 8 <= a.hidden) {
                     v = *reinterpret_cast<const uint4*>(row + c);
@@ -919,10 +944,15 @@ __device__ __forceinline__ void stage_tokens(const MoeArgs& a, const MoeTables& 
             }
         } else {
 #pragma unroll 4
-            for (int c = 32 * (i % 4) + lane; c < cols; c += 128)
+            for (int c = threadIdx.x; c < cols; c += kProdThreads)
                 *reinterpret_cast<uint16_t*>(dst + 2 * c) = c < a.hidden ? row[c] : uint16_t(0);
         }
     }
+}
+
+// The power of two that brings a float16 token's largest h to 2^14..2^15.
+__device__ __forceinline__ int h_exponent(uint32_t top) {
+    return top ? max(-100, min(100, 14 - ilogbf(__uint_as_float(top)))) : 0;
 }
 
 // A pass's h as two 16-bit parts, v = hi + lo to 2^-16 of v: the product then
@@ -932,34 +962,32 @@ __device__ __forceinline__ void stage_tokens(const MoeArgs& a, const MoeTables& 
 // underflows is below 2^-39 of the largest.
 template <class T>
 __device__ __forceinline__ void stage_h(const MoeArgs& a, MoeTables& tab, char* to, int first, int count, int cols) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int i = warp; i < count; i += kWarps) {
-        const float* const row = a.h + int64_t(first + i) * a.inter;
+    const int chunks = cols / 4;
+#pragma unroll 4
+    for (int k = threadIdx.x; k < count * chunks; k += kProdThreads) {
+        const int i = k / chunks, c = 4 * (k % chunks);
+        float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (c < a.inter) f = __ldcg(reinterpret_cast<const float4*>(a.h + int64_t(first + i) * a.h_ld + c));
         float up = 1.0f;
         if (std::is_same<T, F16>::value) {
-            float top = 0.0f;
-#pragma unroll 8
-            for (int c = lane; c < a.inter; c += 32) {
-                const float v = fabsf(__ldcg(row + c));
-                if (v < INFINITY) top = fmaxf(top, v);
-            }
-            for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-            const int e = top > 0.0f ? max(-100, min(100, 14 - ilogbf(top))) : 0;
+            const int e = h_exponent(__ldcg(a.h_top + first + i));
             up = ldexpf(1.0f, e);
-            if (lane == 0) tab.scale[i] = ldexpf(1.0f, -e);
+            if (c == 0) tab.scale[i] = ldexpf(1.0f, -e);
         }
-        char* const dst = to + i * a.h_pitch;
-        char* const low = dst + a.cap * a.h_pitch;
-#pragma unroll 8
-        for (int c = lane; c < cols; c += 32) {
-            const float v = c < a.inter ? __ldcg(row + c) * up : 0.0f;
-            const uint16_t hi = T::round(v);
-            const float rest = v - T::widen(hi);
-            reinterpret_cast<uint16_t*>(dst)[c] = hi;
+        const float v[4] = {f.x, f.y, f.z, f.w};
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float s = c + q < a.inter ? v[q] * up : 0.0f;
+            hi[q] = T::round(s);
+            const float rest = s - T::widen(uint16_t(hi[q]));
             // (An infinite v has no rest; one just under the largest may round to
             // infinity in bfloat16, as the result then does.)
-            reinterpret_cast<uint16_t*>(low)[c] = T::round(isfinite(rest) ? rest : 0.0f);
+            lo[q] = T::round(isfinite(rest) ? rest : 0.0f);
         }
+        char* const dst = to + i * a.h_pitch + 2 * c;
+        *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+        *reinterpret_cast<uint2*>(dst + a.cap * a.h_pitch) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
     }
 }
 
@@ -977,7 +1005,10 @@ __device__ __forceinline__ void moe_batch(const MoeArgs& a, const MoePhase* ph, 
     const uint32_t fifo_at = smem_at(fifo);
     const char* x[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) x[n] = region + min(8 * n + g, count - 1) * pitch + 16 * t;
+    for (int n = 0; n < NT; ++n) {
+        const int i = min(8 * n + g, count - 1);
+        x[n] = region + (PHASE == 0 && a.all_x ? tab.token[first + i] : i) * pitch + 16 * t;
+    }
 
     auto put_item = [&](int i, int ln, int n, const float (&v)[4]) {
         const int strip = (p.f0 + i) % int(p.m.strips);
@@ -987,10 +1018,14 @@ __device__ __forceinline__ void moe_batch(const MoeArgs& a, const MoePhase* ph, 
             const int tok = 8 * n + 2 * (ln & 3) + k;
             if (tok >= count) continue;
             if (PHASE == 0) {
-                if (lo >= 0) __stcg(a.h + int64_t(first + tok) * a.inter + lo, silu(v[k]) * v[2 + k]);
+                if (lo < 0) continue;
+                const float h = silu(v[k]) * v[2 + k];
+                __stcg(a.h + int64_t(first + tok) * a.h_ld + lo, h);
+                if (std::is_same<T, F16>::value && fabsf(h) < INFINITY)
+                    atomicMax(a.h_top + first + tok, __float_as_uint(fabsf(h)));
             } else {
                 const float s = std::is_same<T, F16>::value ? tab.scale[tok] : 1.0f;
-                float* const y = a.y + int64_t(first + tok) * a.hidden;
+                float* const y = a.y + int64_t(first + tok) * a.y_ld;
                 if (lo >= 0) __stcg(y + lo, v[k] * s);
                 if (hi >= 0) __stcg(y + hi, v[2 + k] * s);
             }
@@ -1044,7 +1079,7 @@ __device__ __forceinline__ void moe_phase(const MoeArgs& a, const MoePhase* ph, 
     for (int i0 = 0; i0 < p.n;) {
         const int i1 = p.batch_end(i0), pass = (p.f0 + i0) / int(p.m.strips);
         const int first = tab.pass_first[pass], count = tab.pass_count[pass];
-        if (pass != staged) {
+        if (pass != staged && !(PHASE == 0 && a.all_x)) {
             __syncthreads();
             if (PHASE == 0) stage_tokens(a, tab, region, first, count, p.blocks * Weights<W>::kCols);
             else stage_h<T>(a, tab, region, first, count, p.blocks * Weights<W>::kCols);
@@ -1085,20 +1120,19 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
     __syncthreads();
     if (tab.stop) return;
 
-    // Logits.
+    // Logits; meanwhile, tokens to shared memory, where all of them fit.
     {
-        const int each = a.tokens == 1 ? 1 : a.tokens <= 4 ? 4 : 8;
-        const int groups = (a.tokens + each - 1) / each;
-        for (int i = warp * gridDim.x + blockIdx.x; i < a.n_experts * groups; i += kWarps * gridDim.x) {
-            const int e = i % a.n_experts, t0 = i / a.n_experts * each, n = min(each, a.tokens - t0);
-            if (each == 1) logit_item<T, 1>(a, e, t0, n, lane);
-            else if (each == 4) logit_item<T, 4>(a, e, t0, n, lane);
-            else logit_item<T, 8>(a, e, t0, n, lane);
-        }
+        const int groups = (a.n_experts + 7) / 8;
+        for (int i = blockIdx.x; i < groups * ((a.tokens + 15) / 16); i += gridDim.x)
+            logit_item<T>(a, i % groups * 8, i / groups * 16, reinterpret_cast<float4*>(smem));
+        if (a.all_x) stage_tokens(a, tab, region, 0, a.tokens, (a.hidden + Weights<W>::kCols - 1) / Weights<W>::kCols * Weights<W>::kCols);
+        if (blockIdx.x == gridDim.x - 1)
+            for (int i = threadIdx.x; i < a.tokens * min(a.top_k, a.n_local); i += kProdThreads) a.h_top[i] = 0;
     }
     if (!grid_barrier(a, tab, 0)) return;
 
-    for (int t = warp; t < a.tokens; t += kWarps) choose(a, tab, t, lane);
+    if (a.n_experts <= 128) choose<4>(a, tab, warp, lane);
+    else choose<kMaxExperts / 32>(a, tab, warp, lane);
     __syncthreads();
     // Pairs by expert, then token; passes of up to `cap` tokens of one expert.
     {
@@ -1129,31 +1163,36 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
         for (uint32_t m = m1; m; m &= m - 1) tab.token[pair++] = uint8_t(31 + __ffs(m));
         __syncthreads();
     }
-    // The phases' items, and the team of the fewest rounds (a join costs one).
-    if (threadIdx.x < 2) {
-        const int k = threadIdx.x, passes = int(tab.total & 0xFFFF);
-        MoePhase p;
-        p.base = k ? a.w2 : a.w13;
-        p.m.rows = k ? a.hidden : 2 * a.inter;
-        p.m.cols = k ? a.inter : a.hidden;
-        p.m.pair = !k;
-        p.m.strips = k ? (a.hidden + 15) / 16 : (a.inter + 7) / 8;
-        p.m.blocks = (p.m.cols + kBlock - 1) / kBlock;
-        p.m.matrix_bytes = p.m.strips * p.m.blocks * block_bytes(W >= 32 ? W : 128);
-        p.blocks = int(p.m.cols + Weights<W>::kCols - 1) / Weights<W>::kCols;
-        const int all = passes * int(p.m.strips), grid = gridDim.x;      // under 2^31: 1024 passes of 2048 strips
-        p.f0 = int(int64_t(blockIdx.x) * all / grid);
-        p.n = int(int64_t(blockIdx.x + 1) * all / grid) - p.f0;
+    // The phases' items, and the team of the fewest rounds (a join costs one):
+    // lane 8 k + i looks at phase k and teams of 2^i.
+    if (warp == 0) {
+        const int k = lane >> 3 & 1, team = 1 << min(lane & 7, 4), teams = kWarps / team;
+        const int passes = int(tab.total & 0xFFFF);
+        const int cols = k ? a.inter : a.hidden, strips = k ? (a.hidden + 15) / 16 : (a.inter + 7) / 8;
+        const int blocks = (cols + Weights<W>::kCols - 1) / Weights<W>::kCols;
+        const int all = passes * strips, grid = gridDim.x;      // under 2^31: 1024 passes of 2048 strips
         const int most = (all + grid - 1) / grid;
-        int best = INT_MAX;
-        for (int team = 1; team <= kWarps; team *= 2) {
-            const int teams = kWarps / team;
-            const int batch = team == 1 ? INT_MAX / 2 : kJoinBytes / (512 * (a.tokens > 8 ? 2 : 1) * team) / teams * teams;
-            const int steps = (p.blocks + team - 1) / team;
-            const int cost = (most + teams - 1) / teams * steps + (team == 1 ? 0 : (most + batch - 1) / batch);
-            if (cost < best) best = cost, p.team = team, p.batch = batch;
+        const int batch = team == 1 ? INT_MAX / 2 : kJoinBytes / (512 * (a.tokens > 8 ? 2 : 1) * team) / teams * teams;
+        const int cost = (most + teams - 1) / teams * ((blocks + team - 1) / team) + (team == 1 ? 0 : (most + batch - 1) / batch);
+        uint32_t best = uint32_t(min(cost, 0xFFFFFF)) << 3 | uint32_t(min(lane & 7, 4));
+        const uint32_t own = best;
+        for (int o = 1; o < 8; o *= 2) best = min(best, __shfl_xor_sync(~0u, best, o));
+        if (lane < 16 && own == best && (lane & 7) <= 4) {
+            MoePhase p;
+            p.base = k ? a.w2 : a.w13;
+            p.m.rows = k ? a.hidden : 2 * a.inter;
+            p.m.cols = cols;
+            p.m.pair = !k;
+            p.m.strips = strips;
+            p.m.blocks = (cols + kBlock - 1) / kBlock;
+            p.m.matrix_bytes = p.m.strips * p.m.blocks * block_bytes(W >= 32 ? W : 128);
+            p.blocks = blocks;
+            p.f0 = int(int64_t(blockIdx.x) * all / grid);
+            p.n = int(int64_t(blockIdx.x + 1) * all / grid) - p.f0;
+            p.team = team;
+            p.batch = batch;
+            ph[k] = p;
         }
-        ph[k] = p;
     }
     __syncthreads();
 
@@ -1174,19 +1213,24 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
     copy_wait<0>();
     if (!grid_barrier(a, tab, 2)) return;
 
-    for (int64_t i = int64_t(blockIdx.x) * kProdThreads + threadIdx.x; i < int64_t(a.tokens) * a.hidden;
-         i += int64_t(gridDim.x) * kProdThreads) {
-        const int t = int(i / a.hidden), n = int(i % a.hidden);
-        float sum = 0.0f;
+    // A warp takes 128 columns of a token.
+    const int parts = (a.hidden + 127) / 128;
+    for (int i = warp * gridDim.x + blockIdx.x; i < a.tokens * parts; i += kWarps * gridDim.x) {
+        const int t = i / parts, n = i % parts * 128 + 4 * lane;
+        float sum[4] = {};
 #pragma unroll 8
         for (int j = 0; j < a.top_k; ++j) {
             const int e = tab.chosen[t * a.top_k + j] - a.first;
-            if (e < 0 || e >= a.n_local) continue;
+            if (e < 0 || e >= a.n_local || n >= a.hidden) continue;
             const uint32_t m0 = tab.mask[0][e], m1 = tab.mask[1][e];
             const int before = t < 32 ? __popc(m0 & ((1u << t) - 1)) : __popc(m0) + __popc(m1 & ((1u << (t - 32)) - 1));
-            sum += tab.c[t * a.top_k + j] * __ldcg(a.y + int64_t(tab.first[e] + before) * a.hidden + n);
+            const float c = tab.c[t * a.top_k + j];
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(a.y + int64_t(tab.first[e] + before) * a.y_ld + n));
+            sum[0] += c * y.x, sum[1] += c * y.y, sum[2] += c * y.z, sum[3] += c * y.w;
         }
-        a.out[t * a.ldo + n] = T::round(sum);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (n + q < a.hidden) a.out[t * a.ldo + n + q] = T::round(sum[q]);
     }
     // The last block to finish leaves the counters at zero for the next call.
     __syncthreads();
@@ -1296,7 +1340,8 @@ rr_status check_moe(const rr_moe_layer* L) {
 
 // Workspace: a control block, then the arrays.  Offsets in bytes.
 struct MoeSpace {
-    int64_t logits, h, y, total;
+    int64_t logits, top, h, y, total;
+    int32_t h_ld, y_ld;
 };
 constexpr int64_t kControlBytes = 256;
 
@@ -1306,9 +1351,12 @@ MoeSpace moe_space(const rr_moe_layer* L, int64_t tokens) {
     MoeSpace s;
     const int64_t pairs = tokens * std::min(L->top_k, L->n_local);
     s.logits = kControlBytes;
-    s.h = s.logits + up16(4 * tokens * L->n_experts);
-    s.y = s.h + up16(4 * pairs * L->inter);
-    s.total = s.y + up16(4 * pairs * L->hidden);
+    s.h_ld = int32_t((L->inter + 3) / 4 * 4);
+    s.y_ld = int32_t((L->hidden + 3) / 4 * 4);
+    s.top = s.logits + up16(4 * tokens * L->n_experts);
+    s.h = s.top + up16(4 * pairs);
+    s.y = s.h + 4 * pairs * s.h_ld;
+    s.total = s.y + 4 * pairs * s.y_ld;
     return s;
 }
 
@@ -1327,7 +1375,8 @@ rr_status launch_moe(MoeArgs a, cudaStream_t stream) {
     if (a.cap > 8 && a.cap < 16) a.cap = 8;
     a.cap = std::min(a.cap, a.tokens);
     if (a.cap < 1) return rr_fail(RR_ELAYOUT, "hidden %d, inter %d: rows too long", a.hidden, a.inter);
-    const int smem = kFixed - 1024 + a.cap * each;
+    a.all_x = a.cap == a.tokens || int64_t(a.tokens) * a.x_pitch <= room;
+    const int smem = kFixed - 1024 + std::max(a.cap * each, a.all_x ? a.tokens * a.x_pitch : 0);
     static std::mutex mutex;
     static int grids[16] = {};
     int dev = 0, grid;
@@ -1644,6 +1693,9 @@ extern "C" rr_status rr_moe(const rr_moe_layer* L, const void* router, const voi
     a.logits = reinterpret_cast<float*>(ws + S.logits);
     a.h = reinterpret_cast<float*>(ws + S.h);
     a.y = reinterpret_cast<float*>(ws + S.y);
+    a.h_top = reinterpret_cast<uint32_t*>(ws + S.top);
+    a.h_ld = S.h_ld;
+    a.y_ld = S.y_ld;
     a.tokens = n_tokens;
     a.n_experts = L->n_experts;
     a.first = L->first_expert;
