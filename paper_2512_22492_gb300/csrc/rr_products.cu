@@ -560,12 +560,14 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
 constexpr int kMaxExperts = 512, kMaxTopK = 16, kMaxHidden = 32768, kMaxInter = 16384;
 constexpr int kMaxPairs = RR_MOE_MAX_TOKENS * kMaxTopK;
 constexpr int kJoinBytes = 24 * 1024;   // shared memory of the teams' sums
+constexpr int kClusterBlocks = 8;       // of a layer small enough for one cluster
+constexpr int64_t kClusterBytes = 1 << 20;
 constexpr int kSmem = 227 * 1024;
 
 // The workspace's control block.
 struct MoeControl {
     uint32_t error;        // a wait ran out: calls do nothing until rr_moe_check
-    uint32_t barrier[3];   // blocks that have arrived
+    uint32_t barrier[4];   // blocks that have arrived
     uint32_t left;         // blocks that have finished
 };
 
@@ -588,6 +590,11 @@ struct MoeArgs {
     int32_t cap;               // tokens of a pass: at most 16
     int32_t x_pitch, h_pitch;  // bytes between tokens in shared memory
     int32_t all_x;             // shared memory holds every token's row
+    int32_t fold;              // rows of h and one of zeros, where shared memory holds all; else 0
+    int32_t one;               // the grid is one cluster
+    int64_t m13_bytes, m2_bytes;       // of an expert's matrices
+    int32_t* far_chosen;       // [tokens * top_k]: choices made by other blocks
+    float* far_c;
 };
 
 // A warp's stages of weights.  W: 0 for 16-bit matrices whose rows start at 16
@@ -709,6 +716,7 @@ __device__ __forceinline__ uint32_t rank_key(float l) {
 struct MoeTables {
     uint32_t mask[2][kMaxExperts];     // the tokens of a local expert
     float c[kMaxPairs];                // by token and rank
+    float pair_c[kMaxPairs];           // by pair
     int16_t chosen[kMaxPairs];
     uint16_t first[kMaxExperts];       // a local expert's first pair
     uint16_t pass_expert[kMaxPairs], pass_first[kMaxPairs];
@@ -719,6 +727,12 @@ struct MoeTables {
     uint32_t total;                    // pairs << 16 | passes
     uint32_t stop;
 };
+
+// The pair of a local expert and one of its tokens.
+__device__ __forceinline__ int pair_of(const MoeTables& tab, int local, int t) {
+    const uint32_t m0 = tab.mask[0][local], m1 = tab.mask[1][local];
+    return tab.first[local] + (t < 32 ? __popc(m0 & ((1u << t) - 1)) : __popc(m0) + __popc(m1 & ((1u << (t - 32)) - 1)));
+}
 
 // Logits of 16 tokens from t0 and 8 experts from e0: a block's warps share the
 // columns, tokens are operand A, router rows operand B.  red: 8 KB.
@@ -768,85 +782,97 @@ __device__ __forceinline__ void logit_item(const MoeArgs& a, int e0, int t0, flo
     __syncthreads();
 }
 
-// One warp: the softmax and the top_k experts of tokens warp, warp + kWarps, ...
-// kEach: experts of a lane.
+// Notes choice i, of token t.
+__device__ __forceinline__ void take_choice(const MoeArgs& a, MoeTables& tab, int i, int t, int id, float c) {
+    const int local = id - a.first;
+    tab.chosen[i] = int16_t(id);
+    tab.c[i] = c;
+    if (local >= 0 && local < a.n_local) atomicOr(&tab.mask[t >> 5][local], 1u << (t & 31));
+    if (blockIdx.x == 0) {
+        if (a.ids) a.ids[i] = id;
+        if (a.weights) a.weights[i] = c;
+    }
+}
+
+// One warp: the softmax and the top_k experts of token t.  kEach: experts of a
+// lane, every 32nd.  far: for every block to read, else for this one.
 template <int kEach>
-__device__ __forceinline__ void choose(const MoeArgs& a, MoeTables& tab, int warp, int lane) {
-    constexpr int kTokens = RR_MOE_MAX_TOKENS / kWarps;
-    float l[kTokens][kEach];
+__device__ __forceinline__ void choose(const MoeArgs& a, MoeTables& tab, int t, int lane, bool far) {
+    const float* const row = a.logits + t * a.n_experts;
+    float l[kEach];
+    uint32_t key[kEach];
 #pragma unroll
-    for (int q = 0; q < kTokens; ++q)
+    for (int i = 0; i < kEach; ++i) l[i] = 32 * i + lane < a.n_experts ? __ldcg(row + 32 * i + lane) : 0.0f;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int t = warp + q * kWarps, e = 32 * i + lane;
-            l[q][i] = t < a.tokens && e < a.n_experts ? __ldcg(a.logits + t * a.n_experts + e) : 0.0f;
-        }
+    for (int i = 0; i < kEach; ++i) key[i] = 32 * i + lane < a.n_experts ? rank_key(l[i]) : 0;
+    float top = 0.0f, mine = 0.0f;
+    int my_id = 0;
+    for (int j = 0; j < a.top_k; ++j) {
+        // The largest key; of equal ones, the lowest index.
+        uint32_t best = 0;
 #pragma unroll
-    for (int q = 0; q < kTokens; ++q) {
-        const int t = warp + q * kWarps;
-        if (t >= a.tokens) break;
-        uint32_t key[kEach];
-        float top = -INFINITY;
+        for (int i = 0; i < kEach; ++i) best = max(best, key[i]);
+        best = __reduce_max_sync(~0u, best);
+        uint32_t at = ~0u;
+        float lv = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const bool in = 32 * i + lane < a.n_experts;
-            key[i] = in ? rank_key(l[q][i]) : 0;
-            if (in) top = fmaxf(top, l[q][i]);
-        }
-#pragma unroll
-        for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-        float sum = 0.0f;
+        for (int i = kEach - 1; i >= 0; --i)
+            if (key[i] == best) at = 32 * i + lane, lv = l[i];
+        const uint32_t e = __reduce_min_sync(~0u, at);
+        lv = __shfl_sync(~0u, lv, e & 31);
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
-            if (32 * i + lane < a.n_experts) sum += expf(l[q][i] - top);
-        sum = warp_sum(sum);
-        float mine = -INFINITY;
-        int my_id = 0;
-        for (int j = 0; j < a.top_k; ++j) {
-            uint32_t best = 0;
+            if (32 * i + lane == int(e)) key[i] = 0;
+        if (j == 0) top = lv;       // (NaN where there is one: so are the weights)
+        if (lane == j) mine = lv, my_id = int(e);
+    }
+    float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) best = max(best, key[i]);
-            best = __reduce_max_sync(~0u, best);
-            uint32_t at = ~0u;
-            float lv = 0.0f;
-#pragma unroll
-            for (int i = kEach - 1; i >= 0; --i)
-                if (key[i] == best) at = 32 * i + lane, lv = l[q][i];
-            const uint32_t e = __reduce_min_sync(~0u, at);
-            lv = __shfl_sync(~0u, lv, e & 31);
-#pragma unroll
-            for (int i = 0; i < kEach; ++i)
-                if (32 * i + lane == int(e)) key[i] = 0;
-            if (lane == j) mine = lv, my_id = int(e);
-        }
-        float p = lane < a.top_k ? expf(mine - top) / sum : 0.0f;
-        if (a.norm) p /= warp_sum(p);
-        if (lane < a.top_k) {
-            const int i = t * a.top_k + lane;
-            tab.chosen[i] = int16_t(my_id);
-            tab.c[i] = p;
-            const int local = my_id - a.first;
-            if (local >= 0 && local < a.n_local) atomicOr(&tab.mask[t >> 5][local], 1u << (t & 31));
-            if (blockIdx.x == 0) {
-                if (a.ids) a.ids[i] = my_id;
-                if (a.weights) a.weights[i] = p;
-            }
+    for (int i = 0; i < kEach; ++i)
+        if (32 * i + lane < a.n_experts) sum += expf(l[i] - top);
+    sum = warp_sum(sum);
+    float p = lane < a.top_k ? expf(mine - top) / sum : 0.0f;
+    if (a.norm) p /= warp_sum(p);
+    if (lane < a.top_k) {
+        const int i = t * a.top_k + lane;
+        if (far) {
+            __stcg(a.far_chosen + i, my_id);
+            __stcg(a.far_c + i, p);
+        } else {
+            take_choice(a, tab, i, t, my_id, p);
         }
     }
 }
 
-// Waits until every block has arrived; false when the wait ran out (about two
-// seconds), which marks the workspace.
-__device__ bool grid_barrier(const MoeArgs& a, MoeTables& tab, int which) {
+// A barrier of all blocks, in two halves.  What a block wrote before it arrived is
+// there for every block that has waited.  Within one cluster it is the hardware's;
+// else the wait is bounded: false when it ran out (about two seconds), which marks
+// the workspace, or when an earlier call's did.
+__device__ __forceinline__ void grid_arrive(const MoeArgs& a, int which) {
+    if (a.one) {
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        return;
+    }
     __syncthreads();
+    if (threadIdx.x == 0)
+        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(&a.control->barrier[which]) : "memory");
+}
+__device__ __forceinline__ bool grid_wait(const MoeArgs& a, MoeTables& tab, int which) {
+    if (a.one) {
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+        return true;
+    }
     if (threadIdx.x == 0) {
-        uint32_t* const b = &a.control->barrier[which];
-        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(b) : "memory");
         uint32_t seen = 0;
         long long since = 0;
         for (;;) {
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(b) : "memory");
-            if (seen >= gridDim.x) break;
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(&a.control->barrier[which]) : "memory");
+            if (seen >= gridDim.x) {
+                // A call whose wait ran out may have left counts behind.
+                asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(&a.control->error) : "memory");
+                tab.stop = seen;
+                break;
+            }
             long long now;
             asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
             if (since == 0) since = now;
@@ -868,46 +894,48 @@ struct MoePhase {
     int blocks;            // of a strip
     int f0, n;             // this block's items: pass f / strips, strip f % strips
     int team, batch;
+    int strips;
+    uint32_t inverse;      // 2^32 / strips, rounded up: exact for f * strips <= 2^32
+    __device__ __forceinline__ int pass(int f) const {
+        return strips == 1 ? f : int(__umulhi(uint32_t(f), inverse));
+    }
     // Items between two joins, all of one pass.
     __device__ __forceinline__ int batch_end(int i0) const {
-        const int strips = int(m.strips), f = f0 + i0;
-        return min(min(i0 + batch, n), (f / strips + 1) * strips - f0);
+        return min(min(i0 + batch, n), (pass(f0 + i0) + 1) * strips - f0);
     }
 };
 
-// The order in which a warp takes a phase's blocks of weights.
+// The order in which a warp takes the blocks of weights of a run of items.
 template <int W>
 struct Feed {
     Weights<W> w;
-    int phase, i, i1, b;
-    // The next item of this warp from batch i0 on; moves to the next phase at the end.
-    __device__ __forceinline__ void find(const MoePhase* ph, const MoeTables& tab, int i0, int warp, int lane) {
-        while (phase < 2) {
-            const MoePhase& p = ph[phase];
-            const int part = warp % p.team, team = warp / p.team;
-            if (part < p.blocks) {
-                while (i0 < p.n) {
-                    i1 = p.batch_end(i0);
-                    i = i0 + team;
-                    if (i < i1) {
-                        aim(p, tab, part, lane);
-                        return;
-                    }
-                    i0 = i1;
-                }
-            }
-            ++phase;
-            i0 = 0;
-        }
-    }
+    int i, i1, b;
+    bool done;
     __device__ __forceinline__ void aim(const MoePhase& p, const MoeTables& tab, int part, int lane) {
-        const int strips = int(p.m.strips), f = p.f0 + i;
+        const int f = p.f0 + i, pass = p.pass(f);
         b = part;
-        w.seek(p.base, tab.pass_expert[f / strips], p.m, f % strips, b, lane);
+        w.seek(p.base, tab.pass_expert[pass], p.m, f - pass * p.strips, b, lane);
     }
-    __device__ __forceinline__ void load(const MoePhase* ph, const MoeTables& tab, uint32_t to, int warp, int lane) {
-        if (phase < 2) {
-            const MoePhase& p = ph[phase];
+    // The first item of this warp from batch i0 on.
+    __device__ __forceinline__ void find(const MoePhase& p, const MoeTables& tab, int i0, int warp, int lane) {
+        const int part = warp % p.team, team = warp / p.team;
+        if (part < p.blocks) {
+            while (i0 < p.n) {
+                i1 = p.batch_end(i0);
+                i = i0 + team;
+                if (i < i1) {
+                    aim(p, tab, part, lane);
+                    done = false;
+                    return;
+                }
+                i0 = i1;
+            }
+        }
+        done = true;
+    }
+    // The next block to a stage; an empty group when there is none.
+    __device__ __forceinline__ void load(const MoePhase& p, const MoeTables& tab, uint32_t to, int warp, int lane) {
+        if (!done) {
             w.load(to, p.base, lane);
             b += p.team;
             if (b < p.blocks) {
@@ -915,10 +943,19 @@ struct Feed {
             } else {
                 i += kWarps / p.team;
                 if (i < i1) aim(p, tab, warp % p.team, lane);
-                else find(ph, tab, i1, warp, lane);
+                else find(p, tab, i1, warp, lane);
             }
         }
         copy_commit();
+    }
+    // Starts on a run: all stages but one, from `slot` on.
+    __device__ __forceinline__ void start(const MoePhase& p, const MoeTables& tab, uint32_t fifo, int slot, int warp,
+                                          int lane) {
+        find(p, tab, 0, warp, lane);
+        for (int k = 0; k < Weights<W>::kStages - 1; ++k) {
+            load(p, tab, fifo + slot * Weights<W>::kBytes, warp, lane);
+            slot = slot + 1 == Weights<W>::kStages ? 0 : slot + 1;
+        }
     }
 };
 
@@ -1011,7 +1048,7 @@ __device__ __forceinline__ void moe_batch(const MoeArgs& a, const MoePhase* ph, 
     }
 
     auto put_item = [&](int i, int ln, int n, const float (&v)[4]) {
-        const int strip = (p.f0 + i) % int(p.m.strips);
+        const int strip = p.f0 + i - p.pass(p.f0 + i) * p.strips;
         const int64_t lo = p.m.row(strip, ln >> 2), hi = p.m.row(strip, 8 + (ln >> 2));
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -1036,16 +1073,16 @@ __device__ __forceinline__ void moe_batch(const MoeArgs& a, const MoePhase* ph, 
         float sum[NT][4] = {};
         int shift_lo = 0, shift_hi = 0;
         if constexpr (W == 1) {
-            const int f = p.f0 + i, strips = int(p.m.strips);
+            const int f = p.f0 + i, pass = p.pass(f);
             Weights<1> w;
-            w.seek(p.base, tab.pass_expert[f / strips], p.m, f % strips, 0, lane);
+            w.seek(p.base, tab.pass_expert[pass], p.m, f - pass * p.strips, 0, lane);
             shift_lo = int(reinterpret_cast<uintptr_t>(w.lo) & 15);
             shift_hi = int(reinterpret_cast<uintptr_t>(w.hi) & 15);
         }
         for (int b = part; b < p.blocks; b += p.team) {
             copy_wait<kStages - 2>();
             __syncwarp();      // what lanes share is there, and the last stage has been read
-            feed.load(ph, tab, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
+            feed.load(p, tab, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
             moe_block<T, W, NT, kParts>(sum, fifo + slot * kBytes, x, a.cap * a.h_pitch,
                                         b * (2 * Weights<W>::kCols), shift_lo, shift_hi, lane);
             slot = slot + 1 == kStages ? 0 : slot + 1;
@@ -1072,12 +1109,12 @@ __device__ __forceinline__ void moe_batch(const MoeArgs& a, const MoePhase* ph, 
 }
 
 template <class T, int W, int PHASE>
-__device__ __forceinline__ void moe_phase(const MoeArgs& a, const MoePhase* ph, MoeTables& tab, Feed<W>& feed,
+__device__ __forceinline__ void moe_phase(const MoeArgs& a, MoePhase* ph, MoeTables& tab, Feed<W>& feed,
                                           char* fifo, int& slot, char* region, float4* red) {
     const MoePhase& p = ph[PHASE];
     int staged = -1;
     for (int i0 = 0; i0 < p.n;) {
-        const int i1 = p.batch_end(i0), pass = (p.f0 + i0) / int(p.m.strips);
+        const int i1 = p.batch_end(i0), pass = p.pass(p.f0 + i0);
         const int first = tab.pass_first[pass], count = tab.pass_count[pass];
         if (pass != staged && !(PHASE == 0 && a.all_x)) {
             __syncthreads();
@@ -1091,6 +1128,165 @@ __device__ __forceinline__ void moe_phase(const MoeArgs& a, const MoePhase* ph, 
         i0 = i1;
     }
 }
+
+// The second phase for few tokens, whose every h fits a block's shared memory: an
+// item is a strip of the output over all chosen experts, a warp takes every 16th
+// of its blocks of weights, and the block joins the warps' sums.  No pair's part
+// goes through memory, and no barrier follows.
+template <int W>
+struct FoldFeed {
+    Weights<W> w;
+    int strip, end, pass, b;
+    __device__ __forceinline__ void load(const MoePhase& p, const MoeTables& tab, int passes, uint32_t to, int warp,
+                                         int lane) {
+        if (strip < end) {
+            w.seek(p.base, tab.pass_expert[pass], p.m, strip, b, lane);
+            w.load(to, p.base, lane);
+            next(p, passes, warp);
+        }
+        copy_commit();
+    }
+    __device__ __forceinline__ void next(const MoePhase& p, int passes, int warp) {
+        b += kWarps;
+        wrap(p);
+        if (pass >= passes) ++strip, first(p, passes, warp);
+    }
+    __device__ __forceinline__ void first(const MoePhase& p, int passes, int warp) {
+        pass = 0;
+        b = warp;
+        wrap(p);
+        if (pass >= passes) strip = end;     // fewer blocks than warps: none here
+    }
+    __device__ __forceinline__ void wrap(const MoePhase& p) {
+        while (b >= p.blocks) b -= p.blocks, ++pass;
+    }
+};
+
+template <class T, int W>
+__device__ __forceinline__ void stage_fold(const MoeArgs& a, MoeTables& tab, char* region, int pairs, int cols) {
+    const bool half = std::is_same<T, F16>::value;
+    if (half) {
+        // One power of two for all of a token's parts of the sum.
+        if (threadIdx.x < a.tokens) {
+            float top = 0.0f;
+            for (int j = 0; j < a.top_k; ++j) {
+                const int k = threadIdx.x * a.top_k + j, local = tab.chosen[k] - a.first;
+                if (local < 0 || local >= a.n_local) continue;
+                const float v = tab.c[k] * __uint_as_float(__ldcg(a.h_top + pair_of(tab, local, threadIdx.x)));
+                if (v < INFINITY) top = fmaxf(top, v);
+            }
+            const int e = h_exponent(__float_as_uint(top));
+            tab.scale[threadIdx.x] = ldexpf(1.0f, -e);
+            tab.scale[8 + threadIdx.x] = ldexpf(1.0f, e);
+        }
+        __syncthreads();
+    }
+    const int chunks = cols / 4, apart = a.fold * a.h_pitch;
+#pragma unroll 4
+    for (int k = threadIdx.x; k < (pairs + 1) * chunks; k += kProdThreads) {
+        const int i = k / chunks, c = 4 * (k % chunks);
+        float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float up = 0.0f;
+        if (i < pairs) {
+            if (c < a.inter) f = __ldcg(reinterpret_cast<const float4*>(a.h + int64_t(i) * a.h_ld + c));
+            up = tab.pair_c[i];
+            if (half) up *= tab.scale[8 + tab.token[i]];
+        }
+        const float v[4] = {f.x, f.y, f.z, f.w};
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float s = i < pairs && c + q < a.inter ? v[q] * up : 0.0f;
+            hi[q] = T::round(s);
+            const float rest = s - T::widen(uint16_t(hi[q]));
+            lo[q] = T::round(isfinite(rest) ? rest : 0.0f);
+        }
+        // The row of zeros that absent tokens read is the last.
+        char* const dst = region + (i < pairs ? i : a.fold - 1) * a.h_pitch + 2 * c;
+        *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+        *reinterpret_cast<uint2*>(dst + apart) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+    }
+}
+
+template <class T, int W>
+__device__ __forceinline__ void moe_fold(const MoeArgs& a, const MoePhase& p, MoeTables& tab, FoldFeed<W>& feed,
+                                         char* fifo, int& slot, const char* region, float4* red, int passes) {
+    constexpr int kStages = Weights<W>::kStages, kBytes = Weights<W>::kBytes;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int apart = a.fold * a.h_pitch;
+    const uint32_t fifo_at = smem_at(fifo);
+    for (int strip = p.f0; strip < p.f0 + p.n; ++strip) {
+        float sum[1][4] = {};
+        int b = warp, pass = 0;
+        for (;;) {
+            while (b >= p.blocks) b -= p.blocks, ++pass;
+            if (pass >= passes) break;
+            const int e = tab.pass_expert[pass];
+            const uint32_t mask = tab.mask[0][e];
+            const int row = mask >> g & 1 ? tab.first[e] + __popc(mask & ((1u << g) - 1)) : a.fold - 1;
+            const char* const x[1] = {region + row * a.h_pitch + 16 * t};
+            int shift_lo = 0, shift_hi = 0;
+            if constexpr (W == 1) {
+                Weights<1> w;
+                w.seek(p.base, e, p.m, strip, 0, lane);
+                shift_lo = int(reinterpret_cast<uintptr_t>(w.lo) & 15);
+                shift_hi = int(reinterpret_cast<uintptr_t>(w.hi) & 15);
+            }
+            copy_wait<kStages - 2>();
+            __syncwarp();
+            feed.load(p, tab, passes, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
+            moe_block<T, W, 1, 2>(sum, fifo + slot * kBytes, x, apart, b * (2 * Weights<W>::kCols), shift_lo, shift_hi,
+                                  lane);
+            slot = slot + 1 == kStages ? 0 : slot + 1;
+            b += kWarps;
+        }
+        red[threadIdx.x] = make_float4(sum[0][0], sum[0][1], sum[0][2], sum[0][3]);
+        __syncthreads();
+        if (threadIdx.x < 128) {
+            const int i = threadIdx.x, tok = 2 * (i / 4 % 4) + (i & 1);
+            float v = 0.0f;
+#pragma unroll
+            for (int q = 0; q < kWarps; ++q) v += reinterpret_cast<const float*>(red)[128 * q + i];
+            const int64_t n = p.m.row(strip, i / 16 + 8 * (i >> 1 & 1));
+            if (tok < a.tokens && n >= 0) {
+                if (std::is_same<T, F16>::value) v *= tab.scale[tok];
+                a.out[tok * a.ldo + n] = T::round(v);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Items that a block is about to take, to L2: HBM then has work while the blocks
+// wait for one another.  (The rows of a strip, and a packed strip, are one run.)
+template <int W>
+__device__ __forceinline__ void prefetch_item(const MoePhase& p, int expert, int strip) {
+    const char* at;
+    int64_t bytes;
+    if (W >= 32) {
+        at = p.base + expert * p.m.matrix_bytes + strip * p.m.blocks * block_bytes(W >= 32 ? W : 128);
+        bytes = p.m.blocks * block_bytes(W >= 32 ? W : 128);
+    } else {
+        at = p.base + (expert * p.m.rows + int64_t(strip) * kStrip) * p.m.cols * 2;
+        bytes = min(int64_t(kStrip), p.m.rows - int64_t(strip) * kStrip) * p.m.cols * 2;
+    }
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at), "r"(uint32_t(bytes)) : "memory");
+}
+
+// The last block to finish leaves the counters at zero for the next call.
+__device__ __forceinline__ void finish(const MoeArgs& a) {
+    if (a.one) return;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        if (atomicAdd(&a.control->left, 1u) == gridDim.x - 1) {
+            for (int i = 0; i < 4; ++i) a.control->barrier[i] = 0;
+            a.control->left = 0;
+        }
+    }
+}
+
+constexpr int kPrefetch = 8;       // strips of the second phase that a block asks for ahead
 
 // The whole layer in one cooperative launch, one block per SM:
 //   logits, a warp per expert row and 8 tokens          | barrier
@@ -1111,28 +1307,38 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
     float4* const red = reinterpret_cast<float4*>(smem + kFifo);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 
-    if (threadIdx.x == 0) {
-        uint32_t e;
-        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(e) : "l"(&a.control->error) : "memory");
-        tab.stop = e;
-    }
+    after_previous();
+    if (threadIdx.x == 0) tab.stop = 0;
     for (int i = threadIdx.x; i < a.n_local; i += kProdThreads) tab.mask[0][i] = tab.mask[1][i] = 0;
-    __syncthreads();
-    if (tab.stop) return;
 
-    // Logits; meanwhile, tokens to shared memory, where all of them fit.
+    // Logits; then, while other blocks are at theirs, tokens to shared memory where all of them fit.
     {
         const int groups = (a.n_experts + 7) / 8;
         for (int i = blockIdx.x; i < groups * ((a.tokens + 15) / 16); i += gridDim.x)
             logit_item<T>(a, i % groups * 8, i / groups * 16, reinterpret_cast<float4*>(smem));
-        if (a.all_x) stage_tokens(a, tab, region, 0, a.tokens, (a.hidden + Weights<W>::kCols - 1) / Weights<W>::kCols * Weights<W>::kCols);
         if (blockIdx.x == gridDim.x - 1)
             for (int i = threadIdx.x; i < a.tokens * min(a.top_k, a.n_local); i += kProdThreads) a.h_top[i] = 0;
+        grid_arrive(a, 0);
+        if (a.all_x) {
+            constexpr int kCols = Weights<W>::kCols;
+            stage_tokens(a, tab, region, 0, a.tokens, (a.hidden + kCols - 1) / kCols * kCols);
+        }
     }
-    if (!grid_barrier(a, tab, 0)) return;
+    if (!grid_wait(a, tab, 0)) return;
 
-    if (a.n_experts <= 128) choose<4>(a, tab, warp, lane);
-    else choose<kMaxExperts / 32>(a, tab, warp, lane);
+    // Up to a token a warp, every block chooses for itself; more tokens are shared out
+    // over the blocks (64 of them took every block 9 us, against 2 and a barrier).
+    const bool far = a.tokens > kWarps;
+    for (int t = far ? warp * gridDim.x + blockIdx.x : warp; t < a.tokens; t += far ? kWarps * gridDim.x : kWarps) {
+        if (a.n_experts <= 128) choose<4>(a, tab, t, lane, far);
+        else choose<kMaxExperts / 32>(a, tab, t, lane, far);
+    }
+    if (far) {
+        grid_arrive(a, 3);
+        if (!grid_wait(a, tab, 3)) return;
+        for (int i = threadIdx.x; i < a.tokens * a.top_k; i += kProdThreads)
+            take_choice(a, tab, i, i / a.top_k, __ldcg(a.far_chosen + i), __ldcg(a.far_c + i));
+    }
     __syncthreads();
     // Pairs by expert, then token; passes of up to `cap` tokens of one expert.
     {
@@ -1147,34 +1353,47 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
         }
         if (lane == 31) tab.scan[warp] = v;
         __syncthreads();
-        uint32_t before = 0;
-        for (int q = 0; q < warp; ++q) before += tab.scan[q];
-        v += before;
+        uint32_t warps = lane < kWarps ? tab.scan[lane] : 0;      // every warp adds up the warps' sums
+#pragma unroll
+        for (int o = 1; o < kWarps; o *= 2) {
+            const uint32_t u = __shfl_up_sync(~0u, warps, o);
+            if (lane >= o) warps += u;
+        }
+        const uint32_t before = __shfl_sync(~0u, warps, (warp + 31) & 31);
+        v += warp ? before : 0;
         if (threadIdx.x == kProdThreads - 1) tab.total = v;
         v -= own;
-        int pair = int(v >> 16), pass = int(v & 0xFFFF);
+        const int pair = int(v >> 16);
+        int pass = int(v & 0xFFFF);
         if (e < a.n_local) tab.first[e] = uint16_t(pair);
         for (int q = 0; q < passes; ++q, ++pass) {
             tab.pass_expert[pass] = uint16_t(e);
             tab.pass_first[pass] = uint16_t(pair + q * a.cap);
             tab.pass_count[pass] = uint8_t(min(a.cap, count - q * a.cap));
         }
-        for (uint32_t m = m0; m; m &= m - 1) tab.token[pair++] = uint8_t(__ffs(m) - 1);
-        for (uint32_t m = m1; m; m &= m - 1) tab.token[pair++] = uint8_t(31 + __ffs(m));
         __syncthreads();
     }
-    // The phases' items, and the team of the fewest rounds (a join costs one):
-    // lane 8 k + i looks at phase k and teams of 2^i.
-    if (warp == 0) {
+    if (warp < kWarps - 1) {
+        for (int i = threadIdx.x; i < a.tokens * a.top_k; i += kProdThreads - 32) {
+            const int local = tab.chosen[i] - a.first, t = i / a.top_k;
+            if (local < 0 || local >= a.n_local) continue;
+            const int pair = pair_of(tab, local, t);
+            tab.token[pair] = uint8_t(t);
+            tab.pair_c[pair] = tab.c[i];
+        }
+    } else {
+        // The phases' items, and the team of the fewest rounds (a join costs one):
+        // lane 8 k + i looks at phase k and teams of 2^i.
         const int k = lane >> 3 & 1, team = 1 << min(lane & 7, 4), teams = kWarps / team;
         const int passes = int(tab.total & 0xFFFF);
         const int cols = k ? a.inter : a.hidden, strips = k ? (a.hidden + 15) / 16 : (a.inter + 7) / 8;
         const int blocks = (cols + Weights<W>::kCols - 1) / Weights<W>::kCols;
-        const int all = passes * strips, grid = gridDim.x;      // under 2^31: 1024 passes of 2048 strips
-        const int most = (all + grid - 1) / grid;
+        const uint32_t all = k && a.fold ? strips : passes * strips;    // at most 1024 passes of 2048 strips
+        const uint32_t grid = gridDim.x, most = (all + grid - 1) / grid;
         const int batch = team == 1 ? INT_MAX / 2 : kJoinBytes / (512 * (a.tokens > 8 ? 2 : 1) * team) / teams * teams;
-        const int cost = (most + teams - 1) / teams * ((blocks + team - 1) / team) + (team == 1 ? 0 : (most + batch - 1) / batch);
-        uint32_t best = uint32_t(min(cost, 0xFFFFFF)) << 3 | uint32_t(min(lane & 7, 4));
+        const uint32_t cost =
+            (most + teams - 1) / teams * ((blocks + team - 1) / team) + (team == 1 ? 0 : (most + batch - 1) / batch);
+        uint32_t best = min(cost, 0xFFFFFFu) << 3 | uint32_t(min(lane & 7, 4));
         const uint32_t own = best;
         for (int o = 1; o < 8; o *= 2) best = min(best, __shfl_xor_sync(~0u, best, o));
         if (lane < 16 && own == best && (lane & 7) <= 4) {
@@ -1187,8 +1406,11 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
             p.m.blocks = (cols + kBlock - 1) / kBlock;
             p.m.matrix_bytes = p.m.strips * p.m.blocks * block_bytes(W >= 32 ? W : 128);
             p.blocks = blocks;
-            p.f0 = int(int64_t(blockIdx.x) * all / grid);
-            p.n = int(int64_t(blockIdx.x + 1) * all / grid) - p.f0;
+            // (Products under 2^32 for grids of up to 1024 blocks.)
+            p.f0 = int(blockIdx.x * all / grid);
+            p.n = int((blockIdx.x + 1) * all / grid) - p.f0;
+            p.strips = strips;
+            p.inverse = uint32_t(0xFFFFFFFFu / uint32_t(strips)) + 1;
             p.team = team;
             p.batch = batch;
             ph[k] = p;
@@ -1199,48 +1421,75 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
     char* const fifo = smem + warp * (Weights<W>::kStages * Weights<W>::kBytes);
     int slot = 0;
     Feed<W> feed;
-    feed.phase = 0;
-    feed.find(ph, tab, 0, warp, lane);
-    for (int i = 0; i < Weights<W>::kStages - 1; ++i)
-        feed.load(ph, tab, smem_at(fifo) + i * Weights<W>::kBytes, warp, lane);
-
+    feed.start(ph[0], tab, smem_at(fifo), slot, warp, lane);
     moe_phase<T, W, 0>(a, ph, tab, feed, fifo, slot, region, red);
-    if (!grid_barrier(a, tab, 1)) {
+    grid_arrive(a, 1);
+    const int passes = int(tab.total & 0xFFFF);
+    if (a.fold) {
+        FoldFeed<W> fold;
+        fold.strip = ph[1].f0;
+        fold.end = ph[1].f0 + ph[1].n;
+        fold.first(ph[1], passes, warp);
+        for (int i = 0, to = slot; i < Weights<W>::kStages - 1; ++i) {
+            fold.load(ph[1], tab, passes, smem_at(fifo) + to * Weights<W>::kBytes, warp, lane);
+            to = to + 1 == Weights<W>::kStages ? 0 : to + 1;
+        }
+        if (W != 1 && int(threadIdx.x) < passes && ph[1].n > 0)
+            prefetch_item<W>(ph[1], tab.pass_expert[threadIdx.x], ph[1].f0);
+        if (!grid_wait(a, tab, 1)) {
+            copy_wait<0>();
+            return;
+        }
+        stage_fold<T, W>(a, tab, region, int(tab.total >> 16), ph[1].blocks * Weights<W>::kCols);
+        __syncthreads();
+        moe_fold<T, W>(a, ph[1], tab, fold, fifo, slot, region, red, passes);
+        copy_wait<0>();
+        finish(a);
+        return;
+    }
+    feed.start(ph[1], tab, smem_at(fifo), slot, warp, lane);
+    if (W != 1 && int(threadIdx.x) < min(ph[1].n, kPrefetch)) {
+        const int f = ph[1].f0 + threadIdx.x, pass = ph[1].pass(f);
+        prefetch_item<W>(ph[1], tab.pass_expert[pass], f - pass * ph[1].strips);
+    }
+    if (!grid_wait(a, tab, 1)) {
         copy_wait<0>();
         return;
     }
     moe_phase<T, W, 1>(a, ph, tab, feed, fifo, slot, region, red);
     copy_wait<0>();
-    if (!grid_barrier(a, tab, 2)) return;
+    grid_arrive(a, 2);
+    if (!grid_wait(a, tab, 2)) return;
 
     // A warp takes 128 columns of a token.
     const int parts = (a.hidden + 127) / 128;
     for (int i = warp * gridDim.x + blockIdx.x; i < a.tokens * parts; i += kWarps * gridDim.x) {
         const int t = i / parts, n = i % parts * 128 + 4 * lane;
         float sum[4] = {};
-#pragma unroll 8
-        for (int j = 0; j < a.top_k; ++j) {
-            const int e = tab.chosen[t * a.top_k + j] - a.first;
-            if (e < 0 || e >= a.n_local || n >= a.hidden) continue;
-            const uint32_t m0 = tab.mask[0][e], m1 = tab.mask[1][e];
-            const int before = t < 32 ? __popc(m0 & ((1u << t) - 1)) : __popc(m0) + __popc(m1 & ((1u << (t - 32)) - 1));
-            const float c = tab.c[t * a.top_k + j];
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(a.y + int64_t(tab.first[e] + before) * a.y_ld + n));
-            sum[0] += c * y.x, sum[1] += c * y.y, sum[2] += c * y.z, sum[3] += c * y.w;
+        for (int j0 = 0; j0 < a.top_k; j0 += 8) {
+            float4 y[8];
+            float c[8];
+            bool here[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {      // every load before the first sum
+                const int k = t * a.top_k + min(j0 + j, a.top_k - 1), e = tab.chosen[k] - a.first;
+                here[j] = j0 + j < a.top_k && e >= 0 && e < a.n_local;
+                const int le = here[j] ? e : 0;
+                const int pair = pair_of(tab, le, t);
+                c[j] = tab.c[k];
+                y[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (here[j] && n < a.hidden)
+                    y[j] = __ldcg(reinterpret_cast<const float4*>(a.y + int64_t(pair) * a.y_ld + n));
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (here[j]) sum[0] += c[j] * y[j].x, sum[1] += c[j] * y[j].y, sum[2] += c[j] * y[j].z, sum[3] += c[j] * y[j].w;
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q)
             if (n + q < a.hidden) a.out[t * a.ldo + n + q] = T::round(sum[q]);
     }
-    // The last block to finish leaves the counters at zero for the next call.
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        if (atomicAdd(&a.control->left, 1u) == gridDim.x - 1) {
-            a.control->barrier[0] = a.control->barrier[1] = a.control->barrier[2] = 0;
-            a.control->left = 0;
-        }
-    }
+    finish(a);
 }
 
 // ---------------------------------------------------------------------------
@@ -1340,7 +1589,7 @@ rr_status check_moe(const rr_moe_layer* L) {
 
 // Workspace: a control block, then the arrays.  Offsets in bytes.
 struct MoeSpace {
-    int64_t logits, top, h, y, total;
+    int64_t logits, top, chosen, c, h, y, total;
     int32_t h_ld, y_ld;
 };
 constexpr int64_t kControlBytes = 256;
@@ -1354,7 +1603,9 @@ MoeSpace moe_space(const rr_moe_layer* L, int64_t tokens) {
     s.h_ld = int32_t((L->inter + 3) / 4 * 4);
     s.y_ld = int32_t((L->hidden + 3) / 4 * 4);
     s.top = s.logits + up16(4 * tokens * L->n_experts);
-    s.h = s.top + up16(4 * pairs);
+    s.chosen = s.top + up16(4 * pairs);
+    s.c = s.chosen + up16(4 * tokens * L->top_k);
+    s.h = s.c + up16(4 * tokens * L->top_k);
     s.y = s.h + 4 * pairs * s.h_ld;
     s.total = s.y + 4 * pairs * s.y_ld;
     return s;
@@ -1376,7 +1627,32 @@ rr_status launch_moe(MoeArgs a, cudaStream_t stream) {
     a.cap = std::min(a.cap, a.tokens);
     if (a.cap < 1) return rr_fail(RR_ELAYOUT, "hidden %d, inter %d: rows too long", a.hidden, a.inter);
     a.all_x = a.cap == a.tokens || int64_t(a.tokens) * a.x_pitch <= room;
-    const int smem = kFixed - 1024 + std::max(a.cap * each, a.all_x ? a.tokens * a.x_pitch : 0);
+    // Every h at once, for up to 8 tokens (one group of columns).
+    const int64_t rows = int64_t(a.tokens) * std::min(a.top_k, a.n_local) + 1;
+    a.fold = a.tokens <= 8 && a.cap == a.tokens && rows * 2 * a.h_pitch <= room ? int32_t(rows) : 0;
+    const int smem = kFixed - 1024 + std::max(a.fold ? a.fold * 2 * a.h_pitch : a.cap * each, a.all_x ? a.tokens * a.x_pitch : 0);
+    // A layer of little work runs in one cluster, whose barriers and whose launch
+    // cost less than a grid's, although 8 SMs then read all of its weights.
+    const int64_t bytes = std::min<int64_t>(int64_t(a.tokens) * a.top_k, a.n_local) * (a.m13_bytes + a.m2_bytes);
+    a.one = bytes <= kClusterBytes;
+    if (a.one) {
+        RR_CUDA(cudaFuncSetAttribute(rr_moe_kernel<T, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem - 1024));
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = kClusterBlocks;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(kClusterBlocks);
+        cfg.blockDim = dim3(kProdThreads);
+        cfg.dynamicSmemBytes = size_t(smem);
+        cfg.stream = stream;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        RR_CUDA(cudaLaunchKernelEx(&cfg, rr_moe_kernel<T, W>, a));
+        return RR_OK;
+    }
     static std::mutex mutex;
     static int grids[16] = {};
     int dev = 0, grid;
@@ -1394,6 +1670,8 @@ rr_status launch_moe(MoeArgs a, cudaStream_t stream) {
         }
         grid = grids[dev];
     }
+    // (Programmatic dependent launch besides left the gap between two launches at
+    // the same 4 us.)
     void* args[] = {&a};
     RR_CUDA(cudaLaunchCooperativeKernel((const void*)rr_moe_kernel<T, W>, dim3(unsigned(grid)), dim3(kProdThreads), args,
                                         size_t(smem), stream));
@@ -1694,6 +1972,8 @@ extern "C" rr_status rr_moe(const rr_moe_layer* L, const void* router, const voi
     a.h = reinterpret_cast<float*>(ws + S.h);
     a.y = reinterpret_cast<float*>(ws + S.y);
     a.h_top = reinterpret_cast<uint32_t*>(ws + S.top);
+    a.far_chosen = reinterpret_cast<int32_t*>(ws + S.chosen);
+    a.far_c = reinterpret_cast<float*>(ws + S.c);
     a.h_ld = S.h_ld;
     a.y_ld = S.y_ld;
     a.tokens = n_tokens;
@@ -1706,6 +1986,8 @@ extern "C" rr_status rr_moe(const rr_moe_layer* L, const void* router, const voi
     a.inter = int32_t(L->inter);
     a.x_vec = (uintptr_t)x % 16 == 0 && (ldx % 8 == 0 || n_tokens == 1);
     a.r_vec = L->hidden % 8 == 0;
+    a.m13_bytes = L->group ? packed_of(2 * L->inter, L->hidden, L->group, 1).matrix_bytes : 4 * L->inter * L->hidden;
+    a.m2_bytes = L->group ? packed_of(L->hidden, L->inter, L->group, 0).matrix_bytes : 2 * L->inter * L->hidden;
     return with_group(L->dtype, L->group, [&](auto t, auto g) -> rr_status {
         using T = decltype(t);
         constexpr int G = decltype(g)::value;
