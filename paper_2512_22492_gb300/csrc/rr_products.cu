@@ -589,6 +589,8 @@ struct MoeArgs {
     int32_t x_vec, r_vec;      // rows of x, of the router can be read 16 bytes at a time
     int32_t cap;               // tokens of a pass: at most 16
     int32_t x_pitch, h_pitch;  // bytes between tokens in shared memory
+    int32_t x_rows, h_rows;    // tokens' rows of x, of h that fit there
+    int32_t tiles;             // groups of 8 tokens of the largest pass possible
     int32_t all_x;             // shared memory holds every token's row
     int32_t fold;              // rows of h and one of zeros, where shared memory holds all; else 0
     int32_t one;               // the grid is one cluster
@@ -722,7 +724,8 @@ struct MoeTables {
     uint16_t pass_expert[kMaxPairs], pass_first[kMaxPairs];
     uint8_t pass_count[kMaxPairs];
     uint8_t token[kMaxPairs];          // of a pair
-    float scale[16];                   // of the pass's tokens' h (float16)
+    float scale[kMaxPairs];            // of h (float16): by pair, or by token
+    uint32_t most;                     // tokens of the largest pass
     uint32_t scan[kWarps];
     uint32_t total;                    // pairs << 16 | passes
     uint32_t stop;
@@ -899,10 +902,14 @@ struct MoePhase {
     __device__ __forceinline__ int pass(int f) const {
         return strips == 1 ? f : int(__umulhi(uint32_t(f), inverse));
     }
-    // Items between two joins, all of one pass.
-    __device__ __forceinline__ int batch_end(int i0) const {
-        return min(min(i0 + batch, n), (pass(f0 + i0) + 1) * strips - f0);
+    int window;            // passes whose tokens are in shared memory at once
+    // The end of the item's window: every `window` passes from the first one's.
+    __device__ __forceinline__ int window_end(int i) const {
+        const int first = pass(f0), w = (pass(f0 + i) - first) / window + 1;
+        return min(n, (first + w * window) * strips - f0);
     }
+    // Items between two joins, all of one window.
+    __device__ __forceinline__ int batch_end(int i0) const { return min(i0 + batch, window_end(i0)); }
 };
 
 // The order in which a warp takes the blocks of weights of a run of items.
@@ -1009,7 +1016,7 @@ __device__ __forceinline__ void stage_h(const MoeArgs& a, MoeTables& tab, char* 
         if (std::is_same<T, F16>::value) {
             const int e = h_exponent(__ldcg(a.h_top + first + i));
             up = ldexpf(1.0f, e);
-            if (c == 0) tab.scale[i] = ldexpf(1.0f, -e);
+            if (c == 0) tab.scale[first + i] = ldexpf(1.0f, -e);
         }
         const float v[4] = {f.x, f.y, f.z, f.w};
         uint32_t hi[4], lo[4];
@@ -1024,108 +1031,129 @@ __device__ __forceinline__ void stage_h(const MoeArgs& a, MoeTables& tab, char* 
         }
         char* const dst = to + i * a.h_pitch + 2 * c;
         *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-        *reinterpret_cast<uint2*>(dst + a.cap * a.h_pitch) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+        *reinterpret_cast<uint2*>(dst + a.h_rows * a.h_pitch) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
     }
 }
 
-// One pass's strips [i0, i1) of a phase.  NT: groups of 8 tokens.  The first phase
-// ends in silu(gate) * up, the second in the pair's part of the output.
-template <class T, int W, int NT, int PHASE>
-__device__ __forceinline__ void moe_batch(const MoeArgs& a, const MoePhase* ph, const MoeTables& tab, Feed<W>& feed,
-                                          char* fifo, int& slot, const char* region, float4* red, int i0, int i1,
-                                          int first, int count) {
-    constexpr int kParts = PHASE == 0 ? 1 : 2, kStages = Weights<W>::kStages, kBytes = Weights<W>::kBytes;
-    const MoePhase& p = ph[PHASE];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int team = warp / p.team, part = warp % p.team, teams = kWarps / p.team;
-    const int pitch = PHASE == 0 ? a.x_pitch : a.h_pitch;
-    const uint32_t fifo_at = smem_at(fifo);
-    const char* x[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int i = min(8 * n + g, count - 1);
-        x[n] = region + (PHASE == 0 && a.all_x ? tab.token[first + i] : i) * pitch + 16 * t;
-    }
+// A phase's items [i0, i1), whose tokens are in shared memory from pair `base` on.
+// The first phase ends in silu(gate) * up, the second in the pair's part of the
+// output.
+template <class T, int W, int PHASE>
+struct MoeBatch {
+    static constexpr int kParts = PHASE == 0 ? 1 : 2, kStages = Weights<W>::kStages, kBytes = Weights<W>::kBytes;
+    const MoeArgs& a;
+    const MoePhase& p;
+    const MoeTables& tab;
+    Feed<W>& feed;
+    char* fifo;
+    int& slot;
+    const char* region;
+    float4* red;
+    int base;
 
-    auto put_item = [&](int i, int ln, int n, const float (&v)[4]) {
-        const int strip = p.f0 + i - p.pass(p.f0 + i) * p.strips;
+    // Rows g, g + 8 of tokens 2 t, 2 t + 1 (+ 8 n) of a strip and a pass.
+    __device__ __forceinline__ void put(int pass, int strip, int ln, int n, const float (&v)[4]) const {
+        const int first = tab.pass_first[pass], count = tab.pass_count[pass];
         const int64_t lo = p.m.row(strip, ln >> 2), hi = p.m.row(strip, 8 + (ln >> 2));
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const int tok = 8 * n + 2 * (ln & 3) + k;
-            if (tok >= count) continue;
+            if (tok >= count || lo < 0) continue;
             if (PHASE == 0) {
-                if (lo < 0) continue;
                 const float h = silu(v[k]) * v[2 + k];
                 __stcg(a.h + int64_t(first + tok) * a.h_ld + lo, h);
                 if (std::is_same<T, F16>::value && fabsf(h) < INFINITY)
                     atomicMax(a.h_top + first + tok, __float_as_uint(fabsf(h)));
             } else {
-                const float s = std::is_same<T, F16>::value ? tab.scale[tok] : 1.0f;
+                const float s = std::is_same<T, F16>::value ? tab.scale[first + tok] : 1.0f;
                 float* const y = a.y + int64_t(first + tok) * a.y_ld;
-                if (lo >= 0) __stcg(y + lo, v[k] * s);
+                __stcg(y + lo, v[k] * s);
                 if (hi >= 0) __stcg(y + hi, v[2 + k] * s);
             }
         }
-    };
-
-    for (int i = i0 + team; i < i1; i += teams) {
-        float sum[NT][4] = {};
+    }
+    // This warp's blocks of an item.  NT: groups of 8 tokens.
+    template <int NT>
+    __device__ __forceinline__ void item(int i, int i0, int part) const {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+        const int f = p.f0 + i, pass = p.pass(f), strip = f - pass * p.strips;
+        const int first = tab.pass_first[pass], count = tab.pass_count[pass];
+        const int pitch = PHASE == 0 ? a.x_pitch : a.h_pitch;
+        const uint32_t fifo_at = smem_at(fifo);
+        const char* x[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int pair = first + min(8 * n + g, count - 1);
+            x[n] = region + (PHASE == 0 && a.all_x ? tab.token[pair] : pair - base) * pitch + 16 * t;
+        }
         int shift_lo = 0, shift_hi = 0;
         if constexpr (W == 1) {
-            const int f = p.f0 + i, pass = p.pass(f);
             Weights<1> w;
-            w.seek(p.base, tab.pass_expert[pass], p.m, f - pass * p.strips, 0, lane);
+            w.seek(p.base, tab.pass_expert[pass], p.m, strip, 0, lane);
             shift_lo = int(reinterpret_cast<uintptr_t>(w.lo) & 15);
             shift_hi = int(reinterpret_cast<uintptr_t>(w.hi) & 15);
         }
+        float sum[NT][4] = {};
         for (int b = part; b < p.blocks; b += p.team) {
             copy_wait<kStages - 2>();
             __syncwarp();      // what lanes share is there, and the last stage has been read
             feed.load(p, tab, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
-            moe_block<T, W, NT, kParts>(sum, fifo + slot * kBytes, x, a.cap * a.h_pitch,
+            moe_block<T, W, NT, kParts>(sum, fifo + slot * kBytes, x, a.h_rows * a.h_pitch,
                                         b * (2 * Weights<W>::kCols), shift_lo, shift_hi, lane);
             slot = slot + 1 == kStages ? 0 : slot + 1;
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            if (p.team == 1) put_item(i, lane, n, sum[n]);
+            if (p.team == 1) put(pass, strip, lane, n, sum[n]);
             else
-                red[((part * p.batch + i - i0) * NT + n) * 32 + lane] =
+                red[((part * p.batch + i - i0) * a.tiles + n) * 32 + lane] =
                     make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
         }
     }
-    if (p.team == 1) return;
-    __syncthreads();
-    for (int k = threadIdx.x; k < (i1 - i0) * NT * 32; k += kProdThreads) {
-        float v[4] = {};
-        for (int q = 0; q < p.team; ++q) {
-            const float4 f = red[q * p.batch * NT * 32 + k];
-            v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+    __device__ __forceinline__ void run(int i0, int i1) const {
+        const int warp = threadIdx.x >> 5, team = warp / p.team, part = warp % p.team, teams = kWarps / p.team;
+        for (int i = i0 + team; i < i1; i += teams) {
+            if (tab.pass_count[p.pass(p.f0 + i)] <= 8) item<1>(i, i0, part);
+            else item<2>(i, i0, part);
         }
-        put_item(i0 + k / (NT * 32), k & 31, k / 32 % NT, v);
+        if (p.team == 1) return;
+        __syncthreads();
+        for (int k = threadIdx.x; k < (i1 - i0) * a.tiles * 32; k += kProdThreads) {
+            const int i = k / (a.tiles * 32), n = k / 32 % a.tiles;
+            const int f = p.f0 + i0 + i, pass = p.pass(f);
+            if (8 * n >= tab.pass_count[pass]) continue;
+            float v[4] = {};
+            for (int q = 0; q < p.team; ++q) {
+                const float4 r = red[q * p.batch * a.tiles * 32 + k];
+                v[0] += r.x, v[1] += r.y, v[2] += r.z, v[3] += r.w;
+            }
+            put(pass, f - pass * p.strips, k & 31, n, v);
+        }
+        __syncthreads();
     }
-    __syncthreads();
-}
+};
 
+// Tokens of as many passes as fit are staged at once, so that warps go from one
+// pass to the next without meeting.
 template <class T, int W, int PHASE>
-__device__ __forceinline__ void moe_phase(const MoeArgs& a, MoePhase* ph, MoeTables& tab, Feed<W>& feed,
+__device__ __forceinline__ void moe_phase(const MoeArgs& a, const MoePhase* ph, MoeTables& tab, Feed<W>& feed,
                                           char* fifo, int& slot, char* region, float4* red) {
     const MoePhase& p = ph[PHASE];
-    int staged = -1;
     for (int i0 = 0; i0 < p.n;) {
-        const int i1 = p.batch_end(i0), pass = p.pass(p.f0 + i0);
-        const int first = tab.pass_first[pass], count = tab.pass_count[pass];
-        if (pass != staged && !(PHASE == 0 && a.all_x)) {
+        const int end = p.window_end(i0), from = p.pass(p.f0 + i0), to = p.pass(p.f0 + end - 1);
+        const int base = tab.pass_first[from], pairs = tab.pass_first[to] + tab.pass_count[to] - base;
+        if (!(PHASE == 0 && a.all_x)) {
             __syncthreads();
-            if (PHASE == 0) stage_tokens(a, tab, region, first, count, p.blocks * Weights<W>::kCols);
-            else stage_h<T>(a, tab, region, first, count, p.blocks * Weights<W>::kCols);
+            if (PHASE == 0) stage_tokens(a, tab, region, base, pairs, p.blocks * Weights<W>::kCols);
+            else stage_h<T>(a, tab, region, base, pairs, p.blocks * Weights<W>::kCols);
             __syncthreads();
-            staged = pass;
         }
-        if (count <= 8) moe_batch<T, W, 1, PHASE>(a, ph, tab, feed, fifo, slot, region, red, i0, i1, first, count);
-        else moe_batch<T, W, 2, PHASE>(a, ph, tab, feed, fifo, slot, region, red, i0, i1, first, count);
-        i0 = i1;
+        MoeBatch<T, W, PHASE> batch{a, p, tab, feed, fifo, slot, region, red, base};
+        while (i0 < end) {
+            const int i1 = p.batch_end(i0);
+            batch.run(i0, i1);
+            i0 = i1;
+        }
     }
 }
 
@@ -1308,7 +1336,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 
     after_previous();
-    if (threadIdx.x == 0) tab.stop = 0;
+    if (threadIdx.x == 0) tab.stop = tab.most = 0;
     for (int i = threadIdx.x; i < a.n_local; i += kProdThreads) tab.mask[0][i] = tab.mask[1][i] = 0;
 
     // Logits; then, while other blocks are at theirs, tokens to shared memory where all of them fit.
@@ -1345,6 +1373,8 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
         const int e = threadIdx.x;
         const uint32_t m0 = e < a.n_local ? tab.mask[0][e] : 0, m1 = e < a.n_local ? tab.mask[1][e] : 0;
         const int count = __popc(m0) + __popc(m1), passes = (count + a.cap - 1) / a.cap;
+        const uint32_t most = __reduce_max_sync(~0u, uint32_t(min(count, a.cap)));
+        if (lane == 0 && most) atomicMax(&tab.most, most);
         uint32_t v = uint32_t(count) << 16 | uint32_t(passes);
         const uint32_t own = v;
         for (int o = 1; o < 32; o *= 2) {
@@ -1382,15 +1412,16 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
             tab.pair_c[pair] = tab.c[i];
         }
     } else {
-        // The phases' items, and the team of the fewest rounds (a join costs one):
-        // lane 8 k + i looks at phase k and teams of 2^i.
+        // The phases' items, and the team that takes the busiest block least: lane
+        // 8 k + i looks at phase k and teams of 2^i.
         const int k = lane >> 3 & 1, team = 1 << min(lane & 7, 4), teams = kWarps / team;
         const int passes = int(tab.total & 0xFFFF);
         const int cols = k ? a.inter : a.hidden, strips = k ? (a.hidden + 15) / 16 : (a.inter + 7) / 8;
         const int blocks = (cols + Weights<W>::kCols - 1) / Weights<W>::kCols;
         const uint32_t all = k && a.fold ? strips : passes * strips;    // at most 1024 passes of 2048 strips
         const uint32_t grid = gridDim.x, most = (all + grid - 1) / grid;
-        const int batch = team == 1 ? INT_MAX / 2 : kJoinBytes / (512 * (a.tokens > 8 ? 2 : 1) * team) / teams * teams;
+        const int batch = team == 1 ? INT_MAX / 2 : kJoinBytes / (512 * a.tiles * team) / teams * teams;
+        // In blocks of weights: rounds of the teams, and joins.
         const uint32_t cost =
             (most + teams - 1) / teams * ((blocks + team - 1) / team) + (team == 1 ? 0 : (most + batch - 1) / batch);
         uint32_t best = min(cost, 0xFFFFFFu) << 3 | uint32_t(min(lane & 7, 4));
@@ -1413,6 +1444,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
             p.inverse = uint32_t(0xFFFFFFFFu / uint32_t(strips)) + 1;
             p.team = team;
             p.batch = batch;
+            p.window = !k && a.all_x ? 1 << 20 : max(1, (k ? a.h_rows : a.x_rows) / max(1, int(tab.most)));
             ph[k] = p;
         }
     }
@@ -1434,8 +1466,8 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
             fold.load(ph[1], tab, passes, smem_at(fifo) + to * Weights<W>::kBytes, warp, lane);
             to = to + 1 == Weights<W>::kStages ? 0 : to + 1;
         }
-        if (W != 1 && int(threadIdx.x) < passes && ph[1].n > 0)
-            prefetch_item<W>(ph[1], tab.pass_expert[threadIdx.x], ph[1].f0);
+        if (W != 1 && warp == kWarps / 2 && ph[1].n > 0)
+            for (int i = lane; i < passes; i += 32) prefetch_item<W>(ph[1], tab.pass_expert[i], ph[1].f0);
         if (!grid_wait(a, tab, 1)) {
             copy_wait<0>();
             return;
@@ -1448,8 +1480,8 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
         return;
     }
     feed.start(ph[1], tab, smem_at(fifo), slot, warp, lane);
-    if (W != 1 && int(threadIdx.x) < min(ph[1].n, kPrefetch)) {
-        const int f = ph[1].f0 + threadIdx.x, pass = ph[1].pass(f);
+    if (W != 1 && warp == kWarps / 2 && lane < min(ph[1].n, kPrefetch)) {
+        const int f = ph[1].f0 + lane, pass = ph[1].pass(f);
         prefetch_item<W>(ph[1], tab.pass_expert[pass], f - pass * ph[1].strips);
     }
     if (!grid_wait(a, tab, 1)) {
@@ -1626,11 +1658,14 @@ rr_status launch_moe(MoeArgs a, cudaStream_t stream) {
     if (a.cap > 8 && a.cap < 16) a.cap = 8;
     a.cap = std::min(a.cap, a.tokens);
     if (a.cap < 1) return rr_fail(RR_ELAYOUT, "hidden %d, inter %d: rows too long", a.hidden, a.inter);
-    a.all_x = a.cap == a.tokens || int64_t(a.tokens) * a.x_pitch <= room;
+    a.tiles = a.cap > 8 ? 2 : 1;
+    a.x_rows = room / a.x_pitch;
+    a.h_rows = room / (2 * a.h_pitch);
+    a.all_x = a.tokens <= a.x_rows;
     // Every h at once, for up to 8 tokens (one group of columns).
     const int64_t rows = int64_t(a.tokens) * std::min(a.top_k, a.n_local) + 1;
-    a.fold = a.tokens <= 8 && a.cap == a.tokens && rows * 2 * a.h_pitch <= room ? int32_t(rows) : 0;
-    const int smem = kFixed - 1024 + std::max(a.fold ? a.fold * 2 * a.h_pitch : a.cap * each, a.all_x ? a.tokens * a.x_pitch : 0);
+    a.fold = a.tokens <= 8 && a.cap == a.tokens && rows <= a.h_rows ? int32_t(rows) : 0;
+    const int smem = kFixed - 1024 + room;
     // A layer of little work runs in one cluster, whose barriers and whose launch
     // cost less than a grid's, although 8 SMs then read all of its weights.
     const int64_t bytes = std::min<int64_t>(int64_t(a.tokens) * a.top_k, a.n_local) * (a.m13_bytes + a.m2_bytes);
