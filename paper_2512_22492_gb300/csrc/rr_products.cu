@@ -590,7 +590,6 @@ struct MoeArgs {
     int32_t cap;               // tokens of a pass: at most 16
     int32_t x_pitch, h_pitch;  // bytes between tokens in shared memory
     int32_t x_rows, h_rows;    // tokens' rows of x, of h that fit there
-    int32_t tiles;             // groups of 8 tokens of the largest pass possible
     int32_t all_x;             // shared memory holds every token's row
     int32_t fold;              // rows of h and one of zeros, where shared memory holds all; else 0
     int32_t one;               // the grid is one cluster
@@ -613,7 +612,7 @@ struct Weights {
     __device__ __forceinline__ void seek(const char* base, int64_t mat, const Packed& m, int64_t strip, int b,
                                          int lane) {
         const int64_t l = m.row(strip, lane >> 2), h = m.row(strip, 8 + (lane >> 2));
-        const char* const at = base + mat * m.rows * m.cols * 2 + b * (2 * kCols);
+        const char* const at = base + mat * m.matrix_bytes + b * (2 * kCols);
         lo = l < 0 ? nullptr : at + l * m.cols * 2;
         hi = h < 0 ? nullptr : at + h * m.cols * 2;
         left = int32_t(2 * (m.cols - int64_t(b) * kCols));
@@ -896,7 +895,9 @@ struct MoePhase {
     Packed m;
     int blocks;            // of a strip
     int f0, n;             // this block's items: pass f / strips, strip f % strips
-    int team, batch;
+    int n1;                // items that a warp takes alone; the rest go to teams
+    int team, batch;       //   of warps, joined after every `batch`
+    int tiles;             // groups of 8 tokens of the largest pass
     int strips;
     uint32_t inverse;      // 2^32 / strips, rounded up: exact for f * strips <= 2^32
     __device__ __forceinline__ int pass(int f) const {
@@ -908,15 +909,18 @@ struct MoePhase {
         const int first = pass(f0), w = (pass(f0 + i) - first) / window + 1;
         return min(n, (first + w * window) * strips - f0);
     }
-    // Items between two joins, all of one window.
-    __device__ __forceinline__ int batch_end(int i0) const { return min(i0 + batch, window_end(i0)); }
+    __device__ __forceinline__ int team_at(int i) const { return i < n1 ? 1 : team; }
+    // The end of a batch: items of one window and one size of team, between two joins.
+    __device__ __forceinline__ int batch_end(int i0) const {
+        return min(i0 < n1 ? n1 : i0 + batch, window_end(i0));
+    }
 };
 
 // The order in which a warp takes the blocks of weights of a run of items.
 template <int W>
 struct Feed {
     Weights<W> w;
-    int i, i1, b;
+    int i, i1, b, team;
     bool done;
     __device__ __forceinline__ void aim(const MoePhase& p, const MoeTables& tab, int part, int lane) {
         const int f = p.f0 + i, pass = p.pass(f);
@@ -925,18 +929,16 @@ struct Feed {
     }
     // The first item of this warp from batch i0 on.
     __device__ __forceinline__ void find(const MoePhase& p, const MoeTables& tab, int i0, int warp, int lane) {
-        const int part = warp % p.team, team = warp / p.team;
-        if (part < p.blocks) {
-            while (i0 < p.n) {
-                i1 = p.batch_end(i0);
-                i = i0 + team;
-                if (i < i1) {
-                    aim(p, tab, part, lane);
-                    done = false;
-                    return;
-                }
-                i0 = i1;
+        while (i0 < p.n) {
+            team = p.team_at(i0);
+            i1 = p.batch_end(i0);
+            i = i0 + warp / team;
+            if (i < i1 && warp % team < p.blocks) {
+                aim(p, tab, warp % team, lane);
+                done = false;
+                return;
             }
+            i0 = i1;
         }
         done = true;
     }
@@ -944,12 +946,12 @@ struct Feed {
     __device__ __forceinline__ void load(const MoePhase& p, const MoeTables& tab, uint32_t to, int warp, int lane) {
         if (!done) {
             w.load(to, p.base, lane);
-            b += p.team;
+            b += team;
             if (b < p.blocks) {
-                w.skip(p.team);
+                w.skip(team);
             } else {
-                i += kWarps / p.team;
-                if (i < i1) aim(p, tab, warp % p.team, lane);
+                i += kWarps / team;
+                if (i < i1) aim(p, tab, warp % team, lane);
                 else find(p, tab, i1, warp, lane);
             }
         }
@@ -1074,7 +1076,7 @@ struct MoeBatch {
     }
     // This warp's blocks of an item.  NT: groups of 8 tokens.
     template <int NT>
-    __device__ __forceinline__ void item(int i, int i0, int part) const {
+    __device__ __forceinline__ void item(int i, int i0, int part, int team) const {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
         const int f = p.f0 + i, pass = p.pass(f), strip = f - pass * p.strips;
         const int first = tab.pass_first[pass], count = tab.pass_count[pass];
@@ -1094,7 +1096,7 @@ struct MoeBatch {
             shift_hi = int(reinterpret_cast<uintptr_t>(w.hi) & 15);
         }
         float sum[NT][4] = {};
-        for (int b = part; b < p.blocks; b += p.team) {
+        for (int b = part; b < p.blocks; b += team) {
             copy_wait<kStages - 2>();
             __syncwarp();      // what lanes share is there, and the last stage has been read
             feed.load(p, tab, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
@@ -1104,27 +1106,27 @@ struct MoeBatch {
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            if (p.team == 1) put(pass, strip, lane, n, sum[n]);
+            if (team == 1) put(pass, strip, lane, n, sum[n]);
             else
-                red[((part * p.batch + i - i0) * a.tiles + n) * 32 + lane] =
+                red[((part * p.batch + i - i0) * p.tiles + n) * 32 + lane] =
                     make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
         }
     }
     __device__ __forceinline__ void run(int i0, int i1) const {
-        const int warp = threadIdx.x >> 5, team = warp / p.team, part = warp % p.team, teams = kWarps / p.team;
-        for (int i = i0 + team; i < i1; i += teams) {
-            if (tab.pass_count[p.pass(p.f0 + i)] <= 8) item<1>(i, i0, part);
-            else item<2>(i, i0, part);
+        const int warp = threadIdx.x >> 5, team = p.team_at(i0), part = warp % team;
+        for (int i = i0 + warp / team; i < i1; i += kWarps / team) {
+            if (tab.pass_count[p.pass(p.f0 + i)] <= 8) item<1>(i, i0, part, team);
+            else item<2>(i, i0, part, team);
         }
-        if (p.team == 1) return;
+        if (team == 1) return;
         __syncthreads();
-        for (int k = threadIdx.x; k < (i1 - i0) * a.tiles * 32; k += kProdThreads) {
-            const int i = k / (a.tiles * 32), n = k / 32 % a.tiles;
+        for (int k = threadIdx.x; k < (i1 - i0) * p.tiles * 32; k += kProdThreads) {
+            const int i = k / (p.tiles * 32), n = k / 32 % p.tiles;
             const int f = p.f0 + i0 + i, pass = p.pass(f);
             if (8 * n >= tab.pass_count[pass]) continue;
             float v[4] = {};
-            for (int q = 0; q < p.team; ++q) {
-                const float4 r = red[q * p.batch * a.tiles * 32 + k];
+            for (int q = 0; q < team; ++q) {
+                const float4 r = red[q * p.batch * p.tiles * 32 + k];
                 v[0] += r.x, v[1] += r.y, v[2] += r.z, v[3] += r.w;
             }
             put(pass, f - pass * p.strips, k & 31, n, v);
@@ -1295,7 +1297,7 @@ __device__ __forceinline__ void prefetch_item(const MoePhase& p, int expert, int
         at = p.base + expert * p.m.matrix_bytes + strip * p.m.blocks * block_bytes(W >= 32 ? W : 128);
         bytes = p.m.blocks * block_bytes(W >= 32 ? W : 128);
     } else {
-        at = p.base + (expert * p.m.rows + int64_t(strip) * kStrip) * p.m.cols * 2;
+        at = p.base + expert * p.m.matrix_bytes + int64_t(strip) * kStrip * p.m.cols * 2;
         bytes = min(int64_t(kStrip), p.m.rows - int64_t(strip) * kStrip) * p.m.cols * 2;
     }
     asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at), "r"(uint32_t(bytes)) : "memory");
@@ -1314,6 +1316,10 @@ __device__ __forceinline__ void finish(const MoeArgs& a) {
     }
 }
 
+// What an item's start and end, and a join, take of a warp's time, in blocks of
+// weights (from a token's 5 or 6 items of 32 blocks a block: 10 us in teams of 8,
+// 15 in teams of 16, which by blocks alone would be the faster).
+constexpr int kItemCost = 3, kJoinCost = 2;
 constexpr int kPrefetch = 8;       // strips of the second phase that a block asks for ahead
 
 // The whole layer in one cooperative launch, one block per SM:
@@ -1412,18 +1418,19 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
             tab.pair_c[pair] = tab.c[i];
         }
     } else {
-        // The phases' items, and the team that takes the busiest block least: lane
-        // 8 k + i looks at phase k and teams of 2^i.
+        // The phases' items.  Whole rounds of 16 go to single warps, and the rest to the
+        // team that is through soonest: lane 8 k + i looks at phase k and teams of 2^i.
         const int k = lane >> 3 & 1, team = 1 << min(lane & 7, 4), teams = kWarps / team;
-        const int passes = int(tab.total & 0xFFFF);
+        const int passes = int(tab.total & 0xFFFF), tiles = tab.most > 8 ? 2 : 1;
         const int cols = k ? a.inter : a.hidden, strips = k ? (a.hidden + 15) / 16 : (a.inter + 7) / 8;
         const int blocks = (cols + Weights<W>::kCols - 1) / Weights<W>::kCols;
         const uint32_t all = k && a.fold ? strips : passes * strips;    // at most 1024 passes of 2048 strips
-        const uint32_t grid = gridDim.x, most = (all + grid - 1) / grid;
-        const int batch = team == 1 ? INT_MAX / 2 : kJoinBytes / (512 * a.tiles * team) / teams * teams;
-        // In blocks of weights: rounds of the teams, and joins.
-        const uint32_t cost =
-            (most + teams - 1) / teams * ((blocks + team - 1) / team) + (team == 1 ? 0 : (most + batch - 1) / batch);
+        const uint32_t grid = gridDim.x;
+        // (Products under 2^32 for grids of up to 1024 blocks.)
+        const int f0 = int(blockIdx.x * all / grid), n = int((blockIdx.x + 1) * all / grid) - f0, rest = n % kWarps;
+        const int batch = team == 1 ? kWarps : kJoinBytes / (512 * tiles * team) / teams * teams;
+        const uint32_t cost = (rest + teams - 1) / teams * ((blocks + team - 1) / team + kItemCost) +
+                              (team == 1 ? 0 : (rest + batch - 1) / batch * kJoinCost);
         uint32_t best = min(cost, 0xFFFFFFu) << 3 | uint32_t(min(lane & 7, 4));
         const uint32_t own = best;
         for (int o = 1; o < 8; o *= 2) best = min(best, __shfl_xor_sync(~0u, best, o));
@@ -1435,16 +1442,23 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
             p.m.pair = !k;
             p.m.strips = strips;
             p.m.blocks = (cols + kBlock - 1) / kBlock;
-            p.m.matrix_bytes = p.m.strips * p.m.blocks * block_bytes(W >= 32 ? W : 128);
+            p.m.matrix_bytes = k ? a.m2_bytes : a.m13_bytes;
             p.blocks = blocks;
-            // (Products under 2^32 for grids of up to 1024 blocks.)
-            p.f0 = int(blockIdx.x * all / grid);
-            p.n = int((blockIdx.x + 1) * all / grid) - p.f0;
-            p.strips = strips;
-            p.inverse = uint32_t(0xFFFFFFFFu / uint32_t(strips)) + 1;
+            p.f0 = f0;
+            p.n = n;
+            p.n1 = n - rest;
             p.team = team;
             p.batch = batch;
-            p.window = !k && a.all_x ? 1 << 20 : max(1, (k ? a.h_rows : a.x_rows) / max(1, int(tab.most)));
+            p.tiles = tiles;
+            p.strips = strips;
+            p.inverse = uint32_t(0xFFFFFFFFu / uint32_t(strips)) + 1;
+            p.window = 1 << 20;
+            if (n > 0 && !(k && a.fold) && !(!k && a.all_x)) {
+                // All of the block's passes where their tokens fit, else as many as always do.
+                const int rows = k ? a.h_rows : a.x_rows, from = p.pass(f0), to = p.pass(f0 + n - 1);
+                if (tab.pass_first[to] + tab.pass_count[to] - tab.pass_first[from] > rows)
+                    p.window = max(1, rows / int(tab.most));
+            }
             ph[k] = p;
         }
     }
@@ -1658,7 +1672,6 @@ rr_status launch_moe(MoeArgs a, cudaStream_t stream) {
     if (a.cap > 8 && a.cap < 16) a.cap = 8;
     a.cap = std::min(a.cap, a.tokens);
     if (a.cap < 1) return rr_fail(RR_ELAYOUT, "hidden %d, inter %d: rows too long", a.hidden, a.inter);
-    a.tiles = a.cap > 8 ? 2 : 1;
     a.x_rows = room / a.x_pitch;
     a.h_rows = room / (2 * a.h_pitch);
     a.all_x = a.tokens <= a.x_rows;
