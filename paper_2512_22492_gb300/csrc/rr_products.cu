@@ -270,23 +270,45 @@ __device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a
             : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 
-// Codes n and n + 4 of a word (columns 2 n, 2 n + 1) as a pair of 16-bit numbers:
-// placed in the low mantissa bits of 128 (float16: 1024) they read 128 + q + 8,
-// and the subtraction is exact.
+// A word's codes as four pairs of 16-bit numbers q * kStep, exact; pair n is codes
+// n and n + 4 (columns 2 n, 2 n + 1).  One shift serves two pairs: codes in bits 0..3
+// and 4..7 of a half become numbers where they are.  What bounds the packed products
+// is this arithmetic (half the shifts of one per pair: lm_head of Qwen3-8B, one
+// token, 59 -> 55 us).
+//   bfloat16: the low 8 bits of a pattern without others stand for their value times
+//   2^-133 (the subnormals and the binade above them are evenly spaced), so a
+//   multiplication by 2^127 or 2^123 brings either code to c 2^-6.
+//   float16: under the exponent of 1024 they read 1024 + c and 1024 + 16 c.
 template <class T>
-__device__ __forceinline__ uint32_t codes(uint32_t word, int n) {
-    constexpr bool kB = std::is_same<T, BF16>::value;
-    uint32_t v;
-    asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(v) : "r"(word >> (4 * n)), "r"(kB ? 0x43004300u : 0x64006400u));
-    if (kB) {
-        const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v),
-                                         __nv_bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308)));
-        return *reinterpret_cast<const uint32_t*>(&d);
+struct Codes {
+    static constexpr float kStep = std::is_same<T, BF16>::value ? 1.0f / 64 : 1.0f;
+    static __device__ __forceinline__ uint32_t pair(uint32_t v, bool high) {
+        uint32_t d;
+        if (std::is_same<T, BF16>::value) {
+            // 2^127, 2^123; - 8 * 2^-6.
+            asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(v), "r"(high ? 0x7D007D00u : 0x7F007F00u), "r"(0xBE00BE00u));
+        } else {
+            // 1, 1 / 16; - 1032, - 72.
+            asm("fma.rn.f16x2 %0, %1, %2, %3;"
+                : "=r"(d) : "r"(v), "r"(high ? 0x2C002C00u : 0x3C003C00u), "r"(high ? 0xD480D480u : 0xE408E408u));
+        }
+        return d;
     }
-    const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&v),
-                              __half2(__ushort_as_half(0x6408), __ushort_as_half(0x6408)));
-    return *reinterpret_cast<const uint32_t*>(&d);
-}
+    static __device__ __forceinline__ uint32_t mask(uint32_t w, bool high) {
+        if (std::is_same<T, BF16>::value) return w & (high ? 0x00F000F0u : 0x000F000Fu);
+        uint32_t v;
+        if (high) asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0xEA;" : "=r"(v) : "r"(w), "r"(0x64006400u));
+        else asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(v) : "r"(w), "r"(0x64006400u));
+        return v;
+    }
+    static __device__ __forceinline__ void unpack(uint32_t (&to)[4], uint32_t w) {
+        const uint32_t u = w >> 8;
+        to[0] = pair(mask(w, false), false);
+        to[1] = pair(mask(w, true), true);
+        to[2] = pair(mask(u, false), false);
+        to[3] = pair(mask(u, true), true);
+    }
+};
 
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
 
@@ -352,8 +374,8 @@ __device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* s
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         uint32_t al[4], ah[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) al[i] = codes<T>(wl[j], i), ah[i] = codes<T>(wh[j], i);
+        Codes<T>::unpack(al, wl[j]);
+        Codes<T>::unpack(ah, wh[j]);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const uint4 v = *reinterpret_cast<const uint4*>(x[n] + at + 64 * j);
@@ -370,10 +392,12 @@ __device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* s
             const float sl = T::widen(uint16_t(s[32 * j / G])), sh = T::widen(uint16_t(s[32 * j / G] >> 16));
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                sum[n][0] = fmaf(sl, part[n][0], sum[n][0]);
-                sum[n][1] = fmaf(sl, part[n][1], sum[n][1]);
-                sum[n][2] = fmaf(sh, part[n][2], sum[n][2]);
-                sum[n][3] = fmaf(sh, part[n][3], sum[n][3]);
+                // (The scale times 64 might overflow.)
+                constexpr float kUp = 1.0f / Codes<T>::kStep;
+                sum[n][0] = fmaf(sl, kUp * part[n][0], sum[n][0]);
+                sum[n][1] = fmaf(sl, kUp * part[n][1], sum[n][1]);
+                sum[n][2] = fmaf(sh, kUp * part[n][2], sum[n][2]);
+                sum[n][3] = fmaf(sh, kUp * part[n][3], sum[n][3]);
             }
         }
     }
