@@ -328,30 +328,17 @@ __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group 
 constexpr int kWarps = 16;         // of a block: one block per SM
 constexpr int kProdThreads = 32 * kWarps;
 
-// A warp's stages of U adjacent blocks of codes each: enough of them that a block
-// has 64 to 100 KB in flight, and a wait, a copy's address and a loop's step for
-// U blocks at a time.  A lane copies the 16-byte runs that it reads itself; of
-// the scales, which four lanes share, lanes 0..7 copy a slot pair's each.
-template <int G, int U>
-struct Stage {
-    static constexpr int kScale = 512 / G;                 // bytes of a slot pair's scales
-    static constexpr int kBlockBytes = kCodes + 8 * kScale;     // = block_bytes(G)
-    static constexpr int kBytes = U * kBlockBytes;
-    static constexpr int kStages = 6 / U;
-    // from: the block's codes at this lane's run; scales: at this lane's (< 8) scales.
-    static __device__ __forceinline__ void copy(uint32_t to, const char* from, const char* scales, int lane) {
+// A warp's blocks of codes in flight.  A lane copies the 16-byte runs that it reads
+// itself; of the scales, which four lanes share, lanes 0..7 copy a slot pair's each.
+template <int G>
+struct Block {
+    static constexpr int kScale = 512 / G;                      // bytes of a slot pair's scales
+    static constexpr int kBytes = kCodes + 8 * kScale;          // = block_bytes(G)
+    // from: the block's codes at this lane's run.
+    static __device__ __forceinline__ void copy(uint32_t to, const char* from, int lane) {
         copy_async<16>(to + 16 * lane, from);
         copy_async<16>(to + 512 + 16 * lane, from + 512);
-        if (lane < 8) copy_async<kScale>(to + kCodes + kScale * lane, scales);
-    }
-    static __device__ __forceinline__ void load(uint32_t to, const char* from, const char* scales, int blocks,
-                                                int lane) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (u > 0 && blocks <= u) break;
-            copy(to + u * kBlockBytes, from + u * kBlockBytes, scales + u * kBlockBytes, lane);
-        }
-        copy_commit();
+        if (lane < 8) copy_async<kScale>(to + kCodes + kScale * lane, from + (kCodes + (kScale - 16) * lane));
     }
 };
 
@@ -416,9 +403,8 @@ struct MatvecArgs {
     int32_t tokens, f32;
     int32_t vec;          // x's rows can be read 16 bytes at a time
     int32_t pitch;        // bytes between tokens in shared memory
-    int32_t team;         // warps that share a strip's columns: 1, 2, 4, 8 or 16
     int32_t cluster;      // blocks that share the columns
-    int32_t batch;        // strips between two joins of the teams' sums
+    int32_t batch;        // strips between two joins of a cluster's sums
 };
 
 __device__ __forceinline__ void cluster_sync() {
@@ -450,55 +436,42 @@ __device__ __forceinline__ void put_strip(const MatvecArgs& a, int64_t strip, in
     }
 }
 
+// A run of `total` blocks of weights, shared out evenly over a thread block's warps
+// wherever strips begin and end: warp w takes [share_from(w), share_from(w + 1)).
+// A strip that lies in one warp's share is finished there; of another, each warp
+// leaves its part: the last one (and only it) as its first part, the others as
+// their last.  Parts are joined in the order of the warps.
+__device__ __forceinline__ int share_from(int w, int total) { return int(uint32_t(w) * uint32_t(total) / kWarps); }
+__device__ __forceinline__ int share_of(int p, int total) { return int((kWarps * uint32_t(p + 1) - 1) / uint32_t(total)); }
+
 // A cluster takes a run of strips; each of its blocks takes a share of the
-// columns, whose tokens it keeps in shared memory, and of these each warp of a
-// team every team-th run of U blocks of 128.  Warps stream their blocks through
-// stages of their own without meeting; sums of a batch of strips are joined
-// through shared memory in a fixed order.
-template <class T, int G, int NT, int U>
+// columns, whose tokens it keeps in shared memory, and a warp an even share of
+// the run's blocks of weights, which it streams through stages of U blocks of its own
+// without meeting others.  Parts of strips are joined through shared memory at
+// the end, and a cluster's sums through its blocks' shared memory after each
+// `batch` of strips.  ST: blocks in flight.
+template <class T, int G, int NT, int U, int ST>
 __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid_constant__ MatvecArgs a) {
     extern __shared__ __align__(128) char smem[];
-    using S = Stage<G, U>;
+    using S = Block<G>;
+    constexpr int kStages = ST / U, kStageBytes = U * S::kBytes;
+    constexpr int kPart = NT * 32;                    // float4 of a strip's sums
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rank = blockIdx.x % a.cluster, cl = blockIdx.x / a.cluster, n_cl = gridDim.x / a.cluster;
     after_previous();
-    char* const fifo = smem + warp * (S::kStages * S::kBytes);
-    char* const xs = smem + kWarps * S::kStages * S::kBytes;
-    float4* const red = reinterpret_cast<float4*>(xs + a.tokens * a.pitch);
+    // Stages; the tokens; each warp's first part; a cluster's sums by strip.  A warp's
+    // last part goes where its stages were.
+    char* const fifo = smem + warp * (ST * S::kBytes);
+    char* const xs = smem + kWarps * ST * S::kBytes;
+    float4* const parts = reinterpret_cast<float4*>(xs + a.tokens * a.pitch);
+    float4* const full = parts + kWarps * kPart;
+    float4* const last = reinterpret_cast<float4*>(fifo);
 
     const int64_t s0 = cl * a.m.strips / n_cl, s1 = (cl + 1) * a.m.strips / n_cl;
-    const int b0 = int(rank * a.m.blocks / a.cluster), b1 = int((rank + 1) * a.m.blocks / a.cluster);
-    const int teams = kWarps / a.team, team = warp / a.team, part = warp % a.team;
-
-    // This warp takes runs part, part + team, ... of a strip.  The load cursor
-    // goes over them, strip after strip, ahead of the products.
-    const int runs = (b1 - b0 + U - 1) / U;
-    const int steps = (runs - part + a.team - 1) / a.team;
-    int left_strips = steps > 0 ? int((s1 - s0 - team + teams - 1) / teams) : 0;
-    int lb = b0 + U * part, slot = 0;
-    const char* from = a.packed + ((s0 + team) * a.m.blocks + lb) * S::kBlockBytes + 16 * lane;
-    const int64_t scales = kCodes + (S::kScale - 16) * lane;      // from a run's codes to its scales
-    const int64_t next_run = int64_t(a.team) * S::kBytes;
-    const int64_t next_strip = (teams * a.m.blocks - int64_t(steps - 1) * a.team * U) * S::kBlockBytes;
-    const uint32_t fifo_at = smem_at(fifo);
-    auto load = [&](int to) {
-        if (left_strips > 0) {
-            S::load(fifo_at + to * S::kBytes, from, from + scales, b1 - lb, lane);
-            lb += a.team * U;
-            if (lb >= b1) {
-                lb = b0 + U * part;
-                --left_strips;
-                from += next_strip;
-            } else {
-                from += next_run;
-            }
-        } else {
-            copy_commit();
-        }
-    };
+    const int b0 = int(rank * a.m.blocks / a.cluster), nb = int((rank + 1) * a.m.blocks / a.cluster) - b0;
 
     // Tokens: this block's columns, zeros past the matrix's.
-    const int cols = (b1 - b0) * kBlock;
+    const int cols = nb * kBlock;
     const int64_t c0 = int64_t(b0) * kBlock;
     if (a.vec) {
         // 16-byte copies, cut off (and zero-filled) at the row's end.
@@ -516,65 +489,107 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
                     c0 + c < a.m.cols ? a.x[n * a.ldx + c0 + c] : uint16_t(0);
     }
     copy_commit();
-    for (int i = 0; i < S::kStages - 1; ++i) load(i);
-    copy_wait<S::kStages - 1>();
-    __syncthreads();
-
     // A lane of an absent token reads the last one's row; its sums go nowhere.
     const char* x[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
         x[n] = xs + min(8 * n + (lane >> 2), a.tokens - 1) * a.pitch + 16 * (lane & 3);
-    const bool alone = a.team == 1 && a.cluster == 1;
-    for (int64_t from = s0; from < s1; from += a.batch) {
-        const int64_t to = min(from + a.batch, s1);
-        for (int64_t strip = from + team; strip < to; strip += teams) {
-            float sum[NT][4] = {};
-            for (int i = 0; i < steps; ++i) {
-                copy_wait<S::kStages - 2>();
-                __syncwarp();      // the scales are there for every lane, and the last stage has been read
-                load(slot == 0 ? S::kStages - 1 : slot - 1);
-                const int at = U * (part + i * a.team);
+
+    const uint32_t fifo_at = smem_at(fifo);
+    const int64_t next_strip = (a.m.blocks - nb) * S::kBytes;      // from a strip's last block here to the next's first
+    bool staged = false;
+    for (int64_t f = s0; f < s1; f += a.batch) {
+        const int strips = int(min(int64_t(a.batch), s1 - f)), total = strips * nb;
+        const int lo = share_from(warp, total), hi = share_from(warp + 1, total);
+        int strip = lo / nb, b = lo - strip * nb;
+        // The load cursor, kStages - 1 stages ahead.
+        const char* from = a.packed + ((f + strip) * a.m.blocks + b0 + b) * S::kBytes + 16 * lane;
+        int lb = b, left = hi - lo, slot = 0;
+        auto load = [&](int to) {
+            if (a.cluster == 1 && left >= U) {
+                // Strip follows strip.
+#pragma unroll
+                for (int u = 0; u < U; ++u) S::copy(fifo_at + to * kStageBytes + u * S::kBytes, from + u * S::kBytes, lane);
+                from += U * S::kBytes;
+            } else {
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-                    if (u == 0 || at + u < b1 - b0)
-                        block_product<T, G, NT>(sum, fifo + slot * S::kBytes + u * S::kBlockBytes, x,
-                                                (at + u) * (2 * kBlock), lane);
-                slot = slot + 1 == S::kStages ? 0 : slot + 1;
+                    if (left > u) {
+                        S::copy(fifo_at + to * kStageBytes + u * S::kBytes, from, lane);
+                        from += S::kBytes;
+                        if (++lb == nb) lb = 0, from += next_strip;
+                    }
             }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                if (alone) put_strip<T>(a, strip, lane, n, sum[n]);
-                else
-                    red[((part * a.batch + int(strip - from)) * NT + n) * 32 + lane] =
-                        make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
-            }
+            left -= U;
+            copy_commit();
+        };
+        for (int i = 0; i < kStages - 1; ++i) load(i);
+        if (!staged) {
+            copy_wait<kStages - 1>();
+            __syncthreads();
+            staged = true;
         }
-        if (alone) continue;
-        if (a.cluster > 1) cluster_sync();
-        else __syncthreads();
-        const int count = int(to - from) * NT * 32;
-        for (int i = rank * kProdThreads + threadIdx.x; i < count; i += a.cluster * kProdThreads) {
-            float v[4] = {};
-            for (int r = 0; r < a.cluster; ++r) {
-                uint32_t at = smem_at(red + i);
-                if (a.cluster > 1) asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(at), "r"(r));
-                for (int p = 0; p < a.team; ++p) {
-                    float4 f;
-                    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
-                                 : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
-                                 : "r"(at + uint32_t(p * a.batch * NT * 32 * sizeof(float4))) : "memory");
-                    v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+        float sum[NT][4] = {};
+        bool whole = b == 0;       // this warp has the strip from its first block on
+        for (int p = lo; p < hi; p += U) {
+            copy_wait<kStages - 2>();
+            __syncwarp();          // the scales are there for every lane, and the last stage has been read
+            load(slot == 0 ? kStages - 1 : slot - 1);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (u > 0 && p + u >= hi) break;
+                block_product<T, G, NT>(sum, fifo + slot * kStageBytes + u * S::kBytes, x, b * (2 * kBlock), lane);
+                if (++b == nb) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        if (whole && a.cluster == 1) put_strip<T>(a, f + strip, lane, n, sum[n]);
+                        else
+                            (whole ? full + strip * kPart : parts + warp * kPart)[n * 32 + lane] =
+                                make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
+                        sum[n][0] = sum[n][1] = sum[n][2] = sum[n][3] = 0.0f;
+                    }
+                    b = 0;
+                    ++strip;
+                    whole = true;
                 }
             }
-            put_strip<T>(a, from + i / (NT * 32), i & 31, i / 32 % NT, v);
+            slot = slot + 1 == kStages ? 0 : slot + 1;
+        }
+        copy_wait<0>();
+        __syncwarp();
+        if (b != 0)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) last[n * 32 + lane] = make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
+        __syncthreads();
+        for (int i = threadIdx.x; i < strips * kPart; i += kProdThreads) {
+            const int k = i / kPart, first = share_of(k * nb, total), end = share_of(k * nb + nb - 1, total);
+            if (first == end) continue;
+            float v[4] = {};
+            for (int w = first; w <= end; ++w) {
+                const float4 r = (w < end ? reinterpret_cast<const float4*>(smem + w * (ST * S::kBytes)) : parts + w * kPart)[i % kPart];
+                v[0] += r.x, v[1] += r.y, v[2] += r.z, v[3] += r.w;
+            }
+            if (a.cluster == 1) put_strip<T>(a, f + k, i & 31, i / 32 % NT, v);
+            else full[i] = make_float4(v[0], v[1], v[2], v[3]);
+        }
+        if (a.cluster == 1) continue;      // (one batch)
+        cluster_sync();
+        for (int i = rank * kProdThreads + threadIdx.x; i < strips * kPart; i += a.cluster * kProdThreads) {
+            float v[4] = {};
+            for (int r = 0; r < a.cluster; ++r) {
+                uint32_t at;
+                float4 q;
+                asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_at(full + i)), "r"(r));
+                asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+                             : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "r"(at) : "memory");
+                v[0] += q.x, v[1] += q.y, v[2] += q.z, v[3] += q.w;
+            }
+            put_strip<T>(a, f + i / kPart, i & 31, i / 32 % NT, v);
         }
         // The sums have been read, here and by the cluster's other blocks, before
         // they are overwritten or this block ends.
-        if (a.cluster > 1) cluster_sync();
-        else __syncthreads();
+        cluster_sync();
     }
-    copy_wait<0>();
 }
 
 // ---------------------------------------------------------------------------
@@ -685,8 +700,8 @@ struct Weights {
 
 template <int G>
 struct PackedWeights {
-    using S = Stage<G, 1>;
-    static constexpr int kCols = kBlock, kBytes = S::kBytes, kStages = S::kStages;
+    using S = Block<G>;
+    static constexpr int kCols = kBlock, kBytes = S::kBytes, kStages = 6;
     const char* from;
     __device__ __forceinline__ void seek(const char* base, int64_t mat, const Packed& m, int64_t strip, int b,
                                          int lane) {
@@ -694,7 +709,7 @@ struct PackedWeights {
     }
     __device__ __forceinline__ void skip(int blocks) { from += int64_t(blocks) * kBytes; }
     __device__ __forceinline__ void load(uint32_t to, const char*, int lane) const {
-        S::copy(to, from, from + (kCodes + (S::kScale - 16) * lane), lane);
+        S::copy(to, from, lane);
     }
 };
 template <> struct Weights<32> : PackedWeights<32> {};
@@ -1839,7 +1854,7 @@ namespace {
 struct MatvecShape {
     unsigned grid;
     int smem;
-    int run;        // blocks of a stage
+    bool deep;      // 6 blocks of weights in flight a warp, else 4
 };
 
 // Clusters of a size that this GPU runs at once with one block per SM (GB300: 152,
@@ -1875,48 +1890,35 @@ int clusters_at_once(K* kernel, int cluster) {
     return known[dev][i];
 }
 
-// How a product is shared out, for a.tokens tokens; false if these do not fit.
-// The time of a launch goes by the blocks of 128 columns that the busiest warp
-// takes; joins cost about one of them.  Measured on GB300: see the table of
-// DESIGN.
+// How a product is shared out, for a.tokens tokens; false if these do not fit.  The
+// fewest blocks of a cluster for which its share of the tokens fits a block's shared
+// memory, with 6 blocks of weights in flight a warp where there is room, else 4;
+// more, where strips are too few to go round and a block's share is long.
 bool matvec_shape(MatvecArgs* a, int group, MatvecShape* shape) {
-    const int tiles = a->tokens > 8 ? 2 : 1;
-    const int fifo = kWarps * 6 * block_bytes(group);
-    const int room = kSmem - fifo - kJoinBytes;
+    const int tiles = a->tokens > 8 ? 2 : 1, part = 512 * tiles;
     int64_t best = INT64_MAX;
-    for (int cluster = 1; cluster <= 8; cluster *= 2) {
-        if (cluster > a->m.blocks) break;
+    for (int cluster = 1; cluster <= 8 && cluster <= a->m.blocks; cluster *= 2) {
         const int64_t blocks = (a->m.blocks + cluster - 1) / cluster;
         // Rows 64 bytes past a multiple of 128, so that two tokens' rows are on
         // different halves of the banks.
         const int64_t pitch = blocks * 2 * kBlock + 64;
-        if (pitch * a->tokens > room) continue;
-        const int64_t groups = std::min<int64_t>(clusters_at_once(rr_matvec_kernel<BF16, 128, 1, 1>, cluster), a->m.strips);
+        const int64_t groups = std::min<int64_t>(clusters_at_once(rr_matvec_kernel<BF16, 128, 1, 2, 6>, cluster), a->m.strips);
         const int64_t strips = (a->m.strips + groups - 1) / groups;
-        for (int team = 1; team <= kWarps; team *= 2) {
-            const int teams = kWarps / team;
-            // (Warps stream on from batch to batch: whole rounds of the teams.)
-            const bool alone = team == 1 && cluster == 1;
-            const int64_t fit = kJoinBytes / (512 * tiles * team) / teams * teams;
-            const int64_t batch = alone ? strips : std::min(strips, fit);
-            const int64_t joins = alone ? 0 : (strips + batch - 1) / batch;
-            // Runs of two blocks where they cost nothing.
-            const int64_t one = (blocks + team - 1) / team, two = 2 * (((blocks + 1) / 2 + team - 1) / team);
-            const int64_t steps = one;
-            int64_t cost = 0;
-            for (int64_t left = strips; left > 0; left -= batch)
-                cost += (std::min(left, batch) + teams - 1) / teams * steps;
-            cost += joins * (cluster > 1 ? 2 : 1);
+        for (int stages = 6; stages >= 4; stages -= 2) {
+            const int64_t room = kSmem - kWarps * (stages * block_bytes(group) + part) - pitch * a->tokens;
+            const int64_t batch = cluster == 1 ? strips : std::min(strips, room / part);
+            if (room < 0 || batch < 1) continue;
+            const int64_t joins = cluster == 1 ? 0 : (strips + batch - 1) / batch;
+            // In blocks of weights of the busiest warp.
+            const int64_t cost = (strips * blocks + kWarps - 1) / kWarps + 4 * joins + (stages == 4 ? 1 : 0);
             if (cost >= best) continue;
             best = cost;
             a->pitch = int32_t(pitch);
-            a->team = team;
             a->cluster = cluster;
             a->batch = int32_t(batch);
-            shape->run = two == one ? 2 : 1;
+            shape->deep = stages == 6;
             shape->grid = unsigned(groups * cluster);
-            shape->smem = fifo + int(pitch) * a->tokens
-                          + (joins ? int(batch) * 512 * tiles * team : 0);
+            shape->smem = int(kSmem - room + (cluster == 1 ? 0 : batch * part));
         }
     }
     return best != INT64_MAX;
@@ -1983,12 +1985,9 @@ extern "C" rr_status rr_matvec(const rr_quant* q, const void* packed, const void
                 if (a.tokens == 1) return rr_fail(RR_ELAYOUT, "rows of %lld columns", (long long)q->cols);
                 a.tokens = (a.tokens + 1) / 2;
             }
-            const cudaError_t e =
-                a.tokens > 8
-                    ? shape.run == 2 ? launch_matvec(rr_matvec_kernel<T, G, 2, 2>, a, shape, stream)
-                                     : launch_matvec(rr_matvec_kernel<T, G, 2, 1>, a, shape, stream)
-                    : shape.run == 2 ? launch_matvec(rr_matvec_kernel<T, G, 1, 2>, a, shape, stream)
-                                     : launch_matvec(rr_matvec_kernel<T, G, 1, 1>, a, shape, stream);
+            const auto kernel = a.tokens > 8 ? shape.deep ? rr_matvec_kernel<T, G, 2, 2, 6> : rr_matvec_kernel<T, G, 2, 1, 4>
+                                             : shape.deep ? rr_matvec_kernel<T, G, 1, 2, 6> : rr_matvec_kernel<T, G, 1, 1, 4>;
+            const cudaError_t e = launch_matvec(kernel, a, shape, stream);
             if (e != cudaSuccess) return cuda_fail(e, "rr_matvec");
         }
         return RR_OK;
