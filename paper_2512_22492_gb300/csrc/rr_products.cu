@@ -598,7 +598,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
 
 constexpr int kMaxExperts = 512, kMaxTopK = 16, kMaxHidden = 32768, kMaxInter = 16384;
 constexpr int kMaxPairs = RR_MOE_MAX_TOKENS * kMaxTopK;
-constexpr int kJoinBytes = 24 * 1024;   // shared memory of the teams' sums
+constexpr int kJoinBytes = 2 * kWarps * 2 * 512;   // shared memory of the warps' parts of strips
 constexpr int kClusterBlocks = 8;       // of a layer small enough for one cluster
 constexpr int64_t kClusterBytes = 1 << 20;
 constexpr int kSmem = 227 * 1024;
@@ -756,7 +756,7 @@ __device__ __forceinline__ uint32_t rank_key(float l) {
 struct MoeTables {
     uint32_t mask[2][kMaxExperts];     // the tokens of a local expert
     float c[kMaxPairs];                // by token and rank
-    float pair_c[kMaxPairs];           // by pair
+    float pair_c[8 * kMaxTopK];        // by pair (of up to 8 tokens)
     int16_t chosen[kMaxPairs];
     uint16_t first[kMaxExperts];       // a local expert's first pair
     uint16_t pass_expert[kMaxPairs], pass_first[kMaxPairs];
@@ -934,8 +934,6 @@ struct MoePhase {
     Packed m;
     int blocks;            // of a strip
     int f0, n;             // this block's items: pass f / strips, strip f % strips
-    int n1;                // items that a warp takes alone; the rest go to teams
-    int team, batch;       //   of warps, joined after every `batch`
     int tiles;             // groups of 8 tokens of the largest pass
     int strips;
     uint32_t inverse;      // 2^32 / strips, rounded up: exact for f * strips <= 2^32
@@ -948,55 +946,71 @@ struct MoePhase {
         const int first = pass(f0), w = (pass(f0 + i) - first) / window + 1;
         return min(n, (first + w * window) * strips - f0);
     }
-    __device__ __forceinline__ int team_at(int i) const { return i < n1 ? 1 : team; }
-    // The end of a batch: items of one window and one size of team, between two joins.
-    __device__ __forceinline__ int batch_end(int i0) const {
-        return min(i0 < n1 ? n1 : i0 + batch, window_end(i0));
-    }
 };
 
-// The order in which a warp takes the blocks of weights of a run of items.
+// The order in which a warp takes a phase's blocks of weights: of each window's
+// items, whole rounds of 16 one item a warp (adjacent warps then read adjacent
+// rows: 120 us for gate and up of 64 tokens, against 131 with a contiguous share for
+// each warp), and of the rest an even share of their blocks.
 template <int W>
 struct Feed {
     Weights<W> w;
-    int i, i1, b, team;
-    bool done;
-    __device__ __forceinline__ void aim(const MoePhase& p, const MoeTables& tab, int part, int lane) {
+    int i, b, left;            // item, block, blocks left in this run
+    int rest, end;             // where the window's rounds and the window end
+    __device__ __forceinline__ void aim(const MoePhase& p, const MoeTables& tab, int lane) {
         const int f = p.f0 + i, pass = p.pass(f);
-        b = part;
         w.seek(p.base, tab.pass_expert[pass], p.m, f - pass * p.strips, b, lane);
     }
-    // The first item of this warp from batch i0 on.
+    // This warp's first item from i0 on: i0 begins a window, or is the end of its rounds.
     __device__ __forceinline__ void find(const MoePhase& p, const MoeTables& tab, int i0, int warp, int lane) {
+        left = 0;
         while (i0 < p.n) {
-            team = p.team_at(i0);
-            i1 = p.batch_end(i0);
-            i = i0 + warp / team;
-            if (i < i1 && warp % team < p.blocks) {
-                aim(p, tab, warp % team, lane);
-                done = false;
+            end = p.window_end(i0);
+            rest = end - (end - i0) % kWarps;
+            if (rest > i0) {
+                i = i0 + warp;
+                b = 0;
+                left = p.blocks;
+            } else {
+                const int total = (end - i0) * p.blocks, lo = share_from(warp, total);
+                left = share_from(warp + 1, total) - lo;
+                i = i0 + lo / p.blocks;
+                b = lo % p.blocks;
+                rest = -1;         // the rest itself
+            }
+            if (left > 0) {
+                aim(p, tab, lane);
                 return;
             }
-            i0 = i1;
+            i0 = end;
         }
-        done = true;
     }
     // The next block to a stage; an empty group when there is none.
     __device__ __forceinline__ void load(const MoePhase& p, const MoeTables& tab, uint32_t to, int warp, int lane) {
-        if (!done) {
+        if (left > 0) {
             w.load(to, p.base, lane);
-            b += team;
-            if (b < p.blocks) {
-                w.skip(team);
+            if (--left > 0) {
+                if (++b < p.blocks) {
+                    w.skip(1);
+                } else {
+                    b = 0;
+                    ++i;
+                    aim(p, tab, lane);
+                }
+            } else if (rest < 0) {
+                find(p, tab, end, warp, lane);
+            } else if (i + kWarps < rest) {
+                i += kWarps;
+                b = 0;
+                left = p.blocks;
+                aim(p, tab, lane);
             } else {
-                i += kWarps / team;
-                if (i < i1) aim(p, tab, warp % team, lane);
-                else find(p, tab, i1, warp, lane);
+                find(p, tab, rest, warp, lane);
             }
         }
         copy_commit();
     }
-    // Starts on a run: all stages but one, from `slot` on.
+    // Starts on a phase: all stages but one, from `slot` on.
     __device__ __forceinline__ void start(const MoePhase& p, const MoeTables& tab, uint32_t fifo, int slot, int warp,
                                           int lane) {
         find(p, tab, 0, warp, lane);
@@ -1076,109 +1090,142 @@ __device__ __forceinline__ void stage_h(const MoeArgs& a, MoeTables& tab, char* 
     }
 }
 
-// A phase's items [i0, i1), whose tokens are in shared memory from pair `base` on.
-// The first phase ends in silu(gate) * up, the second in the pair's part of the
-// output.
-template <class T, int W, int PHASE>
-struct MoeBatch {
-    static constexpr int kParts = PHASE == 0 ? 1 : 2, kStages = Weights<W>::kStages, kBytes = Weights<W>::kBytes;
-    const MoeArgs& a;
-    const MoePhase& p;
-    const MoeTables& tab;
-    Feed<W>& feed;
-    char* fifo;
-    int& slot;
-    const char* region;
-    float4* red;
-    int base;
+// Rows g, g + 8 of tokens 2 t, 2 t + 1 (+ 8 n) of a strip and a pass: the first phase
+// ends in silu(gate) * up, the second in the pair's part of the output.
+template <class T, int PHASE>
+__device__ __forceinline__ void moe_put(const MoeArgs& a, const MoePhase& p, const MoeTables& tab, int f, int lane,
+                                        int n, const float (&v)[4]) {
+    const int pass = p.pass(f), strip = f - pass * p.strips;
+    const int first = tab.pass_first[pass], count = tab.pass_count[pass];
+    const int64_t lo = p.m.row(strip, lane >> 2), hi = p.m.row(strip, 8 + (lane >> 2));
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int tok = 8 * n + 2 * (lane & 3) + k;
+        if (tok >= count || lo < 0) continue;
+        if (PHASE == 0) {
+            const float h = silu(v[k]) * v[2 + k];
+            __stcg(a.h + int64_t(first + tok) * a.h_ld + lo, h);
+            if (std::is_same<T, F16>::value && fabsf(h) < INFINITY)
+                atomicMax(a.h_top + first + tok, __float_as_uint(fabsf(h)));
+        } else {
+            const float s = std::is_same<T, F16>::value ? tab.scale[first + tok] : 1.0f;
+            float* const y = a.y + int64_t(first + tok) * a.y_ld;
+            __stcg(y + lo, v[k] * s);
+            if (hi >= 0) __stcg(y + hi, v[2 + k] * s);
+        }
+    }
+}
 
-    // Rows g, g + 8 of tokens 2 t, 2 t + 1 (+ 8 n) of a strip and a pass.
-    __device__ __forceinline__ void put(int pass, int strip, int ln, int n, const float (&v)[4]) const {
-        const int first = tab.pass_first[pass], count = tab.pass_count[pass];
-        const int64_t lo = p.m.row(strip, ln >> 2), hi = p.m.row(strip, 8 + (ln >> 2));
+// Blocks [b, stop) of item f by one warp: its sums go out where `whole` says that the
+// warp has the item from its first block on and this is its last, else to `first`
+// (the item ends here) or `last`.  NT: groups of 8 tokens.
+template <class T, int W, int PHASE, int NT>
+__device__ __forceinline__ void moe_item(const MoeArgs& a, const MoePhase& p, const MoeTables& tab, Feed<W>& feed,
+                                         char* fifo, int& slot, const char* region, float4* firsts, float4* lasts,
+                                         int base, int f, int b, int stop, bool whole) {
+    constexpr int kParts = PHASE == 0 ? 1 : 2, kStages = Weights<W>::kStages, kBytes = Weights<W>::kBytes;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int pitch = PHASE == 0 ? a.x_pitch : a.h_pitch, apart = a.h_rows * a.h_pitch;
+    const int pass = p.pass(f), first = tab.pass_first[pass], count = tab.pass_count[pass];
+    const uint32_t fifo_at = smem_at(fifo);
+    const char* x[NT];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int tok = 8 * n + 2 * (ln & 3) + k;
-            if (tok >= count || lo < 0) continue;
-            if (PHASE == 0) {
-                const float h = silu(v[k]) * v[2 + k];
-                __stcg(a.h + int64_t(first + tok) * a.h_ld + lo, h);
-                if (std::is_same<T, F16>::value && fabsf(h) < INFINITY)
-                    atomicMax(a.h_top + first + tok, __float_as_uint(fabsf(h)));
-            } else {
-                const float s = std::is_same<T, F16>::value ? tab.scale[first + tok] : 1.0f;
-                float* const y = a.y + int64_t(first + tok) * a.y_ld;
-                __stcg(y + lo, v[k] * s);
-                if (hi >= 0) __stcg(y + hi, v[2 + k] * s);
-            }
+    for (int n = 0; n < NT; ++n) {
+        const int pair = first + min(8 * n + g, count - 1);
+        x[n] = region + (PHASE == 0 && a.all_x ? tab.token[pair] : pair - base) * pitch + 16 * t;
+    }
+    int shift_lo = 0, shift_hi = 0;
+    if constexpr (W == 1) {
+        Weights<1> w;
+        w.seek(p.base, tab.pass_expert[pass], p.m, f - pass * p.strips, 0, lane);
+        shift_lo = int(reinterpret_cast<uintptr_t>(w.lo) & 15);
+        shift_hi = int(reinterpret_cast<uintptr_t>(w.hi) & 15);
+    }
+    float sum[NT][4] = {};
+    for (; b < stop; ++b) {
+        copy_wait<kStages - 2>();
+        __syncwarp();      // what lanes share is there, and the last stage has been read
+        feed.load(p, tab, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
+        moe_block<T, W, NT, kParts>(sum, fifo + slot * kBytes, x, apart, b * (2 * Weights<W>::kCols), shift_lo, shift_hi,
+                                    lane);
+        slot = slot + 1 == kStages ? 0 : slot + 1;
+    }
+    const bool ends = stop == p.blocks;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        if (ends && whole) moe_put<T, PHASE>(a, p, tab, f, lane, n, sum[n]);
+        else (ends ? firsts : lasts)[(warp * 2 + n) * 32 + lane] = make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
+    }
+}
+
+// A window's items [i0, end), whose tokens are in shared memory from pair `base` on, in
+// the order of Feed.
+template <class T, int W, int PHASE>
+__device__ __forceinline__ void moe_window(const MoeArgs& a, const MoePhase& p, const MoeTables& tab, Feed<W>& feed,
+                                           char* fifo, int& slot, const char* region, float4* parts, int base, int i0,
+                                           int end) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float4* const firsts = parts;                          // [warp][tile][lane]
+    float4* const lasts = parts + kWarps * 2 * 32;
+    const auto item = [&](int f, int b, int stop, bool whole) {
+        if (tab.pass_count[p.pass(f)] <= 8)
+            moe_item<T, W, PHASE, 1>(a, p, tab, feed, fifo, slot, region, firsts, lasts, base, f, b, stop, whole);
+        else
+            moe_item<T, W, PHASE, 2>(a, p, tab, feed, fifo, slot, region, firsts, lasts, base, f, b, stop, whole);
+    };
+    const int rest = end - (end - i0) % kWarps;
+    const int total = (end - rest) * p.blocks, lo = share_from(warp, total), hi = share_from(warp + 1, total);
+    // First the rounds' items, then the share of the rest, in one loop (one copy of
+    // the code).
+    int i = i0 + warp, b = 0, at = lo;
+    bool whole = true, round = i < rest;
+    if (!round) i = rest + lo / p.blocks, b = lo % p.blocks, whole = b == 0;
+    while (round || at < hi) {
+        const int stop = round ? p.blocks : min(p.blocks, b + hi - at);
+        item(p.f0 + i, b, stop, whole);
+        if (round) {
+            i += kWarps;
+            round = i < rest;
+            if (!round) i = rest + lo / p.blocks, b = lo % p.blocks, whole = b == 0;
+        } else {
+            at += stop - b;
+            b = 0;
+            ++i;
+            whole = true;
         }
     }
-    // This warp's blocks of an item.  NT: groups of 8 tokens.
-    template <int NT>
-    __device__ __forceinline__ void item(int i, int i0, int part, int team) const {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-        const int f = p.f0 + i, pass = p.pass(f), strip = f - pass * p.strips;
-        const int first = tab.pass_first[pass], count = tab.pass_count[pass];
-        const int pitch = PHASE == 0 ? a.x_pitch : a.h_pitch;
-        const uint32_t fifo_at = smem_at(fifo);
-        const char* x[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int pair = first + min(8 * n + g, count - 1);
-            x[n] = region + (PHASE == 0 && a.all_x ? tab.token[pair] : pair - base) * pitch + 16 * t;
-        }
-        int shift_lo = 0, shift_hi = 0;
-        if constexpr (W == 1) {
-            Weights<1> w;
-            w.seek(p.base, tab.pass_expert[pass], p.m, strip, 0, lane);
-            shift_lo = int(reinterpret_cast<uintptr_t>(w.lo) & 15);
-            shift_hi = int(reinterpret_cast<uintptr_t>(w.hi) & 15);
-        }
-        float sum[NT][4] = {};
-        for (int b = part; b < p.blocks; b += team) {
-            copy_wait<kStages - 2>();
-            __syncwarp();      // what lanes share is there, and the last stage has been read
-            feed.load(p, tab, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
-            moe_block<T, W, NT, kParts>(sum, fifo + slot * kBytes, x, a.h_rows * a.h_pitch,
-                                        b * (2 * Weights<W>::kCols), shift_lo, shift_hi, lane);
-            slot = slot + 1 == kStages ? 0 : slot + 1;
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (team == 1) put(pass, strip, lane, n, sum[n]);
-            else
-                red[((part * p.batch + i - i0) * p.tiles + n) * 32 + lane] =
-                    make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
-        }
+    if (total == 0) return;
+    i0 = rest;
+    b = lo % p.blocks;
+    if (lo == hi && b != 0) {          // no share, within an item that others have
+        lasts[(warp * 2) * 32 + lane] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        lasts[(warp * 2 + 1) * 32 + lane] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
-    __device__ __forceinline__ void run(int i0, int i1) const {
-        const int warp = threadIdx.x >> 5, team = p.team_at(i0), part = warp % team;
-        for (int i = i0 + warp / team; i < i1; i += kWarps / team) {
-            if (tab.pass_count[p.pass(p.f0 + i)] <= 8) item<1>(i, i0, part, team);
-            else item<2>(i, i0, part, team);
+    __syncthreads();
+    // Items that several warps have: at most one begins in each warp's share.
+    for (int k = threadIdx.x; k < kWarps * p.tiles * 32; k += kProdThreads) {
+        const int w = k / (p.tiles * 32), n = k / 32 % p.tiles, ln = k & 31;
+        const int wlo = share_from(w, total), whi = share_from(w + 1, total);
+        if (wlo == whi) continue;
+        const int item = (whi - 1) / p.blocks;             // the last one of this warp
+        const int from = item * p.blocks, to = from + p.blocks;
+        if (from < wlo || to <= whi) continue;             // begun before, or ended here
+        if (8 * n >= tab.pass_count[p.pass(p.f0 + i0 + item)]) continue;
+        const int last = share_of(to - 1, total);
+        float v[4] = {};
+        for (int q = w; q <= last; ++q) {
+            const float4 r = (q < last ? lasts : firsts)[(q * 2 + n) * 32 + ln];
+            v[0] += r.x, v[1] += r.y, v[2] += r.z, v[3] += r.w;
         }
-        if (team == 1) return;
-        __syncthreads();
-        for (int k = threadIdx.x; k < (i1 - i0) * p.tiles * 32; k += kProdThreads) {
-            const int i = k / (p.tiles * 32), n = k / 32 % p.tiles;
-            const int f = p.f0 + i0 + i, pass = p.pass(f);
-            if (8 * n >= tab.pass_count[pass]) continue;
-            float v[4] = {};
-            for (int q = 0; q < team; ++q) {
-                const float4 r = red[q * p.batch * p.tiles * 32 + k];
-                v[0] += r.x, v[1] += r.y, v[2] += r.z, v[3] += r.w;
-            }
-            put(pass, f - pass * p.strips, k & 31, n, v);
-        }
-        __syncthreads();
+        moe_put<T, PHASE>(a, p, tab, p.f0 + i0 + item, ln, n, v);
     }
-};
+}
 
 // Tokens of as many passes as fit are staged at once, so that warps go from one
 // pass to the next without meeting.
 template <class T, int W, int PHASE>
 __device__ __forceinline__ void moe_phase(const MoeArgs& a, const MoePhase* ph, MoeTables& tab, Feed<W>& feed,
-                                          char* fifo, int& slot, char* region, float4* red) {
+                                          char* fifo, int& slot, char* region, float4* parts) {
     const MoePhase& p = ph[PHASE];
     for (int i0 = 0; i0 < p.n;) {
         const int end = p.window_end(i0), from = p.pass(p.f0 + i0), to = p.pass(p.f0 + end - 1);
@@ -1189,12 +1236,8 @@ __device__ __forceinline__ void moe_phase(const MoeArgs& a, const MoePhase* ph, 
             else stage_h<T>(a, tab, region, base, pairs, p.blocks * Weights<W>::kCols);
             __syncthreads();
         }
-        MoeBatch<T, W, PHASE> batch{a, p, tab, feed, fifo, slot, region, red, base};
-        while (i0 < end) {
-            const int i1 = p.batch_end(i0);
-            batch.run(i0, i1);
-            i0 = i1;
-        }
+        moe_window<T, W, PHASE>(a, p, tab, feed, fifo, slot, region, parts, base, i0, end);
+        i0 = end;
     }
 }
 
@@ -1355,10 +1398,6 @@ __device__ __forceinline__ void finish(const MoeArgs& a) {
     }
 }
 
-// What an item's start and end, and a join, take of a warp's time, in blocks of
-// weights (from a token's 5 or 6 items of 32 blocks a block: 10 us in teams of 8,
-// 15 in teams of 16, which by blocks alone would be the faster).
-constexpr int kItemCost = 3, kJoinCost = 2;
 constexpr int kPrefetch = 8;       // strips of the second phase that a block asks for ahead
 
 // The whole layer in one cooperative launch, one block per SM:
@@ -1454,26 +1493,18 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
             if (local < 0 || local >= a.n_local) continue;
             const int pair = pair_of(tab, local, t);
             tab.token[pair] = uint8_t(t);
-            tab.pair_c[pair] = tab.c[i];
+            if (a.fold) tab.pair_c[pair] = tab.c[i];
         }
     } else {
-        // The phases' items.  Whole rounds of 16 go to single warps, and the rest to the
-        // team that is through soonest: lane 8 k + i looks at phase k and teams of 2^i.
-        const int k = lane >> 3 & 1, team = 1 << min(lane & 7, 4), teams = kWarps / team;
-        const int passes = int(tab.total & 0xFFFF), tiles = tab.most > 8 ? 2 : 1;
+        // The phases' items: lane k looks at phase k.
+        const int k = lane & 1;
+        const int passes = int(tab.total & 0xFFFF);
         const int cols = k ? a.inter : a.hidden, strips = k ? (a.hidden + 15) / 16 : (a.inter + 7) / 8;
-        const int blocks = (cols + Weights<W>::kCols - 1) / Weights<W>::kCols;
         const uint32_t all = k && a.fold ? strips : passes * strips;    // at most 1024 passes of 2048 strips
         const uint32_t grid = gridDim.x;
         // (Products under 2^32 for grids of up to 1024 blocks.)
-        const int f0 = int(blockIdx.x * all / grid), n = int((blockIdx.x + 1) * all / grid) - f0, rest = n % kWarps;
-        const int batch = team == 1 ? kWarps : kJoinBytes / (512 * tiles * team) / teams * teams;
-        const uint32_t cost = (rest + teams - 1) / teams * ((blocks + team - 1) / team + kItemCost) +
-                              (team == 1 ? 0 : (rest + batch - 1) / batch * kJoinCost);
-        uint32_t best = min(cost, 0xFFFFFFu) << 3 | uint32_t(min(lane & 7, 4));
-        const uint32_t own = best;
-        for (int o = 1; o < 8; o *= 2) best = min(best, __shfl_xor_sync(~0u, best, o));
-        if (lane < 16 && own == best && (lane & 7) <= 4) {
+        const int f0 = int(blockIdx.x * all / grid), n = int((blockIdx.x + 1) * all / grid) - f0;
+        if (lane < 2) {
             MoePhase p;
             p.base = k ? a.w2 : a.w13;
             p.m.rows = k ? a.hidden : 2 * a.inter;
@@ -1482,16 +1513,13 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
             p.m.strips = strips;
             p.m.blocks = (cols + kBlock - 1) / kBlock;
             p.m.matrix_bytes = k ? a.m2_bytes : a.m13_bytes;
-            p.blocks = blocks;
+            p.blocks = (cols + Weights<W>::kCols - 1) / Weights<W>::kCols;
             p.f0 = f0;
             p.n = n;
-            p.n1 = n - rest;
-            p.team = team;
-            p.batch = batch;
-            p.tiles = tiles;
+            p.tiles = tab.most > 8 ? 2 : 1;
             p.strips = strips;
             p.inverse = uint32_t(0xFFFFFFFFu / uint32_t(strips)) + 1;
-            p.window = 1 << 20;
+            p.window = 2 * kMaxPairs;          // no end within the passes
             if (n > 0 && !(k && a.fold) && !(!k && a.all_x)) {
                 // All of the block's passes where their tokens fit, else as many as always do.
                 const int rows = k ? a.h_rows : a.x_rows, from = p.pass(f0), to = p.pass(f0 + n - 1);
@@ -1704,6 +1732,7 @@ rr_status launch_moe(MoeArgs a, cudaStream_t stream) {
     constexpr int kCols = Weights<W>::kCols;
     // Rows 64 bytes past a multiple of 128, as for the matrix-vector products.
     const auto pitch = [](int cols) { return (cols + kCols - 1) / kCols * (2 * kCols) + 64; };
+    static_assert(kSmem - kFixed >= 2 * kMaxHidden + 64 && kSmem - kFixed >= 2 * (2 * kMaxInter + 64), "the longest rows fit");
     a.x_pitch = pitch(a.hidden);
     a.h_pitch = pitch(a.inter);
     const int each = std::max(a.x_pitch, 2 * a.h_pitch), room = kSmem - kFixed;
