@@ -885,6 +885,54 @@ __device__ __forceinline__ void choose(const MoeArgs& a, MoeTables& tab, int t, 
     }
 }
 
+// The same for up to 4 tokens and 128 experts by the whole block: an expert's rank is
+// the number of those before it, counted by four threads, in place of top_k exchanges
+// one after another (one token: FIXME us, so).  buffer: 5 KB.
+__device__ __forceinline__ void choose_few(const MoeArgs& a, MoeTables& tab, char* buffer) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    uint32_t* const key = reinterpret_cast<uint32_t*>(buffer);               // [4][128]
+    float* const logit = reinterpret_cast<float*>(buffer + 2048);            // [4][128]
+    float* const best = reinterpret_cast<float*>(buffer + 4096);             // [4][16]
+    int* const id = reinterpret_cast<int*>(buffer + 4096 + 256);             // [4][16]
+    {
+        const int t = tid >> 7, e = tid & 127;
+        const bool in = t < a.tokens && e < a.n_experts;
+        const float l = in ? __ldcg(a.logits + t * a.n_experts + e) : 0.0f;
+        key[tid] = in ? rank_key(l) : 0;
+        logit[tid] = l;
+    }
+    __syncthreads();
+    for (int t = 0; t < a.tokens; ++t) {
+        const int e = tid >> 2, from = 32 * (tid & 3);
+        const uint32_t mine = key[128 * t + e];
+        int before = 0;
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            const uint4 k = *reinterpret_cast<const uint4*>(key + 128 * t + from + i);
+            before += k.x > mine || (k.x == mine && from + i < e);
+            before += k.y > mine || (k.y == mine && from + i + 1 < e);
+            before += k.z > mine || (k.z == mine && from + i + 2 < e);
+            before += k.w > mine || (k.w == mine && from + i + 3 < e);
+        }
+        before += __shfl_xor_sync(~0u, before, 1);
+        before += __shfl_xor_sync(~0u, before, 2);
+        if ((tid & 3) == 0 && e < a.n_experts && before < a.top_k)
+            best[16 * t + before] = logit[128 * t + e], id[16 * t + before] = e;
+    }
+    __syncthreads();
+    if (warp < a.tokens) {
+        const float top = best[16 * warp];
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (32 * i + lane < a.n_experts) sum += expf(logit[128 * warp + 32 * i + lane] - top);
+        sum = warp_sum(sum);
+        float p = lane < a.top_k ? expf(best[16 * warp + lane] - top) / sum : 0.0f;
+        if (a.norm) p /= warp_sum(p);
+        if (lane < a.top_k) take_choice(a, tab, warp * a.top_k + lane, warp, id[16 * warp + lane], p);
+    }
+}
+
 // A barrier of all blocks, in two halves.  What a block wrote before it arrived is
 // there for every block that has waited.  Within one cluster it is the hardware's;
 // else the wait is bounded: false when it ran out (about two seconds), which marks
@@ -925,6 +973,7 @@ __device__ __forceinline__ bool grid_wait(const MoeArgs& a, MoeTables& tab, int 
         }
     }
     __syncthreads();
+    if (tab.stop) copy_wait<0>();
     return tab.stop == 0;
 }
 
@@ -1022,31 +1071,31 @@ struct Feed {
 };
 
 // Tokens' rows (16-bit) to shared memory, zero-filled to whole blocks: those of
-// pairs first, first + 1, ..., or with all_x simply tokens 0, 1, ...
+// pairs first, first + 1, ..., or with all_x simply tokens 0, 1, ...  (Copies are in
+// flight when this returns: a group of cp.async.)
 __device__ __forceinline__ void stage_tokens(const MoeArgs& a, const MoeTables& tab, char* to, int first, int count,
                                              int cols) {
-#pragma unroll 4
-    for (int i = 0; i < count; ++i) {
-        const uint16_t* const row = a.x + (a.all_x ? i : tab.token[first + i]) * a.ldx;
-        char* const dst = to + i * a.x_pitch;
-        if (a.x_vec) {
+    if (a.x_vec) {
+        for (int i = 0; i < count; ++i) {
+            const uint16_t* const row = a.x + (a.all_x ? i : tab.token[first + i]) * a.ldx;
             for (int c = 8 * threadIdx.x; c < cols; c += 8 * kProdThreads) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (c + 8 <= a.hidden) {
-                    v = *reinterpret_cast<const uint4*>(row + c);
-                } else if (c < a.hidden) {
-                    uint32_t p[4] = {0, 0, 0, 0};
-                    for (int k = 0; c + k < a.hidden; ++k) p[k / 2] |= uint32_t(row[c + k]) << (16 * (k % 2));
-                    v = make_uint4(p[0], p[1], p[2], p[3]);
-                }
-                *reinterpret_cast<uint4*>(dst + 2 * c) = v;
+                const int left = a.hidden - c;
+                copy_async_cut(smem_at(to + i * a.x_pitch + 2 * c), row + (left > 0 ? c : 0),
+                               left >= 8 ? 16 : left > 0 ? 2 * left : 0);
             }
-        } else {
-#pragma unroll 4
-            for (int c = threadIdx.x; c < cols; c += kProdThreads)
+        }
+    } else {
+        // A warp a row, or part of one.
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, split = count >= kWarps ? 1 : kWarps / count;
+        for (int i = warp / split; i < count; i += kWarps / split) {
+            const uint16_t* const row = a.x + (a.all_x ? i : tab.token[first + i]) * a.ldx;
+            char* const dst = to + i * a.x_pitch;
+#pragma unroll 8
+            for (int c = 32 * (warp % split) + lane; c < cols; c += 32 * split)
                 *reinterpret_cast<uint16_t*>(dst + 2 * c) = c < a.hidden ? row[c] : uint16_t(0);
         }
     }
+    copy_commit();
 }
 
 // The power of two that brings a float16 token's largest h to 2^14..2^15.
@@ -1098,6 +1147,7 @@ __device__ __forceinline__ void moe_put(const MoeArgs& a, const MoePhase& p, con
     const int pass = p.pass(f), strip = f - pass * p.strips;
     const int first = tab.pass_first[pass], count = tab.pass_count[pass];
     const int64_t lo = p.m.row(strip, lane >> 2), hi = p.m.row(strip, 8 + (lane >> 2));
+    uint32_t top[2] = {0, 0};
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int tok = 8 * n + 2 * (lane & 3) + k;
@@ -1105,8 +1155,7 @@ __device__ __forceinline__ void moe_put(const MoeArgs& a, const MoePhase& p, con
         if (PHASE == 0) {
             const float h = silu(v[k]) * v[2 + k];
             __stcg(a.h + int64_t(first + tok) * a.h_ld + lo, h);
-            if (std::is_same<T, F16>::value && fabsf(h) < INFINITY)
-                atomicMax(a.h_top + first + tok, __float_as_uint(fabsf(h)));
+            top[k] = fabsf(h) < INFINITY ? __float_as_uint(fabsf(h)) : 0;
         } else {
             const float s = std::is_same<T, F16>::value ? tab.scale[first + tok] : 1.0f;
             float* const y = a.y + int64_t(first + tok) * a.y_ld;
@@ -1114,6 +1163,13 @@ __device__ __forceinline__ void moe_put(const MoeArgs& a, const MoePhase& p, con
             if (hi >= 0) __stcg(y + hi, v[2 + k] * s);
         }
     }
+    if (PHASE == 0 && std::is_same<T, F16>::value)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {      // of the strip's rows, one lane each
+            const int tok = 8 * n + 2 * (lane & 3) + k;
+            for (int o = 4; o < 32; o *= 2) top[k] = max(top[k], __shfl_xor_sync(~0u, top[k], o));
+            if (lane < 4 && tok < count && top[k]) atomicMax(a.h_top + first + tok, top[k]);
+        }
 }
 
 // Blocks [b, stop) of item f by one warp: its sums go out where `whole` says that the
@@ -1234,6 +1290,7 @@ __device__ __forceinline__ void moe_phase(const MoeArgs& a, const MoePhase* ph, 
             __syncthreads();
             if (PHASE == 0) stage_tokens(a, tab, region, base, pairs, p.blocks * Weights<W>::kCols);
             else stage_h<T>(a, tab, region, base, pairs, p.blocks * Weights<W>::kCols);
+            copy_wait<0>();
             __syncthreads();
         }
         moe_window<T, W, PHASE>(a, p, tab, feed, fifo, slot, region, parts, base, i0, end);
@@ -1441,7 +1498,8 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
     // Up to a token a warp, every block chooses for itself; more tokens are shared out
     // over the blocks (64 of them took every block 9 us, against 2 and a barrier).
     const bool far = a.tokens > kWarps;
-    for (int t = far ? warp * gridDim.x + blockIdx.x : warp; t < a.tokens; t += far ? kWarps * gridDim.x : kWarps) {
+    if (a.tokens <= 4 && a.n_experts <= 128) choose_few(a, tab, smem);
+    else for (int t = far ? warp * gridDim.x + blockIdx.x : warp; t < a.tokens; t += far ? kWarps * gridDim.x : kWarps) {
         if (a.n_experts <= 128) choose<4>(a, tab, t, lane, far);
         else choose<kMaxExperts / 32>(a, tab, t, lane, far);
     }
@@ -1529,6 +1587,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
             ph[k] = p;
         }
     }
+    copy_wait<0>();        // the tokens
     __syncthreads();
 
     char* const fifo = smem + warp * (Weights<W>::kStages * Weights<W>::kBytes);
@@ -1549,10 +1608,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
         }
         if (W != 1 && warp == kWarps / 2 && ph[1].n > 0)
             for (int i = lane; i < passes; i += 32) prefetch_item<W>(ph[1], tab.pass_expert[i], ph[1].f0);
-        if (!grid_wait(a, tab, 1)) {
-            copy_wait<0>();
-            return;
-        }
+        if (!grid_wait(a, tab, 1)) return;
         stage_fold<T, W>(a, tab, region, int(tab.total >> 16), ph[1].blocks * Weights<W>::kCols);
         __syncthreads();
         moe_fold<T, W>(a, ph[1], tab, fold, fifo, slot, region, red, passes);
@@ -1565,10 +1621,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
         const int f = ph[1].f0 + lane, pass = ph[1].pass(f);
         prefetch_item<W>(ph[1], tab.pass_expert[pass], f - pass * ph[1].strips);
     }
-    if (!grid_wait(a, tab, 1)) {
-        copy_wait<0>();
-        return;
-    }
+    if (!grid_wait(a, tab, 1)) return;
     moe_phase<T, W, 1>(a, ph, tab, feed, fifo, slot, region, red);
     copy_wait<0>();
     grid_arrive(a, 2);
