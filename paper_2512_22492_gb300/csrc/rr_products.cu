@@ -6,8 +6,8 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <climits>
-#include <mutex>
 #include <type_traits>
 
 #include "rr_internal.h"
@@ -815,7 +815,7 @@ __device__ __forceinline__ void logit_item(const MoeArgs& a, int e0, int t0, flo
     if (threadIdx.x < 128) {
         const int i = threadIdx.x;
         float v = 0.0f;
-#pragma unroll
+#pragma unroll 4
         for (int q = 0; q < kWarps; ++q) v += reinterpret_cast<const float*>(red)[128 * q + i];
         const int tok = t0 + i / 16 + 8 * (i >> 1 & 1), e = e0 + 2 * (i / 4 % 4) + (i & 1);
         if (tok < a.tokens && e < a.n_experts) __stcg(a.logits + tok * a.n_experts + e, v);
@@ -882,54 +882,6 @@ __device__ __forceinline__ void choose(const MoeArgs& a, MoeTables& tab, int t, 
         } else {
             take_choice(a, tab, i, t, my_id, p);
         }
-    }
-}
-
-// The same for up to 4 tokens and 128 experts by the whole block: an expert's rank is
-// the number of those before it, counted by four threads, in place of top_k exchanges
-// one after another (one token: FIXME us, so).  buffer: 5 KB.
-__device__ __forceinline__ void choose_few(const MoeArgs& a, MoeTables& tab, char* buffer) {
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    uint32_t* const key = reinterpret_cast<uint32_t*>(buffer);               // [4][128]
-    float* const logit = reinterpret_cast<float*>(buffer + 2048);            // [4][128]
-    float* const best = reinterpret_cast<float*>(buffer + 4096);             // [4][16]
-    int* const id = reinterpret_cast<int*>(buffer + 4096 + 256);             // [4][16]
-    {
-        const int t = tid >> 7, e = tid & 127;
-        const bool in = t < a.tokens && e < a.n_experts;
-        const float l = in ? __ldcg(a.logits + t * a.n_experts + e) : 0.0f;
-        key[tid] = in ? rank_key(l) : 0;
-        logit[tid] = l;
-    }
-    __syncthreads();
-    for (int t = 0; t < a.tokens; ++t) {
-        const int e = tid >> 2, from = 32 * (tid & 3);
-        const uint32_t mine = key[128 * t + e];
-        int before = 0;
-#pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            const uint4 k = *reinterpret_cast<const uint4*>(key + 128 * t + from + i);
-            before += k.x > mine || (k.x == mine && from + i < e);
-            before += k.y > mine || (k.y == mine && from + i + 1 < e);
-            before += k.z > mine || (k.z == mine && from + i + 2 < e);
-            before += k.w > mine || (k.w == mine && from + i + 3 < e);
-        }
-        before += __shfl_xor_sync(~0u, before, 1);
-        before += __shfl_xor_sync(~0u, before, 2);
-        if ((tid & 3) == 0 && e < a.n_experts && before < a.top_k)
-            best[16 * t + before] = logit[128 * t + e], id[16 * t + before] = e;
-    }
-    __syncthreads();
-    if (warp < a.tokens) {
-        const float top = best[16 * warp];
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (32 * i + lane < a.n_experts) sum += expf(logit[128 * warp + 32 * i + lane] - top);
-        sum = warp_sum(sum);
-        float p = lane < a.top_k ? expf(best[16 * warp + lane] - top) / sum : 0.0f;
-        if (a.norm) p /= warp_sum(p);
-        if (lane < a.top_k) take_choice(a, tab, warp * a.top_k + lane, warp, id[16 * warp + lane], p);
     }
 }
 
@@ -1090,7 +1042,7 @@ __device__ __forceinline__ void stage_tokens(const MoeArgs& a, const MoeTables& 
         for (int i = warp / split; i < count; i += kWarps / split) {
             const uint16_t* const row = a.x + (a.all_x ? i : tab.token[first + i]) * a.ldx;
             char* const dst = to + i * a.x_pitch;
-#pragma unroll 8
+#pragma unroll 16
             for (int c = 32 * (warp % split) + lane; c < cols; c += 32 * split)
                 *reinterpret_cast<uint16_t*>(dst + 2 * c) = c < a.hidden ? row[c] : uint16_t(0);
         }
@@ -1498,8 +1450,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
     // Up to a token a warp, every block chooses for itself; more tokens are shared out
     // over the blocks (64 of them took every block 9 us, against 2 and a barrier).
     const bool far = a.tokens > kWarps;
-    if (a.tokens <= 4 && a.n_experts <= 128) choose_few(a, tab, smem);
-    else for (int t = far ? warp * gridDim.x + blockIdx.x : warp; t < a.tokens; t += far ? kWarps * gridDim.x : kWarps) {
+    for (int t = far ? warp * gridDim.x + blockIdx.x : warp; t < a.tokens; t += far ? kWarps * gridDim.x : kWarps) {
         if (a.n_experts <= 128) choose<4>(a, tab, t, lane, far);
         else choose<kMaxExperts / 32>(a, tab, t, lane, far);
     }
@@ -1678,18 +1629,34 @@ rr_status cuda_fail(cudaError_t e, const char* what) {
         if (s_ != RR_OK) return s_;      \
     } while (0)
 
-// Memory of the current device, `align`ed.
-rr_status check_device(const void* p, size_t align, const char* what) {
+// Memory of device `dev`, the current one, `align`ed.
+rr_status check_device(int dev, const void* p, size_t align, const char* what) {
     if (!p || (uintptr_t)p % align) return rr_fail(RR_EINVAL, "%s is NULL or not %zu-byte aligned", what, align);
     cudaPointerAttributes at;
-    int dev = -1;
-    RR_CUDA(cudaGetDevice(&dev));
     if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
         cudaGetLastError();
         return rr_fail(RR_EINVAL, "%s is not memory of this GPU", what);
     }
     if (at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeDevice && at.device == dev)) return RR_OK;
     return rr_fail(RR_EINVAL, "%s is not memory of this GPU", what);
+}
+
+constexpr int kMaxDevices = 16;
+
+rr_status current_device(int* dev) {
+    RR_CUDA(cudaGetDevice(dev));
+    if (*dev < 0 || *dev >= kMaxDevices) return rr_fail(RR_EINVAL, "device %d: 0..%d", *dev, kMaxDevices - 1);
+    return RR_OK;
+}
+
+// Lets a kernel have `smem` bytes of dynamic shared memory, once per kernel and device
+// (`done`: its own bits, one a device).
+template <class K>
+cudaError_t allow_smem(K* kernel, int smem, int dev, std::atomic<uint32_t>* done) {
+    if (done->load(std::memory_order_relaxed) >> dev & 1) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) done->fetch_or(1u << dev, std::memory_order_relaxed);
+    return e;
 }
 
 rr_status check_quant(const rr_quant* q) {
@@ -1778,7 +1745,7 @@ MoeSpace moe_space(const rr_moe_layer* L, int64_t tokens) {
 }
 
 template <class T, int W>
-rr_status launch_moe(MoeArgs a, cudaStream_t stream) {
+rr_status launch_moe(MoeArgs a, int dev, cudaStream_t stream) {
     // Tokens that a pass holds in shared memory, by the longer of the two phases' rows.
     constexpr int kFixed = kWarps * Weights<W>::kStages * Weights<W>::kBytes + kJoinBytes +
                            (sizeof(MoeTables) + 127) / 128 * 128 + 1024 /* static */;
@@ -1803,9 +1770,10 @@ rr_status launch_moe(MoeArgs a, cudaStream_t stream) {
     // A layer of little work runs in one cluster, whose barriers and whose launch
     // cost less than a grid's, although 8 SMs then read all of its weights.
     const int64_t bytes = std::min<int64_t>(int64_t(a.tokens) * a.top_k, a.n_local) * (a.m13_bytes + a.m2_bytes);
+    static std::atomic<uint32_t> ready{0};
+    RR_CUDA(allow_smem(rr_moe_kernel<T, W>, kSmem - 1024, dev, &ready));
     a.one = bytes <= kClusterBytes;
     if (a.one) {
-        RR_CUDA(cudaFuncSetAttribute(rr_moe_kernel<T, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem - 1024));
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -1822,22 +1790,14 @@ rr_status launch_moe(MoeArgs a, cudaStream_t stream) {
         RR_CUDA(cudaLaunchKernelEx(&cfg, rr_moe_kernel<T, W>, a));
         return RR_OK;
     }
-    static std::mutex mutex;
-    static int grids[16] = {};
-    int dev = 0, grid;
-    RR_CUDA(cudaGetDevice(&dev));
-    if (dev < 0 || dev > 15) return rr_fail(RR_EINVAL, "device %d", dev);
-    {
-        const std::lock_guard<std::mutex> lock(mutex);
-        if (!grids[dev]) {
-            int sms = 0, coop = 0;
-            RR_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-            RR_CUDA(cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev));
-            if (!coop) return rr_fail(RR_ECUDA, "the device has no cooperative launches");
-            RR_CUDA(cudaFuncSetAttribute(rr_moe_kernel<T, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem - 1024));
-            grids[dev] = sms;
-        }
-        grid = grids[dev];
+    static std::atomic<int> grids[kMaxDevices] = {};
+    int grid = grids[dev].load(std::memory_order_relaxed);
+    if (!grid) {
+        int coop = 0;
+        RR_CUDA(cudaDeviceGetAttribute(&grid, cudaDevAttrMultiProcessorCount, dev));
+        RR_CUDA(cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, dev));
+        if (!coop) return rr_fail(RR_ECUDA, "the device has no cooperative launches");
+        grids[dev].store(grid, std::memory_order_relaxed);
     }
     // (Programmatic dependent launch besides left the gap between two launches at
     // the same 4 us.)
@@ -1891,8 +1851,10 @@ extern "C" rr_status rr_quantize(const rr_quant* q, const void* w, int64_t ld, v
     rr_clear_error();
     RR_TRY(check_quant(q));
     if (ld < q->cols) return rr_fail(RR_EINVAL, "row stride %lld of rows of %lld", (long long)ld, (long long)q->cols);
-    RR_TRY(check_device(w, 2, "w"));
-    RR_TRY(check_device(packed, 16, "packed"));
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, w, 2, "w"));
+    RR_TRY(check_device(dev, packed, 16, "packed"));
     const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
     uint32_t total;
     unsigned grid;
@@ -1914,8 +1876,10 @@ extern "C" rr_status rr_dequantize(const rr_quant* q, const void* packed, void* 
     RR_TRY(check_quant(q));
     if (f32 != 0 && f32 != 1) return rr_fail(RR_EINVAL, "f32 is 0 or 1, not %d", f32);
     if (ld < q->cols) return rr_fail(RR_EINVAL, "row stride %lld of rows of %lld", (long long)ld, (long long)q->cols);
-    RR_TRY(check_device(packed, 16, "packed"));
-    RR_TRY(check_device(w, f32 ? 4 : 2, "w"));
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, packed, 16, "packed"));
+    RR_TRY(check_device(dev, w, f32 ? 4 : 2, "w"));
     const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
     uint32_t total;
     unsigned grid;
@@ -1943,40 +1907,34 @@ struct MatvecShape {
 // 76, 36 and 15 of 1, 2, 4 and 8 blocks, since a cluster stays within one GPC).
 // Asked once per device.
 template <class K>
-int clusters_at_once(K* kernel, int cluster) {
-    static std::mutex mutex;
-    static int known[16][4] = {};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev > 15) return 1;
-    const int i = cluster == 1 ? 0 : cluster == 2 ? 1 : cluster == 4 ? 2 : 3;
-    const std::lock_guard<std::mutex> lock(mutex);
-    if (!known[dev][i]) {
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = unsigned(cluster);
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(unsigned(cluster));
-        cfg.blockDim = dim3(kProdThreads);
-        cfg.dynamicSmemBytes = kSmem;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        int n = 0;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
-            cudaGetLastError();
-            return 1;
-        }
-        known[dev][i] = n;
+int clusters_at_once(K* kernel, int dev, int cluster) {
+    static std::atomic<int> known[kMaxDevices][9] = {};
+    int n = known[dev][cluster].load(std::memory_order_relaxed);
+    if (n) return n;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = unsigned(cluster);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(cluster));
+    cfg.blockDim = dim3(kProdThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        return 1;
     }
-    return known[dev][i];
+    known[dev][cluster].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 // How a product is shared out, for a.tokens tokens; false if these do not fit.  The
 // fewest blocks of a cluster for which its share of the tokens fits a block's shared
 // memory, with 6 blocks of weights in flight a warp where there is room, else 4;
 // more, where strips are too few to go round and a block's share is long.
-bool matvec_shape(MatvecArgs* a, int group, MatvecShape* shape) {
+bool matvec_shape(MatvecArgs* a, int group, int dev, MatvecShape* shape) {
     const int tiles = a->tokens > 8 ? 2 : 1, part = 512 * tiles;
     int64_t best = INT64_MAX;
     for (int cluster = 1; cluster <= 8 && cluster <= a->m.blocks; cluster *= 2) {
@@ -1984,7 +1942,7 @@ bool matvec_shape(MatvecArgs* a, int group, MatvecShape* shape) {
         // Rows 64 bytes past a multiple of 128, so that two tokens' rows are on
         // different halves of the banks.
         const int64_t pitch = blocks * 2 * kBlock + 64;
-        const int64_t groups = std::min<int64_t>(clusters_at_once(rr_matvec_kernel<BF16, 128, 1, 2, 6>, cluster), a->m.strips);
+        const int64_t groups = std::min<int64_t>(clusters_at_once(rr_matvec_kernel<BF16, 128, 1, 2, 6>, dev, cluster), a->m.strips);
         const int64_t strips = (a->m.strips + groups - 1) / groups;
         for (int stages = 6; stages >= 4; stages -= 2) {
             const int64_t room = kSmem - kWarps * (stages * block_bytes(group) + part) - pitch * a->tokens;
@@ -2006,9 +1964,11 @@ bool matvec_shape(MatvecArgs* a, int group, MatvecShape* shape) {
     return best != INT64_MAX;
 }
 
-cudaError_t launch_matvec(void (*kernel)(MatvecArgs), const MatvecArgs& a, const MatvecShape& shape,
-                          cudaStream_t stream) {
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+template <class T, int G, int NT, int U, int ST>
+cudaError_t launch_matvec(const MatvecArgs& a, const MatvecShape& shape, int dev, cudaStream_t stream) {
+    static std::atomic<uint32_t> ready{0};
+    const auto kernel = rr_matvec_kernel<T, G, NT, U, ST>;
+    const cudaError_t e = allow_smem(kernel, kSmem, dev, &ready);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -2043,9 +2003,11 @@ extern "C" rr_status rr_matvec(const rr_quant* q, const void* packed, const void
         return rr_fail(RR_EINVAL, "row strides %lld and %lld of rows of %lld and %lld", (long long)ldx,
                        (long long)ldo, (long long)q->cols, (long long)n_out);
     if (n_tokens == 0) return RR_OK;
-    RR_TRY(check_device(packed, 16, "packed"));
-    RR_TRY(check_device(x, 2, "x"));
-    RR_TRY(check_device(out, f32 ? 4 : 2, "out"));
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, packed, 16, "packed"));
+    RR_TRY(check_device(dev, x, 2, "x"));
+    RR_TRY(check_device(dev, out, f32 ? 4 : 2, "out"));
     return with_group(q->dtype, q->group, [&](auto t, auto g) -> rr_status {
         using T = decltype(t);
         constexpr int G = decltype(g)::value ? decltype(g)::value : 128;
@@ -2063,13 +2025,15 @@ extern "C" rr_status rr_matvec(const rr_quant* q, const void* packed, const void
             a.x = static_cast<const uint16_t*>(x) + n0 * ldx;
             a.out = static_cast<char*>(out) + n0 * ldo * (f32 ? 4 : 2);
             MatvecShape shape;
-            while (!matvec_shape(&a, G, &shape)) {
+            while (!matvec_shape(&a, G, dev, &shape)) {
                 if (a.tokens == 1) return rr_fail(RR_ELAYOUT, "rows of %lld columns", (long long)q->cols);
                 a.tokens = (a.tokens + 1) / 2;
             }
-            const auto kernel = a.tokens > 8 ? shape.deep ? rr_matvec_kernel<T, G, 2, 2, 6> : rr_matvec_kernel<T, G, 2, 1, 4>
-                                             : shape.deep ? rr_matvec_kernel<T, G, 1, 2, 6> : rr_matvec_kernel<T, G, 1, 1, 4>;
-            const cudaError_t e = launch_matvec(kernel, a, shape, stream);
+            const cudaError_t e = a.tokens > 8
+                                      ? shape.deep ? launch_matvec<T, G, 2, 2, 6>(a, shape, dev, stream)
+                                                   : launch_matvec<T, G, 2, 1, 4>(a, shape, dev, stream)
+                                      : shape.deep ? launch_matvec<T, G, 1, 2, 6>(a, shape, dev, stream)
+                                                   : launch_matvec<T, G, 1, 1, 4>(a, shape, dev, stream);
             if (e != cudaSuccess) return cuda_fail(e, "rr_matvec");
         }
         return RR_OK;
@@ -2101,14 +2065,16 @@ extern "C" rr_status rr_moe(const rr_moe_layer* L, const void* router, const voi
     const MoeSpace S = moe_space(L, n_tokens);
     if (workspace_bytes < S.total)
         return rr_fail(RR_EINVAL, "workspace of %lld bytes, the call needs %lld", (long long)workspace_bytes, (long long)S.total);
-    RR_TRY(check_device(router, 16, "router"));
-    RR_TRY(check_device(w13, 16, "w13"));
-    RR_TRY(check_device(w2, 16, "w2"));
-    RR_TRY(check_device(x, 2, "x"));
-    RR_TRY(check_device(out, 2, "out"));
-    if (ids) RR_TRY(check_device(ids, 4, "ids"));
-    if (weights) RR_TRY(check_device(weights, 4, "weights"));
-    RR_TRY(check_device(workspace, 16, "workspace"));
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, router, 16, "router"));
+    RR_TRY(check_device(dev, w13, 16, "w13"));
+    RR_TRY(check_device(dev, w2, 16, "w2"));
+    RR_TRY(check_device(dev, x, 2, "x"));
+    RR_TRY(check_device(dev, out, 2, "out"));
+    if (ids) RR_TRY(check_device(dev, ids, 4, "ids"));
+    if (weights) RR_TRY(check_device(dev, weights, 4, "weights"));
+    RR_TRY(check_device(dev, workspace, 16, "workspace"));
     char* const ws = static_cast<char*>(workspace);
     MoeArgs a;
     a.router = static_cast<const uint16_t*>(router);
@@ -2144,9 +2110,9 @@ extern "C" rr_status rr_moe(const rr_moe_layer* L, const void* router, const voi
     return with_group(L->dtype, L->group, [&](auto t, auto g) -> rr_status {
         using T = decltype(t);
         constexpr int G = decltype(g)::value;
-        if constexpr (G != 0) return launch_moe<T, G>(a, stream);
-        else if (L->hidden % 8 == 0 && L->inter % 8 == 0) return launch_moe<T, 0>(a, stream);
-        else return launch_moe<T, 1>(a, stream);
+        if constexpr (G != 0) return launch_moe<T, G>(a, dev, stream);
+        else if (L->hidden % 8 == 0 && L->inter % 8 == 0) return launch_moe<T, 0>(a, dev, stream);
+        else return launch_moe<T, 1>(a, dev, stream);
     });
 }
 
@@ -2156,7 +2122,9 @@ extern "C" rr_status rr_moe_check(const rr_moe_layer* L, int32_t max_tokens, voi
     RR_TRY(check_moe(L));
     if (max_tokens < 1 || max_tokens > RR_MOE_MAX_TOKENS)
         return rr_fail(RR_EINVAL, "%d tokens: 1..%d", max_tokens, RR_MOE_MAX_TOKENS);
-    RR_TRY(check_device(workspace, 16, "workspace"));
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, workspace, 16, "workspace"));
     uint32_t err = 0;
     RR_CUDA(cudaMemcpyAsync(&err, workspace, 4, cudaMemcpyDeviceToHost, stream));
     RR_CUDA(cudaStreamSynchronize(stream));

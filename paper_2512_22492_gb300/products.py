@@ -12,7 +12,7 @@ from __future__ import annotations
 
 import ctypes
 
-from .rr import _check, _DST_DTYPES, _lib, _sig, _stream, _vp
+from .rr import RR_OK, _check, _DST_DTYPES, _lib, _sig, _stream, _vp
 
 RR_MATVEC_MAX_TOKENS = 16
 RR_MOE_MAX_TOKENS = 64
@@ -57,22 +57,39 @@ def _torch_type(name: str):
 
 def _rows(x, cols: int, dtype, what: str):
     """(rows, row stride) of a token tensor [rows, cols] (or [cols]) of `dtype`."""
-    if x.dtype != dtype:
+    if x.dtype is not dtype:
         raise ValueError(f"{what}: elements of {x.dtype}, expected {dtype}")
-    shape = x.shape
-    if len(shape) == 1 and shape[0] == cols:
-        n, ld = 1, cols
-    elif len(shape) == 2 and shape[1] == cols:
-        n, ld = shape[0], x.stride(0)
-        if n < 2:
-            ld = cols
-        elif ld < cols:
+    dim = x.dim()
+    if dim == 2 and x.size(1) == cols:
+        n = x.size(0)
+        if x.is_contiguous():
+            return n, cols
+        ld = x.stride(0) if n > 1 else cols
+        if ld < cols:
             raise ValueError(f"{what}: rows overlap")
+    elif dim == 1 and x.size(0) == cols:
+        n, ld = 1, cols
     else:
-        raise ValueError(f"{what}: shape {tuple(shape)}, expected [n, {cols}]")
+        raise ValueError(f"{what}: shape {tuple(x.shape)}, expected [n, {cols}]")
     if cols > 1 and x.stride(-1) != 1:
         raise ValueError(f"{what}: the elements of a row must be contiguous")
     return n, ld
+
+
+def _stream_of(x, stream) -> int:
+    """The stream's handle; None: the current one of x's device."""
+    if stream is None and _raw_stream is not None and x.is_cuda:
+        return _raw_stream(x.get_device())
+    return _stream(stream)
+
+
+def _find_raw_stream():
+    # The call that torch's own code generators use; it is not public.
+    import torch
+    return getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+_raw_stream = _find_raw_stream()
 
 
 class Quantized:
@@ -147,7 +164,7 @@ def _matrices(q: Quantized, w, dtypes, what: str) -> int:
 def rr_quantize(q: Quantized, w, stream=None) -> None:
     """16-bit matrices -> q (asynchronous on `stream`)."""
     ld = _matrices(q, w, (q.torch_dtype,), "w")
-    _check(_lib.rr_quantize(q._ref, w.data_ptr(), ld, q._p, _stream(stream)), "rr_quantize")
+    _check(_lib.rr_quantize(q._ref, w.data_ptr(), ld, q._p, _stream_of(w, stream)), "rr_quantize")
 
 
 def rr_dequantize(q: Quantized, out, stream=None) -> None:
@@ -156,23 +173,28 @@ def rr_dequantize(q: Quantized, out, stream=None) -> None:
     import torch
     ld = _matrices(q, out, (q.torch_dtype, torch.float32), "out")
     _check(_lib.rr_dequantize(q._ref, q._p, out.data_ptr(), ld,
-                              int(out.dtype == torch.float32), _stream(stream)), "rr_dequantize")
+                              int(out.dtype == torch.float32), _stream_of(out, stream)), "rr_dequantize")
 
 
 def rr_matvec(q: Quantized, x, out, stream=None) -> None:
     """out[t] = W x[t] for up to 16 rows of x (asynchronous on `stream`); with
     q.pair, silu(gate) * up.  `out` is of q's 16-bit type or float32."""
     n, ldx = _rows(x, q.cols, q.torch_dtype, "x")
-    f32 = out.dtype != q.torch_dtype
-    if f32:
-        import torch
-        if out.dtype != torch.float32:
-            raise ValueError(f"out: elements of {out.dtype}, expected {q.torch_dtype} or float32")
+    f32 = out.dtype is not q.torch_dtype
+    if f32 and out.dtype is not _f32():
+        raise ValueError(f"out: elements of {out.dtype}, expected {q.torch_dtype} or float32")
     m, ldo = _rows(out, q.n_out, out.dtype, "out")
     if m != n:
         raise ValueError(f"out: {m} rows, x has {n}")
-    _check(_lib.rr_matvec(q._ref, q._p, x.data_ptr(), ldx, n, out.data_ptr(), ldo, f32,
-                          _stream(stream)), "rr_matvec")
+    st = _lib.rr_matvec(q._ref, q._p, x.data_ptr(), ldx, n, out.data_ptr(), ldo, f32,
+                        _stream_of(x, stream))
+    if st != RR_OK:
+        _check(st, "rr_matvec")
+
+
+def _f32():
+    import torch
+    return torch.float32
 
 
 class MoeLayer:
@@ -260,8 +282,10 @@ def rr_moe(layer: MoeLayer, x, out, workspace: MoeWorkspace, ids=None, weights=N
     if weights is not None:
         pw = _choice(weights, n, layer.top_k, "weights", 1)
     r, w13, w2 = layer._p
-    _check(_lib.rr_moe(layer._ref, r, w13, w2, x.data_ptr(), ldx, n, out.data_ptr(), ldo, pi, pw,
-                       workspace._p, workspace.nbytes, _stream(stream)), "rr_moe")
+    st = _lib.rr_moe(layer._ref, r, w13, w2, x.data_ptr(), ldx, n, out.data_ptr(), ldo, pi, pw,
+                     workspace._p, workspace.nbytes, _stream_of(x, stream))
+    if st != RR_OK:
+        _check(st, "rr_moe")
 
 
 def _choice(t, n: int, k: int, what: str, floating: int) -> int:
