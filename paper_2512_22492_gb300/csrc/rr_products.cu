@@ -321,6 +321,31 @@ __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
 __device__ __forceinline__ void copy_async_cut(uint32_t to, const void* from, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
+// Eight adjacent 16-bit elements from p on, wherever p lies, of a buffer [begin, end);
+// zeros from `left` elements on.  Two aligned 16-byte loads where both are within the
+// buffer.
+__device__ __forceinline__ uint4 load_any(const uint16_t* p, int left, const uint16_t* begin, const uint16_t* end) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p), shift = at & 15;
+    const uint4* const from = reinterpret_cast<const uint4*>(at - shift);
+    if (left >= 8 && reinterpret_cast<const uint16_t*>(from) >= begin && reinterpret_cast<const uint16_t*>(from + 2) <= end) {
+        const uint4 u = from[0], v = from[1];
+        uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 6; ++i)
+            if (shift & 8) w[i] = w[i + 2];
+#pragma unroll
+        for (int i = 0; i < 5; ++i)
+            if (shift & 4) w[i] = w[i + 1];
+        const uint32_t pick = shift & 2 ? 0x5432 : 0x3210;
+        return make_uint4(__byte_perm(w[0], w[1], pick), __byte_perm(w[1], w[2], pick), __byte_perm(w[2], w[3], pick),
+                          __byte_perm(w[3], w[4], pick));
+    }
+    uint32_t w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = k < left ? p[k] : 0u;
+    return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+}
+
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -482,11 +507,12 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
                                left >= 8 ? 16 : left > 0 ? 2 * int(left) : 0);
             }
     } else {
-        for (int n = 0; n < a.tokens; ++n)
-#pragma unroll 8
-            for (int c = threadIdx.x; c < cols; c += kProdThreads)
-                *reinterpret_cast<uint16_t*>(xs + n * a.pitch + 2 * c) =
-                    c0 + c < a.m.cols ? a.x[n * a.ldx + c0 + c] : uint16_t(0);
+        const uint16_t* const end = a.x + (a.tokens - 1) * a.ldx + a.m.cols;
+        for (int c = 8 * threadIdx.x; c < cols; c += 8 * kProdThreads)
+#pragma unroll 4
+            for (int n = 0; n < a.tokens; ++n)
+                *reinterpret_cast<uint4*>(xs + n * a.pitch + 2 * c) =
+                    load_any(a.x + n * a.ldx + c0 + c, int(max(int64_t(0), min(int64_t(8), a.m.cols - c0 - c))), a.x, end);
     }
     copy_commit();
     // A lane of an absent token reads the last one's row; its sums go nowhere.
@@ -797,17 +823,16 @@ __device__ __forceinline__ void logit_item(const MoeArgs& a, int e0, int t0, flo
             mma<T>(sum, u.z, v.z, u.w, v.w, w.z, w.w);
         }
     } else {
+        const uint16_t* const x_end = a.x + (a.tokens - 1) * a.ldx + a.hidden;
+        const uint16_t* const r_end = a.router + int64_t(a.n_experts) * a.hidden;
+#pragma unroll 2
         for (int k = 32 * warp; k < a.hidden; k += 32 * kWarps) {
-            uint32_t w[4], u[4], v[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const bool in0 = k + 8 * t + 2 * q < a.hidden, in1 = k + 8 * t + 2 * q + 1 < a.hidden;
-                w[q] = (in0 ? r[k + 2 * q] : 0u) | (in1 ? uint32_t(r[k + 2 * q + 1]) << 16 : 0u);
-                u[q] = (in0 ? lo[k + 2 * q] : 0u) | (in1 ? uint32_t(lo[k + 2 * q + 1]) << 16 : 0u);
-                v[q] = (in0 ? hi[k + 2 * q] : 0u) | (in1 ? uint32_t(hi[k + 2 * q + 1]) << 16 : 0u);
-            }
-            mma<T>(sum, u[0], v[0], u[1], v[1], w[0], w[1]);
-            mma<T>(sum, u[2], v[2], u[3], v[3], w[2], w[3]);
+            const int left = a.hidden - k - 8 * t;
+            const uint4 w = load_any(r + k, left, a.router, r_end), u = load_any(lo + k, left, a.x, x_end);
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (t0 + 8 < a.tokens) v = load_any(hi + k, left, a.x, x_end);
+            mma<T>(sum, u.x, v.x, u.y, v.y, w.x, w.y);
+            mma<T>(sum, u.z, v.z, u.w, v.w, w.z, w.w);
         }
     }
     red[threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
@@ -1037,14 +1062,13 @@ __device__ __forceinline__ void stage_tokens(const MoeArgs& a, const MoeTables& 
             }
         }
     } else {
-        // A warp a row, or part of one.
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, split = count >= kWarps ? 1 : kWarps / count;
-        for (int i = warp / split; i < count; i += kWarps / split) {
+        const uint16_t* const end = a.x + (a.tokens - 1) * a.ldx + a.hidden;
+        const int chunks = cols / 8;
+#pragma unroll 4
+        for (int k = threadIdx.x; k < count * chunks; k += kProdThreads) {
+            const int i = k / chunks, c = 8 * (k % chunks);
             const uint16_t* const row = a.x + (a.all_x ? i : tab.token[first + i]) * a.ldx;
-            char* const dst = to + i * a.x_pitch;
-#pragma unroll 16
-            for (int c = 32 * (warp % split) + lane; c < cols; c += 32 * split)
-                *reinterpret_cast<uint16_t*>(dst + 2 * c) = c < a.hidden ? row[c] : uint16_t(0);
+            *reinterpret_cast<uint4*>(to + i * a.x_pitch + 2 * c) = load_any(row + c, a.hidden - c, a.x, end);
         }
     }
     copy_commit();
@@ -1930,10 +1954,10 @@ int clusters_at_once(K* kernel, int dev, int cluster) {
     return n;
 }
 
-// How a product is shared out, for a.tokens tokens; false if these do not fit.  The
-// fewest blocks of a cluster for which its share of the tokens fits a block's shared
-// memory, with 6 blocks of weights in flight a warp where there is room, else 4;
-// more, where strips are too few to go round and a block's share is long.
+// How a product is shared out, for a.tokens tokens; false if these do not fit.  A
+// cluster's blocks share the columns where a block's shared memory would not hold the
+// tokens, or where strips are too few to go round.  6 blocks of weights in flight a
+// warp, or 4 where that makes room.
 bool matvec_shape(MatvecArgs* a, int group, int dev, MatvecShape* shape) {
     const int tiles = a->tokens > 8 ? 2 : 1, part = 512 * tiles;
     int64_t best = INT64_MAX;
@@ -1949,8 +1973,13 @@ bool matvec_shape(MatvecArgs* a, int group, int dev, MatvecShape* shape) {
             const int64_t batch = cluster == 1 ? strips : std::min(strips, room / part);
             if (room < 0 || batch < 1) continue;
             const int64_t joins = cluster == 1 ? 0 : (strips + batch - 1) / batch;
-            // In blocks of weights of the busiest warp.
-            const int64_t cost = (strips * blocks + kWarps - 1) / kWarps + 4 * joins + (stages == 4 ? 1 : 0);
+            // In blocks of weights of the busiest warp: those, the copy of the tokens (32 KB
+            // of them cost about as much as a block, 8 KB where they are not aligned), a
+            // cluster's joins.  (720 x 5114, paired, 14 unaligned tokens: 14.1 us with no
+            // clusters, 10.7 so; 24576 x 4096, paired, 16 aligned ones: 19.0 us so, 21.0 with
+            // clusters of 2.)
+            const int64_t cost = (strips * blocks + kWarps - 1) / kWarps + pitch * a->tokens / (a->vec ? 32768 : 8192) +
+                                 4 * joins + (stages == 4 ? 1 : 0);
             if (cost >= best) continue;
             best = cost;
             a->pitch = int32_t(pitch);
