@@ -430,6 +430,77 @@ def test_moe_streams_and_graph():
         assert torch.equal(got, want[1])
 
 
+def test_moe_a_wait_that_runs_out():
+    """A count that can never be reached makes the blocks' wait run out (about two
+    seconds): the call ends, rr_moe_check says so, and after it the workspace works
+    again; until then calls on it do nothing."""
+    gen = torch.Generator().manual_seed(71)
+    layer, router, v13, v2 = layer_of(gen, 16, 512, 512, "bf16", 0, 4)
+    x = P.grid_tokens(gen, 20, 512, "bf16")
+    ws = rr.MoeWorkspace(layer, 20)
+    want, _, _ = run_moe(layer, x, ws)
+    # The count wraps round to below the number of blocks.
+    ws.data[4:8] = torch.tensor([0xCD, 0xFF, 0xFF, 0xFF], dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(want)
+    rr.rr_moe(layer, x.cuda(), out, ws)
+    with pytest.raises(rr.RRError, match="RR_ECUDA"):
+        rr.rr_moe_check(layer, ws)
+    got, _, _ = run_moe(layer, x, ws)
+    assert torch.equal(got, want)
+    ws.data[0] = 1                 # an earlier call's mark
+    out.fill_(5.0)
+    rr.rr_moe(layer, x.cuda(), out, ws)
+    with pytest.raises(rr.RRError, match="RR_ECUDA"):
+        rr.rr_moe_check(layer, ws)
+    assert bool((out == 5).all())
+    got, _, _ = run_moe(layer, x, ws)
+    assert torch.equal(got, want)
+
+
+def test_offsets_past_32_bits():
+    """Matrices of more than 2^31 elements: their last rows, and a stack's last expert."""
+    gen = torch.Generator().manual_seed(73)
+    rows, cols = 70000, 32768
+    w = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    tail = weights(gen, (48, cols), "bf16").cuda()
+    w[-48:] = tail
+    q = rr.Quantized(rows, cols, 128)
+    rr.rr_quantize(q, w)
+    small = rr.Quantized(48, cols, 128)
+    rr.rr_quantize(small, tail)
+    assert torch.equal(q.data[-small.nbytes:], small.data)
+    x = torch.randn(3, cols, generator=gen).bfloat16().cuda()
+    out, few = torch.empty(3, rows, device="cuda"), torch.empty(3, 48, device="cuda")
+    rr.rr_matvec(q, x, out)
+    rr.rr_matvec(small, x, few)
+    vals = torch.empty(48, cols, device="cuda")
+    rr.rr_dequantize(small, vals)
+    want, tol = P.matvec(vals.cpu().double(), x.cpu(), False, "f32")
+    P.check(few, want, tol)
+    P.check(out[:, -48:], want, tol)
+    assert bool((out[:, :-48] == 0).all())
+    w.fill_(7.0)
+    rr.rr_dequantize(q, w)
+    back = torch.empty_like(tail)
+    rr.rr_dequantize(small, back)
+    assert torch.equal(w[-48:], back) and bool((w[:-48] == 0).all())
+    del w, q, out
+    experts, hidden, inter = 64, 8192, 2304
+    router = P.grid_router(gen, experts, hidden, "bf16")
+    router[experts - 1] = 0.25
+    w13 = torch.zeros(experts, 2 * inter, hidden, dtype=torch.bfloat16, device="cuda")
+    w2 = torch.zeros(experts, hidden, inter, dtype=torch.bfloat16, device="cuda")
+    one13, one2 = weights(gen, (2 * inter, hidden), "bf16", 0.02), weights(gen, (hidden, inter), "bf16", 0.02)
+    w13[-1], w2[-1] = one13.cuda(), one2.cuda()
+    x = P.grid_tokens(gen, 2, hidden, "bf16").abs()
+    layer = rr.MoeLayer(router.cuda(), w13, w2, 1)
+    out, ids, c = run_moe(layer, x)
+    assert bool((ids == experts - 1).all())
+    zeros = torch.zeros(2, 1, dtype=torch.int64)
+    P.check(out, *P.moe(x, zeros, torch.ones(2, 1, dtype=torch.float64), one13.unsqueeze(0).double(),
+                        one2.unsqueeze(0).double(), 0, "bf16"))
+
+
 # ---------------------------------------------------------------------------
 # Refusals
 # ---------------------------------------------------------------------------
