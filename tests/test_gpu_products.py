@@ -352,6 +352,30 @@ def test_moe_not_finite():
     assert ids[2].tolist() == [0, 1, 2]
 
 
+@pytest.mark.parametrize("group", [0, 32])
+@pytest.mark.parametrize("tokens", [1, 3, 8, 20])
+def test_moe_bad_expert(tokens, group):
+    """An expert whose weights are not finite is felt by the tokens that chose it alone."""
+    gen = torch.Generator().manual_seed(51)
+    router = P.grid_router(gen, 8, 96, "bf16")
+    w13, w2 = weights(gen, (8, 96, 96), "bf16"), weights(gen, (8, 96, 48), "bf16")
+    x = P.grid_tokens(gen, tokens, 96, "bf16")
+    ids, _ = P.route(x, router, 2, True)
+    bad = int(ids[0, 0])
+    outs = []
+    for spoil in (False, True):
+        if spoil:
+            w2[bad] = math.nan
+            w13[bad, 5] = math.inf
+        a, b = (quantized(w13, group, "bf16", True)[0], quantized(w2, group, "bf16")[0]) if group \
+            else (w13.cuda(), w2.cuda())
+        outs.append(run_moe(rr.MoeLayer(router.cuda(), a, b, 2), x)[0].cpu())
+    hit = (ids == bad).any(1)
+    assert bool(torch.isnan(outs[1][hit]).all()) and bool(hit[0])
+    assert torch.equal(outs[0][~hit], outs[1][~hit])
+    assert tokens == 1 or bool((~hit).any())
+
+
 def test_moe_large_hidden_values_f16():
     """silu(gate) * up past float16's range, and far below it, is held in 32 bits."""
     gen = torch.Generator().manual_seed(53)
