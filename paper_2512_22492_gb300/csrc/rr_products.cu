@@ -1275,35 +1275,37 @@ __device__ __forceinline__ void moe_phase(const MoeArgs& a, const MoePhase* ph, 
 }
 
 // The second phase for few tokens, whose every h fits a block's shared memory: an
-// item is a strip of the output over all chosen experts, a warp takes every 16th
-// of its blocks of weights, and the block joins the warps' sums.  No pair's part
-// goes through memory, and no barrier follows.
+// item is a strip of the output over all chosen experts, whose blocks of weights the
+// warps share evenly, and the block joins the warps' sums.  No pair's part goes
+// through memory, and no barrier follows.
 template <int W>
 struct FoldFeed {
     Weights<W> w;
-    int strip, end, pass, b;
+    int strip, end, pass, b, left;
+    __device__ __forceinline__ void start(const MoePhase& p, const MoeTables& tab, int passes, int warp, int lane) {
+        const int total = passes * p.blocks, lo = share_from(warp, total);
+        left = share_from(warp + 1, total) - lo;
+        if (left == 0) strip = end;
+        if (strip >= end) return;
+        pass = lo / p.blocks;
+        b = lo % p.blocks;
+        w.seek(p.base, tab.pass_expert[pass], p.m, strip, b, lane);
+    }
     __device__ __forceinline__ void load(const MoePhase& p, const MoeTables& tab, int passes, uint32_t to, int warp,
                                          int lane) {
         if (strip < end) {
-            w.seek(p.base, tab.pass_expert[pass], p.m, strip, b, lane);
             w.load(to, p.base, lane);
-            next(p, passes, warp);
+            if (--left == 0) {
+                ++strip;
+                start(p, tab, passes, warp, lane);
+            } else if (++b < p.blocks) {
+                w.skip(1);
+            } else {
+                b = 0;
+                w.seek(p.base, tab.pass_expert[++pass], p.m, strip, 0, lane);
+            }
         }
         copy_commit();
-    }
-    __device__ __forceinline__ void next(const MoePhase& p, int passes, int warp) {
-        b += kWarps;
-        wrap(p);
-        if (pass >= passes) ++strip, first(p, passes, warp);
-    }
-    __device__ __forceinline__ void first(const MoePhase& p, int passes, int warp) {
-        pass = 0;
-        b = warp;
-        wrap(p);
-        if (pass >= passes) strip = end;     // fewer blocks than warps: none here
-    }
-    __device__ __forceinline__ void wrap(const MoePhase& p) {
-        while (b >= p.blocks) b -= p.blocks, ++pass;
     }
 };
 
@@ -1329,7 +1331,7 @@ __device__ __forceinline__ void stage_fold(const MoeArgs& a, MoeTables& tab, cha
     const int chunks = cols / 4, apart = a.fold * a.h_pitch;
 #pragma unroll 4
     for (int k = threadIdx.x; k < (pairs + 1) * chunks; k += kProdThreads) {
-        const int i = k / chunks, c = 4 * (k % chunks);
+        const int i = k / chunks, c = 4 * (k - i * chunks);
         float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         float up = 0.0f;
         if (i < pairs) {
@@ -1360,13 +1362,12 @@ __device__ __forceinline__ void moe_fold(const MoeArgs& a, const MoePhase& p, Mo
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int apart = a.fold * a.h_pitch;
     const uint32_t fifo_at = smem_at(fifo);
+    const int total = passes * p.blocks, lo = share_from(warp, total), hi = share_from(warp + 1, total);
     for (int strip = p.f0; strip < p.f0 + p.n; ++strip) {
         float sum[4] = {};
-        int b = warp, pass = 0;
-        for (;;) {
-            while (b >= p.blocks) b -= p.blocks, ++pass;
-            if (pass >= passes) break;
-            const int e = tab.pass_expert[pass];
+        int pass = lo / p.blocks, b = lo % p.blocks;
+        for (int at = lo; at < hi; ++pass, b = 0) {
+            const int e = tab.pass_expert[pass], stop = min(p.blocks, b + hi - at);
             const uint32_t mask = tab.mask[0][e];
             const int row = mask >> g & 1 ? tab.first[e] + __popc(mask & ((1u << g) - 1)) : a.fold - 1;
             const char* const x[1] = {region + row * a.h_pitch + 16 * t};
@@ -1377,19 +1378,21 @@ __device__ __forceinline__ void moe_fold(const MoeArgs& a, const MoePhase& p, Mo
                 shift_lo = int(reinterpret_cast<uintptr_t>(w.lo) & 15);
                 shift_hi = int(reinterpret_cast<uintptr_t>(w.hi) & 15);
             }
-            copy_wait<kStages - 2>();
-            __syncwarp();
-            feed.load(p, tab, passes, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
             float part[1][4] = {};
-            moe_block<T, W, 1, 2>(part, fifo + slot * kBytes, x, apart, b * (2 * Weights<W>::kCols), shift_lo, shift_hi,
-                                  lane);
+            at += stop - b;
+            for (; b < stop; ++b) {
+                copy_wait<kStages - 2>();
+                __syncwarp();
+                feed.load(p, tab, passes, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
+                moe_block<T, W, 1, 2>(part, fifo + slot * kBytes, x, apart, b * (2 * Weights<W>::kCols), shift_lo,
+                                      shift_hi, lane);
+                slot = slot + 1 == kStages ? 0 : slot + 1;
+            }
             // Only of tokens that chose the expert: zeros times its weights are not zero
             // where these are infinite or NaN.
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (mask >> (2 * t + (k & 1)) & 1) sum[k] += part[0][k];
-            slot = slot + 1 == kStages ? 0 : slot + 1;
-            b += kWarps;
         }
         red[threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
         __syncthreads();
@@ -1587,7 +1590,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
         FoldFeed<W> fold;
         fold.strip = ph[1].f0;
         fold.end = ph[1].f0 + ph[1].n;
-        fold.first(ph[1], passes, warp);
+        fold.start(ph[1], tab, passes, warp, lane);
         for (int i = 0, to = slot; i < Weights<W>::kStages - 1; ++i) {
             fold.load(ph[1], tab, passes, smem_at(fifo) + to * Weights<W>::kBytes, warp, lane);
             to = to + 1 == Weights<W>::kStages ? 0 : to + 1;
