@@ -625,8 +625,11 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
 constexpr int kMaxExperts = 512, kMaxTopK = 16, kMaxHidden = 32768, kMaxInter = 16384;
 constexpr int kMaxPairs = RR_MOE_MAX_TOKENS * kMaxTopK;
 constexpr int kJoinBytes = 2 * kWarps * 2 * 512;   // shared memory of the warps' parts of strips
-constexpr int kClusterBlocks = 8;       // of a layer small enough for one cluster
-constexpr int64_t kClusterBytes = 1 << 20;
+// A layer of little work runs in one cluster, whose barriers and whose launch cost
+// less than a grid's, although few SMs then read all of its weights.  A call with 0.15
+// and 2.4 MB of them: 10.4 and 17.9 us on 8 blocks, 10.7 and 13.8 us on 16, 14.6 us both
+// on a grid; with 4.7 MB 18.1 us on 16 and 14.6.
+constexpr int64_t kCluster8Bytes = 256 << 10, kCluster16Bytes = 5 << 19;
 constexpr int kSmem = 227 * 1024;
 
 // The workspace's control block.
@@ -1443,7 +1446,7 @@ __device__ __forceinline__ void finish(const MoeArgs& a) {
 constexpr int kPrefetch = 8;       // strips of the second phase that a block asks for ahead
 
 // The whole layer in one cooperative launch, one block per SM (a small layer: in one
-// cluster of 8):
+// cluster):
 //   logits, a block per 8 experts and 16 tokens            | barrier
 //   softmax and choice (over 16 tokens: shared out | barrier), every expert's tokens
 //   gate and up of every chosen expert, silu               | barrier
@@ -1805,21 +1808,25 @@ rr_status launch_moe(MoeArgs a, int dev, cudaStream_t stream) {
     const int64_t rows = int64_t(a.tokens) * std::min(a.top_k, a.n_local) + 1;
     a.fold = a.tokens <= 8 && a.cap == a.tokens && rows <= a.h_rows ? int32_t(rows) : 0;
     const int smem = kFixed - 1024 + room;
-    // A layer of little work runs in one cluster, whose barriers and whose launch
-    // cost less than a grid's, although 8 SMs then read all of its weights.
     const int64_t bytes = std::min<int64_t>(int64_t(a.tokens) * a.top_k, a.n_local) * (a.m13_bytes + a.m2_bytes);
+    a.one = bytes <= kCluster16Bytes;
     static std::atomic<uint32_t> ready{0};
     RR_CUDA(allow_smem(rr_moe_kernel<T, W>, kSmem - 1024, dev, &ready));
-    a.one = bytes <= kClusterBytes;
     if (a.one) {
+        const unsigned blocks = bytes <= kCluster8Bytes ? 8 : 16;
+        static std::atomic<uint32_t> large{0};     // more than 8 blocks are asked for by name
+        if (blocks > 8 && !(large.load(std::memory_order_relaxed) >> dev & 1)) {
+            RR_CUDA(cudaFuncSetAttribute(rr_moe_kernel<T, W>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+            large.fetch_or(1u << dev, std::memory_order_relaxed);
+        }
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[0].val.programmaticStreamSerializationAllowed = 1;
         attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = kClusterBlocks;
+        attr[1].val.clusterDim.x = blocks;
         attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(kClusterBlocks);
+        cfg.gridDim = dim3(blocks);
         cfg.blockDim = dim3(kProdThreads);
         cfg.dynamicSmemBytes = size_t(smem);
         cfg.stream = stream;
