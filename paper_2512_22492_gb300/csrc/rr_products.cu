@@ -508,11 +508,13 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
             }
     } else {
         const uint16_t* const end = a.x + (a.tokens - 1) * a.ldx + a.m.cols;
-        for (int c = 8 * threadIdx.x; c < cols; c += 8 * kProdThreads)
+        const int chunks = cols / 8;
 #pragma unroll 4
-            for (int n = 0; n < a.tokens; ++n)
-                *reinterpret_cast<uint4*>(xs + n * a.pitch + 2 * c) =
-                    load_any(a.x + n * a.ldx + c0 + c, int(max(int64_t(0), min(int64_t(8), a.m.cols - c0 - c))), a.x, end);
+        for (int k = threadIdx.x; k < a.tokens * chunks; k += kProdThreads) {
+            const int n = k / chunks, c = 8 * (k - n * chunks);
+            *reinterpret_cast<uint4*>(xs + n * a.pitch + 2 * c) =
+                load_any(a.x + n * a.ldx + c0 + c, int(max(int64_t(0), min(int64_t(8), a.m.cols - c0 - c))), a.x, end);
+        }
     }
     copy_commit();
     // A lane of an absent token reads the last one's row; its sums go nowhere.
@@ -1995,11 +1997,11 @@ bool matvec_shape(MatvecArgs* a, int group, int dev, MatvecShape* shape) {
             if (room < 0 || batch < 1) continue;
             const int64_t joins = cluster == 1 ? 0 : (strips + batch - 1) / batch;
             // In blocks of weights of the busiest warp: those, the copy of the tokens (32 KB
-            // of them cost about as much as a block, 8 KB where they are not aligned), a
-            // cluster's joins.  (720 x 5114, paired, 14 unaligned tokens: 14.1 us with no
-            // clusters, 10.7 so; 24576 x 4096, paired, 16 aligned ones: 19.0 us so, 21.0 with
-            // clusters of 2.)
-            const int64_t cost = (strips * blocks + kWarps - 1) / kWarps + pitch * a->tokens / (a->vec ? 32768 : 8192) +
+            // of them cost about as much as a block, 12 KB where they are not aligned), a
+            // cluster's joins.  (24576 x 4096, paired, 16 aligned tokens: 19.0 us so, in one
+            // block's shared memory each, and 21.0 in clusters of 2; 30001 x 4097, 9 unaligned
+            // ones: 22.4 us so, 25.2 where 4 KB count as a block.)
+            const int64_t cost = (strips * blocks + kWarps - 1) / kWarps + pitch * a->tokens / (a->vec ? 32768 : 12288) +
                                  4 * joins + (stages == 4 ? 1 : 0);
             if (cost >= best) continue;
             best = cost;
