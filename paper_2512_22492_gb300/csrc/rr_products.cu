@@ -71,6 +71,31 @@ __device__ __forceinline__ int code(uint32_t word, int i) {
     return int((word >> (4 * (i / 2 + 4 * (i % 2)))) & 15u) - 8;
 }
 
+// Eight adjacent 16-bit elements from p on, wherever p lies, of a buffer [begin, end);
+// zeros from `left` elements on.  Two aligned 16-byte loads where both are within the
+// buffer.
+__device__ __forceinline__ uint4 load_any(const uint16_t* p, int left, const uint16_t* begin, const uint16_t* end) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p), shift = at & 15;
+    const uint4* const from = reinterpret_cast<const uint4*>(at - shift);
+    if (left >= 8 && reinterpret_cast<const uint16_t*>(from) >= begin && reinterpret_cast<const uint16_t*>(from + 2) <= end) {
+        const uint4 u = from[0], v = from[1];
+        uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 6; ++i)
+            if (shift & 8) w[i] = w[i + 2];
+#pragma unroll
+        for (int i = 0; i < 5; ++i)
+            if (shift & 4) w[i] = w[i + 1];
+        const uint32_t pick = shift & 2 ? 0x5432 : 0x3210;
+        return make_uint4(__byte_perm(w[0], w[1], pick), __byte_perm(w[1], w[2], pick), __byte_perm(w[2], w[3], pick),
+                          __byte_perm(w[3], w[4], pick));
+    }
+    uint32_t w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = k < left ? p[k] : 0u;
+    return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+}
+
 // A block of 128 columns by its number within a stack.
 struct Item {
     int64_t mat, strip;
@@ -112,7 +137,8 @@ __device__ __forceinline__ uint32_t code_bits(float v, float inverse) {
 // by HBM: 2 bytes read and about half a byte written per element.
 template <class T, int G, bool VEC>
 __global__ void __launch_bounds__(256) rr_quantize_kernel(const __grid_constant__ Packed m, const uint16_t* w,
-                                                          int64_t ld, char* packed, uint32_t total) {
+                                                          const uint16_t* end, int64_t ld, char* packed,
+                                                          uint32_t total) {
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const uint32_t i = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
     after_previous();
@@ -130,11 +156,8 @@ __global__ void __launch_bounds__(256) rr_quantize_kernel(const __grid_constant_
             uint4 u = make_uint4(0, 0, 0, 0);
             if (VEC && row >= 0 && c + 8 <= m.cols) {
                 u = __ldcs(reinterpret_cast<const uint4*>(src + c));
-            } else if (row >= 0) {
-                uint32_t p[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) p[k] = c + k < m.cols ? src[c + k] : 0;
-                u = make_uint4(p[0] | p[1] << 16, p[2] | p[3] << 16, p[4] | p[5] << 16, p[6] | p[7] << 16);
+            } else if (row >= 0 && c < m.cols) {
+                u = load_any(src + c, int(min(int64_t(8), m.cols - c)), w, end);
             }
             v[half][j][0] = u.x, v[half][j][1] = u.y, v[half][j][2] = u.z, v[half][j][3] = u.w;
         }
@@ -226,6 +249,21 @@ __global__ void __launch_bounds__(256) rr_dequantize_kernel(const __grid_constan
 #pragma unroll
                     for (int k = 0; k < 4; ++k) p[k] = uint32_t(T::round(f[2 * k])) | uint32_t(T::round(f[2 * k + 1])) << 16;
                     *reinterpret_cast<uint4*>(static_cast<uint16_t*>(w) + at) = make_uint4(p[0], p[1], p[2], p[3]);
+                }
+            } else if (!F32 && c + 8 <= m.cols) {
+                // At any alignment: words, and halves at the ends.
+                uint16_t* const p = static_cast<uint16_t*>(w) + at;
+                const bool odd = reinterpret_cast<uintptr_t>(p) & 2;
+                uint16_t e[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) e[k] = T::round(f[k]);
+                uint32_t* const word = reinterpret_cast<uint32_t*>(p + odd);
+                if (odd) p[0] = e[0], p[7] = e[7];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k == 3 && odd) break;
+                    word[k] = odd ? uint32_t(e[2 * k + 1]) | uint32_t(e[(2 * k + 2) & 7]) << 16
+                                  : uint32_t(e[2 * k]) | uint32_t(e[2 * k + 1]) << 16;
                 }
             } else {
 #pragma unroll
@@ -321,31 +359,6 @@ __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
 __device__ __forceinline__ void copy_async_cut(uint32_t to, const void* from, int bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
-// Eight adjacent 16-bit elements from p on, wherever p lies, of a buffer [begin, end);
-// zeros from `left` elements on.  Two aligned 16-byte loads where both are within the
-// buffer.
-__device__ __forceinline__ uint4 load_any(const uint16_t* p, int left, const uint16_t* begin, const uint16_t* end) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p), shift = at & 15;
-    const uint4* const from = reinterpret_cast<const uint4*>(at - shift);
-    if (left >= 8 && reinterpret_cast<const uint16_t*>(from) >= begin && reinterpret_cast<const uint16_t*>(from + 2) <= end) {
-        const uint4 u = from[0], v = from[1];
-        uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 6; ++i)
-            if (shift & 8) w[i] = w[i + 2];
-#pragma unroll
-        for (int i = 0; i < 5; ++i)
-            if (shift & 4) w[i] = w[i + 1];
-        const uint32_t pick = shift & 2 ? 0x5432 : 0x3210;
-        return make_uint4(__byte_perm(w[0], w[1], pick), __byte_perm(w[1], w[2], pick), __byte_perm(w[2], w[3], pick),
-                          __byte_perm(w[3], w[4], pick));
-    }
-    uint32_t w[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = k < left ? p[k] : 0u;
-    return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
-}
-
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -1911,7 +1924,9 @@ extern "C" rr_status rr_quantize(const rr_quant* q, const void* w, int64_t ld, v
         using T = decltype(t);
         constexpr int G = decltype(g)::value ? decltype(g)::value : 128;
         RR_CUDA(launch_after(vec ? rr_quantize_kernel<T, G, true> : rr_quantize_kernel<T, G, false>, grid, 256, stream,
-                             m, static_cast<const uint16_t*>(w), ld, static_cast<char*>(packed), total));
+                             m, static_cast<const uint16_t*>(w),
+                             static_cast<const uint16_t*>(w) + (q->rows * q->count - 1) * ld + q->cols, ld,
+                             static_cast<char*>(packed), total));
         return RR_OK;
     });
 }
