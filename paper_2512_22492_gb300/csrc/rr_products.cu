@@ -229,47 +229,87 @@ __global__ void __launch_bounds__(256) rr_dequantize_kernel(const __grid_constan
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         const int64_t row = m.row(it.strip, 8 * half + g);
-        if (row < 0) continue;
         const uint32_t words[4] = {codes_of[half].x, codes_of[half].y, codes_of[half].z, codes_of[half].w};
+        const int64_t c0 = int64_t(it.b) * kBlock + 8 * t, at0 = (it.mat * m.rows + row) * ld + c0;
+        uint32_t before[4];        // the 8 elements to the left of this lane's
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float s = T::widen(uint16_t(half ? scale[32 * j / G] >> 16 : scale[32 * j / G]));
-            const int64_t c = int64_t(it.b) * kBlock + 32 * j + 8 * t;
-            const int64_t at = (it.mat * m.rows + row) * ld + c;
+            const int64_t c = c0 + 32 * j, at = at0 + 32 * j;
             float f[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) f[k] = s * float(code(words[j], k));
-            if (VEC && c + 8 <= m.cols) {
-                if (F32) {
+            if (F32) {
+                if (row < 0) continue;
+                if (VEC && c + 8 <= m.cols) {
                     float4* const p = reinterpret_cast<float4*>(static_cast<float*>(w) + at);
                     p[0] = make_float4(f[0], f[1], f[2], f[3]);
                     p[1] = make_float4(f[4], f[5], f[6], f[7]);
                 } else {
-                    uint32_t p[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) p[k] = uint32_t(T::round(f[2 * k])) | uint32_t(T::round(f[2 * k + 1])) << 16;
-                    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(w) + at) = make_uint4(p[0], p[1], p[2], p[3]);
+                    for (int k = 0; k < 8; ++k)
+                        if (c + k < m.cols) put<T, true>(w, at + k, f[k]);
                 }
-            } else if (!F32 && c + 8 <= m.cols) {
-                // At any alignment: words, and halves at the ends.
-                uint16_t* const p = static_cast<uint16_t*>(w) + at;
-                const bool odd = reinterpret_cast<uintptr_t>(p) & 2;
-                uint16_t e[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) e[k] = T::round(f[k]);
-                uint32_t* const word = reinterpret_cast<uint32_t*>(p + odd);
-                if (odd) p[0] = e[0], p[7] = e[7];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (k == 3 && odd) break;
-                    word[k] = odd ? uint32_t(e[2 * k + 1]) | uint32_t(e[(2 * k + 2) & 7]) << 16
-                                  : uint32_t(e[2 * k]) | uint32_t(e[2 * k + 1]) << 16;
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (c + k < m.cols) put<T, F32>(w, at + k, f[k]);
+                continue;
             }
+            uint32_t own[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) own[k] = uint32_t(T::round(f[2 * k])) | uint32_t(T::round(f[2 * k + 1])) << 16;
+            uint16_t* const p = static_cast<uint16_t*>(w) + at;
+            if (VEC) {
+                if (row < 0) continue;
+                if (c + 8 <= m.cols) {
+                    *reinterpret_cast<uint4*>(p) = make_uint4(own[0], own[1], own[2], own[3]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (c + k < m.cols) p[k] = uint16_t(own[k / 2] >> (16 * (k % 2)));
+                }
+                continue;
+            }
+            // At any alignment: the 16 aligned bytes that begin with the end of the lane to
+            // the left (of lane 0: lane 3's, 32 columns back) and end with this lane's first
+            // elements; those that no lane completes, one by one.
+            uint32_t left[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t l = __shfl_sync(~0u, own[k], (lane - 1) & 31), far = __shfl_sync(~0u, j ? before[k] : 0, lane | 3);
+                left[k] = t ? l : far;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) before[k] = own[k];
+            if (row < 0) continue;
+            const int over = int(reinterpret_cast<uintptr_t>(p) & 15) / 2;      // elements past an aligned address
+            const bool first = j == 0 && t == 0, whole = c + 8 <= m.cols;
+            if (whole && over == 0) {
+                *reinterpret_cast<uint4*>(p) = make_uint4(own[0], own[1], own[2], own[3]);
+            } else if (whole && !first) {
+                uint32_t v[8] = {left[0], left[1], left[2], left[3], own[0], own[1], own[2], own[3]};
+                const int from = 2 * (8 - over);      // the byte of v that goes to the aligned address
+#pragma unroll
+                for (int i = 0; i < 6; ++i)
+                    if (from & 8) v[i] = v[i + 2];
+#pragma unroll
+                for (int i = 0; i < 5; ++i)
+                    if (from & 4) v[i] = v[i + 1];
+                const uint32_t pick = from & 2 ? 0x5432 : 0x3210;
+                *reinterpret_cast<uint4*>(p - over) =
+                    make_uint4(__byte_perm(v[0], v[1], pick), __byte_perm(v[1], v[2], pick), __byte_perm(v[2], v[3], pick),
+                               __byte_perm(v[3], v[4], pick));
+            }
+            // This lane's own elements from `lo` on: none where the lane to the right
+            // completes them, the last `over` where there is none, all of them where this one
+            // wrote nothing.
+            const bool ended = !(j == 3 && t == 3) && c + 16 <= m.cols;      // the next lane's are whole
+            int lo = 8, hi = 8;
+            if (over || !whole) {
+                if (!whole) lo = 0, hi = int(max(int64_t(0), min(int64_t(8), m.cols - c)));
+                else if (first) lo = 0, hi = ended ? 8 - over : 8;
+                else if (!ended) lo = 8 - over;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k >= lo && k < hi) p[k] = uint16_t(own[k / 2] >> (16 * (k % 2)));
         }
     }
 }
