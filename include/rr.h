@@ -572,16 +572,18 @@ rr_status rr_plan_selftest_wait(const rr_plan* plan, cudaStream_t stream);
  * own (Section 7.1).  rr_quantize follows a sync, so that the step reads a
  * quarter of the bytes; rr_matvec and rr_moe are the products.
  *
- * All of these calls are stream-ordered and asynchronous, allocate nothing, may be
- * captured into a CUDA graph (rr_moe_check apart, which blocks), and may run from several threads and streams at once
- * as long as their outputs and workspaces are distinct.  Matrices are in this
- * GPU's device (or managed) memory, 16-byte aligned; tokens, outputs, ids and weights
- * have their elements' alignment.  Row strides (ld...) are in elements and at
- * least the row's length.  Argument errors come back at once (RR_EINVAL; a
+ * All of these calls are stream-ordered and asynchronous, allocate nothing, may
+ * be captured into a CUDA graph (rr_moe_check apart, which blocks), and may run
+ * from several threads and on several streams at once as long as their outputs
+ * and workspaces are distinct.  Matrices are in this GPU's device (or managed)
+ * memory, 16-byte aligned; tokens, outputs, ids and weights have their
+ * elements' alignment.  Row strides (ld...) are in elements and at least the
+ * row's length.  Argument errors come back at once (RR_EINVAL; a
  * shape outside the limits RR_ELAYOUT) and nothing is launched.
  *
- * Arithmetic.  Products of 16-bit values are summed in float32; a result is
- * rounded once to its type.  Infinities and NaN follow the formulas.
+ * Arithmetic.  Products of 16-bit values are summed in float32, in an order that
+ * the shapes alone fix (a call gives the same bits each time); a result is rounded
+ * once to its type.  Infinities and NaN follow the formulas.
  * ------------------------------------------------------------------------- */
 
 /* A stack of matrices in 4 bits with group scales.  Per row, columns
@@ -641,9 +643,9 @@ rr_status rr_matvec(const rr_quant* q, const void* packed, const void* x, int64_
  * p = softmax(l), a token takes the top_k experts of largest l (ties: the
  * lowest index; NaN counts as the largest), with weights c = p, or, with
  * norm_topk, p / (sum of the chosen p).  Its output is the sum over the chosen
- * experts e in first_expert .. first_expert + n_local - 1, in the order of
- * their rank, of c W2_e (silu(W1_e x) * (W3_e x)); zero if there is none.  A rank of
- * an expert-parallel or tensor-parallel rollout thus gets its part of the sum.
+ * experts e in first_expert .. first_expert + n_local - 1 of
+ * c W2_e (silu(W1_e x) * (W3_e x)), zero if there is none: a rank of an expert-
+ * or tensor-parallel rollout gets its part of the layer's sum.
  *   router: [n_experts, hidden] 16-bit elements.
  *   w13, w2: with group 0, 16-bit stacks as rr_unpack writes them:
  *     w13 [n_local, 2 inter, hidden], each expert [gate; up], and

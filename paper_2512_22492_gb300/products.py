@@ -76,20 +76,20 @@ def _rows(x, cols: int, dtype, what: str):
     return n, ld
 
 
+_raw_stream = None
+
+
 def _stream_of(x, stream) -> int:
     """The stream's handle; None: the current one of x's device."""
-    if stream is None and _raw_stream is not None and x.is_cuda:
-        return _raw_stream(x.get_device())
-    return _stream(stream)
-
-
-def _find_raw_stream():
-    # The call that torch's own code generators use; it is not public.
-    import torch
-    return getattr(torch._C, "_cuda_getCurrentRawStream", None)
-
-
-_raw_stream = _find_raw_stream()
+    global _raw_stream
+    if stream is not None or not x.is_cuda:
+        return _stream(stream)
+    if _raw_stream is None:
+        # The call that torch's own code generators use; it is not public.
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda device: int(torch.cuda.current_stream(device).cuda_stream))
+    return _raw_stream(x.get_device())
 
 
 class Quantized:

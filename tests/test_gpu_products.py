@@ -115,6 +115,28 @@ def test_quantize_strides_and_stacks(offset, extra):
             and bool((out[-8:] == 9).all())
 
 
+@pytest.mark.parametrize("cols", [1, 2, 7, 8, 9, 121, 127, 128, 129, 135, 136, 137, 250, 255, 257])
+@pytest.mark.parametrize("offset", [0, 1, 2, 3, 4, 5, 6, 7])
+def test_quantize_every_alignment(cols, offset):
+    """Rows that begin at every 2-byte offset from 16 bytes, of lengths around a
+    block's and a vector's; NaN beside the matrix is not read into it."""
+    gen = torch.Generator().manual_seed(cols)
+    rows, ld = 19, cols + offset % 3
+    w = weights(gen, (rows, cols), "f16")
+    store = torch.full((offset + rows * ld + 9,), math.nan, dtype=torch.float16, device="cuda")
+    view = store[offset:offset + rows * ld].view(rows, ld)[:, :cols]
+    view.copy_(w)
+    q = rr.Quantized(rows, cols, 32, "f16")
+    rr.rr_quantize(q, view)
+    codes, scales = P.quantize(w, 32)
+    assert np.array_equal(q.data.cpu().numpy(), P.pack(codes, scales, 32, False))
+    out = torch.full_like(store, 9.0)
+    to = out[offset:offset + rows * ld].view(rows, ld)
+    rr.rr_dequantize(q, to[:, :cols])
+    assert torch.equal(to[:, :cols].cpu(), P.values(codes, scales, 32).half())
+    assert bool((to[:, cols:] == 9).all()) and bool((out[:offset] == 9).all()) and bool((out[-9:] == 9).all())
+
+
 def test_quantize_flat_destination_tensor():
     """A sync's destination tensors are flat."""
     w = weights(torch.Generator().manual_seed(8), (48, 160), "f16")
