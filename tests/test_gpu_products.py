@@ -193,6 +193,21 @@ def test_matvec_strides(offset, extra):
         and bool((out[-8:] == 3).all())
 
 
+@pytest.mark.parametrize("rows,cols,tokens,pair", [(40, 1 << 18, 3, False), (34, (1 << 18) - 5, 2, True),
+                                                   (50, 100000, 16, False), (3000, 30000, 13, True)])
+def test_matvec_longest_rows(rows, cols, tokens, pair):
+    """Rows whose tokens fit no block's shared memory, in clusters and in several launches."""
+    gen = torch.Generator().manual_seed(rows)
+    q = rr.Quantized(rows, cols, 128, "bf16", pair)
+    rr.rr_quantize(q, weights(gen, (rows, cols), "bf16", 0.01).cuda())
+    vals = torch.empty(rows, cols, device="cuda")
+    rr.rr_dequantize(q, vals)
+    x = torch.randn(tokens, cols, generator=gen).bfloat16()
+    out = torch.empty(tokens, q.n_out, device="cuda")
+    rr.rr_matvec(q, x.cuda(), out)
+    P.check(out, *P.matvec(vals.cpu().double(), x, pair, "f32"))
+
+
 def test_matvec_one_dimensional_and_none():
     gen = torch.Generator().manual_seed(2)
     q, vals = quantized(weights(gen, (40, 96), "f16"), 32, "f16")
@@ -322,6 +337,23 @@ def test_moe(experts, hidden, inter, tokens, top_k, first, local, group, kind, n
     assert torch.equal(ids.cpu().long(), want_ids)
     P.check(c, want_c, 2.0 ** -18 * want_c)
     P.check(out, *P.moe(x, want_ids, want_c, v13, v2, first, kind))
+
+
+@pytest.mark.parametrize("hidden,inter,tokens,group,kind", [
+    (32768, 24, 5, 0, "bf16"), (32761, 16, 9, 0, "f16"), (32768, 40, 20, 32, "bf16"),
+    (64, 16384, 6, 0, "f16"), (33, 16381, 18, 0, "bf16"), (64, 16384, 3, 64, "bf16")])
+def test_moe_longest_rows(hidden, inter, tokens, group, kind):
+    """The longest rows that are accepted: a block's shared memory holds one token's."""
+    gen = torch.Generator().manual_seed(hidden + inter)
+    layer, router, v13, v2 = layer_of(gen, 3, hidden, inter, kind, group, 2)
+    x = P.grid_tokens(gen, tokens, hidden, kind)
+    out, ids, c = run_moe(layer, x)
+    want_ids, want_c = P.route(x, router, 2, True)
+    assert torch.equal(ids.cpu().long(), want_ids)
+    P.check(out, *P.moe(x, want_ids, want_c, v13, v2, 0, kind))
+    with pytest.raises(rr.RRError, match="RR_ELAYOUT"):
+        rr.MoeLayer(torch.zeros(2, 32769, dtype=torch.bfloat16), torch.zeros(2, 2, 32769, dtype=torch.bfloat16),
+                    torch.zeros(2, 32769, 1, dtype=torch.bfloat16), 1)
 
 
 def test_moe_ties_and_empty_tokens():
