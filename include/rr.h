@@ -583,7 +583,9 @@ rr_status rr_plan_selftest_wait(const rr_plan* plan, cudaStream_t stream);
  *
  * Arithmetic.  Products of 16-bit values are summed in float32, in an order that
  * the shapes alone fix (a call gives the same bits each time); a result is rounded
- * once to its type.  Infinities and NaN follow the formulas.
+ * once to its type.  Between a layer's two products, silu(gate) * up is float32; of
+ * float16 layers the second product takes it to 2^-22 of itself or 2^-39 of the
+ * token's largest, whichever is more.  Infinities and NaN follow the formulas.
  * ------------------------------------------------------------------------- */
 
 /* A stack of matrices in 4 bits with group scales.  Per row, columns

@@ -423,13 +423,43 @@ struct Block {
     }
 };
 
+// How a product's tokens lie in shared memory, 16 bytes per 8 columns and plane:
+//   kWhole: 16-bit elements;
+//   kHalves, kThirds: the sum of two, of three 16-bit parts, a plane each;
+//   kFloats: float32, of each 8 columns the first 4 in one plane, the last 4 in another.
+enum Form { kWhole = 1, kHalves = 2, kThirds = 3, kFloats = 4 };
+__host__ __device__ constexpr int planes_of(Form f) { return f == kFloats ? 2 : int(f); }
+
+// 8 float32 numbers as three bfloat16 parts each, without an error (but under 2^-110,
+// where the last part's bits end): a part is the upper half of what the ones before it
+// leave, 8 of the 24 bits.  inf: there are infinities, whose other parts are zeros.
+struct Parts {
+    uint32_t w[3][4];
+    __device__ __forceinline__ Parts(const char* x, int apart, bool inf) {
+        const uint4 u = *reinterpret_cast<const uint4*>(x), v = *reinterpret_cast<const uint4*>(x + apart);
+        uint32_t f[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[p][k] = __byte_perm(f[2 * k], f[2 * k + 1], 0x7632);
+            if (p == 2) break;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                f[i] = __float_as_uint(__uint_as_float(f[i]) - __uint_as_float(f[i] & 0xFFFF0000u));
+            if (p == 0 && inf)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (!isfinite(__uint_as_float(f[i]))) f[i] = 0;
+        }
+    }
+};
+
 // sum += W x over one block of 128 columns.  x[n]: this lane's 16 bytes of its
-// token's row at the block's first column, in shared memory (with PARTS 2, the
-// element is the sum of that and one `apart` bytes on).  Groups are summed in the
-// matrix unit and scaled in float32.
-template <class T, int G, int NT, int PARTS = 1>
+// token's row at the block's first column, in shared memory; planes are `apart` bytes
+// apart.  Groups are summed in the matrix unit and scaled in float32.
+template <class T, int G, int NT, Form FORM = kWhole>
 __device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* stage, const char* const (&x)[NT],
-                                              int at, int lane, int apart = 0) {
+                                              int at, int lane, int apart = 0, bool inf = false) {
     const int g = lane >> 2;
     const uint4 lo = *reinterpret_cast<const uint4*>(stage + 16 * lane);
     const uint4 hi = *reinterpret_cast<const uint4*>(stage + 512 + 16 * lane);
@@ -446,12 +476,23 @@ __device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* s
         Codes<T>::unpack(ah, wh[j]);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+            if constexpr (FORM == kFloats) {
+                const Parts v(x[n] + at + 64 * j, apart, inf);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) {
+                    if (p == 0 && 32 * j % G == 0) mma_first<T>(part[n], al[0], ah[0], al[1], ah[1], v.w[p][0], v.w[p][1]);
+                    else mma<T>(part[n], al[0], ah[0], al[1], ah[1], v.w[p][0], v.w[p][1]);
+                    mma<T>(part[n], al[2], ah[2], al[3], ah[3], v.w[p][2], v.w[p][3]);
+                }
+                continue;
+            }
             const uint4 v = *reinterpret_cast<const uint4*>(x[n] + at + 64 * j);
             if (32 * j % G == 0) mma_first<T>(part[n], al[0], ah[0], al[1], ah[1], v.x, v.y);
             else mma<T>(part[n], al[0], ah[0], al[1], ah[1], v.x, v.y);
             mma<T>(part[n], al[2], ah[2], al[3], ah[3], v.z, v.w);
-            if (PARTS == 2) {
-                const uint4 r = *reinterpret_cast<const uint4*>(x[n] + apart + at + 64 * j);
+#pragma unroll
+            for (int p = 1; p < FORM; ++p) {
+                const uint4 r = *reinterpret_cast<const uint4*>(x[n] + p * apart + at + 64 * j);
                 mma<T>(part[n], al[0], ah[0], al[1], ah[1], r.x, r.y);
                 mma<T>(part[n], al[2], ah[2], al[3], ah[3], r.z, r.w);
             }
@@ -723,7 +764,7 @@ struct MoeArgs {
     int32_t x_rows, h_rows;    // tokens' rows of x, of h that fit there
     int32_t all_x;             // shared memory holds every token's row
     int32_t fold;              // rows of h and one of zeros, where shared memory holds all; else 0
-    int32_t one;               // the grid is one cluster
+    int32_t one;               // the grid is one cluster of as many blocks, or 0
     int64_t m13_bytes, m2_bytes;       // of an expert's matrices
     int32_t* far_chosen;       // [tokens * top_k]: choices made by other blocks
     float* far_c;
@@ -808,26 +849,58 @@ template <> struct Weights<32> : PackedWeights<32> {};
 template <> struct Weights<64> : PackedWeights<64> {};
 template <> struct Weights<128> : PackedWeights<128> {};
 
-// sum += W x over one block, x in PARTS 16-bit parts `apart` bytes from one another.
-template <class T, int W, int NT, int PARTS>
-__device__ __forceinline__ void moe_block(float (&sum)[NT][4], const char* stage, const char* const (&x)[NT],
-                                          int apart, int at, int shift_lo, int shift_hi, int lane) {
+// sum += W x over one block.  low: of the second and third parts of an element, whose
+// sums, 2^-8 of the others, then lose nothing beside them.
+template <class T, int W, int NT, Form FORM>
+__device__ __forceinline__ void moe_block(float (&sum)[NT][4], float (&low)[NT][4], const char* stage,
+                                          const char* const (&x)[NT], int apart, int at, int shift_lo, int shift_hi,
+                                          int lane, bool inf) {
     if constexpr (W >= 32) {
-        block_product<T, W, NT, PARTS>(sum, stage, x, at, lane, apart);
+        block_product<T, W, NT, FORM>(sum, stage, x, at, lane, apart, inf);
     } else {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const uint4 l = Weights<W>::read(stage, 0, j, shift_lo, lane);
             const uint4 h = Weights<W>::read(stage, 1, j, shift_hi, lane);
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n) {
+                if constexpr (FORM == kFloats) {
+                    const Parts v(x[n] + at + 64 * j, apart, inf);
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(x[n] + p * apart + at + 64 * j);
-                    mma<T>(sum[n], l.x, h.x, l.y, h.y, v.x, v.y);
-                    mma<T>(sum[n], l.z, h.z, l.w, h.w, v.z, v.w);
+                    for (int p = 0; p < 3; ++p) {
+                        mma<T>(p ? low[n] : sum[n], l.x, h.x, l.y, h.y, v.w[p][0], v.w[p][1]);
+                        mma<T>(p ? low[n] : sum[n], l.z, h.z, l.w, h.w, v.w[p][2], v.w[p][3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int p = 0; p < FORM; ++p) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(x[n] + p * apart + at + 64 * j);
+                        mma<T>(p && FORM == kThirds ? low[n] : sum[n], l.x, h.x, l.y, h.y, v.x, v.y);
+                        mma<T>(p && FORM == kThirds ? low[n] : sum[n], l.z, h.z, l.w, h.w, v.z, v.w);
+                    }
                 }
+            }
         }
+    }
+}
+
+// Four elements of h from column c on to the planes of their row.
+template <class T, Form H>
+__device__ __forceinline__ void put_hidden(char* row, int apart, int c, float (&v)[4]) {
+    if (H == kFloats) {
+        *reinterpret_cast<float4*>(row + (c & 4 ? apart : 0) + 2 * (c & ~7)) = make_float4(v[0], v[1], v[2], v[3]);
+        return;
+    }
+#pragma unroll
+    for (int p = 0; p < planes_of(H); ++p) {
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            w[q] = H == kThirds ? __float_as_uint(v[q]) >> 16 : T::round(v[q]);
+            v[q] -= T::widen(uint16_t(w[q]));
+            if (!isfinite(v[q])) v[q] = 0.0f;      // (an infinite element has no rest)
+        }
+        *reinterpret_cast<uint2*>(row + p * apart + 2 * c) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
     }
 }
 
@@ -859,6 +932,7 @@ struct MoeTables {
     uint32_t scan[kWarps];
     uint32_t total;                    // pairs << 16 | passes
     uint32_t stop;
+    uint32_t inf;                      // an element of h here is not finite
 };
 
 // The pair of a local expert and one of its tokens.
@@ -1145,12 +1219,13 @@ __device__ __forceinline__ int h_exponent(uint32_t top) {
     return top ? max(-100, min(100, 14 - ilogbf(__uint_as_float(top)))) : 0;
 }
 
-// A pass's h as two 16-bit parts, v = hi + lo to 2^-16 of v: the product then
-// keeps what float32 h would give, at twice the matrix instructions, which are
-// not what bounds it.  float16 parts are of v times a power of two that brings the
-// token's largest finite element to 2^14..2^15, so that none overflows and what
-// underflows is below 2^-39 of the largest.
-template <class T>
+// A pass's h, which the first product left in float32.
+//   bfloat16: three parts, which hold all of its 24 bits, or float32 as it is where three
+//   planes leave a pass too few rows (prepare_moe); a lane then splits what it reads.
+//   float16: two parts, v = hi + lo to 2^-22 of v, of v times a power of two that brings
+//   the token's largest finite element to 2^14..2^15, so that none overflows and what
+//   underflows is below 2^-39 of the largest.
+template <class T, Form H>
 __device__ __forceinline__ void stage_h(const MoeArgs& a, MoeTables& tab, char* to, int first, int count, int cols) {
     const int chunks = cols / 4;
 #pragma unroll 4
@@ -1159,25 +1234,18 @@ __device__ __forceinline__ void stage_h(const MoeArgs& a, MoeTables& tab, char* 
         float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (c < a.inter) f = __ldcg(reinterpret_cast<const float4*>(a.h + int64_t(first + i) * a.h_ld + c));
         float up = 1.0f;
-        if (std::is_same<T, F16>::value) {
+        if (H == kHalves) {
             const int e = h_exponent(__ldcg(a.h_top + first + i));
             up = ldexpf(1.0f, e);
             if (c == 0) tab.scale[first + i] = ldexpf(1.0f, -e);
         }
-        const float v[4] = {f.x, f.y, f.z, f.w};
-        uint32_t hi[4], lo[4];
+        float v[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const float s = c + q < a.inter ? v[q] * up : 0.0f;
-            hi[q] = T::round(s);
-            const float rest = s - T::widen(uint16_t(hi[q]));
-            // (An infinite v has no rest; one just under the largest may round to
-            // infinity in bfloat16, as the result then does.)
-            lo[q] = T::round(isfinite(rest) ? rest : 0.0f);
+            v[q] = c + q < a.inter ? v[q] * up : 0.0f;
+            if (H == kFloats && !isfinite(v[q])) tab.inf = 1;
         }
-        char* const dst = to + i * a.h_pitch + 2 * c;
-        *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-        *reinterpret_cast<uint2*>(dst + a.h_rows * a.h_pitch) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+        put_hidden<T, H>(to + i * a.h_pitch, a.h_rows * a.h_pitch, c, v);
     }
 }
 
@@ -1217,11 +1285,12 @@ __device__ __forceinline__ void moe_put(const MoeArgs& a, const MoePhase& p, con
 // Blocks [b, stop) of item f by one warp: its sums go out where `whole` says that the
 // warp has the item from its first block on and this is its last, else to `first`
 // (the item ends here) or `last`.  NT: groups of 8 tokens.
-template <class T, int W, int PHASE, int NT>
+template <class T, int W, Form H, int PHASE, int NT>
 __device__ __forceinline__ void moe_item(const MoeArgs& a, const MoePhase& p, const MoeTables& tab, Feed<W>& feed,
                                          char* fifo, int& slot, const char* region, float4* firsts, float4* lasts,
                                          int base, int f, int b, int stop, bool whole) {
-    constexpr int kParts = PHASE == 0 ? 1 : 2, kStages = Weights<W>::kStages, kBytes = Weights<W>::kBytes;
+    constexpr Form kForm = PHASE == 0 ? kWhole : H;
+    constexpr int kStages = Weights<W>::kStages, kBytes = Weights<W>::kBytes;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int pitch = PHASE == 0 ? a.x_pitch : a.h_pitch, apart = a.h_rows * a.h_pitch;
     const int pass = p.pass(f), first = tab.pass_first[pass], count = tab.pass_count[pass];
@@ -1239,18 +1308,22 @@ __device__ __forceinline__ void moe_item(const MoeArgs& a, const MoePhase& p, co
         shift_lo = int(reinterpret_cast<uintptr_t>(w.lo) & 15);
         shift_hi = int(reinterpret_cast<uintptr_t>(w.hi) & 15);
     }
-    float sum[NT][4] = {};
+    const bool inf = kForm == kFloats && tab.inf;
+    float sum[NT][4] = {}, low[NT][4] = {};
     for (; b < stop; ++b) {
         copy_wait<kStages - 2>();
         __syncwarp();      // what lanes share is there, and the last stage has been read
         feed.load(p, tab, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
-        moe_block<T, W, NT, kParts>(sum, fifo + slot * kBytes, x, apart, b * (2 * Weights<W>::kCols), shift_lo, shift_hi,
-                                    lane);
+        moe_block<T, W, NT, kForm>(sum, low, fifo + slot * kBytes, x, apart, b * (2 * Weights<W>::kCols), shift_lo,
+                                   shift_hi, lane, inf);
         slot = slot + 1 == kStages ? 0 : slot + 1;
     }
     const bool ends = stop == p.blocks;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+            if (kForm >= kThirds && W < 32)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[n][k] += low[n][k];
         if (ends && whole) moe_put<T, PHASE>(a, p, tab, f, lane, n, sum[n]);
         else (ends ? firsts : lasts)[(warp * 2 + n) * 32 + lane] = make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
     }
@@ -1258,7 +1331,7 @@ __device__ __forceinline__ void moe_item(const MoeArgs& a, const MoePhase& p, co
 
 // A window's items [i0, end), whose tokens are in shared memory from pair `base` on, in
 // the order of Feed.
-template <class T, int W, int PHASE>
+template <class T, int W, Form H, int PHASE>
 __device__ __forceinline__ void moe_window(const MoeArgs& a, const MoePhase& p, const MoeTables& tab, Feed<W>& feed,
                                            char* fifo, int& slot, const char* region, float4* parts, int base, int i0,
                                            int end) {
@@ -1267,9 +1340,9 @@ __device__ __forceinline__ void moe_window(const MoeArgs& a, const MoePhase& p, 
     float4* const lasts = parts + kWarps * 2 * 32;
     const auto item = [&](int f, int b, int stop, bool whole) {
         if (tab.pass_count[p.pass(f)] <= 8)
-            moe_item<T, W, PHASE, 1>(a, p, tab, feed, fifo, slot, region, firsts, lasts, base, f, b, stop, whole);
+            moe_item<T, W, H, PHASE, 1>(a, p, tab, feed, fifo, slot, region, firsts, lasts, base, f, b, stop, whole);
         else
-            moe_item<T, W, PHASE, 2>(a, p, tab, feed, fifo, slot, region, firsts, lasts, base, f, b, stop, whole);
+            moe_item<T, W, H, PHASE, 2>(a, p, tab, feed, fifo, slot, region, firsts, lasts, base, f, b, stop, whole);
     };
     const int rest = end - (end - i0) % kWarps;
     const int total = (end - rest) * p.blocks, lo = share_from(warp, total), hi = share_from(warp + 1, total);
@@ -1321,7 +1394,7 @@ __device__ __forceinline__ void moe_window(const MoeArgs& a, const MoePhase& p, 
 
 // Tokens of as many passes as fit are staged at once, so that warps go from one
 // pass to the next without meeting.
-template <class T, int W, int PHASE>
+template <class T, int W, Form H, int PHASE>
 __device__ __forceinline__ void moe_phase(const MoeArgs& a, const MoePhase* ph, MoeTables& tab, Feed<W>& feed,
                                           char* fifo, int& slot, char* region, float4* parts) {
     const MoePhase& p = ph[PHASE];
@@ -1331,11 +1404,11 @@ __device__ __forceinline__ void moe_phase(const MoeArgs& a, const MoePhase* ph, 
         if (!(PHASE == 0 && a.all_x)) {
             __syncthreads();
             if (PHASE == 0) stage_tokens(a, tab, region, base, pairs, p.blocks * Weights<W>::kCols);
-            else stage_h<T>(a, tab, region, base, pairs, p.blocks * Weights<W>::kCols);
+            else stage_h<T, H>(a, tab, region, base, pairs, p.blocks * Weights<W>::kCols);
             copy_wait<0>();
             __syncthreads();
         }
-        moe_window<T, W, PHASE>(a, p, tab, feed, fifo, slot, region, parts, base, i0, end);
+        moe_window<T, W, H, PHASE>(a, p, tab, feed, fifo, slot, region, parts, base, i0, end);
         i0 = end;
     }
 }
@@ -1375,7 +1448,7 @@ struct FoldFeed {
     }
 };
 
-template <class T, int W>
+template <class T, int W, Form H>
 __device__ __forceinline__ void stage_fold(const MoeArgs& a, MoeTables& tab, char* region, int pairs, int cols) {
     const bool half = std::is_same<T, F16>::value;
     if (half) {
@@ -1405,28 +1478,24 @@ __device__ __forceinline__ void stage_fold(const MoeArgs& a, MoeTables& tab, cha
             up = tab.pair_c[i];
             if (half) up *= tab.scale[8 + tab.token[i]];
         }
-        const float v[4] = {f.x, f.y, f.z, f.w};
-        uint32_t hi[4], lo[4];
+        float v[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const float s = i < pairs && c + q < a.inter ? v[q] * up : 0.0f;
-            hi[q] = T::round(s);
-            const float rest = s - T::widen(uint16_t(hi[q]));
-            lo[q] = T::round(isfinite(rest) ? rest : 0.0f);
+            v[q] = i < pairs && c + q < a.inter ? v[q] * up : 0.0f;
+            if (H == kFloats && !isfinite(v[q])) tab.inf = 1;
         }
         // The row of zeros that absent tokens read is the last.
-        char* const dst = region + (i < pairs ? i : a.fold - 1) * a.h_pitch + 2 * c;
-        *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-        *reinterpret_cast<uint2*>(dst + apart) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+        put_hidden<T, H>(region + (i < pairs ? i : a.fold - 1) * a.h_pitch, apart, c, v);
     }
 }
 
-template <class T, int W>
+template <class T, int W, Form H>
 __device__ __forceinline__ void moe_fold(const MoeArgs& a, const MoePhase& p, MoeTables& tab, FoldFeed<W>& feed,
                                          char* fifo, int& slot, const char* region, float4* red, int passes) {
     constexpr int kStages = Weights<W>::kStages, kBytes = Weights<W>::kBytes;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int apart = a.fold * a.h_pitch;
+    const bool inf = H == kFloats && tab.inf;
     const uint32_t fifo_at = smem_at(fifo);
     const int total = passes * p.blocks, lo = share_from(warp, total), hi = share_from(warp + 1, total);
     for (int strip = p.f0; strip < p.f0 + p.n; ++strip) {
@@ -1444,21 +1513,21 @@ __device__ __forceinline__ void moe_fold(const MoeArgs& a, const MoePhase& p, Mo
                 shift_lo = int(reinterpret_cast<uintptr_t>(w.lo) & 15);
                 shift_hi = int(reinterpret_cast<uintptr_t>(w.hi) & 15);
             }
-            float part[1][4] = {};
+            float part[1][4] = {}, low[1][4] = {};
             at += stop - b;
             for (; b < stop; ++b) {
                 copy_wait<kStages - 2>();
                 __syncwarp();
                 feed.load(p, tab, passes, fifo_at + (slot == 0 ? kStages - 1 : slot - 1) * kBytes, warp, lane);
-                moe_block<T, W, 1, 2>(part, fifo + slot * kBytes, x, apart, b * (2 * Weights<W>::kCols), shift_lo,
-                                      shift_hi, lane);
+                moe_block<T, W, 1, H>(part, low, fifo + slot * kBytes, x, apart, b * (2 * Weights<W>::kCols), shift_lo,
+                                      shift_hi, lane, inf);
                 slot = slot + 1 == kStages ? 0 : slot + 1;
             }
             // Only of tokens that chose the expert: zeros times its weights are not zero
             // where these are infinite or NaN.
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (mask >> (2 * t + (k & 1)) & 1) sum[k] += part[0][k];
+                if (mask >> (2 * t + (k & 1)) & 1) sum[k] += part[0][k] + low[0][k];
         }
         red[threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
         __syncthreads();
@@ -1522,7 +1591,7 @@ constexpr int kPrefetch = 8;       // strips of the second phase that a block as
 // Each chosen expert's weights are read once per 16 tokens.  Blocks take equal runs of
 // (pass, strip of 16 rows) items; warps stream weights through stages that already
 // fill with the next phase's while the blocks wait.
-template <class T, int W>
+template <class T, int W, Form H>
 __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_constant__ MoeArgs a) {
     extern __shared__ __align__(128) char smem[];
     constexpr int kFifo = kWarps * Weights<W>::kStages * Weights<W>::kBytes;
@@ -1533,7 +1602,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 
     after_previous();
-    if (threadIdx.x == 0) tab.stop = tab.most = 0;
+    if (threadIdx.x == 0) tab.stop = tab.most = tab.inf = 0;
     for (int i = threadIdx.x; i < a.n_local; i += kProdThreads) tab.mask[0][i] = tab.mask[1][i] = 0;
 
     // Logits; then, while other blocks are at theirs, tokens to shared memory where all of them fit.
@@ -1649,7 +1718,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
     int slot = 0;
     Feed<W> feed;
     feed.start(ph[0], tab, smem_at(fifo), slot, warp, lane);
-    moe_phase<T, W, 0>(a, ph, tab, feed, fifo, slot, region, red);
+    moe_phase<T, W, H, 0>(a, ph, tab, feed, fifo, slot, region, red);
     grid_arrive(a, 1);
     const int passes = int(tab.total & 0xFFFF);
     if (a.fold) {
@@ -1664,9 +1733,9 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
         if (W != 1 && warp == kWarps / 2 && ph[1].n > 0)
             for (int i = lane; i < passes; i += 32) prefetch_item<W>(ph[1], tab.pass_expert[i], ph[1].f0);
         if (!grid_wait(a, tab, 1)) return;
-        stage_fold<T, W>(a, tab, region, int(tab.total >> 16), ph[1].blocks * Weights<W>::kCols);
+        stage_fold<T, W, H>(a, tab, region, int(tab.total >> 16), ph[1].blocks * Weights<W>::kCols);
         __syncthreads();
-        moe_fold<T, W>(a, ph[1], tab, fold, fifo, slot, region, red, passes);
+        moe_fold<T, W, H>(a, ph[1], tab, fold, fifo, slot, region, red, passes);
         copy_wait<0>();
         finish(a);
         return;
@@ -1677,7 +1746,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
         prefetch_item<W>(ph[1], tab.pass_expert[pass], f - pass * ph[1].strips);
     }
     if (!grid_wait(a, tab, 1)) return;
-    moe_phase<T, W, 1>(a, ph, tab, feed, fifo, slot, region, red);
+    moe_phase<T, W, H, 1>(a, ph, tab, feed, fifo, slot, region, red);
     copy_wait<0>();
     grid_arrive(a, 2);
     if (!grid_wait(a, tab, 2)) return;
@@ -1848,8 +1917,25 @@ MoeSpace moe_space(const rr_moe_layer* L, int64_t tokens) {
     return s;
 }
 
+// How the rows of a call's tokens share a block's shared memory.
+void moe_rows(MoeArgs* a, int room, Form form) {
+    const int h_row = planes_of(form) * a->h_pitch, each = std::max(a->x_pitch, h_row);
+    a->cap = std::min(16, room / each);
+    if (a->cap > 8 && a->cap < 16) a->cap = 8;
+    a->cap = std::min(a->cap, a->tokens);
+    a->x_rows = room / a->x_pitch;
+    a->h_rows = room / h_row;
+    a->all_x = a->tokens <= a->x_rows;
+    // Every h at once, for up to 8 tokens (one group of columns).
+    const int64_t rows = int64_t(a->tokens) * std::min(a->top_k, a->n_local) + 1;
+    a->fold = a->tokens <= 8 && a->cap == a->tokens && rows <= a->h_rows ? int32_t(rows) : 0;
+}
+
+template <class T, int W, Form H>
+rr_status launch_moe(const MoeArgs& a, int smem, int dev, cudaStream_t stream);
+
 template <class T, int W>
-rr_status launch_moe(MoeArgs a, int dev, cudaStream_t stream) {
+rr_status prepare_moe(MoeArgs a, int dev, cudaStream_t stream) {
     // Tokens that a pass holds in shared memory, by the longer of the two phases' rows.
     constexpr int kFixed = kWarps * Weights<W>::kStages * Weights<W>::kBytes + kJoinBytes +
                            (sizeof(MoeTables) + 127) / 128 * 128 + 1024 /* static */;
@@ -1859,27 +1945,36 @@ rr_status launch_moe(MoeArgs a, int dev, cudaStream_t stream) {
     static_assert(kSmem - kFixed >= 2 * kMaxHidden + 64 && kSmem - kFixed >= 2 * (2 * kMaxInter + 64), "the longest rows fit");
     a.x_pitch = pitch(a.hidden);
     a.h_pitch = pitch(a.inter);
-    const int each = std::max(a.x_pitch, 2 * a.h_pitch), room = kSmem - kFixed;
-    a.cap = std::min(16, room / each);
-    if (a.cap > 8 && a.cap < 16) a.cap = 8;
-    a.cap = std::min(a.cap, a.tokens);
-    if (a.cap < 1) return rr_fail(RR_ELAYOUT, "hidden %d, inter %d: rows too long", a.hidden, a.inter);
-    a.x_rows = room / a.x_pitch;
-    a.h_rows = room / (2 * a.h_pitch);
-    a.all_x = a.tokens <= a.x_rows;
-    // Every h at once, for up to 8 tokens (one group of columns).
-    const int64_t rows = int64_t(a.tokens) * std::min(a.top_k, a.n_local) + 1;
-    a.fold = a.tokens <= 8 && a.cap == a.tokens && rows <= a.h_rows ? int32_t(rows) : 0;
-    const int smem = kFixed - 1024 + room;
+    constexpr int room = kSmem - kFixed, smem = kFixed - 1024 + room;
     const int64_t bytes = std::min<int64_t>(int64_t(a.tokens) * a.top_k, a.n_local) * (a.m13_bytes + a.m2_bytes);
-    a.one = bytes <= kCluster16Bytes;
+    a.one = bytes <= kCluster8Bytes ? 8 : bytes <= kCluster16Bytes ? 16 : 0;
+    if constexpr (std::is_same<T, F16>::value) {
+        moe_rows(&a, room, kHalves);
+        return launch_moe<T, W, kHalves>(a, smem, dev, stream);
+    } else {
+        // In three parts (Qwen3-30B-A3B, 64 tokens: 230 us, in float32 260; two parts, which
+        // do not hold all of h, 217) where a pass holds as many tokens so, or twice an
+        // expert's mean, but for float32's less room in the second phase without a third
+        // barrier.  (16 experts of 2048 x 4096, 8 tokens, 3 against 4 a pass: 113 and 131 us;
+        // 64 tokens 350 and 316; 8 of 4096 x 8192, 64 tokens, 1 against 2: 3551 and 2052.)
+        MoeArgs parts = a;
+        moe_rows(&a, room, kFloats);
+        moe_rows(&parts, room, kThirds);
+        const bool enough = parts.cap == a.cap || int64_t(parts.cap) * a.n_experts >= 2 * int64_t(a.tokens) * a.top_k;
+        if (parts.cap >= 1 && enough && parts.fold == a.fold) return launch_moe<T, W, kThirds>(parts, smem, dev, stream);
+        return launch_moe<T, W, kFloats>(a, smem, dev, stream);
+    }
+}
+
+template <class T, int W, Form H>
+rr_status launch_moe(const MoeArgs& a, int smem, int dev, cudaStream_t stream) {
     static std::atomic<uint32_t> ready{0};
-    RR_CUDA(allow_smem(rr_moe_kernel<T, W>, kSmem - 1024, dev, &ready));
+    RR_CUDA(allow_smem(rr_moe_kernel<T, W, H>, kSmem - 1024, dev, &ready));
     if (a.one) {
-        const unsigned blocks = bytes <= kCluster8Bytes ? 8 : 16;
+        const unsigned blocks = unsigned(a.one);
         static std::atomic<uint32_t> large{0};     // more than 8 blocks are asked for by name
         if (blocks > 8 && !(large.load(std::memory_order_relaxed) >> dev & 1)) {
-            RR_CUDA(cudaFuncSetAttribute(rr_moe_kernel<T, W>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+            RR_CUDA(cudaFuncSetAttribute(rr_moe_kernel<T, W, H>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
             large.fetch_or(1u << dev, std::memory_order_relaxed);
         }
         cudaLaunchAttribute attr[2];
@@ -1895,7 +1990,7 @@ rr_status launch_moe(MoeArgs a, int dev, cudaStream_t stream) {
         cfg.stream = stream;
         cfg.attrs = attr;
         cfg.numAttrs = 2;
-        RR_CUDA(cudaLaunchKernelEx(&cfg, rr_moe_kernel<T, W>, a));
+        RR_CUDA(cudaLaunchKernelEx(&cfg, rr_moe_kernel<T, W, H>, a));
         return RR_OK;
     }
     static std::atomic<int> grids[kMaxDevices] = {};
@@ -1909,8 +2004,8 @@ rr_status launch_moe(MoeArgs a, int dev, cudaStream_t stream) {
     }
     // (Programmatic dependent launch besides left the gap between two launches at
     // the same 4 us.)
-    void* args[] = {&a};
-    RR_CUDA(cudaLaunchCooperativeKernel((const void*)rr_moe_kernel<T, W>, dim3(unsigned(grid)), dim3(kProdThreads), args,
+    void* args[] = {const_cast<MoeArgs*>(&a)};
+    RR_CUDA(cudaLaunchCooperativeKernel((const void*)rr_moe_kernel<T, W, H>, dim3(unsigned(grid)), dim3(kProdThreads), args,
                                         size_t(smem), stream));
     return RR_OK;
 }
@@ -2225,9 +2320,9 @@ extern "C" rr_status rr_moe(const rr_moe_layer* L, const void* router, const voi
     return with_group(L->dtype, L->group, [&](auto t, auto g) -> rr_status {
         using T = decltype(t);
         constexpr int G = decltype(g)::value;
-        if constexpr (G != 0) return launch_moe<T, G>(a, dev, stream);
-        else if (L->hidden % 8 == 0 && L->inter % 8 == 0) return launch_moe<T, 0>(a, dev, stream);
-        else return launch_moe<T, 1>(a, dev, stream);
+        if constexpr (G != 0) return prepare_moe<T, G>(a, dev, stream);
+        else if (L->hidden % 8 == 0 && L->inter % 8 == 0) return prepare_moe<T, 0>(a, dev, stream);
+        else return prepare_moe<T, 1>(a, dev, stream);
     });
 }
 
