@@ -849,8 +849,10 @@ template <> struct Weights<32> : PackedWeights<32> {};
 template <> struct Weights<64> : PackedWeights<64> {};
 template <> struct Weights<128> : PackedWeights<128> {};
 
-// sum += W x over one block.  low: of the second and third parts of an element, whose
-// sums, 2^-8 of the others, then lose nothing beside them.
+// sum += W x over one block.  low (16-bit weights): of the second and third parts of an
+// element, whose sums, 2^-8 of the others, then lose nothing beside them.  Where the
+// first parts' sum is infinite or NaN it is the result: a part of zero times an infinite
+// weight would make NaN of what is infinite (join_low).
 template <class T, int W, int NT, Form FORM>
 __device__ __forceinline__ void moe_block(float (&sum)[NT][4], float (&low)[NT][4], const char* stage,
                                           const char* const (&x)[NT], int apart, int at, int shift_lo, int shift_hi,
@@ -875,14 +877,16 @@ __device__ __forceinline__ void moe_block(float (&sum)[NT][4], float (&low)[NT][
 #pragma unroll
                     for (int p = 0; p < FORM; ++p) {
                         const uint4 v = *reinterpret_cast<const uint4*>(x[n] + p * apart + at + 64 * j);
-                        mma<T>(p && FORM == kThirds ? low[n] : sum[n], l.x, h.x, l.y, h.y, v.x, v.y);
-                        mma<T>(p && FORM == kThirds ? low[n] : sum[n], l.z, h.z, l.w, h.w, v.z, v.w);
+                        mma<T>(p ? low[n] : sum[n], l.x, h.x, l.y, h.y, v.x, v.y);
+                        mma<T>(p ? low[n] : sum[n], l.z, h.z, l.w, h.w, v.z, v.w);
                     }
                 }
             }
         }
     }
 }
+
+__device__ __forceinline__ float join_low(float sum, float low) { return fabsf(sum) < INFINITY ? sum + low : sum; }
 
 // Four elements of h from column c on to the planes of their row.
 template <class T, Form H>
@@ -1308,7 +1312,7 @@ __device__ __forceinline__ void moe_item(const MoeArgs& a, const MoePhase& p, co
         shift_lo = int(reinterpret_cast<uintptr_t>(w.lo) & 15);
         shift_hi = int(reinterpret_cast<uintptr_t>(w.hi) & 15);
     }
-    const bool inf = kForm == kFloats && tab.inf;
+    const bool inf = kForm == kFloats && W >= 32 && tab.inf;
     float sum[NT][4] = {}, low[NT][4] = {};
     for (; b < stop; ++b) {
         copy_wait<kStages - 2>();
@@ -1321,9 +1325,9 @@ __device__ __forceinline__ void moe_item(const MoeArgs& a, const MoePhase& p, co
     const bool ends = stop == p.blocks;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-            if (kForm >= kThirds && W < 32)
+            if (kForm != kWhole && W < 32)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum[n][k] += low[n][k];
+            for (int k = 0; k < 4; ++k) sum[n][k] = join_low(sum[n][k], low[n][k]);
         if (ends && whole) moe_put<T, PHASE>(a, p, tab, f, lane, n, sum[n]);
         else (ends ? firsts : lasts)[(warp * 2 + n) * 32 + lane] = make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
     }
@@ -1495,11 +1499,11 @@ __device__ __forceinline__ void moe_fold(const MoeArgs& a, const MoePhase& p, Mo
     constexpr int kStages = Weights<W>::kStages, kBytes = Weights<W>::kBytes;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int apart = a.fold * a.h_pitch;
-    const bool inf = H == kFloats && tab.inf;
+    const bool inf = H == kFloats && W >= 32 && tab.inf;
     const uint32_t fifo_at = smem_at(fifo);
     const int total = passes * p.blocks, lo = share_from(warp, total), hi = share_from(warp + 1, total);
     for (int strip = p.f0; strip < p.f0 + p.n; ++strip) {
-        float sum[4] = {};
+        float sum[4] = {}, low_sum[4] = {};
         int pass = lo / p.blocks, b = lo % p.blocks;
         for (int at = lo; at < hi; ++pass, b = 0) {
             const int e = tab.pass_expert[pass], stop = min(p.blocks, b + hi - at);
@@ -1527,8 +1531,14 @@ __device__ __forceinline__ void moe_fold(const MoeArgs& a, const MoePhase& p, Mo
             // where these are infinite or NaN.
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (mask >> (2 * t + (k & 1)) & 1) sum[k] += part[0][k] + low[0][k];
+                if (mask >> (2 * t + (k & 1)) & 1) {
+                    sum[k] += part[0][k];
+                    if (W < 32) low_sum[k] += low[0][k];
+                }
         }
+        if (W < 32)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[k] = join_low(sum[k], low_sum[k]);
         red[threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
         __syncthreads();
         if (threadIdx.x < 128) {
