@@ -351,23 +351,25 @@ __device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a
             : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 
-// A word's codes as four pairs of 16-bit numbers q * kStep, exact; pair n is codes
+// A word's codes as four pairs of 16-bit numbers q / kUp, exact; pair n is codes
 // n and n + 4 (columns 2 n, 2 n + 1).  One shift serves two pairs: codes in bits 0..3
 // and 4..7 of a half become numbers where they are.  What bounds the packed products
 // is this arithmetic (half the shifts of one per pair: lm_head of Qwen3-8B, one
 // token, 59 -> 55 us).
 //   bfloat16: the low 8 bits of a pattern without others stand for their value times
 //   2^-133 (the subnormals and the binade above them are evenly spaced), so a
-//   multiplication by 2^127 or 2^123 brings either code to c 2^-6.
+//   multiplication by 2^123 or 2^119 brings either code to c 2^-10.  A group's 128
+//   products of codes up to 7 2^-10 then stay below the largest element, and no sum
+//   overflows that the result does not; results are multiplied by kUp = 2^10 at the end.
 //   float16: under the exponent of 1024 they read 1024 + c and 1024 + 16 c.
 template <class T>
 struct Codes {
-    static constexpr float kStep = std::is_same<T, BF16>::value ? 1.0f / 64 : 1.0f;
+    static constexpr float kUp = std::is_same<T, BF16>::value ? 1024.0f : 1.0f;
     static __device__ __forceinline__ uint32_t pair(uint32_t v, bool high) {
         uint32_t d;
         if (std::is_same<T, BF16>::value) {
-            // 2^127, 2^123; - 8 * 2^-6.
-            asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(v), "r"(high ? 0x7D007D00u : 0x7F007F00u), "r"(0xBE00BE00u));
+            // 2^123, 2^119; - 8 * 2^-10.
+            asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(v), "r"(high ? 0x7B007B00u : 0x7D007D00u), "r"(0xBC00BC00u));
         } else {
             // 1, 1 / 16; - 1032, - 72.
             asm("fma.rn.f16x2 %0, %1, %2, %3;"
@@ -456,7 +458,8 @@ struct Parts {
 
 // sum += W x over one block of 128 columns.  x[n]: this lane's 16 bytes of its
 // token's row at the block's first column, in shared memory; planes are `apart` bytes
-// apart.  Groups are summed in the matrix unit and scaled in float32.
+// apart.  Groups are summed in the matrix unit and scaled in float32; the sums are
+// 1 / kUp of the product's.
 template <class T, int G, int NT, Form FORM = kWhole>
 __device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* stage, const char* const (&x)[NT],
                                               int at, int lane, int apart = 0, bool inf = false) {
@@ -501,12 +504,10 @@ __device__ __forceinline__ void block_product(float (&sum)[NT][4], const char* s
             const float sl = T::widen(uint16_t(s[32 * j / G])), sh = T::widen(uint16_t(s[32 * j / G] >> 16));
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                // (The scale times 64 might overflow.)
-                constexpr float kUp = 1.0f / Codes<T>::kStep;
-                sum[n][0] = fmaf(sl, kUp * part[n][0], sum[n][0]);
-                sum[n][1] = fmaf(sl, kUp * part[n][1], sum[n][1]);
-                sum[n][2] = fmaf(sh, kUp * part[n][2], sum[n][2]);
-                sum[n][3] = fmaf(sh, kUp * part[n][3], sum[n][3]);
+                sum[n][0] = fmaf(sl, part[n][0], sum[n][0]);
+                sum[n][1] = fmaf(sl, part[n][1], sum[n][1]);
+                sum[n][2] = fmaf(sh, part[n][2], sum[n][2]);
+                sum[n][3] = fmaf(sh, part[n][3], sum[n][3]);
             }
         }
     }
@@ -672,6 +673,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
                 if (++b == nb) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
+                        for (int k = 0; k < 4; ++k) sum[n][k] *= Codes<T>::kUp;
                         if (whole && a.cluster == 1) put_strip<T>(a, f + strip, lane, n, sum[n]);
                         else
                             (whole ? full + strip * kPart : parts + warp * kPart)[n * 32 + lane] =
@@ -689,7 +691,10 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
         __syncwarp();
         if (b != 0)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) last[n * 32 + lane] = make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
+            for (int n = 0; n < NT; ++n) {
+                for (int k = 0; k < 4; ++k) sum[n][k] *= Codes<T>::kUp;
+                last[n * 32 + lane] = make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
+            }
         __syncthreads();
         for (int i = threadIdx.x; i < strips * kPart; i += kProdThreads) {
             const int k = i / kPart, first = share_of(k * nb, total), end = share_of(k * nb + nb - 1, total);
@@ -1325,9 +1330,11 @@ __device__ __forceinline__ void moe_item(const MoeArgs& a, const MoePhase& p, co
     const bool ends = stop == p.blocks;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-            if (kForm != kWhole && W < 32)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) sum[n][k] = join_low(sum[n][k], low[n][k]);
+    #pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (W >= 32) sum[n][k] *= Codes<T>::kUp;
+            else if (kForm != kWhole) sum[n][k] = join_low(sum[n][k], low[n][k]);
+        }
         if (ends && whole) moe_put<T, PHASE>(a, p, tab, f, lane, n, sum[n]);
         else (ends ? firsts : lasts)[(warp * 2 + n) * 32 + lane] = make_float4(sum[n][0], sum[n][1], sum[n][2], sum[n][3]);
     }
@@ -1536,9 +1543,8 @@ __device__ __forceinline__ void moe_fold(const MoeArgs& a, const MoePhase& p, Mo
                     if (W < 32) low_sum[k] += low[0][k];
                 }
         }
-        if (W < 32)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum[k] = join_low(sum[k], low_sum[k]);
+        for (int k = 0; k < 4; ++k) sum[k] = W >= 32 ? sum[k] * Codes<T>::kUp : join_low(sum[k], low_sum[k]);
         red[threadIdx.x] = make_float4(sum[0], sum[1], sum[2], sum[3]);
         __syncthreads();
         if (threadIdx.x < 128) {

@@ -1,4 +1,5 @@
-"""The products at the ends of the number range: infinite weights."""
+"""The products at the ends of the number range: sums that pass it on the way and
+come back, and infinite weights."""
 import math
 
 import pytest
@@ -8,6 +9,27 @@ import paper_2512_22492_gb300 as rr
 from tests import _products as P
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("w_exp,x_exp", [(-30, 126), (-100, 127), (-20, 120), (110, -20), (120, -60), (-60, -30)])
+def test_matvec_large_tokens_small_scales(w_exp, x_exp, group):
+    """Tokens or scales near bfloat16's largest, whose products are far from it:
+    no sum on the way may overflow that the result does not."""
+    gen = torch.Generator().manual_seed(group)
+    rows, cols = 40, 300
+    w = (torch.randn(rows, cols, generator=gen).clamp(-3, 3) * 2.0 ** w_exp).bfloat16()
+    w[3] = 1.5 * 2.0 ** w_exp           # codes of one sign
+    x = ((1 + torch.rand(5, cols, generator=gen) * 0.9) * 2.0 ** x_exp).bfloat16()
+    x[1] *= torch.randn(cols, generator=gen).sign()
+    q = rr.Quantized(rows, cols, group)
+    rr.rr_quantize(q, w.cuda())
+    vals = P.values(*P.quantize(w, group), group)
+    out = torch.empty(5, rows, device="cuda")
+    rr.rr_matvec(q, x.cuda(), out)
+    want, tol = P.matvec(vals, x, False, "f32")
+    assert bool((want.abs() < 2.0 ** 126).all())
+    P.check(out, want, tol)
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
