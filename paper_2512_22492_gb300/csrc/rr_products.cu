@@ -2171,12 +2171,15 @@ bool matvec_shape(MatvecArgs* a, int group, int dev, MatvecShape* shape) {
             if (room < 0 || batch < 1) continue;
             const int64_t joins = cluster == 1 ? 0 : (strips + batch - 1) / batch;
             // In blocks of weights of the busiest warp: those, the copy of the tokens (32 KB
-            // of them cost about as much as a block, 12 KB where they are not aligned), a
-            // cluster's joins.  (24576 x 4096, paired, 16 aligned tokens: 19.0 us so, in one
-            // block's shared memory each, and 21.0 in clusters of 2; 30001 x 4097, 9 unaligned
-            // ones: 22.4 us so, 25.2 where 4 KB count as a block.)
-            const int64_t cost = (strips * blocks + kWarps - 1) / kWarps + pitch * a->tokens / (a->vec ? 32768 : 12288) +
-                                 4 * joins + (stages == 4 ? 1 : 0);
+            // of them cost about as much as a block, 12 KB where rows of that length one
+            // after another are not aligned), a cluster's joins.  (24576 x 4096, paired, 16
+            // tokens: 19.6 us so, in one block's shared memory each, and 21.9 in clusters of 2;
+            // 30001 x 4097, 16: 24.1 us so, 25.0 where 32 KB count as a block.)  Where the tokens
+            // are does not count, as it would then choose the order of the sums: 2048 x 8192,
+            // 8 tokens at an odd address take 10.9 us, and 8.2 with 12 KB.
+            const int64_t cost = (strips * blocks + kWarps - 1) / kWarps +
+                                 pitch * a->tokens / (a->m.cols % 8 == 0 ? 32768 : 12288) + 4 * joins +
+                                 (stages == 4 ? 1 : 0);
             if (cost >= best) continue;
             best = cost;
             a->pitch = int32_t(pitch);
