@@ -581,9 +581,12 @@ rr_status rr_plan_selftest_wait(const rr_plan* plan, cudaStream_t stream);
  * row's length.  Argument errors come back at once (RR_EINVAL; a
  * shape outside the limits RR_ELAYOUT) and nothing is launched.
  *
- * Arithmetic.  Products of 16-bit values are summed in float32, in an order that
- * the shapes alone fix (a call gives the same bits each time); a result is rounded
- * once to its type.  Between a layer's two products, silu(gate) * up is float32; of
+ * Arithmetic.  Products of 16-bit values are summed in float32, and a result is
+ * rounded once to its type.  A call gives the same bits each time, wherever its
+ * tokens, outputs and workspace lie.  The order of rr_matvec's sums follows from the
+ * matrix's description, the number of tokens and the device; that of rr_moe's also
+ * from the experts that the call's tokens choose: a token's last bits may be others
+ * beside tokens that choose other experts.  Between a layer's two products, silu(gate) * up is float32; of
  * float16 layers the second product takes it to 2^-22 of itself or 2^-39 of the
  * token's largest, whichever is more.  Infinities and NaN follow the formulas.
  * ------------------------------------------------------------------------- */
