@@ -671,7 +671,10 @@ enum { RR_MOE_MAX_TOKENS = 64 };
 
 /* Bytes of device workspace that a call with up to max_tokens (1..64) tokens
  * needs.  The caller zero-fills it once; every call leaves it ready for the
- * next.  Calls that overlap in time need distinct workspaces. */
+ * next.  Calls that overlap in time need distinct workspaces.  Blocks of a call wait
+ * for one another, each time for two seconds at most.  A call whose wait runs out
+ * marks its workspace: its outputs are incomplete, and later calls there, though
+ * they return RR_OK, leave theirs as they are until rr_moe_check has reported it. */
 rr_status rr_moe_workspace(const rr_moe_layer* layer, int32_t max_tokens, int64_t* bytes);
 
 /* One layer for n_tokens (0..64) rows of `hidden` 16-bit elements.  ids
@@ -685,8 +688,9 @@ rr_status rr_moe(const rr_moe_layer* layer, const void* router, const void* w13,
                  cudaStream_t stream);
 
 /* Waits for `stream`, then reports (and clears) whether a call on this workspace
- * gave up a bounded wait: RR_ECUDA if so (that call's outputs are incomplete), else
- * RR_OK.  No other call on this workspace may be running. */
+ * gave up a bounded wait: RR_ECUDA if so (the outputs of every call since the last
+ * check that returned RR_OK may be incomplete or unwritten), else RR_OK.  No other
+ * call on this workspace may be running. */
 rr_status rr_moe_check(const rr_moe_layer* layer, int32_t max_tokens, void* workspace,
                        cudaStream_t stream);
 

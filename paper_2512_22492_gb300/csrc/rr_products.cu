@@ -1061,8 +1061,8 @@ __device__ __forceinline__ void choose(const MoeArgs& a, MoeTables& tab, int t, 
 
 // A barrier of all blocks, in two halves.  What a block wrote before it arrived is
 // there for every block that has waited.  Within one cluster it is the hardware's;
-// else the wait is bounded: false when it ran out (about two seconds), which marks
-// the workspace, or when an earlier call's did.
+// else the wait is bounded: it runs out after about two seconds, which marks the
+// workspace.  False then, and where an earlier call's did.
 __device__ __forceinline__ void grid_arrive(const MoeArgs& a, int which) {
     if (a.one) {
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
@@ -1075,7 +1075,8 @@ __device__ __forceinline__ void grid_arrive(const MoeArgs& a, int which) {
 __device__ __forceinline__ bool grid_wait(const MoeArgs& a, MoeTables& tab, int which) {
     if (a.one) {
         asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-        return true;
+        if (tab.stop) copy_wait<0>();
+        return tab.stop == 0;
     }
     if (threadIdx.x == 0) {
         uint32_t seen = 0;
@@ -1618,7 +1619,9 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 
     after_previous();
-    if (threadIdx.x == 0) tab.stop = tab.most = tab.inf = 0;
+    // An earlier call's mark (a grid's blocks look for it when they wait).
+    const uint32_t marked = a.one && threadIdx.x == 0 ? __ldcg(&a.control->error) : 0;
+    if (threadIdx.x == 0) tab.most = tab.inf = 0;
     for (int i = threadIdx.x; i < a.n_local; i += kProdThreads) tab.mask[0][i] = tab.mask[1][i] = 0;
 
     // Logits; then, while other blocks are at theirs, tokens to shared memory where all of them fit.
@@ -1628,6 +1631,7 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_moe_kernel(const __grid_co
             logit_item<T>(a, i % groups * 8, i / groups * 16, reinterpret_cast<float4*>(smem));
         if (blockIdx.x == gridDim.x - 1)
             for (int i = threadIdx.x; i < a.tokens * min(a.top_k, a.n_local); i += kProdThreads) a.h_top[i] = 0;
+        if (threadIdx.x == 0) tab.stop = marked;
         grid_arrive(a, 0);
         if (a.all_x) {
             constexpr int kCols = Weights<W>::kCols;

@@ -255,7 +255,9 @@ class MoeLayer:
 class MoeWorkspace:
     """Device workspace of ``rr_moe`` for up to max_tokens (1..64) tokens of a
     layer, or of any layer of the same shape.  Calls that overlap in time need
-    one each."""
+    one each.  A call whose blocks wait for one another in vain (two seconds) marks
+    its workspace; later calls there leave their outputs as they are until
+    ``rr_moe_check`` has raised."""
 
     def __init__(self, layer: MoeLayer, max_tokens: int):
         import torch
@@ -271,7 +273,8 @@ def rr_moe(layer: MoeLayer, x, out, workspace: MoeWorkspace, ids=None, weights=N
            stream=None) -> None:
     """One mixture-of-experts layer for up to 64 rows of x (asynchronous on
     `stream`).  `ids` (int32) and `weights` (float32), both [n, top_k], receive
-    the chosen experts and their weights."""
+    the chosen experts and their weights.  Outputs hold once ``rr_moe_check`` has
+    found no wait that ran out."""
     n, ldx = _rows(x, layer.hidden, layer.torch_dtype, "x")
     m, ldo = _rows(out, layer.hidden, layer.torch_dtype, "out")
     if m != n:
@@ -297,6 +300,7 @@ def _choice(t, n: int, k: int, what: str, floating: int) -> int:
 
 
 def rr_moe_check(layer: MoeLayer, workspace: MoeWorkspace, stream=None) -> None:
-    """Raise if a call on this workspace gave up a bounded wait (waits for `stream`)."""
+    """Raise if a call on this workspace gave up a bounded wait (waits for `stream`):
+    the outputs since the last check that passed may then be incomplete or unwritten."""
     _check(_lib.rr_moe_check(layer._ref, workspace.max_tokens, workspace._p, _stream(stream)),
            "rr_moe_check")
