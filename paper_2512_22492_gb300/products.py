@@ -254,8 +254,9 @@ class MoeLayer:
 
 class MoeWorkspace:
     """Device workspace of ``rr_moe`` for up to max_tokens (1..64) tokens of a
-    layer, or of any layer of the same shape.  Calls that overlap in time need
-    one each.  A call whose blocks wait for one another in vain (two seconds) marks
+    layer, or of any layer of the same shape, ready on every stream (the constructor
+    waits for its zeros; within a graph capture it cannot, and calls belong to
+    the captured stream).  Calls that overlap in time need one each.  A call whose blocks wait for one another in vain (two seconds) marks
     its workspace; later calls there leave their outputs as they are until
     ``rr_moe_check`` has raised."""
 
@@ -266,6 +267,9 @@ class MoeWorkspace:
                "rr_moe_workspace")
         self.nbytes, self.max_tokens = need.value, max_tokens
         self.data = torch.zeros(self.nbytes, dtype=torch.uint8, device="cuda")
+        # The first call may come on another stream than the zeros.
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()
         self._p = self.data.data_ptr()
 
 

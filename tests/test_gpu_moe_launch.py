@@ -1,5 +1,5 @@
 """How a mixture-of-experts layer is launched: the mark that a wait which ran out
-leaves."""
+leaves, and workspaces."""
 import pytest
 import torch
 
@@ -42,3 +42,18 @@ def test_a_marked_workspace_runs_nothing(experts, hidden, inter, tokens):
     rr.rr_moe(layer, x, out, ws)
     rr.rr_moe_check(layer, ws)
     assert torch.equal(out, want)
+
+
+def test_a_workspace_is_ready_when_it_is_there():
+    """Its zeros have been written when the constructor returns, so that the first call
+    may be on any stream."""
+    layer, _, _, _ = layer_of(7, 8, 128, 96, 2)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)             # about a tenth of a second
+    ws = rr.MoeWorkspace(layer, 4)
+    assert torch.cuda.current_stream().query()
+    x, side = tokens_of(7, 4, 128), torch.cuda.Stream()
+    out = torch.empty_like(x)
+    torch.cuda.synchronize()
+    rr.rr_moe(layer, x, out, ws, stream=side)
+    rr.rr_moe_check(layer, ws, side)
