@@ -735,10 +735,13 @@ constexpr int kMaxExperts = 512, kMaxTopK = 16, kMaxHidden = 32768, kMaxInter = 
 constexpr int kMaxPairs = RR_MOE_MAX_TOKENS * kMaxTopK;
 constexpr int kJoinBytes = 2 * kWarps * 2 * 512;   // shared memory of the warps' parts of strips
 // A layer of little work runs in one cluster, whose barriers and whose launch cost
-// less than a grid's, although few SMs then read all of its weights.  A call with 0.15
-// and 2.4 MB of them: 10.4 and 17.9 us on 8 blocks, 10.7 and 13.8 us on 16, 14.6 us both
-// on a grid; with 4.7 MB 18.1 us on 16 and 14.6.
-constexpr int64_t kCluster8Bytes = 256 << 10, kCluster16Bytes = 5 << 19;
+// less than a grid's, although few SMs then read all of its weights: the experts that
+// tokens may choose, and the router once per 16 tokens.  A call with 0.15 and 2.4 MB of
+// them: 10.4 and 17.9 us on 8 blocks, 10.7 and 13.8 us on 16, 14.6 us both on a grid; with
+// 4.7 MB 18.1 us on 16 and 14.6.  Few experts of a large router: 128 x 2048 and 4 narrow
+// ones, 16 tokens (1.3 MB) 15.6 us on 16 blocks and 20.6; 256 x 4096 and one, one token
+// (2.5 MB) 16.1 and 14.4, 64 tokens (9 MB) 40.5 and 18.5.
+constexpr int64_t kCluster8Bytes = 256 << 10, kCluster16Bytes = 2400 << 10;
 constexpr int kSmem = 227 * 1024;
 
 // The workspace's control block.
@@ -1966,7 +1969,8 @@ rr_status prepare_moe(MoeArgs a, int dev, cudaStream_t stream) {
     a.x_pitch = pitch(a.hidden);
     a.h_pitch = pitch(a.inter);
     constexpr int room = kSmem - kFixed, smem = kFixed - 1024 + room;
-    const int64_t bytes = std::min<int64_t>(int64_t(a.tokens) * a.top_k, a.n_local) * (a.m13_bytes + a.m2_bytes);
+    const int64_t bytes = std::min<int64_t>(int64_t(a.tokens) * a.top_k, a.n_local) * (a.m13_bytes + a.m2_bytes) +
+                          int64_t(a.n_experts) * a.hidden * 2 * ((a.tokens + 15) / 16);
     a.one = bytes <= kCluster8Bytes ? 8 : bytes <= kCluster16Bytes ? 16 : 0;
     if constexpr (std::is_same<T, F16>::value) {
         moe_rows(&a, room, kHalves);

@@ -1,5 +1,7 @@
-"""How a mixture-of-experts layer is launched: the mark that a wait which ran out
-leaves, and workspaces."""
+"""How a mixture-of-experts layer is launched: in one cluster or on every SM, the mark
+that a wait which ran out leaves, and workspaces."""
+import ctypes
+
 import pytest
 import torch
 
@@ -20,6 +22,54 @@ def layer_of(seed, experts, hidden, inter, top_k, first=0, local=None):
 
 def tokens_of(seed, n, hidden):
     return P.grid_tokens(torch.Generator().manual_seed(seed), n, hidden, "bf16").cuda()
+
+
+class _KernelParams(ctypes.Structure):       # CUDA_KERNEL_NODE_PARAMS of the driver API
+    _fields_ = [("func", ctypes.c_void_p), ("grid", ctypes.c_uint * 3), ("block", ctypes.c_uint * 3),
+                ("shared", ctypes.c_uint), ("params", ctypes.c_void_p), ("extra", ctypes.c_void_p),
+                ("kern", ctypes.c_void_p), ("ctx", ctypes.c_void_p)]
+
+
+def blocks_of(layer, tokens):
+    """The thread blocks of a call's one kernel, from a capture of it."""
+    cu = ctypes.CDLL("libcuda.so.1")
+    x = torch.zeros(tokens, layer.hidden, dtype=layer.torch_dtype, device="cuda")
+    out, ws = torch.empty_like(x), rr.MoeWorkspace(layer, tokens)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    handle, graph, n = ctypes.c_void_p(stream.cuda_stream), ctypes.c_void_p(), ctypes.c_size_t(8)
+    assert cu.cuStreamBeginCapture_v2(handle, 2) == 0
+    try:
+        rr.rr_moe(layer, x, out, ws, stream=stream)
+    finally:
+        assert cu.cuStreamEndCapture(handle, ctypes.byref(graph)) == 0
+    nodes = (ctypes.c_void_p * 8)()
+    assert cu.cuGraphGetNodes(graph, nodes, ctypes.byref(n)) == 0 and n.value == 1
+    p = _KernelParams()
+    assert cu.cuGraphKernelNodeGetParams_v2(ctypes.c_void_p(nodes[0]), ctypes.byref(p)) == 0
+    assert cu.cuGraphDestroy(graph) == 0
+    return p.grid[0]
+
+
+# experts, hidden, inter, local, top_k, tokens
+@pytest.mark.parametrize("shape,one", [
+    ((8, 128, 96, 8, 2, 1), True), ((8, 128, 96, 8, 2, 20), True),
+    ((256, 4096, 48, 1, 8, 64), False),        # a 2 MB router, read for every 16 tokens
+    ((512, 4096, 16, 2, 4, 1), False), ((512, 8192, 16, 1, 1, 8), False),
+    ((16, 512, 512, 16, 4, 20), False)])
+def test_one_cluster_or_every_sm(shape, one):
+    """A layer runs in one cluster where all that its call reads is little: the
+    router and the tokens count, too."""
+    experts, hidden, inter, local, top_k, tokens = shape
+    layer, router, w13, w2 = layer_of(3, experts, hidden, inter, top_k, 0, local)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert blocks_of(layer, tokens) in ((8, 16) if one else (sms,))
+    x = tokens_of(tokens, tokens, hidden)
+    ws, out = rr.MoeWorkspace(layer, tokens), torch.empty_like(x)
+    rr.rr_moe(layer, x, out, ws)
+    rr.rr_moe_check(layer, ws)
+    ids, c = P.route(x.cpu(), router, top_k, True)
+    P.check(out, *P.moe(x.cpu(), ids, c, w13.double(), w2.double(), 0, "bf16"))
 
 
 @pytest.mark.parametrize("experts,hidden,inter,tokens", [(8, 128, 96, 1), (8, 128, 96, 20), (16, 512, 512, 20)])
