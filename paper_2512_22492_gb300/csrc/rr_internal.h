@@ -138,6 +138,23 @@ struct rr_plan {
 rr_status rr_fail(rr_status s, const char* fmt, ...);
 void rr_clear_error();
 
+// Products (rr_products.cu).  The blocks of the one cluster in which a layer runs that
+// reads `bytes` of weights; 0: every SM instead.  A layer of little work runs in one
+// cluster, whose barriers and whose launch cost less than a grid's, although few SMs
+// then read all of its weights: the experts that tokens may choose, and the router once
+// per 16 tokens.  A call with 0.15 and 2.4 MB of them: 10.4 and 17.9 us on 8 blocks, 10.7
+// and 13.8 us on 16, 14.6 us both on a grid; with 4.7 MB 18.1 us on 16 and 14.6.  Few
+// experts of a large router: 128 x 2048 and 4 narrow ones, 16 tokens (1.3 MB) 15.6 us on
+// 16 blocks and 20.6; 256 x 4096 and one, one token (2.5 MB) 16.1 and 14.4, 64 tokens (9
+// MB) 40.5 and 18.5.
+// most: the largest cluster of such blocks that the device has room for (a part of a
+// GPU may have none for 16, or none at all).
+inline int rr_moe_cluster(int64_t bytes, int most) {
+    constexpr int64_t kBytes8 = 256 << 10, kBytes16 = 2400 << 10;
+    const int blocks = bytes <= kBytes8 ? 8 : bytes <= kBytes16 ? 16 : 0;
+    return blocks <= most ? blocks : 0;
+}
+
 // Device side (rr_device.cu).
 struct rr_grids {
     int32_t bulk_pack, bulk_unpack, reg_pack, reg_unpack, verify, reg_vunpack;

@@ -734,14 +734,6 @@ __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid
 constexpr int kMaxExperts = 512, kMaxTopK = 16, kMaxHidden = 32768, kMaxInter = 16384;
 constexpr int kMaxPairs = RR_MOE_MAX_TOKENS * kMaxTopK;
 constexpr int kJoinBytes = 2 * kWarps * 2 * 512;   // shared memory of the warps' parts of strips
-// A layer of little work runs in one cluster, whose barriers and whose launch cost
-// less than a grid's, although few SMs then read all of its weights: the experts that
-// tokens may choose, and the router once per 16 tokens.  A call with 0.15 and 2.4 MB of
-// them: 10.4 and 17.9 us on 8 blocks, 10.7 and 13.8 us on 16, 14.6 us both on a grid; with
-// 4.7 MB 18.1 us on 16 and 14.6.  Few experts of a large router: 128 x 2048 and 4 narrow
-// ones, 16 tokens (1.3 MB) 15.6 us on 16 blocks and 20.6; 256 x 4096 and one, one token
-// (2.5 MB) 16.1 and 14.4, 64 tokens (9 MB) 40.5 and 18.5.
-constexpr int64_t kCluster8Bytes = 256 << 10, kCluster16Bytes = 2400 << 10;
 constexpr int kSmem = 227 * 1024;
 
 // The workspace's control block.
@@ -1955,7 +1947,7 @@ void moe_rows(MoeArgs* a, int room, Form form) {
 }
 
 template <class T, int W, Form H>
-rr_status launch_moe(const MoeArgs& a, int smem, int dev, cudaStream_t stream);
+rr_status launch_moe(MoeArgs a, int smem, int dev, cudaStream_t stream);
 
 template <class T, int W>
 rr_status prepare_moe(MoeArgs a, int dev, cudaStream_t stream) {
@@ -1969,9 +1961,6 @@ rr_status prepare_moe(MoeArgs a, int dev, cudaStream_t stream) {
     a.x_pitch = pitch(a.hidden);
     a.h_pitch = pitch(a.inter);
     constexpr int room = kSmem - kFixed, smem = kFixed - 1024 + room;
-    const int64_t bytes = std::min<int64_t>(int64_t(a.tokens) * a.top_k, a.n_local) * (a.m13_bytes + a.m2_bytes) +
-                          int64_t(a.n_experts) * a.hidden * 2 * ((a.tokens + 15) / 16);
-    a.one = bytes <= kCluster8Bytes ? 8 : bytes <= kCluster16Bytes ? 16 : 0;
     if constexpr (std::is_same<T, F16>::value) {
         moe_rows(&a, room, kHalves);
         return launch_moe<T, W, kHalves>(a, smem, dev, stream);
@@ -1990,17 +1979,44 @@ rr_status prepare_moe(MoeArgs a, int dev, cudaStream_t stream) {
     }
 }
 
+// The largest cluster of 16 or 8 blocks that the current device has room for, or 0.
+template <class K>
+int largest_cluster(K* kernel, int smem) {
+    for (int blocks = 16; blocks >= 8; blocks /= 2) {
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = unsigned(blocks);
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(unsigned(blocks));
+        cfg.blockDim = dim3(kProdThreads);
+        cfg.dynamicSmemBytes = size_t(smem);
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0) return blocks;
+        cudaGetLastError();
+    }
+    return 0;
+}
+
 template <class T, int W, Form H>
-rr_status launch_moe(const MoeArgs& a, int smem, int dev, cudaStream_t stream) {
+rr_status launch_moe(MoeArgs a, int smem, int dev, cudaStream_t stream) {
     static std::atomic<uint32_t> ready{0};
+    static std::atomic<int> clusters[kMaxDevices] = {};        // largest_cluster + 1, once asked
     RR_CUDA(allow_smem(rr_moe_kernel<T, W, H>, kSmem - 1024, dev, &ready));
+    int most = clusters[dev].load(std::memory_order_relaxed) - 1;
+    if (most < 0) {
+        // More than 8 blocks are asked for by name.
+        RR_CUDA(cudaFuncSetAttribute(rr_moe_kernel<T, W, H>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        most = largest_cluster(rr_moe_kernel<T, W, H>, smem);
+        clusters[dev].store(most + 1, std::memory_order_relaxed);
+    }
+    a.one = rr_moe_cluster(std::min<int64_t>(int64_t(a.tokens) * a.top_k, a.n_local) * (a.m13_bytes + a.m2_bytes) +
+                               int64_t(a.n_experts) * a.hidden * 2 * ((a.tokens + 15) / 16),
+                           most);
     if (a.one) {
         const unsigned blocks = unsigned(a.one);
-        static std::atomic<uint32_t> large{0};     // more than 8 blocks are asked for by name
-        if (blocks > 8 && !(large.load(std::memory_order_relaxed) >> dev & 1)) {
-            RR_CUDA(cudaFuncSetAttribute(rr_moe_kernel<T, W, H>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-            large.fetch_or(1u << dev, std::memory_order_relaxed);
-        }
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -2028,7 +2044,7 @@ rr_status launch_moe(const MoeArgs& a, int smem, int dev, cudaStream_t stream) {
     }
     // (Programmatic dependent launch besides left the gap between two launches at
     // the same 4 us.)
-    void* args[] = {const_cast<MoeArgs*>(&a)};
+    void* args[] = {&a};
     RR_CUDA(cudaLaunchCooperativeKernel((const void*)rr_moe_kernel<T, W, H>, dim3(unsigned(grid)), dim3(kProdThreads), args,
                                         size_t(smem), stream));
     return RR_OK;
