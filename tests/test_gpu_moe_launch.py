@@ -1,6 +1,7 @@
 """How a mixture-of-experts layer is launched: in one cluster or on every SM, the mark
-that a wait which ran out leaves, and workspaces."""
+that a wait which ran out leaves, workspaces, and calls that overlap in time."""
 import ctypes
+import threading
 
 import pytest
 import torch
@@ -107,3 +108,90 @@ def test_a_workspace_is_ready_when_it_is_there():
     torch.cuda.synchronize()
     rr.rr_moe(layer, x, out, ws, stream=side)
     rr.rr_moe_check(layer, ws, side)
+
+
+def product_of(seed, rows, cols):
+    gen = torch.Generator("cuda").manual_seed(seed)
+    q = rr.Quantized(rows, cols, 128)
+    rr.rr_quantize(q, (torch.randn(rows, cols, device="cuda", generator=gen) * 0.05).bfloat16())
+    return q
+
+
+def test_layers_on_every_sm_at_once():
+    """Layers that fill every SM, on two streams, beside products and quantisations on
+    a third: the results of calls one after another, and no wait that runs out."""
+    layer, _, _, _ = layer_of(11, 16, 512, 512, 4)
+    xs = [tokens_of(n, n, 512) for n in (3, 20)]
+    spaces = [rr.MoeWorkspace(layer, 20) for _ in xs]
+    want = [torch.empty_like(x) for x in xs]
+    for x, ws, w in zip(xs, spaces, want):
+        rr.rr_moe(layer, x, w, ws)
+        rr.rr_moe_check(layer, ws)
+    assert blocks_of(layer, 3) == blocks_of(layer, 20) == torch.cuda.get_device_properties(0).multi_processor_count
+    q = product_of(1, 6144, 4096)
+    token = torch.randn(2, 4096, device="cuda").bfloat16()
+    product = torch.empty(2, 6144, device="cuda")
+    rr.rr_matvec(q, token, product)
+    raw = (torch.randn(512, 512, device="cuda") * 0.05).bfloat16()
+    small = rr.Quantized(512, 512, 64)
+    rr.rr_quantize(small, raw)
+    packed, again = small.data.clone(), rr.Quantized(512, 512, 64)
+    outs = [[torch.full_like(w, 9.0) for _ in range(50)] for w in want]
+    products = [torch.full_like(product, 9.0) for _ in range(50)]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for s in streams:              # until every call is queued
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(40_000_000)
+    for i in range(50):
+        for k in range(2):
+            rr.rr_moe(layer, xs[k], outs[k][i], spaces[k], stream=streams[k])
+        rr.rr_matvec(q, token, products[i], stream=streams[2])
+        rr.rr_quantize(again, raw, stream=streams[2])
+    torch.cuda.synchronize()
+    for k in range(2):
+        rr.rr_moe_check(layer, spaces[k])
+        assert all(torch.equal(o, want[k]) for o in outs[k])
+    assert all(torch.equal(p, product) for p in products) and torch.equal(again.data, packed)
+
+
+@pytest.mark.parametrize("inter", [32, 512])
+def test_layers_and_products_from_several_threads(inter):
+    """Four host threads, each with its own stream, workspace and outputs (32: in one
+    cluster; 512: on every SM)."""
+    layer, _, _, _ = layer_of(13, 8, 512, inter, 2)
+    q = product_of(2, 2048, 512)
+    xs = [tokens_of(30 + n, n, 512) for n in (1, 2, 9, 20)]
+    want = []
+    for x in xs:
+        ws, out, product = rr.MoeWorkspace(layer, 20), torch.empty_like(x), torch.empty(min(16, len(x)), 2048, device="cuda")
+        rr.rr_moe(layer, x, out, ws)
+        rr.rr_matvec(q, x[:16], product)
+        rr.rr_moe_check(layer, ws)
+        want.append((out, product))
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(k):
+        try:
+            stream, x = torch.cuda.Stream(), xs[k]
+            ws, out, product = rr.MoeWorkspace(layer, 20), torch.empty_like(x), torch.empty_like(want[k][1])
+            torch.cuda.current_stream().synchronize()
+            for _ in range(40):
+                with torch.cuda.stream(stream):
+                    out.fill_(9.0)
+                    product.fill_(9.0)
+                rr.rr_moe(layer, x, out, ws, stream=stream)
+                rr.rr_matvec(q, x[:16], product, stream=stream)
+                stream.synchronize()
+                assert torch.equal(out, want[k][0]) and torch.equal(product, want[k][1])
+            rr.rr_moe_check(layer, ws, stream)
+        except BaseException as e:
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
