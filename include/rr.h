@@ -614,7 +614,8 @@ rr_status rr_plan_selftest_wait(const rr_plan* plan, cudaStream_t stream);
  *   2 (g * (128 / group) + i) + h of the scales. */
 typedef struct {
     int64_t rows, cols;   /* of one matrix; 1 .. 2^31 - 1 rows, 1 .. 2^18 columns        */
-    int32_t count;        /* matrices in the stack (a layer's experts), 1 .. 65535       */
+    int32_t count;        /* matrices in the stack (a layer's experts), 1 .. 65535; at   */
+                          /* most 2^31 - 1 blocks (below) in all                         */
     int32_t group;        /* columns that share a scale: 32, 64 or 128                   */
     int32_t dtype;        /* rr_dst_dtype of the elements, scales, tokens and outputs    */
     int32_t pair;         /* 1: rows are [gate; up] (an even number), as above; else 0   */

@@ -1847,6 +1847,17 @@ cudaError_t allow_smem(K* kernel, int smem, int dev, std::atomic<uint32_t>* done
     return e;
 }
 
+Packed packed_of(int64_t rows, int64_t cols, int group, int pair) {
+    Packed m;
+    m.rows = rows;
+    m.cols = cols;
+    m.strips = pair ? (rows / 2 + 7) / 8 : (rows + 15) / 16;
+    m.blocks = (cols + kBlock - 1) / kBlock;
+    m.matrix_bytes = m.strips * m.blocks * block_bytes(group ? group : 128);
+    m.pair = pair;
+    return m;
+}
+
 rr_status check_quant(const rr_quant* q) {
     if (!q) return rr_fail(RR_EINVAL, "matrix description is NULL");
     if (q->rows < 1 || q->rows > INT32_MAX || q->cols < 1 || q->cols > kMaxCols)
@@ -1859,18 +1870,12 @@ rr_status check_quant(const rr_quant* q) {
         return rr_fail(RR_EINVAL, "unknown element type %d", q->dtype);
     if (q->pair != 0 && q->pair != 1) return rr_fail(RR_EINVAL, "pair is 0 or 1, not %d", q->pair);
     if (q->pair && q->rows % 2) return rr_fail(RR_ELAYOUT, "paired rows are an even number, not %lld", (long long)q->rows);
+    // The kernels number a stack's blocks in 32 bits; its bytes then fit 64.
+    const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
+    if (m.strips * m.blocks * q->count > INT32_MAX)
+        return rr_fail(RR_ELAYOUT, "%d matrices of %lld x %lld: at most 2^31 - 1 blocks of 16 x 128", q->count,
+                       (long long)q->rows, (long long)q->cols);
     return RR_OK;
-}
-
-Packed packed_of(int64_t rows, int64_t cols, int group, int pair) {
-    Packed m;
-    m.rows = rows;
-    m.cols = cols;
-    m.strips = pair ? (rows / 2 + 7) / 8 : (rows + 15) / 16;
-    m.blocks = (cols + kBlock - 1) / kBlock;
-    m.matrix_bytes = m.strips * m.blocks * block_bytes(group ? group : 128);
-    m.pair = pair;
-    return m;
 }
 
 // Calls f with the element type and the group as template arguments.
@@ -2063,15 +2068,6 @@ extern "C" rr_status rr_quant_bytes(const rr_quant* q, int64_t* matrix_bytes, in
 
 namespace {
 
-// Eight warps to a block, one item each.
-rr_status grid_of(const Packed& m, int32_t count, uint32_t* total, unsigned* grid) {
-    const int64_t n = m.strips * m.blocks * count;
-    if (n > INT32_MAX) return rr_fail(RR_ELAYOUT, "the stack is too large for one call");
-    *total = uint32_t(n);
-    *grid = unsigned((n + 7) / 8);
-    return RR_OK;
-}
-
 template <class... Params, class... Args>
 cudaError_t launch_after(void (*kernel)(Params...), unsigned grid, int threads, cudaStream_t stream, Args... args) {
     cudaLaunchAttribute attr[1];
@@ -2099,9 +2095,9 @@ extern "C" rr_status rr_quantize(const rr_quant* q, const void* w, int64_t ld, v
     RR_TRY(check_device(dev, w, 2, "w"));
     RR_TRY(check_device(dev, packed, 16, "packed"));
     const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
-    uint32_t total;
-    unsigned grid;
-    RR_TRY(grid_of(m, q->count, &total, &grid));
+    // Eight warps to a block, one item each.
+    const uint32_t total = uint32_t(m.strips * m.blocks * q->count);
+    const unsigned grid = (total + 7) / 8;
     const bool vec = (uintptr_t)w % 16 == 0 && ld % 8 == 0;
     return with_group(q->dtype, q->group, [&](auto t, auto g) -> rr_status {
         using T = decltype(t);
@@ -2126,9 +2122,9 @@ extern "C" rr_status rr_dequantize(const rr_quant* q, const void* packed, void* 
     RR_TRY(check_device(dev, packed, 16, "packed"));
     RR_TRY(check_device(dev, w, f32 ? 4 : 2, "w"));
     const Packed m = packed_of(q->rows, q->cols, q->group, q->pair);
-    uint32_t total;
-    unsigned grid;
-    RR_TRY(grid_of(m, q->count, &total, &grid));
+    // Eight warps to a block, one item each.
+    const uint32_t total = uint32_t(m.strips * m.blocks * q->count);
+    const unsigned grid = (total + 7) / 8;
     const bool vec = (uintptr_t)w % 16 == 0 && ld % (f32 ? 4 : 8) == 0;
     return with_group(q->dtype, q->group, [&](auto t, auto g) -> rr_status {
         using T = decltype(t);
