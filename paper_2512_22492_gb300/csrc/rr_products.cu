@@ -849,7 +849,11 @@ template <> struct Weights<32> : PackedWeights<32> {};
 template <> struct Weights<64> : PackedWeights<64> {};
 template <> struct Weights<128> : PackedWeights<128> {};
 
-// sum += W x over one block.  low (16-bit weights): of the second and third parts of an
+// sum += W x over one block.  Of 16-bit weights, a block's 64 columns are summed from
+// zero and then added: a matrix instruction cuts its sum off, towards zero, and a chain
+// of them over a row drifts by 2^-24 a step (2048 x 768, 32 tokens: 0.15% of the outputs
+// one step off so, 0.015% as it is, 0.026% with float32 sums elsewhere; 64 tokens 222 ->
+// 226 us, one token 30.9 -> 31.9).  low: of the second and third parts of an
 // element, whose sums, 2^-8 of the others, then lose nothing beside them.  Where the
 // first parts' sum is infinite or NaN it is the result: a part of zero times an infinite
 // weight would make NaN of what is infinite (join_low).
@@ -860,29 +864,35 @@ __device__ __forceinline__ void moe_block(float (&sum)[NT][4], float (&low)[NT][
     if constexpr (W >= 32) {
         block_product<T, W, NT, FORM>(sum, stage, x, at, lane, apart, inf);
     } else {
+        float part[NT][4];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const uint4 l = Weights<W>::read(stage, 0, j, shift_lo, lane);
             const uint4 h = Weights<W>::read(stage, 1, j, shift_hi, lane);
+            const auto add = [&](int n, int p, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
+                if (p == 0 && j == 0) mma_first<T>(part[n], l.x, h.x, l.y, h.y, x0, x1);
+                else mma<T>(p ? low[n] : part[n], l.x, h.x, l.y, h.y, x0, x1);
+                mma<T>(p ? low[n] : part[n], l.z, h.z, l.w, h.w, x2, x3);
+            };
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 if constexpr (FORM == kFloats) {
                     const Parts v(x[n] + at + 64 * j, apart, inf);
 #pragma unroll
-                    for (int p = 0; p < 3; ++p) {
-                        mma<T>(p ? low[n] : sum[n], l.x, h.x, l.y, h.y, v.w[p][0], v.w[p][1]);
-                        mma<T>(p ? low[n] : sum[n], l.z, h.z, l.w, h.w, v.w[p][2], v.w[p][3]);
-                    }
+                    for (int p = 0; p < 3; ++p) add(n, p, v.w[p][0], v.w[p][1], v.w[p][2], v.w[p][3]);
                 } else {
 #pragma unroll
                     for (int p = 0; p < FORM; ++p) {
                         const uint4 v = *reinterpret_cast<const uint4*>(x[n] + p * apart + at + 64 * j);
-                        mma<T>(p ? low[n] : sum[n], l.x, h.x, l.y, h.y, v.x, v.y);
-                        mma<T>(p ? low[n] : sum[n], l.z, h.z, l.w, h.w, v.z, v.w);
+                        add(n, p, v.x, v.y, v.z, v.w);
                     }
                 }
             }
         }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[n][k] += part[n][k];
     }
 }
 
