@@ -1980,16 +1980,19 @@ rr_status prepare_moe(MoeArgs a, int dev, cudaStream_t stream) {
         moe_rows(&a, room, kHalves);
         return launch_moe<T, W, kHalves>(a, smem, dev, stream);
     } else {
-        // In three parts (Qwen3-30B-A3B, 64 tokens: 230 us, in float32 260; two parts, which
-        // do not hold all of h, 217) where a pass holds as many tokens so, or twice an
-        // expert's mean, but for float32's less room in the second phase without a third
-        // barrier.  (16 experts of 2048 x 4096, 8 tokens, 3 against 4 a pass: 113 and 131 us;
-        // 64 tokens 350 and 316; 8 of 4096 x 8192, 64 tokens, 1 against 2: 3551 and 2052.)
+        // In three parts (Qwen3-30B-A3B, 64 tokens: 234 us, in float32 260; two parts, which
+        // do not hold all of h, 217) where a pass holds as many tokens so, or seven of them
+        // (16 experts of 1024 x 1000, 64 tokens, 8 against 16 a pass: 63 and 68 us), or twice
+        // an expert's mean.  (16 of 2048 x 4096, 8 tokens, 3 against 4 a pass: 120 and 122 us;
+        // 64 tokens 383 and 314; 8 of 4096 x 8192, 64 tokens, 1 against 2: 3527 and 1890.)
+        // That float32's two planes leave more calls without a third barrier weighs less:
+        // one token of 32 experts of 2880 x 2880 57 us in parts, 64 in float32.
         MoeArgs parts = a;
         moe_rows(&a, room, kFloats);
         moe_rows(&parts, room, kThirds);
-        const bool enough = parts.cap == a.cap || int64_t(parts.cap) * a.n_experts >= 2 * int64_t(a.tokens) * a.top_k;
-        if (parts.cap >= 1 && enough && parts.fold == a.fold) return launch_moe<T, W, kThirds>(parts, smem, dev, stream);
+        const bool enough = parts.cap >= std::min(a.cap, 7) ||
+                            int64_t(parts.cap) * a.n_experts >= 2 * int64_t(a.tokens) * a.top_k;
+        if (parts.cap >= 1 && enough) return launch_moe<T, W, kThirds>(parts, smem, dev, stream);
         return launch_moe<T, W, kFloats>(a, smem, dev, stream);
     }
 }
