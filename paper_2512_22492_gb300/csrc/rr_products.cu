@@ -361,7 +361,9 @@ __device__ __forceinline__ void mma_first(float (&c)[4], uint32_t a0, uint32_t a
 //   multiplication by 2^123 or 2^119 brings either code to c 2^-10.  A group's 128
 //   products of codes up to 7 2^-10 then stay below the largest element, and no sum
 //   overflows that the result does not; results are multiplied by kUp = 2^10 at the end.
-//   float16: under the exponent of 1024 they read 1024 + c and 1024 + 16 c.
+//   float16: under the exponent of 1024 they read 1024 + c and 1024 + 16 c (a published
+//   conversion: Kim, Henry, Fahim, Awadalla, "Who Says Elephants Can't Run: Bringing Large
+//   Scale MoE Models into Cloud Scale Production", 2022).
 template <class T>
 struct Codes {
     static constexpr float kUp = std::is_same<T, BF16>::value ? 1024.0f : 1.0f;
@@ -574,9 +576,9 @@ __device__ __forceinline__ int share_of(int p, int total) { return int((kWarps *
 // the end, and a cluster's sums through its blocks' shared memory after each
 // `batch` of strips.  ST: blocks in flight.
 // Bound by unpacking codes where there is much to read, by launch, first loads and
-// join (4 us) where there is little.  On the GPU: 151936 x 4096, one token 55.7 us (5.8
-// TB/s), eight 57.7; 24576 x 4096, four 13.8 us; 5120 x 25600, eight 18.5 us; 6144 x
-// 4096, one 5.7 us.  Even shares, rather than whole strips to teams of warps: 24.0 ->
+// join (4 us) where there is little.  On the GPU: 151936 x 4096, one token 54.5 us (5.9
+// TB/s), eight 57.0; 24576 x 4096, four 13.6 us; 5120 x 25600, eight 18.4 us; 6144 x
+// 4096, one 5.6 us.  Even shares, rather than whole strips to teams of warps: 24.0 ->
 // 18.5 us for 5120 x 25600, whose 320 strips divide badly, 54.5 -> 55.7 for the largest.
 template <class T, int G, int NT, int U, int ST>
 __global__ void __launch_bounds__(kProdThreads, 1) rr_matvec_kernel(const __grid_constant__ MatvecArgs a) {
@@ -1606,11 +1608,14 @@ constexpr int kPrefetch = 8;       // strips of the second phase that a block as
 //   gate and up of every chosen expert, silu               | barrier
 //   down, and for few tokens the weighted sum at once; else | barrier
 //   each token's weighted sum
-// Bound by HBM where there is much to read (Qwen3-30B-A3B: 64 tokens 1.19 GB in 218 us
-// a call, of which gate and up run at 6.3 TB/s and down at 6.0), by the chain of
-// phases where there is little (one token 76 MB in 33 us, of which 17 us are those two
-// phases, 9 us the phases before them and 4 us the gap between two launches).
-// Each chosen expert's weights are read once per 16 tokens.  Blocks take equal runs of
+// Bound by HBM where there is much to read (Qwen3-30B-A3B: 64 tokens 1.2 GB in 226 to 234
+// us a call, of which gate and up run at 6.3 TB/s and down at 6.2, its last block 12 us
+// behind the mean), by the chain of phases where there is little (one token 76 MB in 32
+// us, of which 16.5 us are those two phases, 3 us the barrier between them, 7.5 us the
+// phases before and 4 us the gap between two launches).
+// Each chosen expert's weights are read once per pass of `cap` of its tokens: 16, or as
+// many as have room in shared memory (2048 x 768: 16, 4096 x 1536: 8, 7168 x 2048: 5, 4096
+// x 14336: 1), the rest from L2 where it still holds them.  Blocks take equal runs of
 // (pass, strip of 16 rows) items; warps stream weights through stages that already
 // fill with the next phase's while the blocks wait.
 template <class T, int W, Form H>
