@@ -324,7 +324,6 @@ def prepare(case, seed):
         s.accepted, s.rejected = (torch.empty(c.seqs, dtype=torch.int32, device="cuda")
                                   for _ in range(2))
         s.tokens = torch.empty(rows, dtype=torch.int32, device="cuda")
-        s.workspace = rr.AcceptWorkspace(c.seqs, c.vocab)
         return s
     s.cache = rr.Cache(c.layers, c.n_kv, c.dim, s.n_pages, s.max_seqs, s.max_pages,
                        page_tokens=c.page, dtype=c.dtype, pages=s.pages)
@@ -350,8 +349,8 @@ def prepare(case, seed):
 def _run_own(s):
     c, rr = s.c, s.rr
     if c.op == "accept":
-        rr.rr_accept(s.p, s.drafts, s.u, s.v, s.accepted, s.tokens, s.workspace, q=s.q,
-                     starts=s.starts, rejected=s.rejected)
+        rr.rr_accept(s.p, s.drafts, s.u, s.v, s.accepted, s.tokens, q=s.q, starts=s.starts,
+                     rejected=s.rejected)
         return {"accepted": s.accepted, "tokens": s.tokens, "rejected": s.rejected}
     if c.op == "attend":
         rr.rr_attend(s.cache, s.layer, s.q, s.out, s.seqs, s.workspace, starts=s.starts, lse=s.lse)
