@@ -695,6 +695,132 @@ rr_status rr_moe(const rr_moe_layer* layer, const void* router, const void* w13,
 rr_status rr_moe_check(const rr_moe_layer* layer, int32_t max_tokens, void* workspace,
                        cudaStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * The rollout's key-value cache in pages, attention over it, and drafted tokens.
+ *
+ * What a rollout's token step needs beside the products above.  No counterpart in the
+ * paper, whose rollouts run an inference engine of their own (Section 7.1).
+ * rr_cache_fork gives the samples of one prompt its pages to share; a step takes
+ * pages for its tokens (rr_cache_extend), and each layer writes its keys and values
+ * (rr_cache_append) and attends (rr_attend).  rr_accept holds drafted tokens, of a
+ * rollout that still has the weights of before the sync for instance, against the
+ * model's probabilities; rr_cache_truncate takes refused tokens back, and gives up the
+ * pages of a finished sequence; rr_cache_compact moves the pages in use together.
+ *
+ * As for the products: stream-ordered and asynchronous, no allocation, may be captured
+ * into a CUDA graph (rr_cache_check apart, which blocks); argument errors come back at once and
+ * nothing is launched.  Memory is this GPU's; `pages`, `book` and workspaces are 16-byte
+ * aligned, all else to its elements.  Calls on one cache that write its book (all but
+ * rr_cache_append and rr_attend) must not overlap with any other call on it;
+ * rr_cache_append must not with one that reads or writes the same layer.  Every call gives the
+ * same bits each time.
+ *
+ * Lists (sequences, counts, starts) are on the device, where the host does not see
+ * what they hold.  A call that finds a number out of range, a sequence listed twice or
+ * the pool without room leaves the cache as it was and marks it; later calls then leave
+ * all as it is, until rr_cache_check has reported the mark.  rr_cache_append and rr_attend
+ * leave out what does not fit, and mark the cache likewise.
+ * ------------------------------------------------------------------------- */
+
+/* The cache's shape.
+ *   pages: n_pages of [layers, 2, n_kv, page_tokens, pitch] 16-bit elements, keys before
+ *     values; pitch is dim rounded up to a multiple of 8 (what lies behind dim is
+ *     written as 0 and never looked at).
+ *   book: 32-bit integers.  64 of the calls' own; then, each part beginning at a multiple of 4,
+ *     the table [max_seqs, max_pages] (page numbers of a sequence's tokens in order: entry j holds
+ *     tokens j * page_tokens on; behind the last page -1), lengths [max_seqs] (tokens), refs
+ *     [n_pages] (how many sequences hold the page; 0: free); then more of the calls' own.  A copy of a
+ *     book, put back, is the cache of then, as far as pages were not written since. */
+typedef struct {
+    int32_t layers, n_kv, dim;                /* 1 .. 1024, 1 .. 1024, 1 .. 256          */
+    int32_t page_tokens;                      /* 8, 16, 32, 64 or 128                    */
+    int32_t n_pages, max_seqs, max_pages;     /* 1 .. 2^26, 1 .. 65536; max_pages *      */
+                                              /* page_tokens up to 2^30                  */
+    int32_t dtype;                            /* rr_dst_dtype                            */
+} rr_cache;
+
+/* Bytes of one page, its pitch in elements, and bytes of the book.  Any may be NULL. */
+rr_status rr_cache_bytes(const rr_cache* cache, int64_t* page_bytes, int64_t* pitch,
+                         int64_t* book_bytes);
+
+/* Makes a book that of an empty cache.  The first call on a book. */
+rr_status rr_cache_clear(const rr_cache* cache, void* book, cudaStream_t stream);
+
+/* children[i] (0 tokens) comes to hold the tokens of parents[i], in the same pages, i <
+ * n.  No child is listed twice or is a parent as well; a parent may be several times. */
+rr_status rr_cache_fork(const rr_cache* cache, void* book, const int32_t* parents,
+                        const int32_t* children, int32_t n, cudaStream_t stream);
+
+/* Room for starts[i + 1] - starts[i] (starts NULL: one) new tokens of seqs[i], i < n: its length
+ * grows by so many.  A page that is partly filled and that others hold too is
+ * first replaced by a copy, by each listed sequence that gets tokens; where these are all
+ * of its holders, the last of them keeps the page itself.  Pages are taken from the
+ * pool's free ones in ascending order: sequence by sequence as listed, the copy before the
+ * new pages. */
+rr_status rr_cache_extend(const rr_cache* cache, void* pages, void* book, const int32_t* seqs,
+                          const int32_t* starts, int32_t n, cudaStream_t stream);
+
+/* One layer's keys and values of new tokens: `rows` rows of n_kv * dim elements.  Rows
+ * starts[i] .. starts[i + 1] - 1 are the last tokens of seqs[i]; with starts NULL, row i
+ * is the last one of seqs[i], and rows is n.  Rows of no sequence are left out. */
+rr_status rr_cache_append(const rr_cache* cache, void* pages, void* book, int32_t layer,
+                          const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t rows,
+                          const int32_t* seqs, const int32_t* starts, int32_t n,
+                          cudaStream_t stream);
+
+/* Takes the last drop[i] tokens of seqs[i] back (drop NULL: all of them); pages without a
+ * token left are given up. */
+rr_status rr_cache_truncate(const rr_cache* cache, void* book, const int32_t* seqs,
+                            const int32_t* drop, int32_t n, cudaStream_t stream);
+
+/* Moves pages so that the pages in use, U of them, are 0 .. U - 1: the k-th free page below U
+ * receives the k-th page in use at or above U.  Tables and refs follow. */
+rr_status rr_cache_compact(const rr_cache* cache, void* pages, void* book, cudaStream_t stream);
+
+/* Waits for `stream`, then reports (and clears) the cache's mark: RR_EINVAL if a call left
+ * something undone, else RR_OK. */
+rr_status rr_cache_check(const rr_cache* cache, void* book, cudaStream_t stream);
+
+/* Attention of new tokens, whose keys and values are in the cache.  Rows as for
+ * rr_cache_append; a row is n_q heads of dim elements, and head h goes with key head
+ * h / (n_q / n_kv).  Row j (of m) of a sequence of L tokens sees its tokens t < L - m + 1 + j:
+ *   s_t = scale q . k_t,   lse = ln sum_t exp(s_t),   out = sum_t exp(s_t - lse) v_t.
+ * A row that sees no token has out 0 and lse -infinity, as has one whose scores are all
+ * -infinity.  Tokens that a row does not see do not touch it, whatever they hold.
+ * Scores and sums are float32; the weights exp(s_t - max) enter the product with the
+ * values as two bfloat16 parts (to 2^-16 of themselves) or as float16 (2^-11, or 2^-32 of
+ * the largest); the result is rounded once.  Which keys are summed together depends on the
+ * call's lengths: beside other sequences a row's last bits may be others.
+ *   lse: rows x n_q floats, or NULL.  Rows of no listed sequence are left as they are.
+ *   workspace: rr_attend_workspace's bytes, zero before its first call; every call
+ *     leaves it ready for the next, of the same head size.  Calls that overlap in time need distinct ones.
+ * out must not overlap with q. */
+rr_status rr_attend_workspace(const rr_cache* cache, int32_t n_q, int64_t* bytes);
+rr_status rr_attend(const rr_cache* cache, const void* pages, void* book, int32_t layer,
+                    const void* q, int64_t ldq, int32_t n_q, int32_t rows, void* out, int64_t ldo,
+                    float* lse, const int32_t* seqs, const int32_t* starts, int32_t n, float scale,
+                    void* workspace, int64_t workspace_bytes, cudaStream_t stream);
+
+/* Drafted tokens of n sequences.  Rows starts[i] .. starts[i + 1] - 1 of p and q (rows x
+ * vocab probabilities; 1 .. 2^20 tokens), of drafts and of u belong to sequence i: one for each draft,
+ * and one more, whose draft and u are not looked at (starts NULL: every row is a sequence without
+ * drafts; drafts and u may then be NULL).
+ *   Draft x in row r is accepted if all before it were and u[r] q[r][x] < p[r][x] (exact
+ *   products), refused otherwise (NaN, and x outside the vocabulary, included).  q NULL:
+ *   the drafts are sure, q[r][x] is 1.
+ *   The next token follows the accepted ones, from its row of p, or, where a draft x was
+ *   refused, from max(p - q, 0) (float32; q NULL: p without x), or, if that is all 0, p.  In
+ *   whole numbers of 2^-42 (values clamped to 0 .. 1, ties to even, NaN as 0), with T their sum, it is
+ *   the first token whose sum with those before it is above floor(T v'), v' = v[i] in whole
+ *   numbers of 2^-31, 0 .. 1 - 2^-31; -1 if T is 0.  So p and q may differ from exact probabilities, and
+ *   the same numbers give the same token anywhere.
+ * accepted[i], rejected[i] (or NULL): how many drafts were; accepted -1, and no token, where starts
+ * do not fit.  tokens[r]: the accepted drafts, the next token, then -1. */
+rr_status rr_accept(const float* p, int64_t ldp, const float* q, int64_t ldq,
+                    const int32_t* drafts, const int32_t* starts, const float* u, const float* v,
+                    int32_t rows, int32_t n, int32_t vocab, int32_t* accepted, int32_t* tokens,
+                    int32_t* rejected, cudaStream_t stream);
+
 /* A static description of a status code ("RR_OK", "RR_EINVAL: invalid
  * argument", ...; "unknown rr_status" otherwise), and this thread's
  * description of its most recent failure ("" if none).  The

@@ -15,6 +15,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(HERE, "_build")
+KERNELS = ("rr_device.cu", "rr_products.cu", "rr_cache.cu", "rr_attend.cu")
 LIB = os.path.join(HERE, "librr.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -31,9 +32,8 @@ def _cuda_home() -> str:
 
 
 def _sources():
-    return [os.path.join(CSRC, f) for f in ("rr_plan.cpp", "rr_device.cu", "rr_products.cu",
-                                             "rr_internal.h")] + \
-        [os.path.join(INCLUDE, "rr.h")]
+    return [os.path.join(CSRC, f) for f in ("rr_plan.cpp",) + KERNELS +
+            ("rr_internal.h", "rr_kernels.cuh", "rr_cache.cuh")] + [os.path.join(INCLUDE, "rr.h")]
 
 
 def stale() -> bool:
@@ -53,17 +53,14 @@ def build(force: bool = False, verbose: bool = False) -> str:
         nvcc = "nvcc"
     inc = ["-I", INCLUDE, "-I", CSRC, "-I", os.path.join(cuda, "include")]
     plan_o = os.path.join(BUILD, "rr_plan.o")
-    dev_o = os.path.join(BUILD, "rr_device.o")
-    prod_o = os.path.join(BUILD, "rr_products.o")
+    objects = [os.path.join(BUILD, f.replace(".cu", ".o")) for f in KERNELS]
     device = [nvcc, "-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xptxas", "-v"] + \
         ARCH + os.environ.get("RR_EXTRA_NVCC_FLAGS", "").split()
     jobs = [
         ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall"] +
         os.environ.get("RR_EXTRA_CXX_FLAGS", "").split() +
         ["-c", os.path.join(CSRC, "rr_plan.cpp"), "-o", plan_o] + inc,
-        device + ["-c", os.path.join(CSRC, "rr_device.cu"), "-o", dev_o] + inc,
-        device + ["-c", os.path.join(CSRC, "rr_products.cu"), "-o", prod_o] + inc,
-    ]
+    ] + [device + ["-c", os.path.join(CSRC, f), "-o", o] + inc for f, o in zip(KERNELS, objects)]
     procs = [subprocess.Popen(j, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
              for j in jobs]
     logs = []
@@ -73,11 +70,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if p.returncode != 0:
             raise RuntimeError(f"build failed: {' '.join(j)}\n{out}")
     with open(os.path.join(BUILD, "ptxas.log"), "w") as f:
-        f.write(logs[1] + logs[2])
+        f.write("".join(logs[1:]))
     if verbose:
-        print(logs[1] + logs[2])
+        print("".join(logs[1:]))
     tmp = LIB + ".tmp"
-    subprocess.check_call([nvcc, "-shared"] + ARCH + [plan_o, dev_o, prod_o, "-o", tmp])
+    subprocess.check_call([nvcc, "-shared"] + ARCH + [plan_o] + objects + ["-o", tmp])
     os.replace(tmp, LIB)
     return LIB
 

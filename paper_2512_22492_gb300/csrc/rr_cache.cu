@@ -1,0 +1,949 @@
+// The rollout's key-value cache in pages (fork, extend, append, truncate, compact) and the
+// verification of drafted tokens, for GB300 (sm_103a); include/rr.h has the definitions.
+#include <algorithm>
+#include <climits>
+
+#include "rr_cache.cuh"
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// Bookkeeping
+// ---------------------------------------------------------------------------
+//
+// Each of these calls reads short lists and tables and writes some entries: a chain of a
+// few dependent loads, whose latency is the cost, so that few launches and few barriers
+// are what counts.  One cluster of 1 or 8 blocks does a call; its barriers are the
+// hardware's.  Every block checks the whole of the call's lists by itself, and nothing
+// is written before all of them have (a call that fails leaves the cache as it was).
+
+constexpr int kBookThreads = 512;
+constexpr int kBookWarps = kBookThreads / 32;
+constexpr int kBookRanks = 8;
+
+__device__ __forceinline__ int cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return int(r);
+}
+__device__ __forceinline__ int cluster_size() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return int(r);
+}
+// Everything that the cluster's threads wrote before is seen by all of them after.
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+
+struct Ranks {
+    int rank, size;
+    __device__ __forceinline__ Ranks() : rank(cluster_rank()), size(cluster_size()) {}
+    // This block's part of n things, in order.
+    __device__ __forceinline__ int64_t first(int64_t n) const { return n * rank / size; }
+    __device__ __forceinline__ int64_t end(int64_t n) const { return n * (rank + 1) / size; }
+    // This thread's or warp's number among the cluster's, and how many there are.
+    __device__ __forceinline__ int thread() const { return rank * kBookThreads + int(threadIdx.x); }
+    __device__ __forceinline__ int threads() const { return size * kBookThreads; }
+    __device__ __forceinline__ int warp() const { return rank * kBookWarps + int(threadIdx.x >> 5); }
+    __device__ __forceinline__ int warps() const { return size * kBookWarps; }
+};
+
+// One bit for each sequence of the cache, in shared memory.
+struct Listed {
+    uint32_t* bits;
+    __device__ __forceinline__ Listed(uint32_t* shared, int max_seqs) : bits(shared) {
+        for (int i = threadIdx.x; i < (max_seqs + 31) / 32; i += kBookThreads) bits[i] = 0;
+        __syncthreads();
+    }
+    __device__ __forceinline__ bool add(int s) { return atomicOr(&bits[s >> 5], 1u << (s & 31)) >> (s & 31) & 1; }
+    __device__ __forceinline__ bool has(int s) const { return bits[s >> 5] >> (s & 31) & 1; }
+};
+
+// The block's OR of bad, the same in all of its threads.
+__device__ __forceinline__ int agree(int bad) {
+    __shared__ int all;
+    if (threadIdx.x == 0) all = 0;
+    __syncthreads();
+    bad = __reduce_or_sync(~0u, bad);
+    if (bad && (threadIdx.x & 31) == 0) atomicOr(&all, bad);
+    __syncthreads();
+    const int r = all;
+    __syncthreads();
+    return r;
+}
+
+// Exclusive sum of v over the block's threads; *total: of all of them.
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* total) {
+    __shared__ int64_t part[kBookWarps];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    int64_t s = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t o = __shfl_up_sync(~0u, s, d);
+        if (lane >= d) s += o;
+    }
+    if (lane == 31) part[w] = s;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < kBookWarps; ++i) {
+        if (i < w) before += part[i];
+        all += part[i];
+    }
+    __syncthreads();
+    *total = all;
+    return before + s - v;
+}
+
+// Sums over the cluster's blocks, from what each put into b.sums[k * kBookRanks + rank]
+// before a barrier: of the ranks before this one, and of all.
+__device__ __forceinline__ int64_t rank_sum(const Book& b, const Ranks& r, int k, int64_t* total) {
+    int64_t before = 0, all = 0;
+    for (int i = 0; i < r.size; ++i) {
+        const int64_t v = __ldcg(&b.sums[k * kBookRanks + i]);
+        if (i < r.rank) before += v;
+        all += v;
+    }
+    *total = all;
+    return before;
+}
+
+// Four pages' holders from page p on (a multiple of 4); pages from `end` on count as held.
+__device__ __forceinline__ int4 four(const int32_t* refs, int64_t p, int64_t end) {
+    int4 v = make_int4(1, 1, 1, 1);
+    if (p + 3 < end) return __ldcg(reinterpret_cast<const int4*>(refs + p));
+    if (p < end) v.x = __ldcg(refs + p);
+    if (p + 1 < end) v.y = __ldcg(refs + p + 1);
+    if (p + 2 < end) v.z = __ldcg(refs + p + 2);
+    return v;
+}
+__device__ __forceinline__ int zeros(const int4& v) { return (v.x == 0) + (v.y == 0) + (v.z == 0) + (v.w == 0); }
+
+// A rank's pages: whole fours, so that vectors stay aligned.
+struct Pages {
+    int64_t first, end;
+    __device__ __forceinline__ Pages(const Ranks& r, int n_pages) {
+        const int64_t fours = (int64_t(n_pages) + 3) / 4;
+        first = r.first(fours) * 4;
+        end = min(r.end(fours) * 4, int64_t(n_pages));
+    }
+    // Free pages among them.
+    __device__ __forceinline__ int64_t free(const int32_t* refs) const {
+        int n = 0;
+#pragma unroll 4
+        for (int64_t p = first + 4 * int64_t(threadIdx.x); p < end; p += 4 * kBookThreads) n += zeros(four(refs, p, end));
+        int64_t all;
+        block_scan(n, &all);
+        return all;
+    }
+};
+
+__device__ __forceinline__ int32_t pages_of(int32_t tokens, int shift) {
+    return int32_t((int64_t(tokens) + (1 << shift) - 1) >> shift);
+}
+
+// Ends a call that cannot be done; all of its blocks come here.
+__device__ __forceinline__ void fail(const Book& b, const Ranks& r, int bad) {
+    if (r.rank == 0 && threadIdx.x == 0) atomicOr(&b.control[kState], bad);
+}
+
+extern __shared__ uint32_t shared_bits[];
+
+__global__ void __launch_bounds__(kBookThreads) rr_cache_fork_kernel(const __grid_constant__ CacheShape c, const Book b,
+                                                                     const int32_t* parents, const int32_t* children, int n) {
+    after_previous();
+    const Ranks r;
+    Listed listed(shared_bits, c.max_seqs);
+    int bad = __ldcg(&b.control[kState]) | __ldcg(&b.control[kLate]);
+    for (int i = threadIdx.x; i < n; i += kBookThreads) {
+        const int p = parents[i], s = children[i];
+        if (!c.has_seq(p) || !c.has_seq(s)) {
+            bad |= kBadRange;
+            continue;
+        }
+        if (listed.add(s)) bad |= kBadTwice;
+        if (__ldcg(&b.lengths[s]) != 0) bad |= kBadChild;
+        if (!c.has_length(__ldcg(&b.lengths[p]))) bad |= kBadRange;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kBookThreads)
+        if (c.has_seq(parents[i]) && listed.has(parents[i])) bad |= kBadTwice;
+    bad = agree(bad);
+    cluster_barrier();
+    if (bad) return fail(b, r, bad);
+    // A warp takes 128 entries of one parent's row.
+    constexpr int kEach = 128;
+    const int lane = threadIdx.x & 31;
+    const int chunks = (c.max_pages + kEach - 1) / kEach;
+    for (int64_t task = r.warp(); task < int64_t(n) * chunks; task += r.warps()) {
+        const int i = int(task / chunks), first = int(task % chunks) * kEach;
+        const int p = parents[i], s = children[i], length = __ldcg(&b.lengths[p]);
+        const int end = min(pages_of(length, c.shift), first + kEach);
+        if (first == 0 && lane == 0) b.lengths[s] = length;
+        int32_t id[kEach / 32];
+#pragma unroll
+        for (int k = 0; k < kEach / 32; ++k) {
+            const int j = first + lane + 32 * k;
+            id[k] = j < end ? __ldcg(&b.table[int64_t(p) * c.max_pages + j]) : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kEach / 32; ++k) {
+            const int j = first + lane + 32 * k;
+            if (j >= end) continue;
+            b.table[int64_t(s) * c.max_pages + j] = id[k];
+            if (c.has_page(id[k])) atomicAdd(&b.refs[id[k]], 1);
+            else atomicOr(&b.control[kLate], kBadTable);
+        }
+    }
+}
+
+__device__ __forceinline__ int new_tokens(const int32_t* starts, int i) { return starts ? starts[i + 1] - starts[i] : 1; }
+
+// A listed sequence's next tokens: where they begin, and the page that is partly filled.
+struct Growth {
+    int s, length, count, filled;
+    int32_t page;        // partly filled (-1: none, or no tokens come)
+    int64_t entry;       // its place in the table
+    __device__ __forceinline__ Growth(const CacheShape& c, const Book& b, const int32_t* seqs, const int32_t* starts, int i) {
+        s = seqs[i];
+        count = new_tokens(starts, i);
+        length = __ldcg(&b.lengths[s]);
+        filled = length & (c.page - 1);
+        entry = int64_t(s) * c.max_pages + (length >> c.shift);
+        page = filled && count ? __ldcg(&b.table[entry]) : -1;
+        if (!c.has_page(page)) page = -1;
+    }
+    __device__ __forceinline__ int grown(const CacheShape& c) const {
+        return pages_of(length + count, c.shift) - pages_of(length, c.shift);
+    }
+};
+
+__global__ void __launch_bounds__(kBookThreads) rr_cache_extend_kernel(const __grid_constant__ CacheShape c, const Book b,
+                                                                       const int32_t* seqs, const int32_t* starts, int n) {
+    after_previous();
+    const Ranks r;
+    Listed listed(shared_bits, c.max_seqs);
+    int bad = __ldcg(&b.control[kState]) | __ldcg(&b.control[kLate]);
+    for (int i = threadIdx.x; i < n; i += kBookThreads) {
+        const int s = seqs[i], count = new_tokens(starts, i);
+        if (!c.has_seq(s)) {
+            bad |= kBadRange;
+            continue;
+        }
+        if (listed.add(s)) bad |= kBadTwice;
+        const int length = __ldcg(&b.lengths[s]);
+        if (!c.has_length(length) || count < 0) bad |= kBadRange;
+        else if (int64_t(length) + count > c.max_length()) bad |= kBadPool;
+        else if (count && (length & (c.page - 1)) && !c.has_page(__ldcg(&b.table[int64_t(s) * c.max_pages + (length >> c.shift)])))
+            bad |= kBadTable;
+    }
+    bad = agree(bad);
+    if (r.rank == 0 && threadIdx.x == 0) b.control[kMoves] = 0;
+    const int lo = int(r.first(n)), hi = int(r.end(n));
+    // Who holds each shared page that is partly filled, among the listed ones.
+    if (!bad) {
+        for (int i = lo + int(threadIdx.x); i < hi; i += kBookThreads) {
+            const Growth g(c, b, seqs, starts, i);
+            if (g.page >= 0 && __ldcg(&b.refs[g.page]) > 1) {
+                atomicAdd(&b.held[g.page], 1);
+                atomicMax(&b.last[g.page], i + 1);
+            }
+        }
+    }
+    cluster_barrier();
+    if (bad) return fail(b, r, bad);
+    // A copy for each holder, but for the last where all of them are listed; then whole
+    // pages.  b.plan: the sequence's place among the pages to be taken, and whether a copy is.
+    int64_t needed = 0;
+    for (int base = lo; base < hi; base += kBookThreads) {
+        const int i = base + int(threadIdx.x);
+        int need = 0, copy = 0;
+        if (i < hi) {
+            const Growth g(c, b, seqs, starts, i);
+            if (g.page >= 0) {
+                const int holders = __ldcg(&b.refs[g.page]);
+                copy = holders > 1 && !(__ldcg(&b.held[g.page]) == holders && __ldcg(&b.last[g.page]) == i + 1);
+            }
+            need = copy + g.grown(c);
+        }
+        int64_t total;
+        const int64_t at = needed + block_scan(need, &total);
+        // (A place past the pool's end only in a call that fails.)
+        if (i < hi) b.plan[i] = int32_t(min(at, int64_t(INT_MAX / 2))) * 2 + copy;
+        needed += total;
+    }
+    const Pages mine(r, c.n_pages);
+    const int64_t free = mine.free(b.refs);
+    if (threadIdx.x == 0) {
+        b.sums[r.rank] = needed;
+        b.sums[kBookRanks + r.rank] = free;
+    }
+    cluster_barrier();
+    int64_t all_needed, all_free;
+    const int64_t needed_before = rank_sum(b, r, 0, &all_needed);
+    int64_t k = rank_sum(b, r, 1, &all_free);
+    if (all_needed > all_free) bad = kBadPool;
+    // The lowest free pages, in order.
+    if (!bad) {
+        for (int64_t base = mine.first; base < mine.end && k < all_needed; base += 4 * kBookThreads) {
+            const int64_t p = base + 4 * int64_t(threadIdx.x);
+            const int4 v = four(b.refs, p, mine.end);
+            int64_t total, at = k + block_scan(zeros(v), &total);
+            if (v.x == 0 && at < all_needed) b.free[at++] = int32_t(p);
+            if (v.y == 0 && at < all_needed) b.free[at++] = int32_t(p + 1);
+            if (v.z == 0 && at < all_needed) b.free[at++] = int32_t(p + 2);
+            if (v.w == 0 && at < all_needed) b.free[at++] = int32_t(p + 3);
+            k += total;
+        }
+    }
+    cluster_barrier();
+    const int lane = threadIdx.x & 31;
+    for (int i = lo + int(threadIdx.x >> 5); i < hi; i += kBookWarps) {
+        const Growth g(c, b, seqs, starts, i);
+        __syncwarp();
+        if (g.page >= 0 && lane == 0) b.held[g.page] = b.last[g.page] = 0;
+        if (bad) continue;
+        const int plan = b.plan[i], copy = plan & 1;
+        const int64_t at = needed_before + (plan >> 1);
+        if (copy && lane == 0) {
+            const int to = __ldcg(&b.free[at]);
+            b.table[g.entry] = to;
+            b.refs[to] = 1;
+            atomicSub(&b.refs[g.page], 1);
+            b.moves[atomicAdd(&b.control[kMoves], 1)] = make_int4(g.page, to, g.filled, 0);
+        }
+        const int first = pages_of(g.length, c.shift), grown = g.grown(c);
+        for (int j = lane; j < grown; j += 32) {
+            const int to = __ldcg(&b.free[at + copy + j]);
+            b.table[int64_t(g.s) * c.max_pages + first + j] = to;
+            b.refs[to] = 1;
+        }
+        if (lane == 0) b.lengths[g.s] = g.length + g.count;
+    }
+    if (bad) fail(b, r, bad);
+}
+
+// The filled tokens of the pages that rr_cache_extend_kernel took copies of.  A warp
+// takes one run: a layer's keys or values of one head, `filled` rows of `pitch`.
+__global__ void __launch_bounds__(256) rr_cache_copy_rows_kernel(const __grid_constant__ CacheShape c, const Book b, char* pages) {
+    after_previous();
+    if (__ldcg(&b.control[kState])) return;
+    const int moves = __ldcg(&b.control[kMoves]);
+    const int lane = threadIdx.x & 31;
+    const int64_t warp = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5), warps = int64_t(gridDim.x) * 8;
+    const int vecs_row = c.pitch / 8;
+    for (int64_t task = warp; task < int64_t(moves) * c.runs; task += warps) {
+        const int4 m = __ldcg(&b.moves[task / c.runs]);
+        const int64_t run = task % c.runs * c.run_bytes;
+        const uint4* from = reinterpret_cast<const uint4*>(pages + m.x * c.page_bytes + run);
+        uint4* to = reinterpret_cast<uint4*>(pages + m.y * c.page_bytes + run);
+        const int vecs = m.z * vecs_row;
+        for (int i = lane; i < vecs; i += 128) {
+            uint4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + 32 * k < vecs) v[k] = from[i + 32 * k];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + 32 * k < vecs) to[i + 32 * k] = v[k];
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kBookThreads) rr_cache_truncate_kernel(const __grid_constant__ CacheShape c, const Book b,
+                                                                         const int32_t* seqs, const int32_t* drop, int n) {
+    after_previous();
+    const Ranks r;
+    Listed listed(shared_bits, c.max_seqs);
+    int bad = __ldcg(&b.control[kState]) | __ldcg(&b.control[kLate]);
+    for (int i = threadIdx.x; i < n; i += kBookThreads) {
+        const int s = seqs[i];
+        if (!c.has_seq(s)) {
+            bad |= kBadRange;
+            continue;
+        }
+        if (listed.add(s)) bad |= kBadTwice;
+        const int length = __ldcg(&b.lengths[s]);
+        if (!c.has_length(length) || (drop && (drop[i] < 0 || drop[i] > length))) bad |= kBadRange;
+    }
+    bad = agree(bad);
+    cluster_barrier();
+    if (bad) return fail(b, r, bad);
+    const int lane = threadIdx.x & 31;
+    for (int i = r.warp(); i < n; i += r.warps()) {
+        const int s = seqs[i], length = __ldcg(&b.lengths[s]), left = drop ? length - drop[i] : 0;
+        __syncwarp();
+        int32_t* const row = b.table + int64_t(s) * c.max_pages;
+#pragma unroll 4
+        for (int j = pages_of(left, c.shift) + lane; j < pages_of(length, c.shift); j += 32) {
+            const int id = row[j];
+            row[j] = -1;
+            if (c.has_page(id)) atomicSub(&b.refs[id], 1);
+            else atomicOr(&b.control[kLate], kBadTable);
+        }
+        if (lane == 0) b.lengths[s] = left;
+    }
+}
+
+// With U(p) the pages in use before page p and U pages in use in all: hole number
+// p - U(p) is page p < U that is free, and of the pages p >= U in use, U - 1 - U(p) are
+// behind p.  The k-th hole gets the k-th of these pages.
+__global__ void __launch_bounds__(kBookThreads) rr_cache_compact_kernel(const __grid_constant__ CacheShape c, const Book b) {
+    after_previous();
+    const Ranks r;
+    const int bad = __ldcg(&b.control[kState]) | __ldcg(&b.control[kLate]);
+    const Pages mine(r, c.n_pages);
+    const int64_t free = mine.free(b.refs);
+    if (threadIdx.x == 0) b.sums[r.rank] = mine.end - mine.first - free;
+    cluster_barrier();
+    if (bad) return;
+    int64_t used;
+    int64_t before = rank_sum(b, r, 0, &used);
+    int64_t holes = 0;
+    for (int64_t base = mine.first; base < mine.end; base += 4 * kBookThreads) {
+        const int64_t p = base + 4 * int64_t(threadIdx.x);
+        const int4 v = four(b.refs, p, mine.end);
+        const int refs[4] = {v.x, v.y, v.z, v.w};
+        const int n = int(max(min(mine.end - p, int64_t(4)), int64_t(0)));
+        int64_t total, u = before + block_scan(n - zeros(v), &total);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k >= n) continue;
+            if (refs[k]) {
+                if (p + k >= used) b.moves[used - 1 - u].w = int32_t(p + k);
+                ++u;
+            } else if (p + k < used) {
+                b.moves[p + k - u].y = int32_t(p + k);
+                ++holes;
+            }
+        }
+        before += total;
+    }
+    block_scan(holes, &holes);
+    if (threadIdx.x == 0) b.sums[kBookRanks + r.rank] = holes;
+    cluster_barrier();
+    int64_t moves;
+    rank_sum(b, r, 1, &moves);
+    if (r.rank == 0 && threadIdx.x == 0) {
+        b.control[kMoves] = int32_t(moves);
+        b.control[kUsed] = int32_t(used);
+    }
+    for (int64_t k = r.thread(); k < moves; k += r.threads()) {
+        const int from = __ldcg(&b.moves[moves - 1 - k].w), to = __ldcg(&b.moves[k].y);
+        b.moves[k].x = from;
+        b.free[from] = to;
+        b.refs[to] = __ldcg(&b.refs[from]);
+        b.refs[from] = 0;
+    }
+}
+
+// The moved pages' contents, 16 KiB a block and turn, and their places in the table.
+constexpr int kMoveChunk = 16384;
+__global__ void __launch_bounds__(256) rr_cache_move_kernel(const __grid_constant__ CacheShape c, const Book b, char* pages) {
+    after_previous();
+    if (__ldcg(&b.control[kState])) return;
+    const int moves = __ldcg(&b.control[kMoves]), used = __ldcg(&b.control[kUsed]);
+    if (!moves) return;
+    const int64_t chunks = (c.page_bytes + kMoveChunk - 1) / kMoveChunk;
+    for (int64_t task = blockIdx.x; task < moves * chunks; task += gridDim.x) {
+        const int4 m = __ldcg(&b.moves[task / chunks]);
+        const int64_t at = task % chunks * kMoveChunk;
+        const int vecs = int(min(c.page_bytes - at, int64_t(kMoveChunk)) / 16);
+        const uint4* from = reinterpret_cast<const uint4*>(pages + m.x * c.page_bytes + at);
+        uint4* to = reinterpret_cast<uint4*>(pages + m.y * c.page_bytes + at);
+        uint4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (int(threadIdx.x) + 256 * k < vecs) v[k] = __ldcs(&from[threadIdx.x + 256 * k]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (int(threadIdx.x) + 256 * k < vecs) __stcs(&to[threadIdx.x + 256 * k], v[k]);
+    }
+    const int lane = threadIdx.x & 31;
+    for (int s = int(blockIdx.x * 8 + (threadIdx.x >> 5)); s < c.max_seqs; s += int(gridDim.x) * 8) {
+        const int length = __ldcg(&b.lengths[s]);
+        if (!c.has_length(length)) continue;
+        int32_t* const row = b.table + int64_t(s) * c.max_pages;
+        const int n = pages_of(length, c.shift);
+#pragma unroll 4
+        for (int j = lane; j < n; j += 32) {
+            const int id = row[j];
+            if (id >= used && id < c.n_pages) row[j] = __ldcg(&b.free[id]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// New tokens' keys and values
+// ---------------------------------------------------------------------------
+
+// A warp takes one token's row: 2 n_kv vectors of `dim` elements, `pitch` in the page.
+// VEC: rows can be read 16 bytes at a time.
+template <bool VEC>
+__global__ void __launch_bounds__(256) rr_cache_append_kernel(const __grid_constant__ CacheShape c, const Book b, char* pages, int layer,
+                                                              const uint16_t* k, int64_t ldk, const uint16_t* v, int64_t ldv,
+                                                              const int32_t* seqs, const int32_t* starts, int n, int rows) {
+    after_previous();
+    if (__ldcg(&b.control[kState])) return;
+    const int lane = threadIdx.x & 31, row = int(blockIdx.x * 8 + (threadIdx.x >> 5));
+    if (row >= rows) return;
+    int i = row, j = 0, count = 1;
+    if (starts) {
+        // The last sequence that starts at or before the row.
+        int lo = 0, hi = n;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (starts[mid + 1] > row) hi = mid;
+            else lo = mid + 1;
+        }
+        i = lo;
+        if (i >= n || row < starts[i]) return;
+        j = row - starts[i];
+        count = starts[i + 1] - starts[i];
+    }
+    const int s = seqs[i];
+    int length = 0, id = -1, bad = 0;
+    if (!c.has_seq(s)) bad = kBadRange;
+    else length = __ldcg(&b.lengths[s]);
+    const int64_t pos = int64_t(length) - count + j;
+    if (!bad && (!c.has_length(length) || pos < 0)) bad = kBadRange;
+    if (!bad) id = __ldcg(&b.table[int64_t(s) * c.max_pages + (pos >> c.shift)]);
+    if (!bad && !c.has_page(id)) bad = kBadTable;
+    if (bad) {
+        if (lane == 0) atomicOr(&b.control[kLate], bad);
+        return;
+    }
+    char* const to = pages + id * c.page_bytes + layer * c.layer_bytes + (pos & (c.page - 1)) * (2 * c.pitch);
+    const int each = c.pitch / 8, half = c.n_kv * each;
+    for (int x = lane; x < 2 * half; x += 32) {
+        const int head = x / each, d = (x - head * each) * 8;      // heads of the keys, then of the values
+        const bool val = head >= c.n_kv;
+        const uint16_t* from = (val ? v + row * ldv + int64_t(head - c.n_kv) * c.dim : k + row * ldk + int64_t(head) * c.dim) + d;
+        uint4 u;
+        if (VEC) {
+            u = *reinterpret_cast<const uint4*>(from);
+        } else {
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = d + e < c.dim ? from[e] : 0u;
+            u = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+        }
+        *reinterpret_cast<uint4*>(to + head * c.run_bytes + 2 * d) = u;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Drafted tokens
+// ---------------------------------------------------------------------------
+
+constexpr int kAcceptRanks = 8;
+constexpr int kAcceptThreads = 1024;      // at most
+constexpr int kMaxVocab = 1 << 20;
+
+// A probability in whole numbers of 2^-42, ties to even; NaN counts as 0.  (x 2^42 is
+// exact in float32.)
+__device__ __forceinline__ uint64_t units(float x) {
+    return __float2ull_rn(fminf(fmaxf(x, 0.0f), 1.0f) * 4398046511104.0f);
+}
+
+struct AcceptArgs {
+    const float *p, *q;
+    int64_t ldp, ldq;
+    const int32_t *drafts, *starts;
+    const float *u, *v;
+    int32_t *accepted, *tokens, *rejected;
+    int32_t rows, vocab;
+};
+
+// Four entries of what the token is drawn from, from entry i on: in units, of the
+// rest (p, less q or without the refused draft) and of p itself.
+struct Draw {
+    const float *p, *q;       // q NULL: no draft was refused, or it came without probabilities
+    int without;              // the refused draft's token, or -1
+    int vocab;
+    bool vec;
+    __device__ __forceinline__ float4 load(const float* x, int i, int end) const {
+        if (vec && i + 3 < end) return *reinterpret_cast<const float4*>(x + i);
+        float4 r = make_float4(0, 0, 0, 0);
+        if (i < end) r.x = x[i];
+        if (i + 1 < end) r.y = x[i + 1];
+        if (i + 2 < end) r.z = x[i + 2];
+        if (i + 3 < end) r.w = x[i + 3];
+        return r;
+    }
+    __device__ __forceinline__ void four(int i, int end, bool rest, uint64_t* n) const {
+        const float4 a = load(p, i, end);
+        float x[4] = {a.x, a.y, a.z, a.w};
+        if (rest && q) {
+            const float4 c = load(q, i, end);
+            x[0] -= c.x, x[1] -= c.y, x[2] -= c.z, x[3] -= c.w;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) n[k] = rest && i + k == without ? 0 : units(x[k]);
+    }
+};
+
+// One cluster of 8 blocks takes a sequence.  Its blocks find the accepted drafts each for
+// itself; every warp adds up its run of the vocabulary, all sums go to all blocks, and the
+// warp whose run holds the drawn number looks through it again.  Sums of whole
+// numbers: their order changes nothing.  Bound by HBM: one row of p, and of q where a
+// draft was refused.
+__global__ void __launch_bounds__(kAcceptThreads, 1) rr_accept_kernel(const __grid_constant__ AcceptArgs a) {
+    __shared__ uint64_t sums[2][kAcceptRanks * kAcceptThreads / 32];
+    __shared__ int first_refused;
+    after_previous();
+    const int i = blockIdx.x / kAcceptRanks, rank = cluster_rank();
+    const int lane = threadIdx.x & 31, per_block = blockDim.x / 32, w = rank * per_block + int(threadIdx.x >> 5);
+    const int all = kAcceptRanks * per_block;
+    const int start = a.starts ? a.starts[i] : i, end = a.starts ? a.starts[i + 1] : i + 1;
+    const bool fits = start >= 0 && end <= a.rows && end > start;
+    const int n = fits ? end - start - 1 : 0;
+    if (threadIdx.x == 0) first_refused = n;
+    __syncthreads();
+    for (int j = threadIdx.x; j < n; j += blockDim.x) {
+        const int x = a.drafts[start + j];
+        bool ok = x >= 0 && x < a.vocab;
+        if (ok) {
+            const double own = a.q ? double(a.q[(start + j) * a.ldq + x]) : 1.0;
+            ok = double(a.u[start + j]) * own < double(a.p[(start + j) * a.ldp + x]);
+        }
+        if (!ok) atomicMin(&first_refused, j);
+    }
+    __syncthreads();
+    const int got = first_refused;
+    const int64_t row = start + got;
+    Draw d;
+    d.vocab = a.vocab;
+    d.p = a.p + row * a.ldp;
+    d.q = got < n && a.q ? a.q + row * a.ldq : nullptr;
+    d.without = got < n && !a.q ? a.drafts[row] : -1;
+    d.vec = reinterpret_cast<uintptr_t>(d.p) % 16 == 0 && reinterpret_cast<uintptr_t>(d.q) % 16 == 0;
+    const bool refused = got < n;
+    const int each = (a.vocab + 4 * all - 1) / (4 * all) * 4;
+    const int lo = min(w * each, a.vocab), hi = fits ? min(lo + each, a.vocab) : lo;
+    uint64_t rest = 0, whole = 0;
+#pragma unroll 4
+    for (int k = lo + 4 * lane; k < hi; k += 128) {
+        uint64_t x[4];
+        d.four(k, hi, true, x);
+        rest += x[0] + x[1] + x[2] + x[3];
+        if (refused) {
+            d.four(k, hi, false, x);
+            whole += x[0] + x[1] + x[2] + x[3];
+        }
+    }
+#pragma unroll
+    for (int m = 16; m; m >>= 1) {
+        rest += __shfl_xor_sync(~0u, rest, m);
+        whole += __shfl_xor_sync(~0u, whole, m);
+    }
+    if (lane < kAcceptRanks) {
+        uint32_t at0 = uint32_t(__cvta_generic_to_shared(&sums[0][w])), at1 = uint32_t(__cvta_generic_to_shared(&sums[1][w])), to0, to1;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to0) : "r"(at0), "r"(lane));
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to1) : "r"(at1), "r"(lane));
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to0), "l"(rest) : "memory");
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to1), "l"(whole) : "memory");
+    }
+    cluster_barrier();
+    if (!fits) {
+        if (rank == 0 && threadIdx.x == 0) {
+            a.accepted[i] = -1;
+            if (a.rejected) a.rejected[i] = 0;
+        }
+        return;
+    }
+    // The number drawn: floor(total v), v in whole numbers of 2^-31.
+    uint64_t before[2] = {0, 0}, total[2] = {0, 0};
+    for (int k = lane; k < all; k += 32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint64_t x = sums[h][k];
+            total[h] += x;
+            if (k < w) before[h] += x;
+        }
+    }
+#pragma unroll
+    for (int m = 16; m; m >>= 1) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            total[h] += __shfl_xor_sync(~0u, total[h], m);
+            before[h] += __shfl_xor_sync(~0u, before[h], m);
+        }
+    }
+    const bool use_rest = total[0] != 0;
+    const uint64_t sum = use_rest ? total[0] : total[1], ahead = use_rest ? before[0] : before[1];
+    const uint64_t own = use_rest ? sums[0][w] : sums[1][w];
+    const uint64_t v31 = min(uint64_t(fminf(fmaxf(a.v[i], 0.0f), 1.0f) * 2147483648.0f), uint64_t((1u << 31) - 1));
+    const uint64_t t = (sum >> 31) * v31 + ((sum & ((1u << 31) - 1)) * v31 >> 31);
+    if (rank == 0) {
+        for (int j = threadIdx.x; j <= n; j += blockDim.x) {
+            if (j < got) a.tokens[start + j] = a.drafts[start + j];
+            else if (j > got || sum == 0) a.tokens[start + j] = -1;
+        }
+        if (threadIdx.x == 0) {
+            a.accepted[i] = got;
+            if (a.rejected) a.rejected[i] = n - got;
+        }
+    }
+    if (sum == 0 || t < ahead || t - ahead >= own) return;
+    uint64_t left = t - ahead;
+    for (int k = lo; k < hi; k += 128) {
+        uint64_t x[4];
+        d.four(k + 4 * lane, hi, use_rest, x);
+        const uint64_t mine = x[0] + x[1] + x[2] + x[3];
+        uint64_t up = mine;
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) {
+            const uint64_t o = __shfl_up_sync(~0u, up, m);
+            if (lane >= m) up += o;
+        }
+        if (up > left && up - mine <= left) {
+            uint64_t y = left - (up - mine);
+            int e = 0;
+            while (e < 3 && y >= x[e]) y -= x[e++];
+            a.tokens[row] = k + 4 * lane + e;
+        }
+        const uint64_t last = __shfl_sync(~0u, up, 31);
+        if (last > left) break;
+        left -= last;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+
+// A launch as one or several clusters, behind the launch before it.
+template <class... Params, class... Args>
+cudaError_t launch_clusters(void (*kernel)(Params...), int cluster, unsigned grid, int threads, size_t smem, cudaStream_t stream,
+                            Args... args) {
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = unsigned(cluster);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(unsigned(threads));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+}
+
+size_t bits_bytes(const rr_cache* C) { return size_t(C->max_seqs + 31) / 32 * 4; }
+
+// Blocks that share a call's bookkeeping: with 8 the lists and the pool are gone through
+// 8 times as fast, but a barrier takes longer.
+int book_ranks(int64_t entries) { return entries <= 4 * kBookThreads ? 1 : kBookRanks; }
+
+rr_status check_list(int n, const rr_cache* C) {
+    if (n < 0 || n > C->max_seqs) return rr_fail(RR_EINVAL, "%d sequences: 0..%d", n, C->max_seqs);
+    return RR_OK;
+}
+
+rr_status copy_grid(int dev, unsigned* grid) {
+    static std::atomic<int> sms[kMaxDevices] = {};
+    int n = sms[dev].load(std::memory_order_relaxed);
+    if (!n) {
+        RR_CUDA(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
+        sms[dev].store(n, std::memory_order_relaxed);
+    }
+    *grid = unsigned(n) * 8;
+    return RR_OK;
+}
+
+}  // namespace
+
+extern "C" rr_status rr_cache_bytes(const rr_cache* C, int64_t* page_bytes, int64_t* pitch, int64_t* book_bytes) {
+    rr_clear_error();
+    RR_TRY(check_cache(C));
+    const CacheShape c = shape_of(C);
+    if (page_bytes) *page_bytes = c.page_bytes;
+    if (pitch) *pitch = c.pitch;
+    if (book_bytes) *book_bytes = book_of(C, nullptr, nullptr);
+    return RR_OK;
+}
+
+extern "C" rr_status rr_cache_clear(const rr_cache* C, void* book, cudaStream_t stream) {
+    RR_TRACE("rr_cache_clear");
+    rr_clear_error();
+    RR_TRY(check_cache(C));
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, book, 16, "book"));
+    Book b;
+    const int64_t bytes = book_of(C, book, &b);
+    RR_CUDA(cudaMemsetAsync(book, 0, size_t(bytes), stream));
+    RR_CUDA(cudaMemsetAsync(b.table, 0xFF, size_t(C->max_seqs) * C->max_pages * 4, stream));
+    return RR_OK;
+}
+
+extern "C" rr_status rr_cache_fork(const rr_cache* C, void* book, const int32_t* parents, const int32_t* children, int32_t n,
+                                   cudaStream_t stream) {
+    RR_TRACE("rr_cache_fork");
+    rr_clear_error();
+    RR_TRY(check_cache(C));
+    RR_TRY(check_list(n, C));
+    if (n == 0) return RR_OK;
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, book, 16, "book"));
+    RR_TRY(check_device(dev, parents, 4, "parents"));
+    RR_TRY(check_device(dev, children, 4, "children"));
+    Book b;
+    book_of(C, book, &b);
+    const int ranks = book_ranks(int64_t(n) * C->max_pages);
+    RR_CUDA(launch_clusters(rr_cache_fork_kernel, ranks, unsigned(ranks), kBookThreads, bits_bytes(C), stream, shape_of(C), b, parents,
+                            children, n));
+    return RR_OK;
+}
+
+extern "C" rr_status rr_cache_extend(const rr_cache* C, void* pages, void* book, const int32_t* seqs, const int32_t* starts, int32_t n,
+                                     cudaStream_t stream) {
+    RR_TRACE("rr_cache_extend");
+    rr_clear_error();
+    RR_TRY(check_cache(C));
+    RR_TRY(check_list(n, C));
+    if (n == 0) return RR_OK;
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, pages, 16, "pages"));
+    RR_TRY(check_device(dev, book, 16, "book"));
+    RR_TRY(check_device(dev, seqs, 4, "seqs"));
+    if (starts) RR_TRY(check_device(dev, starts, 4, "starts"));
+    Book b;
+    book_of(C, book, &b);
+    const CacheShape c = shape_of(C);
+    unsigned most;
+    RR_TRY(copy_grid(dev, &most));
+    const int ranks = book_ranks(std::max<int64_t>(4 * int64_t(n), C->n_pages / 2));
+    RR_CUDA(launch_clusters(rr_cache_extend_kernel, ranks, unsigned(ranks), kBookThreads, bits_bytes(C), stream, c, b, seqs, starts, n));
+    const unsigned grid = unsigned(std::min<int64_t>(most, (int64_t(n) * c.runs + 7) / 8));
+    RR_CUDA(launch_after(rr_cache_copy_rows_kernel, grid, 256, stream, c, b, static_cast<char*>(pages)));
+    return RR_OK;
+}
+
+extern "C" rr_status rr_cache_append(const rr_cache* C, void* pages, void* book, int32_t layer, const void* k, int64_t ldk, const void* v,
+                                     int64_t ldv, int32_t rows, const int32_t* seqs, const int32_t* starts, int32_t n,
+                                     cudaStream_t stream) {
+    RR_TRACE("rr_cache_append");
+    rr_clear_error();
+    RR_TRY(check_cache(C));
+    RR_TRY(check_list(n, C));
+    if (layer < 0 || layer >= C->layers) return rr_fail(RR_EINVAL, "layer %d of %d", layer, C->layers);
+    if (rows < 0 || (!starts && rows != n)) return rr_fail(RR_EINVAL, "%d rows of %d sequences", rows, n);
+    const int64_t cols = int64_t(C->n_kv) * C->dim;
+    if (ldk < cols || ldv < cols)
+        return rr_fail(RR_EINVAL, "row strides %lld and %lld of rows of %lld", (long long)ldk, (long long)ldv, (long long)cols);
+    if (n == 0 || rows == 0) return RR_OK;
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, pages, 16, "pages"));
+    RR_TRY(check_device(dev, book, 16, "book"));
+    RR_TRY(check_device(dev, k, 2, "k"));
+    RR_TRY(check_device(dev, v, 2, "v"));
+    RR_TRY(check_device(dev, seqs, 4, "seqs"));
+    if (starts) RR_TRY(check_device(dev, starts, 4, "starts"));
+    Book b;
+    book_of(C, book, &b);
+    const bool vec = (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0 && ldk % 8 == 0 && ldv % 8 == 0 && C->dim % 8 == 0;
+    RR_CUDA(launch_after(vec ? rr_cache_append_kernel<true> : rr_cache_append_kernel<false>, unsigned((int64_t(rows) + 7) / 8), 256, stream,
+                         shape_of(C), b, static_cast<char*>(pages), layer, static_cast<const uint16_t*>(k), ldk,
+                         static_cast<const uint16_t*>(v), ldv, seqs, starts, n, rows));
+    return RR_OK;
+}
+
+extern "C" rr_status rr_cache_truncate(const rr_cache* C, void* book, const int32_t* seqs, const int32_t* drop, int32_t n,
+                                       cudaStream_t stream) {
+    RR_TRACE("rr_cache_truncate");
+    rr_clear_error();
+    RR_TRY(check_cache(C));
+    RR_TRY(check_list(n, C));
+    if (n == 0) return RR_OK;
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, book, 16, "book"));
+    RR_TRY(check_device(dev, seqs, 4, "seqs"));
+    if (drop) RR_TRY(check_device(dev, drop, 4, "drop"));
+    Book b;
+    book_of(C, book, &b);
+    const int ranks = book_ranks(32 * int64_t(n));
+    RR_CUDA(launch_clusters(rr_cache_truncate_kernel, ranks, unsigned(ranks), kBookThreads, bits_bytes(C), stream, shape_of(C), b, seqs,
+                            drop, n));
+    return RR_OK;
+}
+
+extern "C" rr_status rr_cache_compact(const rr_cache* C, void* pages, void* book, cudaStream_t stream) {
+    RR_TRACE("rr_cache_compact");
+    rr_clear_error();
+    RR_TRY(check_cache(C));
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, pages, 16, "pages"));
+    RR_TRY(check_device(dev, book, 16, "book"));
+    Book b;
+    book_of(C, book, &b);
+    const CacheShape c = shape_of(C);
+    unsigned most;
+    RR_TRY(copy_grid(dev, &most));
+    const int ranks = book_ranks(C->n_pages / 2);
+    RR_CUDA(launch_clusters(rr_cache_compact_kernel, ranks, unsigned(ranks), kBookThreads, 0, stream, c, b));
+    const int64_t chunks = (c.page_bytes + kMoveChunk - 1) / kMoveChunk * (C->n_pages / 2);
+    const unsigned grid = unsigned(std::max<int64_t>(1, std::min<int64_t>(most, std::max<int64_t>(chunks, (C->max_seqs + 7) / 8))));
+    RR_CUDA(launch_after(rr_cache_move_kernel, grid, 256, stream, c, b, static_cast<char*>(pages)));
+    return RR_OK;
+}
+
+extern "C" rr_status rr_cache_check(const rr_cache* C, void* book, cudaStream_t stream) {
+    rr_clear_error();
+    RR_TRY(check_cache(C));
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, book, 16, "book"));
+    int32_t words[2] = {0, 0};       // kState, kLate
+    RR_CUDA(cudaMemcpyAsync(words, book, 8, cudaMemcpyDeviceToHost, stream));
+    RR_CUDA(cudaStreamSynchronize(stream));
+    const int state = words[0] | words[1];
+    if (!state) return RR_OK;
+    RR_CUDA(cudaMemsetAsync(book, 0, 8, stream));
+    RR_CUDA(cudaStreamSynchronize(stream));
+    return rr_fail(RR_EINVAL, "a call on the cache was not done:%s%s%s%s%s", state & kBadRange ? " a sequence, length or count is out of range;" : "",
+                   state & kBadTwice ? " a sequence is listed twice;" : "", state & kBadPool ? " no room for the new tokens;" : "",
+                   state & kBadChild ? " a child holds tokens;" : "", state & kBadTable ? " the table has a page out of range;" : "");
+}
+
+extern "C" rr_status rr_accept(const float* p, int64_t ldp, const float* q, int64_t ldq, const int32_t* drafts, const int32_t* starts,
+                               const float* u, const float* v, int32_t rows, int32_t n, int32_t vocab, int32_t* accepted, int32_t* tokens,
+                               int32_t* rejected, cudaStream_t stream) {
+    RR_TRACE("rr_accept");
+    rr_clear_error();
+    if (vocab < 1 || vocab > kMaxVocab) return rr_fail(RR_ELAYOUT, "%d tokens in the vocabulary: 1..%d", vocab, kMaxVocab);
+    if (n < 0 || n > INT_MAX / kAcceptRanks || rows < 0 || (!starts && rows != n))
+        return rr_fail(RR_EINVAL, "%d rows of %d sequences", rows, n);
+    if (ldp < vocab || (q && ldq < vocab))
+        return rr_fail(RR_EINVAL, "row strides %lld and %lld of rows of %d", (long long)ldp, (long long)ldq, vocab);
+    if (n == 0) return RR_OK;
+    if (rows == 0) return rr_fail(RR_EINVAL, "0 rows of %d sequences", n);
+    int dev;
+    RR_TRY(current_device(&dev));
+    RR_TRY(check_device(dev, p, 4, "p"));
+    if (q) RR_TRY(check_device(dev, q, 4, "q"));
+    if (starts) {
+        RR_TRY(check_device(dev, starts, 4, "starts"));
+        RR_TRY(check_device(dev, drafts, 4, "drafts"));
+        RR_TRY(check_device(dev, u, 4, "u"));
+    }
+    RR_TRY(check_device(dev, v, 4, "v"));
+    RR_TRY(check_device(dev, accepted, 4, "accepted"));
+    RR_TRY(check_device(dev, tokens, 4, "tokens"));
+    if (rejected) RR_TRY(check_device(dev, rejected, 4, "rejected"));
+    const AcceptArgs a = {p, q, ldp, ldq, drafts, starts, u, v, accepted, tokens, rejected, rows, vocab};
+    const int threads = n > 16 ? 256 : kAcceptThreads;
+    RR_CUDA(launch_clusters(rr_accept_kernel, kAcceptRanks, unsigned(n) * kAcceptRanks, threads, 0, stream, a));
+    return RR_OK;
+}
