@@ -3,26 +3,45 @@
 //
 // Bound by HBM: every key and value of the listed sequences is read once, 4 dim bytes for
 // 4 dim x (query heads per key head) x (new tokens) operations.  The work of a call is one
-// line of units, 32 keys of one sequence, key head and tile of rows each; every warp of the
-// grid takes an even, contiguous run of it, wherever sequences begin and end, so that
+// line of units, 128 keys of one sequence, key head and tile of rows each; every block (one
+// an SM) takes an even, contiguous run of it, wherever sequences begin and end, so that
 // short and long sequences load the SMs alike.  Where a run's edge cuts a tile's keys,
-// the pieces (their softmax's maximum and sum, and their normalised output) are joined:
-// among a block's warps, then, by the last of a tile's blocks to come, among blocks, in
-// the order of the keys each time.
+// the pieces (their softmax's maximum and sum, and their normalised output) are joined by
+// the last of the tile's blocks to come, in the order of the keys each time.
+//
+// Within a block, per unit: one warp has the pages' keys and values copied to shared
+// memory by TMA, which lays them out as the matrix instructions want them and fills what is
+// past a head's end with zeros; one thread issues tcgen05 products,
+//     S^T [128 keys, rows] = K Q^T,    D^T [dim, rows] = V^T P^T,
+// with keys, then head elements, as the 128 rows of the accumulator in TMEM, so that
+// a few rows of queries cost few columns and keys and values go from shared memory into the
+// product as they lie; eight warps turn scores into weights and add the products' sums up
+// in registers; one more warp fetches the next tile's queries.  S^T of the next unit is
+// computed while the softmax of this one runs.
 #include <algorithm>
 #include <climits>
 #include <type_traits>
+
+#include <cuda.h>
+#include <cudaTypedefs.h>
 
 #include "rr_cache.cuh"
 
 namespace {
 
-constexpr int kUnit = 32;               // keys
+constexpr int kUnit = 128;              // keys
 constexpr int kMostBlocks = 192;
+constexpr int kMostStages = 12;
+constexpr int kThreads = 11 * 32;       // softmax: warps 0..7; then copies, products, queries
+constexpr int kSoft = 256;
+constexpr int kSmem = 220 * 1024;       // of a block, beside its static part
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
 // A row's reference for its exponentials may stay this much (of log2) under its maximum.
 constexpr float kSlack = 8.0f;
+// In place of minus the reference of a row that has seen nothing yet.
+constexpr float kNothing = 3e38f;
+constexpr long long kWaitCycles = 4000000000;
 
 struct AttendArgs {
     CacheShape c;
@@ -34,25 +53,35 @@ struct AttendArgs {
     float* lse;
     int64_t ldq, ldo;
     const int32_t *seqs, *starts;
-    float* pieces;                 // the warps', then two a block
+    float* pieces;                 // two a block
     uint32_t* arrived;             // per block: arrivals for the tile that starts in it and goes on
     int64_t piece_floats;
     int32_t n, rows, n_q, group;
+    int32_t stages, atoms;         // of the ring; 64 elements of a head each
     float scale;                   // with log2(e)
     int32_t qvec, ovec;
 };
 
-template <class T>
-__device__ __forceinline__ void mma(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    if (std::is_same<T, BF16>::value)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-    else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
+// What a kernel is compiled for: T, the element type; MT, head sizes up to 128 MT; NG, tiles
+// of up to 8 NG rows.
+template <class T_, int MT_, int NG_>
+struct Kind {
+    using T = T_;
+    static constexpr int MT = MT_, NG = NG_;
+    static constexpr int kRows = 8 * NG;
+    static constexpr int D = 128 * MT;
+    // Bfloat16 keeps 8 bits of a weight: it enters the second product in two parts, 16
+    // bits in all.  Float16's 11 bits are one part: as far off as the result's own
+    // rounding is.  Its weights are 2^7 to 2^15 at a row's maximum, so that those 2^-21 of
+    // the largest still have all of their bits (under 2^-32 of it they are 0).
+    static constexpr int kParts = std::is_same<T, BF16>::value ? 2 : 1;
+    static constexpr float kLift = std::is_same<T, BF16>::value ? 0.0f : 7.0f;
+    static constexpr int kQ = MT * NG * 2048;           // bytes of a tile's queries
+    static constexpr int kP = NG * 2048;                // of one part of the weights
+    static constexpr int kFixed = 2 * kQ + kParts * kP;
+    static constexpr int kColumns = (2 + MT) * kRows <= 64 ? 64 : (2 + MT) * kRows <= 128 ? 128 : (2 + MT) * kRows <= 256 ? 256 : 512;
+    static_assert((2 + MT) * kRows <= 512, "TMEM");
+};
 
 // Two floats as one word of 16-bit elements, the first in the low half.
 template <class T>
@@ -63,77 +92,24 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     return r;
 }
 
-// The transpose of an 8 x 8 matrix of 16-bit elements, a word a lane.
-__device__ __forceinline__ uint32_t transposed(uint32_t x) {
-    uint32_t r;
-    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
-    return r;
-}
-
-// `bytes` (0..16) from global memory and zeros after them, to shared memory.
-__device__ __forceinline__ void copy_async(uint32_t to, const void* from, int bytes) {
-    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ uint4 lds(uint32_t at) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint2 lds2(uint32_t at) {
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
-    return v;
-}
-__device__ __forceinline__ void sts(uint32_t at, uint4 v) {
-    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-
-// What a kernel is compiled for: T, the element type; C, head sizes up to 64 C; NT, tiles
-// of up to 8 NT rows.
-template <class T_, int C_, int NT_>
-struct Kind {
-    using T = T_;
-    static constexpr int C = C_, NT = NT_;
-    static constexpr int kRows = 8 * NT;
-    static constexpr int kWarps = C > 2 ? 4 : 8, kThreads = 32 * kWarps;
-    static constexpr int kStage = C * 4096;                       // bytes of a unit's keys, or values
-    static constexpr int kQ = NT * C * 1024;                      // bytes of a tile's queries
-    static constexpr int kRoom = 224 * 1024 / kWarps;    // bytes a warp has
-    static constexpr int kMost = (kRoom - kQ) / kStage;
-    static constexpr int kStages = kMost > 6 ? 6 : kMost;
-    static constexpr int kPieceFloats = kRows * (64 * C + 2);
-    static constexpr int kWarpBytes = kQ + kStages * kStage;
-    static constexpr int kSmem = kWarps * kWarpBytes;
-    static_assert(kStages >= 2, "keys and values in turn");
-    static_assert(kPieceFloats * 4 <= kWarpBytes, "a piece takes the place of the stages");
-    // Bfloat16 keeps 8 bits of a weight: it enters the second product in two parts, 16
-    // bits in all.  Float16's 11 bits are one part: as far off as the result's own
-    // rounding is.  Its weights lie between 2^(7 - 2^..) and 2^15, so that those 2^-21 of
-    // the largest still have all of their bits (under 2^-32 of it they are 0).
-    static constexpr int kParts = std::is_same<T, BF16>::value ? 2 : 1;
-    static constexpr float kLift = std::is_same<T, BF16>::value ? 0.0f : 7.0f;
-};
-
 // One tile of rows over one sequence's keys.  Row r of a sequence is head r % group of new
 // token r / group.
 struct Tile {
     int length, first, count;      // tokens of the sequence; its first new one among the call's, and how many
     int slot;                      // the sequence
-    int head, tile;                // key head; which 8 NT rows
-    int units;                     // of 32 keys
+    int head, tile;                // key head; which 8 NG rows
+    int units;                     // of 128 keys
+};
+
+// A tile's part in a block's run.
+struct Item {
+    Tile t;
+    int first, n;                  // units
+    int64_t begin;                 // of the tile in the call's line
 };
 
 // The last key (+ 1) that a row sees.
 __device__ __forceinline__ int seen(const Tile& t, int group, int row) { return t.length - t.count + 1 + row / group; }
-
-// Where one warp's tile or one piece goes.
-struct Ends {
-    int64_t begin, end;            // the tile's units in the call's line; begin < 0: none
-    Tile t;
-};
 
 // One listed sequence, checked: a sequence that does not fit has no units (and marks
 // the cache).
@@ -158,311 +134,14 @@ __device__ __forceinline__ int64_t work_of(const AttendArgs& a, int length, int 
     return int64_t(a.c.n_kv) * tiles_of<K>(a, count) * units_of(length);
 }
 
-// The warps' runs: worker w has units [T w / N, T (w + 1) / N).
+// The blocks' runs: block b has units [T b / N, T (b + 1) / N).
 struct Line {
     int64_t total;
-    int workers;
-    __device__ __forceinline__ int64_t begin(int w) const { return total * min(w, workers) / workers; }
+    int blocks;
+    __device__ __forceinline__ int64_t begin(int b) const { return total * b / blocks; }
     // Whose run holds unit u.
-    __device__ __forceinline__ int owner(int64_t u) const { return int(((u + 1) * workers - 1) / total); }
+    __device__ __forceinline__ int owner(int64_t u) const { return int(((u + 1) * blocks - 1) / total); }
 };
-
-// ---------------------------------------------------------------------------
-// Results
-// ---------------------------------------------------------------------------
-
-// Eight adjacent elements of the result, as T.
-template <class T>
-__device__ __forceinline__ void put8(uint16_t* to, int d, int dim, bool vec, const float* x) {
-    if (vec && d + 8 <= dim) {
-        *reinterpret_cast<uint4*>(to + d) =
-            make_uint4(pack<T>(x[0], x[1]), pack<T>(x[2], x[3]), pack<T>(x[4], x[5]), pack<T>(x[6], x[7]));
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-        if (d + k < dim) to[d + k] = T::round(x[k]);
-}
-
-// Puts a tile's results where they belong: to `piece` if that is given, else to the
-// outputs.  o: normalised, as the products leave it: [nt][c][i][.], of the 64 c + 8 g + 2 i-th
-// element and the next, of rows 8 nt + 2 t and the next.  top and sum: of those two rows.
-template <class K>
-__device__ __forceinline__ void emit(const AttendArgs& a, const Tile& t, float* piece, const float (&o)[K::NT][K::C][4][4],
-                                     const float (&top)[K::NT][2], const float (&sum)[K::NT][2]) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, c4 = lane & 3;
-    const int left = t.count * a.group - t.tile * K::kRows;
-#pragma unroll
-    for (int nt = 0; nt < K::NT; ++nt) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = 8 * nt + 2 * c4 + e;
-            if (r >= left) continue;
-            const int row = t.tile * K::kRows + r;
-            const int64_t token = t.first + row / a.group;
-            const int head = t.head * a.group + row % a.group;
-#pragma unroll
-            for (int c = 0; c < K::C; ++c) {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[2 * i] = o[nt][c][i][e];
-                    x[2 * i + 1] = o[nt][c][i][2 + e];
-                }
-                if (piece) {
-                    float4* to = reinterpret_cast<float4*>(piece + r * (64 * K::C) + 64 * c + 8 * g);
-                    to[0] = make_float4(x[0], x[1], x[2], x[3]);
-                    to[1] = make_float4(x[4], x[5], x[6], x[7]);
-                } else {
-                    put8<typename K::T>(a.out + token * a.ldo + int64_t(head) * a.c.dim, 64 * c + 8 * g, a.c.dim, a.ovec, x);
-                }
-            }
-            if (g == 0) {
-                if (piece) {
-                    piece[64 * K::C * K::kRows + 2 * r] = top[nt][e];
-                    piece[64 * K::C * K::kRows + 2 * r + 1] = sum[nt][e];
-                } else if (a.lse) {
-                    a.lse[token * a.n_q + head] = sum[nt][e] == 0.0f ? -kInf : (top[nt][e] + log2f(sum[nt][e])) * kLn2;
-                }
-            }
-        }
-    }
-}
-
-// A warp joins row r of n pieces, given by at(i): to `piece`, or, if that is NULL, to
-// the outputs.  A piece counts by its sum at the largest of the maxima.
-template <class K, bool FAR, class At>
-__device__ __forceinline__ void join_row(const AttendArgs& a, const Tile& t, int r, int n, At at, float* piece) {
-    constexpr int D = 64 * K::C, kMl = D * K::kRows;
-    const int lane = threadIdx.x & 31;
-    const auto get = [](const float* x) { return FAR ? __ldcg(x) : *x; };
-    const auto get4 = [](const float4* x) { return FAR ? __ldcg(x) : *x; };
-    float top = -kInf;
-    for (int i = lane; i < n; i += 32) top = fmaxf(top, get(at(i) + kMl + 2 * r));
-#pragma unroll
-    for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
-    const auto share = [&](int i) {
-        const float m = get(at(i) + kMl + 2 * r);
-        return m == -kInf ? 0.0f : get(at(i) + kMl + 2 * r + 1) * exp2f(m - top);
-    };
-    float sum = 0;
-    for (int i = lane; i < n; i += 32) sum += share(i);
-#pragma unroll
-    for (int m = 16; m; m >>= 1) sum += __shfl_xor_sync(~0u, sum, m);
-    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
-    // 8 adjacent elements a lane; lanes past the head's end help with other pieces.
-    constexpr int kLanes = D / 8, kTeams = 32 / kLanes;
-    const int d = 8 * (lane % kLanes), team = lane / kLanes;
-    float x[8] = {};
-    for (int base = 0; base < n; base += 32) {
-        const float mine = base + lane < n ? share(base + lane) * inverse : 0.0f;
-#pragma unroll 4
-        for (int k = 0; k < min(n - base, 32); k += kTeams) {
-            const int i = base + k + team;
-            const float w = __shfl_sync(~0u, mine, (k + team) & 31);
-            if (k + team >= 32 || i >= n || w == 0.0f) continue;
-            const float4* from = reinterpret_cast<const float4*>(at(i) + r * D + d);
-            const float4 u = get4(from), v = get4(from + 1);
-            x[0] = fmaf(w, u.x, x[0]), x[1] = fmaf(w, u.y, x[1]), x[2] = fmaf(w, u.z, x[2]), x[3] = fmaf(w, u.w, x[3]);
-            x[4] = fmaf(w, v.x, x[4]), x[5] = fmaf(w, v.y, x[5]), x[6] = fmaf(w, v.z, x[6]), x[7] = fmaf(w, v.w, x[7]);
-        }
-    }
-#pragma unroll
-    for (int m = kLanes; m < 32; m <<= 1) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] += __shfl_xor_sync(~0u, x[k], m);
-    }
-    if (team) return;
-    if (piece) {
-        float4* to = reinterpret_cast<float4*>(piece + r * D + d);
-        to[0] = make_float4(x[0], x[1], x[2], x[3]);
-        to[1] = make_float4(x[4], x[5], x[6], x[7]);
-        if (lane == 0) piece[kMl + 2 * r] = top, piece[kMl + 2 * r + 1] = sum;
-        return;
-    }
-    const int row = t.tile * K::kRows + r, head = t.head * a.group + row % a.group;
-    const int64_t token = t.first + row / a.group;
-    put8<typename K::T>(a.out + token * a.ldo + int64_t(head) * a.c.dim, d, a.c.dim, a.ovec, x);
-    if (lane == 0 && a.lse) a.lse[token * a.n_q + head] = sum == 0.0f ? -kInf : (top + log2f(sum)) * kLn2;
-}
-
-// FAR: the pieces come from other blocks too.
-template <class K, bool FAR, class At>
-__device__ __forceinline__ void join(const AttendArgs& a, const Tile& t, int n, At at, float* piece) {
-    const int rows = min(t.count * a.group - t.tile * K::kRows, K::kRows);
-    for (int r = threadIdx.x >> 5; r < rows; r += K::kWarps) join_row<K, FAR>(a, t, r, n, at, piece);
-}
-
-// ---------------------------------------------------------------------------
-// One warp's run
-// ---------------------------------------------------------------------------
-
-// Lane 4 g + t's part of a tile's query rows: of row 8 nt + g, elements 32 k + 8 t + 0..7.
-template <class K>
-__device__ __forceinline__ uint4 load_q(const AttendArgs& a, const Tile& t, int nt, int k) {
-    const int lane = threadIdx.x & 31, row = t.tile * K::kRows + 8 * nt + (lane >> 2), d = 32 * k + 8 * (lane & 3);
-    if (row >= t.count * a.group || d >= a.c.dim) return make_uint4(0, 0, 0, 0);
-    const uint16_t* from = a.q + (t.first + row / a.group) * a.ldq + int64_t(t.head * a.group + row % a.group) * a.c.dim + d;
-    if (a.qvec) return *reinterpret_cast<const uint4*>(from);
-    uint32_t w[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = d + e < a.c.dim ? from[e] : 0u;
-    return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
-}
-
-// The scores of 32 keys: s[h][nt][.] of keys 8 (h) + g (and 8 more in [2], [3]) of each half h of 16, rows
-// 8 nt + 2 t and the next.
-template <class K>
-__device__ __forceinline__ void mask(const AttendArgs& a, const Tile& t, int key0, float (&s)[2][K::NT][4]) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, c4 = lane & 3;
-#pragma unroll
-    for (int nt = 0; nt < K::NT; ++nt) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int end = seen(t, a.group, t.tile * K::kRows + 8 * nt + 2 * c4 + e) - key0 - g;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (16 * h >= end) s[h][nt][e] = -kInf;
-                if (16 * h + 8 >= end) s[h][nt][2 + e] = -kInf;
-            }
-        }
-    }
-}
-
-// The address of 8 adjacent tokens of a page, or NULL past the sequence's end.
-__device__ __forceinline__ const char* tokens8(const AttendArgs& a, const Tile& t, int key, int id) {
-    if (key >= t.length) return nullptr;
-    return a.pages + id * a.c.page_bytes + t.head * a.c.run_bytes + (key & (a.c.page - 1)) * (2 * a.c.pitch);
-}
-
-// Units [u0, u1) of a tile once more, one key after another, for values that are not
-// finite or nearly too large: a product of weight and value only where the row sees the
-// key, weights in float32 and 2^-32 of what they are, so that sums stay finite.
-template <class K>
-__device__ __noinline__ void carefully(const AttendArgs& a, const Tile& t, int u0, int u1, float* piece) {
-    using T = typename K::T;
-    const int lane = threadIdx.x & 31, g = lane >> 2, c4 = lane & 3;
-    float o[K::NT][K::C][4][4] = {}, top[K::NT][2], sum[K::NT][2] = {};
-#pragma unroll
-    for (int nt = 0; nt < K::NT; ++nt) top[nt][0] = top[nt][1] = -kInf;
-    for (int pass = 0; pass < 2; ++pass) {
-        for (int u = u0; u < u1; ++u) {
-            const int key0 = u * kUnit;
-            float s[2][K::NT][4] = {};
-            const char* at[4];
-            for (int h = 0; h < 4; ++h) {
-                const int key = key0 + 8 * h;
-                int id = key < t.length ? __ldcg(&a.table[int64_t(t.slot) * a.c.max_pages + (key >> a.c.shift)]) : -1;
-                at[h] = a.c.has_page(id) ? tokens8(a, t, key, id) : nullptr;
-            }
-#pragma unroll 1
-            for (int k = 0; k < 2 * K::C; ++k) {
-                uint4 r[4];
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    r[h] = make_uint4(0, 0, 0, 0);
-                    const int d = 32 * k + 8 * c4;
-                    if (!at[h] || key0 + 8 * h + g >= t.length || d >= a.c.dim) continue;
-                    r[h] = *reinterpret_cast<const uint4*>(at[h] + g * (2 * a.c.pitch) + 2 * d);
-                    // (The pad behind the last element is not looked at.)
-                    uint32_t* w = &r[h].x;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        if (d + 2 * x >= a.c.dim) w[x] = 0;
-                        else if (d + 2 * x + 1 >= a.c.dim) w[x] &= 0xFFFFu;
-                    }
-                }
-#pragma unroll
-                for (int nt = 0; nt < K::NT; ++nt) {
-                    const uint4 b = load_q<K>(a, t, nt, k);
-                    mma<T>(s[0][nt], r[0].x, r[1].x, r[0].y, r[1].y, b.x, b.y);
-                    mma<T>(s[0][nt], r[0].z, r[1].z, r[0].w, r[1].w, b.z, b.w);
-                    mma<T>(s[1][nt], r[2].x, r[3].x, r[2].y, r[3].y, b.x, b.y);
-                    mma<T>(s[1][nt], r[2].z, r[3].z, r[2].w, r[3].w, b.z, b.w);
-                }
-            }
-#pragma unroll
-            for (int nt = 0; nt < K::NT; ++nt)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[h][nt][e] *= a.scale;
-            mask<K>(a, t, key0, s);
-            if (pass == 0) {
-#pragma unroll
-                for (int nt = 0; nt < K::NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float m = fmaxf(fmaxf(s[0][nt][e], s[0][nt][2 + e]), fmaxf(s[1][nt][e], s[1][nt][2 + e]));
-#pragma unroll
-                        for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, x));
-                        top[nt][e] = fmaxf(top[nt][e], m);
-                    }
-                continue;
-            }
-#pragma unroll
-            for (int nt = 0; nt < K::NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float m = top[nt][e & 1] == -kInf ? 0.0f : top[nt][e & 1];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        s[h][nt][e] = exp2f(s[h][nt][e] - m);
-                        sum[nt][e & 1] += s[h][nt][e];
-                    }
-                }
-#pragma unroll 1
-            for (int x = 0; x < kUnit; ++x) {
-                if (key0 + x >= t.length) break;
-                const char* from = at[x >> 3];
-#pragma unroll
-                for (int nt = 0; nt < K::NT; ++nt) {
-                    const int other = (x & 7) * 4 + c4;
-                    float p[2];
-                    bool sees[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float lo = x & 16 ? s[1][nt][e] : s[0][nt][e], hi = x & 16 ? s[1][nt][2 + e] : s[0][nt][2 + e];
-                        p[e] = __shfl_sync(~0u, x & 8 ? hi : lo, other) * 0x1p-32f;
-                        sees[e] = key0 + x < seen(t, a.group, t.tile * K::kRows + 8 * nt + 2 * c4 + e);
-                    }
-#pragma unroll
-                    for (int c = 0; c < K::C; ++c) {
-                        const int d = 64 * c + 8 * g;
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (from && d < a.c.pitch)
-                            v = *reinterpret_cast<const uint4*>(from + int64_t(a.c.n_kv) * a.c.run_bytes + (x & 7) * (2 * a.c.pitch) + 2 * d);
-                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                if (!sees[e]) continue;
-                                o[nt][c][i][e] = fmaf(p[e], T::widen(uint16_t(w[i])), o[nt][c][i][e]);
-                                o[nt][c][i][2 + e] = fmaf(p[e], T::widen(uint16_t(w[i] >> 16)), o[nt][c][i][2 + e]);
-                            }
-                    }
-                }
-            }
-        }
-    }
-#pragma unroll
-    for (int nt = 0; nt < K::NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-#pragma unroll
-            for (int x = 4; x < 32; x <<= 1) sum[nt][e] += __shfl_xor_sync(~0u, sum[nt][e], x);
-            const float inverse = sum[nt][e] == 0.0f ? 0.0f : 0x1p32f / sum[nt][e];
-#pragma unroll
-            for (int c = 0; c < K::C; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    o[nt][c][i][e] *= inverse;
-                    o[nt][c][i][2 + e] *= inverse;
-                }
-        }
-    emit<K>(a, t, piece, o, top, sum);
-}
 
 // Walks the listed sequences' tiles from a place in the call's line on; 32 sequences'
 // numbers at a time, one a lane.
@@ -503,434 +182,885 @@ struct Walk {
     }
 };
 
-// What a unit's copies and its products need to agree on, in shared memory.
+// ---------------------------------------------------------------------------
+// Barriers, copies, products
+// ---------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t smem_of(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void bar_init(uint32_t bar, int count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, int parity) {
+    uint32_t done;
+    asm volatile(
+        "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done;
+}
+// Whether the barrier's phase came.  A wait that runs out (two seconds or so) raises *quit, on
+// which the block's other waits give up too.
+__device__ __noinline__ bool bar_wait_on(uint32_t bar, int parity, volatile int* quit, int32_t* control) {
+    const long long t0 = clock64();
+    for (;;) {
+        for (int k = 0; k < 64; ++k)
+            if (bar_try(bar, parity)) return true;
+        if (*quit) return false;
+        if (clock64() - t0 > kWaitCycles) {
+            *quit = 1;
+            atomicOr(&control[kLate], kBadWait);
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, int parity, volatile int* quit, int32_t* control) {
+    return bar_try(bar, parity) || bar_wait_on(bar, parity, quit, control);
+}
+
+// The softmax warps' own barrier, with the OR of what they bring.
+__device__ __forceinline__ bool soft_any(bool x) {
+    uint32_t r;
+    asm volatile(
+        "{ .reg .pred p, q; setp.ne.u32 p, %1, 0; barrier.cta.red.or.pred q, 1, %2, p; selp.u32 %0, 1, 0, q; }"
+        : "=r"(r)
+        : "r"(uint32_t(x)), "n"(kSoft)
+        : "memory");
+    return r;
+}
+__device__ __forceinline__ void soft_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kSoft) : "memory"); }
+
+__device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+        : "memory");
+}
+
+// A descriptor of a matrix in shared memory: strides in bytes, layout 2 for rows of 128
+// bytes swizzled, 0 for 8 x 16 bytes as they lie.
+__device__ __forceinline__ uint64_t descriptor(uint32_t at, uint32_t leading, uint32_t stride, uint64_t layout) {
+    return uint64_t((at & 0x3FFFF) >> 4) | uint64_t(leading >> 4) << 16 | uint64_t(stride >> 4) << 32 | uint64_t(1) << 46 | layout << 61;
+}
+// Of an instruction: float32 sums, 128 x n; which operands have their rows' index adjacent.
+template <class T>
+__device__ __forceinline__ uint32_t instruction(int n, bool a_rows, bool b_rows) {
+    const uint32_t type = std::is_same<T, BF16>::value ? 1 : 0;
+    return 1u << 4 | type << 7 | type << 10 | uint32_t(a_rows) << 15 | uint32_t(b_rows) << 16 | uint32_t(n >> 3) << 17 | (128u >> 4) << 24;
+}
+__device__ __forceinline__ void product(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, bool add) {
+    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b),
+                 "r"(instr), "r"(uint32_t(add))
+                 : "memory");
+}
+// The barrier's arrival when all products issued so far are done.
+__device__ __forceinline__ void products_arrive(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Eight columns of this lane's row, in pairs.
+__device__ __forceinline__ void tmem_load(uint32_t at, unsigned long long* x) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(at)
+                 : "memory");
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = (unsigned long long)(r[2 * e + 1]) << 32 | r[2 * e];
+}
+__device__ __forceinline__ void tmem_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Generic writes to shared memory, before the copies' and products' side reads them.
+__device__ __forceinline__ void to_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// Two floats, for which one instruction does.
+using F2 = unsigned long long;
+__device__ __forceinline__ F2 both(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float low(F2 x) { return __uint_as_float(uint32_t(x)); }
+__device__ __forceinline__ float high(F2 x) { return __uint_as_float(uint32_t(x >> 32)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ bool elected() {
+    uint32_t r;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(r));
+    return r;
+}
+// The same in all lanes, and known to be.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(~0u, x, 0); }
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    // (Weights under 2^-126 are 0.)
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// ---------------------------------------------------------------------------
+// Results
+// ---------------------------------------------------------------------------
+
+// Eight adjacent elements of the result, as T.
+template <class T>
+__device__ __forceinline__ void put8(uint16_t* to, int d, int dim, bool vec, const float* x) {
+    if (vec && d + 8 <= dim) {
+        *reinterpret_cast<uint4*>(to + d) =
+            make_uint4(pack<T>(x[0], x[1]), pack<T>(x[2], x[3]), pack<T>(x[4], x[5]), pack<T>(x[6], x[7]));
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if (d + k < dim) to[d + k] = T::round(x[k]);
+}
+
+// Element d of row r's result, or its maximum and sum, where they belong: in `piece` if
+// that is given, else in the outputs.
+template <class K>
+struct Place {
+    float* piece;
+    uint16_t* out;
+    float* lse;
+    __device__ __forceinline__ Place(const AttendArgs& a, const Tile& t, int r, float* to) {
+        const int row = t.tile * K::kRows + r, head = t.head * a.group + row % a.group;
+        const int64_t token = t.first + row / a.group;
+        piece = to ? to + r * K::D : nullptr;
+        out = a.out + token * a.ldo + int64_t(head) * a.c.dim;
+        lse = to ? to + K::kRows * K::D + 2 * r : a.lse ? a.lse + token * a.n_q + head : nullptr;
+    }
+    __device__ __forceinline__ void element(const AttendArgs& a, int d, float x) const {
+        if (piece) piece[d] = x;
+        else if (d < a.c.dim) out[d] = K::T::round(x);
+    }
+    __device__ __forceinline__ void sums(float top, float sum) const {
+        if (piece) lse[0] = top, lse[1] = sum;
+        else if (lse) *lse = sum == 0.0f ? -kInf : (top + log2f(sum)) * kLn2;
+    }
+};
+
+// A warp joins row r of n pieces, given by at(i), in the outputs.  A piece counts by its sum
+// at the largest of the maxima.
+template <class K, class At>
+__device__ __forceinline__ void join_row(const AttendArgs& a, const Tile& t, int r, int n, At at) {
+    constexpr int kMl = K::D * K::kRows;
+    const int lane = threadIdx.x & 31;
+    float top = -kInf;
+    for (int i = lane; i < n; i += 32) top = fmaxf(top, __ldcg(at(i) + kMl + 2 * r));
+#pragma unroll
+    for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
+    const auto share = [&](int i) {
+        const float m = __ldcg(at(i) + kMl + 2 * r);
+        return m == -kInf ? 0.0f : __ldcg(at(i) + kMl + 2 * r + 1) * exp2f(m - top);
+    };
+    float sum = 0;
+    for (int i = lane; i < n; i += 32) sum += share(i);
+#pragma unroll
+    for (int m = 16; m; m >>= 1) sum += __shfl_xor_sync(~0u, sum, m);
+    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+    // 8 adjacent elements a lane; with 16 lanes' worth of them, half the lanes take every
+    // other piece.
+    constexpr int kLanes = K::D / 8, kTeams = 32 / kLanes;
+    const int d = 8 * (lane % kLanes), team = lane / kLanes;
+    float x[8] = {};
+    for (int base = 0; base < n; base += 32) {
+        const float mine = base + lane < n ? share(base + lane) * inverse : 0.0f;
+#pragma unroll 4
+        for (int k = 0; k < min(n - base, 32); k += kTeams) {
+            const int i = base + k + team;
+            const float w = __shfl_sync(~0u, mine, (k + team) & 31);
+            if (k + team >= 32 || i >= n || w == 0.0f) continue;
+            const float4* from = reinterpret_cast<const float4*>(at(i) + r * K::D + d);
+            const float4 u = __ldcg(from), v = __ldcg(from + 1);
+            x[0] = fmaf(w, u.x, x[0]), x[1] = fmaf(w, u.y, x[1]), x[2] = fmaf(w, u.z, x[2]), x[3] = fmaf(w, u.w, x[3]);
+            x[4] = fmaf(w, v.x, x[4]), x[5] = fmaf(w, v.y, x[5]), x[6] = fmaf(w, v.z, x[6]), x[7] = fmaf(w, v.w, x[7]);
+        }
+    }
+#pragma unroll
+    for (int m = kLanes; m < 32; m <<= 1) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] += __shfl_xor_sync(~0u, x[k], m);
+    }
+    if (team) return;
+    const Place<K> place(a, t, r, nullptr);
+    put8<typename K::T>(place.out, d, a.c.dim, a.ovec, x);
+    if (lane == 0) place.sums(top, sum);
+}
+
+// Keys [k0, k1) of one row once more, by one warp, one key after another, for values
+// that are not finite or nearly too large: a product of weight and value only where the
+// row sees the key, weights in float32 and 2^-32 of what they are, so that sums stay
+// finite.
+template <class K>
+__device__ __noinline__ void carefully(const AttendArgs& a, const Tile& t, int r, int k0, int k1, float* piece) {
+    using T = typename K::T;
+    constexpr int kEach = K::D / 32;
+    const int lane = threadIdx.x & 31, row = t.tile * K::kRows + r;
+    const int end = min(k1, seen(t, a.group, row));
+    const uint16_t* q = a.q + (t.first + row / a.group) * a.ldq + int64_t(t.head * a.group + row % a.group) * a.c.dim;
+    float top = -kInf, sum = 0, o[kEach] = {};
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int key0 = k0; key0 < end; key0 += 32) {
+            const int key = key0 + lane;
+            const int id = key < end ? __ldcg(&a.table[int64_t(t.slot) * a.c.max_pages + (key >> a.c.shift)]) : -1;
+            const char* at = nullptr;
+            float s = -kInf;
+            if (a.c.has_page(id)) {
+                at = a.pages + id * a.c.page_bytes + t.head * a.c.run_bytes + (key & (a.c.page - 1)) * (2 * a.c.pitch);
+                s = 0;
+                for (int d = 0; d < a.c.dim; d += 8) {
+                    const uint4 k = *reinterpret_cast<const uint4*>(at + 2 * d);
+                    const uint32_t w[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (d + e < a.c.dim) s = fmaf(T::widen(q[d + e]), T::widen(uint16_t(w[e / 2] >> (16 * (e & 1)))), s);
+                }
+                s *= a.scale;
+            }
+            if (pass == 0) {
+                top = fmaxf(top, s);
+                continue;
+            }
+            const float p = exp2f(s - (top == -kInf ? 0.0f : top));
+            sum += p;
+            float part[kEach] = {};
+            for (int x = 0; x < min(end - key0, 32); ++x) {
+                const float w = __shfl_sync(~0u, p, x) * 0x1p-32f;
+                const char* from = reinterpret_cast<const char*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(at), x));
+                if (!from) continue;
+                const uint16_t* v = reinterpret_cast<const uint16_t*>(from + int64_t(a.c.n_kv) * a.c.run_bytes);
+#pragma unroll
+                for (int e = 0; e < kEach; ++e)
+                    if (lane + 32 * e < a.c.dim) part[e] = fmaf(w, T::widen(v[lane + 32 * e]), part[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) o[e] += part[e];
+        }
+        if (pass == 0) {
+#pragma unroll
+            for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
+        }
+    }
+#pragma unroll
+    for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(~0u, sum, x);
+    const float inverse = sum == 0.0f ? 0.0f : 0x1p32f / sum;
+    const Place<K> place(a, t, r, piece);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) place.element(a, lane + 32 * e, o[e] * inverse);
+    if (lane == 0) place.sums(top, sum);
+}
+
+// ---------------------------------------------------------------------------
+// The kernel
+// ---------------------------------------------------------------------------
+
 template <class K>
 struct Shared {
-    Ends heads[K::kWarps], tails[K::kWarps];
-    int64_t scan[K::kWarps];
-    int64_t starts[K::kWarps];       // where a warp's run begins within its first sequence
-    int seqs[K::kWarps];
-    int last;
-    Tile ring[K::kWarps][4];
+    uint64_t full[kMostStages], empty[kMostStages];   // of the ring's stages
+    uint64_t scores[2], weights, sums;                // S^T is there (two of them, in turn); P^T; D^T
+    uint64_t q_full[2], q_free[2];                    // a tile's queries and all that is said of it below
+    Item items[2];
+    alignas(16) int seen[2][K::kRows];
+    int64_t out[2][K::kRows];                         // where a row's result begins
+    // Of a row: what a score has added before its exponential; what sums are multiplied by
+    // when that moves; 1 / the sum of weights.
+    alignas(16) float zero[8], bias[K::kRows], factor[K::kRows], inverse[K::kRows];
+    float parts[4][K::kRows];
+    int64_t scan[kThreads / 32];
+    int64_t start;                                    // where the block's run begins within its first sequence
+    int seq;                                          // that sequence
+    int quit, last;
+    uint32_t tmem;
+};
+
+// Eight rows' values, one a lane each, over the warp's lanes: lane l ends with row
+// 4 (l / 16) + 2 (l / 8 % 2) + l / 4 % 2 of them.
+template <class F>
+__device__ __forceinline__ float over_lanes(const F2* pairs, F f) {
+    const int lane = threadIdx.x & 31;
+    const float x[8] = {low(pairs[0]), high(pairs[0]), low(pairs[1]), high(pairs[1]), low(pairs[2]), high(pairs[2]), low(pairs[3]), high(pairs[3])};
+    float a[4], b[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float keep = lane & 16 ? x[i + 4] : x[i], give = lane & 16 ? x[i] : x[i + 4];
+        a[i] = f(keep, __shfl_xor_sync(~0u, give, 16));
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float keep = lane & 8 ? a[i + 2] : a[i], give = lane & 8 ? a[i] : a[i + 2];
+        b[i] = f(keep, __shfl_xor_sync(~0u, give, 8));
+    }
+    const float keep = lane & 4 ? b[1] : b[0], give = lane & 4 ? b[0] : b[1];
+    float c = f(keep, __shfl_xor_sync(~0u, give, 4));
+    c = f(c, __shfl_xor_sync(~0u, c, 2));
+    return f(c, __shfl_xor_sync(~0u, c, 1));
+}
+__device__ __forceinline__ int row_of_lane() { return (threadIdx.x >> 4 & 1) * 4 + (threadIdx.x >> 3 & 1) * 2 + (threadIdx.x >> 2 & 1); }
+
+// A place in the ring, and the parity of its turn.
+struct Stage {
+    int at = 0, turn = 0;
+    __device__ __forceinline__ void next(int stages) {
+        if (++at == stages) at = 0, turn ^= 1;
+    }
 };
 
 template <class K>
-__global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
     using T = typename K::T;
-    constexpr int C = K::C, NT = K::NT, W = K::kWarps;
-    extern __shared__ __align__(128) char memory[];
+    constexpr int NG = K::NG, MT = K::MT, N = K::kRows;
+    extern __shared__ char memory[];
     __shared__ Shared<K> sh;
     after_previous();
     if (__ldcg(&a.control[kState])) return;
-    const int lane = threadIdx.x & 31, g = lane >> 2, c4 = lane & 3, w = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
 
-    // The line, and where this block's warps begin in it.
+    // The line, and where this block's run begins in it.
     Line line;
-    int64_t mine = 0;
-    int64_t kept = 0;
-    for (int i = threadIdx.x; i < a.n; i += K::kThreads) {
-        int slot, length, first, count;
-        load_seq(a, i, &slot, &length, &first, &count);
-        kept = work_of<K>(a, length, count);
-        mine += kept;
-    }
-    const auto scan = [&](int64_t v, int64_t* total) {
-        int64_t s = v;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int64_t o = __shfl_up_sync(~0u, s, d);
-            if (lane >= d) s += o;
-        }
-        if (lane == 31) sh.scan[w] = s;
-        __syncthreads();
-        int64_t before = 0, all = 0;
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if (i < w) before += sh.scan[i];
-            all += sh.scan[i];
-        }
-        __syncthreads();
-        *total = all;
-        return before + s - v;
-    };
-    scan(mine, &line.total);
-    if (line.total == 0) return;
-    // Blocks of a few units a warp where there are few.
-    constexpr int kLeast = 2 * W;
-    const int blocks = int(min(int64_t(gridDim.x), (line.total + kLeast - 1) / kLeast));
-    if (int(blockIdx.x) >= blocks) return;
-    line.workers = int(min(int64_t(blocks) * W, line.total));      // (so that none is without units between others)
-    const int worker = blockIdx.x * W + w;
+    int64_t begin, end;
     {
-        int64_t before = 0;
-        const int64_t last = line.begin(blockIdx.x * W + W - 1);
-        for (int base = 0; base < a.n && before <= last; base += K::kThreads) {
-            const int i = base + int(threadIdx.x);
-            int64_t work = kept;
-            if (a.n > K::kThreads) {
-                int slot, length, first, count;
-                work = 0;
-                if (i < a.n) {
-                    load_seq(a, i, &slot, &length, &first, &count);
-                    work = work_of<K>(a, length, count);
-                }
-            }
-            int64_t total;
-            const int64_t at = before + scan(work, &total);
+        const auto scan = [&](int64_t v, int64_t* total) {
+            int64_t s = v;
 #pragma unroll
-            for (int x = 0; x < W; ++x) {
-                const int64_t u = line.begin(blockIdx.x * W + x);
-                if (u >= at && u < at + work) {
-                    sh.seqs[x] = i;
-                    sh.starts[x] = u - at;
-                }
+            for (int d = 1; d < 32; d <<= 1) {
+                const int64_t o = __shfl_up_sync(~0u, s, d);
+                if (lane >= d) s += o;
+            }
+            if (lane == 31) sh.scan[w] = s;
+            __syncthreads();
+            int64_t before = 0, all = 0;
+#pragma unroll
+            for (int i = 0; i < kThreads / 32; ++i) {
+                if (i < w) before += sh.scan[i];
+                all += sh.scan[i];
+            }
+            __syncthreads();
+            *total = all;
+            return before + s - v;
+        };
+        const auto work = [&](int i) -> int64_t {
+            if (i >= a.n) return 0;
+            int slot, length, first, count;
+            load_seq(a, i, &slot, &length, &first, &count);
+            return work_of<K>(a, length, count);
+        };
+        int64_t mine = 0, kept = 0;
+        for (int i = threadIdx.x; i < a.n; i += kThreads) mine += kept = work(i);
+        int64_t at = scan(mine, &line.total);
+        if (line.total == 0) return;
+        line.blocks = int(min(int64_t(gridDim.x), line.total));
+        if (int(blockIdx.x) >= line.blocks) return;
+        begin = line.begin(blockIdx.x), end = line.begin(blockIdx.x + 1);
+        int64_t before = 0;
+        for (int base = 0; base < a.n && before <= begin; base += kThreads) {
+            int64_t total = line.total;
+            if (a.n > kThreads) {
+                kept = work(base + int(threadIdx.x));
+                at = before + scan(kept, &total);
+            }
+            if (begin >= at && begin < at + kept) {
+                sh.seq = base + int(threadIdx.x);
+                sh.start = begin - at;
             }
             before += total;
         }
-        if (lane == 0) sh.heads[w].begin = sh.tails[w].begin = -1;
-        __syncthreads();
     }
 
-    char* const own = memory + w * K::kWarpBytes;
-    const uint32_t q_at = uint32_t(__cvta_generic_to_shared(own)), stage_at = q_at + K::kQ;
-    const int64_t begin = line.begin(worker), end = line.begin(worker + 1);
-    if (begin < end) {
-        // The copies' side: iteration `made` is the next whose keys are asked for.
-        Walk<K> walk(a, sh.seqs[w]);
-        walk.enter();
-        int unit;                        // of the walk's tile: the next iteration's
-        {
-            const int64_t at = sh.starts[w], tile = at / walk.t.units;
-            const int tiles = tiles_of<K>(a, walk.t.count);
-            unit = int(at - tile * walk.t.units);
-            walk.t.head = int(tile / tiles);
-            walk.t.tile = int(tile % tiles);
+    const uint32_t ring = (smem_of(memory) + 1023) / 1024 * 1024, stage_bytes = a.atoms * 16384;
+    const uint32_t q_at = ring + a.stages * stage_bytes, p_at = q_at + 2 * K::kQ;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.stages; ++i) {
+            bar_init(smem_of(&sh.full[i]), 1);
+            bar_init(smem_of(&sh.empty[i]), 1);
         }
-        const int64_t first_tile = begin - unit;      // the first tile's begin in the line
-        const int first_unit = unit;
-        int64_t made = begin;
-        int ids = -1;                    // lane h < 4: the page of the next iteration's tokens 8 h on
-        const auto fetch_ids = [&] {
-            ids = -1;
-            const int key = unit * kUnit + 8 * lane;
-            if (made < end && lane < 4 && key < walk.t.length) {
-                ids = __ldg(&a.table[int64_t(walk.t.slot) * a.c.max_pages + (key >> a.c.shift)]);
-                if (!a.c.has_page(ids)) {
-                    ids = -1;
-                    atomicOr(&a.control[kLate], kBadTable);
-                }
-            }
-        };
-        fetch_ids();
-        const char* at[4];               // the tokens whose values are asked for next
-        int valid[4];                    // how many of the 8 there are
-        uint32_t stage_in = stage_at, stage_out = stage_at;
-        const auto step = [&](uint32_t* s) {
-            *s += K::kStage;
-            if (*s == stage_at + K::kStages * K::kStage) *s = stage_at;
-        };
-        const int64_t to_values = int64_t(a.c.n_kv) * a.c.run_bytes;
-        const int row_bytes = 2 * a.c.pitch, dim_bytes = 2 * a.c.dim;
-        const auto ask_keys = [&] {
-            if (made < end) {
-                if (lane == 0) sh.ring[w][made & 3] = walk.t;
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const int key = unit * kUnit + 8 * h, id = __shfl_sync(~0u, ids, h);
-                    valid[h] = id < 0 ? 0 : min(walk.t.length - key, 8);
-                    at[h] = id < 0 ? a.pages
-                                   : a.pages + id * a.c.page_bytes + walk.t.head * a.c.run_bytes + (key & (a.c.page - 1)) * row_bytes;
-                }
-#pragma unroll
-                for (int k = 0; k < 2 * C; ++k) {
-                    const int d = 64 * k + 16 * c4, bytes = min(max(dim_bytes - d, 0), 16);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        const bool there = g < valid[h] && bytes;
-                        copy_async(stage_in + (k * 4 + h) * 512 + lane * 16, there ? at[h] + g * row_bytes + d : a.pages, there ? bytes : 0);
-                    }
-                }
-                // On to the next iteration, but for what the values need.
-                ++made;
-                if (++unit == walk.t.units) {
-                    unit = 0;
-                    if (made < end) walk.next();
-                }
-                fetch_ids();
-            } else {
-#pragma unroll
-                for (int h = 0; h < 4; ++h) valid[h] = -1;
-            }
-            copies_end();
-            step(&stage_in);
-        };
-        const auto ask_values = [&] {
-            if (valid[0] >= 0) {
-#pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    const int d = 128 * c + 16 * g, bytes = min(max(dim_bytes - d, 0), 16);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const bool there = 2 * c4 + e < valid[h] && bytes;
-                            copy_async(stage_in + (c * 8 + h * 2 + e) * 512 + lane * 16,
-                                       there ? at[h] + to_values + (2 * c4 + e) * row_bytes + d : a.pages, there ? bytes : 0);
-                        }
-                    }
-                }
-            }
-            copies_end();
-            step(&stage_in);
-        };
-        bool keys_next = true;
-        const auto ask = [&] {
-            if (keys_next) ask_keys();
-            else ask_values();
-            keys_next = !keys_next;
-        };
-#pragma unroll
-        for (int i = 0; i < K::kStages; ++i) ask();
+        for (int i = 0; i < 2; ++i) {
+            bar_init(smem_of(&sh.scores[i]), 1);
+            bar_init(smem_of(&sh.q_full[i]), 1);
+            bar_init(smem_of(&sh.q_free[i]), kSoft / 32);
+        }
+        bar_init(smem_of(&sh.weights), kSoft / 32);
+        bar_init(smem_of(&sh.sums), 1);
+        sh.quit = 0;
+        for (int i = 0; i < 8; ++i) sh.zero[i] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (w == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_of(&sh.tmem)), "n"(K::kColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tmem_before();
+    __syncthreads();
+    tmem_after();
+    const uint32_t tmem = sh.tmem;
+    const int64_t n = end - begin;
+    const auto wait = [&](uint64_t& bar, int parity) { return bar_wait(smem_of(&bar), parity, &sh.quit, a.control); };
 
-        // The products' side.
-        float o[NT][C][4][4], top[NT][2], sum[NT][2];
-        uint4 q1[NT == 1 ? 2 * C : 1];
-        Tile t;
-        int u = 0, u0 = 0;
-        int64_t tile_begin = 0;
-        bool fresh = true;
+    // The walk's first tile and unit.
+    const auto enter = [&](Walk<K>& walk) {
+        walk.enter();
+        const int64_t at = sh.start, tile = at / walk.t.units;
+        const int tiles = tiles_of<K>(a, walk.t.count);
+        walk.t.head = int(tile / tiles);
+        walk.t.tile = int(tile % tiles);
+        return int(at - tile * walk.t.units);
+    };
+
+    if (w == 8) {
+        // Copies.
+        Walk<K> walk(a, sh.seq);
+        int unit = enter(walk);
+        const int tokens = a.c.page, pages = kUnit >> a.c.shift;
+        const auto fetch = [&] {
+            const int key = unit * kUnit + lane * tokens;
+            if (lane >= pages || key >= walk.t.length) return -1;
+            const int id = __ldg(&a.table[int64_t(walk.t.slot) * a.c.max_pages + (key >> a.c.shift)]);
+            if (a.c.has_page(id)) return id;
+            atomicOr(&a.control[kLate], kBadTable);
+            return -1;
+        };
+        Stage s;
+        int asked = 0;
+        const auto load = [&](int id, int head) {
+            if (!__all_sync(~0u, wait(sh.empty[s.at], s.turn ^ 1))) return false;
+            const uint32_t bar = smem_of(&sh.full[s.at]);
+            const int there = __popc(__ballot_sync(~0u, id >= 0));
+            if (lane == 0) bar_expect(bar, uint32_t(there * a.atoms * tokens * 128));
+            __syncwarp();
+            if (id >= 0)
+                for (int x = 0; x < a.atoms; ++x)
+                    tma_load(ring + s.at * stage_bytes + x * 16384 + lane * tokens * 128, &map, 64 * x, 0, head, id, bar);
+            s.next(a.stages);
+            asked = min(asked + 1, a.stages);
+            return true;
+        };
+        int id = fetch(), head = walk.t.head, last_id = -1, last_head = 0;
+        bool ok = true;
+        for (int64_t i = 0; ok && i <= n; ++i) {
+            int next_id = -1, next_head = 0;
+            if (i < n) {
+                ok = load(id, head);
+                if (i + 1 < n) {
+                    if (++unit == walk.t.units) {
+                        unit = 0;
+                        walk.next();
+                    }
+                    next_id = fetch();
+                    next_head = walk.t.head;
+                }
+            }
+            if (ok && i > 0) ok = load(last_id, a.c.n_kv + last_head);
+            last_id = id, last_head = head;
+            id = next_id, head = next_head;
+        }
+        if (!ok) {
+            // What is on its way has to land before the block ends.
+            for (int k = 0; k < asked; ++k) {
+                // (From the last one back.)
+                if (--s.at < 0) s.at = a.stages - 1, s.turn ^= 1;
+                for (int x = 0; x < 1 << 20 && !bar_try(smem_of(&sh.full[s.at]), s.turn); ++x) {}
+            }
+        }
+    } else if (w == 9) {
+        // Products.  (All lanes go along; one of them issues.)
+        const int k16 = (a.c.dim + 15) / 16;
+        // The ring's order: K0 K1 V0 K2 V1 ...
+        Stage st;
+        int q_item = 0, v_item = 0, q_left = 0, v_left = 0, v_unit = 0, v_length = 0;
+        uint32_t q_instr = 0, v_instr = 0;
+        const auto columns = [&](const Tile& t) { return uniform(min((t.count * a.group - t.tile * K::kRows + 15) / 16 * 16, N)); };
+        const uint32_t first_tmem = uniform(tmem);
+        const int units = int(n);
+        for (int i = 0; i <= units; ++i) {
+            if (i < units) {
+                const int slot = q_item & 1;
+                if (q_left == 0) {
+                    if (!__all_sync(~0u, wait(sh.q_full[slot], q_item >> 1 & 1))) break;
+                    q_left = uniform(sh.items[slot].n);
+                    q_instr = instruction<T>(columns(sh.items[slot].t), false, false);
+                }
+                if (!__all_sync(~0u, wait(sh.full[st.at], st.turn))) break;
+                tmem_after();
+                if (elected()) {
+                    // (A descriptor's address counts 16 bytes.)
+                    const uint64_t dk = descriptor(ring + st.at * stage_bytes, 16, 1024, 2), dq = descriptor(q_at + slot * K::kQ, N * 16, 128, 0);
+#pragma unroll 1
+                    for (int j = 0; j < k16; ++j)
+                        product(first_tmem + uint32_t(i & 1) * N, dk + (j >> 2) * 1024 + (j & 3) * 2, dq + j * (2 * N), q_instr, j > 0);
+                    products_arrive(smem_of(&sh.empty[st.at]));
+                    products_arrive(smem_of(&sh.scores[i & 1]));
+                }
+                st.next(a.stages);
+                if (--q_left == 0) ++q_item;
+            }
+            if (i > 0) {
+                if (v_left == 0) {
+                    const Item& item = sh.items[v_item & 1];
+                    v_left = uniform(item.n);
+                    v_unit = uniform(item.first);
+                    v_length = uniform(item.t.length);
+                    v_instr = instruction<T>(columns(item.t), true, true);
+                    ++v_item;
+                }
+                if (!__all_sync(~0u, wait(sh.full[st.at], st.turn))) break;
+                if (!__all_sync(~0u, wait(sh.weights, (i - 1) & 1))) break;
+                tmem_after();
+                const int steps = max((min(v_length - v_unit * kUnit, kUnit) + 15) / 16, 1);
+                if (elected()) {
+                    const uint64_t dv = descriptor(ring + st.at * stage_bytes, 16384, 1024, 2), dp = descriptor(p_at, 128, 2048, 0);
+#pragma unroll 1
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll 1
+                        for (int part = K::kParts - 1; part >= 0; --part)
+#pragma unroll 1
+                            for (int j = 0; j < steps; ++j)
+                                product(first_tmem + (2 + m) * N, dv + m * 2048 + j * 128, dp + part * (K::kP / 16) + j * 16, v_instr,
+                                        j > 0 || part < K::kParts - 1);
+                    products_arrive(smem_of(&sh.empty[st.at]));
+                    products_arrive(smem_of(&sh.sums));
+                }
+                st.next(a.stages);
+                ++v_unit;
+                --v_left;
+            }
+        }
         __syncwarp();
-        for (int64_t done = begin; done < end; ++done) {
-            if (fresh) {
-                __syncwarp();
-                t = sh.ring[w][done & 3];
-                u = u0 = done == begin ? first_unit : 0;
-                tile_begin = done == begin ? first_tile : done;
+    } else if (w == 10) {
+        // Queries, and what the others need to know of a tile.
+        Walk<K> walk(a, sh.seq);
+        int unit = enter(walk);
+        int64_t at = begin;
+        const int chunks = (a.c.dim + 15) / 16 * 2;
+        for (int64_t item = 0; at < end; ++item) {
+            const int slot = int(item & 1);
+            if (!__all_sync(~0u, wait(sh.q_free[slot], int(item >> 1 & 1) ^ 1))) break;
+            const Tile& t = walk.t;
+            const int left = min(t.count * a.group - t.tile * K::kRows, K::kRows), rows = (left + 15) / 16 * 16;
+            const uint32_t to = q_at + slot * K::kQ;
+            for (int base = 0; base < rows * chunks; base += 8 * 32) {
+                uint4 x[8];
+                uint32_t where[8];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    top[nt][0] = top[nt][1] = -kInf;
-                    sum[nt][0] = sum[nt][1] = 0;
+                for (int e = 0; e < 8; ++e) {
+                    const int i = base + 32 * e + lane, r = i / chunks, c = i - r * chunks, d = 8 * c, row = t.tile * K::kRows + r;
+                    where[e] = i < rows * chunks ? to + c * (N * 16) + r * 16 : 0;
+                    x[e] = make_uint4(0, 0, 0, 0);
+                    if (r >= left || d >= a.c.dim || i >= rows * chunks) continue;
+                    const uint16_t* from = a.q + (t.first + row / a.group) * a.ldq + int64_t(t.head * a.group + row % a.group) * a.c.dim + d;
+                    if (a.qvec) {
+                        x[e] = *reinterpret_cast<const uint4*>(from);
+                    } else {
+                        uint32_t v[8];
 #pragma unroll
-                    for (int c = 0; c < C; ++c)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[nt][c][i][e] = 0;
-#pragma unroll
-                    for (int k = 0; k < 2 * C; ++k) {
-                        const uint4 x = load_q<K>(a, t, nt, k);
-                        if (NT == 1) q1[k] = x;
-                        else sts(q_at + (nt * 2 * C + k) * 512 + lane * 16, x);
+                        for (int k = 0; k < 8; ++k) v[k] = d + k < a.c.dim ? from[k] : 0u;
+                        x[e] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
                     }
                 }
-                fresh = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (where[e])
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(where[e]), "r"(x[e].x), "r"(x[e].y), "r"(x[e].z), "r"(x[e].w)
+                                     : "memory");
             }
-            const int key0 = u * kUnit;
-            float s[2][NT][4];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[h][nt][e] = 0;
-            copies_wait<K::kStages - 1>();
-#pragma unroll
-            for (int k = 0; k < 2 * C; ++k) {
-                uint4 r[4];
-#pragma unroll
-                for (int h = 0; h < 4; ++h) r[h] = lds(stage_out + (k * 4 + h) * 512 + lane * 16);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const uint4 b = NT == 1 ? q1[NT == 1 ? k : 0] : lds(q_at + (nt * 2 * C + k) * 512 + lane * 16);
-                    mma<T>(s[0][nt], r[0].x, r[1].x, r[0].y, r[1].y, b.x, b.y);
-                    mma<T>(s[1][nt], r[2].x, r[3].x, r[2].y, r[3].y, b.x, b.y);
-                    mma<T>(s[0][nt], r[0].z, r[1].z, r[0].w, r[1].w, b.z, b.w);
-                    mma<T>(s[1][nt], r[2].z, r[3].z, r[2].w, r[3].w, b.z, b.w);
-                }
+            for (int r = lane; r < N; r += 32) {
+                const int row = t.tile * K::kRows + r, token = row / a.group;
+                sh.seen[slot][r] = r < left ? t.length - t.count + 1 + token : 0;
+                sh.out[slot][r] = (t.first + token) * a.ldo + int64_t(t.head * a.group + row - token * a.group) * a.c.dim;
             }
-            step(&stage_out);
-            ask();
-
-            // Weights 2^(s - top + lift); `top` moves only where a score is far over it.
-            bool far = false;
+            const int units = int(min(int64_t(t.units - unit), end - at));
+            if (lane == 0) {
+                Item& it = sh.items[slot];
+                it.t = t;
+                it.first = unit;
+                it.n = units;
+                it.begin = at - unit;
+            }
+            to_async();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_of(&sh.q_full[slot]));
+            at += units;
+            unit = 0;
+            if (at < end) walk.next();
+        }
+    } else {
+        // Softmax and sums.  Lane l of warp w has key, or element, 32 (w % 4) + l; warps 0..3 take
+        // the even groups of 8 rows, warps 4..7 the odd ones (MT 2: of the sums, elements 128 on).
+        constexpr int GS = (NG + 1) / 2, GO = MT == 1 ? GS : NG;
+        const int set = w >> 2, key = threadIdx.x & 127;
+        const uint32_t lanes = uint32_t(w & 3) << 21;
+        const auto group_of = [&](int j) { return set + 2 * j; };
+        const F2 scale2 = both(a.scale, a.scale);
+        const auto sum_group = [&](int j) { return MT == 1 ? set + 2 * j : j; };
+        int64_t i = 0;
+        bool over = false;
+        for (int64_t item = 0; i < n && !over; ++item) {
+            const int slot = int(item & 1);
+            bool ok = __all_sync(~0u, wait(sh.q_full[slot], int(item >> 1 & 1)));
+            const Item it = sh.items[slot];
+            const int left = ok ? min(it.t.count * a.group - it.t.tile * K::kRows, K::kRows) : 0, groups = (left + 7) / 8;
+            const int units = ok ? it.n : 1, first_seen = seen(it.t, a.group, it.t.tile * K::kRows);
+            F2 o[GO][4], sum[GS][4];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int j = 0; j < GO; ++j)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int e = 0; e < 4; ++e) o[j][e] = 0;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[h][nt][e] *= a.scale;
-            if (key0 + kUnit > seen(t, a.group, t.tile * K::kRows)) mask<K>(a, t, key0, s);
+            for (int j = 0; j < GS; ++j)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int e = 0; e < 4; ++e) sum[j][e] = 0;
+            // (The first scores are over any reference: it is set then.)
+            if (int(threadIdx.x) < N) sh.bias[threadIdx.x] = kNothing;
+            soft_sync();
+            const auto add_sums = [&] {
+                // (Two groups at a time: registers are short.)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float m = fmaxf(fmaxf(s[0][nt][e], s[0][nt][2 + e]), fmaxf(s[1][nt][e], s[1][nt][2 + e]));
-                    far |= m > top[nt][e] + kSlack;
-                }
-            if (__any_sync(~0u, far)) {
+                for (int j = 0; j < GO; j += 2) {
+                    F2 x[2][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                    for (int k = 0; k < 2; ++k)
+                        if (j + k < GO && sum_group(j + k) < groups)
+                            tmem_load(tmem + lanes + (2 + (MT == 2 ? set : 0)) * N + 8 * sum_group(j + k), x[k]);
+                    tmem_loaded();
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float m = fmaxf(fmaxf(s[0][nt][e], s[0][nt][2 + e]), fmaxf(s[1][nt][e], s[1][nt][2 + e]));
+                    for (int k = 0; k < 2; ++k) {
+                        if (j + k >= GO || sum_group(j + k) >= groups) continue;
 #pragma unroll
-                        for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, x));
-                        m = fmaxf(m, top[nt][e]);
-                        const float f = m == top[nt][e] ? 1.0f : exp2f(top[nt][e] - m);
-                        top[nt][e] = m;
-                        sum[nt][e] *= f;
-#pragma unroll
-                        for (int c = 0; c < C; ++c)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                o[nt][c][i][e] *= f;
-                                o[nt][c][i][2 + e] *= f;
-                            }
+                        for (int e = 0; e < 4; ++e) o[j + k < GO ? j + k : 0][e] = add2(o[j + k < GO ? j + k : 0][e], x[k][e]);
                     }
-            }
-            uint32_t p[K::kParts][2][NT][2];
+                }
+            };
+            for (int u = 0; u < units; ++u, ++i) {
+                const int key0 = (it.first + u) * kUnit;
+                ok &= __all_sync(~0u, wait(sh.scores[i & 1], int(i >> 1 & 1)));
+                tmem_after();
+                F2 s[GS][4];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const float m0 = top[nt][0] == -kInf ? 0.0f : top[nt][0] - K::kLift, m1 = top[nt][1] == -kInf ? 0.0f : top[nt][1] - K::kLift;
+                for (int j = 0; j < GS; ++j)
+                    if (group_of(j) < groups) tmem_load(tmem + lanes + uint32_t(i & 1) * N + 8 * group_of(j), s[j]);
+                tmem_loaded();
+                // Which keys the rows see, where that is not all.
+                const bool edge = key0 + kUnit > first_seen;
+                uint32_t sees[GS];
+                if (edge) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                    for (int j = 0; j < GS; ++j) {
+                        if (group_of(j) >= groups) continue;
+                        sees[j] = 0;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sees[j] |= uint32_t(key0 + key < sh.seen[slot][8 * group_of(j) + e]) << e;
+                    }
+                }
+                // Weights are 2^x, x = scale s - reference.
+                const auto refer = [&](int j, F2* x, const float* from) {
+                    const float4* const bias = reinterpret_cast<const float4*>(from);
+                    const float4 b0 = bias[0], b1 = bias[1];
+                    x[0] = fma2(s[j][0], scale2, both(b0.x, b0.y));
+                    x[1] = fma2(s[j][1], scale2, both(b0.z, b0.w));
+                    x[2] = fma2(s[j][2], scale2, both(b1.x, b1.y));
+                    x[3] = fma2(s[j][3], scale2, both(b1.z, b1.w));
+                    if (edge) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            x[e] = both(sees[j] >> (2 * e) & 1 ? low(x[e]) : -kInf, sees[j] >> (2 * e + 1) & 1 ? high(x[e]) : -kInf);
+                    }
+                };
+                float most = -kInf;
+#pragma unroll
+                for (int j = 0; j < GS; ++j) {
+                    if (group_of(j) >= groups) continue;
+                    F2 x[4];
+                    refer(j, x, &sh.bias[8 * group_of(j)]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(low(x[e]), high(x[e])));
+                }
+                const bool moved = soft_any(!ok || most > kSlack + K::kLift);
+                if (moved) {
+                    if (soft_any(!ok || *(volatile int*)&sh.quit)) {
+                        over = true;
+                        break;
+                    }
+#pragma unroll
+                    for (int j = 0; j < GS; ++j) {
+                        if (group_of(j) >= groups) continue;
+                        F2 y[4];
+                        refer(j, y, sh.zero);
+                        const float m = over_lanes(y, [](float p, float q) { return fmaxf(p, q); });
+                        if ((lane & 3) == 0) sh.parts[w & 3][8 * group_of(j) + row_of_lane()] = m;
+                    }
+                    soft_sync();
+                    if (int(threadIdx.x) < 8 * groups) {
+                        const int r = threadIdx.x;
+                        const float m = fmaxf(fmaxf(sh.parts[0][r], sh.parts[1][r]), fmaxf(sh.parts[2][r], sh.parts[3][r]));
+                        const float before = sh.bias[r], after = m == -kInf ? kNothing : K::kLift - m;
+                        const bool moves = after < before;
+                        sh.factor[r] = moves ? exp2f(after - before) : 1.0f;
+                        if (moves) sh.bias[r] = after;
+                    }
+                    soft_sync();
+#pragma unroll
+                    for (int j = 0; j < GS; ++j) {
+                        if (group_of(j) >= groups) continue;
+                        const F2* const f = reinterpret_cast<const F2*>(&sh.factor[8 * group_of(j)]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sum[j][e] = mul2(sum[j][e], f[e]);
+                    }
+                }
+                uint32_t p[GS][K::kParts][4];
+#pragma unroll
+                for (int j = 0; j < GS; ++j) {
+                    if (group_of(j) >= groups) continue;
+                    F2 x[4];
+                    refer(j, x, &sh.bias[8 * group_of(j)]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        s[h][nt][e] = exp2f(s[h][nt][e] - (e & 1 ? m1 : m0));
-                        sum[nt][e & 1] += s[h][nt][e];
-                    }
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const float lo = s[h][nt][2 * x], hi = s[h][nt][2 * x + 1];
+                        const float lo = exp2_fast(low(x[e])), hi = exp2_fast(high(x[e]));
+                        const F2 y = both(lo, hi);
+                        sum[j][e] = add2(sum[j][e], y);
                         const uint32_t big = pack<T>(lo, hi);
-                        p[0][h][nt][x] = transposed(big);
-                        if (K::kParts == 2)
-                            p[K::kParts - 1][h][nt][x] = transposed(pack<T>(lo - T::widen(uint16_t(big)), hi - T::widen(uint16_t(big >> 16))));
-                    }
-                }
-            }
-
-            // Sums over 32 keys from zero by the matrix instructions, which cut off, added in
-            // float32, which rounds.
-            copies_wait<K::kStages - 1>();
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint2 v[8];
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) v[x] = lds2(stage_out + (c * 8 + x) * 512 + lane * 16 + half * 8);
-#pragma unroll
-                    for (int i2 = 0; i2 < 2; ++i2) {
-                        uint32_t f[2][4];
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint32_t v0 = i2 ? v[4 * h].y : v[4 * h].x, v1 = i2 ? v[4 * h + 1].y : v[4 * h + 1].x;
-                            const uint32_t v2 = i2 ? v[4 * h + 2].y : v[4 * h + 2].x, v3 = i2 ? v[4 * h + 3].y : v[4 * h + 3].x;
-                            f[h][0] = __byte_perm(v0, v1, 0x5410);
-                            f[h][1] = __byte_perm(v0, v1, 0x7632);
-                            f[h][2] = __byte_perm(v2, v3, 0x5410);
-                            f[h][3] = __byte_perm(v2, v3, 0x7632);
-                        }
-                        const int i = 2 * half + i2;
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            float d[4] = {0, 0, 0, 0};
-#pragma unroll
-                            for (int part = K::kParts - 1; part >= 0; --part)
-#pragma unroll
-                                for (int h = 0; h < 2; ++h)
-                                    mma<T>(d, f[h][0], f[h][1], f[h][2], f[h][3], p[part][h][nt][0], p[part][h][nt][1]);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[nt][c][i][e] += d[e];
+                        p[j][0][e] = big;
+                        if (K::kParts == 2) {
+                            const F2 rest = fma2(both(T::widen(uint16_t(big)), T::widen(uint16_t(big >> 16))), both(-1.0f, -1.0f), y);
+                            p[j][K::kParts - 1][e] = pack<T>(low(rest), high(rest));
                         }
                     }
                 }
-            }
-            step(&stage_out);
-            ask();
-
-            ++u;
-            if (u < t.units && done + 1 < end) continue;
-            // The run leaves this tile.
-            float* piece = nullptr;
-            const bool ends = u == t.units, whole = ends && tile_begin >= begin;
-            if (!whole && ends) piece = a.pieces + worker * a.piece_floats;
-            if (!ends) {
-                // The stages are free: nothing is asked for any more.
-                copies_wait<0>();
+                // The sums of the unit before, which refer to the reference before; then the weights
+                // may be overwritten.
+                if (u > 0) {
+                    wait(sh.sums, int((i - 1) & 1));
+                    tmem_after();
+                    add_sums();
+                }
+                if (moved) {
+#pragma unroll
+                    for (int j = 0; j < GO; ++j) {
+                        if (sum_group(j) >= groups) continue;
+                        const F2* const f = reinterpret_cast<const F2*>(&sh.factor[8 * sum_group(j)]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[j][e] = mul2(o[j][e], f[e]);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < GS; ++j) {
+                    if (group_of(j) >= groups) continue;
+#pragma unroll
+                    for (int x = 0; x < K::kParts; ++x)
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_at + x * K::kP + group_of(j) * 2048 + key * 16),
+                                     "r"(p[j][x][0]), "r"(p[j][x][1]), "r"(p[j][x][2]), "r"(p[j][x][3])
+                                     : "memory");
+                }
+                const int valid = min(it.t.length - key0, kUnit);
+                if (valid < kUnit) {
+                    // Behind the sequence's end the page holds anything: values there become 0.
+                    const int64_t k = i + 1 < n ? 2 * i + 2 : 2 * i + 1;      // in the ring's order
+                    const int stage = int(k % a.stages);
+                    wait(sh.full[stage], int(k / a.stages & 1));
+                    const int rows = max((valid + 15) / 16 * 16, 16) - valid;
+                    for (int x = threadIdx.x; x < rows * a.atoms * 8; x += kSoft) {
+                        const int atom = x / (rows * 8), y = x - atom * (rows * 8);
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(ring + stage * stage_bytes + atom * 16384 + valid * 128 + y * 16), "r"(0)
+                                     : "memory");
+                    }
+                }
+                to_async();
+                tmem_before();
                 __syncwarp();
-                piece = reinterpret_cast<float*>(own);
+                if (lane == 0) bar_arrive(smem_of(&sh.weights));
             }
-            if (lane == 0 && !whole) {
-                Ends& e = ends ? sh.heads[w] : sh.tails[w];
-                e.begin = tile_begin;
-                e.end = tile_begin + t.units;
-                e.t = t;
+            if (over) break;
+
+            // The run leaves the tile.
+            __syncwarp();
+            wait(sh.sums, int((i - 1) & 1));
+            tmem_after();
+            __syncwarp();
+            add_sums();
+#pragma unroll
+            for (int j = 0; j < GS; ++j) {
+                if (group_of(j) >= groups) continue;
+                const float m = over_lanes(sum[j], [](float x, float y) { return x + y; });
+                if ((lane & 3) == 0) sh.parts[w & 3][8 * group_of(j) + row_of_lane()] = m;
             }
+            soft_sync();
+            const bool starts = it.first == 0, ends = it.first + it.n == it.t.units;
+            float* const piece = starts && ends ? nullptr : a.pieces + (2 * int64_t(blockIdx.x) + starts) * a.piece_floats;
+            if (int(threadIdx.x) < left) {
+                const int r = threadIdx.x;
+                const float total = sh.parts[0][r] + sh.parts[1][r] + sh.parts[2][r] + sh.parts[3][r], bias = sh.bias[r];
+                // (A row whose sum is NaN is all NaN in any case.)
+                sh.inverse[r] = total == 0.0f ? 0.0f : 1.0f / total;
+                Place<K>(a, it.t, r, piece).sums(bias == kNothing ? -kInf : -bias, total);
+            }
+            soft_sync();
+            const int d = key + (MT == 2 ? 128 * set : 0);
             bool odd = false;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int j = 0; j < GO; ++j) {
+                if (sum_group(j) >= groups) continue;
+                const F2* const f = reinterpret_cast<const F2*>(&sh.inverse[8 * sum_group(j)]);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                    for (int x = 4; x < 32; x <<= 1) sum[nt][e] += __shfl_xor_sync(~0u, sum[nt][e], x);
-                    const float inverse = sum[nt][e] == 0.0f ? 0.0f : 1.0f / sum[nt][e];
-#pragma unroll
-                    for (int c = 0; c < C; ++c)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            o[nt][c][i][e] *= inverse;
-                            o[nt][c][i][2 + e] *= inverse;
-                            // (A row whose sum is NaN is all NaN in any case.)
-                            odd |= sum[nt][e] == sum[nt][e] && !(fabsf(o[nt][c][i][e]) < kInf && fabsf(o[nt][c][i][2 + e]) < kInf);
-                        }
-                    if (top[nt][e] != -kInf) top[nt][e] -= K::kLift;
+                for (int e = 0; e < 4; ++e) {
+                    o[j][e] = mul2(o[j][e], f[e]);
+                    const int r = 8 * sum_group(j) + 2 * e;
+                    odd |= r < left && low(f[e]) == low(f[e]) && !(fabsf(low(o[j][e])) < kInf);
+                    odd |= r + 1 < left && high(f[e]) == high(f[e]) && !(fabsf(high(o[j][e])) < kInf);
                 }
-            if (__any_sync(~0u, odd)) carefully<K>(a, t, u0, u, piece);
-            else emit<K>(a, t, piece, o, top, sum);
-            fresh = true;
+            }
+            if (soft_any(odd && d < a.c.dim)) {
+                for (int r = w; r < left; r += kSoft / 32) carefully<K>(a, it.t, r, it.first * kUnit, (it.first + it.n) * kUnit, piece);
+            } else {
+#pragma unroll
+                for (int j = 0; j < GO; ++j) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int r = 8 * sum_group(j) + e;
+                        const float x = e & 1 ? high(o[j][e / 2]) : low(o[j][e / 2]);
+                        if (r >= left) continue;
+                        if (piece) piece[r * K::D + d] = x;
+                        else if (d < a.c.dim) a.out[sh.out[slot][r] + d] = T::round(x);
+                    }
+                }
+            }
+            if (piece) {
+                // Of a tile that several blocks share: the last of them to come joins its pieces.
+                const int b0 = line.owner(it.begin), b1 = line.owner(it.begin + it.t.units - 1);
+                __threadfence();
+                soft_sync();
+                if (threadIdx.x == 0) {
+                    sh.last = atomicAdd(&a.arrived[b0], 1) == unsigned(b1 - b0);
+                    if (sh.last) a.arrived[b0] = 0;
+                }
+                soft_sync();
+                if (sh.last) {
+                    __threadfence();
+                    for (int r = w; r < left; r += kSoft / 32)
+                        join_row<K>(a, it.t, r, b1 - b0 + 1, [&](int x) { return a.pieces + (2 * int64_t(b0 + x) + (x == 0)) * a.piece_floats; });
+                }
+            }
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_of(&sh.q_free[slot]));
         }
-        copies_wait<0>();
     }
+    tmem_before();
     __syncthreads();
-
-    // Joins: of the tiles that end here after an earlier warp's run, then of the one that
-    // goes on in the next block.
-    const int64_t block_begin = line.begin(blockIdx.x * W);
-    const auto tail_of = [&](int x) { return reinterpret_cast<const float*>(memory + x * K::kWarpBytes); };
-    float* const block_pieces = a.pieces + int64_t(gridDim.x) * W * a.piece_floats;
-    for (int x = 0; x <= W; ++x) {
-        // (x = W: the tail that goes on.)
-        const Ends& e = x < W ? sh.heads[x] : sh.tails[W - 1];
-        if (e.begin < 0) continue;
-        int from = x < W ? x : W - 1;
-        while (from > 0 && sh.tails[from - 1].begin == e.begin) --from;
-        const int n = (x < W ? x : W - 1) - from + 1;
-        const auto at = [&](int i) { return x < W && i == n - 1 ? a.pieces + (int64_t(blockIdx.x) * W + x) * a.piece_floats : tail_of(from + i); };
-        const bool before = e.begin < block_begin, after = x == W;
-        if (!before && !after) {
-            join<K, false>(a, e.t, n, at, nullptr);
-            continue;
-        }
-        // Of a tile that several blocks share: this block's part, and, for the last of them to
-        // come, the whole.
-        join<K, false>(a, e.t, n, at, block_pieces + (2 * int64_t(blockIdx.x) + !before) * a.piece_floats);
-        const int b0 = line.owner(e.begin) / W, b1 = line.owner(e.end - 1) / W;
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            sh.last = atomicAdd(&a.arrived[b0], 1) == unsigned(b1 - b0);
-            if (sh.last) a.arrived[b0] = 0;
-        }
-        __syncthreads();
-        if (sh.last) {
-            __threadfence();
-            join<K, true>(a, e.t, b1 - b0 + 1,
-                    [&](int i) { return block_pieces + (2 * int64_t(b0 + i) + (i == 0)) * a.piece_floats; }, nullptr);
-        }
-        __syncthreads();
-    }
+    if (w == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(K::kColumns) : "memory");
 }
 
 // ---------------------------------------------------------------------------
@@ -939,11 +1069,9 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
 
 constexpr int64_t kArrivedBytes = kMostBlocks * 4;
 
-// The largest piece of a cache's head size.
-int64_t piece_floats(const rr_cache* C) {
-    return C->dim <= 64 ? Kind<BF16, 1, 5>::kPieceFloats : C->dim <= 128 ? Kind<BF16, 2, 5>::kPieceFloats : Kind<BF16, 4, 2>::kPieceFloats;
-}
-int64_t workspace_of(const rr_cache* C) { return kArrivedBytes + int64_t(kMostBlocks) * (C->dim > 128 ? 4 + 2 : 8 + 2) * piece_floats(C) * 4; }
+// The largest piece of a cache's head size: rows of D elements, a maximum and a sum.
+int64_t piece_floats(const rr_cache* C) { return C->dim <= 128 ? 64 * (128 + 2) : 32 * (256 + 2); }
+int64_t workspace_of(const rr_cache* C) { return kArrivedBytes + int64_t(kMostBlocks) * 2 * piece_floats(C) * 4; }
 
 rr_status check_heads(const rr_cache* C, int32_t n_q) {
     if (n_q < 1 || n_q % C->n_kv || n_q / C->n_kv > 1024)
@@ -951,42 +1079,70 @@ rr_status check_heads(const rr_cache* C, int32_t n_q) {
     return RR_OK;
 }
 
+// One layer's pages as TMA sees them: elements, tokens of a page, heads of the keys and then of the
+// values, pages; a copy is 64 elements of a page's tokens, swizzled as the products
+// read them, zeros past the head's end.
+rr_status map_pages(const rr_cache* C, const CacheShape& c, const char* pages, CUtensorMap* map) {
+    static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> known{nullptr};
+    PFN_cuTensorMapEncodeTiled_v12000 encode = known.load(std::memory_order_relaxed);
+    if (!encode) {
+        cudaDriverEntryPointQueryResult found;
+        void* f = nullptr;
+        RR_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found));
+        if (!f || found != cudaDriverEntryPointSuccess) return rr_fail(RR_ECUDA, "the driver has no cuTensorMapEncodeTiled");
+        encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+        known.store(encode, std::memory_order_relaxed);
+    }
+    const cuuint64_t size[4] = {cuuint64_t(c.dim), cuuint64_t(c.page), cuuint64_t(2 * c.n_kv), cuuint64_t(c.n_pages)};
+    const cuuint64_t stride[3] = {cuuint64_t(2 * c.pitch), cuuint64_t(c.run_bytes), cuuint64_t(c.page_bytes)};
+    const cuuint32_t box[4] = {64, cuuint32_t(c.page), 1, 1}, step[4] = {1, 1, 1, 1};
+    const CUresult e = encode(map, C->dtype == RR_DST_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+                              const_cast<char*>(pages), size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (e != CUDA_SUCCESS) return rr_fail(RR_ECUDA, "cuTensorMapEncodeTiled: error %d", int(e));
+    return RR_OK;
+}
+
 template <class K>
-rr_status launch(AttendArgs& a, int dev, cudaStream_t stream) {
+rr_status launch(AttendArgs& a, const CUtensorMap& map, int dev, cudaStream_t stream) {
     static std::atomic<uint32_t> ready{0};
     static std::atomic<int> sms[kMaxDevices] = {};
-    RR_CUDA(allow_smem(rr_attend_kernel<K>, K::kSmem, dev, &ready));
+    RR_CUDA(allow_smem(rr_attend_kernel<K>, kSmem, dev, &ready));
     int grid = sms[dev].load(std::memory_order_relaxed);
     if (!grid) {
         RR_CUDA(cudaDeviceGetAttribute(&grid, cudaDevAttrMultiProcessorCount, dev));
         sms[dev].store(grid, std::memory_order_relaxed);
     }
     grid = std::min(grid, kMostBlocks);
+    // The ring has what the queries and weights leave.  (The products of a head of an odd number
+    // of 64s read, and leave out, 16 KiB behind its values: within the block's memory.)
+    a.atoms = (a.c.dim + 63) / 64;
+    const int room = kSmem - 1024 - K::kFixed, stage = a.atoms * 16384;
+    a.stages = std::min(room / stage, kMostStages);
+    if (a.atoms % 2 && a.stages * stage + 16384 > kSmem - 1024) --a.stages;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(grid));
-    cfg.blockDim = dim3(K::kThreads);
-    cfg.dynamicSmemBytes = K::kSmem;
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    RR_CUDA(cudaLaunchKernelEx(&cfg, rr_attend_kernel<K>, a));
+    RR_CUDA(cudaLaunchKernelEx(&cfg, rr_attend_kernel<K>, a, map));
     return RR_OK;
 }
 
 // The rows that a tile is to hold: of sequences of the call's mean number of new tokens,
 // and up to as many again.
-template <class T, int C>
-rr_status choose(AttendArgs& a, int dev, cudaStream_t stream) {
+template <class T>
+rr_status choose(AttendArgs& a, const CUtensorMap& map, int dev, cudaStream_t stream) {
     const int mean = (a.rows + a.n - 1) / a.n, most = std::min(2 * mean - 1, a.rows - a.n + 1);
     const int64_t rows = int64_t(a.group) * std::max(most, 1);
-    if (rows <= 8) return launch<Kind<T, C, 1>>(a, dev, stream);
-    if constexpr (C <= 2) {
-        if (rows > 16) return launch<Kind<T, C, 5>>(a, dev, stream);
-    }
-    return launch<Kind<T, C, 2>>(a, dev, stream);
+    if (a.c.dim > 128) return rows <= 16 ? launch<Kind<T, 2, 2>>(a, map, dev, stream) : launch<Kind<T, 2, 4>>(a, map, dev, stream);
+    if (rows <= 16) return launch<Kind<T, 1, 2>>(a, map, dev, stream);
+    return launch<Kind<T, 1, 8>>(a, map, dev, stream);
 }
 
 }  // namespace
@@ -1051,11 +1207,11 @@ extern "C" rr_status rr_attend(const rr_cache* C, const void* pages, void* book,
     a.scale = scale * kLog2e;
     a.qvec = (uintptr_t)q % 16 == 0 && ldq % 8 == 0 && C->dim % 8 == 0;
     a.ovec = (uintptr_t)out % 16 == 0 && ldo % 8 == 0 && C->dim % 8 == 0;
+    CUtensorMap map;
+    RR_TRY(map_pages(C, a.c, a.pages, &map));
     const auto with = [&](auto t) -> rr_status {
         using T = decltype(t);
-        if (C->dim <= 64) return choose<T, 1>(a, dev, stream);
-        if (C->dim <= 128) return choose<T, 2>(a, dev, stream);
-        return choose<T, 4>(a, dev, stream);
+        return choose<T>(a, map, dev, stream);
     };
     return C->dtype == RR_DST_F16 ? with(F16{}) : with(BF16{});
 }

@@ -912,6 +912,7 @@ extern "C" rr_status rr_cache_check(const rr_cache* C, void* book, cudaStream_t 
     if (!state) return RR_OK;
     RR_CUDA(cudaMemsetAsync(book, 0, 8, stream));
     RR_CUDA(cudaStreamSynchronize(stream));
+    if (state & kBadWait) return rr_fail(RR_ECUDA, "a wait within rr_attend ran out");
     return rr_fail(RR_EINVAL, "a call on the cache was not done:%s%s%s%s%s", state & kBadRange ? " a sequence, length or count is out of range;" : "",
                    state & kBadTwice ? " a sequence is listed twice;" : "", state & kBadPool ? " no room for the new tokens;" : "",
                    state & kBadChild ? " a child holds tokens;" : "", state & kBadTable ? " the table has a page out of range;" : "");

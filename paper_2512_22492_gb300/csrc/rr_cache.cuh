@@ -12,7 +12,7 @@ enum { kState = 0, kLate = 1, kMoves = 2, kUsed = 3 };
 constexpr int kControlWords = 64;
 
 // Bits of its state.
-enum { kBadRange = 1, kBadTwice = 2, kBadPool = 4, kBadChild = 8, kBadTable = 16 };
+enum { kBadRange = 1, kBadTwice = 2, kBadPool = 4, kBadChild = 8, kBadTable = 16, kBadWait = 32 };
 
 struct Book {
     int32_t *control, *table, *lengths, *refs;
