@@ -32,8 +32,6 @@ namespace {
 constexpr int kUnit = 128;              // keys
 constexpr int kMostBlocks = 192;
 constexpr int kMostStages = 12;
-constexpr int kThreads = 11 * 32;       // softmax: warps 0..7; then copies, products, queries
-constexpr int kSoft = 256;
 constexpr int kSmem = 220 * 1024;       // of a block, beside its static part
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
@@ -58,6 +56,9 @@ struct AttendArgs {
     int64_t piece_floats;
     int32_t n, rows, n_q, group;
     int32_t stages, atoms;         // of the ring; 64 elements of a head each
+    // Of a unit's keys or values in shared memory, where 8 tokens' 64 elements are 1 KiB together:
+    // from 64 elements to the next, from 8 tokens to the next; and how many elements one copy has.
+    int32_t atom_bytes, eight_bytes, copy_atoms;
     float scale;                   // with log2(e)
     int32_t qvec, ovec;
 };
@@ -70,6 +71,11 @@ struct Kind {
     static constexpr int MT = MT_, NG = NG_;
     static constexpr int kRows = 8 * NG;
     static constexpr int D = 128 * MT;
+    // Sets of four softmax warps; copies, products and queries have a warp each.  (96 sequences of
+    // five tokens of 8 heads each: @@SETS@@)
+    static constexpr int kSets = NG == 8 ? 3 : 2;
+    static constexpr int kSoft = 128 * kSets, kThreads = kSoft + 96;
+    static constexpr int kCopies = kSoft / 32, kProducts = kCopies + 1, kQueries = kCopies + 2;
     // Bfloat16 keeps 8 bits of a weight: it enters the second product in two parts, 16
     // bits in all.  Float16's 11 bits are one part: as far off as the result's own
     // rounding is.  Its weights are 2^7 to 2^15 at a row's maximum, so that those 2^-21 of
@@ -205,11 +211,12 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, int parity) {
 }
 // Whether the barrier's phase came.  A wait that runs out (two seconds or so) raises *quit, on
 // which the block's other waits give up too.
-__device__ __noinline__ bool bar_wait_on(uint32_t bar, int parity, volatile int* quit, int32_t* control) {
+__device__ __forceinline__ bool bar_wait(uint32_t bar, int parity, volatile int* quit, int32_t* control) {
+    if (bar_try(bar, parity)) return true;
     const long long t0 = clock64();
-    for (;;) {
-        for (int k = 0; k < 64; ++k)
-            if (bar_try(bar, parity)) return true;
+#pragma unroll 1
+    for (int k = 0; !bar_try(bar, parity); ++k) {
+        if (k & 31) continue;
         if (*quit) return false;
         if (clock64() - t0 > kWaitCycles) {
             *quit = 1;
@@ -217,26 +224,26 @@ __device__ __noinline__ bool bar_wait_on(uint32_t bar, int parity, volatile int*
             return false;
         }
     }
-}
-__device__ __forceinline__ bool bar_wait(uint32_t bar, int parity, volatile int* quit, int32_t* control) {
-    return bar_try(bar, parity) || bar_wait_on(bar, parity, quit, control);
+    return true;
 }
 
 // The softmax warps' own barrier, with the OR of what they bring.
+template <int THREADS>
 __device__ __forceinline__ bool soft_any(bool x) {
     uint32_t r;
     asm volatile(
         "{ .reg .pred p, q; setp.ne.u32 p, %1, 0; barrier.cta.red.or.pred q, 1, %2, p; selp.u32 %0, 1, 0, q; }"
         : "=r"(r)
-        : "r"(uint32_t(x)), "n"(kSoft)
+        : "r"(uint32_t(x)), "n"(THREADS)
         : "memory");
-    return r;
+    return __any_sync(~0u, r);
 }
-__device__ __forceinline__ void soft_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kSoft) : "memory"); }
+template <int THREADS>
+__device__ __forceinline__ void soft_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(THREADS) : "memory"); }
 
 __device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
     asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(to),
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, 0, %3, %4, %5}], [%6];" ::"r"(to),
         "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
         : "memory");
 }
@@ -358,46 +365,56 @@ struct Place {
 };
 
 // A warp joins row r of n pieces, given by at(i), in the outputs.  A piece counts by its sum
-// at the largest of the maxima.
+// at the largest of the maxima.  What bounds it is the time of a load: those of 16 pieces are on
+// their way at once, the first of them with the maxima and sums.
 template <class K, class At>
 __device__ __forceinline__ void join_row(const AttendArgs& a, const Tile& t, int r, int n, At at) {
     constexpr int kMl = K::D * K::kRows;
-    const int lane = threadIdx.x & 31;
-    float top = -kInf;
-    for (int i = lane; i < n; i += 32) top = fmaxf(top, __ldcg(at(i) + kMl + 2 * r));
-#pragma unroll
-    for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
-    const auto share = [&](int i) {
-        const float m = __ldcg(at(i) + kMl + 2 * r);
-        return m == -kInf ? 0.0f : __ldcg(at(i) + kMl + 2 * r + 1) * exp2f(m - top);
-    };
-    float sum = 0;
-    for (int i = lane; i < n; i += 32) sum += share(i);
-#pragma unroll
-    for (int m = 16; m; m >>= 1) sum += __shfl_xor_sync(~0u, sum, m);
-    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
     // 8 adjacent elements a lane; with 16 lanes' worth of them, half the lanes take every
     // other piece.
-    constexpr int kLanes = K::D / 8, kTeams = 32 / kLanes;
-    const int d = 8 * (lane % kLanes), team = lane / kLanes;
-    float x[8] = {};
-    for (int base = 0; base < n; base += 32) {
-        const float mine = base + lane < n ? share(base + lane) * inverse : 0.0f;
-#pragma unroll 4
-        for (int k = 0; k < min(n - base, 32); k += kTeams) {
-            const int i = base + k + team;
-            const float w = __shfl_sync(~0u, mine, (k + team) & 31);
-            if (k + team >= 32 || i >= n || w == 0.0f) continue;
-            const float4* from = reinterpret_cast<const float4*>(at(i) + r * K::D + d);
-            const float4 u = __ldcg(from), v = __ldcg(from + 1);
-            x[0] = fmaf(w, u.x, x[0]), x[1] = fmaf(w, u.y, x[1]), x[2] = fmaf(w, u.z, x[2]), x[3] = fmaf(w, u.w, x[3]);
-            x[4] = fmaf(w, v.x, x[4]), x[5] = fmaf(w, v.y, x[5]), x[6] = fmaf(w, v.z, x[6]), x[7] = fmaf(w, v.w, x[7]);
+    constexpr int kLanes = K::D / 8, kTeams = 32 / kLanes, kBatch = 16 / kTeams;
+    const int lane = threadIdx.x & 31, d = 8 * (lane % kLanes), team = lane / kLanes;
+    float4 u[kBatch], v[kBatch];
+    const auto load = [&](int k) {
+#pragma unroll
+        for (int e = 0; e < kBatch; ++e) {
+            const float4* from = reinterpret_cast<const float4*>(at(min(k + e * kTeams + team, n - 1)) + r * K::D + d);
+            u[e] = __ldcg(from), v[e] = __ldcg(from + 1);
+        }
+    };
+    // (Maximum, sum) of a piece.
+    const auto sums_of = [&](int i) { return i < n ? __ldcg(reinterpret_cast<const float2*>(at(i) + kMl + 2 * r)) : make_float2(-kInf, 0); };
+    const auto share_of = [](float2 y, float top) { return y.x == -kInf ? 0.0f : y.y * exp2f(y.x - top); };
+    load(0);
+    float2 mine = sums_of(lane);
+    float top = mine.x;
+    for (int i = 32 + lane; i < n; i += 32) top = fmaxf(top, sums_of(i).x);
+#pragma unroll
+    for (int y = 16; y; y >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, y));
+    float sum = share_of(mine, top);
+    for (int i = 32 + lane; i < n; i += 32) sum += share_of(sums_of(i), top);
+#pragma unroll
+    for (int y = 16; y; y >>= 1) sum += __shfl_xor_sync(~0u, sum, y);
+    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+    float share = share_of(mine, top) * inverse, x[8] = {};
+#pragma unroll 1
+    for (int k = 0; k < n; k += 16) {
+        if (k) {
+            load(k);
+            if (k % 32 == 0) share = share_of(sums_of(k + lane), top) * inverse;
+        }
+#pragma unroll
+        for (int e = 0; e < kBatch; ++e) {
+            const float w = __shfl_sync(~0u, share, (k + e * kTeams + team) & 31);
+            if (k + e * kTeams + team >= n) continue;
+            x[0] = fmaf(w, u[e].x, x[0]), x[1] = fmaf(w, u[e].y, x[1]), x[2] = fmaf(w, u[e].z, x[2]), x[3] = fmaf(w, u[e].w, x[3]);
+            x[4] = fmaf(w, v[e].x, x[4]), x[5] = fmaf(w, v[e].y, x[5]), x[6] = fmaf(w, v[e].z, x[6]), x[7] = fmaf(w, v[e].w, x[7]);
         }
     }
 #pragma unroll
-    for (int m = kLanes; m < 32; m <<= 1) {
+    for (int k = 0; k < 8; ++k) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] += __shfl_xor_sync(~0u, x[k], m);
+        for (int m = kLanes; m < 32; m <<= 1) x[k] += __shfl_xor_sync(~0u, x[k], m);
     }
     if (team) return;
     const Place<K> place(a, t, r, nullptr);
@@ -484,7 +501,7 @@ struct Shared {
     // when that moves; 1 / the sum of weights.
     alignas(16) float zero[8], bias[K::kRows], factor[K::kRows], inverse[K::kRows];
     float parts[4][K::kRows];
-    int64_t scan[kThreads / 32];
+    int64_t scan[K::kThreads / 32];
     int64_t start;                                    // where the block's run begins within its first sequence
     int seq;                                          // that sequence
     int quit, last;
@@ -524,14 +541,14 @@ struct Stage {
 };
 
 template <class K>
-__global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
     using T = typename K::T;
     constexpr int NG = K::NG, MT = K::MT, N = K::kRows;
     extern __shared__ char memory[];
     __shared__ Shared<K> sh;
     after_previous();
     if (__ldcg(&a.control[kState])) return;
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, w = uniform(threadIdx.x >> 5);
 
     // The line, and where this block's run begins in it.
     Line line;
@@ -548,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
             __syncthreads();
             int64_t before = 0, all = 0;
 #pragma unroll
-            for (int i = 0; i < kThreads / 32; ++i) {
+            for (int i = 0; i < K::kThreads / 32; ++i) {
                 if (i < w) before += sh.scan[i];
                 all += sh.scan[i];
             }
@@ -563,16 +580,16 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
             return work_of<K>(a, length, count);
         };
         int64_t mine = 0, kept = 0;
-        for (int i = threadIdx.x; i < a.n; i += kThreads) mine += kept = work(i);
+        for (int i = threadIdx.x; i < a.n; i += K::kThreads) mine += kept = work(i);
         int64_t at = scan(mine, &line.total);
         if (line.total == 0) return;
         line.blocks = int(min(int64_t(gridDim.x), line.total));
         if (int(blockIdx.x) >= line.blocks) return;
         begin = line.begin(blockIdx.x), end = line.begin(blockIdx.x + 1);
         int64_t before = 0;
-        for (int base = 0; base < a.n && before <= begin; base += kThreads) {
+        for (int base = 0; base < a.n && before <= begin; base += K::kThreads) {
             int64_t total = line.total;
-            if (a.n > kThreads) {
+            if (a.n > K::kThreads) {
                 kept = work(base + int(threadIdx.x));
                 at = before + scan(kept, &total);
             }
@@ -594,15 +611,15 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
         for (int i = 0; i < 2; ++i) {
             bar_init(smem_of(&sh.scores[i]), 1);
             bar_init(smem_of(&sh.q_full[i]), 1);
-            bar_init(smem_of(&sh.q_free[i]), kSoft / 32);
+            bar_init(smem_of(&sh.q_free[i]), K::kSoft / 32);
         }
-        bar_init(smem_of(&sh.weights), kSoft / 32);
+        bar_init(smem_of(&sh.weights), K::kSoft / 32);
         bar_init(smem_of(&sh.sums), 1);
         sh.quit = 0;
         for (int i = 0; i < 8; ++i) sh.zero[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (w == 9) {
+    if (w == K::kProducts) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_of(&sh.tmem)), "n"(K::kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -623,11 +640,11 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
         return int(at - tile * walk.t.units);
     };
 
-    if (w == 8) {
+    if (w == K::kCopies) {
         // Copies.
         Walk<K> walk(a, sh.seq);
         int unit = enter(walk);
-        const int tokens = a.c.page, pages = kUnit >> a.c.shift;
+        const int tokens = a.c.page, pages = kUnit >> a.c.shift, eights = tokens / 8;
         const auto fetch = [&] {
             const int key = unit * kUnit + lane * tokens;
             if (lane >= pages || key >= walk.t.length) return -1;
@@ -642,11 +659,13 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
             if (!__all_sync(~0u, wait(sh.empty[s.at], s.turn ^ 1))) return false;
             const uint32_t bar = smem_of(&sh.full[s.at]);
             const int there = __popc(__ballot_sync(~0u, id >= 0));
-            if (lane == 0) bar_expect(bar, uint32_t(there * a.atoms * tokens * 128));
+            if (elected()) bar_expect(bar, uint32_t(there * a.atoms * tokens * 128));
             __syncwarp();
-            if (id >= 0)
-                for (int x = 0; x < a.atoms; ++x)
-                    tma_load(ring + s.at * stage_bytes + x * 16384 + lane * tokens * 128, &map, 64 * x, 0, head, id, bar);
+            if (id >= 0) {
+                const uint32_t to = ring + s.at * stage_bytes + lane * eights * a.eight_bytes;
+                for (int y = 0; y < a.atoms; y += a.copy_atoms)
+                    tma_load(to + y * a.atom_bytes, &map, a.copy_atoms > 1 ? 0 : 64 * y, 0, head * eights, id, bar);
+            }
             s.next(a.stages);
             asked = min(asked + 1, a.stages);
             return true;
@@ -678,7 +697,7 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                 for (int x = 0; x < 1 << 20 && !bar_try(smem_of(&sh.full[s.at]), s.turn); ++x) {}
             }
         }
-    } else if (w == 9) {
+    } else if (w == K::kProducts) {
         // Products.  (All lanes go along; one of them issues.)
         const int k16 = (a.c.dim + 15) / 16;
         // The ring's order: K0 K1 V0 K2 V1 ...
@@ -700,10 +719,10 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                 tmem_after();
                 if (elected()) {
                     // (A descriptor's address counts 16 bytes.)
-                    const uint64_t dk = descriptor(ring + st.at * stage_bytes, 16, 1024, 2), dq = descriptor(q_at + slot * K::kQ, N * 16, 128, 0);
+                    const uint64_t dk = descriptor(ring + st.at * stage_bytes, 16, a.eight_bytes, 2), dq = descriptor(q_at + slot * K::kQ, N * 16, 128, 0);
 #pragma unroll 1
                     for (int j = 0; j < k16; ++j)
-                        product(first_tmem + uint32_t(i & 1) * N, dk + (j >> 2) * 1024 + (j & 3) * 2, dq + j * (2 * N), q_instr, j > 0);
+                        product(first_tmem + uint32_t(i & 1) * N, dk + (j >> 2) * (a.atom_bytes / 16) + (j & 3) * 2, dq + j * (2 * N), q_instr, j > 0);
                     products_arrive(smem_of(&sh.empty[st.at]));
                     products_arrive(smem_of(&sh.scores[i & 1]));
                 }
@@ -724,14 +743,14 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                 tmem_after();
                 const int steps = max((min(v_length - v_unit * kUnit, kUnit) + 15) / 16, 1);
                 if (elected()) {
-                    const uint64_t dv = descriptor(ring + st.at * stage_bytes, 16384, 1024, 2), dp = descriptor(p_at, 128, 2048, 0);
+                    const uint64_t dv = descriptor(ring + st.at * stage_bytes, a.atom_bytes, a.eight_bytes, 2), dp = descriptor(p_at, 128, 2048, 0);
 #pragma unroll 1
                     for (int m = 0; m < MT; ++m)
 #pragma unroll 1
                         for (int part = K::kParts - 1; part >= 0; --part)
 #pragma unroll 1
                             for (int j = 0; j < steps; ++j)
-                                product(first_tmem + (2 + m) * N, dv + m * 2048 + j * 128, dp + part * (K::kP / 16) + j * 16, v_instr,
+                                product(first_tmem + (2 + m) * N, dv + m * (a.atom_bytes / 8) + j * (a.eight_bytes / 8), dp + part * (K::kP / 16) + j * 16, v_instr,
                                         j > 0 || part < K::kParts - 1);
                     products_arrive(smem_of(&sh.empty[st.at]));
                     products_arrive(smem_of(&sh.sums));
@@ -742,15 +761,15 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
             }
         }
         __syncwarp();
-    } else if (w == 10) {
+    } else if (w == K::kQueries) {
         // Queries, and what the others need to know of a tile.
         Walk<K> walk(a, sh.seq);
         int unit = enter(walk);
         int64_t at = begin;
         const int chunks = (a.c.dim + 15) / 16 * 2;
-        for (int64_t item = 0; at < end; ++item) {
-            const int slot = int(item & 1);
-            if (!__all_sync(~0u, wait(sh.q_free[slot], int(item >> 1 & 1) ^ 1))) break;
+        for (int item = 0; at < end; ++item) {
+            const int slot = item & 1;
+            if (!__all_sync(~0u, wait(sh.q_free[slot], (item >> 1 & 1) ^ 1))) break;
             const Tile& t = walk.t;
             const int left = min(t.count * a.group - t.tile * K::kRows, K::kRows), rows = (left + 15) / 16 * 16;
             const uint32_t to = q_at + slot * K::kQ;
@@ -800,22 +819,25 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
             if (at < end) walk.next();
         }
     } else {
-        // Softmax and sums.  Lane l of warp w has key, or element, 32 (w % 4) + l; warps 0..3 take
-        // the even groups of 8 rows, warps 4..7 the odd ones (MT 2: of the sums, elements 128 on).
-        constexpr int GS = (NG + 1) / 2, GO = MT == 1 ? GS : NG;
-        const int set = w >> 2, key = threadIdx.x & 127;
+        // Softmax and sums.  Lane l of warp w has key, or element, 32 (w % 4) + l; the sets of four
+        // warps share the groups of 8 rows in turn (MT 2: of the sums, half of the sets each 128
+        // elements).
+        constexpr int kSets = K::kSets, GS = (NG + kSets - 1) / kSets, kSumSets = kSets / MT, GO = (NG + kSumSets - 1) / kSumSets;
+        const int set = w >> 2, key = threadIdx.x & 127, half = MT == 2 ? set & 1 : 0;
         const uint32_t lanes = uint32_t(w & 3) << 21;
-        const auto group_of = [&](int j) { return set + 2 * j; };
+        const auto group_of = [&](int j) { return set + kSets * j; };
         const F2 scale2 = both(a.scale, a.scale);
-        const auto sum_group = [&](int j) { return MT == 1 ? set + 2 * j : j; };
-        int64_t i = 0;
+        const auto sum_group = [&](int j) { return set / MT + kSumSets * j; };
+        const int all = int(n);
+        int i = 0;
         bool over = false;
-        for (int64_t item = 0; i < n && !over; ++item) {
-            const int slot = int(item & 1);
-            bool ok = __all_sync(~0u, wait(sh.q_full[slot], int(item >> 1 & 1)));
+        for (int item = 0; i < all && !over; ++item) {
+            const int slot = item & 1;
+            bool ok = __all_sync(~0u, wait(sh.q_full[slot], (item >> 1 & 1)));
             const Item it = sh.items[slot];
-            const int left = ok ? min(it.t.count * a.group - it.t.tile * K::kRows, K::kRows) : 0, groups = (left + 7) / 8;
-            const int units = ok ? it.n : 1, first_seen = seen(it.t, a.group, it.t.tile * K::kRows);
+            const int left = uniform(ok ? min(it.t.count * a.group - it.t.tile * K::kRows, K::kRows) : 0), groups = (left + 7) / 8;
+            const int units = uniform(ok ? it.n : 1), first_seen = uniform(seen(it.t, a.group, it.t.tile * K::kRows));
+            const int first_key = uniform(it.first * kUnit);
             F2 o[GO][4], sum[GS][4];
 #pragma unroll
             for (int j = 0; j < GO; ++j)
@@ -827,7 +849,7 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                 for (int e = 0; e < 4; ++e) sum[j][e] = 0;
             // (The first scores are over any reference: it is set then.)
             if (int(threadIdx.x) < N) sh.bias[threadIdx.x] = kNothing;
-            soft_sync();
+            soft_sync<K::kSoft>();
             const auto add_sums = [&] {
                 // (Two groups at a time: registers are short.)
 #pragma unroll
@@ -836,7 +858,7 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
                         if (j + k < GO && sum_group(j + k) < groups)
-                            tmem_load(tmem + lanes + (2 + (MT == 2 ? set : 0)) * N + 8 * sum_group(j + k), x[k]);
+                            tmem_load(tmem + lanes + (2 + half) * N + 8 * sum_group(j + k), x[k]);
                     tmem_loaded();
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
@@ -847,8 +869,8 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                 }
             };
             for (int u = 0; u < units; ++u, ++i) {
-                const int key0 = (it.first + u) * kUnit;
-                ok &= __all_sync(~0u, wait(sh.scores[i & 1], int(i >> 1 & 1)));
+                const int key0 = first_key + u * kUnit;
+                ok &= __all_sync(~0u, wait(sh.scores[i & 1], i >> 1 & 1));
                 tmem_after();
                 F2 s[GS][4];
 #pragma unroll
@@ -890,9 +912,9 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
 #pragma unroll
                     for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(low(x[e]), high(x[e])));
                 }
-                const bool moved = soft_any(!ok || most > kSlack + K::kLift);
+                const bool moved = soft_any<K::kSoft>(!ok || most > kSlack + K::kLift);
                 if (moved) {
-                    if (soft_any(!ok || *(volatile int*)&sh.quit)) {
+                    if (soft_any<K::kSoft>(!ok || *(volatile int*)&sh.quit)) {
                         over = true;
                         break;
                     }
@@ -904,7 +926,7 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                         const float m = over_lanes(y, [](float p, float q) { return fmaxf(p, q); });
                         if ((lane & 3) == 0) sh.parts[w & 3][8 * group_of(j) + row_of_lane()] = m;
                     }
-                    soft_sync();
+                    soft_sync<K::kSoft>();
                     if (int(threadIdx.x) < 8 * groups) {
                         const int r = threadIdx.x;
                         const float m = fmaxf(fmaxf(sh.parts[0][r], sh.parts[1][r]), fmaxf(sh.parts[2][r], sh.parts[3][r]));
@@ -913,7 +935,7 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                         sh.factor[r] = moves ? exp2f(after - before) : 1.0f;
                         if (moves) sh.bias[r] = after;
                     }
-                    soft_sync();
+                    soft_sync<K::kSoft>();
 #pragma unroll
                     for (int j = 0; j < GS; ++j) {
                         if (group_of(j) >= groups) continue;
@@ -944,7 +966,7 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                 // The sums of the unit before, which refer to the reference before; then the weights
                 // may be overwritten.
                 if (u > 0) {
-                    wait(sh.sums, int((i - 1) & 1));
+                    wait(sh.sums, (i - 1) & 1);
                     tmem_after();
                     add_sums();
                 }
@@ -969,14 +991,14 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                 const int valid = min(it.t.length - key0, kUnit);
                 if (valid < kUnit) {
                     // Behind the sequence's end the page holds anything: values there become 0.
-                    const int64_t k = i + 1 < n ? 2 * i + 2 : 2 * i + 1;      // in the ring's order
-                    const int stage = int(k % a.stages);
-                    wait(sh.full[stage], int(k / a.stages & 1));
+                    const int k = i + 1 < all ? 2 * i + 2 : 2 * i + 1;      // in the ring's order
+                    const int stage = k % a.stages;
+                    wait(sh.full[stage], k / a.stages & 1);
                     const int rows = max((valid + 15) / 16 * 16, 16) - valid;
-                    for (int x = threadIdx.x; x < rows * a.atoms * 8; x += kSoft) {
-                        const int atom = x / (rows * 8), y = x - atom * (rows * 8);
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(ring + stage * stage_bytes + atom * 16384 + valid * 128 + y * 16), "r"(0)
-                                     : "memory");
+                    for (int x = threadIdx.x; x < rows * a.atoms * 8; x += K::kSoft) {
+                        const int atom = x / (rows * 8), y = x - atom * (rows * 8), token = valid + (y >> 3);
+                        const uint32_t at = ring + stage * stage_bytes + atom * a.atom_bytes + (token >> 3) * a.eight_bytes + (token & 7) * 128 + (y & 7) * 16;
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(at), "r"(0) : "memory");
                     }
                 }
                 to_async();
@@ -988,7 +1010,7 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
 
             // The run leaves the tile.
             __syncwarp();
-            wait(sh.sums, int((i - 1) & 1));
+            wait(sh.sums, (i - 1) & 1);
             tmem_after();
             __syncwarp();
             add_sums();
@@ -998,7 +1020,7 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                 const float m = over_lanes(sum[j], [](float x, float y) { return x + y; });
                 if ((lane & 3) == 0) sh.parts[w & 3][8 * group_of(j) + row_of_lane()] = m;
             }
-            soft_sync();
+            soft_sync<K::kSoft>();
             const bool starts = it.first == 0, ends = it.first + it.n == it.t.units;
             float* const piece = starts && ends ? nullptr : a.pieces + (2 * int64_t(blockIdx.x) + starts) * a.piece_floats;
             if (int(threadIdx.x) < left) {
@@ -1008,8 +1030,8 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                 sh.inverse[r] = total == 0.0f ? 0.0f : 1.0f / total;
                 Place<K>(a, it.t, r, piece).sums(bias == kNothing ? -kInf : -bias, total);
             }
-            soft_sync();
-            const int d = key + (MT == 2 ? 128 * set : 0);
+            soft_sync<K::kSoft>();
+            const int d = key + 128 * half;
             bool odd = false;
 #pragma unroll
             for (int j = 0; j < GO; ++j) {
@@ -1023,8 +1045,8 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                     odd |= r + 1 < left && high(f[e]) == high(f[e]) && !(fabsf(high(o[j][e])) < kInf);
                 }
             }
-            if (soft_any(odd && d < a.c.dim)) {
-                for (int r = w; r < left; r += kSoft / 32) carefully<K>(a, it.t, r, it.first * kUnit, (it.first + it.n) * kUnit, piece);
+            if (soft_any<K::kSoft>(odd && d < a.c.dim)) {
+                for (int r = w; r < left; r += K::kSoft / 32) carefully<K>(a, it.t, r, it.first * kUnit, (it.first + it.n) * kUnit, piece);
             } else {
 #pragma unroll
                 for (int j = 0; j < GO; ++j) {
@@ -1042,15 +1064,15 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
                 // Of a tile that several blocks share: the last of them to come joins its pieces.
                 const int b0 = line.owner(it.begin), b1 = line.owner(it.begin + it.t.units - 1);
                 __threadfence();
-                soft_sync();
+                soft_sync<K::kSoft>();
                 if (threadIdx.x == 0) {
                     sh.last = atomicAdd(&a.arrived[b0], 1) == unsigned(b1 - b0);
                     if (sh.last) a.arrived[b0] = 0;
                 }
-                soft_sync();
+                soft_sync<K::kSoft>();
                 if (sh.last) {
                     __threadfence();
-                    for (int r = w; r < left; r += kSoft / 32)
+                    for (int r = w; r < left; r += K::kSoft / 32)
                         join_row<K>(a, it.t, r, b1 - b0 + 1, [&](int x) { return a.pieces + (2 * int64_t(b0 + x) + (x == 0)) * a.piece_floats; });
                 }
             }
@@ -1060,7 +1082,7 @@ __global__ void __launch_bounds__(kThreads, 1) rr_attend_kernel(const __grid_con
     }
     tmem_before();
     __syncthreads();
-    if (w == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(K::kColumns) : "memory");
+    if (w == K::kProducts) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(K::kColumns) : "memory");
 }
 
 // ---------------------------------------------------------------------------
@@ -1079,10 +1101,12 @@ rr_status check_heads(const rr_cache* C, int32_t n_q) {
     return RR_OK;
 }
 
-// One layer's pages as TMA sees them: elements, tokens of a page, heads of the keys and then of the
-// values, pages; a copy is 64 elements of a page's tokens, swizzled as the products
-// read them, zeros past the head's end.
-rr_status map_pages(const rr_cache* C, const CacheShape& c, const char* pages, CUtensorMap* map) {
+// The pages as TMA sees them: 64 elements, 8 tokens, 64 elements after 64, 8 tokens after
+// 8 (through a page's heads, keys and values), pages.  A copy is one page's tokens of a
+// head, swizzled as the products read them: heads of whole 64s at once; others 64 elements
+// at a time, zeros past the end.
+rr_status map_pages(const AttendArgs& a, int dtype, CUtensorMap* map) {
+    const CacheShape& c = a.c;
     static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> known{nullptr};
     PFN_cuTensorMapEncodeTiled_v12000 encode = known.load(std::memory_order_relaxed);
     if (!encode) {
@@ -1093,11 +1117,13 @@ rr_status map_pages(const rr_cache* C, const CacheShape& c, const char* pages, C
         encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
         known.store(encode, std::memory_order_relaxed);
     }
-    const cuuint64_t size[4] = {cuuint64_t(c.dim), cuuint64_t(c.page), cuuint64_t(2 * c.n_kv), cuuint64_t(c.n_pages)};
-    const cuuint64_t stride[3] = {cuuint64_t(2 * c.pitch), cuuint64_t(c.run_bytes), cuuint64_t(c.page_bytes)};
-    const cuuint32_t box[4] = {64, cuuint32_t(c.page), 1, 1}, step[4] = {1, 1, 1, 1};
-    const CUresult e = encode(map, C->dtype == RR_DST_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
-                              const_cast<char*>(pages), size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    const bool joined = a.copy_atoms > 1;
+    const cuuint64_t size[5] = {cuuint64_t(joined ? 64 : c.dim), 8, cuuint64_t(joined ? a.atoms : 1), cuuint64_t(2 * c.n_kv * (c.page / 8)),
+                                cuuint64_t(c.n_pages)};
+    const cuuint64_t stride[4] = {cuuint64_t(2 * c.pitch), 128, cuuint64_t(16 * c.pitch), cuuint64_t(c.page_bytes)};
+    const cuuint32_t box[5] = {64, 8, cuuint32_t(a.copy_atoms), cuuint32_t(c.page / 8), 1}, step[5] = {1, 1, 1, 1, 1};
+    const CUresult e = encode(map, dtype == RR_DST_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5,
+                              const_cast<char*>(a.pages), size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (e != CUDA_SUCCESS) return rr_fail(RR_ECUDA, "cuTensorMapEncodeTiled: error %d", int(e));
     return RR_OK;
@@ -1116,7 +1142,6 @@ rr_status launch(AttendArgs& a, const CUtensorMap& map, int dev, cudaStream_t st
     grid = std::min(grid, kMostBlocks);
     // The ring has what the queries and weights leave.  (The products of a head of an odd number
     // of 64s read, and leave out, 16 KiB behind its values: within the block's memory.)
-    a.atoms = (a.c.dim + 63) / 64;
     const int room = kSmem - 1024 - K::kFixed, stage = a.atoms * 16384;
     a.stages = std::min(room / stage, kMostStages);
     if (a.atoms % 2 && a.stages * stage + 16384 > kSmem - 1024) --a.stages;
@@ -1125,7 +1150,7 @@ rr_status launch(AttendArgs& a, const CUtensorMap& map, int dev, cudaStream_t st
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(grid));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(K::kThreads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = stream;
     cfg.attrs = attr;
@@ -1208,7 +1233,11 @@ extern "C" rr_status rr_attend(const rr_cache* C, const void* pages, void* book,
     a.qvec = (uintptr_t)q % 16 == 0 && ldq % 8 == 0 && C->dim % 8 == 0;
     a.ovec = (uintptr_t)out % 16 == 0 && ldo % 8 == 0 && C->dim % 8 == 0;
     CUtensorMap map;
-    RR_TRY(map_pages(C, a.c, a.pages, &map));
+    a.atoms = (a.c.dim + 63) / 64;
+    a.copy_atoms = a.c.dim % 64 == 0 ? a.atoms : 1;
+    a.atom_bytes = a.copy_atoms > 1 ? 1024 : 16384;
+    a.eight_bytes = a.copy_atoms > 1 ? 1024 * a.atoms : 1024;
+    RR_TRY(map_pages(a, C->dtype, &map));
     const auto with = [&](auto t) -> rr_status {
         using T = decltype(t);
         return choose<T>(a, map, dev, stream);
