@@ -30,6 +30,7 @@
 namespace {
 
 constexpr int kUnit = 128;              // keys
+constexpr int kGather = 8;              // units whose sums gather in TMEM
 constexpr int kMostBlocks = 192;
 constexpr int kMostStages = 12;
 constexpr int kSmem = 220 * 1024;       // of a block, beside its static part
@@ -74,8 +75,8 @@ struct Kind {
     // Sets of four softmax warps; copies, products and queries have a warp each.  (96 sequences of
     // five tokens of 8 heads each: @@SETS@@)
     static constexpr int kSets = NG == 8 ? 3 : 2;
-    static constexpr int kSoft = 128 * kSets, kThreads = kSoft + 96;
-    static constexpr int kCopies = kSoft / 32, kProducts = kCopies + 1, kQueries = kCopies + 2;
+    static constexpr int kSoft = 128 * kSets, kThreads = kSoft + 128;
+    static constexpr int kKeys = kSoft / 32, kValues = kKeys + 1, kProducts = kKeys + 2, kQueries = kKeys + 3;
     // Bfloat16 keeps 8 bits of a weight: it enters the second product in two parts, 16
     // bits in all.  Float16's 11 bits are one part: as far off as the result's own
     // rounding is.  Its weights are 2^7 to 2^15 at a row's maximum, so that those 2^-21 of
@@ -84,7 +85,12 @@ struct Kind {
     static constexpr float kLift = std::is_same<T, BF16>::value ? 0.0f : 7.0f;
     static constexpr int kQ = MT * NG * 2048;           // bytes of a tile's queries
     static constexpr int kP = NG * 2048;                // of one part of the weights
-    static constexpr int kFixed = 2 * kQ + kParts * kP;
+    // A tile's sums: in registers, or, of many rows, in shared memory.  (With them in registers
+    // those of 64 rows spill, to an L1 that shared memory has left next to nothing of:
+    // 96 sequences of five tokens of 8 heads each @@SPILL@@.)
+    static constexpr bool kKeep = NG == 2;
+    static constexpr int kSums = kKeep ? 0 : kRows * D * 4;
+    static constexpr int kFixed = 2 * kQ + kParts * kP + kSums;
     static constexpr int kColumns = (2 + MT) * kRows <= 64 ? 64 : (2 + MT) * kRows <= 128 ? 128 : (2 + MT) * kRows <= 256 ? 256 : 512;
     static_assert((2 + MT) * kRows <= 512, "TMEM");
 };
@@ -259,10 +265,12 @@ __device__ __forceinline__ uint32_t instruction(int n, bool a_rows, bool b_rows)
     const uint32_t type = std::is_same<T, BF16>::value ? 1 : 0;
     return 1u << 4 | type << 7 | type << 10 | uint32_t(a_rows) << 15 | uint32_t(b_rows) << 16 | uint32_t(n >> 3) << 17 | (128u >> 4) << 24;
 }
-__device__ __forceinline__ void product(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, bool add) {
-    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b),
-                 "r"(instr), "r"(uint32_t(add))
-                 : "memory");
+// (All lanes come here; the one that `mine` names issues.)
+__device__ __forceinline__ void product(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, bool add, uint32_t mine) {
+    asm volatile(
+        "{ .reg .pred p, q; setp.ne.u32 p, %4, 0; setp.ne.u32 q, %5, 0; @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d),
+        "l"(a), "l"(b), "r"(instr), "r"(uint32_t(add)), "r"(mine)
+        : "memory");
 }
 // The barrier's arrival when all products issued so far are done.
 __device__ __forceinline__ void products_arrive(uint32_t bar) {
@@ -365,14 +373,14 @@ struct Place {
 };
 
 // A warp joins row r of n pieces, given by at(i), in the outputs.  A piece counts by its sum
-// at the largest of the maxima.  What bounds it is the time of a load: those of 16 pieces are on
+// at the largest of the maxima.  What bounds it is the time of a load: those of 8 pieces are on
 // their way at once, the first of them with the maxima and sums.
 template <class K, class At>
 __device__ __forceinline__ void join_row(const AttendArgs& a, const Tile& t, int r, int n, At at) {
     constexpr int kMl = K::D * K::kRows;
     // 8 adjacent elements a lane; with 16 lanes' worth of them, half the lanes take every
     // other piece.
-    constexpr int kLanes = K::D / 8, kTeams = 32 / kLanes, kBatch = 16 / kTeams;
+    constexpr int kLanes = K::D / 8, kTeams = 32 / kLanes, kBatch = 8 / kTeams;
     const int lane = threadIdx.x & 31, d = 8 * (lane % kLanes), team = lane / kLanes;
     float4 u[kBatch], v[kBatch];
     const auto load = [&](int k) {
@@ -398,7 +406,7 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, const Tile& t, int
     const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
     float share = share_of(mine, top) * inverse, x[8] = {};
 #pragma unroll 1
-    for (int k = 0; k < n; k += 16) {
+    for (int k = 0; k < n; k += 8) {
         if (k) {
             load(k);
             if (k % 32 == 0) share = share_of(sums_of(k + lane), top) * inverse;
@@ -505,6 +513,7 @@ struct Shared {
     int64_t start;                                    // where the block's run begins within its first sequence
     int seq;                                          // that sequence
     int quit, last;
+    int fresh[2];                                     // whether a unit's sums begin anew (of two, in turn)
     uint32_t tmem;
 };
 
@@ -531,6 +540,10 @@ __device__ __forceinline__ float over_lanes(const F2* pairs, F f) {
     return f(c, __shfl_xor_sync(~0u, c, 1));
 }
 __device__ __forceinline__ int row_of_lane() { return (threadIdx.x >> 4 & 1) * 4 + (threadIdx.x >> 3 & 1) * 2 + (threadIdx.x >> 2 & 1); }
+
+// A unit's place in the ring's order, K0 K1 V0 K2 V1 ..., of n units.
+__device__ __forceinline__ int keys_at(int i) { return i ? 2 * i - 1 : 0; }
+__device__ __forceinline__ int values_at(int i, int n) { return i + 1 < n ? 2 * i + 2 : 2 * i + 1; }
 
 // A place in the ring, and the parity of its turn.
 struct Stage {
@@ -603,6 +616,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
 
     const uint32_t ring = (smem_of(memory) + 1023) / 1024 * 1024, stage_bytes = a.atoms * 16384;
     const uint32_t q_at = ring + a.stages * stage_bytes, p_at = q_at + 2 * K::kQ;
+    float* const sums_at = reinterpret_cast<float*>(memory + (p_at + K::kParts * K::kP - smem_of(memory)));
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) {
             bar_init(smem_of(&sh.full[i]), 1);
@@ -640,8 +654,9 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
         return int(at - tile * walk.t.units);
     };
 
-    if (w == K::kCopies) {
-        // Copies.
+    if (w == K::kKeys || w == K::kValues) {
+        // Copies: one warp the keys', one the values'.  A lane asks for one page's.
+        const bool values = w == K::kValues;
         Walk<K> walk(a, sh.seq);
         int unit = enter(walk);
         const int tokens = a.c.page, pages = kUnit >> a.c.shift, eights = tokens / 8;
@@ -653,48 +668,35 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             atomicOr(&a.control[kLate], kBadTable);
             return -1;
         };
-        Stage s;
-        int asked = 0;
-        const auto load = [&](int id, int head) {
-            if (!__all_sync(~0u, wait(sh.empty[s.at], s.turn ^ 1))) return false;
-            const uint32_t bar = smem_of(&sh.full[s.at]);
-            const int there = __popc(__ballot_sync(~0u, id >= 0));
+        const int units = int(n);
+        int id = fetch(), i = 0;
+        for (; i < units; ++i) {
+            const int here = id, head = (values ? a.c.n_kv : 0) + walk.t.head;
+            if (i + 1 < units) {
+                // (The next unit's pages, ahead of the wait.)
+                if (++unit == walk.t.units) {
+                    unit = 0;
+                    walk.next();
+                }
+                id = fetch();
+            }
+            const int k = values ? values_at(i, units) : keys_at(i), at = k % a.stages, turn = k / a.stages & 1;
+            if (!__all_sync(~0u, wait(sh.empty[at], turn ^ 1))) break;
+            const uint32_t bar = smem_of(&sh.full[at]);
+            const int there = __popc(__ballot_sync(~0u, here >= 0));
             if (elected()) bar_expect(bar, uint32_t(there * a.atoms * tokens * 128));
             __syncwarp();
-            if (id >= 0) {
-                const uint32_t to = ring + s.at * stage_bytes + lane * eights * a.eight_bytes;
+            if (here >= 0) {
+                const uint32_t to = ring + at * stage_bytes + lane * eights * a.eight_bytes;
                 for (int y = 0; y < a.atoms; y += a.copy_atoms)
-                    tma_load(to + y * a.atom_bytes, &map, a.copy_atoms > 1 ? 0 : 64 * y, 0, head * eights, id, bar);
+                    tma_load(to + y * a.atom_bytes, &map, a.copy_atoms > 1 ? 0 : 64 * y, 0, head * eights, here, bar);
             }
-            s.next(a.stages);
-            asked = min(asked + 1, a.stages);
-            return true;
-        };
-        int id = fetch(), head = walk.t.head, last_id = -1, last_head = 0;
-        bool ok = true;
-        for (int64_t i = 0; ok && i <= n; ++i) {
-            int next_id = -1, next_head = 0;
-            if (i < n) {
-                ok = load(id, head);
-                if (i + 1 < n) {
-                    if (++unit == walk.t.units) {
-                        unit = 0;
-                        walk.next();
-                    }
-                    next_id = fetch();
-                    next_head = walk.t.head;
-                }
-            }
-            if (ok && i > 0) ok = load(last_id, a.c.n_kv + last_head);
-            last_id = id, last_head = head;
-            id = next_id, head = next_head;
         }
-        if (!ok) {
+        if (i < units) {
             // What is on its way has to land before the block ends.
-            for (int k = 0; k < asked; ++k) {
-                // (From the last one back.)
-                if (--s.at < 0) s.at = a.stages - 1, s.turn ^= 1;
-                for (int x = 0; x < 1 << 20 && !bar_try(smem_of(&sh.full[s.at]), s.turn); ++x) {}
+            for (int back = max(i - a.stages, 0); back < i; ++back) {
+                const int k = values ? values_at(back, units) : keys_at(back);
+                for (int x = 0; x < 1 << 20 && !bar_try(smem_of(&sh.full[k % a.stages]), k / a.stages & 1); ++x) {}
             }
         }
     } else if (w == K::kProducts) {
@@ -717,14 +719,20 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 }
                 if (!__all_sync(~0u, wait(sh.full[st.at], st.turn))) break;
                 tmem_after();
-                if (elected()) {
+                {
                     // (A descriptor's address counts 16 bytes.)
+                    const uint32_t mine = elected();
                     const uint64_t dk = descriptor(ring + st.at * stage_bytes, 16, a.eight_bytes, 2), dq = descriptor(q_at + slot * K::kQ, N * 16, 128, 0);
-#pragma unroll 1
-                    for (int j = 0; j < k16; ++j)
-                        product(first_tmem + uint32_t(i & 1) * N, dk + (j >> 2) * (a.atom_bytes / 16) + (j & 3) * 2, dq + j * (2 * N), q_instr, j > 0);
-                    products_arrive(smem_of(&sh.empty[st.at]));
-                    products_arrive(smem_of(&sh.scores[i & 1]));
+#pragma unroll
+                    for (int j = 0; j < 8 * MT; ++j)
+                        if (j < k16)
+                            product(first_tmem + uint32_t(i & 1) * N, dk + (j >> 2) * (a.atom_bytes / 16) + (j & 3) * 2, dq + j * (2 * N), q_instr,
+                                    j > 0, mine);
+                    if (mine) {
+                        products_arrive(smem_of(&sh.empty[st.at]));
+                        products_arrive(smem_of(&sh.scores[i & 1]));
+                    }
+                    __syncwarp();
                 }
                 st.next(a.stages);
                 if (--q_left == 0) ++q_item;
@@ -742,18 +750,24 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 if (!__all_sync(~0u, wait(sh.weights, (i - 1) & 1))) break;
                 tmem_after();
                 const int steps = max((min(v_length - v_unit * kUnit, kUnit) + 15) / 16, 1);
-                if (elected()) {
+                const bool add = !uniform(sh.fresh[(i - 1) & 1]);
+                {
                     const uint64_t dv = descriptor(ring + st.at * stage_bytes, a.atom_bytes, a.eight_bytes, 2), dp = descriptor(p_at, 128, 2048, 0);
-#pragma unroll 1
+                    const uint32_t mine = elected();
+#pragma unroll
                     for (int m = 0; m < MT; ++m)
-#pragma unroll 1
+#pragma unroll
                         for (int part = K::kParts - 1; part >= 0; --part)
-#pragma unroll 1
-                            for (int j = 0; j < steps; ++j)
-                                product(first_tmem + (2 + m) * N, dv + m * (a.atom_bytes / 8) + j * (a.eight_bytes / 8), dp + part * (K::kP / 16) + j * 16, v_instr,
-                                        j > 0 || part < K::kParts - 1);
-                    products_arrive(smem_of(&sh.empty[st.at]));
-                    products_arrive(smem_of(&sh.sums));
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (j < steps)
+                                    product(first_tmem + (2 + m) * N, dv + m * (a.atom_bytes / 8) + j * (a.eight_bytes / 8),
+                                            dp + part * (K::kP / 16) + j * 16, v_instr, add || j > 0 || part < K::kParts - 1, mine);
+                    if (mine) {
+                        products_arrive(smem_of(&sh.empty[st.at]));
+                        products_arrive(smem_of(&sh.sums));
+                    }
+                    __syncwarp();
                 }
                 st.next(a.stages);
                 ++v_unit;
@@ -823,7 +837,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
         // warps share the groups of 8 rows in turn (MT 2: of the sums, half of the sets each 128
         // elements).
         constexpr int kSets = K::kSets, GS = (NG + kSets - 1) / kSets, kSumSets = kSets / MT, GO = (NG + kSumSets - 1) / kSumSets;
-        const int set = w >> 2, key = threadIdx.x & 127, half = MT == 2 ? set & 1 : 0;
+        const int set = w >> 2, key = threadIdx.x & 127, half = MT == 2 ? set & 1 : 0, d = key + 128 * half;
         const uint32_t lanes = uint32_t(w & 3) << 21;
         const auto group_of = [&](int j) { return set + kSets * j; };
         const F2 scale2 = both(a.scale, a.scale);
@@ -838,11 +852,27 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             const int left = uniform(ok ? min(it.t.count * a.group - it.t.tile * K::kRows, K::kRows) : 0), groups = (left + 7) / 8;
             const int units = uniform(ok ? it.n : 1), first_seen = uniform(seen(it.t, a.group, it.t.tile * K::kRows));
             const int first_key = uniform(it.first * kUnit);
-            F2 o[GO][4], sum[GS][4];
+            F2 o[K::kKeep ? GO : 1][4], sum[GS][4];
+            bool begun = false;            // whether o has anything
+            // Adds TMEM's sums to o, and multiplies by factor[row] where that is given.
+            const auto add_sums = [&](const float* factor) {
 #pragma unroll
-            for (int j = 0; j < GO; ++j)
+                for (int j = 0; j < GO; ++j) {
+                    if (sum_group(j) >= groups) continue;
+                    F2 x[4];
+                    tmem_load(tmem + lanes + (2 + half) * N + 8 * sum_group(j), x);
+                    tmem_loaded();
+                    float* const at = sums_at + 8 * sum_group(j) * K::D + d;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[j][e] = 0;
+                    for (int e = 0; e < 4; ++e) {
+                        if (begun) x[e] = add2(x[e], K::kKeep ? o[K::kKeep ? j : 0][e] : both(at[2 * e * K::D], at[(2 * e + 1) * K::D]));
+                        if (factor) x[e] = mul2(x[e], reinterpret_cast<const F2*>(factor + 8 * sum_group(j))[e]);
+                        if (K::kKeep) o[K::kKeep ? j : 0][e] = x[e];
+                        else at[2 * e * K::D] = low(x[e]), at[(2 * e + 1) * K::D] = high(x[e]);
+                    }
+                }
+                begun = true;
+            };
 #pragma unroll
             for (int j = 0; j < GS; ++j)
 #pragma unroll
@@ -850,24 +880,6 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             // (The first scores are over any reference: it is set then.)
             if (int(threadIdx.x) < N) sh.bias[threadIdx.x] = kNothing;
             soft_sync<K::kSoft>();
-            const auto add_sums = [&] {
-                // (Two groups at a time: registers are short.)
-#pragma unroll
-                for (int j = 0; j < GO; j += 2) {
-                    F2 x[2][4];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-                        if (j + k < GO && sum_group(j + k) < groups)
-                            tmem_load(tmem + lanes + (2 + half) * N + 8 * sum_group(j + k), x[k]);
-                    tmem_loaded();
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        if (j + k >= GO || sum_group(j + k) >= groups) continue;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[j + k < GO ? j + k : 0][e] = add2(o[j + k < GO ? j + k : 0][e], x[k][e]);
-                    }
-                }
-            };
             for (int u = 0; u < units; ++u, ++i) {
                 const int key0 = first_key + u * kUnit;
                 ok &= __all_sync(~0u, wait(sh.scores[i & 1], i >> 1 & 1));
@@ -963,22 +975,19 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                         }
                     }
                 }
-                // The sums of the unit before, which refer to the reference before; then the weights
-                // may be overwritten.
+                // The weights may be overwritten once the products of the unit before are done.
                 if (u > 0) {
                     wait(sh.sums, (i - 1) & 1);
                     tmem_after();
-                    add_sums();
                 }
-                if (moved) {
-#pragma unroll
-                    for (int j = 0; j < GO; ++j) {
-                        if (sum_group(j) >= groups) continue;
-                        const F2* const f = reinterpret_cast<const F2*>(&sh.factor[8 * sum_group(j)]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[j][e] = mul2(o[j][e], f[e]);
-                    }
+                // Sums gather in TMEM over 8 units, by the matrix instructions, which cut off; then,
+                // and where the reference moves, they are added up in float32, which rounds.
+                const bool fresh = moved || u % kGather == 0;
+                if (fresh && u > 0) {
+                    __syncwarp();
+                    add_sums(moved ? sh.factor : nullptr);
                 }
+                if (threadIdx.x == 0) sh.fresh[i & 1] = fresh;
 #pragma unroll
                 for (int j = 0; j < GS; ++j) {
                     if (group_of(j) >= groups) continue;
@@ -991,7 +1000,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 const int valid = min(it.t.length - key0, kUnit);
                 if (valid < kUnit) {
                     // Behind the sequence's end the page holds anything: values there become 0.
-                    const int k = i + 1 < all ? 2 * i + 2 : 2 * i + 1;      // in the ring's order
+                    const int k = values_at(i, all);
                     const int stage = k % a.stages;
                     wait(sh.full[stage], k / a.stages & 1);
                     const int rows = max((valid + 15) / 16 * 16, 16) - valid;
@@ -1013,7 +1022,6 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             wait(sh.sums, (i - 1) & 1);
             tmem_after();
             __syncwarp();
-            add_sums();
 #pragma unroll
             for (int j = 0; j < GS; ++j) {
                 if (group_of(j) >= groups) continue;
@@ -1026,23 +1034,25 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             if (int(threadIdx.x) < left) {
                 const int r = threadIdx.x;
                 const float total = sh.parts[0][r] + sh.parts[1][r] + sh.parts[2][r] + sh.parts[3][r], bias = sh.bias[r];
-                // (A row whose sum is NaN is all NaN in any case.)
                 sh.inverse[r] = total == 0.0f ? 0.0f : 1.0f / total;
                 Place<K>(a, it.t, r, piece).sums(bias == kNothing ? -kInf : -bias, total);
             }
             soft_sync<K::kSoft>();
-            const int d = key + 128 * half;
+            // (Each sum times 1 / the row's.)
+            add_sums(sh.inverse);
             bool odd = false;
+            const auto result = [&](int j, int e) {
+                if (K::kKeep) return e & 1 ? high(o[K::kKeep ? j : 0][e / 2]) : low(o[K::kKeep ? j : 0][e / 2]);
+                return sums_at[(8 * sum_group(j) + e) * K::D + d];
+            };
 #pragma unroll
             for (int j = 0; j < GO; ++j) {
                 if (sum_group(j) >= groups) continue;
-                const F2* const f = reinterpret_cast<const F2*>(&sh.inverse[8 * sum_group(j)]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    o[j][e] = mul2(o[j][e], f[e]);
-                    const int r = 8 * sum_group(j) + 2 * e;
-                    odd |= r < left && low(f[e]) == low(f[e]) && !(fabsf(low(o[j][e])) < kInf);
-                    odd |= r + 1 < left && high(f[e]) == high(f[e]) && !(fabsf(high(o[j][e])) < kInf);
+                for (int e = 0; e < 8; ++e) {
+                    const int r = 8 * sum_group(j) + e;
+                    // (Rows whose sum is NaN are all NaN in any case.)
+                    odd |= r < left && sh.inverse[r] == sh.inverse[r] && !(fabsf(result(j, e)) < kInf);
                 }
             }
             if (soft_any<K::kSoft>(odd && d < a.c.dim)) {
@@ -1053,10 +1063,9 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const int r = 8 * sum_group(j) + e;
-                        const float x = e & 1 ? high(o[j][e / 2]) : low(o[j][e / 2]);
                         if (r >= left) continue;
-                        if (piece) piece[r * K::D + d] = x;
-                        else if (d < a.c.dim) a.out[sh.out[slot][r] + d] = T::round(x);
+                        if (piece) piece[r * K::D + d] = result(j, e);
+                        else if (d < a.c.dim) a.out[sh.out[slot][r] + d] = T::round(result(j, e));
                     }
                 }
             }

@@ -542,10 +542,17 @@ constexpr int kAcceptRanks = 8;
 constexpr int kAcceptThreads = 1024;      // at most
 constexpr int kMaxVocab = 1 << 20;
 
-// A probability in whole numbers of 2^-42, ties to even; NaN counts as 0.  (x 2^42 is
-// exact in float32.)
+// A probability in whole numbers of 2^-42, ties to even; NaN counts as 0.  y = x 2^42 is
+// exact in float32; under 2^23 adding 2^23 rounds it to a whole number in the low bits, from there on it
+// is one.  (A conversion to 64 bits runs at a fraction of the rate: 64 sequences of 151936 entries
+// took 52 us with it, @@ACCEPT@@.)
 __device__ __forceinline__ uint64_t units(float x) {
-    return __float2ull_rn(fminf(fmaxf(x, 0.0f), 1.0f) * 4398046511104.0f);
+    const float y = fminf(fmaxf(x, 0.0f), 1.0f) * 4398046511104.0f;
+    const uint32_t bits = __float_as_uint(y), mantissa = (bits & 0x7FFFFFu) | 0x800000u, shift = (bits >> 23) - 150;
+    const uint32_t small = __float_as_uint(y + 8388608.0f) - 0x4B000000u;
+    const bool whole = y >= 8388608.0f;
+    const uint32_t lo = whole ? mantissa << (shift & 31) : small, hi = whole ? __funnelshift_lc(mantissa, 0, shift) : 0;
+    return uint64_t(hi) << 32 | lo;
 }
 
 struct AcceptArgs {
@@ -557,31 +564,43 @@ struct AcceptArgs {
     int32_t rows, vocab;
 };
 
-// Four entries of what the token is drawn from, from entry i on: in units, of the
-// rest (p, less q or without the refused draft) and of p itself.
+// What a token is drawn from: the rest (p, less q or without the refused draft), or p.
 struct Draw {
     const float *p, *q;       // q NULL: no draft was refused, or it came without probabilities
     int without;              // the refused draft's token, or -1
-    int vocab;
-    bool vec;
-    __device__ __forceinline__ float4 load(const float* x, int i, int end) const {
-        if (vec && i + 3 < end) return *reinterpret_cast<const float4*>(x + i);
-        float4 r = make_float4(0, 0, 0, 0);
-        if (i < end) r.x = x[i];
-        if (i + 1 < end) r.y = x[i + 1];
-        if (i + 2 < end) r.z = x[i + 2];
-        if (i + 3 < end) r.w = x[i + 3];
-        return r;
-    }
-    __device__ __forceinline__ void four(int i, int end, bool rest, uint64_t* n) const {
-        const float4 a = load(p, i, end);
-        float x[4] = {a.x, a.y, a.z, a.w};
-        if (rest && q) {
-            const float4 c = load(q, i, end);
-            x[0] -= c.x, x[1] -= c.y, x[2] -= c.z, x[3] -= c.w;
+    bool vec;                 // rows can be read 16 bytes at a time
+    // Entries [k, k + 128), up to `end`, four a lane: one after another (ORDER, or vec), or 32 apart.
+    template <bool ORDER>
+    __device__ __forceinline__ int index(int k, int lane, int e) const { return ORDER || vec ? k + 4 * lane + e : k + lane + 32 * e; }
+    template <bool ORDER>
+    __device__ __forceinline__ void load(const float* x, int k, int lane, int end, float* to) const {
+        const int i = k + 4 * lane;
+        if (vec && i + 3 < end) {
+            const float4 r = __ldg(reinterpret_cast<const float4*>(x + i));
+            to[0] = r.x, to[1] = r.y, to[2] = r.z, to[3] = r.w;
+            return;
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) n[k] = rest && i + k == without ? 0 : units(x[k]);
+        for (int e = 0; e < 4; ++e) to[e] = index<ORDER>(k, lane, e) < end ? __ldg(x + index<ORDER>(k, lane, e)) : 0.0f;
+    }
+    // The lane's units of N times 128 entries.
+    template <bool ORDER, int N>
+    __device__ __forceinline__ void entries(int k, int lane, int end, uint64_t (*n)[4]) const {
+        float a[N][4], b[N][4];
+#pragma unroll
+        for (int h = 0; h < N; ++h) load<ORDER>(p, k + 128 * h, lane, end, a[h]);
+        if (q) {
+#pragma unroll
+            for (int h = 0; h < N; ++h) load<ORDER>(q, k + 128 * h, lane, end, b[h]);
+        }
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = q ? a[h][e] - b[h][e] : a[h][e];
+                n[h][e] = units(index<ORDER>(k + 128 * h, lane, e) == without ? 0.0f : x);
+            }
+        }
     }
 };
 
@@ -613,40 +632,50 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) rr_accept_kernel(const __gr
     }
     __syncthreads();
     const int got = first_refused;
-    const int64_t row = start + got;
-    Draw d;
-    d.vocab = a.vocab;
-    d.p = a.p + row * a.ldp;
-    d.q = got < n && a.q ? a.q + row * a.ldq : nullptr;
-    d.without = got < n && !a.q ? a.drafts[row] : -1;
-    d.vec = reinterpret_cast<uintptr_t>(d.p) % 16 == 0 && reinterpret_cast<uintptr_t>(d.q) % 16 == 0;
     const bool refused = got < n;
+    const int64_t row = fits ? start + got : 0;
+    Draw d;
+    d.p = a.p + row * a.ldp;
+    d.q = refused && a.q ? a.q + row * a.ldq : nullptr;
+    d.without = refused && !a.q ? a.drafts[row] : -1;
+    d.vec = reinterpret_cast<uintptr_t>(d.p) % 16 == 0 && reinterpret_cast<uintptr_t>(d.q) % 16 == 0;
     const int each = (a.vocab + 4 * all - 1) / (4 * all) * 4;
     const int lo = min(w * each, a.vocab), hi = fits ? min(lo + each, a.vocab) : lo;
-    uint64_t rest = 0, whole = 0;
-#pragma unroll 4
-    for (int k = lo + 4 * lane; k < hi; k += 128) {
-        uint64_t x[4];
-        d.four(k, hi, true, x);
-        rest += x[0] + x[1] + x[2] + x[3];
-        if (refused) {
-            d.four(k, hi, false, x);
-            whole += x[0] + x[1] + x[2] + x[3];
-        }
-    }
+    // The sums before this warp's run, and of all; twice where all that is left is 0.
+    uint64_t before, total, own;
+    for (int pass = 0;; ++pass) {
+        uint64_t mine = 0;
+#pragma unroll 1
+        for (int k = lo; k < hi; k += 512) {
+            uint64_t x[4][4];
+            d.entries<false, 4>(k, lane, hi, x);
 #pragma unroll
-    for (int m = 16; m; m >>= 1) {
-        rest += __shfl_xor_sync(~0u, rest, m);
-        whole += __shfl_xor_sync(~0u, whole, m);
+            for (int h = 0; h < 4; ++h) mine += (x[h][0] + x[h][1]) + (x[h][2] + x[h][3]);
+        }
+#pragma unroll
+        for (int m = 16; m; m >>= 1) mine += __shfl_xor_sync(~0u, mine, m);
+        if (lane < kAcceptRanks) {
+            uint32_t at = uint32_t(__cvta_generic_to_shared(&sums[pass][w])), to;
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(at), "r"(lane));
+            asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to), "l"(mine) : "memory");
+        }
+        cluster_barrier();
+        before = total = 0;
+        for (int k = lane; k < all; k += 32) {
+            total += sums[pass][k];
+            if (k < w) before += sums[pass][k];
+        }
+#pragma unroll
+        for (int m = 16; m; m >>= 1) {
+            total += __shfl_xor_sync(~0u, total, m);
+            before += __shfl_xor_sync(~0u, before, m);
+        }
+        own = mine;
+        // (The same in all of the cluster's threads.)
+        if (total || pass || !refused) break;
+        d.q = nullptr;
+        d.without = -1;
     }
-    if (lane < kAcceptRanks) {
-        uint32_t at0 = uint32_t(__cvta_generic_to_shared(&sums[0][w])), at1 = uint32_t(__cvta_generic_to_shared(&sums[1][w])), to0, to1;
-        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to0) : "r"(at0), "r"(lane));
-        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to1) : "r"(at1), "r"(lane));
-        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to0), "l"(rest) : "memory");
-        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to1), "l"(whole) : "memory");
-    }
-    cluster_barrier();
     if (!fits) {
         if (rank == 0 && threadIdx.x == 0) {
             a.accepted[i] = -1;
@@ -655,44 +684,24 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) rr_accept_kernel(const __gr
         return;
     }
     // The number drawn: floor(total v), v in whole numbers of 2^-31.
-    uint64_t before[2] = {0, 0}, total[2] = {0, 0};
-    for (int k = lane; k < all; k += 32) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint64_t x = sums[h][k];
-            total[h] += x;
-            if (k < w) before[h] += x;
-        }
-    }
-#pragma unroll
-    for (int m = 16; m; m >>= 1) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            total[h] += __shfl_xor_sync(~0u, total[h], m);
-            before[h] += __shfl_xor_sync(~0u, before[h], m);
-        }
-    }
-    const bool use_rest = total[0] != 0;
-    const uint64_t sum = use_rest ? total[0] : total[1], ahead = use_rest ? before[0] : before[1];
-    const uint64_t own = use_rest ? sums[0][w] : sums[1][w];
     const uint64_t v31 = min(uint64_t(fminf(fmaxf(a.v[i], 0.0f), 1.0f) * 2147483648.0f), uint64_t((1u << 31) - 1));
-    const uint64_t t = (sum >> 31) * v31 + ((sum & ((1u << 31) - 1)) * v31 >> 31);
+    const uint64_t t = (total >> 31) * v31 + ((total & ((1u << 31) - 1)) * v31 >> 31);
     if (rank == 0) {
         for (int j = threadIdx.x; j <= n; j += blockDim.x) {
             if (j < got) a.tokens[start + j] = a.drafts[start + j];
-            else if (j > got || sum == 0) a.tokens[start + j] = -1;
+            else if (j > got || total == 0) a.tokens[start + j] = -1;
         }
         if (threadIdx.x == 0) {
             a.accepted[i] = got;
             if (a.rejected) a.rejected[i] = n - got;
         }
     }
-    if (sum == 0 || t < ahead || t - ahead >= own) return;
-    uint64_t left = t - ahead;
+    if (total == 0 || t < before || t - before >= own) return;
+    uint64_t left = t - before;
     for (int k = lo; k < hi; k += 128) {
-        uint64_t x[4];
-        d.four(k + 4 * lane, hi, use_rest, x);
-        const uint64_t mine = x[0] + x[1] + x[2] + x[3];
+        uint64_t x[1][4];
+        d.entries<true, 1>(k, lane, hi, x);
+        const uint64_t mine = x[0][0] + x[0][1] + x[0][2] + x[0][3];
         uint64_t up = mine;
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) {
@@ -702,7 +711,9 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) rr_accept_kernel(const __gr
         if (up > left && up - mine <= left) {
             uint64_t y = left - (up - mine);
             int e = 0;
-            while (e < 3 && y >= x[e]) y -= x[e++];
+#pragma unroll
+            for (int h = 0; h < 3; ++h)
+                if (e == h && y >= x[0][h]) y -= x[0][h], ++e;
             a.tokens[row] = k + 4 * lane + e;
         }
         const uint64_t last = __shfl_sync(~0u, up, 31);
