@@ -203,9 +203,11 @@ __device__ __forceinline__ int new_tokens(const int32_t* starts, int i) { return
 
 // A listed sequence's next tokens: where they begin, and the page that is partly filled.
 struct Growth {
-    int s, length, count, filled;
-    int32_t page;        // partly filled (-1: none, or no tokens come)
-    int64_t entry;       // its place in the table
+    int s = 0, length = 0, count = 0, filled = 0;
+    int32_t page = -1;   // partly filled (-1: none, or no tokens come)
+    int32_t holders = 0; // of that page
+    int64_t entry = 0;   // its place in the table
+    __device__ __forceinline__ Growth() {}
     __device__ __forceinline__ Growth(const CacheShape& c, const Book& b, const int32_t* seqs, const int32_t* starts, int i) {
         s = seqs[i];
         count = new_tokens(starts, i);
@@ -214,6 +216,7 @@ struct Growth {
         entry = int64_t(s) * c.max_pages + (length >> c.shift);
         page = filled && count ? __ldcg(&b.table[entry]) : -1;
         if (!c.has_page(page)) page = -1;
+        if (page >= 0) holders = __ldcg(&b.refs[page]);
     }
     __device__ __forceinline__ int grown(const CacheShape& c) const {
         return pages_of(length + count, c.shift) - pages_of(length, c.shift);
@@ -242,16 +245,24 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_extend_kernel(const __g
     bad = agree(bad);
     if (r.rank == 0 && threadIdx.x == 0) b.control[kMoves] = 0;
     const int lo = int(r.first(n)), hi = int(r.end(n));
+    // A thread's first sequence stays in its registers; there are others only in long lists.
+    const auto growth_of = [&](int base, const Growth& kept) {
+        const int i = base + int(threadIdx.x);
+        return base == lo || i >= hi ? kept : Growth(c, b, seqs, starts, i);
+    };
+    Growth kept;
+    if (!bad && lo + int(threadIdx.x) < hi) kept = Growth(c, b, seqs, starts, lo + int(threadIdx.x));
     // Who holds each shared page that is partly filled, among the listed ones.
-    if (!bad) {
-        for (int i = lo + int(threadIdx.x); i < hi; i += kBookThreads) {
-            const Growth g(c, b, seqs, starts, i);
-            if (g.page >= 0 && __ldcg(&b.refs[g.page]) > 1) {
-                atomicAdd(&b.held[g.page], 1);
-                atomicMax(&b.last[g.page], i + 1);
-            }
+    for (int base = lo; !bad && base < hi; base += kBookThreads) {
+        const int i = base + int(threadIdx.x);
+        const Growth g = growth_of(base, kept);
+        if (i < hi && g.page >= 0 && g.holders > 1) {
+            atomicAdd(&b.held[g.page], 1);
+            atomicMax(&b.last[g.page], i + 1);
         }
     }
+    const Pages mine(r, c.n_pages);
+    const int64_t free = bad ? 0 : mine.free(b.refs);
     cluster_barrier();
     if (bad) return fail(b, r, bad);
     // A copy for each holder, but for the last where all of them are listed; then whole
@@ -259,13 +270,10 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_extend_kernel(const __g
     int64_t needed = 0;
     for (int base = lo; base < hi; base += kBookThreads) {
         const int i = base + int(threadIdx.x);
+        const Growth g = growth_of(base, kept);
         int need = 0, copy = 0;
         if (i < hi) {
-            const Growth g(c, b, seqs, starts, i);
-            if (g.page >= 0) {
-                const int holders = __ldcg(&b.refs[g.page]);
-                copy = holders > 1 && !(__ldcg(&b.held[g.page]) == holders && __ldcg(&b.last[g.page]) == i + 1);
-            }
+            if (g.page >= 0 && g.holders > 1) copy = !(__ldcg(&b.held[g.page]) == g.holders && __ldcg(&b.last[g.page]) == i + 1);
             need = copy + g.grown(c);
         }
         int64_t total;
@@ -274,8 +282,6 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_extend_kernel(const __g
         if (i < hi) b.plan[i] = int32_t(min(at, int64_t(INT_MAX / 2))) * 2 + copy;
         needed += total;
     }
-    const Pages mine(r, c.n_pages);
-    const int64_t free = mine.free(b.refs);
     if (threadIdx.x == 0) {
         b.sums[r.rank] = needed;
         b.sums[kBookRanks + r.rank] = free;
@@ -300,54 +306,79 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_extend_kernel(const __g
     }
     cluster_barrier();
     const int lane = threadIdx.x & 31;
-    for (int i = lo + int(threadIdx.x >> 5); i < hi; i += kBookWarps) {
-        const Growth g(c, b, seqs, starts, i);
-        __syncwarp();
-        if (g.page >= 0 && lane == 0) b.held[g.page] = b.last[g.page] = 0;
+    for (int base = lo; base < hi; base += kBookThreads) {
+        const int i = base + int(threadIdx.x);
+        Growth g = growth_of(base, kept);
+        if (i >= hi) g.page = -1, g.count = 0;
+        if (g.page >= 0 && g.holders > 1) b.held[g.page] = b.last[g.page] = 0;
         if (bad) continue;
-        const int plan = b.plan[i], copy = plan & 1;
-        const int64_t at = needed_before + (plan >> 1);
-        if (copy && lane == 0) {
+        const int plan = i < hi ? b.plan[i] : 0, copy = plan & 1;
+        int64_t at = needed_before + (plan >> 1);
+        if (copy) {
             const int to = __ldcg(&b.free[at]);
             b.table[g.entry] = to;
             b.refs[to] = 1;
             atomicSub(&b.refs[g.page], 1);
             b.moves[atomicAdd(&b.control[kMoves], 1)] = make_int4(g.page, to, g.filled, 0);
         }
-        const int first = pages_of(g.length, c.shift), grown = g.grown(c);
-        for (int j = lane; j < grown; j += 32) {
-            const int to = __ldcg(&b.free[at + copy + j]);
-            b.table[int64_t(g.s) * c.max_pages + first + j] = to;
+        at += copy;
+        if (i < hi) b.lengths[g.s] = g.length + g.count;
+        // New pages: of a sequence that takes many, by its warp.
+        const int grown = i < hi ? g.grown(c) : 0;
+        int64_t entry = i < hi ? int64_t(g.s) * c.max_pages + pages_of(g.length, c.shift) : 0;
+        for (int j = 0; j < min(grown, 2); ++j) {
+            const int to = __ldcg(&b.free[at + j]);
+            b.table[entry + j] = to;
             b.refs[to] = 1;
         }
-        if (lane == 0) b.lengths[g.s] = g.length + g.count;
+        for (uint32_t many = __ballot_sync(~0u, grown > 2); many; many &= many - 1) {
+            const int x = __ffs(many) - 1, n = __shfl_sync(~0u, grown, x);
+            const int64_t from = __shfl_sync(~0u, at, x), into = __shfl_sync(~0u, entry, x);
+            for (int j = 2 + lane; j < n; j += 32) {
+                const int to = __ldcg(&b.free[from + j]);
+                b.table[into + j] = to;
+                b.refs[to] = 1;
+            }
+        }
     }
     if (bad) fail(b, r, bad);
 }
 
-// The filled tokens of the pages that rr_cache_extend_kernel took copies of.  A warp
-// takes one run: a layer's keys or values of one head, `filled` rows of `pitch`.
+// The filled tokens of the pages that rr_cache_extend_kernel took copies of.  A run is
+// a layer's keys or values of one head, `filled` rows of `pitch`; a block takes 16 runs of a
+// page, two a warp.
+constexpr int kRuns = 16;
 __global__ void __launch_bounds__(256) rr_cache_copy_rows_kernel(const __grid_constant__ CacheShape c, const Book b, char* pages) {
     after_previous();
     if (__ldcg(&b.control[kState])) return;
     const int moves = __ldcg(&b.control[kMoves]);
-    const int lane = threadIdx.x & 31;
-    const int64_t warp = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5), warps = int64_t(gridDim.x) * 8;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int vecs_row = c.pitch / 8;
-    for (int64_t task = warp; task < int64_t(moves) * c.runs; task += warps) {
-        const int4 m = __ldcg(&b.moves[task / c.runs]);
-        const int64_t run = task % c.runs * c.run_bytes;
-        const uint4* from = reinterpret_cast<const uint4*>(pages + m.x * c.page_bytes + run);
-        uint4* to = reinterpret_cast<uint4*>(pages + m.y * c.page_bytes + run);
+    const unsigned parts = unsigned(c.runs + kRuns - 1) / kRuns;
+    for (uint64_t task = blockIdx.x; task < uint64_t(moves) * parts; task += gridDim.x) {
+        const unsigned move = task >> 32 ? unsigned(task / parts) : unsigned(task) / parts;
+        const int run = int(task - uint64_t(move) * parts) * kRuns + 2 * w;
+        if (run >= c.runs) continue;
+        const bool second = run + 1 < c.runs;
+        const int4 m = __ldcg(&b.moves[move]);
+        const int64_t step = c.run_bytes / 16;
+        const uint4* from = reinterpret_cast<const uint4*>(pages + m.x * c.page_bytes + run * c.run_bytes);
+        uint4* to = reinterpret_cast<uint4*>(pages + m.y * c.page_bytes + run * c.run_bytes);
         const int vecs = m.z * vecs_row;
         for (int i = lane; i < vecs; i += 128) {
-            uint4 v[4];
+            uint4 u[4], v[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (i + 32 * k < vecs) v[k] = from[i + 32 * k];
+                if (i + 32 * k < vecs) {
+                    u[k] = from[i + 32 * k];
+                    if (second) v[k] = from[step + i + 32 * k];
+                }
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (i + 32 * k < vecs) to[i + 32 * k] = v[k];
+                if (i + 32 * k < vecs) {
+                    to[i + 32 * k] = u[k];
+                    if (second) to[step + i + 32 * k] = v[k];
+                }
         }
     }
 }
@@ -439,30 +470,76 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_compact_kernel(const __
     }
 }
 
-// The moved pages' contents, 16 KiB a block and turn, and their places in the table.
-constexpr int kMoveChunk = 16384;
+// The moved pages' contents and their places in the table.  One thread of a block (one an SM)
+// has 32 KiB at a time copied through shared memory by bulk copies, four of them on their
+// way in while two are on theirs out; its other warps see to the table.  (Loads and
+// stores by all threads, 64 bytes of each in flight: 304 MB in 58 us, 5.2 TB/s; so @@MOVE@@.)
+constexpr int kMoveChunk = 32768, kMoveStages = 6, kMoveAhead = 4;
 __global__ void __launch_bounds__(256) rr_cache_move_kernel(const __grid_constant__ CacheShape c, const Book b, char* pages) {
+    extern __shared__ __align__(128) char stages[];
+    __shared__ uint64_t full[kMoveStages];
     after_previous();
     if (__ldcg(&b.control[kState])) return;
     const int moves = __ldcg(&b.control[kMoves]), used = __ldcg(&b.control[kUsed]);
     if (!moves) return;
-    const int64_t chunks = (c.page_bytes + kMoveChunk - 1) / kMoveChunk;
-    for (int64_t task = blockIdx.x; task < moves * chunks; task += gridDim.x) {
-        const int4 m = __ldcg(&b.moves[task / chunks]);
-        const int64_t at = task % chunks * kMoveChunk;
-        const int vecs = int(min(c.page_bytes - at, int64_t(kMoveChunk)) / 16);
-        const uint4* from = reinterpret_cast<const uint4*>(pages + m.x * c.page_bytes + at);
-        uint4* to = reinterpret_cast<uint4*>(pages + m.y * c.page_bytes + at);
-        uint4 v[4];
+    if (threadIdx.x == 0) {
+        const auto smem = [](const void* p) { return uint32_t(__cvta_generic_to_shared(p)); };
+        for (int i = 0; i < kMoveStages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem(&full[i])) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        const int64_t chunks = (c.page_bytes + kMoveChunk - 1) / kMoveChunk, all = moves * chunks;
+        const int n = int(all > blockIdx.x ? (all - blockIdx.x + gridDim.x - 1) / gridDim.x : 0);
+        int4 move = make_int4(0, 0, 0, 0);
+        int64_t out[kMoveStages];
+        int bytes[kMoveStages];
+        // (Unrolled by stage, so that out and bytes are registers.)
+        bool ok = true;
+        for (int base = 0; ok && base < n + kMoveAhead; base += kMoveStages) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (int(threadIdx.x) + 256 * k < vecs) v[k] = __ldcs(&from[threadIdx.x + 256 * k]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (int(threadIdx.x) + 256 * k < vecs) __stcs(&to[threadIdx.x + 256 * k], v[k]);
+            for (int s = 0; s < kMoveStages; ++s) {
+                const int i = base + s;
+                if (ok && i < n) {
+                    // The stage's last copy out has been read.
+                    if (i >= kMoveStages) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kMoveStages - kMoveAhead - 1) : "memory");
+                    const int64_t task = blockIdx.x + int64_t(i) * gridDim.x, m = task / chunks, at = (task - m * chunks) * kMoveChunk;
+                    move = __ldcg(&b.moves[m]);
+                    bytes[s] = int(min(c.page_bytes - at, int64_t(kMoveChunk)));
+                    out[s] = move.y * c.page_bytes + at;
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem(&full[s])), "r"(bytes[s]) : "memory");
+                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                                     smem(stages + s * kMoveChunk)),
+                                 "l"(pages + move.x * c.page_bytes + at), "r"(bytes[s]), "r"(smem(&full[s]))
+                                 : "memory");
+                }
+                constexpr int kBack = kMoveStages - kMoveAhead;
+                const int j = i - kMoveAhead, from = (s + kBack) % kMoveStages;
+                if (ok && j >= 0 && j < n) {
+                    uint32_t done = 0;
+                    const long long t0 = clock64();
+                    while (!done) {
+                        asm volatile(
+                            "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                            : "=r"(done)
+                            : "r"(smem(&full[from])), "r"(j / kMoveStages & 1)
+                            : "memory");
+                        if (!done && clock64() - t0 > 4000000000ll) break;       // two seconds or so
+                    }
+                    if (!done) {
+                        atomicOr(&b.control[kLate], kBadWait);
+                        ok = false;
+                    } else {
+                        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(pages + out[from]),
+                                     "r"(smem(stages + from * kMoveChunk)), "r"(bytes[from])
+                                     : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                }
+            }
+        }
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
+    if (threadIdx.x < 32) return;
     const int lane = threadIdx.x & 31;
-    for (int s = int(blockIdx.x * 8 + (threadIdx.x >> 5)); s < c.max_seqs; s += int(gridDim.x) * 8) {
+    for (int s = int(blockIdx.x * 7 + (threadIdx.x >> 5)) - 1; s < c.max_seqs; s += int(gridDim.x) * 7) {
         const int length = __ldcg(&b.lengths[s]);
         if (!c.has_length(length)) continue;
         int32_t* const row = b.table + int64_t(s) * c.max_pages;
@@ -491,15 +568,17 @@ __global__ void __launch_bounds__(256) rr_cache_append_kernel(const __grid_const
     if (row >= rows) return;
     int i = row, j = 0, count = 1;
     if (starts) {
-        // The last sequence that starts at or before the row.
-        int lo = 0, hi = n;
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (starts[mid + 1] > row) hi = mid;
-            else lo = mid + 1;
+        // The first sequence that ends behind the row; 32 places looked at at a time.
+        int lo = 0, left = n;
+        while (left > 0) {
+            const int step = (left + 31) / 32, at = lo + min((lane + 1) * step, left);
+            const int before = __popc(__ballot_sync(~0u, starts[at] <= row && (lane + 1) * step <= left));
+            // (Sequences lo .. lo + before * step - 1 end at or before it.)
+            lo += before * step;
+            left = min(step - 1, left - before * step);
         }
         i = lo;
-        if (i >= n || row < starts[i]) return;
+        if (i >= n || row < starts[i] || row >= starts[i + 1]) return;
         j = row - starts[i];
         count = starts[i + 1] - starts[i];
     }
@@ -748,9 +827,9 @@ cudaError_t launch_clusters(void (*kernel)(Params...), int cluster, unsigned gri
 
 size_t bits_bytes(const rr_cache* C) { return size_t(C->max_seqs + 31) / 32 * 4; }
 
-// Blocks that share a call's bookkeeping: with 8 the lists and the pool are gone through
-// 8 times as fast, but a barrier takes longer.
-int book_ranks(int64_t entries) { return entries <= 4 * kBookThreads ? 1 : kBookRanks; }
+// Blocks that share a call's bookkeeping: one where it has a warp for each part of the work and
+// goes through the pool's pages at once.
+int book_ranks(int64_t warps, int64_t pages) { return warps <= kBookWarps && pages <= 4 * kBookThreads ? 1 : kBookRanks; }
 
 rr_status check_list(int n, const rr_cache* C) {
     if (n < 0 || n > C->max_seqs) return rr_fail(RR_EINVAL, "%d sequences: 0..%d", n, C->max_seqs);
@@ -808,7 +887,7 @@ extern "C" rr_status rr_cache_fork(const rr_cache* C, void* book, const int32_t*
     RR_TRY(check_device(dev, children, 4, "children"));
     Book b;
     book_of(C, book, &b);
-    const int ranks = book_ranks(int64_t(n) * C->max_pages);
+    const int ranks = book_ranks(int64_t(n) * ((C->max_pages + 127) / 128), 0);
     RR_CUDA(launch_clusters(rr_cache_fork_kernel, ranks, unsigned(ranks), kBookThreads, bits_bytes(C), stream, shape_of(C), b, parents,
                             children, n));
     return RR_OK;
@@ -832,9 +911,9 @@ extern "C" rr_status rr_cache_extend(const rr_cache* C, void* pages, void* book,
     const CacheShape c = shape_of(C);
     unsigned most;
     RR_TRY(copy_grid(dev, &most));
-    const int ranks = book_ranks(std::max<int64_t>(4 * int64_t(n), C->n_pages / 2));
+    const int ranks = book_ranks(n / 32, C->n_pages);
     RR_CUDA(launch_clusters(rr_cache_extend_kernel, ranks, unsigned(ranks), kBookThreads, bits_bytes(C), stream, c, b, seqs, starts, n));
-    const unsigned grid = unsigned(std::min<int64_t>(most, (int64_t(n) * c.runs + 7) / 8));
+    const unsigned grid = unsigned(std::min<int64_t>(most, int64_t(n) * ((c.runs + kRuns - 1) / kRuns)));
     RR_CUDA(launch_after(rr_cache_copy_rows_kernel, grid, 256, stream, c, b, static_cast<char*>(pages)));
     return RR_OK;
 }
@@ -883,7 +962,7 @@ extern "C" rr_status rr_cache_truncate(const rr_cache* C, void* book, const int3
     if (drop) RR_TRY(check_device(dev, drop, 4, "drop"));
     Book b;
     book_of(C, book, &b);
-    const int ranks = book_ranks(32 * int64_t(n));
+    const int ranks = book_ranks(n, 0);
     RR_CUDA(launch_clusters(rr_cache_truncate_kernel, ranks, unsigned(ranks), kBookThreads, bits_bytes(C), stream, shape_of(C), b, seqs,
                             drop, n));
     return RR_OK;
@@ -902,11 +981,14 @@ extern "C" rr_status rr_cache_compact(const rr_cache* C, void* pages, void* book
     const CacheShape c = shape_of(C);
     unsigned most;
     RR_TRY(copy_grid(dev, &most));
-    const int ranks = book_ranks(C->n_pages / 2);
+    const int ranks = book_ranks(0, C->n_pages);
     RR_CUDA(launch_clusters(rr_cache_compact_kernel, ranks, unsigned(ranks), kBookThreads, 0, stream, c, b));
+    constexpr int kSmem = kMoveStages * kMoveChunk;
+    static std::atomic<uint32_t> ready{0};
+    RR_CUDA(allow_smem(rr_cache_move_kernel, kSmem, dev, &ready));
     const int64_t chunks = (c.page_bytes + kMoveChunk - 1) / kMoveChunk * (C->n_pages / 2);
-    const unsigned grid = unsigned(std::max<int64_t>(1, std::min<int64_t>(most, std::max<int64_t>(chunks, (C->max_seqs + 7) / 8))));
-    RR_CUDA(launch_after(rr_cache_move_kernel, grid, 256, stream, c, b, static_cast<char*>(pages)));
+    const unsigned grid = unsigned(std::max<int64_t>(1, std::min<int64_t>(most / 8, std::max<int64_t>(chunks, (C->max_seqs + 6) / 7))));
+    RR_CUDA(launch_clusters(rr_cache_move_kernel, 1, grid, 256, kSmem, stream, c, b, static_cast<char*>(pages)));
     return RR_OK;
 }
 
@@ -923,7 +1005,7 @@ extern "C" rr_status rr_cache_check(const rr_cache* C, void* book, cudaStream_t 
     if (!state) return RR_OK;
     RR_CUDA(cudaMemsetAsync(book, 0, 8, stream));
     RR_CUDA(cudaStreamSynchronize(stream));
-    if (state & kBadWait) return rr_fail(RR_ECUDA, "a wait within rr_attend ran out");
+    if (state & kBadWait) return rr_fail(RR_ECUDA, "a wait of a call on the cache ran out");
     return rr_fail(RR_EINVAL, "a call on the cache was not done:%s%s%s%s%s", state & kBadRange ? " a sequence, length or count is out of range;" : "",
                    state & kBadTwice ? " a sequence is listed twice;" : "", state & kBadPool ? " no room for the new tokens;" : "",
                    state & kBadChild ? " a child holds tokens;" : "", state & kBadTable ? " the table has a page out of range;" : "");
