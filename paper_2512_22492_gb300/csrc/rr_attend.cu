@@ -91,8 +91,10 @@ struct Kind {
     static constexpr bool kKeep = NG == 2;
     static constexpr int kSums = kKeep ? 0 : kRows * D * 4;
     static constexpr int kFixed = 2 * kQ + kParts * kP + kSums;
-    static constexpr int kColumns = (2 + MT) * kRows <= 64 ? 64 : (2 + MT) * kRows <= 128 ? 128 : (2 + MT) * kRows <= 256 ? 256 : 512;
-    static_assert((2 + MT) * kRows <= 512, "TMEM");
+    // TMEM: S^T twice, then D^T, whose columns are the rows' first parts, then their second ones.
+    static constexpr int kD = kParts * kRows, kUsed = 2 * kRows + MT * kD;
+    static constexpr int kColumns = kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : 256;
+    static_assert(kUsed <= 256, "TMEM");
 };
 
 // Two floats as one word of 16-bit elements, the first in the low half.
@@ -706,7 +708,8 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
         Stage st;
         int q_item = 0, v_item = 0, q_left = 0, v_left = 0, v_unit = 0, v_length = 0;
         uint32_t q_instr = 0, v_instr = 0;
-        const auto columns = [&](const Tile& t) { return uniform(min((t.count * a.group - t.tile * K::kRows + 15) / 16 * 16, N)); };
+        const auto rows_of = [&](const Tile& t) { return min(t.count * a.group - t.tile * K::kRows, N); };
+        const auto columns = [&](const Tile& t) { return uniform((rows_of(t) + 15) / 16 * 16); };
         const uint32_t first_tmem = uniform(tmem);
         const int units = int(n);
         for (int i = 0; i <= units; ++i) {
@@ -743,7 +746,9 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                     v_left = uniform(item.n);
                     v_unit = uniform(item.first);
                     v_length = uniform(item.t.length);
-                    v_instr = instruction<T>(columns(item.t), true, true);
+                    // (One product for both parts of the weights, side by side: a product takes about 75
+                    // cycles and one more for each column or so.)
+                    v_instr = instruction<T>(K::kParts == 1 ? columns(item.t) : 2 * uniform((rows_of(item.t) + 7) / 8 * 8), true, true);
                     ++v_item;
                 }
                 if (!__all_sync(~0u, wait(sh.full[st.at], st.turn))) break;
@@ -757,12 +762,10 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
 #pragma unroll
                     for (int m = 0; m < MT; ++m)
 #pragma unroll
-                        for (int part = K::kParts - 1; part >= 0; --part)
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (j < steps)
-                                    product(first_tmem + (2 + m) * N, dv + m * (a.atom_bytes / 8) + j * (a.eight_bytes / 8),
-                                            dp + part * (K::kP / 16) + j * 16, v_instr, add || j > 0 || part < K::kParts - 1, mine);
+                        for (int j = 0; j < 8; ++j)
+                            if (j < steps)
+                                product(first_tmem + 2 * N + m * K::kD, dv + m * (a.atom_bytes / 8) + j * (a.eight_bytes / 8), dp + j * 16, v_instr,
+                                        add || j > 0, mine);
                     if (mine) {
                         products_arrive(smem_of(&sh.empty[st.at]));
                         products_arrive(smem_of(&sh.sums));
@@ -860,8 +863,17 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 for (int j = 0; j < GO; ++j) {
                     if (sum_group(j) >= groups) continue;
                     F2 x[4];
-                    tmem_load(tmem + lanes + (2 + half) * N + 8 * sum_group(j), x);
-                    tmem_loaded();
+                    const uint32_t columns = tmem + lanes + 2 * N + half * K::kD + 8 * sum_group(j);
+                    tmem_load(columns, x);
+                    if (K::kParts == 2) {
+                        F2 y[4];
+                        tmem_load(columns + 8 * groups, y);
+                        tmem_loaded();
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = add2(x[e], y[e]);
+                    } else {
+                        tmem_loaded();
+                    }
                     float* const at = sums_at + 8 * sum_group(j) * K::D + d;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -993,7 +1005,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                     if (group_of(j) >= groups) continue;
 #pragma unroll
                     for (int x = 0; x < K::kParts; ++x)
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_at + x * K::kP + group_of(j) * 2048 + key * 16),
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(p_at + (x * groups + group_of(j)) * 2048 + key * 16),
                                      "r"(p[j][x][0]), "r"(p[j][x][1]), "r"(p[j][x][2]), "r"(p[j][x][3])
                                      : "memory");
                 }
