@@ -621,18 +621,23 @@ constexpr int kAcceptRanks = 8;
 constexpr int kAcceptThreads = 1024;      // at most
 constexpr int kMaxVocab = 1 << 20;
 
-// A probability in whole numbers of 2^-42, ties to even; NaN counts as 0.  y = x 2^42 is
-// exact in float32; under 2^23 adding 2^23 rounds it to a whole number in the low bits, from there on it
-// is one.  (A conversion to 64 bits runs at a fraction of the rate: 64 sequences of 151936 entries
-// took 52 us with it, @@ACCEPT@@.)
-__device__ __forceinline__ uint64_t units(float x) {
-    const float y = fminf(fmaxf(x, 0.0f), 1.0f) * 4398046511104.0f;
-    const uint32_t bits = __float_as_uint(y), mantissa = (bits & 0x7FFFFFu) | 0x800000u, shift = (bits >> 23) - 150;
-    const uint32_t small = __float_as_uint(y + 8388608.0f) - 0x4B000000u;
-    const bool whole = y >= 8388608.0f;
-    const uint32_t lo = whole ? mantissa << (shift & 31) : small, hi = whole ? __funnelshift_lc(mantissa, 0, shift) : 0;
-    return uint64_t(hi) << 32 | lo;
-}
+// A probability x in whole numbers of 2^-42, ties to even; NaN counts as 0.  In two parts, in
+// float32: h = floor(x 2^22), by adding 2^23 and cutting off, and the rest x 2^42 - h 2^20, which is exact
+// and is rounded to a whole number by adding 2^23.  Both stand in the low bits of a float from
+// kMagic on.  (Conversions to 64-bit integers run at a fraction of the rate: 64 sequences of 151936
+// entries took 52 us with them; mantissas shifted as integers 24 us; so @@ACCEPT@@.)
+constexpr uint32_t kMagic = 0x4B000000u;      // 2^23
+struct Units {
+    uint32_t high, low;       // kMagic + h, kMagic + the rest
+    __device__ __forceinline__ Units(float x) {
+        x = __saturatef(x);
+        const float h = __fadd_rz(x * 4194304.0f, 8388608.0f);
+        const float rest = fmaf(h - 8388608.0f, -1048576.0f, x * 4398046511104.0f);
+        high = __float_as_uint(h);
+        low = __float_as_uint(rest + 8388608.0f);
+    }
+    __device__ __forceinline__ uint64_t value() const { return (uint64_t(high - kMagic) << 20) + (low - kMagic); }
+};
 
 struct AcceptArgs {
     const float *p, *q;
@@ -662,23 +667,19 @@ struct Draw {
 #pragma unroll
         for (int e = 0; e < 4; ++e) to[e] = index<ORDER>(k, lane, e) < end ? __ldg(x + index<ORDER>(k, lane, e)) : 0.0f;
     }
-    // The lane's units of N times 128 entries.
+    // Of N times 128 entries from k on, the lane's.
     template <bool ORDER, int N>
-    __device__ __forceinline__ void entries(int k, int lane, int end, uint64_t (*n)[4]) const {
-        float a[N][4], b[N][4];
+    __device__ __forceinline__ void values(int k, int lane, int end, float (*x)[4]) const {
+        float b[N][4];
 #pragma unroll
-        for (int h = 0; h < N; ++h) load<ORDER>(p, k + 128 * h, lane, end, a[h]);
+        for (int h = 0; h < N; ++h) load<ORDER>(p, k + 128 * h, lane, end, x[h]);
         if (q) {
 #pragma unroll
             for (int h = 0; h < N; ++h) load<ORDER>(q, k + 128 * h, lane, end, b[h]);
-        }
 #pragma unroll
-        for (int h = 0; h < N; ++h) {
+            for (int h = 0; h < N; ++h)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float x = q ? a[h][e] - b[h][e] : a[h][e];
-                n[h][e] = units(index<ORDER>(k + 128 * h, lane, e) == without ? 0.0f : x);
-            }
+                for (int e = 0; e < 4; ++e) x[h][e] -= b[h][e];
         }
     }
 };
@@ -726,11 +727,22 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) rr_accept_kernel(const __gr
         uint64_t mine = 0;
 #pragma unroll 1
         for (int k = lo; k < hi; k += 512) {
-            uint64_t x[4][4];
-            d.entries<false, 4>(k, lane, hi, x);
+            float x[4][4];
+            d.values<false, 4>(k, lane, hi, x);
+            // (16 of them stay within 32 bits.)
+            uint32_t high = 0, low = 0;
 #pragma unroll
-            for (int h = 0; h < 4; ++h) mine += (x[h][0] + x[h][1]) + (x[h][2] + x[h][3]);
+            for (int h = 0; h < 4; ++h) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const Units u(x[h][e]);
+                    high += u.high;
+                    low += u.low;
+                }
+            }
+            mine += (uint64_t(high - 16 * kMagic) << 20) + (low - 16 * kMagic);
         }
+        if (lane == 0 && d.without >= lo && d.without < hi) mine -= Units(d.p[d.without]).value();
 #pragma unroll
         for (int m = 16; m; m >>= 1) mine += __shfl_xor_sync(~0u, mine, m);
         if (lane < kAcceptRanks) {
@@ -778,9 +790,12 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) rr_accept_kernel(const __gr
     if (total == 0 || t < before || t - before >= own) return;
     uint64_t left = t - before;
     for (int k = lo; k < hi; k += 128) {
-        uint64_t x[1][4];
-        d.entries<true, 1>(k, lane, hi, x);
-        const uint64_t mine = x[0][0] + x[0][1] + x[0][2] + x[0][3];
+        float y[1][4];
+        uint64_t x[4];
+        d.values<true, 1>(k, lane, hi, y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = k + 4 * lane + e == d.without ? 0 : Units(y[0][e]).value();
+        const uint64_t mine = x[0] + x[1] + x[2] + x[3];
         uint64_t up = mine;
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) {
@@ -788,11 +803,11 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) rr_accept_kernel(const __gr
             if (lane >= m) up += o;
         }
         if (up > left && up - mine <= left) {
-            uint64_t y = left - (up - mine);
+            uint64_t rest = left - (up - mine);
             int e = 0;
 #pragma unroll
             for (int h = 0; h < 3; ++h)
-                if (e == h && y >= x[0][h]) y -= x[0][h], ++e;
+                if (e == h && rest >= x[h]) rest -= x[h], ++e;
             a.tokens[row] = k + 4 * lane + e;
         }
         const uint64_t last = __shfl_sync(~0u, up, 31);
