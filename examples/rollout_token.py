@@ -5,10 +5,11 @@ into buckets, pulled and unpacked into the rollout's tensors
 (``rr_pack``, ``rr_unpack_verify``).  The rollout then quantises its dense
 matrices to 4 bits (``rr_quantize``) and runs one token step for a batch of
 one-token prompts: fused QKV, output projection and logits with ``rr_matvec``,
+attention over a paged cache (``rr_cache_extend``, ``rr_cache_append``, ``rr_attend``),
 the experts with ``rr_moe`` on the stacked tensors as the sync left them (or, with
-``--experts 4bit``, quantised as well).  With one position, attention is the
-identity on the values and the rotation is by zero, so the products are the
-whole step but for the norms, which torch does.
+``--experts 4bit``, quantised as well), and the next token with ``rr_accept``.  At
+the first position the rotation is by zero, so these are the whole step but for the
+norms and the softmax, which torch does.
 
     python examples/rollout_token.py [--tokens 4] [--experts 16bit|4bit]
 """
@@ -85,18 +86,27 @@ class Rollout:
                                 tensors[at + "post_attention_layernorm"]))
         self.lm_head = packed("lm_head", shape.vocab, h)
         self.workspace = rr.MoeWorkspace(self.layers[0][2], max_tokens)
+        # A page of 16 tokens for each prompt.
+        self.cache = rr.Cache(shape.layers, shape.n_kv, shape.head_dim, max_tokens, max_tokens, 1)
+        self.attention = rr.AttendWorkspace(self.cache, shape.n_q)
+        self.seqs = torch.arange(max_tokens, dtype=torch.int32, device="cuda")
 
     def step(self, prompt):
         """Logits [tokens, vocab] (float32) for one-token prompts."""
         s, n = self.shape, prompt.numel()
         new = lambda *shape, dtype=torch.bfloat16: torch.empty(*shape, dtype=dtype, device="cuda")
+        # The prompts of before are done with; these take their pages.
+        seqs = self.seqs[:n]
+        rr.rr_cache_truncate(self.cache, self.seqs)
+        rr.rr_cache_extend(self.cache, seqs)
         x = self.t["embed_tokens"].view(s.vocab, s.hidden)[prompt]
-        for qkv_proj, o_proj, moe, norm1, norm2 in self.layers:
+        for i, (qkv_proj, o_proj, moe, norm1, norm2) in enumerate(self.layers):
             qkv, attn, y = new(n, self.q + 2 * self.kv), new(n, s.hidden), new(n, s.hidden)
+            heads = new(n, self.q)
             rr.rr_matvec(qkv_proj, norm(x, norm1), qkv)
-            # One position: every head's output is its group's value.
-            v = qkv[:, self.q + self.kv:].view(n, s.n_kv, 1, s.head_dim)
-            heads = v.expand(n, s.n_kv, s.n_q // s.n_kv, s.head_dim).reshape(n, self.q)
+            q, k, v = qkv.split((self.q, self.kv, self.kv), 1)
+            rr.rr_cache_append(self.cache, i, k, v, seqs)
+            rr.rr_attend(self.cache, i, q, heads, seqs, self.attention)
             rr.rr_matvec(o_proj, heads, attn)
             x = x + attn
             rr.rr_moe(moe, norm(x, norm2), y, self.workspace)
@@ -104,6 +114,14 @@ class Rollout:
         logits = new(n, s.vocab, dtype=torch.float32)
         rr.rr_matvec(self.lm_head, norm(x, self.t["norm"]), logits)
         return logits
+
+
+def sample(logits, numbers):
+    """A token for each row of logits, by its number of [0, 1)."""
+    p = torch.softmax(logits, -1)
+    tokens = torch.empty(len(p), dtype=torch.int32, device="cuda")
+    rr.rr_accept(p, None, None, numbers, torch.empty_like(tokens), tokens)
+    return tokens
 
 
 def main():
@@ -117,7 +135,10 @@ def main():
     logits = rollout.step(prompt)
     for layer in rollout.layers:
         rr.rr_moe_check(layer[2], rollout.workspace)
-    print("prompt", prompt.tolist(), "next", logits.argmax(-1).tolist())
+    rr.rr_cache_check(rollout.cache)
+    numbers = torch.rand(args.tokens, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    print("prompt", prompt.tolist(), "likeliest", logits.argmax(-1).tolist(), "drawn",
+          sample(logits, numbers).tolist())
 
 
 if __name__ == "__main__":

@@ -719,7 +719,10 @@ rr_status rr_moe_check(const rr_moe_layer* layer, int32_t max_tokens, void* work
  * what they hold.  A call that finds a number out of range, a sequence listed twice or
  * the pool without room leaves the cache as it was and marks it; later calls then leave
  * all as it is, until rr_cache_check has reported the mark.  rr_cache_append and rr_attend
- * leave out what does not fit, and mark the cache likewise.
+ * leave out what does not fit (a row whose pages are out of range holds anything), and mark the
+ * cache likewise.  rr_attend and rr_cache_compact wait within a block, each time for two
+ * seconds or so at most; a wait that runs out marks the cache, too (RR_ECUDA): outputs and pages
+ * are then incomplete, and rr_attend's workspace has to be filled with zeros again.
  * ------------------------------------------------------------------------- */
 
 /* The cache's shape.
@@ -778,7 +781,7 @@ rr_status rr_cache_truncate(const rr_cache* cache, void* book, const int32_t* se
 rr_status rr_cache_compact(const rr_cache* cache, void* pages, void* book, cudaStream_t stream);
 
 /* Waits for `stream`, then reports (and clears) the cache's mark: RR_EINVAL if a call left
- * something undone, else RR_OK. */
+ * something undone, RR_ECUDA if a wait ran out, else RR_OK. */
 rr_status rr_cache_check(const rr_cache* cache, void* book, cudaStream_t stream);
 
 /* Attention of new tokens, whose keys and values are in the cache.  Rows as for
