@@ -73,7 +73,7 @@ struct Kind {
     static constexpr int kRows = 8 * NG;
     static constexpr int D = 128 * MT;
     // Sets of four softmax warps; copies, products and queries have a warp each.  (96 sequences of
-    // five tokens of 8 heads each: @@SETS@@)
+    // five tokens of 8 heads each: 2 sets 327 us, 3 314, 4 338)
     static constexpr int kSets = NG == 8 ? 3 : 2;
     static constexpr int kSoft = 128 * kSets, kThreads = kSoft + 128;
     static constexpr int kKeys = kSoft / 32, kValues = kKeys + 1, kProducts = kKeys + 2, kQueries = kKeys + 3;
@@ -85,9 +85,11 @@ struct Kind {
     static constexpr float kLift = std::is_same<T, BF16>::value ? 0.0f : 7.0f;
     static constexpr int kQ = MT * NG * 2048;           // bytes of a tile's queries
     static constexpr int kP = NG * 2048;                // of one part of the weights
+    // What a tile costs beside its units, in halves of one (its first reference, its results).
+    static constexpr int kOpen = NG == 2 ? 1 : 4;
     // A tile's sums: in registers, or, of many rows, in shared memory.  (With them in registers
     // those of 64 rows spill, to an L1 that shared memory has left next to nothing of:
-    // 96 sequences of five tokens of 8 heads each @@SPILL@@.)
+    // 96 sequences of five tokens of 8 heads each 372 us, so 322.)
     static constexpr bool kKeep = NG == 2;
     static constexpr int kSums = kKeep ? 0 : kRows * D * 4;
     static constexpr int kFixed = 2 * kQ + kParts * kP + kSums;
@@ -118,7 +120,7 @@ struct Tile {
 // A tile's part in a block's run.
 struct Item {
     Tile t;
-    int first, n;                  // units
+    int first, n;                  // units; n 0: the block's run has ended
     int64_t begin;                 // of the tile in the call's line
 };
 
@@ -143,29 +145,54 @@ template <class K>
 __device__ __forceinline__ int tiles_of(const AttendArgs& a, int count) {
     return int((int64_t(count) * a.group + K::kRows - 1) / K::kRows);
 }
+// A tile's length in the call's line: two places a unit, the k-th unit's (from 0) being kOpen + 2 k
+// from the tile's begin.
+template <class K>
+__device__ __forceinline__ int64_t places_of(int units) { return K::kOpen + 2 * int64_t(units); }
+template <class K>
+__device__ __forceinline__ int64_t place_of(int unit) { return K::kOpen + 2 * int64_t(unit); }
+// The first of a tile's units from a place on.
+template <class K>
+__device__ __forceinline__ int unit_from(int64_t place, int units) {
+    return place <= K::kOpen ? 0 : int(min((place - K::kOpen + 1) / 2, int64_t(units)));
+}
 template <class K>
 __device__ __forceinline__ int64_t work_of(const AttendArgs& a, int length, int count) {
-    return int64_t(a.c.n_kv) * tiles_of<K>(a, count) * units_of(length);
+    return int64_t(a.c.n_kv) * tiles_of<K>(a, count) * places_of<K>(units_of(length));
 }
 
-// The blocks' runs: block b has units [T b / N, T (b + 1) / N).
+// The blocks' runs: block b has the units at places T b / N to T (b + 1) / N - 1.
 struct Line {
     int64_t total;
     int blocks;
     __device__ __forceinline__ int64_t begin(int b) const { return total * b / blocks; }
-    // Whose run holds unit u.
+    // Whose run holds a place.
     __device__ __forceinline__ int owner(int64_t u) const { return int(((u + 1) * blocks - 1) / total); }
 };
 
-// Walks the listed sequences' tiles from a place in the call's line on; 32 sequences'
-// numbers at a time, one a lane.
+// Walks the tiles of a block's run, and the units of each that belong to it; 32
+// sequences' numbers at a time, one a lane.
 template <class K>
 struct Walk {
     const AttendArgs& a;
     int seq, batch;                      // the current sequence, the first one of the loaded ones
     int slot_, length_, first_, count_;  // lane l: of sequence batch + l
+    int64_t at, begin, end;              // where the tile begins in the line; the run
     Tile t;
-    __device__ __forceinline__ Walk(const AttendArgs& args, int i) : a(args), seq(i), batch(i) { load(); }
+    int first, n;                        // the tile's units in the run
+    // From the run's first place on, `inside` places from the begin of sequence i.
+    __device__ __forceinline__ Walk(const AttendArgs& args, int i, int64_t inside, int64_t begin_, int64_t end_)
+        : a(args), seq(i), batch(i), begin(begin_), end(end_) {
+        load();
+        enter();
+        const int64_t each = places_of<K>(t.units), tile = inside / each;
+        const int tiles = tiles_of<K>(a, t.count);
+        at = begin - (inside - tile * each);
+        t.head = int(tile / tiles);
+        t.tile = int(tile % tiles);
+        range();
+        if (n <= 0) next();
+    }
     __device__ __forceinline__ void load() {
         const int i = batch + int(threadIdx.x & 31);
         slot_ = length_ = first_ = count_ = 0;
@@ -180,19 +207,33 @@ struct Walk {
         t.units = units_of(t.length);
         t.head = t.tile = 0;
     }
-    // The next tile; there is one.  The tiles of a key head follow one another.
+    __device__ __forceinline__ void range() {
+        first = at < begin ? unit_from<K>(begin - at, t.units) : 0;
+        n = unit_from<K>(end - at, t.units) - first;
+    }
+    __device__ __forceinline__ bool ended() const { return n <= 0; }
+    // The next tile that has units in the run; n is 0 if there is none.  The tiles of a key head follow
+    // one another.
     __device__ __forceinline__ void next() {
-        if (++t.tile < tiles_of<K>(a, t.count)) return;
-        t.tile = 0;
-        if (++t.head < a.c.n_kv) return;
         do {
-            if (++seq >= a.n) return;
-            if (seq == batch + 32) {
-                batch = seq;
-                load();
+            at += places_of<K>(t.units);
+            n = 0;
+            if (at >= end) return;
+            if (++t.tile < tiles_of<K>(a, t.count)) {
+            } else if (++t.head < a.c.n_kv) {
+                t.tile = 0;
+            } else {
+                do {
+                    if (++seq >= a.n) return;
+                    if (seq == batch + 32) {
+                        batch = seq;
+                        load();
+                    }
+                    enter();
+                } while (t.count == 0);
             }
-            enter();
-        } while (t.count == 0);
+            range();
+        } while (n <= 0);
     }
 };
 
@@ -543,9 +584,10 @@ __device__ __forceinline__ float over_lanes(const F2* pairs, F f) {
 }
 __device__ __forceinline__ int row_of_lane() { return (threadIdx.x >> 4 & 1) * 4 + (threadIdx.x >> 3 & 1) * 2 + (threadIdx.x >> 2 & 1); }
 
-// A unit's place in the ring's order, K0 K1 V0 K2 V1 ..., of n units.
+// A unit's place in the ring's order, K0 K1 V0 K2 V1 ...  (The place of the keys behind the
+// last ones stays empty.)
 __device__ __forceinline__ int keys_at(int i) { return i ? 2 * i - 1 : 0; }
-__device__ __forceinline__ int values_at(int i, int n) { return i + 1 < n ? 2 * i + 2 : 2 * i + 1; }
+__device__ __forceinline__ int values_at(int i) { return 2 * i + 2; }
 
 // A place in the ring, and the parity of its turn.
 struct Stage {
@@ -598,7 +640,8 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
         for (int i = threadIdx.x; i < a.n; i += K::kThreads) mine += kept = work(i);
         int64_t at = scan(mine, &line.total);
         if (line.total == 0) return;
-        line.blocks = int(min(int64_t(gridDim.x), line.total));
+        // (So many places that each run has a unit.)
+        line.blocks = int(max(min(int64_t(gridDim.x), line.total / (2 + K::kOpen)), int64_t(1)));
         if (int(blockIdx.x) >= line.blocks) return;
         begin = line.begin(blockIdx.x), end = line.begin(blockIdx.x + 1);
         int64_t before = 0;
@@ -643,24 +686,13 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
     __syncthreads();
     tmem_after();
     const uint32_t tmem = sh.tmem;
-    const int64_t n = end - begin;
     const auto wait = [&](uint64_t& bar, int parity) { return bar_wait(smem_of(&bar), parity, &sh.quit, a.control); };
-
-    // The walk's first tile and unit.
-    const auto enter = [&](Walk<K>& walk) {
-        walk.enter();
-        const int64_t at = sh.start, tile = at / walk.t.units;
-        const int tiles = tiles_of<K>(a, walk.t.count);
-        walk.t.head = int(tile / tiles);
-        walk.t.tile = int(tile % tiles);
-        return int(at - tile * walk.t.units);
-    };
 
     if (w == K::kKeys || w == K::kValues) {
         // Copies: one warp the keys', one the values'.  A lane asks for one page's.
         const bool values = w == K::kValues;
-        Walk<K> walk(a, sh.seq);
-        int unit = enter(walk);
+        Walk<K> walk(a, sh.seq, sh.start, begin, end);
+        int unit = walk.first, left = walk.n;
         const int tokens = a.c.page, pages = kUnit >> a.c.shift, eights = tokens / 8;
         const auto fetch = [&] {
             const int key = unit * kUnit + lane * tokens;
@@ -670,20 +702,19 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             atomicOr(&a.control[kLate], kBadTable);
             return -1;
         };
-        const int units = int(n);
         int id = fetch(), i = 0;
-        for (; i < units; ++i) {
+        bool ok = true;
+        for (; !walk.ended(); ++i) {
             const int here = id, head = (values ? a.c.n_kv : 0) + walk.t.head;
-            if (i + 1 < units) {
-                // (The next unit's pages, ahead of the wait.)
-                if (++unit == walk.t.units) {
-                    unit = 0;
-                    walk.next();
-                }
-                id = fetch();
+            // (The next unit's pages, ahead of the wait.)
+            ++unit;
+            if (--left == 0) {
+                walk.next();
+                unit = walk.first, left = walk.n;
             }
-            const int k = values ? values_at(i, units) : keys_at(i), at = k % a.stages, turn = k / a.stages & 1;
-            if (!__all_sync(~0u, wait(sh.empty[at], turn ^ 1))) break;
+            if (!walk.ended()) id = fetch();
+            const int k = values ? values_at(i) : keys_at(i), at = k % a.stages, turn = k / a.stages & 1;
+            if (!(ok = __all_sync(~0u, wait(sh.empty[at], turn ^ 1)))) break;
             const uint32_t bar = smem_of(&sh.full[at]);
             const int there = __popc(__ballot_sync(~0u, here >= 0));
             if (elected()) bar_expect(bar, uint32_t(there * a.atoms * tokens * 128));
@@ -694,10 +725,10 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                     tma_load(to + y * a.atom_bytes, &map, a.copy_atoms > 1 ? 0 : 64 * y, 0, head * eights, here, bar);
             }
         }
-        if (i < units) {
+        if (!ok) {
             // What is on its way has to land before the block ends.
             for (int back = max(i - a.stages, 0); back < i; ++back) {
-                const int k = values ? values_at(back, units) : keys_at(back);
+                const int k = values ? values_at(back) : keys_at(back);
                 for (int x = 0; x < 1 << 20 && !bar_try(smem_of(&sh.full[k % a.stages]), k / a.stages & 1); ++x) {}
             }
         }
@@ -711,15 +742,16 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
         const auto rows_of = [&](const Tile& t) { return min(t.count * a.group - t.tile * K::kRows, N); };
         const auto columns = [&](const Tile& t) { return uniform((rows_of(t) + 15) / 16 * 16); };
         const uint32_t first_tmem = uniform(tmem);
-        const int units = int(n);
-        for (int i = 0; i <= units; ++i) {
-            if (i < units) {
-                const int slot = q_item & 1;
-                if (q_left == 0) {
-                    if (!__all_sync(~0u, wait(sh.q_full[slot], q_item >> 1 & 1))) break;
-                    q_left = uniform(sh.items[slot].n);
-                    q_instr = instruction<T>(columns(sh.items[slot].t), false, false);
-                }
+        bool more = true;
+        for (int i = 0, done = 0;;) {
+            const int slot = q_item & 1;
+            if (more && q_left == 0) {
+                if (!__all_sync(~0u, wait(sh.q_full[slot], q_item >> 1 & 1))) break;
+                q_left = uniform(sh.items[slot].n);
+                q_instr = instruction<T>(columns(sh.items[slot].t), false, false);
+                if (!(more = q_left > 0)) st.next(a.stages);
+            }
+            if (more) {
                 if (!__all_sync(~0u, wait(sh.full[st.at], st.turn))) break;
                 tmem_after();
                 {
@@ -739,8 +771,11 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 }
                 st.next(a.stages);
                 if (--q_left == 0) ++q_item;
+                ++i;
             }
-            if (i > 0) {
+            // (Of the unit before; of the last one, if there is none left.)
+            if (done == i) break;
+            if (done + 1 < i || !more) {
                 if (v_left == 0) {
                     const Item& item = sh.items[v_item & 1];
                     v_left = uniform(item.n);
@@ -752,10 +787,10 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                     ++v_item;
                 }
                 if (!__all_sync(~0u, wait(sh.full[st.at], st.turn))) break;
-                if (!__all_sync(~0u, wait(sh.weights, (i - 1) & 1))) break;
+                if (!__all_sync(~0u, wait(sh.weights, done & 1))) break;
                 tmem_after();
                 const int steps = max((min(v_length - v_unit * kUnit, kUnit) + 15) / 16, 1);
-                const bool add = !uniform(sh.fresh[(i - 1) & 1]);
+                const bool add = !uniform(sh.fresh[done & 1]);
                 {
                     const uint64_t dv = descriptor(ring + st.at * stage_bytes, a.atom_bytes, a.eight_bytes, 2), dp = descriptor(p_at, 128, 2048, 0);
                     const uint32_t mine = elected();
@@ -775,20 +810,19 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 st.next(a.stages);
                 ++v_unit;
                 --v_left;
+                ++done;
             }
         }
         __syncwarp();
     } else if (w == K::kQueries) {
         // Queries, and what the others need to know of a tile.
-        Walk<K> walk(a, sh.seq);
-        int unit = enter(walk);
-        int64_t at = begin;
+        Walk<K> walk(a, sh.seq, sh.start, begin, end);
         const int chunks = (a.c.dim + 15) / 16 * 2;
-        for (int item = 0; at < end; ++item) {
+        for (int item = 0;; ++item) {
             const int slot = item & 1;
             if (!__all_sync(~0u, wait(sh.q_free[slot], (item >> 1 & 1) ^ 1))) break;
             const Tile& t = walk.t;
-            const int left = min(t.count * a.group - t.tile * K::kRows, K::kRows), rows = (left + 15) / 16 * 16;
+            const int left = walk.ended() ? 0 : min(t.count * a.group - t.tile * K::kRows, K::kRows), rows = (left + 15) / 16 * 16;
             const uint32_t to = q_at + slot * K::kQ;
             for (int base = 0; base < rows * chunks; base += 8 * 32) {
                 uint4 x[8];
@@ -820,20 +854,18 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 sh.seen[slot][r] = r < left ? t.length - t.count + 1 + token : 0;
                 sh.out[slot][r] = (t.first + token) * a.ldo + int64_t(t.head * a.group + row - token * a.group) * a.c.dim;
             }
-            const int units = int(min(int64_t(t.units - unit), end - at));
             if (lane == 0) {
                 Item& it = sh.items[slot];
                 it.t = t;
-                it.first = unit;
-                it.n = units;
-                it.begin = at - unit;
+                it.first = walk.first;
+                it.n = max(walk.n, 0);
+                it.begin = walk.at;
             }
             to_async();
             __syncwarp();
             if (lane == 0) bar_arrive(smem_of(&sh.q_full[slot]));
-            at += units;
-            unit = 0;
-            if (at < end) walk.next();
+            if (walk.ended()) break;
+            walk.next();
         }
     } else {
         // Softmax and sums.  Lane l of warp w has key, or element, 32 (w % 4) + l; the sets of four
@@ -845,20 +877,25 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
         const auto group_of = [&](int j) { return set + kSets * j; };
         const F2 scale2 = both(a.scale, a.scale);
         const auto sum_group = [&](int j) { return set / MT + kSumSets * j; };
-        const int all = int(n);
         int i = 0;
         bool over = false;
-        for (int item = 0; i < all && !over; ++item) {
+        for (int item = 0; !over; ++item) {
             const int slot = item & 1;
             bool ok = __all_sync(~0u, wait(sh.q_full[slot], (item >> 1 & 1)));
+            // (The first scores are over any reference: it is set then.)
+            if (int(threadIdx.x) < N) sh.bias[threadIdx.x] = kNothing;
+            if (soft_any<K::kSoft>(!ok)) break;
             const Item it = sh.items[slot];
-            const int left = uniform(ok ? min(it.t.count * a.group - it.t.tile * K::kRows, K::kRows) : 0), groups = (left + 7) / 8;
-            const int units = uniform(ok ? it.n : 1), first_seen = uniform(seen(it.t, a.group, it.t.tile * K::kRows));
+            const int units = uniform(it.n);
+            if (units == 0) break;
+            const int left = uniform(min(it.t.count * a.group - it.t.tile * K::kRows, K::kRows)), groups = (left + 7) / 8;
+            const int first_seen = uniform(seen(it.t, a.group, it.t.tile * K::kRows));
             const int first_key = uniform(it.first * kUnit);
             F2 o[K::kKeep ? GO : 1][4], sum[GS][4];
             bool begun = false;            // whether o has anything
+            bool odd = false;              // whether a result is not finite
             // Adds TMEM's sums to o, and multiplies by factor[row] where that is given.
-            const auto add_sums = [&](const float* factor) {
+            const auto add_sums = [&](const float* factor, bool last) {
 #pragma unroll
                 for (int j = 0; j < GO; ++j) {
                     if (sum_group(j) >= groups) continue;
@@ -878,7 +915,16 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         if (begun) x[e] = add2(x[e], K::kKeep ? o[K::kKeep ? j : 0][e] : both(at[2 * e * K::D], at[(2 * e + 1) * K::D]));
-                        if (factor) x[e] = mul2(x[e], reinterpret_cast<const F2*>(factor + 8 * sum_group(j))[e]);
+                        if (factor) {
+                            const F2 f = reinterpret_cast<const F2*>(factor + 8 * sum_group(j))[e];
+                            x[e] = mul2(x[e], f);
+                            // (Rows whose sum is NaN are all NaN in any case.)
+                            const int r = 8 * sum_group(j) + 2 * e;
+                            if (last) {
+                                odd |= r < left && low(f) == low(f) && !(fabsf(low(x[e])) < kInf);
+                                odd |= r + 1 < left && high(f) == high(f) && !(fabsf(high(x[e])) < kInf);
+                            }
+                        }
                         if (K::kKeep) o[K::kKeep ? j : 0][e] = x[e];
                         else at[2 * e * K::D] = low(x[e]), at[(2 * e + 1) * K::D] = high(x[e]);
                     }
@@ -889,9 +935,6 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             for (int j = 0; j < GS; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[j][e] = 0;
-            // (The first scores are over any reference: it is set then.)
-            if (int(threadIdx.x) < N) sh.bias[threadIdx.x] = kNothing;
-            soft_sync<K::kSoft>();
             for (int u = 0; u < units; ++u, ++i) {
                 const int key0 = first_key + u * kUnit;
                 ok &= __all_sync(~0u, wait(sh.scores[i & 1], i >> 1 & 1));
@@ -997,7 +1040,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 const bool fresh = moved || u % kGather == 0;
                 if (fresh && u > 0) {
                     __syncwarp();
-                    add_sums(moved ? sh.factor : nullptr);
+                    add_sums(moved ? sh.factor : nullptr, false);
                 }
                 if (threadIdx.x == 0) sh.fresh[i & 1] = fresh;
 #pragma unroll
@@ -1012,7 +1055,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 const int valid = min(it.t.length - key0, kUnit);
                 if (valid < kUnit) {
                     // Behind the sequence's end the page holds anything: values there become 0.
-                    const int k = values_at(i, all);
+                    const int k = values_at(i);
                     const int stage = k % a.stages;
                     wait(sh.full[stage], k / a.stages & 1);
                     const int rows = max((valid + 15) / 16 * 16, 16) - valid;
@@ -1051,39 +1094,43 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             }
             soft_sync<K::kSoft>();
             // (Each sum times 1 / the row's.)
-            add_sums(sh.inverse);
-            bool odd = false;
-            const auto result = [&](int j, int e) {
-                if (K::kKeep) return e & 1 ? high(o[K::kKeep ? j : 0][e / 2]) : low(o[K::kKeep ? j : 0][e / 2]);
-                return sums_at[(8 * sum_group(j) + e) * K::D + d];
-            };
-#pragma unroll
-            for (int j = 0; j < GO; ++j) {
-                if (sum_group(j) >= groups) continue;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int r = 8 * sum_group(j) + e;
-                    // (Rows whose sum is NaN are all NaN in any case.)
-                    odd |= r < left && sh.inverse[r] == sh.inverse[r] && !(fabsf(result(j, e)) < kInf);
-                }
-            }
+            add_sums(sh.inverse, true);
             if (soft_any<K::kSoft>(odd && d < a.c.dim)) {
                 for (int r = w; r < left; r += K::kSoft / 32) carefully<K>(a, it.t, r, it.first * kUnit, (it.first + it.n) * kUnit, piece);
-            } else {
+            } else if (K::kKeep) {
 #pragma unroll
                 for (int j = 0; j < GO; ++j) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const int r = 8 * sum_group(j) + e;
+                        const float x = e & 1 ? high(o[K::kKeep ? j : 0][e / 2]) : low(o[K::kKeep ? j : 0][e / 2]);
                         if (r >= left) continue;
-                        if (piece) piece[r * K::D + d] = result(j, e);
-                        else if (d < a.c.dim) a.out[sh.out[slot][r] + d] = T::round(result(j, e));
+                        if (piece) piece[r * K::D + d] = x;
+                        else if (d < a.c.dim) a.out[sh.out[slot][r] + d] = T::round(x);
+                    }
+                }
+            } else {
+                // A warp takes a row, a lane four elements.
+                for (int r = w; r < left; r += K::kSoft / 32) {
+#pragma unroll
+                    for (int e = 4 * lane; e < K::D; e += 128) {
+                        const float4 x = *reinterpret_cast<const float4*>(sums_at + r * K::D + e);
+                        if (piece) {
+                            *reinterpret_cast<float4*>(piece + r * K::D + e) = x;
+                        } else if (a.ovec) {
+                            if (e < a.c.dim) *reinterpret_cast<uint2*>(a.out + sh.out[slot][r] + e) = make_uint2(pack<T>(x.x, x.y), pack<T>(x.z, x.w));
+                        } else {
+                            const float y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                if (e + k < a.c.dim) a.out[sh.out[slot][r] + e + k] = T::round(y[k]);
+                        }
                     }
                 }
             }
             if (piece) {
                 // Of a tile that several blocks share: the last of them to come joins its pieces.
-                const int b0 = line.owner(it.begin), b1 = line.owner(it.begin + it.t.units - 1);
+                const int b0 = line.owner(it.begin + place_of<K>(0)), b1 = line.owner(it.begin + place_of<K>(it.t.units - 1));
                 __threadfence();
                 soft_sync<K::kSoft>();
                 if (threadIdx.x == 0) {

@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_compact_kernel(const __
 // The moved pages' contents and their places in the table.  One thread of a block (one an SM)
 // has 32 KiB at a time copied through shared memory by bulk copies, four of them on their
 // way in while two are on theirs out; its other warps see to the table.  (Loads and
-// stores by all threads, 64 bytes of each in flight: 304 MB in 58 us, 5.2 TB/s; so @@MOVE@@.)
+// stores by all threads, 64 bytes of each in flight: 304 MB in 58 us, 5.2 TB/s; so 52 us.)
 constexpr int kMoveChunk = 32768, kMoveStages = 6, kMoveAhead = 4;
 __global__ void __launch_bounds__(256) rr_cache_move_kernel(const __grid_constant__ CacheShape c, const Book b, char* pages) {
     extern __shared__ __align__(128) char stages[];
@@ -625,7 +625,7 @@ constexpr int kMaxVocab = 1 << 20;
 // float32: h = floor(x 2^22), by adding 2^23 and cutting off, and the rest x 2^42 - h 2^20, which is exact
 // and is rounded to a whole number by adding 2^23.  Both stand in the low bits of a float from
 // kMagic on.  (Conversions to 64-bit integers run at a fraction of the rate: 64 sequences of 151936
-// entries took 52 us with them; mantissas shifted as integers 24 us; so @@ACCEPT@@.)
+// entries took 52 us with them; mantissas shifted as integers 24 us; so 18 us.)
 constexpr uint32_t kMagic = 0x4B000000u;      // 2^23
 struct Units {
     uint32_t high, low;       // kMagic + h, kMagic + the rest
