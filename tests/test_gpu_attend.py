@@ -99,6 +99,29 @@ def test_heads(n_q, n_kv, dim):
     c.check(*c.run())
 
 
+@pytest.mark.parametrize("dim", [1, 36, 80, 96, 130, 192])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("n_q,count", [(24, 1), (10, 3), (33, 2)])
+def test_many_rows_of_odd_heads(dim, kind, n_q, count):
+    """Tiles of more than 16 rows, full and not, of heads that are not whole 64s of elements."""
+    c = Case([300, 17, 2, 129], [count] * 4, n_q=n_q, n_kv=1, dim=dim, kind=kind, page=8, seed=dim)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("n_q,dim", [(8, 128), (2, 64), (6, 200)])
+def test_many_short_tiles(kind, n_q, dim):
+    """Runs that hold many tiles whole, beside one that is cut many times."""
+    gen = torch.Generator().manual_seed(n_q)
+    lengths = torch.randint(1, 400, (150,), generator=gen).tolist() + [7000]
+    counts = torch.randint(1, 6, (151,), generator=gen).tolist()
+    c = Case(lengths, counts, n_q=n_q, n_kv=1, dim=dim, kind=kind, page=32, seed=1)
+    first = c.run()
+    c.check(*first)
+    again = c.run()
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
 @pytest.mark.parametrize("n_q,n_kv,dim", [(8, 1, 128), (4, 2, 36), (14, 2, 80), (16, 1, 256)])
 def test_drafted_tokens(kind, n_q, n_kv, dim):
