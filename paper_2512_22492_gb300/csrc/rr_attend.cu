@@ -133,7 +133,7 @@ __device__ __forceinline__ void load_seq(const AttendArgs& a, int i, int* slot, 
     *slot = a.seqs[i];
     *first = a.starts ? a.starts[i] : i;
     *count = a.starts ? a.starts[i + 1] - *first : 1;
-    *length = a.c.has_seq(*slot) ? __ldg(&a.lengths[*slot]) : -1;
+    *length = a.c.has_seq(*slot) ? __ldcg(&a.lengths[*slot]) : -1;
     if (!a.c.has_length(*length) || *first < 0 || *count < 0 || *count > a.rows || *first > a.rows - *count) {
         *length = 0;
         *count = 0;
@@ -603,9 +603,41 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
     constexpr int NG = K::NG, MT = K::MT, N = K::kRows;
     extern __shared__ char memory[];
     __shared__ Shared<K> sh;
-    after_previous();
-    if (__ldcg(&a.control[kState])) return;
     const int lane = threadIdx.x & 31, w = uniform(threadIdx.x >> 5);
+
+    // What needs no memory of the call's, while the launch before may still run.
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.stages; ++i) {
+            bar_init(smem_of(&sh.full[i]), 1);
+            bar_init(smem_of(&sh.empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(smem_of(&sh.scores[i]), 1);
+            bar_init(smem_of(&sh.q_full[i]), 1);
+            bar_init(smem_of(&sh.q_free[i]), K::kSoft / 32);
+        }
+        bar_init(smem_of(&sh.weights), K::kSoft / 32);
+        bar_init(smem_of(&sh.sums), 1);
+        sh.quit = 0;
+        for (int i = 0; i < 8; ++i) sh.zero[i] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (w == K::kProducts) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_of(&sh.tmem)), "n"(K::kColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tmem_before();
+    __syncthreads();
+    tmem_after();
+    const uint32_t tmem = sh.tmem;
+    // (All of the block's threads come here.)
+    const auto leave = [&] {
+        tmem_before();
+        __syncthreads();
+        if (w == K::kProducts) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(K::kColumns) : "memory");
+    };
+    after_previous();
+    if (__ldcg(&a.control[kState])) return leave();
 
     // The line, and where this block's run begins in it.
     Line line;
@@ -639,10 +671,10 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
         int64_t mine = 0, kept = 0;
         for (int i = threadIdx.x; i < a.n; i += K::kThreads) mine += kept = work(i);
         int64_t at = scan(mine, &line.total);
-        if (line.total == 0) return;
+        if (line.total == 0) return leave();
         // (So many places that each run has a unit.)
         line.blocks = int(max(min(int64_t(gridDim.x), line.total / (2 + K::kOpen)), int64_t(1)));
-        if (int(blockIdx.x) >= line.blocks) return;
+        if (int(blockIdx.x) >= line.blocks) return leave();
         begin = line.begin(blockIdx.x), end = line.begin(blockIdx.x + 1);
         int64_t before = 0;
         for (int base = 0; base < a.n && before <= begin; base += K::kThreads) {
@@ -662,30 +694,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
     const uint32_t ring = (smem_of(memory) + 1023) / 1024 * 1024, stage_bytes = a.atoms * 16384;
     const uint32_t q_at = ring + a.stages * stage_bytes, p_at = q_at + 2 * K::kQ;
     float* const sums_at = reinterpret_cast<float*>(memory + (p_at + K::kParts * K::kP - smem_of(memory)));
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < a.stages; ++i) {
-            bar_init(smem_of(&sh.full[i]), 1);
-            bar_init(smem_of(&sh.empty[i]), 1);
-        }
-        for (int i = 0; i < 2; ++i) {
-            bar_init(smem_of(&sh.scores[i]), 1);
-            bar_init(smem_of(&sh.q_full[i]), 1);
-            bar_init(smem_of(&sh.q_free[i]), K::kSoft / 32);
-        }
-        bar_init(smem_of(&sh.weights), K::kSoft / 32);
-        bar_init(smem_of(&sh.sums), 1);
-        sh.quit = 0;
-        for (int i = 0; i < 8; ++i) sh.zero[i] = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (w == K::kProducts) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_of(&sh.tmem)), "n"(K::kColumns) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-    tmem_before();
     __syncthreads();
-    tmem_after();
-    const uint32_t tmem = sh.tmem;
     const auto wait = [&](uint64_t& bar, int parity) { return bar_wait(smem_of(&bar), parity, &sh.quit, a.control); };
 
     if (w == K::kKeys || w == K::kValues) {
@@ -697,7 +706,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
         const auto fetch = [&] {
             const int key = unit * kUnit + lane * tokens;
             if (lane >= pages || key >= walk.t.length) return -1;
-            const int id = __ldg(&a.table[int64_t(walk.t.slot) * a.c.max_pages + (key >> a.c.shift)]);
+            const int id = __ldcg(&a.table[int64_t(walk.t.slot) * a.c.max_pages + (key >> a.c.shift)]);
             if (a.c.has_page(id)) return id;
             atomicOr(&a.control[kLate], kBadTable);
             return -1;
@@ -1148,9 +1157,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             if (lane == 0) bar_arrive(smem_of(&sh.q_free[slot]));
         }
     }
-    tmem_before();
-    __syncthreads();
-    if (w == K::kProducts) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(K::kColumns) : "memory");
+    leave();
 }
 
 // ---------------------------------------------------------------------------

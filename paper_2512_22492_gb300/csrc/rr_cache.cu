@@ -660,12 +660,12 @@ struct Draw {
     __device__ __forceinline__ void load(const float* x, int k, int lane, int end, float* to) const {
         const int i = k + 4 * lane;
         if (vec && i + 3 < end) {
-            const float4 r = __ldg(reinterpret_cast<const float4*>(x + i));
+            const float4 r = __ldcg(reinterpret_cast<const float4*>(x + i));
             to[0] = r.x, to[1] = r.y, to[2] = r.z, to[3] = r.w;
             return;
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) to[e] = index<ORDER>(k, lane, e) < end ? __ldg(x + index<ORDER>(k, lane, e)) : 0.0f;
+        for (int e = 0; e < 4; ++e) to[e] = index<ORDER>(k, lane, e) < end ? __ldcg(x + index<ORDER>(k, lane, e)) : 0.0f;
     }
     // Of N times 128 entries from k on, the lane's.
     template <bool ORDER, int N>
