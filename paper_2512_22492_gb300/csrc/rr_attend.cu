@@ -32,6 +32,7 @@ namespace {
 constexpr int kUnit = 128;              // keys
 constexpr int kGather = 8;              // units whose sums gather in TMEM
 constexpr int kMostBlocks = 192;
+constexpr int kListed = 128;            // sequences whose numbers a block keeps (loading them again: 1 us)
 constexpr int kMostStages = 12;
 constexpr int kSmem = 220 * 1024;       // of a block, beside its static part
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -175,14 +176,15 @@ struct Line {
 template <class K>
 struct Walk {
     const AttendArgs& a;
+    const int4* info;                    // NULL, or all sequences' numbers
     int seq, batch;                      // the current sequence, the first one of the loaded ones
     int slot_, length_, first_, count_;  // lane l: of sequence batch + l
     int64_t at, begin, end;              // where the tile begins in the line; the run
     Tile t;
     int first, n;                        // the tile's units in the run
     // From the run's first place on, `inside` places from the begin of sequence i.
-    __device__ __forceinline__ Walk(const AttendArgs& args, int i, int64_t inside, int64_t begin_, int64_t end_)
-        : a(args), seq(i), batch(i), begin(begin_), end(end_) {
+    __device__ __forceinline__ Walk(const AttendArgs& args, const int4* info_, int i, int64_t inside, int64_t begin_, int64_t end_)
+        : a(args), info(info_), seq(i), batch(i), begin(begin_), end(end_) {
         load();
         enter();
         const int64_t each = places_of<K>(t.units), tile = inside / each;
@@ -196,7 +198,13 @@ struct Walk {
     __device__ __forceinline__ void load() {
         const int i = batch + int(threadIdx.x & 31);
         slot_ = length_ = first_ = count_ = 0;
-        if (i < a.n) load_seq(a, i, &slot_, &length_, &first_, &count_);
+        if (i >= a.n) return;
+        if (info) {
+            const int4 x = info[i];
+            slot_ = x.x, length_ = x.y, first_ = x.z, count_ = x.w;
+        } else {
+            load_seq(a, i, &slot_, &length_, &first_, &count_);
+        }
     }
     __device__ __forceinline__ void enter() {
         const int l = seq - batch;
@@ -552,6 +560,7 @@ struct Shared {
     // when that moves; 1 / the sum of weights.
     alignas(16) float zero[8], bias[K::kRows], factor[K::kRows], inverse[K::kRows];
     float parts[4][K::kRows];
+    int4 info[kListed];                               // the listed sequences, where there are no more
     int64_t scan[K::kThreads / 32];
     int64_t start;                                    // where the block's run begins within its first sequence
     int seq;                                          // that sequence
@@ -666,6 +675,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             if (i >= a.n) return 0;
             int slot, length, first, count;
             load_seq(a, i, &slot, &length, &first, &count);
+            if (a.n <= kListed) sh.info[i] = make_int4(slot, length, first, count);
             return work_of<K>(a, length, count);
         };
         int64_t mine = 0, kept = 0;
@@ -695,12 +705,13 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
     const uint32_t q_at = ring + a.stages * stage_bytes, p_at = q_at + 2 * K::kQ;
     float* const sums_at = reinterpret_cast<float*>(memory + (p_at + K::kParts * K::kP - smem_of(memory)));
     __syncthreads();
+    const int4* const info = a.n <= kListed ? sh.info : nullptr;
     const auto wait = [&](uint64_t& bar, int parity) { return bar_wait(smem_of(&bar), parity, &sh.quit, a.control); };
 
     if (w == K::kKeys || w == K::kValues) {
         // Copies: one warp the keys', one the values'.  A lane asks for one page's.
         const bool values = w == K::kValues;
-        Walk<K> walk(a, sh.seq, sh.start, begin, end);
+        Walk<K> walk(a, info, sh.seq, sh.start, begin, end);
         int unit = walk.first, left = walk.n;
         const int tokens = a.c.page, pages = kUnit >> a.c.shift, eights = tokens / 8;
         const auto fetch = [&] {
@@ -825,7 +836,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
         __syncwarp();
     } else if (w == K::kQueries) {
         // Queries, and what the others need to know of a tile.
-        Walk<K> walk(a, sh.seq, sh.start, begin, end);
+        Walk<K> walk(a, info, sh.seq, sh.start, begin, end);
         const int chunks = (a.c.dim + 15) / 16 * 2;
         for (int item = 0;; ++item) {
             const int slot = item & 1;
