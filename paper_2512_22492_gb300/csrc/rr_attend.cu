@@ -1225,7 +1225,10 @@ rr_status launch(AttendArgs& a, const CUtensorMap& map, int dev, cudaStream_t st
         RR_CUDA(cudaDeviceGetAttribute(&grid, cudaDevAttrMultiProcessorCount, dev));
         sms[dev].store(grid, std::memory_order_relaxed);
     }
-    grid = std::min(grid, kMostBlocks);
+    // No more blocks than there can be units.
+    const int64_t tiles = a.c.n_kv * (int64_t(a.rows) * a.group / K::kRows + a.n);
+    const int64_t each = (int64_t(a.c.max_pages) * a.c.page + kUnit - 1) / kUnit;
+    grid = int(std::min<int64_t>(std::min(grid, kMostBlocks), tiles * each));
     // The ring has what the queries and weights leave.  (The products of a head of an odd number
     // of 64s read, and leave out, 16 KiB behind its values: within the block's memory.)
     const int room = kSmem - 1024 - K::kFixed, stage = a.atoms * 16384;

@@ -789,30 +789,35 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) rr_accept_kernel(const __gr
     }
     if (total == 0 || t < before || t - before >= own) return;
     uint64_t left = t - before;
-    for (int k = lo; k < hi; k += 128) {
-        float y[1][4];
-        uint64_t x[4];
-        d.values<true, 1>(k, lane, hi, y);
+    bool found = false;
+    for (int base = lo; base < hi && !found; base += 512) {
+        float y[4][4];
+        d.values<true, 4>(base, lane, hi, y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = k + 4 * lane + e == d.without ? 0 : Units(y[0][e]).value();
-        const uint64_t mine = x[0] + x[1] + x[2] + x[3];
-        uint64_t up = mine;
+        for (int h = 0; h < 4; ++h) {
+            const int k = base + 128 * h + 4 * lane;
+            uint64_t x[4];
 #pragma unroll
-        for (int m = 1; m < 32; m <<= 1) {
-            const uint64_t o = __shfl_up_sync(~0u, up, m);
-            if (lane >= m) up += o;
+            for (int e = 0; e < 4; ++e) x[e] = k + e == d.without ? 0 : Units(y[h][e]).value();
+            const uint64_t mine = x[0] + x[1] + x[2] + x[3];
+            uint64_t up = mine;
+#pragma unroll
+            for (int m = 1; m < 32; m <<= 1) {
+                const uint64_t o = __shfl_up_sync(~0u, up, m);
+                if (lane >= m) up += o;
+            }
+            if (!found && up > left && up - mine <= left) {
+                uint64_t rest = left - (up - mine);
+                int e = 0;
+#pragma unroll
+                for (int z = 0; z < 3; ++z)
+                    if (e == z && rest >= x[z]) rest -= x[z], ++e;
+                a.tokens[row] = k + e;
+            }
+            const uint64_t last = __shfl_sync(~0u, up, 31);
+            found |= last > left;
+            left -= last;
         }
-        if (up > left && up - mine <= left) {
-            uint64_t rest = left - (up - mine);
-            int e = 0;
-#pragma unroll
-            for (int h = 0; h < 3; ++h)
-                if (e == h && rest >= x[h]) rest -= x[h], ++e;
-            a.tokens[row] = k + 4 * lane + e;
-        }
-        const uint64_t last = __shfl_sync(~0u, up, 31);
-        if (last > left) break;
-        left -= last;
     }
 }
 
