@@ -97,9 +97,13 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* total) {
     return before + s - v;
 }
 
-// Sums over the cluster's blocks, from what each put into b.sums[k * kBookRanks + rank]
-// before a barrier: of the ranks before this one, and of all.
-__device__ __forceinline__ int64_t rank_sum(const Book& b, const Ranks& r, int k, int64_t* total) {
+// Sums over the cluster's blocks of what each has counted, and put into b.sums[k * kBookRanks +
+// rank] before a barrier (a block alone need not): of the ranks before this one, and of all.
+__device__ __forceinline__ int64_t rank_sum(const Book& b, const Ranks& r, int k, int64_t mine, int64_t* total) {
+    if (r.size == 1) {
+        *total = mine;
+        return 0;
+    }
     int64_t before = 0, all = 0;
     for (int i = 0; i < r.size; ++i) {
         const int64_t v = __ldcg(&b.sums[k * kBookRanks + i]);
@@ -288,8 +292,8 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_extend_kernel(const __g
     }
     cluster_barrier();
     int64_t all_needed, all_free;
-    const int64_t needed_before = rank_sum(b, r, 0, &all_needed);
-    int64_t k = rank_sum(b, r, 1, &all_free);
+    const int64_t needed_before = rank_sum(b, r, 0, needed, &all_needed);
+    int64_t k = rank_sum(b, r, 1, free, &all_free);
     if (all_needed > all_free) bad = kBadPool;
     // The lowest free pages, in order.
     if (!bad) {
@@ -431,7 +435,7 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_compact_kernel(const __
     cluster_barrier();
     if (bad) return;
     int64_t used;
-    int64_t before = rank_sum(b, r, 0, &used);
+    int64_t before = rank_sum(b, r, 0, mine.end - mine.first - free, &used);
     int64_t holes = 0;
     for (int64_t base = mine.first; base < mine.end; base += 4 * kBookThreads) {
         const int64_t p = base + 4 * int64_t(threadIdx.x);
@@ -456,7 +460,7 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_compact_kernel(const __
     if (threadIdx.x == 0) b.sums[kBookRanks + r.rank] = holes;
     cluster_barrier();
     int64_t moves;
-    rank_sum(b, r, 1, &moves);
+    rank_sum(b, r, 1, holes, &moves);
     if (r.rank == 0 && threadIdx.x == 0) {
         b.control[kMoves] = int32_t(moves);
         b.control[kUsed] = int32_t(used);
