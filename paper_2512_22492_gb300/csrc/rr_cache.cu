@@ -13,8 +13,8 @@ namespace {
 //
 // Each of these calls reads short lists and tables and writes some entries: a chain of a
 // few dependent loads, whose latency is the cost, so that few launches and few barriers
-// are what counts.  One cluster of 1 or 8 blocks does a call; its barriers are the
-// hardware's.  Every block checks the whole of the call's lists by itself, and nothing
+// are what counts (3 to 6 us a call among others).  One cluster of 1 or 8 blocks does a call; its
+// barriers are the hardware's.  Every block checks the whole of the call's lists by itself, and nothing
 // is written before all of them have (a call that fails leaves the cache as it was).
 
 constexpr int kBookThreads = 512;

@@ -149,6 +149,78 @@ def test_split_over_blocks(kind):
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_a_million_tokens(kind):
+    """One sequence of 2^20 tokens, whose values have a mean: long sums do not drift.
+
+    8192 units over 152 blocks or fewer: a sum goes through at most 64 additions that cut off at
+    2^-23 (8 units, 8 products each), then 54 / 8 of a block's and 152 of the joined pieces, which
+    round; the weights' own through 54 + 9 + 152.  Less than 2^-15 of A in all (GPUs of fewer
+    SMs: twice that many units a block for half the pieces)."""
+    n, dim = 1 << 20, 64
+    gen = torch.Generator("cuda").manual_seed(3)
+    t = R.TYPES[kind]
+    c = rr.Cache(1, 1, dim, n // 64, 1, n // 64, page_tokens=64, dtype=kind)
+    c.pages.normal_(0, 1, generator=gen)
+    c.pages[:, 0, 1] = (c.pages[:, 0, 1].float().abs() * 0.5 + 0.5).to(t)
+    c.table[0] = torch.randperm(n // 64, device="cuda", generator=gen).int()
+    c.lengths.fill_(n)
+    q = (0.5 * torch.randn(1, 2, dim, device="cuda", generator=gen)).to(t)
+    out, lse = torch.empty_like(q), torch.empty(1, 2, device="cuda")
+    rr.rr_attend(c, 0, q, out, ints([0]), rr.AttendWorkspace(c, 2), lse=lse)
+    rr.rr_cache_check(c)
+    order = c.table[0].long()
+    k, v = (c.pages[order, 0, x, 0].flatten(0, 1).double() for x in (0, 1))
+    for h in range(2):
+        s = dim ** -0.5 * (k @ q[0, h].double())
+        size = dim ** -0.5 * (k.abs() @ q[0, h].double().abs())
+        e = float((size * (dim / 8 + 64) * 2.0 ** -23 + 4 * s.abs() * 2.0 ** -24).max())
+        w = torch.softmax(s, 0)
+        want, a = w @ v, w @ v.abs()
+        tol = a * (2 * math.expm1(e) + 2.0 ** -20 + R.CUT[kind] + 2.0 ** -15) * (1 + R.ROUND[kind]) + R.ROUND[kind] * want.abs()
+        assert bool(((out[0, h].double() - want).abs() <= tol).all())
+        assert abs(float(lse[0, h]) - float(torch.logsumexp(s, 0))) <= e + 2.0 ** -15 + 2.0 ** -22 * 20
+
+
+def test_first_calls_captured():
+    """A process whose first calls are captured ones."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+import paper_2512_22492_gb300 as rr
+ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+c = rr.Cache(1, 2, 64, 8, 4, 4, page_tokens=8)
+ws = rr.AttendWorkspace(c, 4)
+seqs, drop = ints(0, 2), ints(1, 0)
+q = torch.randn(2, 4, 64, device="cuda").bfloat16()
+k = torch.randn(2, 2, 64, device="cuda").bfloat16()
+out = torch.empty_like(q)
+p = torch.full((2, 50), 0.02, device="cuda")
+v, acc, tok = torch.tensor([0.0, 0.5], device="cuda"), ints(0, 0), ints(0, 0)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    rr.rr_cache_extend(c, seqs)
+    rr.rr_cache_append(c, 0, k, k, seqs)
+    rr.rr_attend(c, 0, q, out, seqs, ws)
+    rr.rr_accept(p, None, None, v, acc, tok)
+    rr.rr_cache_truncate(c, seqs, drop)
+    rr.rr_cache_compact(c)
+g.replay()
+rr.rr_cache_check(c)
+assert c.lengths.tolist() == [0, 0, 1, 0], c.lengths.tolist()
+assert torch.equal(out, k.repeat_interleave(2, 1)) and tok.tolist() == [0, 25]
+g.replay()
+rr.rr_cache_check(c)
+assert c.lengths.tolist() == [0, 0, 2, 0]
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
 def test_many_sequences():
     """More of them than a block has threads, and than a warp looks at at once."""
     gen = torch.Generator().manual_seed(1)
