@@ -557,6 +557,7 @@ template <class K>
 struct Shared {
     uint64_t full[kMostStages], empty[kMostStages];   // of the ring's stages
     uint64_t scores[2], weights, sums;                // S^T is there (two of them, in turn); P^T; D^T
+    uint64_t drained;                                 // (of a call that gave up) no product is under way
     uint64_t q_full[2], q_free[2];                    // a tile's queries and all that is said of it below
     Item items[2];
     alignas(16) int seen[2][K::kRows];
@@ -632,6 +633,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
         }
         bar_init(smem_of(&sh.weights), K::kSoft / 32);
         bar_init(smem_of(&sh.sums), 1);
+        bar_init(smem_of(&sh.drained), 1);
         sh.quit = 0;
         for (int i = 0; i < 8; ++i) sh.zero[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -837,6 +839,13 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 ++v_unit;
                 --v_left;
                 ++done;
+            }
+        }
+        if (sh.quit) {
+            // The products under way have to end before their memory is given back.
+            if (elected()) {
+                products_arrive(smem_of(&sh.drained));
+                for (int x = 0; x < 1 << 20 && !bar_try(smem_of(&sh.drained), 0); ++x) {}
             }
         }
         __syncwarp();

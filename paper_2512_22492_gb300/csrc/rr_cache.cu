@@ -497,6 +497,7 @@ __global__ void __launch_bounds__(256) rr_cache_move_kernel(const __grid_constan
         int bytes[kMoveStages];
         // (Unrolled by stage, so that out and bytes are registers.)
         bool ok = true;
+        int asked = 0, landed = 0;
         for (int base = 0; ok && base < n + kMoveAhead; base += kMoveStages) {
 #pragma unroll
             for (int s = 0; s < kMoveStages; ++s) {
@@ -513,6 +514,7 @@ __global__ void __launch_bounds__(256) rr_cache_move_kernel(const __grid_constan
                                      smem(stages + s * kMoveChunk)),
                                  "l"(pages + move.x * c.page_bytes + at), "r"(bytes[s]), "r"(smem(&full[s]))
                                  : "memory");
+                    asked = i + 1;
                 }
                 constexpr int kBack = kMoveStages - kMoveAhead;
                 const int j = i - kMoveAhead, from = (s + kBack) % kMoveStages;
@@ -535,9 +537,20 @@ __global__ void __launch_bounds__(256) rr_cache_move_kernel(const __grid_constan
                                      "r"(smem(stages + from * kMoveChunk)), "r"(bytes[from])
                                      : "memory");
                         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        landed = j + 1;
                     }
                 }
             }
+        }
+        // (Of a call that gave up: what is on its way has to land before the block ends.)
+        for (int i = landed; !ok && i < asked; ++i) {
+            uint32_t done = 0;
+            for (int x = 0; x < 1 << 20 && !done; ++x)
+                asm volatile(
+                    "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                    : "=r"(done)
+                    : "r"(smem(&full[i % kMoveStages])), "r"(i / kMoveStages & 1)
+                    : "memory");
         }
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
