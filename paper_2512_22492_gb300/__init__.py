@@ -16,7 +16,7 @@ from .rr import (Block, DstLayout, DstTensor, Param, Plan, PlanOptions, Pointers
 from .products import (MoeLayer, MoeWorkspace, Quantized, rr_dequantize, rr_matvec, rr_moe,
                        rr_moe_check, rr_quantize)
 from .cache import (AttendWorkspace, Cache, rr_accept, rr_attend, rr_cache_append, rr_cache_check,
-                    rr_cache_compact, rr_cache_extend, rr_cache_fork, rr_cache_truncate)
+                    rr_cache_clear, rr_cache_compact, rr_cache_extend, rr_cache_fork, rr_cache_truncate)
 from .layouts import qwen3_layer_units, qwen3_manifest, qwen3_rollout, qwen3_sync
 
 __all__ = ["Block", "DstLayout", "DstTensor", "Param", "Plan", "PlanOptions", "Pointers",
@@ -27,5 +27,5 @@ __all__ = ["Block", "DstLayout", "DstTensor", "Param", "Plan", "PlanOptions", "P
            "Quantized", "MoeLayer", "MoeWorkspace", "rr_quantize", "rr_dequantize", "rr_matvec",
            "rr_moe", "rr_moe_check",
            "Cache", "AttendWorkspace", "rr_cache_fork", "rr_cache_extend", "rr_cache_append",
-           "rr_cache_truncate", "rr_cache_compact", "rr_cache_check", "rr_attend", "rr_accept",
+           "rr_cache_truncate", "rr_cache_compact", "rr_cache_check", "rr_cache_clear", "rr_attend", "rr_accept",
            "qwen3_layer_units", "qwen3_manifest", "qwen3_rollout", "qwen3_sync"]

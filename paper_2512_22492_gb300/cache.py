@@ -145,6 +145,13 @@ def _vectors(x, heads: int, cache: Cache, what: str):
     return n, ld
 
 
+def rr_cache_clear(cache: Cache, stream=None) -> None:
+    """Makes the cache empty: no sequence holds a token, all pages are free, no mark is left."""
+    st = _lib.rr_cache_clear(cache._ref, cache._b, _stream_of(cache.book, stream))
+    if st != RR_OK:
+        _check(st, "rr_cache_clear")
+
+
 def rr_cache_fork(cache: Cache, parents, children, stream=None) -> None:
     """children[i], an empty sequence, comes to hold parents[i]'s tokens: its pages, shared.
     A parent may be listed more than once.  Asynchronous on `stream`, as all calls on a

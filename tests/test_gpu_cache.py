@@ -247,3 +247,18 @@ def test_no_sequences():
     rr.rr_cache_append(b.c, 0, k, k, none)
     rr.rr_cache_compact(b.c)
     b.check()
+
+
+def test_clear():
+    """A used and marked cache is as a new one again."""
+    b = Both()
+    b.add([0, 4], [20, 7])
+    b.fork([0], [1])
+    rr.rr_cache_truncate(b.c, ints([0, 0]))          # (twice: marked)
+    rr.rr_cache_clear(b.c)
+    b.b = R.Book(b.b.pages, 12, 8)
+    b.check()
+    new = rr.Cache(2, 2, 32, 40, 12, 8, page_tokens=8)
+    assert torch.equal(b.c.book[64:], new.book[64:])
+    b.add([4, 2], [9, 9])
+    b.check()
