@@ -791,7 +791,7 @@ rr_status rr_cache_check(const rr_cache* cache, void* book, cudaStream_t stream)
  * A row that sees no token has out 0 and lse -infinity, as has one whose scores are all
  * -infinity.  Tokens that a row does not see do not touch it, whatever they hold.
  * Scores and sums are float32; the weights exp(s_t - max) enter the product with the
- * values as two bfloat16 parts (to 2^-16 of themselves) or as float16 (2^-11, or 2^-32 of
+ * values as two parts, bfloat16 (to 2^-16 of themselves) or float16 (2^-22, or 2^-32 of
  * the largest); the result is rounded once.  Which keys are summed together depends on the
  * call's lengths: beside other sequences a row's last bits may be others.
  *   lse: rows x n_q floats, or NULL.  Rows of no listed sequence are left as they are.

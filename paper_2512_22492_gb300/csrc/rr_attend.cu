@@ -21,7 +21,7 @@
 //
 // Measured: 64 sequences of 200 to 16000 tokens, 32 heads over 4 key heads of 128 (1.06 GB):
 // 172 to 175 us, 6.1 TB/s (the SMs' mean is done after 155, the last after 166); 96 of 500 to
-// 7500, 64 over 8, five tokens each (1.59 GB): 259 to 262 us, 6.1 TB/s; one of 40001, 32 over 8
+// 7500, 64 over 8, five tokens each (1.59 GB): 278 to 280 us, 5.7 TB/s; one of 40001, 32 over 8
 // (164 MB): 36 us, 4.6 TB/s.
 #include <algorithm>
 #include <climits>
@@ -83,11 +83,13 @@ struct Kind {
     static constexpr int kSets = NG == 8 ? 3 : 2;
     static constexpr int kSoft = 128 * kSets, kThreads = kSoft + 128;
     static constexpr int kKeys = kSoft / 32, kValues = kKeys + 1, kProducts = kKeys + 2, kQueries = kKeys + 3;
-    // Bfloat16 keeps 8 bits of a weight: it enters the second product in two parts, 16
-    // bits in all.  Float16's 11 bits are one part: as far off as the result's own
-    // rounding is.  Its weights are 2^7 to 2^15 at a row's maximum, so that those 2^-21 of
-    // the largest still have all of their bits (under 2^-32 of it they are 0).
-    static constexpr int kParts = std::is_same<T, BF16>::value ? 2 : 1;
+    // A weight enters the second product in two parts: of bfloat16 16 bits in all, of float16 22.
+    // (One part is off by up to half of its last bit: float16's 2^-12 would be as much as a result's
+    // own rounding, and more than that where values cancel.)  Float16's weights are 2^7 to 2^15 at
+    // a row's maximum, so that those 2^-21 of the largest still have all bits of their first
+    // part; the second ends at 2^-32 of it.  (Float16's second part: nothing up to 16 rows, and of 64
+    // rows a stage of the ring: 96 sequences of five tokens of 8 heads each 280 us, 260 with one.)
+    static constexpr int kParts = 2;
     static constexpr float kLift = std::is_same<T, BF16>::value ? 0.0f : 7.0f;
     static constexpr int kQ = MT * NG * 2048;           // bytes of a tile's queries
     static constexpr int kP = NG * 2048;                // of one part of the weights
@@ -811,7 +813,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                     v_length = uniform(item.t.length);
                     // (One product for both parts of the weights, side by side: a product takes about 75
                     // cycles and one more for each column or so.)
-                    v_instr = instruction<T>(K::kParts == 1 ? columns(item.t) : 2 * uniform((rows_of(item.t) + 7) / 8 * 8), true, true);
+                    v_instr = instruction<T>(2 * uniform((rows_of(item.t) + 7) / 8 * 8), true, true);
                     ++v_item;
                 }
                 if (!__all_sync(~0u, wait(sh.full[st.at], st.turn))) break;
@@ -934,18 +936,13 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
 #pragma unroll
                 for (int j = 0; j < GO; ++j) {
                     if (sum_group(j) >= groups) continue;
-                    F2 x[4];
+                    F2 x[4], y[4];
                     const uint32_t columns = tmem + lanes + 2 * N + half * K::kD + 8 * sum_group(j);
                     tmem_load(columns, x);
-                    if (K::kParts == 2) {
-                        F2 y[4];
-                        tmem_load(columns + 8 * groups, y);
-                        tmem_loaded();
+                    tmem_load(columns + 8 * groups, y);
+                    tmem_loaded();
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] = add2(x[e], y[e]);
-                    } else {
-                        tmem_loaded();
-                    }
+                    for (int e = 0; e < 4; ++e) x[e] = add2(x[e], y[e]);
                     float* const at = sums_at + 8 * sum_group(j) * K::D + d;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -1059,10 +1056,8 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                         sum[j][e] = add2(sum[j][e], y);
                         const uint32_t big = pack<T>(lo, hi);
                         p[j][0][e] = big;
-                        if (K::kParts == 2) {
-                            const F2 rest = fma2(both(T::widen(uint16_t(big)), T::widen(uint16_t(big >> 16))), both(-1.0f, -1.0f), y);
-                            p[j][K::kParts - 1][e] = pack<T>(low(rest), high(rest));
-                        }
+                        const F2 rest = fma2(both(T::widen(uint16_t(big)), T::widen(uint16_t(big >> 16))), both(-1.0f, -1.0f), y);
+                        p[j][1][e] = pack<T>(low(rest), high(rest));
                     }
                 }
                 // The weights may be overwritten once the products of the unit before are done.
