@@ -433,7 +433,11 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_compact_kernel(const __
     const int64_t free = mine.free(b.refs);
     if (threadIdx.x == 0) b.sums[r.rank] = mine.end - mine.first - free;
     cluster_barrier();
-    if (bad) return;
+    if (bad) {
+        // (fail() stops the launch that moves pages, too.)
+        if (r.rank == 0 && threadIdx.x == 0) b.control[kMoves] = 0;
+        return fail(b, r, bad);
+    }
     int64_t used;
     int64_t before = rank_sum(b, r, 0, mine.end - mine.first - free, &used);
     int64_t holes = 0;

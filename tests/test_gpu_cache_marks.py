@@ -1,0 +1,62 @@
+"""Marked caches on the GPU: what a mark stops, what it leaves, and what is reported of it."""
+import pytest
+import torch
+
+import paper_2512_22492_gb300 as rr
+from tests.test_gpu_cache import Both, ints, same, starts_of, state
+
+pytestmark = pytest.mark.gpu
+
+
+def used(compacted, **kw):
+    """A cache whose last extension took copies, with free pages between others; compacted
+    before that, or never."""
+    b = Both(n_pages=kw.pop("n_pages", 60), **kw)
+    b.add([0, 2, 4], [19, 5, 9])
+    if compacted:
+        b.truncate([2])
+        b.compact()
+        b.add([2], [5])
+    b.add([5, 6], [8, 8])
+    b.truncate([5])
+    b.fork([0], [1])
+    b.add([1, 0], [3, 2])
+    b.truncate([4])
+    b.check()
+    return b
+
+
+def late_mark(b, by):
+    """A mark by a call that does all but for what does not fit (here: nothing fits)."""
+    x = torch.ones(1, 2, 32, dtype=torch.bfloat16, device="cuda")
+    if by == "append":
+        rr.rr_cache_append(b.c, 0, x, x, ints([12]))
+    else:
+        rr.rr_attend(b.c, 0, x, torch.empty_like(x), ints([-1]), rr.AttendWorkspace(b.c, 2))
+
+
+@pytest.mark.parametrize("compacted", [False, True])
+@pytest.mark.parametrize("by", ["append", "attend"])
+@pytest.mark.parametrize("call", ["compact", "fork", "extend", "truncate"])
+@pytest.mark.parametrize("n_pages", [60, 5000])
+def test_calls_behind_a_late_mark(compacted, by, call, n_pages):
+    """The first call that would write the book, and those behind it, leave the cache as it was."""
+    b = used(compacted, n_pages=n_pages)
+    c = b.c
+    before = state(c)
+    late_mark(b, by)
+    calls = {"compact": lambda: rr.rr_cache_compact(c), "fork": lambda: rr.rr_cache_fork(c, ints([0]), ints([7])),
+             "extend": lambda: rr.rr_cache_extend(c, ints([0, 1, 2])), "truncate": lambda: rr.rr_cache_truncate(c, ints([0]))}
+    calls[call]()
+    assert same(c, before)
+    for again in calls.values():
+        again()
+    assert same(c, before)
+    with pytest.raises(rr.RRError, match="range"):
+        rr.rr_cache_check(c)
+    rr.rr_cache_check(c)
+    assert same(c, before)
+    # And goes on as if nothing had been.
+    b.compact()
+    b.add([0, 1, 7], [2, 9, 17])
+    b.check()
