@@ -32,9 +32,11 @@ __device__ __forceinline__ int cluster_size() {
     return int(r);
 }
 // Everything that the cluster's threads wrote before is seen by all of them after.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ void cluster_barrier() {
-    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 
 struct Ranks {
@@ -714,6 +716,9 @@ struct Draw {
 __global__ void __launch_bounds__(kAcceptThreads, 1) rr_accept_kernel(const __grid_constant__ AcceptArgs a) {
     __shared__ uint64_t sums[2][kAcceptRanks * kAcceptThreads / 32];
     __shared__ int first_refused;
+    // Another block's shared memory may be written once that block runs: waited for before
+    // the first sums go there, behind the loads.
+    cluster_arrive();
     after_previous();
     const int i = blockIdx.x / kAcceptRanks, rank = cluster_rank();
     const int lane = threadIdx.x & 31, per_block = blockDim.x / 32, w = rank * per_block + int(threadIdx.x >> 5);
@@ -767,6 +772,7 @@ __global__ void __launch_bounds__(kAcceptThreads, 1) rr_accept_kernel(const __gr
         if (lane == 0 && d.without >= lo && d.without < hi) mine -= Units(d.p[d.without]).value();
 #pragma unroll
         for (int m = 16; m; m >>= 1) mine += __shfl_xor_sync(~0u, mine, m);
+        if (pass == 0) cluster_wait();
         if (lane < kAcceptRanks) {
             uint32_t at = uint32_t(__cvta_generic_to_shared(&sums[pass][w])), to;
             asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(at), "r"(lane));
