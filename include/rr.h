@@ -765,7 +765,9 @@ rr_status rr_cache_extend(const rr_cache* cache, void* pages, void* book, const 
 
 /* One layer's keys and values of new tokens: `rows` rows of n_kv * dim elements.  Rows
  * starts[i] .. starts[i + 1] - 1 are the last tokens of seqs[i]; with starts NULL, row i
- * is the last one of seqs[i], and rows is n.  Rows of no sequence are left out. */
+ * is the last one of seqs[i], and rows is n.  Rows of no sequence are left out.  A sequence whose
+ * starts lie outside 0 .. rows, or descend, is left out and marks the cache; where they
+ * descend, so may other rows be. */
 rr_status rr_cache_append(const rr_cache* cache, void* pages, void* book, int32_t layer,
                           const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t rows,
                           const int32_t* seqs, const int32_t* starts, int32_t n,

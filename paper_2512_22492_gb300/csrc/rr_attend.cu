@@ -140,11 +140,13 @@ __device__ __forceinline__ int seen(const Tile& t, int group, int row) { return 
 __device__ __forceinline__ void load_seq(const AttendArgs& a, int i, int* slot, int* length, int* first, int* count) {
     *slot = a.seqs[i];
     *first = a.starts ? a.starts[i] : i;
-    *count = a.starts ? a.starts[i + 1] - *first : 1;
+    const int end = a.starts ? a.starts[i + 1] : i + 1;
     *length = a.c.has_seq(*slot) ? __ldcg(&a.lengths[*slot]) : -1;
-    if (!a.c.has_length(*length) || *first < 0 || *count < 0 || *count > a.rows || *first > a.rows - *count) {
+    *count = 0;
+    if (a.c.has_length(*length) && *first >= 0 && end >= *first && end <= a.rows) {
+        *count = end - *first;
+    } else {
         *length = 0;
-        *count = 0;
         atomicOr(&a.control[kLate], kBadRange);
     }
 }

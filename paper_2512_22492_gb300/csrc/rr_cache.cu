@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_fork_kernel(const __gri
     }
 }
 
-__device__ __forceinline__ int new_tokens(const int32_t* starts, int i) { return starts ? starts[i + 1] - starts[i] : 1; }
+__device__ __forceinline__ int64_t new_tokens(const int32_t* starts, int i) { return starts ? int64_t(starts[i + 1]) - starts[i] : 1; }
 
 // A listed sequence's next tokens: where they begin, and the page that is partly filled.
 struct Growth {
@@ -216,7 +216,7 @@ struct Growth {
     __device__ __forceinline__ Growth() {}
     __device__ __forceinline__ Growth(const CacheShape& c, const Book& b, const int32_t* seqs, const int32_t* starts, int i) {
         s = seqs[i];
-        count = new_tokens(starts, i);
+        count = int(new_tokens(starts, i));
         length = __ldcg(&b.lengths[s]);
         filled = length & (c.page - 1);
         entry = int64_t(s) * c.max_pages + (length >> c.shift);
@@ -236,7 +236,8 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_extend_kernel(const __g
     Listed listed(shared_bits, c.max_seqs);
     int bad = __ldcg(&b.control[kState]) | __ldcg(&b.control[kLate]);
     for (int i = threadIdx.x; i < n; i += kBookThreads) {
-        const int s = seqs[i], count = new_tokens(starts, i);
+        const int s = seqs[i];
+        const int64_t count = new_tokens(starts, i);
         if (!c.has_seq(s)) {
             bad |= kBadRange;
             continue;
@@ -244,7 +245,7 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_extend_kernel(const __g
         if (listed.add(s)) bad |= kBadTwice;
         const int length = __ldcg(&b.lengths[s]);
         if (!c.has_length(length) || count < 0) bad |= kBadRange;
-        else if (int64_t(length) + count > c.max_length()) bad |= kBadPool;
+        else if (length + count > c.max_length()) bad |= kBadPool;
         else if (count && (length & (c.page - 1)) && !c.has_page(__ldcg(&b.table[int64_t(s) * c.max_pages + (length >> c.shift)])))
             bad |= kBadTable;
     }
@@ -582,13 +583,10 @@ __global__ void __launch_bounds__(256) rr_cache_move_kernel(const __grid_constan
 // A warp takes one token's row: 2 n_kv vectors of `dim` elements, `pitch` in the page.
 // VEC: rows can be read 16 bytes at a time.
 template <bool VEC>
-__global__ void __launch_bounds__(256) rr_cache_append_kernel(const __grid_constant__ CacheShape c, const Book b, char* pages, int layer,
-                                                              const uint16_t* k, int64_t ldk, const uint16_t* v, int64_t ldv,
-                                                              const int32_t* seqs, const int32_t* starts, int n, int rows) {
-    after_previous();
-    if (__ldcg(&b.control[kState])) return;
-    const int lane = threadIdx.x & 31, row = int(blockIdx.x * 8 + (threadIdx.x >> 5));
-    if (row >= rows) return;
+__device__ __forceinline__ void append_row(const CacheShape& c, const Book& b, char* pages, int layer, const uint16_t* k, int64_t ldk,
+                                           const uint16_t* v, int64_t ldv, const int32_t* seqs, const int32_t* starts, int n, int rows,
+                                           int row) {
+    const int lane = threadIdx.x & 31;
     int i = row, j = 0, count = 1;
     if (starts) {
         // The first sequence that ends behind the row; 32 places looked at at a time.
@@ -601,9 +599,12 @@ __global__ void __launch_bounds__(256) rr_cache_append_kernel(const __grid_const
             left = min(step - 1, left - before * step);
         }
         i = lo;
-        if (i >= n || row < starts[i] || row >= starts[i + 1]) return;
-        j = row - starts[i];
-        count = starts[i + 1] - starts[i];
+        if (i >= n) return;
+        const int first = starts[i], end = starts[i + 1];
+        // (A sequence whose rows are not all there is left out, below.)
+        if (first < 0 || row < first || row >= end || end > rows) return;
+        j = row - first;
+        count = end - first;
     }
     const int s = seqs[i];
     int length = 0, id = -1, bad = 0;
@@ -633,6 +634,30 @@ __global__ void __launch_bounds__(256) rr_cache_append_kernel(const __grid_const
             u = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
         }
         *reinterpret_cast<uint4*>(to + head * c.run_bytes + 2 * d) = u;
+    }
+}
+
+template <bool VEC>
+__global__ void __launch_bounds__(256) rr_cache_append_kernel(const __grid_constant__ CacheShape c, const Book b, char* pages, int layer,
+                                                              const uint16_t* k, int64_t ldk, const uint16_t* v, int64_t ldv,
+                                                              const int32_t* seqs, const int32_t* starts, int n, int rows) {
+    after_previous();
+    if (__ldcg(&b.control[kState])) return;
+    const int lane = threadIdx.x & 31, row = int(blockIdx.x * 8 + (threadIdx.x >> 5));
+    if (row >= rows) return;
+    // What of the lists does not fit is seen by no row, or not by all: the warps look through them
+    // together, and have what they look at on its way while the row is written.
+    const int64_t from = int64_t(row) * 32 + lane;
+    int s = 0, first = 0, end = 0;
+    if (starts && from < n) s = seqs[from], first = starts[from], end = starts[from + 1];
+    append_row<VEC>(c, b, pages, layer, k, ldk, v, ldv, seqs, starts, n, rows, row);
+    const auto check = [&] {
+        if (!c.has_seq(s) || first < 0 || end < first || end > rows) atomicOr(&b.control[kLate], kBadRange);
+    };
+    check();
+    for (int64_t i = from + int64_t(rows) * 32; starts && i < n; i += int64_t(rows) * 32) {
+        s = seqs[i], first = starts[i], end = starts[i + 1];
+        check();
     }
 }
 
