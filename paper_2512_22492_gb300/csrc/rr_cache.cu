@@ -177,30 +177,53 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_fork_kernel(const __gri
     for (int i = threadIdx.x; i < n; i += kBookThreads)
         if (c.has_seq(parents[i]) && listed.has(parents[i])) bad |= kBadTwice;
     bad = agree(bad);
-    cluster_barrier();
-    if (bad) return fail(b, r, bad);
-    // A warp takes 128 entries of one parent's row.
+    // A warp takes 128 entries of one parent's row.  All of them are looked at before any is
+    // written (0.3 us; of a parent listed several times in a row once); those of a warp's first task
+    // (there are others only in long calls) stay in its registers.
     constexpr int kEach = 128;
     const int lane = threadIdx.x & 31;
     const int chunks = (c.max_pages + kEach - 1) / kEach;
-    for (int64_t task = r.warp(); task < int64_t(n) * chunks; task += r.warps()) {
-        const int i = int(task / chunks), first = int(task % chunks) * kEach;
-        const int p = parents[i], s = children[i], length = __ldcg(&b.lengths[p]);
-        const int end = min(pages_of(length, c.shift), first + kEach);
-        if (first == 0 && lane == 0) b.lengths[s] = length;
+    struct Task {
+        int s, length, first, end;
         int32_t id[kEach / 32];
+    };
+    const auto task_of = [&](int64_t task) {
+        Task t;
+        const int i = int(task / chunks), p = parents[i];
+        t.first = int(task % chunks) * kEach;
+        t.s = children[i];
+        t.length = __ldcg(&b.lengths[p]);
+        t.end = min(pages_of(t.length, c.shift), t.first + kEach);
 #pragma unroll
         for (int k = 0; k < kEach / 32; ++k) {
-            const int j = first + lane + 32 * k;
-            id[k] = j < end ? __ldcg(&b.table[int64_t(p) * c.max_pages + j]) : -1;
+            const int j = t.first + lane + 32 * k;
+            t.id[k] = j < t.end ? __ldcg(&b.table[int64_t(p) * c.max_pages + j]) : -1;
         }
+        return t;
+    };
+    const int64_t tasks = bad ? 0 : int64_t(n) * chunks;
+    Task kept = {};
+    bool found = false;
+    for (int64_t task = r.warp(); task < tasks; task += r.warps()) {
+        const int i = int(task / chunks);
+        if (task != r.warp() && i && parents[i] == parents[i - 1]) continue;
+        const Task t = task_of(task);
+        if (task == r.warp()) kept = t;
+#pragma unroll
+        for (int k = 0; k < kEach / 32; ++k) found |= t.first + lane + 32 * k < t.end && !c.has_page(t.id[k]);
+    }
+    if (found) atomicOr(&b.control[kState], kBadTable);
+    cluster_barrier();
+    if (bad || __ldcg(&b.control[kState])) return fail(b, r, bad);
+    for (int64_t task = r.warp(); task < tasks; task += r.warps()) {
+        const Task t = task == r.warp() ? kept : task_of(task);
+        if (t.first == 0 && lane == 0) b.lengths[t.s] = t.length;
 #pragma unroll
         for (int k = 0; k < kEach / 32; ++k) {
-            const int j = first + lane + 32 * k;
-            if (j >= end) continue;
-            b.table[int64_t(s) * c.max_pages + j] = id[k];
-            if (c.has_page(id[k])) atomicAdd(&b.refs[id[k]], 1);
-            else atomicOr(&b.control[kLate], kBadTable);
+            const int j = t.first + lane + 32 * k;
+            if (j >= t.end) continue;
+            b.table[int64_t(t.s) * c.max_pages + j] = t.id[k];
+            atomicAdd(&b.refs[t.id[k]], 1);
         }
     }
 }
@@ -407,9 +430,18 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_truncate_kernel(const _
         if (!c.has_length(length) || (drop && (drop[i] < 0 || drop[i] > length))) bad |= kBadRange;
     }
     bad = agree(bad);
-    cluster_barrier();
-    if (bad) return fail(b, r, bad);
     const int lane = threadIdx.x & 31;
+    // The pages are looked at before any is given up (0.6 us).
+    bool found = false;
+    for (int i = r.warp(); !bad && i < n; i += r.warps()) {
+        const int s = seqs[i], length = __ldcg(&b.lengths[s]), left = drop ? length - drop[i] : 0;
+        const int32_t* const row = b.table + int64_t(s) * c.max_pages;
+#pragma unroll 4
+        for (int j = pages_of(left, c.shift) + lane; j < pages_of(length, c.shift); j += 32) found |= !c.has_page(__ldcg(&row[j]));
+    }
+    if (found) atomicOr(&b.control[kState], kBadTable);
+    cluster_barrier();
+    if (bad || __ldcg(&b.control[kState])) return fail(b, r, bad);
     for (int i = r.warp(); i < n; i += r.warps()) {
         const int s = seqs[i], length = __ldcg(&b.lengths[s]), left = drop ? length - drop[i] : 0;
         __syncwarp();
@@ -418,8 +450,7 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_truncate_kernel(const _
         for (int j = pages_of(left, c.shift) + lane; j < pages_of(length, c.shift); j += 32) {
             const int id = row[j];
             row[j] = -1;
-            if (c.has_page(id)) atomicSub(&b.refs[id], 1);
-            else atomicOr(&b.control[kLate], kBadTable);
+            atomicSub(&b.refs[id], 1);
         }
         if (lane == 0) b.lengths[s] = left;
     }

@@ -60,3 +60,28 @@ def test_calls_behind_a_late_mark(compacted, by, call, n_pages):
     b.compact()
     b.add([0, 1, 7], [2, 9, 17])
     b.check()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(n_pages=3000, max_pages=400, max_seqs=40)])
+@pytest.mark.parametrize("page", ["n_pages", -1, -(1 << 31), (1 << 31) - 1])
+@pytest.mark.parametrize("call", ["fork", "truncate", "truncate to 9"])
+def test_pages_out_of_range_are_found_before_anything_is_written(kw, page, call):
+    b = Both(**kw)
+    b.add([0, 2, 3, 4], [40, 5, 9, 30])
+    c = b.c
+    good = int(c.table[0, 3])
+    c.table[0, 3] = c.n_pages if page == "n_pages" else page
+    before = state(c)
+    if call == "fork":
+        rr.rr_cache_fork(c, ints([2, 0, 4, 0]), ints([1, 5, 6, 7]))
+    elif call == "truncate":
+        rr.rr_cache_truncate(c, ints([2, 0, 4]))
+    else:
+        rr.rr_cache_truncate(c, ints([2, 4, 0]), ints([1, 20, 31]))
+    with pytest.raises(rr.RRError, match="table"):
+        rr.rr_cache_check(c)
+    assert same(c, before)
+    c.table[0, 3] = good
+    b.fork([2, 0, 4, 0], [1, 5, 6, 7])
+    b.truncate([2, 0])
+    b.check()
