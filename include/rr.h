@@ -716,13 +716,15 @@ rr_status rr_moe_check(const rr_moe_layer* layer, int32_t max_tokens, void* work
  * same bits each time.
  *
  * Lists (sequences, counts, starts) are on the device, where the host does not see
- * what they hold.  A call that finds a number out of range, a sequence listed twice or
- * the pool without room leaves the cache as it was and marks it; later calls then leave
- * all as it is, until rr_cache_check has reported the mark.  rr_cache_append and rr_attend
- * leave out what does not fit (a row whose pages are out of range holds anything), and mark the
- * cache likewise.  rr_attend and rr_cache_compact wait within a block, each time for two
- * seconds or so at most; a wait that runs out marks the cache, too (RR_ECUDA): outputs and pages
- * are then incomplete, and rr_attend's workspace has to be filled with zeros again.
+ * what they hold.  A call on the book that finds a number out of range, a sequence listed twice or
+ * the pool without room is not done: it leaves the cache as it was and marks it, and later calls,
+ * rr_cache_append and rr_attend among them, leave all as it is until rr_cache_check has
+ * reported the mark.  rr_cache_append and rr_attend themselves leave out what does not fit (a row
+ * whose pages are out of range holds anything), and mark the cache for that: calls on the book
+ * behind such a mark are not done, appends and attentions still do what fits.  rr_attend and
+ * rr_cache_compact wait within a block, each time for two seconds or so at most; a wait that runs
+ * out marks the cache, too (RR_ECUDA): outputs and pages are then incomplete, and rr_attend's
+ * workspace has to be filled with zeros again.
  * ------------------------------------------------------------------------- */
 
 /* The cache's shape.

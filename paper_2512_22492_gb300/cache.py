@@ -209,8 +209,9 @@ def rr_cache_compact(cache: Cache, stream=None) -> None:
 
 def rr_cache_check(cache: Cache, stream=None) -> None:
     """Raise if a call on this cache found its lists or the table out of range, or the pool
-    without room (waits for `stream`).  Such a call, and those after it, left the cache as
-    it was."""
+    without room (waits for `stream`).  Such a call was not done, nor were those after it, and the
+    cache is as it was; ``rr_cache_append`` and ``rr_attend`` left out what did not fit, after which
+    only they go on."""
     _check(_lib.rr_cache_check(cache._ref, cache._b, _stream_of(cache.pages, stream)),
            "rr_cache_check")
 

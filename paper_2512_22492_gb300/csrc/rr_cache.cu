@@ -1110,7 +1110,10 @@ extern "C" rr_status rr_cache_check(const rr_cache* C, void* book, cudaStream_t 
     RR_CUDA(cudaMemsetAsync(book, 0, 8, stream));
     RR_CUDA(cudaStreamSynchronize(stream));
     if (state & kBadWait) return rr_fail(RR_ECUDA, "a wait of a call on the cache ran out");
-    return rr_fail(RR_EINVAL, "a call on the cache was not done:%s%s%s%s%s", state & kBadRange ? " a sequence, length or count is out of range;" : "",
+    // (A call that is not done takes over what one before it left, so that both are reported.)
+    const char* const what = !words[0] ? "a call on the cache left something out" : !words[1] ? "a call on the cache was not done"
+                                       : "a call on the cache left something out, and a later one was not done";
+    return rr_fail(RR_EINVAL, "%s:%s%s%s%s%s", what, state & kBadRange ? " a sequence, length or count is out of range;" : "",
                    state & kBadTwice ? " a sequence is listed twice;" : "", state & kBadPool ? " no room for the new tokens;" : "",
                    state & kBadChild ? " a child holds tokens;" : "", state & kBadTable ? " the table has a page out of range;" : "");
 }

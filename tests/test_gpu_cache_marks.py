@@ -85,3 +85,48 @@ def test_pages_out_of_range_are_found_before_anything_is_written(kw, page, call)
     b.fork([2, 0, 4, 0], [1, 5, 6, 7])
     b.truncate([2, 0])
     b.check()
+
+
+@pytest.mark.parametrize("by", ["append", "attend"])
+def test_what_a_mark_says(by):
+    """A call that left something out was done for the rest; one that was not done was not."""
+    b = used(False)
+    late_mark(b, by)
+    with pytest.raises(rr.RRError) as e:
+        rr.rr_cache_check(b.c)
+    assert "left something out" in str(e.value) and "not done" not in str(e.value)
+    rr.rr_cache_extend(b.c, ints([0, 0]))
+    with pytest.raises(rr.RRError) as e:
+        rr.rr_cache_check(b.c)
+    assert "not done" in str(e.value) and "left something out" not in str(e.value)
+    late_mark(b, by)
+    rr.rr_cache_extend(b.c, ints([0]))
+    with pytest.raises(rr.RRError) as e:
+        rr.rr_cache_check(b.c)
+    assert "left something out" in str(e.value) and "not done" in str(e.value)
+    b.check()
+
+
+def test_append_and_attend_go_on_behind_a_late_mark():
+    """They do what fits, as they do in the call that marks."""
+    b = used(False)
+    late_mark(b, "append")
+    b.append(1, [0, 1, 2])
+    x = torch.ones(1, 2, 32, dtype=torch.bfloat16, device="cuda")
+    out = [torch.zeros_like(x) for _ in range(2)]
+    ws = rr.AttendWorkspace(b.c, 2)
+    rr.rr_attend(b.c, 1, x, out[0], ints([0]), ws)
+    with pytest.raises(rr.RRError, match="left something out"):
+        rr.rr_cache_check(b.c)
+    b.check()
+    rr.rr_attend(b.c, 1, x, out[1], ints([0]), ws)
+    assert out[0].any() and torch.equal(out[0], out[1])
+    # Behind a call that was not done they leave all as it is.
+    rr.rr_cache_extend(b.c, ints([0, 0]))
+    before = state(b.c)
+    out[0].fill_(9.0)
+    rr.rr_cache_append(b.c, 0, x, x, ints([0]))
+    rr.rr_attend(b.c, 1, x, out[0], ints([0]), ws)
+    assert same(b.c, before) and bool((out[0] == 9.0).all())
+    with pytest.raises(rr.RRError, match="not done.*twice"):
+        rr.rr_cache_check(b.c)
