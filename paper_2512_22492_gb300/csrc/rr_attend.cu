@@ -452,7 +452,8 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, const Tile& t, int
     };
     // (Maximum, sum) of a piece.
     const auto sums_of = [&](int i) { return i < n ? __ldcg(reinterpret_cast<const float2*>(at(i) + kMl + 2 * r)) : make_float2(-kInf, 0); };
-    const auto share_of = [](float2 y, float top) { return y.x == -kInf ? 0.0f : y.y * exp2f(y.x - top); };
+    // (Maxima may be infinite, -infinity in a piece without a score but NaN; its sum is NaN then.)
+    const auto share_of = [](float2 y, float top) { return y.x == top ? y.y : y.y * exp2f(y.x - top); };
     load(0);
     float2 mine = sums_of(lane);
     float top = mine.x;
