@@ -793,7 +793,8 @@ rr_status rr_cache_check(const rr_cache* cache, void* book, cudaStream_t stream)
  * h / (n_q / n_kv).  Row j (of m) of a sequence of L tokens sees its tokens t < L - m + 1 + j:
  *   s_t = scale q . k_t,   lse = ln sum_t exp(s_t),   out = sum_t exp(s_t - lse) v_t.
  * A row that sees no token has out 0 and lse -infinity, as has one whose scores are all
- * -infinity.  Tokens that a row does not see do not touch it, whatever they hold.
+ * -infinity.  Scores of infinity make lse infinity and out NaN, NaN ones both NaN.  Tokens
+ * that a row does not see do not touch it, whatever they hold.
  * Scores and sums are float32; the weights exp(s_t - max) enter the product with the
  * values as two parts, bfloat16 (to 2^-16 of themselves) or float16 (2^-22, or 2^-32 of
  * the largest); the result is rounded once.  Which keys are summed together depends on the

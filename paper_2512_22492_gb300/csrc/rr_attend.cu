@@ -492,9 +492,10 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, const Tile& t, int
 }
 
 // Keys [k0, k1) of one row once more, by one warp, one key after another, for values
-// that are not finite or nearly too large: a product of weight and value only where the
-// row sees the key, weights in float32 and 2^-32 of what they are, so that sums stay
-// finite.
+// that are not finite or nearly too large, and scores of infinity: a product of weight and value
+// only where the row sees the key, weights in float32 and 2^-32 of what they are, so that sums stay
+// finite.  A score of infinity has the weight NaN (infinity less infinity) in the result; in the
+// sum it counts 1, so that lse is infinity unless a score is NaN.
 template <class K>
 __device__ __noinline__ void carefully(const AttendArgs& a, const Tile& t, int r, int k0, int k1, float* piece) {
     using T = typename K::T;
@@ -526,7 +527,7 @@ __device__ __noinline__ void carefully(const AttendArgs& a, const Tile& t, int r
                 continue;
             }
             const float p = exp2f(s - (top == -kInf ? 0.0f : top));
-            sum += p;
+            sum += s == kInf ? 1.0f : p;
             float part[kEach] = {};
             for (int x = 0; x < min(end - key0, 32); ++x) {
                 const float w = __shfl_sync(~0u, p, x) * 0x1p-32f;
@@ -1120,16 +1121,18 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             soft_sync<K::kSoft>();
             const bool starts = it.first == 0, ends = it.first + it.n == it.t.units;
             float* const piece = starts && ends ? nullptr : a.pieces + (2 * int64_t(blockIdx.x) + starts) * a.piece_floats;
+            bool far = false;              // whether a score is infinity
             if (int(threadIdx.x) < left) {
                 const int r = threadIdx.x;
                 const float total = sh.parts[0][r] + sh.parts[1][r] + sh.parts[2][r] + sh.parts[3][r], bias = sh.bias[r];
+                far = bias == -kInf;
                 sh.inverse[r] = total == 0.0f ? 0.0f : 1.0f / total;
                 Place<K>(a, it.t, r, piece).sums(bias == kNothing ? -kInf : -bias, total);
             }
             soft_sync<K::kSoft>();
             // (Each sum times 1 / the row's.)
             add_sums(sh.inverse, true);
-            if (soft_any<K::kSoft>(odd && d < a.c.dim)) {
+            if (soft_any<K::kSoft>(far || (odd && d < a.c.dim))) {
                 for (int r = w; r < left; r += K::kSoft / 32) carefully<K>(a, it.t, r, it.first * kUnit, (it.first + it.n) * kUnit, piece);
             } else if (K::kKeep) {
 #pragma unroll
