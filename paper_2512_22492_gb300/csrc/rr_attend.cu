@@ -24,6 +24,7 @@
 // 7500, 64 over 8, five tokens each (1.59 GB): 278 to 280 us, 5.7 TB/s; one of 40001, 32 over 8
 // (164 MB): 36 us, 4.6 TB/s.
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <type_traits>
 
@@ -44,8 +45,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_huge_valf();
 // A row's reference for its exponentials may stay this much (of log2) under its maximum.
 constexpr float kSlack = 8.0f;
-// In place of minus the reference of a row that has seen nothing yet.
-constexpr float kNothing = 3e38f;
+// In place of minus the reference of a row that has seen nothing yet: any score but the least float
+// is above it by more than the slack.
+constexpr float kNothing = FLT_MAX;
 constexpr long long kWaitCycles = 4000000000;
 
 struct AttendArgs {
@@ -452,7 +454,7 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, const Tile& t, int
     };
     // (Maximum, sum) of a piece.
     const auto sums_of = [&](int i) { return i < n ? __ldcg(reinterpret_cast<const float2*>(at(i) + kMl + 2 * r)) : make_float2(-kInf, 0); };
-    // (Maxima may be infinite, -infinity in a piece without a score but NaN; its sum is NaN then.)
+    // (Maxima may be infinite; one without a score but NaN has the sum NaN, one without any 0.)
     const auto share_of = [](float2 y, float top) { return y.x == top ? y.y : y.y * exp2f(y.x - top); };
     load(0);
     float2 mine = sums_of(lane);
@@ -992,14 +994,21 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                         for (int e = 0; e < 8; ++e) sees[j] |= uint32_t(key0 + key < sh.seen[slot][8 * group_of(j) + e]) << e;
                     }
                 }
-                // Weights are 2^x, x = scale s - reference.
+                // Weights are 2^x, x = scale s - reference, with scale s rounded first: what a fused
+                // product keeps of it, half a bit of a score of 2^32, would be a weight of 2^128.
+#pragma unroll
+                for (int j = 0; j < GS; ++j) {
+                    if (group_of(j) >= groups) continue;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[j][e] = mul2(s[j][e], scale2);
+                }
                 const auto refer = [&](int j, F2* x, const float* from) {
                     const float4* const bias = reinterpret_cast<const float4*>(from);
                     const float4 b0 = bias[0], b1 = bias[1];
-                    x[0] = fma2(s[j][0], scale2, both(b0.x, b0.y));
-                    x[1] = fma2(s[j][1], scale2, both(b0.z, b0.w));
-                    x[2] = fma2(s[j][2], scale2, both(b1.x, b1.y));
-                    x[3] = fma2(s[j][3], scale2, both(b1.z, b1.w));
+                    x[0] = add2(s[j][0], both(b0.x, b0.y));
+                    x[1] = add2(s[j][1], both(b0.z, b0.w));
+                    x[2] = add2(s[j][2], both(b1.x, b1.y));
+                    x[3] = add2(s[j][3], both(b1.z, b1.w));
                     if (edge) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
@@ -1127,7 +1136,7 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 const float total = sh.parts[0][r] + sh.parts[1][r] + sh.parts[2][r] + sh.parts[3][r], bias = sh.bias[r];
                 far = bias == -kInf;
                 sh.inverse[r] = total == 0.0f ? 0.0f : 1.0f / total;
-                Place<K>(a, it.t, r, piece).sums(bias == kNothing ? -kInf : -bias, total);
+                Place<K>(a, it.t, r, piece).sums(-bias, total);
             }
             soft_sync<K::kSoft>();
             // (Each sum times 1 / the row's.)

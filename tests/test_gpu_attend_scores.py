@@ -88,3 +88,37 @@ def test_products_past_the_largest_float():
     assert float(lse[0, 0]) == math.inf and bool(out[0, 0].isnan().all())
     assert abs(float(lse[0, 1]) - 800.0) < 1e-3
     assert torch.equal(out[0, 1], c.v[0][17, 0])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("n_q", [1, 40])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("x", [1e6, 3e9, 1e11, 1e20, 3.0e38, 3.1e38, 3.25e38, 3.35e38])
+@pytest.mark.parametrize("tokens", [1, 2, 300, 3000])
+def test_scores_as_large_as_floats(kind, n_q, sign, x, tokens):
+    """Finite scores up to nearly 2^128 (in log2) of either sign: equal ones weigh the same."""
+    c = Case([tokens], [1], n_q=n_q, n_kv=1, dim=1, kind=kind)
+    c.q.fill_(1.0)
+    c.k[0].fill_(sign * 1.5)
+    c.v[0].fill_(2.0)
+    c.v[0][::2] = 4.0
+    put(c)
+    scale = math.log(2.0) * x / 1.5
+    out, lse = c.run(scale=scale)
+    assert bool((out == (4.0 if tokens == 1 else 3.0)).all())
+    # (The factor to log2 and back, the product, the logarithm of the count: a few roundings.)
+    want = sign * x * math.log(2.0) + math.log(tokens)
+    assert bool(((lse.double() / want - 1).abs() < 2.0 ** -20).all())
+    # Twice the score (half of it, where that overflows): one key alone, or all others.
+    if tokens > 2:
+        c.k[0][tokens - 2] = sign * 0.75
+        put(c)
+        out, lse = c.run(scale=scale)
+        if sign < 0:
+            assert bool((out == c.v[0][tokens - 2]).all())
+            want = -0.5 * x * math.log(2.0)
+        else:
+            rest = torch.cat([c.v[0][:tokens - 2], c.v[0][tokens - 1:]]).double().mean()
+            assert bool(((out.double() - rest).abs() <= R.ROUND[kind] * rest + 2.0 ** -13).all())
+            want = x * math.log(2.0) + math.log(tokens - 1)
+        assert bool(((lse.double() / want - 1).abs() < 2.0 ** -20).all())
