@@ -295,6 +295,13 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, int parity, volatile int*
     return true;
 }
 
+// Of a call that gave up: waits until `landed` is true, for a tenth of a second or so after t0 at most.
+template <class Landed>
+__device__ __forceinline__ void drain(long long t0, Landed landed) {
+#pragma unroll 1
+    while (!landed() && clock64() - t0 < kWaitCycles / 20) {}
+}
+
 // The softmax warps' own barrier, with the OR of what they bring.
 template <int THREADS>
 __device__ __forceinline__ bool soft_any(bool x) {
@@ -658,6 +665,14 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
     const auto leave = [&] {
         tmem_before();
         __syncthreads();
+        // (Of a call that gave up: the products under way end before their memory is given back.)
+        if (w == K::kProducts && sh.quit) {
+            if (elected()) {
+                products_arrive(smem_of(&sh.drained));
+                drain(clock64(), [&] { return bar_try(smem_of(&sh.drained), 0); });
+            }
+            __syncwarp();
+        }
         if (w == K::kProducts) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(K::kColumns) : "memory");
     };
     after_previous();
@@ -761,10 +776,12 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
             }
         }
         if (!ok) {
-            // What is on its way has to land before the block ends.
+            // What is on its way has to land before the block ends.  (A stage that has been used since may
+            // have been filled once more, by the other warp: its first copy is seen by its use then.)
+            const long long t0 = clock64();
             for (int back = max(i - a.stages, 0); back < i; ++back) {
-                const int k = values ? values_at(back) : keys_at(back);
-                for (int x = 0; x < 1 << 20 && !bar_try(smem_of(&sh.full[k % a.stages]), k / a.stages & 1); ++x) {}
+                const int k = values ? values_at(back) : keys_at(back), at = k % a.stages, turn = k / a.stages & 1;
+                drain(t0, [&] { return bar_try(smem_of(&sh.full[at]), turn) || bar_try(smem_of(&sh.empty[at]), turn); });
             }
         }
     } else if (w == K::kProducts) {
@@ -849,14 +866,6 @@ __global__ void __launch_bounds__(K::kThreads, 1) rr_attend_kernel(const __grid_
                 ++done;
             }
         }
-        if (sh.quit) {
-            // The products under way have to end before their memory is given back.
-            if (elected()) {
-                products_arrive(smem_of(&sh.drained));
-                for (int x = 0; x < 1 << 20 && !bar_try(smem_of(&sh.drained), 0); ++x) {}
-            }
-        }
-        __syncwarp();
     } else if (w == K::kQueries) {
         // Queries, and what the others need to know of a tile.
         Walk<K> walk(a, info, sh.seq, sh.start, begin, end);

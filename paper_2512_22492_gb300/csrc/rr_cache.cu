@@ -580,10 +580,12 @@ __global__ void __launch_bounds__(256) rr_cache_move_kernel(const __grid_constan
                 }
             }
         }
-        // (Of a call that gave up: what is on its way has to land before the block ends.)
+        // (Of a call that gave up: what is on its way has to land before the block ends; a tenth of a second
+        // or so is waited for it at most.)
+        const long long t0 = clock64();
         for (int i = landed; !ok && i < asked; ++i) {
             uint32_t done = 0;
-            for (int x = 0; x < 1 << 20 && !done; ++x)
+            while (!done && clock64() - t0 < 200000000ll)
                 asm volatile(
                     "{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
                     : "=r"(done)
