@@ -1146,7 +1146,12 @@ extern "C" rr_status rr_accept(const float* p, int64_t ldp, const float* q, int6
     RR_TRY(check_device(dev, tokens, 4, "tokens"));
     if (rejected) RR_TRY(check_device(dev, rejected, 4, "rejected"));
     const AcceptArgs a = {p, q, ldp, ldq, drafts, starts, u, v, accepted, tokens, rejected, rows, vocab};
-    const int threads = n > 16 ? 256 : kAcceptThreads;
+    // One block of 1024 threads fits an SM, and 15 clusters of 8 the GPU: up to there they read a row
+    // soonest, beyond it blocks of 256, four an SM, need not wait for one another.  (us on the GPU, 256 /
+    // 1024 threads, 151936 entries without drafts: n 1 8.5 / 7.2, 12 11.5 / 8.5, 16 12.4 / 12.7, 24 12.7 /
+    // 14.2, 64 14.6 / 31.3; with refused drafts 1 10.4 / 9.0, 12 14.2 / 10.5, 16 14.9 / 16.8, 64 17.9 / 38.7.
+    // 512 entries: 4.3 / 6.0 at 1, less than the host's time of a call either way, 4.9 / 10.6 at 16.)
+    const int threads = n > 15 ? 256 : kAcceptThreads;
     RR_CUDA(launch_clusters(rr_accept_kernel, kAcceptRanks, unsigned(n) * kAcceptRanks, threads, 0, stream, a));
     return RR_OK;
 }
