@@ -177,7 +177,7 @@ def rr_cache_extend(cache: Cache, seqs, starts=None, stream=None) -> None:
 def rr_cache_append(cache: Cache, layer: int, k, v, seqs, starts=None, stream=None) -> None:
     """One layer's keys and values [rows, n_kv, dim] of the sequences' newest tokens: rows
     starts[i] .. starts[i + 1] - 1 are the last ones of seqs[i] (without starts, row i is the
-    last one of seqs[i])."""
+    last one of seqs[i]).  A sequence whose rows are not all there is left out and marks the cache."""
     rows, ldk = _vectors(k, cache.n_kv, cache, "k")
     m, ldv = _vectors(v, cache.n_kv, cache, "v")
     if m != rows:

@@ -20,8 +20,8 @@
 // one runs.
 //
 // Measured: 64 sequences of 200 to 16000 tokens, 32 heads over 4 key heads of 128 (1.06 GB):
-// 172 to 175 us, 6.1 TB/s (the SMs' mean is done after 155, the last after 166); 96 of 500 to
-// 7500, 64 over 8, five tokens each (1.59 GB): 278 to 280 us, 5.7 TB/s; one of 40001, 32 over 8
+// 172 to 176 us, 6.1 TB/s (the SMs' mean is done after 155, the last after 166); 96 of 500 to
+// 7500, 64 over 8, five tokens each (1.59 GB): 288 us, 5.5 TB/s; one of 40001, 32 over 8
 // (164 MB): 36 us, 4.6 TB/s.
 #include <algorithm>
 #include <cfloat>
@@ -90,7 +90,7 @@ struct Kind {
     // own rounding, and more than that where values cancel.)  Float16's weights are 2^7 to 2^15 at
     // a row's maximum, so that those 2^-21 of the largest still have all bits of their first
     // part; the second ends at 2^-32 of it.  (Float16's second part: nothing up to 16 rows, and of 64
-    // rows a stage of the ring: 96 sequences of five tokens of 8 heads each 280 us, 260 with one.)
+    // rows a stage of the ring: 96 sequences of five tokens of 8 heads each 288 us, 263 with one.)
     static constexpr int kParts = 2;
     static constexpr float kLift = std::is_same<T, BF16>::value ? 0.0f : 7.0f;
     static constexpr int kQ = MT * NG * 2048;           // bytes of a tile's queries

@@ -515,7 +515,7 @@ __global__ void __launch_bounds__(kBookThreads) rr_cache_compact_kernel(const __
 // The moved pages' contents and their places in the table.  One thread of a block (one an SM)
 // has 32 KiB at a time copied through shared memory by bulk copies, four of them on their
 // way in while two are on theirs out; its other warps see to the table.  (Loads and
-// stores by all threads, 64 bytes of each in flight: 304 MB in 58 us, 5.2 TB/s; so 52 us.)
+// stores by all threads, 64 bytes of each in flight: 304 MB in 58 us, 5.2 TB/s; so 44 to 45, 6.8.)
 constexpr int kMoveChunk = 32768, kMoveStages = 6, kMoveAhead = 4;
 __global__ void __launch_bounds__(256) rr_cache_move_kernel(const __grid_constant__ CacheShape c, const Book b, char* pages) {
     extern __shared__ __align__(128) char stages[];
@@ -770,7 +770,7 @@ struct Draw {
 // warp whose run holds the drawn number looks through it again.  Sums of whole
 // numbers: their order changes nothing.  Reads one row of p, and of q where a draft was
 // refused; a chain of starts, drafts, their probabilities, sums and search comes on top (64 sequences
-// of 151936 entries: 56 MB, 16.5 us on the GPU, of which HBM takes 8.6; one: 7.5).
+// of 151936 entries: 56 MB, 16.5 us on the GPU, of which HBM takes 8.6; one: 7.8).
 __global__ void __launch_bounds__(kAcceptThreads, 1) rr_accept_kernel(const __grid_constant__ AcceptArgs a) {
     __shared__ uint64_t sums[2][kAcceptRanks * kAcceptThreads / 32];
     __shared__ int first_refused;
