@@ -23,7 +23,7 @@ def test_values_that_cancel(monkeypatch, kind, n_q, dim):
     monkeypatch.setitem(R.CUT, kind, CUT[kind])
     c = Case([2], [1], n_q=n_q, n_kv=1, dim=dim, kind=kind)
     t = R.TYPES[kind]
-    # One product a score, exact in 32 bits: 1/4 of a float with few bits, scale 1.
+    # A score is one product, exact in 32 bits.
     s = torch.linspace(0.01, 0.5, n_q).to(t)
     c.q = torch.zeros(1, n_q, dim, dtype=t)
     c.q[0, :, 0] = s
